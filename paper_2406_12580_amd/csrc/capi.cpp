@@ -5,9 +5,9 @@
 
 #include <hip/hip_runtime.h>
 
-#include <initializer_list>
 #include <utility>
 
+#include "capi_util.hpp"
 #include "gemm.hpp"
 #include "launch.hpp"
 #include "model.hpp"
@@ -16,38 +16,11 @@ using namespace recblr;
 
 namespace {
 
-constexpr size_t kWsAlign = 256;
 constexpr int64_t kMaxDim = (int64_t)1 << 31;       // each of B, L, D
 constexpr int64_t kMaxElems = (int64_t)1 << 40;     // B*L*D
 constexpr int64_t kMaxChannels = (int64_t)1 << 36;  // B*D (grid of B*D/64 workgroups)
 constexpr int64_t kMaxProjD = 1024;
 constexpr int64_t kMaxD = (int64_t)65535 * 64;        // channel groups of the dLambda reduction
-
-inline size_t align_up(size_t v) { return (v + kWsAlign - 1) / kWsAlign * kWsAlign; }
-
-struct Buf {
-    const void* p;
-    size_t bytes;
-};
-
-bool overlaps(Buf a, Buf b) {
-    if (!a.p || !b.p || a.bytes == 0 || b.bytes == 0) return false;
-    uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
-    return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
-}
-
-bool aligned(const void* p, size_t a) { return p == nullptr || ((uintptr_t)p % a) == 0; }
-
-// Outputs must not overlap inputs or each other.
-bool disjoint(std::initializer_list<Buf> outs, std::initializer_list<Buf> ins) {
-    for (auto o = outs.begin(); o != outs.end(); ++o) {
-        for (const Buf& i : ins)
-            if (overlaps(*o, i)) return false;
-        for (auto o2 = o + 1; o2 != outs.end(); ++o2)
-            if (overlaps(*o, *o2)) return false;
-    }
-    return true;
-}
 
 int check_dims(int64_t B, int64_t L, int64_t D, int io) {
     if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
@@ -57,18 +30,6 @@ int check_dims(int64_t B, int64_t L, int64_t D, int io) {
     if (B * D > 0 && L > kMaxElems / (B * D)) return RECBLR_ERR_UNSUPPORTED;
     return RECBLR_OK;
 }
-
-int check_ws(void* ws, size_t ws_bytes, size_t need) {
-    if (need == 0) return RECBLR_OK;
-    if (ws == nullptr || ws_bytes < need || !aligned(ws, kWsAlign)) return RECBLR_ERR_WORKSPACE;
-    return RECBLR_OK;
-}
-
-int status_of(hipError_t e) { return e == hipSuccess ? RECBLR_OK : RECBLR_ERR_HIP; }
-
-IoType io_of(int io) { return io == RECBLR_BF16 ? IoType::kBf16 : IoType::kF32; }
-
-size_t esz(int io) { return io == RECBLR_BF16 ? 2 : 4; }
 
 // ---- workspace layouts of the entry points with gate parameters
 struct FullFwdLayout {

@@ -452,3 +452,232 @@ def adam_update(params, grads, m1, m2, step, lr=1e-3, beta1=0.9, beta2=0.999, ep
     _check(recblr_adam_update(_ptr(params), _ptr(grads), _ptr(m1), _ptr(m2), params.numel(),
                               step, lr, beta1, beta2, eps, _stream(stream)), "recblr_adam_update")
 
+
+
+# ------------------------------------------------------------------ recblr_ops.h
+
+OP_DELTA_FORWARD, OP_DELTA_BACKWARD = 16, 17
+ADAMW_BLOCK = 256
+
+OPS_EXPORTS = (
+    "recblr_delta_step", "recblr_adamw_update", "recblr_adamw_moments",
+    "recblr_sample_workspace_size", "recblr_sample",
+)
+
+
+class AdamWTensor(ctypes.Structure):
+    """recblr_adamw_tensor."""
+    _fields_ = [("param", _p), ("grad", _p), ("m1", _p), ("m2", _p), ("scale1", _p),
+                ("scale2", _p), ("n", _i64), ("weight_decay", ctypes.c_double)]
+
+
+_d = ctypes.c_double
+_OPS_SIGS = {
+    "recblr_delta_step": ([_p] * 8 + [_i64] * 5 + [_f, _int, _p], _int),
+    "recblr_adamw_update": ([ctypes.POINTER(AdamWTensor), _i64, _int, _int, _i64, _d, _d, _d, _d,
+                             _p], _int),
+    "recblr_adamw_moments": ([ctypes.POINTER(AdamWTensor), _i64, _p, _p, _p], _int),
+    "recblr_sample_workspace_size": ([_i64, _i64, _int], _sz),
+    "recblr_sample": ([_p] * 8 + [_i64, _i64, _int, _p, _sz, _p], _int),
+}
+for _name, (_args, _res) in _OPS_SIGS.items():
+    _fn = getattr(_lib, _name)
+    _fn.argtypes = _args
+    _fn.restype = _res
+    globals()[_name] = _fn
+
+
+def _on_device(fn):
+    """Run a wrapper on the device of its first tensor and on its `stream` argument.
+
+    The library launches on the current device; outputs and workspace come from
+    torch's allocator on the stream of the launch, as in _on_stream.
+    """
+    @functools.wraps(fn)
+    def wrapper(first, *args, stream=None, **kwargs):
+        dev = first.device
+        if stream is None and dev.index == torch._C._cuda_getDevice():
+            return fn(first, *args, **kwargs)
+        if dev.type != "cuda":
+            raise ValueError("tensors must live on the GPU")
+        if stream is not None and stream.device != dev:
+            raise ValueError("stream belongs to another device than the tensors")
+        with torch.cuda.device(dev), torch.cuda.stream(stream):
+            return fn(first, *args, **kwargs)
+    return wrapper
+
+
+def _arg(t, shape, dtype, device, name):
+    """The address of a tensor that has to be as described; None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
+    if t.device != device or device.type != "cuda":
+        raise ValueError(f"{name} must live on the GPU, with the other tensors")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _delta_heads(q, k, v):
+    """Checked sizes (H, HV, Dk, Dv) and scale of the gated delta rule's tensors."""
+    if q.dim() < 3 or v.dim() != q.dim() or q.shape[:-2] != v.shape[:-2]:
+        raise ValueError("q and v must have the same rows and steps, and a head axis")
+    H, Dk, HV, Dv = *q.shape[-2:], *v.shape[-2:]
+    if H < 1 or HV < 1 or HV % H:
+        raise ValueError("the number of value heads must be a multiple of the query heads")
+    return H, HV, Dk, Dv
+
+
+@_on_device
+def delta_step(q, k, v, g, beta, h_prev, out=None, scale=None):
+    """One token of the gated delta rule: q, k [B,H,Dk], v [B,HV,Dv], g, beta [B,HV],
+    h_prev [B,HV,Dk,Dv] float32.  Returns (o [B,HV,Dv], h_next float32); out, where the new
+    state goes, may be h_prev.  scale defaults to Dk ** -0.5."""
+    if q.dim() != 3:
+        raise ValueError("q must be [B, H, Dk]")
+    H, HV, Dk, Dv = _delta_heads(q, k, v)
+    B, io, dt, dev = q.shape[0], io_code(q.dtype), q.dtype, q.device
+    st = (B, HV, Dk, Dv)
+    o = torch.empty_like(v)
+    h_next = torch.empty(st, dtype=torch.float32, device=dev) if out is None else out
+    _check(recblr_delta_step(
+        _arg(q, (B, H, Dk), dt, dev, "q"), _arg(k, (B, H, Dk), dt, dev, "k"),
+        _arg(v, (B, HV, Dv), dt, dev, "v"), _arg(g, (B, HV), dt, dev, "g"),
+        _arg(beta, (B, HV), dt, dev, "beta"), _arg(h_prev, st, torch.float32, dev, "h_prev"),
+        o.data_ptr(), _arg(h_next, st, torch.float32, dev, "out"), B, H, HV, Dk, Dv,
+        Dk ** -0.5 if scale is None else scale, io, _stream()), "recblr_delta_step")
+    return o, h_next
+
+
+@_on_device
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
+    """One item a row of logits [B,V], chosen by u [B] (float32, in [0, 1)).
+
+    temperature, top_p, min_p (float32) and top_k (int32) are [B] tensors or None (1, 1, 0
+    and no limit).  Returns (ids [B] int32, prob [B] float32): the item, -1 for a row that has
+    none, and its probability among the items that stayed."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [B, V]")
+    B, V = logits.shape
+    io, dev, f32 = io_code(logits.dtype), logits.device, torch.float32
+    ids = torch.empty(B, dtype=torch.int32, device=dev)
+    prob = torch.empty(B, dtype=f32, device=dev)
+    n = recblr_sample_workspace_size(B, V, io)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _check(recblr_sample(
+        _arg(logits, (B, V), logits.dtype, dev, "logits"), _arg(u, (B,), f32, dev, "u"),
+        _arg(temperature, (B,), f32, dev, "temperature"),
+        _arg(top_k, (B,), torch.int32, dev, "top_k"), _arg(top_p, (B,), f32, dev, "top_p"),
+        _arg(min_p, (B,), f32, dev, "min_p"), ids.data_ptr(), prob.data_ptr(), B, V, io,
+        ws.data_ptr() if n else None, n, _stream()), "recblr_sample")
+    return ids, prob
+
+
+class AdamW:
+    """AdamW over a list of tensors (float32 or bfloat16, all of one type and device).
+
+    weight_decay is one number or one for each tensor.  state_bits = 32 keeps float32 moments
+    m1, m2; 8 keeps codes (m1 int8, m2 uint8) with a float32 scale for each 256 elements (s1,
+    s2).  `state` takes over moments that exist: (m1, m2) or (m1, m2, s1, s2), lists of tensors
+    with as many elements as the parameters (the scales ceil(n / 256)); `step` counts the
+    updates already made.  step(grads) updates parameters and moments in place, on the
+    parameters' device; gradients have the parameters' type and number of elements."""
+
+    def __init__(self, params, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
+                 state_bits=32, state=None, step=0):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no parameters")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self.dtype, self.device = self.params[0].dtype, self.params[0].device
+        self._io = io_code(self.dtype)
+        self.lr, self.beta1, self.beta2, self.eps = lr, beta1, beta2, eps
+        self.state_bits, self.steps = state_bits, step
+        sizes = [p.numel() for p in self.params]
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) \
+            else [weight_decay] * len(sizes)
+        if len(decay) != len(sizes):
+            raise ValueError("weight_decay must be a number or one for each parameter")
+        codes = state_bits == 8
+        types = (torch.int8, torch.uint8) if codes else (torch.float32, torch.float32)
+        blocks = [-(-n // ADAMW_BLOCK) for n in sizes]
+        if state is None:
+            def zeros(counts, dtype):
+                return [torch.zeros(n, dtype=dtype, device=self.device) for n in counts]
+            state = [zeros(sizes, t) for t in types]
+            state += [zeros(blocks, torch.float32) for _ in range(2)] if codes else []
+        if len(state) != (4 if codes else 2):
+            raise ValueError("state must be (m1, m2), with (s1, s2) too for 8 bits")
+        state = [list(s) for s in state]
+        self.m1, self.m2 = state[:2]
+        self.s1, self.s2 = state[2:] if codes else (None, None)
+        self._table = (AdamWTensor * len(sizes))()
+
+        def fill(field, tensors, dtype, counts, name):
+            if len(tensors) != len(sizes):
+                raise ValueError(f"{name}: one tensor for each parameter is needed")
+            for entry, t, n in zip(self._table, tensors, counts):
+                setattr(entry, field, self._flat(t, dtype, n, name))
+
+        fill("param", self.params, self.dtype, sizes, "params")
+        fill("m1", self.m1, types[0], sizes, "m1")
+        fill("m2", self.m2, types[1], sizes, "m2")
+        if codes:
+            fill("scale1", self.s1, torch.float32, blocks, "s1")
+            fill("scale2", self.s2, torch.float32, blocks, "s2")
+        for entry, n, w in zip(self._table, sizes, decay):
+            entry.n, entry.weight_decay = n, w
+        self._sizes = sizes
+
+    def _flat(self, t, dtype, n, name):
+        if t.dtype != dtype or t.numel() != n:
+            raise ValueError(f"{name}: a tensor must be {dtype} with {n} elements")
+        if t.device != self.device or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name}: tensors must be contiguous, on the parameters' GPU")
+        return t.data_ptr()
+
+    def step(self, grads, lr=None, stream=None):
+        """One update with grads, a tensor for each parameter; lr overrides the rate."""
+        if len(grads) != len(self._sizes):
+            raise ValueError("grads: one tensor for each parameter is needed")
+        for entry, t, n in zip(self._table, grads, self._sizes):
+            entry.grad = self._flat(t, self.dtype, n, "grads")
+        _adamw_step(self, self.lr if lr is None else lr, stream=stream)
+        self.steps += 1
+
+    def moments(self, out=None, stream=None):
+        """The moments as float32: (m1, m2), lists of tensors; out takes them where given."""
+        if self.state_bits == 32:
+            if out is None:
+                return list(self.m1), list(self.m2)
+            for ours, theirs in zip((self.m1, self.m2), out):
+                for a, b in zip(ours, theirs):
+                    b.copy_(a.reshape(b.shape))
+            return out
+        return _adamw_moments(self, out, stream=stream)
+
+
+@_on_device
+def _adamw_step(opt, lr):
+    _check(recblr_adamw_update(opt._table, len(opt._sizes), opt.state_bits, opt._io,
+                               opt.steps + 1, lr, opt.beta1, opt.beta2, opt.eps, _stream()),
+           "recblr_adamw_update")
+
+
+@_on_device
+def _adamw_moments(opt, out):
+    if out is None:
+        out = tuple([torch.empty(p.shape, dtype=torch.float32, device=opt.device)
+                     for p in opt.params] for _ in range(2))
+    ptrs = []
+    for tensors in out:
+        if len(tensors) != len(opt._sizes):
+            raise ValueError("out: one tensor for each parameter is needed")
+        ptrs.append((_p * len(tensors))(*(opt._flat(t, torch.float32, n, "out")
+                                          for t, n in zip(tensors, opt._sizes))))
+    _check(recblr_adamw_moments(opt._table, len(opt._sizes), *ptrs, _stream()),
+           "recblr_adamw_moments")
+    return out
