@@ -38,6 +38,38 @@ extern "C" {
  */
 enum { RECBLR_OP_DELTA_FORWARD = 16, RECBLR_OP_DELTA_BACKWARD = 17 };
 
+/* Steps between two kept states (below), and the bytes of workspace that `op` needs
+ * (0: none, ws may be NULL; 0 for invalid arguments too). */
+enum { RECBLR_DELTA_CHUNK = 64 };
+size_t recblr_delta_workspace_size(int op, int64_t B, int64_t L, int64_t H, int64_t HV,
+                                   int64_t Dk, int64_t Dv, int io);
+
+/*
+ * Forward from h0 (NULL: zero) to o and the final state hT (may be NULL).
+ *   states : [B][HV][ceil(L / 64)][Dk][Dv] float or NULL, the states before the
+ *            steps 0, 64, 128, ..., which the backward reads
+ * L == 0 writes hT := h0 only.
+ */
+int recblr_delta_forward(const void* q, const void* k, const void* v, const void* g,
+                         const void* beta, const float* h0, void* o, float* hT, float* states,
+                         int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk, int64_t Dv,
+                         float scale, int io, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward of recblr_delta_forward: the exact adjoint of the recurrence.
+ *   states : the forward's (the initial state is the first of them)
+ *   d_o : [B][L][HV][Dv] io;  dhT : [B][HV][Dk][Dv] float or NULL
+ * Outputs: dq, dk [B][L][H][Dk], dv [B][L][HV][Dv], dg, dbeta [B][L][HV] io, dq and dk
+ * summed over the value heads that share a query head; dh0 [B][HV][Dk][Dv] float
+ * or NULL.  L == 0 writes dh0 := dhT (0 for NULL) only.
+ */
+int recblr_delta_backward(const void* q, const void* k, const void* v, const void* g,
+                          const void* beta, const float* states, const void* d_o,
+                          const float* dhT, void* dq, void* dk, void* dv, void* dg, void* dbeta,
+                          float* dh0, int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk,
+                          int64_t Dv, float scale, int io, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* One token: q, k [B][H][Dk], v, o [B][HV][Dv], g, beta [B][HV];
  * h_prev, h_next [B][HV][Dk][Dv] float (h_next may == h_prev).  No workspace. */
 int recblr_delta_step(const void* q, const void* k, const void* v, const void* g,

@@ -156,6 +156,16 @@ int recblr_sample(const void* logits, const float* u, const float* temperature,
 
 // ------------------------------------------------------------------ gated delta rule
 
+struct DeltaBytes {
+    size_t q, v, g, state, states;
+};
+static DeltaBytes delta_bytes(int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk, int64_t Dv,
+                              int io) {
+    const size_t e = esz(io), s = (size_t)(B * HV * Dk * Dv) * 4;
+    return DeltaBytes{(size_t)(B * L * H * Dk) * e, (size_t)(B * L * HV * Dv) * e,
+                      (size_t)(B * L * HV) * e, s, s * (size_t)((L + 63) / 64)};
+}
+
 static int delta_sizes(int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk, int64_t Dv,
                        int io) {
     if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
@@ -163,11 +173,85 @@ static int delta_sizes(int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk, 
         return RECBLR_ERR_INVALID_ARGUMENT;
     if (Dk > 128 || Dv > 128) return RECBLR_ERR_UNSUPPORTED;
     const int64_t top = (int64_t)1 << 24;
-    if (B >= top || HV > 65536 || L >= ((int64_t)1 << 31)) return RECBLR_ERR_UNSUPPORTED;
+    if (B >= top || HV > 4096 || L >= ((int64_t)1 << 31)) return RECBLR_ERR_UNSUPPORTED;
     // A strip of at least 32 columns, and a chunk of 64 steps, is a workgroup of its own.
     if (B * HV > ((int64_t)1 << 28)) return RECBLR_ERR_UNSUPPORTED;
     if (B > 0 && (L + 63) / 64 * 4 > 0x7FFFFFFF / (B * HV)) return RECBLR_ERR_UNSUPPORTED;
     return RECBLR_OK;
+}
+
+size_t recblr_delta_workspace_size(int op, int64_t B, int64_t L, int64_t H, int64_t HV,
+                                   int64_t Dk, int64_t Dv, int io) {
+    if (delta_sizes(B, L, H, HV, Dk, Dv, io) != RECBLR_OK || B == 0 || L == 0) return 0;
+    if (op == RECBLR_OP_DELTA_FORWARD)
+        return delta_forward_workspace(B, L, HV, (int)Dk, (int)Dv, io_of(io));
+    if (op == RECBLR_OP_DELTA_BACKWARD)
+        return delta_backward_workspace(B, L, HV, (int)Dk, (int)Dv, io_of(io));
+    return 0;
+}
+
+int recblr_delta_forward(const void* q, const void* k, const void* v, const void* g,
+                         const void* beta, const float* h0, void* o, float* hT, float* states,
+                         int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk, int64_t Dv,
+                         float scale, int io, void* ws, size_t ws_bytes, void* stream) {
+    int st = delta_sizes(B, L, H, HV, Dk, Dv, io);
+    if (st) return st;
+    if (B == 0) return RECBLR_OK;
+    if (L > 0 && (!q || !k || !v || !g || !beta || !o)) return RECBLR_ERR_INVALID_ARGUMENT;
+    const DeltaBytes n = delta_bytes(B, L, H, HV, Dk, Dv, io);
+    for (const void* p : {q, k, v, g, beta, (const void*)o})
+        if (!aligned(p, esz(io))) return RECBLR_ERR_INVALID_ARGUMENT;
+    for (const float* p : {h0, (const float*)hT, (const float*)states})
+        if (!aligned(p, 4)) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!disjoint({{o, n.v}, {hT, n.state}, {states, n.states}},
+                  {{q, n.q}, {k, n.q}, {v, n.v}, {g, n.g}, {beta, n.g}, {h0, n.state}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t need = recblr_delta_workspace_size(RECBLR_OP_DELTA_FORWARD, B, L, H, HV, Dk, Dv,
+                                                    io);
+    st = check_ws(ws, ws_bytes, need);
+    if (st) return st;
+    if (!disjoint({{ws, need}}, {{q, n.q}, {k, n.q}, {v, n.v}, {g, n.g}, {beta, n.g},
+                                 {h0, n.state}, {o, n.v}, {hT, n.state}, {states, n.states}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const DeltaFwdArgs a{q, k, v, g, beta, h0, o, hT, states, B, L, (int)H, (int)HV, (int)Dk,
+                         (int)Dv, scale, io_of(io)};
+    return status_of(launch_delta_forward(a, ws, (hipStream_t)stream));
+}
+
+int recblr_delta_backward(const void* q, const void* k, const void* v, const void* g,
+                          const void* beta, const float* states, const void* d_o,
+                          const float* dhT, void* dq, void* dk, void* dv, void* dg, void* dbeta,
+                          float* dh0, int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk,
+                          int64_t Dv, float scale, int io, void* ws, size_t ws_bytes,
+                          void* stream) {
+    int st = delta_sizes(B, L, H, HV, Dk, Dv, io);
+    if (st) return st;
+    if (B == 0) return RECBLR_OK;
+    if (L > 0 && (!q || !k || !v || !g || !beta || !states || !d_o || !dq || !dk || !dv || !dg ||
+                  !dbeta))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const DeltaBytes n = delta_bytes(B, L, H, HV, Dk, Dv, io);
+    for (const void* p : {q, k, v, g, beta, d_o, (const void*)dq, (const void*)dk,
+                          (const void*)dv, (const void*)dg, (const void*)dbeta})
+        if (!aligned(p, esz(io))) return RECBLR_ERR_INVALID_ARGUMENT;
+    for (const float* p : {states, dhT, (const float*)dh0})
+        if (!aligned(p, 4)) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!disjoint({{dq, n.q}, {dk, n.q}, {dv, n.v}, {dg, n.g}, {dbeta, n.g}, {dh0, n.state}},
+                  {{q, n.q}, {k, n.q}, {v, n.v}, {g, n.g}, {beta, n.g}, {states, n.states},
+                   {d_o, n.v}, {dhT, n.state}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t need = recblr_delta_workspace_size(RECBLR_OP_DELTA_BACKWARD, B, L, H, HV, Dk, Dv,
+                                                    io);
+    st = check_ws(ws, ws_bytes, need);
+    if (st) return st;
+    if (!disjoint({{ws, need}},
+                  {{q, n.q}, {k, n.q}, {v, n.v}, {g, n.g}, {beta, n.g}, {states, n.states},
+                   {d_o, n.v}, {dhT, n.state}, {dq, n.q}, {dk, n.q}, {dv, n.v}, {dg, n.g},
+                   {dbeta, n.g}, {dh0, n.state}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const DeltaBwdArgs a{q, k, v, g, beta, states, d_o, dhT, dq, dk, dv, dg, dbeta, dh0, B, L,
+                         (int)H, (int)HV, (int)Dk, (int)Dv, scale, io_of(io)};
+    return status_of(launch_delta_backward(a, ws, (hipStream_t)stream));
 }
 
 int recblr_delta_step(const void* q, const void* k, const void* v, const void* g,

@@ -1,0 +1,385 @@
+// Pieces shared by the chunked kernels of the gated delta rule (delta_fwd.hip,
+// delta_bwd.hip): matrix-core operands from LDS, decays of a chunk, and the inverse of a
+// chunk's unit triangular matrix.
+//
+// A workgroup of four waves works on 64 steps at a time; wave w owns the strip of rows
+// 16 w .. 16 w + 15.  All products are of 16 x 16 tiles, whose accumulator gives lane l
+// column l % 16 and rows 4 (l / 16) .. + 3, and whose operands give lane l row (or column)
+// l % 16.  With g = l / 16, the lane's k are
+//   bf16 I/O: v_mfma_f32_16x16x32_bf16, k = 8 g .. 8 g + 7 of 32 (16 bytes),
+//   fp32 I/O: four v_mfma_f32_16x16x4_f32, k = 4 g .. 4 g + 3 of 16 (16 bytes; the j-th
+//     instruction contracts the j-th value of every lane).
+// fp32 I/O is thus multiplied in fp32.  With bf16 I/O the inputs are exact operands, and what
+// is computed from them (states, updates, the inverse) is a pair of bf16 planes, hi + lo with
+// hi = bf16(x), lo = bf16(x - hi): 16 bits of mantissa, products of two such as
+// hi hi + hi lo + lo hi, relative error about 3 * 2^-17 each.  Against 64 bits the chunked
+// recurrence then shows some 5e-6 on the float states over 2048 steps; a single plane gives
+// 1e-3.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "device_common.hpp"
+#include "ops.hpp"
+#include "wave_tile.hpp"
+
+namespace recblr {
+namespace dtile {
+
+using wtile::b8;
+using wtile::f4;
+using wtile::lds_barrier;
+
+constexpr int C = 64;     // steps of a chunk
+constexpr int NT = 256;   // threads
+constexpr int TS = 68;    // floats in a row of the triangular matrix in LDS
+typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+
+// ------------------------------------------------------------------ operands
+struct F32Op {  // fp32: given and computed operands alike
+    f4 v;
+};
+struct Bf16Op {  // a given operand, exact
+    b8 h;
+};
+struct Bf16Op2 {  // a computed one, two planes
+    b8 h, l;
+};
+
+template <typename T>
+struct Io;
+template <>
+struct Io<float> {
+    using Elem = float;
+    using Given = F32Op;
+    using Made = F32Op;
+    static constexpr int kPlanes = 1, kStep = 16, kPad = 4, kUnit = 4;  // kUnit: elements in 16 bytes
+};
+template <>
+struct Io<bf16> {
+    using Elem = __bf16;
+    using Given = Bf16Op;
+    using Made = Bf16Op2;
+    static constexpr int kPlanes = 2, kStep = 32, kPad = 8, kUnit = 8;
+};
+
+__device__ __forceinline__ f4 mma16(b8 a, b8 b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f4 mma(f4 c, const F32Op& a, const F32Op& b) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+    return c;
+}
+__device__ __forceinline__ f4 mma(f4 c, const Bf16Op& a, const Bf16Op& b) {
+    return mma16(a.h, b.h, c);
+}
+__device__ __forceinline__ f4 mma(f4 c, const Bf16Op& a, const Bf16Op2& b) {
+    return mma16(a.h, b.h, mma16(a.h, b.l, c));
+}
+__device__ __forceinline__ f4 mma(f4 c, const Bf16Op2& a, const Bf16Op& b) {
+    return mma16(a.h, b.h, mma16(a.l, b.h, c));
+}
+__device__ __forceinline__ f4 mma(f4 c, const Bf16Op2& a, const Bf16Op2& b) {
+    return mma16(a.h, b.h, mma16(a.h, b.l, mma16(a.l, b.h, c)));
+}
+
+// Eight floats as two planes.
+__device__ __forceinline__ Bf16Op2 split(const float (&x)[8]) {
+    Bf16Op2 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        o.h[e] = (__bf16)x[e];
+        o.l[e] = (__bf16)(x[e] - (float)o.h[e]);
+    }
+    return o;
+}
+
+// A matrix in LDS whose rows run along the contraction: operand row `row`, k from k0.
+__device__ __forceinline__ F32Op given(const float* m, int stride, int row, int k0, int g) {
+    return {*(const f4*)(m + row * stride + k0 + 4 * g)};
+}
+__device__ __forceinline__ Bf16Op given(const __bf16* m, int stride, int row, int k0, int g) {
+    return {*(const b8*)(m + row * stride + k0 + 8 * g)};
+}
+// The same of a computed matrix; `plane`: elements from one plane to the next.
+__device__ __forceinline__ F32Op made(const float* m, int, int stride, int row, int k0, int g) {
+    return given(m, stride, row, k0, g);
+}
+__device__ __forceinline__ Bf16Op2 made(const __bf16* m, int plane, int stride, int row, int k0,
+                                        int g) {
+    const __bf16* p = m + row * stride + k0 + 8 * g;
+    return {*(const b8*)p, *(const b8*)(p + plane)};
+}
+// The k order that accumulators of two neighbouring tiles have: 4 g .. of the first, then of
+// the second.  An operand made of accumulators is multiplied by one that is read this way.
+__device__ __forceinline__ F32Op made_acc(const float* m, int, int stride, int row, int k0, int g) {
+    return given(m, stride, row, k0, g);
+}
+__device__ __forceinline__ Bf16Op2 made_acc(const __bf16* m, int plane, int stride, int row,
+                                            int k0, int g) {
+    const __bf16* p = m + row * stride + k0 + 4 * g;
+    const b4 h0 = *(const b4*)p, h1 = *(const b4*)(p + 16);
+    const b4 l0 = *(const b4*)(p + plane), l1 = *(const b4*)(p + plane + 16);
+    return {__builtin_shufflevector(h0, h1, 0, 1, 2, 3, 4, 5, 6, 7),
+            __builtin_shufflevector(l0, l1, 0, 1, 2, 3, 4, 5, 6, 7)};
+}
+// A matrix whose columns run along the contraction: operand row = column `col0 + l % 16`, k
+// from row k0 on, in natural order.
+__device__ __forceinline__ F32Op given_t(const float* m, int stride, int k0, int col0, int ll,
+                                         int g) {
+    const float* p = m + (k0 + 4 * g) * stride + col0 + ll;
+    return {{p[0], p[stride], p[2 * stride], p[3 * stride]}};
+}
+__device__ __forceinline__ Bf16Op given_t(const __bf16* m, int stride, int k0, int col0, int ll,
+                                          int g) {
+    const __bf16* p = m + (k0 + 8 * g + (ll >> 2)) * stride + col0 + 4 * (ll & 3);
+    return {wtile::tr_pair((const char*)p, (const char*)(p + 4 * stride))};
+}
+__device__ __forceinline__ F32Op made_t(const float* m, int, int stride, int k0, int col0, int ll,
+                                        int g) {
+    return given_t(m, stride, k0, col0, ll, g);
+}
+__device__ __forceinline__ Bf16Op2 made_t(const __bf16* m, int plane, int stride, int k0,
+                                          int col0, int ll, int g) {
+    return {given_t(m, stride, k0, col0, ll, g).h, given_t(m + plane, stride, k0, col0, ll, g).h};
+}
+
+// As given_t, in the k order of accumulators.
+__device__ __forceinline__ F32Op given_t_acc(const float* m, int stride, int k0, int col0, int ll,
+                                             int g) {
+    return given_t(m, stride, k0, col0, ll, g);
+}
+__device__ __forceinline__ Bf16Op given_t_acc(const __bf16* m, int stride, int k0, int col0,
+                                              int ll, int g) {
+    const __bf16* p = m + (k0 + 4 * g + (ll >> 2)) * stride + col0 + 4 * (ll & 3);
+    return {wtile::tr_pair((const char*)p, (const char*)(p + 16 * stride))};
+}
+
+// Four accumulator values (consecutive k of a row of the operand that they become).
+__device__ __forceinline__ void put(float* m, int, int stride, int row, int k0, const f4& v) {
+    *(f4*)(m + row * stride + k0) = v;
+}
+__device__ __forceinline__ void put(__bf16* m, int plane, int stride, int row, int k0,
+                                    const f4& v) {
+    b4 h, l;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        h[r] = (__bf16)v[r];
+        l[r] = (__bf16)(v[r] - (float)h[r]);
+    }
+    __bf16* p = m + row * stride + k0;
+    *(b4*)p = h;
+    *(b4*)(p + plane) = l;
+}
+
+// A given operand with its k-th column times s[k] (s in LDS, natural order from k0).
+__device__ __forceinline__ F32Op scaled(const F32Op& a, const float* s, int k0, int g) {
+    return {a.v * *(const f4*)(s + k0 + 4 * g)};
+}
+__device__ __forceinline__ Bf16Op2 scaled(const Bf16Op& a, const float* s, int k0, int g) {
+    const f4 s0 = *(const f4*)(s + k0 + 8 * g), s1 = *(const f4*)(s + k0 + 8 * g + 4);
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)a.h[e] * (e < 4 ? s0[e & 3] : s1[e & 3]);
+    return split(x);
+}
+
+// An operand from accumulators: tile t of fp32, tiles 2 t and 2 t + 1 of bf16.
+template <typename T>
+__device__ __forceinline__ typename Io<T>::Made from_acc(const f4* acc, int t) {
+    if constexpr (sizeof(T) == 4) {
+        return F32Op{acc[t]};
+    } else {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = acc[2 * t + (e >> 2)][e & 3];
+        return split(x);
+    }
+}
+
+// ------------------------------------------------------------------ global memory
+// A chunk's rows of one head, as a buffer: row r, element e at byte (r step + e) sizeof(T).
+// Accesses outside of the rows that exist read zeros and write nothing, so no branch guards
+// them; elements behind a row's end (the next head's) have to be sent out of range by `off`.
+constexpr uint32_t kNowhere = 0x7FFFFFF0u;  // an offset behind every buffer's end
+
+template <typename T>
+struct Rows {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t step;  // bytes from row to row
+    // rows [t0, t0 + 64) of the `len` rows from base on, `width` elements wide
+    __device__ __forceinline__ Rows(const T* base, int64_t t0, int64_t len, int64_t row_elems,
+                                    int width) {
+        const int64_t left = len - t0;
+        const int rows = left < C ? (int)left : C;
+        step = (uint32_t)(row_elems * sizeof(T));
+        r = wtile::rsrc(base + t0 * row_elems,
+                        (uint32_t)((rows - 1) * row_elems + width) * (uint32_t)sizeof(T));
+    }
+    __device__ __forceinline__ uint32_t off(int row, int e, int width) const {
+        return e < width ? (uint32_t)row * step + (uint32_t)e * (uint32_t)sizeof(T) : kNowhere;
+    }
+    __device__ __forceinline__ float get(uint32_t o) const {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)o, 0, 0));
+        else
+            return __uint_as_float(
+                (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, (int)o, 0, 0) << 16);
+    }
+    __device__ __forceinline__ void set(uint32_t o, float v) const {
+        if constexpr (sizeof(T) == 4)
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, (int)o, 0, 0);
+        else
+            __builtin_amdgcn_raw_buffer_store_b16((short)from_f32<bf16>(v).bits, r, (int)o, 0, 0);
+    }
+    // 16 bytes from element e of a row; VEC: rows start at multiples of 16 bytes.
+    template <bool VEC>
+    __device__ __forceinline__ wtile::u4v get16(int row, int e, int width) const {
+        if constexpr (VEC) {
+            return __builtin_bit_cast(wtile::u4v, __builtin_amdgcn_raw_buffer_load_b128(
+                                                      r, (int)off(row, e, width), 0, 0));
+        } else {
+            constexpr int U = 16 / sizeof(T);
+            wtile::u4v v = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const uint32_t o = off(row, e + i, width);
+                if constexpr (sizeof(T) == 4)
+                    v[i] = __builtin_amdgcn_raw_buffer_load_b32(r, (int)o, 0, 0);
+                else
+                    v[i >> 1] |= (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(
+                                     r, (int)o, 0, 0)
+                                 << (16 * (i & 1));
+            }
+            return v;
+        }
+    }
+};
+
+// ------------------------------------------------------------------ decays of a chunk
+struct Gates {
+    double cum[C];  // running sum of g log2(e)
+    float eg[C];    // 2^cum_i: decay from the chunk's start through step i
+    float el[C];    // 2^(cum_63 - cum_i): decay behind step i up to the chunk's end
+    float bt[C];    // beta
+    float es[C];    // scale eg
+};
+
+// By one wave, a step to a lane.  The sums are kept in 64 bits: what is used of them is
+// differences, exact to fp32 however strong the decays before them were.  Steps behind the
+// sequence have g = beta = 0.
+__device__ __forceinline__ void gates_of_chunk(Gates* gt, float g, float beta, float scale,
+                                               int lane) {
+    double s = (double)delta_clamp_g(g) * 1.4426950408889634074;
+#pragma unroll
+    for (int d = 1; d < C; d <<= 1) {
+        const double o = __shfl_up(s, d);
+        if (lane >= d) s += o;
+    }
+    const double end = __shfl(s, C - 1);
+    gt->cum[lane] = s;
+    gt->eg[lane] = fast_exp2((float)s);
+    gt->el[lane] = fast_exp2((float)(end - s));
+    gt->bt[lane] = beta;
+    gt->es[lane] = scale * gt->eg[lane];
+}
+
+// ------------------------------------------------------------------ (I + A)^-1
+// A is strictly lower triangular, 64 x 64 floats in `tm` (its tiles on and below the
+// diagonal).  Inverses of the diagonal 16 x 16 tiles by substitution, then of twice the size
+// at a time: the tile below is -D^-1 B A^-1.  All in fp32 (powers of A, as a Neumann series
+// has them, cancel badly where keys are alike).  The tiles (2..3, 0..1) of the result are
+// stored at (0..1, 2..3), where zeros belong, since the ones of A are still read by other
+// waves.  tile_at gives the place.
+
+// Wave w inverts its own diagonal tile.  Lane column ll; A's rows are read by all lanes alike.
+__device__ __forceinline__ void invert_diagonal(float* tm, int w, int ll, int g) {
+    float* b = tm + 16 * w * TS + 16 * w;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float s = i == ll ? 1.0f : 0.0f;
+#pragma unroll
+        for (int m = 0; m < i; m += 4) {
+            const f4 a = *(const f4*)(b + i * TS + m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (m + e < i) s = fmaf(-a[e], x[m + e], s);
+        }
+        x[i] = s;
+    }
+    wave_fence();
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if ((i >> 2) == g) b[i * TS + ll] = x[i];
+}
+
+// Tile product with B as it lies in memory ([k][column]).
+__device__ __forceinline__ f4 tile_mma(f4 c, const float* a, const float* b, int ll, int g) {
+    return mma(c, given(a, TS, ll, 0, g), given_t(b, TS, 0, 0, ll, g));
+}
+__device__ __forceinline__ void tile_put(float* t, const f4& v, int ll, int g) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) t[(4 * g + r) * TS + ll] = v[r];
+}
+__device__ __forceinline__ float* tile(float* tm, int i, int j) { return tm + 16 * i * TS + 16 * j; }
+
+// Waves 0 and 2: the tile (w + 1, w).
+__device__ __forceinline__ void invert_merge1(float* tm, int w, int ll, int g) {
+    if (w & 1) return;
+    const f4 zero = {0, 0, 0, 0};
+    const f4 y = tile_mma(zero, tile(tm, w + 1, w), tile(tm, w, w), ll, g);
+    f4 t = mma(zero, given(tile(tm, w + 1, w + 1), TS, ll, 0, g), F32Op{y});
+    t = -t;
+    wave_fence();
+    tile_put(tile(tm, w + 1, w), t, ll, g);
+}
+// Wave w: the tile (2 + w / 2, w % 2).
+__device__ __forceinline__ void invert_merge2(float* tm, int w, int ll, int g) {
+    const int rb = 2 + (w >> 1), cb = w & 1;
+    const f4 zero = {0, 0, 0, 0};
+    f4 t = zero;
+    for (int k = 2; k <= rb; ++k) {
+        f4 y = zero;
+        for (int m = cb; m < 2; ++m) y = tile_mma(y, tile(tm, k, m), tile(tm, m, cb), ll, g);
+        t = mma(t, given(tile(tm, rb, k), TS, ll, 0, g), F32Op{y});
+    }
+    t = -t;
+    tile_put(tile(tm, cb, rb), t, ll, g);
+}
+// Where tile (i, j) of the inverse lies.
+__device__ __forceinline__ const float* tile_at(const float* tm, int i, int j) {
+    return i >= 2 && j < 2 ? tm + 16 * j * TS + 16 * i : tm + 16 * i * TS + 16 * j;
+}
+
+// Operand of the inverse's rows 16 i .. (k: columns, step s), and of its transpose.
+template <typename T>
+__device__ __forceinline__ typename Io<T>::Made inverse_rows(const float* tm, int i, int s,
+                                                             int ll, int g) {
+    if constexpr (sizeof(T) == 4) {
+        return given(tile_at(tm, i, s), TS, ll, 0, g);
+    } else {
+        const float* p = tile_at(tm, i, 2 * s + (g >> 1)) + ll * TS + 8 * (g & 1);
+        const f4 a = *(const f4*)p, b = *(const f4*)(p + 4);
+        const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        return split(x);
+    }
+}
+template <typename T>
+__device__ __forceinline__ typename Io<T>::Made inverse_cols(const float* tm, int i, int s,
+                                                             int ll, int g) {
+    if constexpr (sizeof(T) == 4) {
+        return given_t(tile_at(tm, s, i), TS, 0, 0, ll, g);
+    } else {
+        const float* p = tile_at(tm, 2 * s + (g >> 1), i) + 8 * (g & 1) * TS + ll;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = p[e * TS];
+        return split(x);
+    }
+}
+
+}  // namespace dtile
+}  // namespace recblr

@@ -52,6 +52,46 @@ struct DeltaStepArgs {
     float scale;
     IoType io;
 };
+struct DeltaFwdArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    const void* g;
+    const void* beta;
+    const float* h0;  // may be null (zero state)
+    void* o;
+    float* hT;      // may be null
+    float* states;  // may be null; [B][HV][ceil(L / 64)][Dk][Dv]
+    int64_t B, L;
+    int H, HV, Dk, Dv;
+    float scale;
+    IoType io;
+};
+size_t delta_forward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv, IoType io);
+hipError_t launch_delta_forward(const DeltaFwdArgs& a, void* ws, hipStream_t stream);
+
+struct DeltaBwdArgs {
+    const void* q;
+    const void* k;
+    const void* v;
+    const void* g;
+    const void* beta;
+    const float* states;
+    const void* d_o;
+    const float* dhT;  // may be null
+    void* dq;
+    void* dk;
+    void* dv;
+    void* dg;
+    void* dbeta;
+    float* dh0;  // may be null
+    int64_t B, L;
+    int H, HV, Dk, Dv;
+    float scale;
+    IoType io;
+};
+size_t delta_backward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv, IoType io);
+hipError_t launch_delta_backward(const DeltaBwdArgs& a, void* ws, hipStream_t stream);
 hipError_t launch_delta_step(const DeltaStepArgs& a, hipStream_t stream);
 
 // Log decays below this count as this: e^-100 of any state is nothing next to it in fp32,

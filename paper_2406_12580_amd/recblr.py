@@ -457,9 +457,11 @@ def adam_update(params, grads, m1, m2, step, lr=1e-3, beta1=0.9, beta2=0.999, ep
 # ------------------------------------------------------------------ recblr_ops.h
 
 OP_DELTA_FORWARD, OP_DELTA_BACKWARD = 16, 17
+DELTA_CHUNK = 64
 ADAMW_BLOCK = 256
 
 OPS_EXPORTS = (
+    "recblr_delta_workspace_size", "recblr_delta_forward", "recblr_delta_backward",
     "recblr_delta_step", "recblr_adamw_update", "recblr_adamw_moments",
     "recblr_sample_workspace_size", "recblr_sample",
 )
@@ -473,6 +475,9 @@ class AdamWTensor(ctypes.Structure):
 
 _d = ctypes.c_double
 _OPS_SIGS = {
+    "recblr_delta_workspace_size": ([_int] + [_i64] * 6 + [_int], _sz),
+    "recblr_delta_forward": ([_p] * 9 + [_i64] * 6 + [_f, _int, _p, _sz, _p], _int),
+    "recblr_delta_backward": ([_p] * 14 + [_i64] * 6 + [_f, _int, _p, _sz, _p], _int),
     "recblr_delta_step": ([_p] * 8 + [_i64] * 5 + [_f, _int, _p], _int),
     "recblr_adamw_update": ([ctypes.POINTER(AdamWTensor), _i64, _int, _int, _i64, _d, _d, _d, _d,
                              _p], _int),
@@ -528,6 +533,71 @@ def _delta_heads(q, k, v):
     if H < 1 or HV < 1 or HV % H:
         raise ValueError("the number of value heads must be a multiple of the query heads")
     return H, HV, Dk, Dv
+
+
+_delta_workspace_size = functools.lru_cache(maxsize=256)(recblr_delta_workspace_size)
+
+
+def _delta_inputs(q, k, v, g, beta):
+    """Checked sizes and the addresses of a sequence's tensors."""
+    if q.dim() != 4:
+        raise ValueError("q must be [B, L, H, Dk]")
+    H, HV, Dk, Dv = _delta_heads(q, k, v)
+    B, L = q.shape[:2]
+    dt, dev = q.dtype, q.device
+    io = io_code(dt)
+    ptrs = (_arg(q, (B, L, H, Dk), dt, dev, "q"), _arg(k, (B, L, H, Dk), dt, dev, "k"),
+            _arg(v, (B, L, HV, Dv), dt, dev, "v"), _arg(g, (B, L, HV), dt, dev, "g"),
+            _arg(beta, (B, L, HV), dt, dev, "beta"))
+    return (B, L, H, HV, Dk, Dv), io, ptrs
+
+
+def _delta_workspace(op, sizes, io, device):
+    n = _delta_workspace_size(op, *sizes, io)
+    return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
+
+
+@_on_device
+def delta_forward(q, k, v, g, beta, h0=None, scale=None, keep_states=False):
+    """Gated delta rule over whole sequences: q, k [B,L,H,Dk], v [B,L,HV,Dv], log decays g and
+    strengths beta [B,L,HV], h0 [B,HV,Dk,Dv] float32.  Returns (o [B,L,HV,Dv], hT float32,
+    states), states (None unless keep_states) being what delta_backward needs of the forward:
+    [B,HV,ceil(L/64),Dk,Dv] float32.  scale defaults to Dk ** -0.5."""
+    sizes, io, ptrs = _delta_inputs(q, k, v, g, beta)
+    B, L, H, HV, Dk, Dv = sizes
+    dev, f32 = q.device, torch.float32
+    o = torch.empty_like(v)
+    hT = torch.empty((B, HV, Dk, Dv), dtype=f32, device=dev)
+    states = torch.empty((B, HV, -(-L // DELTA_CHUNK), Dk, Dv), dtype=f32, device=dev) \
+        if keep_states else None
+    ws, nws = _delta_workspace(OP_DELTA_FORWARD, sizes, io, dev)
+    _check(recblr_delta_forward(
+        *ptrs, _arg(h0, (B, HV, Dk, Dv), f32, dev, "h0"), o.data_ptr(), hT.data_ptr(),
+        states.data_ptr() if keep_states else None, *sizes,
+        Dk ** -0.5 if scale is None else scale, io, ws.data_ptr() if nws else None, nws,
+        _stream()), "recblr_delta_forward")
+    return o, hT, states
+
+
+@_on_device
+def delta_backward(q, k, v, g, beta, states, do, dhT=None, scale=None, need_dh0=True):
+    """Backward of delta_forward (states: what it kept).  Returns a dict with dq, dk, dv, dg,
+    dbeta of the inputs' types and dh0 float32 (None unless need_dh0)."""
+    sizes, io, ptrs = _delta_inputs(q, k, v, g, beta)
+    B, L, H, HV, Dk, Dv = sizes
+    dev, f32 = q.device, torch.float32
+    st = (B, HV, Dk, Dv)
+    out = {"dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v),
+           "dg": torch.empty_like(g), "dbeta": torch.empty_like(beta),
+           "dh0": torch.empty(st, dtype=f32, device=dev) if need_dh0 else None}
+    ws, nws = _delta_workspace(OP_DELTA_BACKWARD, sizes, io, dev)
+    _check(recblr_delta_backward(
+        *ptrs, _arg(states, (B, HV, -(-L // DELTA_CHUNK), Dk, Dv), f32, dev, "states"),
+        _arg(do, (B, L, HV, Dv), q.dtype, dev, "do"), _arg(dhT, st, f32, dev, "dhT"),
+        *(None if t is None else t.data_ptr() for t in out.values()), *sizes,
+        Dk ** -0.5 if scale is None else scale, io, ws.data_ptr() if nws else None, nws,
+        _stream()), "recblr_delta_backward")
+    return out
 
 
 @_on_device
