@@ -186,7 +186,7 @@ size_t recblr_delta_workspace_size(int op, int64_t B, int64_t L, int64_t H, int6
     if (op == RECBLR_OP_DELTA_FORWARD)
         return delta_forward_workspace(B, L, HV, (int)Dk, (int)Dv, io_of(io));
     if (op == RECBLR_OP_DELTA_BACKWARD)
-        return delta_backward_workspace(B, L, HV, (int)Dk, (int)Dv, io_of(io));
+        return delta_backward_workspace(B, L, H, HV, (int)Dk, (int)Dv, io_of(io));
     return 0;
 }
 

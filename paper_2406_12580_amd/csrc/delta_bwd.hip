@@ -25,21 +25,25 @@ namespace {
 using namespace dtile;
 
 struct BwdWs {
-    float* D;  // [B * HV][chunks][Dk][Dv]: gradient of the state behind each chunk
-    float* Y;  // [B * HV][L][Dv]
+    float* D;   // [B * HV][chunks][Dk][Dv]: gradient of the state behind each chunk
+    float* Y;   // [B * HV][L][Dv]
+    float* dq;  // [B][L][H][Dk] each: sums over value heads so far, where they share a query head
+    float* dk;
 };
 
 // ------------------------------------------------------------------ the recurrence
 template <typename T, int DK, int DVT>
 struct StateLds {
     using E = typename Io<T>::Elem;
+    static constexpr int kChain = Io<T>::kChain;
     static constexpr int kKS = DK + Io<T>::kPad, kUS = C + Io<T>::kPad, kOS = DVT + Io<T>::kPad;
-    static constexpr int kDPlane = DVT * kKS, kXPlane = DVT * kUS;
+    static constexpr int kDPlane = DVT * kKS, kXPlane = DVT * kUS, kOPlane = C * kOS;
     E k[C * kKS];
     E q[C * kKS];
-    E d_o[C * kOS];
-    E d[Io<T>::kPlanes * kDPlane];  // [column][d]
-    E x[Io<T>::kPlanes * kXPlane];  // [column][step]: dU, then -dV
+    E d_o[kOPlane];
+    E od[kChain * kOPlane];  // dO times scale e^c
+    // [column][d] the gradient D; then [column][step] dU; then -e^c dV
+    E x[kChain * (kDPlane > kXPlane ? kDPlane : kXPlane)];
     float tm[C * TS];
     Gates gt;
 };
@@ -105,7 +109,8 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
         for (int i = 0; i < SD; ++i)
 #pragma unroll
             for (int j = 0; j < SN; ++j)
-                put(sm.d, L::kDPlane, L::kKS, state_n(j, ll), state_d(i, g), D[i][j]);
+                put<L::kChain>(sm.x, L::kDPlane, L::kKS, state_n(j, ll), state_d(i, g),
+                               D[i][j]);
     };
 #pragma unroll
     for (int i = 0; i < SD; ++i)
@@ -115,7 +120,6 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
         state_io(a.dhT + head * Dk * Dv, [](auto r, f4& s, int e, int o) {
             s[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0));
         });
-    state_put();
 
     wtile::u4v kn[KU], qn[KU], on[OU];
     float gn = 0.0f, bn = 0.0f;
@@ -145,7 +149,8 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
 
     for (int c = chunks - 1; c >= 0; --c) {
         state_store(ws.D + (head * chunks + c) * Dk * Dv);
-        lds_barrier();  // the previous chunk's K, Q and dO have been read
+        lds_barrier();  // what the previous chunk had in LDS has been read
+        state_put();
         {
             const int tid = wtile::fresh(threadIdx.x);
 #pragma unroll
@@ -162,13 +167,35 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
         }
         if (w == 0) gates_of_chunk(&sm.gt, gn, bn, a.scale, lane0);
         lds_barrier();
+        {
+            const int tid = wtile::fresh(threadIdx.x);
+#pragma unroll
+            for (int i = 0; i < OU; ++i) {
+                const int u = tid + i * NT, row = u / OR, n = u % OR * I::kUnit;
+                const float es = sm.gt.es[row];
+#pragma unroll
+                for (int q4 = 0; q4 < I::kUnit / 4; ++q4) {
+                    f4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (sizeof(T) == 4)
+                            v[e] = es * __uint_as_float(on[i][e]);
+                        else
+                            v[e] = es * (e & 1 ? bf16_hi(on[i][2 * q4 + e / 2])
+                                               : bf16_lo(on[i][2 * q4 + e / 2]));
+                    }
+                    put<L::kChain>(sm.od, L::kOPlane, L::kOS, row, n + 4 * q4, v);
+                }
+            }
+        }
         if (c > 0) fetch(c - 1);
         const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
 
+        f4 X[NTL];
         {
             // A's strip (lane: row i = 16 w + ll, columns 16 t + 4 g ..), and the strip of P^T
             // (lane: row j = 16 w + ll, columns i = 16 t + 4 g ..) with dU = scale P^T dO + ...
-            f4 M[4], PT[4], X[NTL], KD[NTL];
+            f4 M[4], PT[4], KD[NTL];
             typename I::Given kw[NK];
 #pragma unroll
             for (int s = 0; s < NK; ++s) kw[s] = given(sm.k, L::kKS, 16 * w + ll, s * I::kStep, g);
@@ -202,26 +229,27 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
                 X[j] = KD[j] = f4{0, 0, 0, 0};
 #pragma unroll
                 for (int s = 0; s < NK; ++s)
-                    KD[j] = mma(KD[j], kw[s], made(sm.d, L::kDPlane, L::kKS, 16 * j + ll,
-                                                   s * I::kStep, g));
+                    KD[j] = mma(KD[j], kw[s], made<L::kChain>(sm.x, L::kDPlane, L::kKS,
+                                                              16 * j + ll, s * I::kStep, g));
             }
 #pragma unroll
             for (int s = 0; s < NC; ++s)
                 if ((s + 1) * I::kStep > 16 * w) {
-                    const auto pt = from_acc<T>(PT, s);
+                    const auto pt = from_acc<T, L::kChain>(PT, s);
 #pragma unroll
                     for (int j = 0; j < NTL; ++j)
                         X[j] = mma(X[j], pt, given_t_acc(sm.d_o, L::kOS, s * I::kStep, 16 * j, ll, g));
                 }
             const f4 el = *(const f4*)(sm.gt.el + 16 * w + 4 * g);
 #pragma unroll
-            for (int j = 0; j < NTL; ++j)
-                put(sm.x, L::kXPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g,
-                    a.scale * X[j] + el * KD[j]);
+            for (int j = 0; j < NTL; ++j) X[j] = a.scale * X[j] + el * KD[j];
         }
         wave_fence();
         invert_diagonal(sm.tm, w, ll, g);
-        lds_barrier();
+        lds_barrier();  // D has been read
+#pragma unroll
+        for (int j = 0; j < NTL; ++j)
+            put<L::kChain>(sm.x, L::kXPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, X[j]);
         invert_merge1(sm.tm, w, ll, g);
         lds_barrier();
         invert_merge2(sm.tm, w, ll, g);
@@ -232,21 +260,22 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
 #pragma unroll
         for (int s = 0; s < NC; ++s)
             if ((s + 1) * I::kStep > 16 * w) {
-                const auto inv = inverse_cols<T>(sm.tm, w, s, ll, g);
+                const auto inv = inverse_cols<T, L::kChain>(sm.tm, w, s, ll, g);
 #pragma unroll
                 for (int j = 0; j < NTL; ++j)
-                    Y[j] = mma(Y[j], inv, made(sm.x, L::kXPlane, L::kUS, 16 * j + ll,
-                                               s * I::kStep, g));
+                    Y[j] = mma(Y[j], inv, made<L::kChain>(sm.x, L::kXPlane, L::kUS, 16 * j + ll,
+                                                          s * I::kStep, g));
             }
         lds_barrier();  // dU has been read
         {
             const f4 bt = *(const f4*)(sm.gt.bt + 16 * w + 4 * g);
+            const f4 eg = *(const f4*)(sm.gt.eg + 16 * w + 4 * g);
             const Rows<T> rv(dvp, (int64_t)c * C, a.L, v_step, width);
             const Rows<float> ry(yp, (int64_t)c * C, a.L, Dv, width);
 #pragma unroll
             for (int j = 0; j < NTL; ++j) {
                 const f4 dv = bt * Y[j];
-                put(sm.x, L::kXPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, -dv);
+                put<L::kChain>(sm.x, L::kXPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, -eg * dv);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     rv.set(rv.off(16 * w + 4 * g + r, 16 * j + ll, width), dv[r]);
@@ -265,40 +294,52 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
 #pragma unroll
             for (int i = 0; i < SD; ++i) {
                 const int d0 = 16 * (wd + DW * i), k0 = s * I::kStep;
-                const auto qt = scaled(given_t(sm.q, L::kKS, k0, d0, ll, g), sm.gt.es, k0, g);
-                const auto kt = scaled(given_t(sm.k, L::kKS, k0, d0, ll, g), sm.gt.eg, k0, g);
+                const auto qt = given_t(sm.q, L::kKS, k0, d0, ll, g);
+                const auto kt = given_t(sm.k, L::kKS, k0, d0, ll, g);
 #pragma unroll
                 for (int j = 0; j < SN; ++j) {
-                    D[i][j] = mma(D[i][j], qt,
-                                  given_t(sm.d_o, L::kOS, k0, 16 * (wn + NWV * j), ll, g));
-                    D[i][j] = mma(D[i][j], kt,
-                                  made(sm.x, L::kXPlane, L::kUS, state_n(j, ll), k0, g));
+                    D[i][j] = mma(D[i][j], qt, made_t<L::kChain>(sm.od, L::kOPlane, L::kOS, k0,
+                                                                 16 * (wn + NWV * j), ll, g));
+                    D[i][j] = mma(D[i][j], kt, made<L::kChain>(sm.x, L::kXPlane, L::kUS,
+                                                               state_n(j, ll), k0, g));
                 }
             }
-        state_put();
     }
     if (a.dh0) state_store(a.dh0 + head * Dk * Dv);
 }
 
 // ------------------------------------------------------------------ the gradients
-constexpr int NTW = 32;  // columns of the state at a time
+// Eight waves: four for b and what it takes (A's inverse first), four for dQ and a.  Waves w
+// and 4 + w share a SIMD and the strip of rows 16 w .., whose triangles of F and Z (j <= i for
+// the one, i >= j for the other) are five tiles together for every w.
+constexpr int GT = 512;
+
+// Columns of the state at a time: what LDS takes.
+template <int DK>
+constexpr int kGradCols = DK <= 64 ? 64 : 32;
 
 template <typename T, int DK>
 struct GradLds {
     using E = typename Io<T>::Elem;
-    static constexpr int kKS = DK + Io<T>::kPad, kUS = C + Io<T>::kPad, kNS = NTW + Io<T>::kPad;
-    static constexpr int kSPlane = DK * kNS, kRPlane = NTW * kUS, kYPlane = C * kNS;
+    static constexpr int kOut = Io<T>::kOut, kCols = kGradCols<DK>;
+    static constexpr int kKS = DK + Io<T>::kPad, kUS = C + Io<T>::kPad, kNS = kCols + Io<T>::kPad;
+    static constexpr int kSPlane = DK * kNS, kRPlane = kCols * kUS, kYPlane = C * kNS;
     E k[C * kKS];
     E q[C * kKS];
     E d_o[C * kNS];
-    E s[Io<T>::kPlanes * kSPlane];  // [d][column]: the state before the chunk
-    E d[Io<T>::kPlanes * kSPlane];  // the gradient behind it
-    E r[Io<T>::kPlanes * kRPlane];  // [column][step]
-    E u[Io<T>::kPlanes * kYPlane];  // [step][column]
-    E y[Io<T>::kPlanes * kYPlane];
+    union {
+        struct {
+            E s[kOut * kSPlane];  // [d][column]: the state before the chunk
+            E d[kOut * kSPlane];  // the gradient behind it
+        };
+        float dk[C * (DK + 4)];   // b, handed over at the head's end
+    };
+    E r[kOut * kRPlane];  // [column][step]
+    E u[kOut * kYPlane];  // [step][column]
+    E y[kOut * kYPlane];
     float tm[C * TS];
     Gates gt;
-    float dc[C], db[C], part[8];
+    float dca[C], dcb[C], db[C], part[8];
 };
 
 __device__ __forceinline__ float sum16(float v) {
@@ -306,19 +347,28 @@ __device__ __forceinline__ float sum16(float v) {
     for (int d = 1; d < 16; d <<= 1) v += __shfl_xor(v, d);
     return v;
 }
+__device__ __forceinline__ float whole(const float* m, int, int at) { return m[at]; }
+__device__ __forceinline__ float whole(const __bf16* m, int plane, int at) {
+    return (float)m[at] + (float)m[at + plane];
+}
 
 template <typename T, int DK, bool VEC>
-__global__ __launch_bounds__(NT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdWs ws) {
+__global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdWs ws) {
     using I = Io<T>;
     using L = GradLds<T, DK>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     L& sm = *(L*)smem;
+    constexpr int NTW = L::kCols;
     constexpr int NK = DK / I::kStep, NC = C / I::kStep, NN = NTW / I::kStep;
     constexpr int DTL = DK / 16, NTL = NTW / 16;
-    constexpr int KU = C * DK / I::kUnit / NT, UR = DK / I::kUnit;
-    constexpr int OU = C * NTW / I::kUnit / NT, OR = NTW / I::kUnit;
+    constexpr int UR = DK / I::kUnit, OR = NTW / I::kUnit;
+    constexpr int KU = (C * UR + GT - 1) / GT, OU = (C * OR + GT - 1) / GT;
+    constexpr int SU = DK * NTW / 4 / GT, YU = C * NTW / 4 / GT;
+    static_assert(SU >= 1 && YU >= 1, "every thread stages");
 
-    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id(), ll = lane & 15, g = lane >> 4;
+    const int lane0 = threadIdx.x % kWave;
+    const int wave = wave_id(), w = wave & 3;
+    const bool side_b = wave < 4;
     const int chunks = (int)((a.L + C - 1) / C);
     const int64_t bh = blockIdx.x / chunks;
     const int c = (int)(blockIdx.x - bh * chunks);
@@ -329,172 +379,263 @@ __global__ __launch_bounds__(NT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
     const int64_t qk_step = (int64_t)a.H * Dk, v_step = (int64_t)a.HV * Dv;
     const int64_t qk_base = (b * a.L * a.H + h) * Dk;
 
+    // What a head's columns need of memory, on its way.
+    wtile::u4v on[OU];
+    f4 sn[SU], dn[SU], yn[YU];
+    float gn = 0.0f, bn = 0.0f;
+    auto fetch = [&](int hv, int n0) {
+        const int tid = wtile::fresh(threadIdx.x), lane = tid % kWave;
+        const int64_t head = b * a.HV + hv;
+        const int width = Dv - n0;
+        const int64_t v_base = (b * a.L * a.HV + hv) * Dv + n0;
+        const Rows<T> ro((const T*)a.d_o + v_base, t0, a.L, v_step, width);
+        const Rows<float> ry(ws.Y + head * a.L * Dv + n0, t0, a.L, Dv, width);
+        const int64_t at = (head * chunks + c) * Dk * Dv;
+        const auto rs = wtile::rsrc(a.states + at, (uint32_t)(Dk * Dv * 4));
+        const auto rd = wtile::rsrc(ws.D + at, (uint32_t)(Dk * Dv * 4));
+#pragma unroll
+        for (int i = 0; i < SU; ++i) {
+            const int u = tid + i * GT, d = u / (NTW / 4), n = u % (NTW / 4) * 4;
+            if constexpr (VEC) {  // Dv is a multiple of four then
+                const int o = n < width ? (d * Dv + n0 + n) * 4 : (int)kNowhere;
+                sn[i] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(rs, o, 0, 0));
+                dn[i] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(rd, o, 0, 0));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int o = n + e < width ? (d * Dv + n0 + n + e) * 4 : (int)kNowhere;
+                    sn[i][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0));
+                    dn[i][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rd, o, 0, 0));
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < YU; ++i) {
+            const int u = tid + i * GT, t = u / (NTW / 4), n = u % (NTW / 4) * 4;
+            if constexpr (VEC) {  // Dv is a multiple of four then
+                yn[i] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                   ry.r, (int)ry.off(t, n, width), 0, 0));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) yn[i][e] = ry.get(ry.off(t, n + e, width));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < OU; ++i) {
+            const int u = tid + i * GT;
+            if (C * OR % GT == 0 || u < C * OR)
+                on[i] = ro.template get16<VEC>(u / OR, u % OR * I::kUnit, width);
+        }
+        if (wave == 4 && n0 == 0) {
+            const int64_t t = t0 + lane, o = (b * a.L + t) * a.HV + hv;
+            gn = t < a.L ? to_f32(((const T*)a.g)[o]) : 0.0f;
+            bn = t < a.L ? to_f32(((const T*)a.beta)[o]) : 0.0f;
+        }
+    };
     {
+        const int tid = threadIdx.x;
         const Rows<T> rk((const T*)a.k + qk_base, t0, a.L, qk_step, Dk);
         const Rows<T> rq((const T*)a.q + qk_base, t0, a.L, qk_step, Dk);
+        wtile::u4v kn[KU], qn[KU];
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
-            const int u = tid + i * NT, at = u / UR * L::kKS + u % UR * I::kUnit;
-            *(wtile::u4v*)(sm.k + at) = rk.template get16<VEC>(u / UR, u % UR * I::kUnit, Dk);
-            *(wtile::u4v*)(sm.q + at) = rq.template get16<VEC>(u / UR, u % UR * I::kUnit, Dk);
+            const int u = tid + i * GT;
+            if (C * UR % GT == 0 || u < C * UR) {
+                kn[i] = rk.template get16<VEC>(u / UR, u % UR * I::kUnit, Dk);
+                qn[i] = rq.template get16<VEC>(u / UR, u % UR * I::kUnit, Dk);
+            }
+        }
+        fetch(h * group, 0);
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            const int u = tid + i * GT, at = u / UR * L::kKS + u % UR * I::kUnit;
+            if (C * UR % GT == 0 || u < C * UR) {
+                *(wtile::u4v*)(sm.k + at) = kn[i];
+                *(wtile::u4v*)(sm.q + at) = qn[i];
+            }
         }
     }
-    f4 dQ[DTL], dK[DTL];
-#pragma unroll
-    for (int i = 0; i < DTL; ++i) dQ[i] = dK[i] = f4{0, 0, 0, 0};
-
     for (int hv = h * group; hv < (h + 1) * group; ++hv) {
-        const int64_t head = b * a.HV + hv;
-        if (w == 0) {
-            const int64_t t = t0 + lane;
-            const int64_t at = (b * a.L + t) * a.HV + hv;
-            gates_of_chunk(&sm.gt, t < a.L ? to_f32(((const T*)a.g)[at]) : 0.0f,
-                           t < a.L ? to_f32(((const T*)a.beta)[at]) : 0.0f, a.scale, lane);
-        }
-        __syncthreads();
-        {
-            f4 M[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                M[t] = f4{0, 0, 0, 0};
-                if (t <= w) {
-#pragma unroll
-                    for (int s = 0; s < NK; ++s)
-                        M[t] = mma(M[t], given(sm.k, L::kKS, 16 * t + ll, s * I::kStep, g),
-                                   given(sm.k, L::kKS, 16 * w + ll, s * I::kStep, g));
-                }
-            }
-            const int i = 16 * w + ll;
-            const double ci = sm.gt.cum[i];
-            const float bi = sm.gt.bt[i];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int j = 16 * t + 4 * g + r;
-                    if (t <= w)
-                        M[t][r] = j < i ? bi * M[t][r] * fast_exp2((float)(ci - sm.gt.cum[j]))
-                                        : 0.0f;
-                }
-                if (t <= (w | 1)) *(f4*)(sm.tm + i * TS + 16 * t + 4 * g) = M[t];
-            }
-        }
-        wave_fence();
-        invert_diagonal(sm.tm, w, ll, g);
-        __syncthreads();
-        invert_merge1(sm.tm, w, ll, g);
-        __syncthreads();
-        invert_merge2(sm.tm, w, ll, g);
-
-        const f4 eg = *(const f4*)(sm.gt.eg + 16 * w + 4 * g);
-        const f4 bt = *(const f4*)(sm.gt.bt + 16 * w + 4 * g);
-        const f4 el = *(const f4*)(sm.gt.el + 16 * w + 4 * g);
-        // OS = dO S^T, YS = Y S^T, UD = U D^T (lane: column d, rows 16 w + 4 g ..).
-        f4 OS[DTL], YS[DTL], UD[DTL], F1[4], Z1[4], F2[4], Z2[4], yv = {0, 0, 0, 0};
+        // Side a: X1 = dO S^T, X2 = Y S^T; side b: X1 = U D^T (lane: column d, rows 16 w + 4 g
+        // ..).  F, Z: side a has row i = 16 w + ll and columns j = 16 t + 4 g .., side b column
+        // j = 16 w + ll and rows i = 16 t + 4 g ...
+        f4 X1[DTL], X2[DTL], F[4], Z[4], yv = {0, 0, 0, 0};
         float sd = 0.0f;
 #pragma unroll
-        for (int i = 0; i < DTL; ++i) OS[i] = YS[i] = UD[i] = f4{0, 0, 0, 0};
+        for (int i = 0; i < DTL; ++i) X1[i] = X2[i] = f4{0, 0, 0, 0};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) F1[t] = Z1[t] = F2[t] = Z2[t] = f4{0, 0, 0, 0};
+        for (int t = 0; t < 4; ++t) F[t] = Z[t] = f4{0, 0, 0, 0};
 
         for (int n0 = 0; n0 < Dv; n0 += NTW) {
             const int width = Dv - n0;
-            const int64_t v_base = (b * a.L * a.HV + hv) * Dv + n0;
-            const Rows<T> ro((const T*)a.d_o + v_base, t0, a.L, v_step, width);
-            const Rows<T> rv((const T*)a.v + v_base, t0, a.L, v_step, width);
-            const Rows<float> ry(ws.Y + head * a.L * Dv + n0, t0, a.L, Dv, width);
-            __syncthreads();  // the previous columns' operands have been read
+            lds_barrier();  // the previous columns' operands, or head's decays, have been read
+            if (wave == 4 && n0 == 0) gates_of_chunk(&sm.gt, gn, bn, a.scale, lane0);
+            const int tid = wtile::fresh(threadIdx.x);
 #pragma unroll
             for (int i = 0; i < OU; ++i) {
-                const int u = tid + i * NT;
-                *(wtile::u4v*)(sm.d_o + u / OR * L::kNS + u % OR * I::kUnit) =
-                    ro.template get16<VEC>(u / OR, u % OR * I::kUnit, width);
+                const int u = tid + i * GT;
+                if (C * OR % GT == 0 || u < C * OR)
+                    *(wtile::u4v*)(sm.d_o + u / OR * L::kNS + u % OR * I::kUnit) = on[i];
             }
-            {
-                const int64_t at = (head * chunks + c) * Dk * Dv;
-                const auto rs = wtile::rsrc(a.states + at, (uint32_t)(Dk * Dv * 4));
-                const auto rd = wtile::rsrc(ws.D + at, (uint32_t)(Dk * Dv * 4));
 #pragma unroll
-                for (int i = 0; i < DK * NTW / 4 / NT; ++i) {
-                    const int u = tid + i * NT, d = u / (NTW / 4), n = u % (NTW / 4) * 4;
-                    f4 s, dd;
+            for (int i = 0; i < SU; ++i) {
+                const int u = tid + i * GT, d = u / (NTW / 4), n = u % (NTW / 4) * 4;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int o = n + e < width ? (d * Dv + n0 + n + e) * 4 : (int)kNowhere;
-                        s[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, o, 0, 0));
-                        dd[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rd, o, 0, 0));
-                        sd = fmaf(s[e], dd[e], sd);
+                for (int e = 0; e < 4; ++e) {
+                    if (n + e >= width) sn[i][e] = dn[i][e] = 0.0f;
+                    sd = fmaf(sn[i][e], dn[i][e], sd);
+                }
+                put<L::kOut>(sm.s, L::kSPlane, L::kNS, d, n, sn[i]);
+                put<L::kOut>(sm.d, L::kSPlane, L::kNS, d, n, dn[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < YU; ++i) {
+                const int u = tid + i * GT, t = u / (NTW / 4), n = u % (NTW / 4) * 4;
+                put<L::kOut>(sm.y, L::kYPlane, L::kNS, t, n, yn[i]);
+            }
+            lds_barrier();
+            if (n0 + NTW < Dv) fetch(hv, n0 + NTW);
+            else if (hv + 1 < (h + 1) * group) fetch(hv + 1, 0);
+
+            if (side_b) {
+                if (n0 == 0) {
+                    const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
+                    f4 M[4];
+                    const int i = 16 * w + ll;
+                    const double ci = sm.gt.cum[i];
+                    const float bi = sm.gt.bt[i];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        M[t] = f4{0, 0, 0, 0};
+                        if (t <= w) {
+#pragma unroll
+                            for (int s = 0; s < NK; ++s)
+                                M[t] = mma(M[t], given(sm.k, L::kKS, 16 * t + ll, s * I::kStep, g),
+                                           given(sm.k, L::kKS, 16 * w + ll, s * I::kStep, g));
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const int j = 16 * t + 4 * g + r;
+                                M[t][r] = j < i ? bi * M[t][r] *
+                                                      fast_exp2((float)(ci - sm.gt.cum[j]))
+                                                : 0.0f;
+                            }
+                        }
+                        if (t <= (w | 1)) *(f4*)(sm.tm + i * TS + 16 * t + 4 * g) = M[t];
                     }
-                    put(sm.s, L::kSPlane, L::kNS, d, n, s);
-                    put(sm.d, L::kSPlane, L::kNS, d, n, dd);
+                    wave_fence();
+                    invert_diagonal(sm.tm, w, ll, g);
+                }
+            } else {
+                const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
+                const int64_t v_base = (b * a.L * a.HV + hv) * Dv + n0;
+                const Rows<T> rv((const T*)a.v + v_base, t0, a.L, v_step, width);
+                const f4 eg = *(const f4*)(sm.gt.eg + 16 * w + 4 * g);
+                const f4 bt = *(const f4*)(sm.gt.bt + 16 * w + 4 * g);
+                float v[NTL][4];
+#pragma unroll
+                for (int j = 0; j < NTL; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        v[j][r] = rv.get(rv.off(16 * w + 4 * g + r, 16 * j + ll, width));
+                f4 KS[NTL];
+#pragma unroll
+                for (int j = 0; j < NTL; ++j) KS[j] = f4{0, 0, 0, 0};
+#pragma unroll
+                for (int s = 0; s < NK; ++s) {
+                    const auto kw = given(sm.k, L::kKS, 16 * w + ll, s * I::kStep, g);
+#pragma unroll
+                    for (int j = 0; j < NTL; ++j)
+                        KS[j] = mma(KS[j], kw, made_t<L::kOut>(sm.s, L::kSPlane, L::kNS,
+                                                               s * I::kStep, 16 * j, ll, g));
+                    step_end(KS[0]);
                 }
 #pragma unroll
-                for (int i = 0; i < C * NTW / 4 / NT; ++i) {
-                    const int u = tid + i * NT, t = u / (NTW / 4), n = u % (NTW / 4) * 4;
-                    f4 y;
+                for (int j = 0; j < NTL; ++j) {
+                    f4 R;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = ry.get(ry.off(t, n + e, width));
-                    put(sm.y, L::kYPlane, L::kNS, t, n, y);
+                    for (int r = 0; r < 4; ++r) {
+                        const float y = whole(sm.y, L::kYPlane,
+                                              (16 * w + 4 * g + r) * L::kNS + 16 * j + ll);
+                        yv[r] = fmaf(y, v[j][r], yv[r]);
+                        R[r] = bt[r] * (v[j][r] - eg[r] * KS[j][r]);
+                    }
+                    put<L::kOut>(sm.r, L::kRPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, R);
                 }
             }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < NTL; ++j) {
-                f4 KS = {0, 0, 0, 0}, R;
-#pragma unroll
-                for (int s = 0; s < NK; ++s)
-                    KS = mma(KS, given(sm.k, L::kKS, 16 * w + ll, s * I::kStep, g),
-                             made_t(sm.s, L::kSPlane, L::kNS, s * I::kStep, 16 * j, ll, g));
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float v = rv.get(rv.off(16 * w + 4 * g + r, 16 * j + ll, width));
-                    const float y = ry.get(ry.off(16 * w + 4 * g + r, 16 * j + ll, width));
-                    yv[r] = fmaf(y, v, yv[r]);
-                    R[r] = bt[r] * (v - eg[r] * KS[r]);
-                }
-                put(sm.r, L::kRPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, R);
+            lds_barrier();
+            if (n0 == 0) {
+                const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
+                if (side_b) invert_merge1(sm.tm, w, ll, g);
+                lds_barrier();
+                if (side_b) invert_merge2(sm.tm, w, ll, g);
             }
-            __syncthreads();
+            if (!side_b) {
+                const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
 #pragma unroll
-            for (int j = 0; j < NTL; ++j) {
+                for (int s = 0; s < NN; ++s) {
+                    const int k0 = s * I::kStep;
+                    const auto ow = given(sm.d_o, L::kNS, 16 * w + ll, k0, g);
+                    const auto yw = made<L::kOut>(sm.y, L::kYPlane, L::kNS, 16 * w + ll, k0, g);
+#pragma unroll
+                    for (int i = 0; i < DTL; ++i) {
+                        const auto st = made<L::kOut>(sm.s, L::kSPlane, L::kNS, 16 * i + ll, k0, g);
+                        X1[i] = mma(X1[i], ow, st);
+                        X2[i] = mma(X2[i], yw, st);
+                        if (i & 1) step_end(X2[i]);
+                    }
+                }
+            }
+            if (n0 == 0) lds_barrier();
+            // U, half of the columns by each side.
+            const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
+#pragma unroll
+            for (int jj = 0; jj < NTL / 2; ++jj) {
+                const int j = jj + (side_b ? 0 : NTL / 2);
                 f4 U = {0, 0, 0, 0};
 #pragma unroll
                 for (int s = 0; s < NC; ++s)
                     if (s * I::kStep < 16 * (w + 1))
-                        U = mma(U, made(sm.r, L::kRPlane, L::kUS, 16 * j + ll, s * I::kStep, g),
-                                inverse_rows<T>(sm.tm, w, s, ll, g));
-                put(sm.u, L::kYPlane, L::kNS, 16 * w + ll, 16 * j + 4 * g, U);
+                        U = mma(U, made<L::kOut>(sm.r, L::kRPlane, L::kUS, 16 * j + ll,
+                                                 s * I::kStep, g),
+                                inverse_rows<T, L::kOut>(sm.tm, w, s, ll, g));
+                put<L::kOut>(sm.u, L::kYPlane, L::kNS, 16 * w + ll, 16 * j + 4 * g, U);
             }
-            __syncthreads();
+            lds_barrier();
 #pragma unroll
             for (int s = 0; s < NN; ++s) {
                 const int k0 = s * I::kStep;
-                const auto ow = given(sm.d_o, L::kNS, 16 * w + ll, k0, g);
-                const auto yw = made(sm.y, L::kYPlane, L::kNS, 16 * w + ll, k0, g);
-                const auto uw = made(sm.u, L::kYPlane, L::kNS, 16 * w + ll, k0, g);
+                if (side_b) {
+                    const auto uw = made<L::kOut>(sm.u, L::kYPlane, L::kNS, 16 * w + ll, k0, g);
 #pragma unroll
-                for (int i = 0; i < DTL; ++i) {
-                    const auto st = made(sm.s, L::kSPlane, L::kNS, 16 * i + ll, k0, g);
-                    OS[i] = mma(OS[i], ow, st);
-                    YS[i] = mma(YS[i], yw, st);
-                    UD[i] = mma(UD[i], uw, made(sm.d, L::kSPlane, L::kNS, 16 * i + ll, k0, g));
-                }
+                    for (int i = 0; i < DTL; ++i) {
+                        X1[i] = mma(X1[i], uw, made<L::kOut>(sm.d, L::kSPlane, L::kNS,
+                                                             16 * i + ll, k0, g));
+                        if (i & 1) step_end(X1[i]);
+                    }
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if (t <= w) {
-                        const auto ut = made(sm.u, L::kYPlane, L::kNS, 16 * t + ll, k0, g);
-                        F1[t] = mma(F1[t], ut, ow);
-                        Z1[t] = mma(Z1[t], ut, yw);
-                    }
-                    if (t >= w) {
-                        F2[t] = mma(F2[t], given(sm.d_o, L::kNS, 16 * t + ll, k0, g), uw);
-                        Z2[t] = mma(Z2[t], made(sm.y, L::kYPlane, L::kNS, 16 * t + ll, k0, g), uw);
-                    }
+                    for (int t = 0; t < 4; ++t)
+                        if (t >= w) {
+                            F[t] = mma(F[t], given(sm.d_o, L::kNS, 16 * t + ll, k0, g), uw);
+                            Z[t] = mma(Z[t], made<L::kOut>(sm.y, L::kYPlane, L::kNS, 16 * t + ll,
+                                                           k0, g), uw);
+                            step_end(Z[t]);
+                        }
+                } else {
+                    const auto ow = given(sm.d_o, L::kNS, 16 * w + ll, k0, g);
+                    const auto yw = made<L::kOut>(sm.y, L::kYPlane, L::kNS, 16 * w + ll, k0, g);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (t <= w) {
+                            const auto ut = made<L::kOut>(sm.u, L::kYPlane, L::kNS, 16 * t + ll,
+                                                          k0, g);
+                            F[t] = mma(F[t], ut, ow);
+                            Z[t] = mma(Z[t], ut, yw);
+                            step_end(Z[t]);
+                        }
                 }
             }
         }
-        // Decays: F1, Z1 have row i = 16 w + ll and columns j = 16 t + 4 g ..; F2, Z2 have
-        // column j = 16 w + ll and rows i = 16 t + 4 g ...
+        const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
         {
             const int own = 16 * w + ll;
             const double co = sm.gt.cum[own];
@@ -504,66 +645,110 @@ __global__ __launch_bounds__(NT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                 for (int r = 0; r < 4; ++r) {
                     const int o = 16 * t + 4 * g + r;
                     const double diff = co - sm.gt.cum[o];
-                    if (t <= w) {
-                        const float e = fast_exp2((float)diff);
-                        F1[t][r] = o <= own ? a.scale * F1[t][r] * e : 0.0f;
-                        Z1[t][r] = o < own ? -Z1[t][r] * e : 0.0f;
-                    }
-                    if (t >= w) {
-                        const float e = fast_exp2((float)-diff);
-                        F2[t][r] = o >= own ? a.scale * F2[t][r] * e : 0.0f;
-                        Z2[t][r] = o > own ? -sm.gt.bt[o] * Z2[t][r] * e : 0.0f;
+                    if (side_b) {
+                        const float e = o >= own ? fast_exp2((float)-diff) : 0.0f;
+                        F[t][r] = o >= own ? a.scale * F[t][r] * e : 0.0f;
+                        Z[t][r] = o > own ? -sm.gt.bt[o] * Z[t][r] * e : 0.0f;
+                    } else {
+                        const float e = o <= own ? fast_exp2((float)diff) : 0.0f;
+                        F[t][r] = o <= own ? a.scale * F[t][r] * e : 0.0f;
+                        Z[t][r] = o < own ? -Z[t][r] * e : 0.0f;
                     }
                 }
         }
-        f4 x1 = {0, 0, 0, 0}, x2 = x1, x3 = x1, x4 = x1;
+        typename I::template Made<L::kOut> fo[NC], zo[NC];
 #pragma unroll
-        for (int i = 0; i < DTL; ++i) {
-            f4 q = a.scale * eg * OS[i], ka = -eg * YS[i], ud = el * UD[i], kb = ud;
-#pragma unroll
-            for (int s = 0; s < NC; ++s) {
-                const int k0 = s * I::kStep;
-                if (k0 < 16 * (w + 1)) {
-                    const auto kt = given_t_acc(sm.k, L::kKS, k0, 16 * i, ll, g);
-                    q = mma(q, from_acc<T>(F1, s), kt);
-                    ka = mma(ka, from_acc<T>(Z1, s), kt);
-                }
-                if (k0 + I::kStep > 16 * w) {
-                    kb = mma(kb, from_acc<T>(F2, s), given_t_acc(sm.q, L::kKS, k0, 16 * i, ll, g));
-                    kb = mma(kb, from_acc<T>(Z2, s), given_t_acc(sm.k, L::kKS, k0, 16 * i, ll, g));
-                }
-            }
+        for (int s = 0; s < NC; ++s) {
+            fo[s] = from_acc<T, L::kOut>(F, s);
+            zo[s] = from_acc<T, L::kOut>(Z, s);
+        }
+        lds_barrier();  // S and D have been read: b may take their place
+        // The value heads of a query head come one after the other: their sum stands in the
+        // workspace as float until the last one (written and read by the same lane).
+        const bool first = hv == h * group, last = hv + 1 == (h + 1) * group;
+        auto emit = [&](const f4& v, void* out, float* part, int i, int ll, int g) {
+            const Rows<T> ro((T*)out + qk_base, t0, a.L, qk_step, Dk);
+            const Rows<float> rp(part + qk_base, t0, a.L, qk_step, Dk);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int at = (16 * w + 4 * g + r) * L::kKS + 16 * i + ll;
-                const float kv = (float)sm.k[at], qv = (float)sm.q[at];
-                x1[r] = fmaf(qv, q[r], x1[r]);
-                x2[r] = fmaf(kv, ka[r], x2[r]);
-                x3[r] = fmaf(kv, kb[r], x3[r]);
-                x4[r] = fmaf(kv, ud[r], x4[r]);
+                float x = v[r];
+                if (!first) x += rp.get(rp.off(16 * w + 4 * g + r, 16 * i + ll, Dk));
+                if (last) ro.set(ro.off(16 * w + 4 * g + r, 16 * i + ll, Dk), x);
+                else rp.set(rp.off(16 * w + 4 * g + r, 16 * i + ll, Dk), x);
             }
-            dQ[i] += q;
-            dK[i] += bt * ka + kb;
-        }
-        float end = 0.0f;
+        };
+        f4 x1 = {0, 0, 0, 0}, x2 = x1, KA[DTL];
+        if (side_b) {
+            const f4 el = *(const f4*)(sm.gt.el + 16 * w + 4 * g);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const float s2 = sum16(x2[r]), db = sum16(yv[r]) + s2;
-            const float dc = sum16(x1[r]) + bt[r] * s2 - sum16(x3[r]);
-            end += x4[r];
-            if (ll == 0) {
-                sm.dc[16 * w + 4 * g + r] = dc;
-                sm.db[16 * w + 4 * g + r] = db;
+            for (int i = 0; i < DTL; ++i) {
+                const f4 ud = el * X1[i];
+                f4 kb = ud;
+#pragma unroll
+                for (int s = 0; s < NC; ++s) {
+                    const int k0 = s * I::kStep;
+                    kb = mma(kb, fo[s], given_t_acc(sm.q, L::kKS, k0, 16 * i, ll, g));
+                    kb = mma(kb, zo[s], given_t_acc(sm.k, L::kKS, k0, 16 * i, ll, g));
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float kv = (float)sm.k[(16 * w + 4 * g + r) * L::kKS + 16 * i + ll];
+                    x1[r] = fmaf(kv, kb[r], x1[r]);
+                    x2[r] = fmaf(kv, ud[r], x2[r]);
+                    sm.dk[(16 * w + 4 * g + r) * (DK + 4) + 16 * i + ll] = kb[r];
+                }
+                step_end(kb);
+            }
+        } else {
+            const f4 eg = *(const f4*)(sm.gt.eg + 16 * w + 4 * g);
+            const f4 bt = *(const f4*)(sm.gt.bt + 16 * w + 4 * g);
+#pragma unroll
+            for (int i = 0; i < DTL; ++i) {
+                f4 q = a.scale * eg * X1[i], ka = -eg * X2[i];
+#pragma unroll
+                for (int s = 0; s < NC; ++s) {
+                    const auto kt = given_t_acc(sm.k, L::kKS, s * I::kStep, 16 * i, ll, g);
+                    q = mma(q, fo[s], kt);
+                    ka = mma(ka, zo[s], kt);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = (16 * w + 4 * g + r) * L::kKS + 16 * i + ll;
+                    x1[r] = fmaf((float)sm.q[at], q[r], x1[r]);
+                    x2[r] = fmaf((float)sm.k[at], ka[r], x2[r]);
+                }
+                emit(q, a.dq, ws.dq, i, ll, g);
+                KA[i] = bt * ka;
+                step_end(KA[i]);
             }
         }
+        // The rows' sums; <S, D> and the decays behind the steps go to the chunk's last one.
+        float end = side_b ? x2[0] + x2[1] + x2[2] + x2[3] : 0.0f;
         end = fmaf(sm.gt.eg[C - 1], sd, end);
 #pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int i = 16 * w + 4 * g + r;
+            const float s1 = sum16(x1[r]);
+            if (side_b) {
+                if (ll == 0) sm.dcb[i] = s1;
+            } else {
+                const float s2 = sum16(x2[r]), sy = sum16(yv[r]);
+                if (ll == 0) {
+                    sm.dca[i] = fmaf(sm.gt.bt[i], s2, s1);
+                    sm.db[i] = sy + s2;
+                }
+            }
+        }
+#pragma unroll
         for (int d = 1; d < kWave; d <<= 1) end += __shfl_xor(end, d);
-        if (lane == 0) sm.part[w] = end;
-        __syncthreads();
-        if (w == 0) {
-            float s = sm.dc[lane] + (lane == C - 1 ? sm.part[0] + sm.part[1] + sm.part[2] + sm.part[3]
-                                                   : 0.0f);
+        if (lane == 0) sm.part[wave] = end;
+        lds_barrier();
+        if (wave == 0) {
+            float s = sm.dca[lane] - sm.dcb[lane];
+            if (lane == C - 1) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s += sm.part[i];
+            }
 #pragma unroll
             for (int d = 1; d < C; d <<= 1) {
                 const float o = __shfl_down(s, d);
@@ -576,19 +761,16 @@ __global__ __launch_bounds__(NT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                 store((T*)a.dbeta + at, sm.db[lane]);
             }
         }
-        // The next head's decays are written by wave 0, which has read this one's sums; the
-        // others' reads of them are behind the barrier above.
-    }
-    const Rows<T> rq((T*)a.dq + qk_base, t0, a.L, qk_step, Dk);
-    const Rows<T> rk((T*)a.dk + qk_base, t0, a.L, qk_step, Dk);
+        if (!side_b) {
 #pragma unroll
-    for (int i = 0; i < DTL; ++i)
+            for (int i = 0; i < DTL; ++i) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const uint32_t o = rq.off(16 * w + 4 * g + r, 16 * i + ll, Dk);
-            rq.set(o, dQ[i][r]);
-            rk.set(o, dK[i][r]);
+                for (int r = 0; r < 4; ++r)
+                    KA[i][r] += sm.dk[(16 * w + 4 * g + r) * (DK + 4) + 16 * i + ll];
+                emit(KA[i], a.dk, ws.dk, i, ll, g);
+            }
         }
+    }
 }
 
 // ------------------------------------------------------------------ launches
@@ -616,7 +798,7 @@ hipError_t launch_grad(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t strea
         allow_dynamic_lds((const void*)delta_bwd_grad_kernel<T, DK, VEC>, bytes, lds_set);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((delta_bwd_grad_kernel<T, DK, VEC>), dim3((unsigned)(a.B * a.H * chunks)),
-                       dim3(NT), bytes, stream, a, ws);
+                       dim3(GT), bytes, stream, a, ws);
     return hipGetLastError();
 }
 
@@ -643,14 +825,28 @@ size_t state_bytes(int64_t B, int64_t L, int64_t HV, int Dk, int Dv) {
     return round_up((size_t)(B * HV * ((L + C - 1) / C) * Dk * Dv) * 4);
 }
 
+size_t y_bytes(int64_t B, int64_t L, int64_t HV, int Dv) {
+    return round_up((size_t)(B * HV * L * Dv) * 4);
+}
+size_t sum_bytes(int64_t B, int64_t L, int64_t H, int Dk) {
+    return round_up((size_t)(B * L * H * Dk) * 4);
+}
+
 }  // namespace
 
-size_t delta_backward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv, IoType) {
-    return state_bytes(B, L, HV, Dk, Dv) + round_up((size_t)(B * HV * L * Dv) * 4);
+size_t delta_backward_workspace(int64_t B, int64_t L, int64_t H, int64_t HV, int Dk, int Dv,
+                                IoType) {
+    return state_bytes(B, L, HV, Dk, Dv) + y_bytes(B, L, HV, Dv) +
+           (HV > H ? 2 * sum_bytes(B, L, H, Dk) : 0);
 }
 
 hipError_t launch_delta_backward(const DeltaBwdArgs& a, void* ws, hipStream_t stream) {
-    const BwdWs s{(float*)ws, (float*)((char*)ws + state_bytes(a.B, a.L, a.HV, a.Dk, a.Dv))};
+    char* p = (char*)ws;
+    BwdWs s{(float*)p, (float*)(p + state_bytes(a.B, a.L, a.HV, a.Dk, a.Dv)), nullptr, nullptr};
+    if (a.HV > a.H) {
+        s.dq = (float*)((char*)s.Y + y_bytes(a.B, a.L, a.HV, a.Dv));
+        s.dk = (float*)((char*)s.dq + sum_bytes(a.B, a.L, a.H, a.Dk));
+    }
     return a.io == IoType::kF32 ? launch_typed<float>(a, s, stream)
                                 : launch_typed<bf16>(a, s, stream);
 }

@@ -8,7 +8,9 @@
 // A workgroup walks the chunks of one head's strip of DVT columns (columns of the state do not
 // mix) with the state in its accumulators and, as an operand, in LDS.  Q stays in registers
 // as the operand of its wave's strip, and so does P, whose accumulators are an operand as they
-// are; K, the inverse of I + A, R = the right-hand side and then U go through LDS.
+// are; K and the inverse of I + A go through LDS, and in one place there, one after the other,
+// the state, the right-hand side R, and U with the decays up to the chunk's end (so that K is
+// an operand of S' as it was given).
 #include <hip/hip_runtime.h>
 
 #include "delta_tile.hpp"
@@ -22,11 +24,13 @@ using namespace dtile;
 template <typename T, int DK, int DVT>
 struct FwdLds {
     using E = typename Io<T>::Elem;
+    static constexpr int kChain = Io<T>::kChain, kOut = Io<T>::kOut;
     static constexpr int kKS = DK + Io<T>::kPad, kUS = C + Io<T>::kPad;
     static constexpr int kSPlane = DVT * kKS, kUPlane = DVT * kUS;
     E k[C * kKS];
-    E s[Io<T>::kPlanes * kSPlane];   // [column][d]
-    E ru[Io<T>::kPlanes * kUPlane];  // [column][step]: R, then U
+    // [column][d] the state; then [column][step] R; then the updates times el
+    E x[kChain * (kSPlane > kUPlane ? kSPlane : kUPlane)];
+    E u[kOut * kUPlane];  // [column][step] the updates
     float tm[C * TS];
     Gates gt;
 };
@@ -94,7 +98,8 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
         for (int i = 0; i < SD; ++i)
 #pragma unroll
             for (int j = 0; j < SN; ++j)
-                put(sm.s, L::kSPlane, L::kKS, state_n(j, ll), state_d(i, g), S[i][j]);
+                put<L::kChain>(sm.x, L::kSPlane, L::kKS, state_n(j, ll), state_d(i, g),
+                               S[i][j]);
     };
 #pragma unroll
     for (int i = 0; i < SD; ++i)
@@ -104,7 +109,6 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
         state_io(a.h0 + head * Dk * Dv, [](auto r, f4& s, int e, int o) {
             s[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0));
         });
-    state_put();
 
     wtile::u4v kn[KU], qn[NK];
     float vn[NTL][4], gn = 0.0f, bn = 0.0f;
@@ -142,7 +146,8 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
 
     for (int c = 0; c < chunks; ++c) {
         if (a.states) state_store(a.states + (head * chunks + c) * Dk * Dv);
-        lds_barrier();  // the previous chunk's K has been read
+        lds_barrier();  // the previous chunk's K and updates have been read
+        state_put();
         {
             const int tid = wtile::fresh(threadIdx.x);
 #pragma unroll
@@ -170,40 +175,40 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 M[t] = P[t] = f4{0, 0, 0, 0};
-                if (t <= w) {
 #pragma unroll
-                    for (int s = 0; s < NK; ++s) {
-                        const auto kt = given(sm.k, L::kKS, 16 * t + ll, s * I::kStep, g);
-                        M[t] = mma(M[t], kt, kw[s]);
-                        P[t] = mma(P[t], kt, qw[s]);
-                    }
+                for (int s = 0; s < NK; ++s) {
+                    const auto kt = given(sm.k, L::kKS, 16 * t + ll, s * I::kStep, g);
+                    M[t] = mma(M[t], kt, kw[s]);
+                    P[t] = mma(P[t], kt, qw[s]);
                 }
+                step_end(P[t]);
             }
 #pragma unroll
             for (int j = 0; j < NTL; ++j) {
                 KS[j] = O[j] = f4{0, 0, 0, 0};
 #pragma unroll
                 for (int s = 0; s < NK; ++s) {
-                    const auto st = made(sm.s, L::kSPlane, L::kKS, 16 * j + ll, s * I::kStep, g);
+                    const auto st = made<L::kChain>(sm.x, L::kSPlane, L::kKS, 16 * j + ll,
+                                                    s * I::kStep, g);
                     KS[j] = mma(KS[j], kw[s], st);
-                    O[j] = mma(O[j], qw[s], st);
+                    O[j] = mma(O[j], qw[s], made<L::kOut>(sm.x, L::kSPlane, L::kKS, 16 * j + ll,
+                                                          s * I::kStep, g));
                 }
+                step_end(O[j]);
             }
             const int i = 16 * w + ll;
             const double ci = sm.gt.cum[i];
             const float bi = sm.gt.bt[i];
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                if (t <= w) {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const int j = 16 * t + 4 * g + r;
-                        const float e = fast_exp2((float)(ci - sm.gt.cum[j]));
-                        P[t][r] = j <= i ? P[t][r] * e : 0.0f;
-                        M[t][r] = j < i ? bi * M[t][r] * e : 0.0f;
-                    }
+                for (int r = 0; r < 4; ++r) {
+                    const int j = 16 * t + 4 * g + r;
+                    const float e = fast_exp2((float)(ci - sm.gt.cum[j]));
+                    P[t][r] = j <= i ? P[t][r] * e : 0.0f;
+                    M[t][r] = j < i ? bi * M[t][r] * e : 0.0f;
                 }
-                if (t <= (w | 1)) *(f4*)(sm.tm + i * TS + 16 * t + 4 * g) = M[t];
+                *(f4*)(sm.tm + i * TS + 16 * t + 4 * g) = M[t];
             }
         }
         {
@@ -211,17 +216,18 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
             const f4 bt = *(const f4*)(sm.gt.bt + 16 * w + 4 * g);
 #pragma unroll
             for (int j = 0; j < NTL; ++j) {
-                f4 R;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) R[r] = bt[r] * (vn[j][r] - eg[r] * KS[j][r]);
-                put(sm.ru, L::kUPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, R);
+                for (int r = 0; r < 4; ++r) KS[j][r] = bt[r] * (vn[j][r] - eg[r] * KS[j][r]);
                 O[j] *= eg;
             }
         }
         if (c + 1 < chunks) fetch_qv(c + 1);
         wave_fence();
         invert_diagonal(sm.tm, w, ll, g);
-        lds_barrier();
+        lds_barrier();  // the state has been read
+#pragma unroll
+        for (int j = 0; j < NTL; ++j)
+            put<L::kChain>(sm.x, L::kUPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, KS[j]);
         invert_merge1(sm.tm, w, ll, g);
         lds_barrier();
         invert_merge2(sm.tm, w, ll, g);
@@ -232,18 +238,22 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
 #pragma unroll
         for (int s = 0; s < NC; ++s)
             if (s * I::kStep < 16 * (w + 1)) {
-                const auto inv = inverse_rows<T>(sm.tm, w, s, ll, g);
+                const auto inv = inverse_rows<T, L::kChain>(sm.tm, w, s, ll, g);
 #pragma unroll
                 for (int j = 0; j < NTL; ++j)
-                    U[j] = mma(U[j], inv, made(sm.ru, L::kUPlane, L::kUS, 16 * j + ll,
-                                               s * I::kStep, g));
+                    U[j] = mma(U[j], inv, made<L::kChain>(sm.x, L::kUPlane, L::kUS, 16 * j + ll,
+                                                          s * I::kStep, g));
             }
         lds_barrier();  // R has been read
+        {
+            const f4 el = *(const f4*)(sm.gt.el + 16 * w + 4 * g);
 #pragma unroll
-        for (int j = 0; j < NTL; ++j)
-            put(sm.ru, L::kUPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, U[j]);
+            for (int j = 0; j < NTL; ++j) {
+                put<L::kOut>(sm.u, L::kUPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, U[j]);
+                put<L::kChain>(sm.x, L::kUPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, el * U[j]);
+            }
+        }
         lds_barrier();
-        // The state first: it is what the next chunk waits for.
         const float et = sm.gt.eg[C - 1];
 #pragma unroll
         for (int i = 0; i < SD; ++i)
@@ -253,22 +263,20 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
         for (int s = 0; s < NC; ++s)
 #pragma unroll
             for (int i = 0; i < SD; ++i) {
-                const auto kt = scaled(given_t(sm.k, L::kKS, s * I::kStep, 16 * (wd + DW * i), ll, g),
-                                       sm.gt.el, s * I::kStep, g);
+                const auto kt = given_t(sm.k, L::kKS, s * I::kStep, 16 * (wd + DW * i), ll, g);
 #pragma unroll
                 for (int j = 0; j < SN; ++j)
-                    S[i][j] = mma(S[i][j], kt, made(sm.ru, L::kUPlane, L::kUS, state_n(j, ll),
-                                                    s * I::kStep, g));
+                    S[i][j] = mma(S[i][j], kt, made<L::kChain>(sm.x, L::kUPlane, L::kUS,
+                                                               state_n(j, ll), s * I::kStep, g));
             }
-        state_put();
 #pragma unroll
         for (int s = 0; s < NC; ++s)
-            if (s * I::kStep < 16 * (w + 1)) {
-                const auto pw = from_acc<T>(P, s);
+            {
+                const auto pw = from_acc<T, L::kOut>(P, s);
 #pragma unroll
                 for (int j = 0; j < NTL; ++j)
-                    O[j] = mma(O[j], pw, made_acc(sm.ru, L::kUPlane, L::kUS, 16 * j + ll,
-                                                  s * I::kStep, g));
+                    O[j] = mma(O[j], pw, made_acc<L::kOut>(sm.u, L::kUPlane, L::kUS, 16 * j + ll,
+                                                           s * I::kStep, g));
             }
         const Rows<T> ro(op, (int64_t)c * C, a.L, v_step, width);
 #pragma unroll

@@ -10,11 +10,11 @@
 //   fp32 I/O: four v_mfma_f32_16x16x4_f32, k = 4 g .. 4 g + 3 of 16 (16 bytes; the j-th
 //     instruction contracts the j-th value of every lane).
 // fp32 I/O is thus multiplied in fp32.  With bf16 I/O the inputs are exact operands, and what
-// is computed from them (states, updates, the inverse) is a pair of bf16 planes, hi + lo with
-// hi = bf16(x), lo = bf16(x - hi): 16 bits of mantissa, products of two such as
-// hi hi + hi lo + lo hi, relative error about 3 * 2^-17 each.  Against 64 bits the chunked
-// recurrence then shows some 5e-6 on the float states over 2048 steps; a single plane gives
-// 1e-3.
+// is computed from them is given as a sum of bf16 planes (x = h + m + l, each the bf16 nearest
+// to what the ones before leave), with the products of planes whose indexes add up to less
+// than their number: three planes, hence fp32's 24 bits, on the way to a state, which is
+// float and lasts (two planes show 3e-6 to 9e-6 against 64 bits there, three 3e-7), and two,
+// 16 bits, where the result is rounded to bf16 at once.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -35,64 +35,72 @@ constexpr int NT = 256;   // threads
 constexpr int TS = 68;    // floats in a row of the triangular matrix in LDS
 typedef __bf16 b4 __attribute__((ext_vector_type(4)));
 
+// Keeps the compiler from starting the LDS reads of the following steps of an unrolled loop
+// before this one's accumulators are formed (left alone it starts all reads at once, and spills
+// what else the wave holds).  No instruction.
+__device__ __forceinline__ void step_end(f4& x) { asm volatile("" : "+v"(x) : : "memory"); }
+
 // ------------------------------------------------------------------ operands
 struct F32Op {  // fp32: given and computed operands alike
     f4 v;
 };
-struct Bf16Op {  // a given operand, exact
-    b8 h;
-};
-struct Bf16Op2 {  // a computed one, two planes
-    b8 h, l;
+template <int P>
+struct Bf16Op {  // P planes
+    b8 p[P];
 };
 
 template <typename T>
 struct Io;
+// kChain, kOut: planes of an operand computed for a state, and for an output of type T.
 template <>
 struct Io<float> {
     using Elem = float;
     using Given = F32Op;
+    template <int P>
     using Made = F32Op;
-    static constexpr int kPlanes = 1, kStep = 16, kPad = 4, kUnit = 4;  // kUnit: elements in 16 bytes
+    static constexpr int kChain = 1, kOut = 1, kStep = 16, kPad = 4, kUnit = 4;
 };
 template <>
 struct Io<bf16> {
     using Elem = __bf16;
-    using Given = Bf16Op;
-    using Made = Bf16Op2;
-    static constexpr int kPlanes = 2, kStep = 32, kPad = 8, kUnit = 8;
-};
+    using Given = Bf16Op<1>;
+    template <int P>
+    using Made = Bf16Op<P>;
+    static constexpr int kChain = 3, kOut = 2, kStep = 32, kPad = 8, kUnit = 8;
+};  // kUnit: elements in 16 bytes
 
-__device__ __forceinline__ f4 mma16(b8 a, b8 b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
 __device__ __forceinline__ f4 mma(f4 c, const F32Op& a, const F32Op& b) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
     return c;
 }
-__device__ __forceinline__ f4 mma(f4 c, const Bf16Op& a, const Bf16Op& b) {
-    return mma16(a.h, b.h, c);
-}
-__device__ __forceinline__ f4 mma(f4 c, const Bf16Op& a, const Bf16Op2& b) {
-    return mma16(a.h, b.h, mma16(a.h, b.l, c));
-}
-__device__ __forceinline__ f4 mma(f4 c, const Bf16Op2& a, const Bf16Op& b) {
-    return mma16(a.h, b.h, mma16(a.l, b.h, c));
-}
-__device__ __forceinline__ f4 mma(f4 c, const Bf16Op2& a, const Bf16Op2& b) {
-    return mma16(a.h, b.h, mma16(a.h, b.l, mma16(a.l, b.h, c)));
+template <int PA, int PB>
+__device__ __forceinline__ f4 mma(f4 c, const Bf16Op<PA>& a, const Bf16Op<PB>& b) {
+    constexpr int N = PA > PB ? PA : PB;
+#pragma unroll
+    for (int n = N - 1; n >= 0; --n)  // the small products first
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            if (n - i >= 0 && n - i < PB)
+                c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[n - i], c, 0, 0, 0);
+    return c;
 }
 
-// Eight floats as two planes.
-__device__ __forceinline__ Bf16Op2 split(const float (&x)[8]) {
-    Bf16Op2 o;
+// Eight floats as planes.
+template <int P>
+__device__ __forceinline__ Bf16Op<P> split(const float (&x)[8]) {
+    Bf16Op<P> o;
+    float r[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        o.h[e] = (__bf16)x[e];
-        o.l[e] = (__bf16)(x[e] - (float)o.h[e]);
-    }
+    for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+    for (int p = 0; p < P; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            o.p[p][e] = (__bf16)r[e];
+            r[e] -= (float)o.p[p][e];
+        }
     return o;
 }
 
@@ -100,30 +108,40 @@ __device__ __forceinline__ Bf16Op2 split(const float (&x)[8]) {
 __device__ __forceinline__ F32Op given(const float* m, int stride, int row, int k0, int g) {
     return {*(const f4*)(m + row * stride + k0 + 4 * g)};
 }
-__device__ __forceinline__ Bf16Op given(const __bf16* m, int stride, int row, int k0, int g) {
-    return {*(const b8*)(m + row * stride + k0 + 8 * g)};
+__device__ __forceinline__ Bf16Op<1> given(const __bf16* m, int stride, int row, int k0, int g) {
+    return {{*(const b8*)(m + row * stride + k0 + 8 * g)}};
 }
 // The same of a computed matrix; `plane`: elements from one plane to the next.
+template <int P>
 __device__ __forceinline__ F32Op made(const float* m, int, int stride, int row, int k0, int g) {
     return given(m, stride, row, k0, g);
 }
-__device__ __forceinline__ Bf16Op2 made(const __bf16* m, int plane, int stride, int row, int k0,
-                                        int g) {
-    const __bf16* p = m + row * stride + k0 + 8 * g;
-    return {*(const b8*)p, *(const b8*)(p + plane)};
+template <int P>
+__device__ __forceinline__ Bf16Op<P> made(const __bf16* m, int plane, int stride, int row, int k0,
+                                          int g) {
+    Bf16Op<P> o;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+        o.p[i] = *(const b8*)(m + i * plane + row * stride + k0 + 8 * g);
+    return o;
 }
 // The k order that accumulators of two neighbouring tiles have: 4 g .. of the first, then of
 // the second.  An operand made of accumulators is multiplied by one that is read this way.
+template <int P>
 __device__ __forceinline__ F32Op made_acc(const float* m, int, int stride, int row, int k0, int g) {
     return given(m, stride, row, k0, g);
 }
-__device__ __forceinline__ Bf16Op2 made_acc(const __bf16* m, int plane, int stride, int row,
-                                            int k0, int g) {
-    const __bf16* p = m + row * stride + k0 + 4 * g;
-    const b4 h0 = *(const b4*)p, h1 = *(const b4*)(p + 16);
-    const b4 l0 = *(const b4*)(p + plane), l1 = *(const b4*)(p + plane + 16);
-    return {__builtin_shufflevector(h0, h1, 0, 1, 2, 3, 4, 5, 6, 7),
-            __builtin_shufflevector(l0, l1, 0, 1, 2, 3, 4, 5, 6, 7)};
+template <int P>
+__device__ __forceinline__ Bf16Op<P> made_acc(const __bf16* m, int plane, int stride, int row,
+                                              int k0, int g) {
+    Bf16Op<P> o;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        const __bf16* p = m + i * plane + row * stride + k0 + 4 * g;
+        o.p[i] = __builtin_shufflevector(*(const b4*)p, *(const b4*)(p + 16), 0, 1, 2, 3, 4, 5, 6,
+                                         7);
+    }
+    return o;
 }
 // A matrix whose columns run along the contraction: operand row = column `col0 + l % 16`, k
 // from row k0 on, in natural order.
@@ -132,70 +150,66 @@ __device__ __forceinline__ F32Op given_t(const float* m, int stride, int k0, int
     const float* p = m + (k0 + 4 * g) * stride + col0 + ll;
     return {{p[0], p[stride], p[2 * stride], p[3 * stride]}};
 }
-__device__ __forceinline__ Bf16Op given_t(const __bf16* m, int stride, int k0, int col0, int ll,
-                                          int g) {
+__device__ __forceinline__ Bf16Op<1> given_t(const __bf16* m, int stride, int k0, int col0, int ll,
+                                             int g) {
     const __bf16* p = m + (k0 + 8 * g + (ll >> 2)) * stride + col0 + 4 * (ll & 3);
-    return {wtile::tr_pair((const char*)p, (const char*)(p + 4 * stride))};
+    return {{wtile::tr_pair((const char*)p, (const char*)(p + 4 * stride))}};
 }
+template <int P>
 __device__ __forceinline__ F32Op made_t(const float* m, int, int stride, int k0, int col0, int ll,
                                         int g) {
     return given_t(m, stride, k0, col0, ll, g);
 }
-__device__ __forceinline__ Bf16Op2 made_t(const __bf16* m, int plane, int stride, int k0,
-                                          int col0, int ll, int g) {
-    return {given_t(m, stride, k0, col0, ll, g).h, given_t(m + plane, stride, k0, col0, ll, g).h};
+template <int P>
+__device__ __forceinline__ Bf16Op<P> made_t(const __bf16* m, int plane, int stride, int k0,
+                                            int col0, int ll, int g) {
+    Bf16Op<P> o;
+#pragma unroll
+    for (int i = 0; i < P; ++i) o.p[i] = given_t(m + i * plane, stride, k0, col0, ll, g).p[0];
+    return o;
 }
-
 // As given_t, in the k order of accumulators.
 __device__ __forceinline__ F32Op given_t_acc(const float* m, int stride, int k0, int col0, int ll,
                                              int g) {
     return given_t(m, stride, k0, col0, ll, g);
 }
-__device__ __forceinline__ Bf16Op given_t_acc(const __bf16* m, int stride, int k0, int col0,
-                                              int ll, int g) {
+__device__ __forceinline__ Bf16Op<1> given_t_acc(const __bf16* m, int stride, int k0, int col0,
+                                                 int ll, int g) {
     const __bf16* p = m + (k0 + 4 * g + (ll >> 2)) * stride + col0 + 4 * (ll & 3);
-    return {wtile::tr_pair((const char*)p, (const char*)(p + 16 * stride))};
+    return {{wtile::tr_pair((const char*)p, (const char*)(p + 16 * stride))}};
 }
 
 // Four accumulator values (consecutive k of a row of the operand that they become).
+template <int P>
 __device__ __forceinline__ void put(float* m, int, int stride, int row, int k0, const f4& v) {
     *(f4*)(m + row * stride + k0) = v;
 }
+template <int P>
 __device__ __forceinline__ void put(__bf16* m, int plane, int stride, int row, int k0,
                                     const f4& v) {
-    b4 h, l;
+    f4 r = v;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-        h[r] = (__bf16)v[r];
-        l[r] = (__bf16)(v[r] - (float)h[r]);
+    for (int i = 0; i < P; ++i) {
+        b4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h[e] = (__bf16)r[e];
+            r[e] -= (float)h[e];
+        }
+        *(b4*)(m + i * plane + row * stride + k0) = h;
     }
-    __bf16* p = m + row * stride + k0;
-    *(b4*)p = h;
-    *(b4*)(p + plane) = l;
-}
-
-// A given operand with its k-th column times s[k] (s in LDS, natural order from k0).
-__device__ __forceinline__ F32Op scaled(const F32Op& a, const float* s, int k0, int g) {
-    return {a.v * *(const f4*)(s + k0 + 4 * g)};
-}
-__device__ __forceinline__ Bf16Op2 scaled(const Bf16Op& a, const float* s, int k0, int g) {
-    const f4 s0 = *(const f4*)(s + k0 + 8 * g), s1 = *(const f4*)(s + k0 + 8 * g + 4);
-    float x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = (float)a.h[e] * (e < 4 ? s0[e & 3] : s1[e & 3]);
-    return split(x);
 }
 
 // An operand from accumulators: tile t of fp32, tiles 2 t and 2 t + 1 of bf16.
-template <typename T>
-__device__ __forceinline__ typename Io<T>::Made from_acc(const f4* acc, int t) {
+template <typename T, int P>
+__device__ __forceinline__ typename Io<T>::template Made<P> from_acc(const f4* acc, int t) {
     if constexpr (sizeof(T) == 4) {
         return F32Op{acc[t]};
     } else {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = acc[2 * t + (e >> 2)][e & 3];
-        return split(x);
+        return split<P>(x);
     }
 }
 
@@ -309,6 +323,9 @@ __device__ __forceinline__ void invert_diagonal(float* tm, int w, int ll, int g)
                 if (m + e < i) s = fmaf(-a[e], x[m + e], s);
         }
         x[i] = s;
+        // Taken through here, x is formed before the next rows' reads: all 30 of them in flight
+        // at once would cost 120 registers.
+        if (i % 4 == 3) asm volatile("" : "+v"(x[i]) : : "memory");
     }
     wave_fence();
 #pragma unroll
@@ -355,21 +372,21 @@ __device__ __forceinline__ const float* tile_at(const float* tm, int i, int j) {
 }
 
 // Operand of the inverse's rows 16 i .. (k: columns, step s), and of its transpose.
-template <typename T>
-__device__ __forceinline__ typename Io<T>::Made inverse_rows(const float* tm, int i, int s,
-                                                             int ll, int g) {
+template <typename T, int P>
+__device__ __forceinline__ typename Io<T>::template Made<P> inverse_rows(const float* tm, int i,
+                                                                        int s, int ll, int g) {
     if constexpr (sizeof(T) == 4) {
         return given(tile_at(tm, i, s), TS, ll, 0, g);
     } else {
         const float* p = tile_at(tm, i, 2 * s + (g >> 1)) + ll * TS + 8 * (g & 1);
         const f4 a = *(const f4*)p, b = *(const f4*)(p + 4);
         const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-        return split(x);
+        return split<P>(x);
     }
 }
-template <typename T>
-__device__ __forceinline__ typename Io<T>::Made inverse_cols(const float* tm, int i, int s,
-                                                             int ll, int g) {
+template <typename T, int P>
+__device__ __forceinline__ typename Io<T>::template Made<P> inverse_cols(const float* tm, int i,
+                                                                        int s, int ll, int g) {
     if constexpr (sizeof(T) == 4) {
         return given_t(tile_at(tm, s, i), TS, 0, 0, ll, g);
     } else {
@@ -377,7 +394,7 @@ __device__ __forceinline__ typename Io<T>::Made inverse_cols(const float* tm, in
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = p[e * TS];
-        return split(x);
+        return split<P>(x);
     }
 }
 

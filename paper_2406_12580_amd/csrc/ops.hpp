@@ -90,7 +90,8 @@ struct DeltaBwdArgs {
     float scale;
     IoType io;
 };
-size_t delta_backward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv, IoType io);
+size_t delta_backward_workspace(int64_t B, int64_t L, int64_t H, int64_t HV, int Dk, int Dv,
+                                IoType io);
 hipError_t launch_delta_backward(const DeltaBwdArgs& a, void* ws, hipStream_t stream);
 hipError_t launch_delta_step(const DeltaStepArgs& a, hipStream_t stream);
 
