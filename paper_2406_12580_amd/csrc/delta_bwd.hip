@@ -370,27 +370,37 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
     const int wave = wave_id(), w = wave & 3;
     const bool side_b = wave < 4;
     const int chunks = (int)((a.L + C - 1) / C);
-    const int64_t bh = blockIdx.x / chunks;
-    const int c = (int)(blockIdx.x - bh * chunks);
-    const int64_t b = bh / a.H;
-    const int h = (int)(bh - b * a.H), group = a.HV / a.H;
+    const int group = a.HV / a.H;
     const int Dk = a.Dk, Dv = a.Dv;
-    const int64_t t0 = (int64_t)c * C;
     const int64_t qk_step = (int64_t)a.H * Dk, v_step = (int64_t)a.HV * Dv;
-    const int64_t qk_base = (b * a.L * a.H + h) * Dk;
+    // A chunk of a query head.
+    struct Item {
+        int64_t b, t0, qk_base;
+        int h, c;
+    };
+    auto item_at = [&](int64_t i) {
+        const int64_t bh = i / chunks;
+        Item o;
+        o.c = (int)(i - bh * chunks);
+        o.b = bh / a.H;
+        o.h = (int)(bh - o.b * a.H);
+        o.t0 = (int64_t)o.c * C;
+        o.qk_base = (o.b * a.L * a.H + o.h) * Dk;
+        return o;
+    };
 
     // What a head's columns need of memory, on its way.
-    wtile::u4v on[OU];
+    wtile::u4v on[OU], kn[KU], qn[KU];
     f4 sn[SU], dn[SU], yn[YU];
-    float gn = 0.0f, bn = 0.0f;
-    auto fetch = [&](int hv, int n0) {
+    float gn = 0.0f, bn = 0.0f, vn[NTL][4];
+    auto fetch = [&](const Item& it, int hv, int n0) {
         const int tid = wtile::fresh(threadIdx.x), lane = tid % kWave;
-        const int64_t head = b * a.HV + hv;
+        const int64_t head = it.b * a.HV + hv;
         const int width = Dv - n0;
-        const int64_t v_base = (b * a.L * a.HV + hv) * Dv + n0;
-        const Rows<T> ro((const T*)a.d_o + v_base, t0, a.L, v_step, width);
-        const Rows<float> ry(ws.Y + head * a.L * Dv + n0, t0, a.L, Dv, width);
-        const int64_t at = (head * chunks + c) * Dk * Dv;
+        const int64_t v_base = (it.b * a.L * a.HV + hv) * Dv + n0;
+        const Rows<T> ro((const T*)a.d_o + v_base, it.t0, a.L, v_step, width);
+        const Rows<float> ry(ws.Y + head * a.L * Dv + n0, it.t0, a.L, Dv, width);
+        const int64_t at = (head * chunks + it.c) * Dk * Dv;
         const auto rs = wtile::rsrc(a.states + at, (uint32_t)(Dk * Dv * 4));
         const auto rd = wtile::rsrc(ws.D + at, (uint32_t)(Dk * Dv * 4));
 #pragma unroll
@@ -426,17 +436,25 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
             if (C * OR % GT == 0 || u < C * OR)
                 on[i] = ro.template get16<VEC>(u / OR, u % OR * I::kUnit, width);
         }
+        if (!side_b) {
+            const int ll = lane & 15, g = lane >> 4;
+            const Rows<T> rv((const T*)a.v + v_base, it.t0, a.L, v_step, width);
+#pragma unroll
+            for (int j = 0; j < NTL; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    vn[j][r] = rv.get(rv.off(16 * w + 4 * g + r, 16 * j + ll, width));
+        }
         if (wave == 4 && n0 == 0) {
-            const int64_t t = t0 + lane, o = (b * a.L + t) * a.HV + hv;
+            const int64_t t = it.t0 + lane, o = (it.b * a.L + t) * a.HV + hv;
             gn = t < a.L ? to_f32(((const T*)a.g)[o]) : 0.0f;
             bn = t < a.L ? to_f32(((const T*)a.beta)[o]) : 0.0f;
         }
     };
-    {
-        const int tid = threadIdx.x;
-        const Rows<T> rk((const T*)a.k + qk_base, t0, a.L, qk_step, Dk);
-        const Rows<T> rq((const T*)a.q + qk_base, t0, a.L, qk_step, Dk);
-        wtile::u4v kn[KU], qn[KU];
+    auto fetch_qk = [&](const Item& it) {
+        const int tid = wtile::fresh(threadIdx.x);
+        const Rows<T> rk((const T*)a.k + it.qk_base, it.t0, a.L, qk_step, Dk);
+        const Rows<T> rq((const T*)a.q + it.qk_base, it.t0, a.L, qk_step, Dk);
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
             const int u = tid + i * GT;
@@ -445,16 +463,18 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                 qn[i] = rq.template get16<VEC>(u / UR, u % UR * I::kUnit, Dk);
             }
         }
-        fetch(h * group, 0);
-#pragma unroll
-        for (int i = 0; i < KU; ++i) {
-            const int u = tid + i * GT, at = u / UR * L::kKS + u % UR * I::kUnit;
-            if (C * UR % GT == 0 || u < C * UR) {
-                *(wtile::u4v*)(sm.k + at) = kn[i];
-                *(wtile::u4v*)(sm.q + at) = qn[i];
-            }
-        }
-    }
+    };
+
+    const int64_t items = a.B * a.H * chunks;
+    Item next = item_at(blockIdx.x);
+    fetch_qk(next);
+    fetch(next, next.h * group, 0);
+    for (int64_t at = blockIdx.x; at < items; at += gridDim.x) {
+    const Item it = next;
+    const int64_t b = it.b, t0 = it.t0, qk_base = it.qk_base;
+    const int h = it.h;
+    const bool more = at + gridDim.x < items;
+    if (more) next = item_at(at + gridDim.x);
     for (int hv = h * group; hv < (h + 1) * group; ++hv) {
         // Side a: X1 = dO S^T, X2 = Y S^T; side b: X1 = U D^T (lane: column d, rows 16 w + 4 g
         // ..).  F, Z: side a has row i = 16 w + ll and columns j = 16 t + 4 g .., side b column
@@ -471,6 +491,16 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
             lds_barrier();  // the previous columns' operands, or head's decays, have been read
             if (wave == 4 && n0 == 0) gates_of_chunk(&sm.gt, gn, bn, a.scale, lane0);
             const int tid = wtile::fresh(threadIdx.x);
+            if (n0 == 0 && hv == h * group) {
+#pragma unroll
+                for (int i = 0; i < KU; ++i) {
+                    const int u = tid + i * GT, o = u / UR * L::kKS + u % UR * I::kUnit;
+                    if (C * UR % GT == 0 || u < C * UR) {
+                        *(wtile::u4v*)(sm.k + o) = kn[i];
+                        *(wtile::u4v*)(sm.q + o) = qn[i];
+                    }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < OU; ++i) {
                 const int u = tid + i * GT;
@@ -494,8 +524,17 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                 put<L::kOut>(sm.y, L::kYPlane, L::kNS, t, n, yn[i]);
             }
             lds_barrier();
-            if (n0 + NTW < Dv) fetch(hv, n0 + NTW);
-            else if (hv + 1 < (h + 1) * group) fetch(hv + 1, 0);
+            // The next operands' reads are started behind the first use of this one's V.
+            auto fetch_next = [&] {
+                if (n0 + NTW < Dv) {
+                    fetch(it, hv, n0 + NTW);
+                } else if (hv + 1 < (h + 1) * group) {
+                    fetch(it, hv + 1, 0);
+                } else if (more) {
+                    fetch_qk(next);
+                    fetch(next, next.h * group, 0);
+                }
+            };
 
             if (side_b) {
                 if (n0 == 0) {
@@ -527,16 +566,8 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                 }
             } else {
                 const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
-                const int64_t v_base = (b * a.L * a.HV + hv) * Dv + n0;
-                const Rows<T> rv((const T*)a.v + v_base, t0, a.L, v_step, width);
                 const f4 eg = *(const f4*)(sm.gt.eg + 16 * w + 4 * g);
                 const f4 bt = *(const f4*)(sm.gt.bt + 16 * w + 4 * g);
-                float v[NTL][4];
-#pragma unroll
-                for (int j = 0; j < NTL; ++j)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        v[j][r] = rv.get(rv.off(16 * w + 4 * g + r, 16 * j + ll, width));
                 f4 KS[NTL];
 #pragma unroll
                 for (int j = 0; j < NTL; ++j) KS[j] = f4{0, 0, 0, 0};
@@ -556,12 +587,13 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                     for (int r = 0; r < 4; ++r) {
                         const float y = whole(sm.y, L::kYPlane,
                                               (16 * w + 4 * g + r) * L::kNS + 16 * j + ll);
-                        yv[r] = fmaf(y, v[j][r], yv[r]);
-                        R[r] = bt[r] * (v[j][r] - eg[r] * KS[j][r]);
+                        yv[r] = fmaf(y, vn[j][r], yv[r]);
+                        R[r] = bt[r] * (vn[j][r] - eg[r] * KS[j][r]);
                     }
                     put<L::kOut>(sm.r, L::kRPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, R);
                 }
             }
+            fetch_next();
             lds_barrier();
             if (n0 == 0) {
                 const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
@@ -771,6 +803,7 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
             }
         }
     }
+    }
 }
 
 // ------------------------------------------------------------------ launches
@@ -797,8 +830,12 @@ hipError_t launch_grad(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t strea
     const hipError_t e =
         allow_dynamic_lds((const void*)delta_bwd_grad_kernel<T, DK, VEC>, bytes, lds_set);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((delta_bwd_grad_kernel<T, DK, VEC>), dim3((unsigned)(a.B * a.H * chunks)),
-                       dim3(GT), bytes, stream, a, ws);
+    // As many workgroups as the chip holds; each takes chunks until there are no more, with the
+    // next one's reads on their way.
+    const int64_t items = a.B * a.H * chunks, fit = 256 * (160 * 1024 / bytes);
+    hipLaunchKernelGGL((delta_bwd_grad_kernel<T, DK, VEC>),
+                       dim3((unsigned)(items < fit ? items : fit)), dim3(GT), bytes, stream, a,
+                       ws);
     return hipGetLastError();
 }
 
