@@ -29,6 +29,7 @@ struct BwdWs {
     float* Y;   // [B * HV][L][Dv]
     float* dq;  // [B][L][H][Dk] each: sums over value heads so far, where they share a query head
     float* dk;
+    void* split;  // the workspace of delta_split.hip
 };
 
 // ------------------------------------------------------------------ the recurrence
@@ -841,8 +842,11 @@ hipError_t launch_grad(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t strea
 
 template <typename T, int DK>
 hipError_t launch_both(const DeltaBwdArgs& a, const BwdWs& ws, bool vec, hipStream_t stream) {
-    const hipError_t e = vec ? launch_state<T, DK, 32, true>(a, ws, stream)
-                             : launch_state<T, DK, 32, false>(a, ws, stream);
+    size_t bytes;
+    const hipError_t e = delta_split(a.B * a.HV, a.L, a.Dv)
+                             ? launch_delta_split_backward(a, ws.D, ws.Y, ws.split, &bytes, stream)
+                         : vec ? launch_state<T, DK, 32, true>(a, ws, stream)
+                               : launch_state<T, DK, 32, false>(a, ws, stream);
     if (e != hipSuccess) return e;
     return vec ? launch_grad<T, DK, true>(a, ws, stream) : launch_grad<T, DK, false>(a, ws, stream);
 }
@@ -872,18 +876,38 @@ size_t sum_bytes(int64_t B, int64_t L, int64_t H, int Dk) {
 }  // namespace
 
 size_t delta_backward_workspace(int64_t B, int64_t L, int64_t H, int64_t HV, int Dk, int Dv,
-                                IoType) {
+                                IoType io) {
+    size_t split = 0;
+    if (delta_split(B * HV, L, Dv)) {
+        DeltaBwdArgs a{};
+        a.B = B;
+        a.L = L;
+        a.H = (int)H;
+        a.HV = (int)HV;
+        a.Dk = Dk;
+        a.Dv = Dv;
+        a.io = io;
+        (void)launch_delta_split_backward(a, nullptr, nullptr, nullptr, &split, nullptr);
+    }
     return state_bytes(B, L, HV, Dk, Dv) + y_bytes(B, L, HV, Dv) +
-           (HV > H ? 2 * sum_bytes(B, L, H, Dk) : 0);
+           (HV > H ? 2 * sum_bytes(B, L, H, Dk) : 0) + split;
 }
 
 hipError_t launch_delta_backward(const DeltaBwdArgs& a, void* ws, hipStream_t stream) {
     char* p = (char*)ws;
-    BwdWs s{(float*)p, (float*)(p + state_bytes(a.B, a.L, a.HV, a.Dk, a.Dv)), nullptr, nullptr};
+    auto take = [&](size_t n) {
+        char* r = p;
+        p += n;
+        return r;
+    };
+    BwdWs s{};
+    s.D = (float*)take(state_bytes(a.B, a.L, a.HV, a.Dk, a.Dv));
+    s.Y = (float*)take(y_bytes(a.B, a.L, a.HV, a.Dv));
     if (a.HV > a.H) {
-        s.dq = (float*)((char*)s.Y + y_bytes(a.B, a.L, a.HV, a.Dv));
-        s.dk = (float*)((char*)s.dq + sum_bytes(a.B, a.L, a.H, a.Dk));
+        s.dq = (float*)take(sum_bytes(a.B, a.L, a.H, a.Dk));
+        s.dk = (float*)take(sum_bytes(a.B, a.L, a.H, a.Dk));
     }
+    s.split = p;
     return a.io == IoType::kF32 ? launch_typed<float>(a, s, stream)
                                 : launch_typed<bf16>(a, s, stream);
 }

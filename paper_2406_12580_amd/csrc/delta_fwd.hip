@@ -318,9 +318,23 @@ hipError_t launch_typed(const DeltaFwdArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t delta_forward_workspace(int64_t, int64_t, int64_t, int, int, IoType) { return 0; }
+size_t delta_forward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv, IoType io) {
+    if (!delta_split(B * HV, L, Dv)) return 0;
+    DeltaFwdArgs a{};
+    a.B = B;
+    a.L = L;
+    a.H = a.HV = (int)HV;
+    a.Dk = Dk;
+    a.Dv = Dv;
+    a.io = io;
+    size_t bytes = 0;
+    (void)launch_delta_split_forward(a, nullptr, &bytes, nullptr);
+    return bytes;
+}
 
-hipError_t launch_delta_forward(const DeltaFwdArgs& a, void*, hipStream_t stream) {
+hipError_t launch_delta_forward(const DeltaFwdArgs& a, void* ws, hipStream_t stream) {
+    size_t bytes;
+    if (delta_split(a.B * a.HV, a.L, a.Dv)) return launch_delta_split_forward(a, ws, &bytes, stream);
     return a.io == IoType::kF32 ? launch_typed<float>(a, stream) : launch_typed<bf16>(a, stream);
 }
 

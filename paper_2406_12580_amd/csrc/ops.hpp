@@ -99,6 +99,14 @@ hipError_t launch_delta_step(const DeltaStepArgs& a, hipStream_t stream);
 // and the running sums of g stay finite, where differences of them are taken.
 constexpr float kDeltaMinG = -100.0f;
 
+// The way of delta_split.hip, where it is the faster one: the forward, and the backward's
+// recurrence into D and Y.  With ws null these write the workspace's size to *bytes only.
+bool delta_split(int64_t heads, int64_t L, int Dv);
+hipError_t launch_delta_split_forward(const DeltaFwdArgs& a, void* ws, size_t* bytes,
+                                      hipStream_t stream);
+hipError_t launch_delta_split_backward(const DeltaBwdArgs& a, float* D, float* Y, void* ws,
+                                       size_t* bytes, hipStream_t stream);
+
 #ifdef __HIPCC__
 __device__ __forceinline__ float delta_clamp_g(float g) { return g < kDeltaMinG ? kDeltaMinG : g; }
 __device__ __forceinline__ float delta_decay(float g) { return expf(delta_clamp_g(g)); }
