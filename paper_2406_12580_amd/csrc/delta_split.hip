@@ -43,6 +43,7 @@ struct SplitWs {
     float* Z;    // [item][strip][d tile][lane][4], backward only
     float* f;    // [item][64]
     float* et;   // [item]
+    float* bt;   // [item][64], backward only
     float* X;    // [head][L][Dv]
     float* S;    // [item][Dk][Dv]
 };
@@ -223,6 +224,7 @@ __global__ __launch_bounds__(NT) void delta_prep_kernel(SplitArgs a, SplitWs ws)
         // What a step's row of W is made of, in place of es, and the walk's f.
         const float eg = sm.gt.eg[lane0], el = sm.gt.el[lane0], bt = sm.gt.bt[lane0];
         ws.f[p.item * C + lane0] = BWD ? -bt * eg : el;
+        if (BWD) ws.bt[p.item * C + lane0] = bt;
         if (lane0 == 0) ws.et[p.item] = sm.gt.eg[C - 1];
         if (!BWD) sm.gt.es[lane0] = bt * eg;
     }
@@ -337,13 +339,12 @@ struct WalkArgs {
     float* s_end;       // may be null
     float* S;           // the state before each chunk (behind it, backwards)
     void* dv;           // backward: dV = beta Y
-    const void* beta;
     int64_t L;
     int HV, Dk, Dv, chunks, strips;
 };
 
 template <typename T, int DK, bool BWD>
-__global__ __launch_bounds__(NT, 1) void delta_walk_kernel(WalkArgs a, SplitWs ws) {
+__global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs ws) {
     using I = Io<T>;
     using E = typename I::Elem;
     constexpr int P = I::kChain, NK = DK / I::kStep, NC = C / I::kStep, DTL = DK / 16;
@@ -352,7 +353,7 @@ __global__ __launch_bounds__(NT, 1) void delta_walk_kernel(WalkArgs a, SplitWs w
     constexpr int kSPlane = SC * kKS, kXPlane = SC * kUS;
     __shared__ __attribute__((aligned(16))) E sS[P * kSPlane];
     __shared__ __attribute__((aligned(16))) E sX[P * kXPlane];
-    const int lane0 = threadIdx.x % kWave, w = wave_id();
+    const int lane = threadIdx.x % kWave, ll = lane & 15, g = lane >> 4, w = wave_id();
     const unsigned head = blockIdx.x / (unsigned)a.strips;
     const int strip = (int)(blockIdx.x - head * (unsigned)a.strips);
     const int n0 = strip * SC, width = a.Dv - n0;
@@ -366,7 +367,6 @@ __global__ __launch_bounds__(NT, 1) void delta_walk_kernel(WalkArgs a, SplitWs w
         float et;
     };
     auto fetch = [&](In& in, int c) {
-        const int lane = wtile::fresh(lane0);
         const int64_t item = (int64_t)head * a.chunks + c;
         const char* W = ws.W + item * kWBytes<T, DK> + (w * NK * P) * Frag<T>::kBytes + lane * 16;
         const char* KT = ws.KT + item * kKBytes<T, DK> + lane * 16;
@@ -399,18 +399,11 @@ __global__ __launch_bounds__(NT, 1) void delta_walk_kernel(WalkArgs a, SplitWs w
                                                    lane) * 4);
             }
         }
-        if constexpr (BWD) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int64_t t = (int64_t)c * C + 16 * w + 4 * (lane >> 4) + r;
-                in.bt[r] = t < a.L ? to_f32(((const T*)a.beta)[(b * a.L + t) * a.HV + hv]) : 0.0f;
-            }
-        }
+        if constexpr (BWD) in.bt = *(const f4*)(ws.bt + item * C + 16 * w + 4 * g);
     };
 
     f4 S[SD];
     auto state_io = [&](const float* p, auto f) {
-        const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
         const auto r = wtile::rsrc(p, (uint32_t)(a.Dk * a.Dv * 4));
         if (has_d) {
 #pragma unroll
@@ -430,7 +423,6 @@ __global__ __launch_bounds__(NT, 1) void delta_walk_kernel(WalkArgs a, SplitWs w
         });
     };
     auto state_put = [&] {
-        const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
         if (has_d) {
 #pragma unroll
             for (int i = 0; i < SD; ++i)
@@ -440,7 +432,6 @@ __global__ __launch_bounds__(NT, 1) void delta_walk_kernel(WalkArgs a, SplitWs w
     const int64_t state = (int64_t)a.Dk * a.Dv;
     auto chunk_at = [&](int i) { return BWD ? a.chunks - 1 - i : i; };
     auto step = [&](In& in, int c) {
-        const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
         f4 x[2] = {in.x0, {0, 0, 0, 0}};
 #pragma unroll
         for (int s = 0; s < NK; ++s)
@@ -478,23 +469,25 @@ __global__ __launch_bounds__(NT, 1) void delta_walk_kernel(WalkArgs a, SplitWs w
 
 #pragma unroll
     for (int i = 0; i < SD; ++i) S[i] = f4{0, 0, 0, 0};
+    // Two chunks' operands are on their way.  Reads behind the last chunk are of that one again:
+    // a read under a condition would have every wait reckon with the branch that has none.
+    const int last = a.chunks - 1;
     In one, two;
     fetch(one, chunk_at(0));
-    if (a.chunks > 1) fetch(two, chunk_at(1));
+    fetch(two, chunk_at(last < 1 ? last : 1));
     if (a.s0)
         state_io(a.s0 + head * state, [](auto r, f4& s, int e, int o) {
             s[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0));
         });
     state_put();
     lds_barrier();
-    for (int i = 0; i < a.chunks; i += 2) {
+    for (int i = 0; i < last; i += 2) {
         step(one, chunk_at(i));
-        if (i + 2 < a.chunks) fetch(one, chunk_at(i + 2));
-        if (i + 1 < a.chunks) {
-            step(two, chunk_at(i + 1));
-            if (i + 3 < a.chunks) fetch(two, chunk_at(i + 3));
-        }
+        fetch(one, chunk_at(i + 2 < last ? i + 2 : last));
+        step(two, chunk_at(i + 1));
+        fetch(two, chunk_at(i + 3 < last ? i + 3 : last));
     }
+    if (a.chunks & 1) step(one, chunk_at(last));
     if (a.s_end) state_store(a.s_end + head * state);
 }
 
@@ -633,6 +626,7 @@ SplitWs layout(char* p, int64_t heads, int64_t L, int64_t chunks, int Dk, int Dv
     if (bwd) ws.Z = (float*)take(items * strips * (DK / 16) * kWave * 16);
     ws.f = (float*)take(items * C * 4);
     ws.et = (float*)take(items * 4);
+    if (bwd) ws.bt = (float*)take(items * C * 4);
     if (own_x) ws.X = (float*)take((size_t)(heads * L * Dv) * 4);
     if (own_s) ws.S = (float*)take(items * Dk * Dv * 4);
     *bytes = at;
@@ -678,7 +672,7 @@ hipError_t forward(const DeltaFwdArgs& a, void* p, size_t* bytes, hipStream_t st
     hipError_t e = vec ? launch_prep<T, DK, false, true>(s, ws, stream)
                        : launch_prep<T, DK, false, false>(s, ws, stream);
     if (e != hipSuccess) return e;
-    e = launch_walk<T, DK, false>(WalkArgs{a.h0, a.hT, ws.S, nullptr, a.beta, a.L, a.HV, a.Dk, a.Dv,
+    e = launch_walk<T, DK, false>(WalkArgs{a.h0, a.hT, ws.S, nullptr, a.L, a.HV, a.Dk, a.Dv,
                                            (int)chunks, strips},
                                   heads, ws, stream);
     if (e != hipSuccess) return e;
@@ -716,7 +710,7 @@ hipError_t backward(const DeltaBwdArgs& a, float* D, float* Y, void* p, size_t* 
     const hipError_t e = vec ? launch_prep<T, DK, true, true>(s, ws, stream)
                              : launch_prep<T, DK, true, false>(s, ws, stream);
     if (e != hipSuccess) return e;
-    return launch_walk<T, DK, true>(WalkArgs{a.dhT, a.dh0, ws.S, a.dv, a.beta, a.L, a.HV, a.Dk,
+    return launch_walk<T, DK, true>(WalkArgs{a.dhT, a.dh0, ws.S, a.dv, a.L, a.HV, a.Dk,
                                              a.Dv, (int)chunks, strips},
                                     heads, ws, stream);
 }
