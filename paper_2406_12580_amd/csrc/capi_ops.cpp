@@ -119,6 +119,7 @@ static int sample_sizes(int64_t B, int64_t V, int io) {
     if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
     if (B < 0 || V < 0) return RECBLR_ERR_INVALID_ARGUMENT;
     if (B > 0x7FFFFFFF || V > ((int64_t)1 << 24)) return RECBLR_ERR_UNSUPPORTED;
+    if (B * ((V + 4095) / 4096) > 0x7FFFFFFF) return RECBLR_ERR_UNSUPPORTED;  // a workgroup each
     return RECBLR_OK;
 }
 

@@ -1,15 +1,22 @@
 // One item a row from logits (recblr_sample): temperature, top-k, top-p, min-p.
 //
 // The items that stay are a run of the order (logit falling, index rising), so a row's
-// selection is one border: a key, and how many of the items with that very key stay.  The
-// border is found by descending the key's 32 bits, 11, 11 and 10 at a time, over a histogram
-// in LDS of counts (top-k) or of weights (top-p); nothing is sorted.  Weights are
-// w = exp((l - max) / temperature) in 64 bits, summed as integers q = round(w 2^F): such sums
-// are exact in any order, so atomics repeat bit for bit and a border falls where 64-bit
-// arithmetic puts it.
+// selection is one border: a key, and how many of the items with that very key stay; nothing
+// is sorted.  Weights w = exp((l - max) / temperature) are formed in 64 bits and summed as
+// integers q = round(w 2^F): such sums are exact in any order, so atomics repeat bit for bit
+// and a border falls where 64-bit arithmetic puts it.  Items with q = 0 can neither be chosen
+// nor move a border that matters; they take no part.
 //
-// One workgroup takes one row.  Waves own consecutive spans of the row, so running sums in
-// order of the index are a wave's sum, then a lane's.
+// The border is found on a histogram of counts and weights over kBins equal steps of the logit
+// (uniform steps spread the items of usual logits evenly; the bits of a float do not: its
+// upper eleven put half of a row in twenty bins, whose atomics then wait for each other).  The
+// bin that holds the border is searched further by its keys' own bits, 8 at a time, until one
+// key is left; equal keys (frequent in bf16) are one key from the start.
+//
+// A row of up to kSpan items is one workgroup's, keys and weights in its registers from a
+// single read.  A longer one takes a workgroup for each span of kSpan items and six short
+// launches: extremes, histogram, the items of the bins that can hold a border, the border
+// itself (on those items alone), sums of the spans, and the choice within one span.
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"
@@ -18,7 +25,14 @@
 namespace recblr {
 namespace {
 
-constexpr int kBins = 2048;
+constexpr int kNT = 256;
+constexpr int kNW = kNT / kWave;
+constexpr int kIT = 4;                 // groups of four items to a lane
+constexpr int kItems = 4 * kIT;
+constexpr int kSpan = kNT * kItems;    // items of a workgroup
+constexpr int kBins = 1024;
+constexpr int kBPT = kBins / kNT;
+constexpr int kFine = 256;             // bins of the further searches
 
 // Order-preserving bits of a float: equal floats (the two zeros among them) have equal keys.
 __device__ __forceinline__ uint32_t key_of(float v) {
@@ -29,7 +43,7 @@ __device__ __forceinline__ float value_of(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
 constexpr uint32_t kKeyNegInf = 0x007FFFFFu;  // key_of(-inf); a NaN's key lies outside
-constexpr uint32_t kKeyPosInf = 0xFF800000u;  // [key_of(-inf), key_of(+inf)]
+constexpr uint32_t kKeyPosInf = 0xFF800000u;  // [key_of(-inf), key_of(+inf)]; 0 is no item's
 
 template <typename V>
 __device__ __forceinline__ V wave_sum(V v) {
@@ -49,108 +63,554 @@ __device__ __forceinline__ V wave_before(V v, int lane) {
     return s - v;
 }
 
-struct RowParams {
-    double inv_t;   // 1 / temperature
-    double max;     // largest logit
-    double scale;   // 2^F
-};
-// The weight of a key, as the integer that is summed.
-__device__ __forceinline__ double weight(uint32_t key, const RowParams& r) {
-    const double x = ((double)value_of(key) - r.max) * r.inv_t;
-    return key > kKeyNegInf && x > -45.0 ? exp(x) : 0.0;  // below e^-45 < 2^-63: rounds to 0
-}
-__device__ __forceinline__ uint64_t fixed(double w, const RowParams& r) {
-    return (uint64_t)(w * r.scale + 0.5);
+typedef unsigned long long u64;
+
+// e^x for x in (-45, 0]: x = n ln 2 + t with |t| <= ln 2 / 2, and e^t by its Taylor polynomial
+// of degree 12, whose remainder is below 2e-16 of it.
+__device__ __forceinline__ double exp_neg(double x) {
+    const double n = __builtin_rint(x * 1.4426950408889634074);
+    // ln 2 as its nearest double and what that leaves.
+    double t = __builtin_fma(n, -0.69314718055994530942, x);
+    t = __builtin_fma(n, -2.3190468138462996e-17, t);
+    double p = 1.0 / 479001600.0;
+    p = __builtin_fma(p, t, 1.0 / 39916800.0);
+    p = __builtin_fma(p, t, 1.0 / 3628800.0);
+    p = __builtin_fma(p, t, 1.0 / 362880.0);
+    p = __builtin_fma(p, t, 1.0 / 40320.0);
+    p = __builtin_fma(p, t, 1.0 / 5040.0);
+    p = __builtin_fma(p, t, 1.0 / 720.0);
+    p = __builtin_fma(p, t, 1.0 / 120.0);
+    p = __builtin_fma(p, t, 1.0 / 24.0);
+    p = __builtin_fma(p, t, 1.0 / 6.0);
+    p = __builtin_fma(p, t, 0.5);
+    p = __builtin_fma(p, t, 1.0);
+    p = __builtin_fma(p, t, 1.0);
+    return __builtin_amdgcn_ldexp(p, (int)n);
 }
 
-template <int NT>
+// What a row asks for, and the measures that its extremes give.
+struct Row {
+    double inv_t, max, scale;
+    float top, bins;     // largest logit; bins to a unit of the logit
+    float top_p, min_p;
+    int64_t k;
+    bool bad, greedy;
+    uint32_t hi;
+
+    // Of a row whose largest and smallest keys are hi and lo.
+    __device__ __forceinline__ Row(const SampleArgs& a, int64_t row, uint32_t hi_, uint32_t lo,
+                                   double scale_) {
+        hi = hi_;
+        scale = scale_;
+        const float temp = a.temperature ? a.temperature[row] : 1.0f;
+        bad = hi <= kKeyNegInf || hi >= kKeyPosInf || lo < kKeyNegInf || !(temp == temp);
+        top_p = a.top_p ? a.top_p[row] : 1.0f;
+        min_p = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.0f;
+        greedy = temp <= 0.0f;
+        k = a.top_k && a.top_k[row] > 0 ? a.top_k[row] : a.V;
+        if (greedy || top_p <= 0.0f) k = 1;
+        inv_t = greedy ? 0.0 : 1.0 / (double)temp;
+        top = value_of(hi);
+        max = (double)top;
+        // Items further down than 45 temperatures weigh nothing.
+        const float range = fminf(45.0f * temp, top - value_of(lo < kKeyNegInf ? hi : lo));
+        bins = range > 0.0f && range < 3e38f ? (float)(kBins - 1) / range : 0.0f;
+    }
+    __device__ __forceinline__ double weight(uint32_t key) const {
+        const double x = ((double)value_of(key) - max) * inv_t;
+        return key > kKeyNegInf && x > -45.0 ? exp_neg(x) : 0.0;  // e^-45 < 2^-63 rounds to 0
+    }
+    __device__ __forceinline__ u64 fixed(uint32_t key) const {
+        return (u64)(weight(key) * scale + 0.5);
+    }
+    // Rising as the logit falls: both roundings keep the order.
+    __device__ __forceinline__ int bin(uint32_t key) const {
+        const float b = (top - value_of(key)) * bins;
+        return b < (float)(kBins - 1) ? (int)b : kBins - 1;
+    }
+    // Whether a border has to be looked for.
+    __device__ __forceinline__ bool cuts(int64_t V) const { return k < V || top_p < 1.0f; }
+};
+
+struct Border {
+    uint32_t key;   // items above it stay,
+    uint32_t ties;  // and the first `ties` of those that have it
+};
+
 struct Shared {
     uint32_t cnt[kBins];
-    unsigned long long mass[kBins];
-    uint32_t wave32[2][NT / kWave];
-    unsigned long long wave64[NT / kWave];
-    int bin;
-    uint32_t above32;
-    unsigned long long above64, at64;
-    uint32_t at32;
+    u64 mass[kBins];
+    uint32_t fine_cnt[kFine];
+    u64 fine_mass[kFine];
+    uint32_t w32[2][kNW];
+    u64 w64[kNW];
+    uint32_t lo, hi;
+    int at;             // bin found
+    uint32_t at_cnt, above_cnt;
+    u64 above_mass, at_mass;
 };
 
-// A row's keys, IT groups of four to a lane: kept in registers, or read again each time.
-template <typename T, int NT, int IT, bool KEEP>
-struct Row {
-    const T* p;
-    int64_t V;
-    int64_t span0;   // first element of the wave's span
-    int groups;      // groups of 256 elements in a span
-    bool vec;
-    uint32_t kept[KEEP ? IT * 4 : 1];
-
-    __device__ __forceinline__ int64_t index(int it, int lane) const {
-        return span0 + (int64_t)it * 256 + lane * 4;
+// Workgroup sums of a count and a weight over lower threads.
+__device__ __forceinline__ void block_before(Shared& sm, uint32_t& c, u64& m, int lane, int w) {
+    const uint32_t c0 = c;
+    const u64 m0 = m;
+    c = wave_before(c, lane);
+    m = wave_before(m, lane);
+    if (lane == kWave - 1) {
+        sm.w32[0][w] = c + c0;
+        sm.w64[w] = m + m0;
     }
-    __device__ __forceinline__ void read(int it, int lane, uint32_t (&k)[4]) const {
-        const int64_t i = index(it, lane);
-        if (vec && i + 4 <= V) {
-            float v[4];
-            unpack_vec<T, 4>(*(const typename VecT<T, 4>::type*)(p + i), v);
+    __syncthreads();
+    for (int i = 0; i < w; ++i) {
+        c += sm.w32[0][i];
+        m += sm.w64[i];
+    }
+}
+
+// The last bin that holds items and has less than is wanted before it: fewer than want_cnt
+// items, or a weight below want_mass.  `cnt`, `mass`: N bins in LDS, N / kNT of them to a
+// thread in order, with c and m before the thread's first (whole arrays, base included).
+template <int N>
+__device__ __forceinline__ void pick(Shared& sm, const uint32_t* cnt, const u64* mass, uint32_t c,
+                                     u64 m, bool by_mass, uint64_t want_cnt, double want_mass,
+                                     int tid) {
+    constexpr int BPT = N / kNT;
+    if (tid == 0) sm.at = -1;
+    __syncthreads();
+    int mine = -1;
+    uint32_t c_at = 0;
+    u64 m_at = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) k[e] = key_of(v[e]);
+    for (int j = 0; j < BPT; ++j) {
+        const int b = tid * BPT + j;
+        const uint32_t n = cnt[b];
+        if (n && (by_mass ? (double)m < want_mass : c < want_cnt)) {
+            mine = b;
+            c_at = c;
+            m_at = m;
+        }
+        c += n;
+        m += mass[b];
+    }
+    if (mine >= 0) atomicMax(&sm.at, mine);
+    __syncthreads();
+    if (mine >= 0 && sm.at == mine) {
+        sm.above_cnt = c_at;
+        sm.above_mass = m_at;
+        sm.at_cnt = cnt[mine];
+        sm.at_mass = mass[mine];
+    }
+    __syncthreads();
+}
+
+// How many of `ties` items of weight q stay when `before` lies above them and less than `want`
+// may lie before one that stays.
+__device__ __forceinline__ uint32_t ties_within(uint32_t ties, u64 q, u64 before, double want) {
+    if (q == 0) return ties;
+    const double guess = ceil((want - (double)before) / (double)q);
+    int64_t n = guess < 1.0 ? 1 : guess > (double)ties ? (int64_t)ties : (int64_t)guess;
+    while (n > 1 && !((double)(before + q * (u64)(n - 1)) < want)) --n;
+    while (n < (int64_t)ties && (double)(before + q * (u64)n) < want) ++n;
+    return (uint32_t)n;
+}
+
+// Searches one bin further.  each(f) calls f(key, q) for the items that may be of it, member()
+// tells which are; `above` of sm is what lies before the bin and is brought to what lies before
+// the key found, which has sm.at_cnt items.
+template <typename Each, typename Member>
+__device__ __forceinline__ uint32_t refine(Shared& sm, const Row& row, Each each, Member member,
+                                           bool by_mass, uint64_t want_cnt, double want_mass,
+                                           int tid, int lane, int w) {
+    uint32_t from = 0, to = 0xFFFFFFFFu;
+    uint32_t base_c = sm.above_cnt;
+    u64 base_m = sm.above_mass;
+    // Each search leaves at most a 128th of the keys' range: five come down to one key.
+    for (int depth = 0; depth < 8; ++depth) {
+        __syncthreads();
+        if (tid == 0) {
+            sm.lo = 0xFFFFFFFFu;
+            sm.hi = 0;
+        }
+        for (int b = tid; b < kFine; b += kNT) {
+            sm.fine_cnt[b] = 0;
+            sm.fine_mass[b] = 0;
+        }
+        __syncthreads();
+        uint32_t lo = 0xFFFFFFFFu, hi = 0;
+        each([&](uint32_t key, u64) {
+            if (key >= from && key <= to && member(key)) {
+                lo = key < lo ? key : lo;
+                hi = key > hi ? key : hi;
+            }
+        });
+        if (lo <= hi) {
+            atomicMin(&sm.lo, lo);
+            atomicMax(&sm.hi, hi);
+        }
+        __syncthreads();
+        lo = sm.lo;
+        hi = sm.hi;
+        if (lo > hi) break;
+        const int bits = 32 - __clz((int)((hi - lo) | 1u));
+        const int shift = bits > 8 ? bits - 8 : 0;
+        each([&](uint32_t key, u64 q) {
+            if (key >= lo && key <= hi && member(key)) {
+                const uint32_t b = (hi - key) >> shift;
+                atomicAdd(&sm.fine_cnt[b], 1u);
+                if (q) atomicAdd(&sm.fine_mass[b], q);
+            }
+        });
+        __syncthreads();
+        uint32_t c = sm.fine_cnt[tid];
+        u64 m = sm.fine_mass[tid];
+        block_before(sm, c, m, lane, w);
+        pick<kFine>(sm, sm.fine_cnt, sm.fine_mass, c + base_c, m + base_m, by_mass, want_cnt,
+                    want_mass, tid);
+        if (sm.at < 0) break;
+        const uint32_t b = (uint32_t)sm.at;
+        base_c = sm.above_cnt;
+        base_m = sm.above_mass;
+        to = hi - (b << shift);
+        from = to - ((1u << shift) - 1) < lo || to < ((1u << shift) - 1) ? lo
+                                                                         : to - ((1u << shift) - 1);
+        if (from == to) break;
+    }
+    return to;
+}
+
+// The row's border, from the whole histogram in sm (items with q > 0) and the items of the bins
+// that may hold it.  All threads return the same.
+template <typename Each>
+__device__ __forceinline__ Border find_border(Shared& sm, const Row& row, Each each, int tid,
+                                              int lane, int w) {
+    uint32_t c = 0;
+    u64 m = 0;
+#pragma unroll
+    for (int j = 0; j < kBPT; ++j) {
+        c += sm.cnt[tid * kBPT + j];
+        m += sm.mass[tid * kBPT + j];
+    }
+    const uint32_t c0 = c;
+    const u64 m0 = m;
+    block_before(sm, c, m, lane, w);
+    // Totals stand behind the last thread's bins.
+    if (tid == kNT - 1) {
+        sm.lo = c + c0;
+        sm.at_mass = m + m0;
+    }
+    __syncthreads();
+    const uint32_t total = sm.lo;
+    u64 above = sm.at_mass;
+    __syncthreads();
+    Border b{0, 0};
+    u64 tie_q = 0;
+    if (row.k < (int64_t)total) {
+        pick<kBins>(sm, sm.cnt, sm.mass, c, m, false, (uint64_t)row.k, 0.0, tid);
+        const int bin = sm.at;
+        b.key = refine(sm, row, each, [&](uint32_t key) { return row.bin(key) == bin; }, false,
+                       (uint64_t)row.k, 0.0, tid, lane, w);
+        b.ties = (uint32_t)(row.k - sm.above_cnt);
+        above = sm.above_mass;
+        tie_q = row.fixed(b.key);
+    }
+    if (row.top_p < 1.0f && row.k > 1) {
+        const double want = (double)row.top_p * (double)(above + tie_q * (u64)b.ties);
+        if ((double)above < want) {
+            if (b.ties) b.ties = ties_within(b.ties, tie_q, above, want);
         } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) k[e] = i + e < V ? key_of(to_f32(p[i + e])) : 0u;
+            const uint32_t edge = b.key;
+            pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, want, tid);
+            const int bin = sm.at;
+            b.key = refine(sm, row, each,
+                           [&](uint32_t key) { return key > edge && row.bin(key) == bin; }, true,
+                           0, want, tid, lane, w);
+            b.ties = ties_within(sm.at_cnt, row.fixed(b.key), sm.above_mass, want);
         }
     }
-    // f(keys of four consecutive elements, group) over the wave's span; 0 stands behind the row.
-    template <typename F>
-    __device__ __forceinline__ void each(int lane, F f) const {
-        if constexpr (KEEP) {
+    return b;
+}
+
+// A span of a row: its keys in order, a wave's 1024 after another's, groups of four to a lane.
+template <typename T>
+struct Span {
+    uint32_t key[kItems];
+    __device__ __forceinline__ static int64_t index(int64_t base, int w, int it, int lane) {
+        return base + (w * kIT + it) * 256 + lane * 4;
+    }
+    __device__ __forceinline__ Span(const T* p, int64_t V, int64_t base, int w, int lane) {
+        const bool vec = ((uintptr_t)p) % (4 * sizeof(T)) == 0;
 #pragma unroll
-            for (int it = 0; it < IT; ++it) {
-                const uint32_t k[4] = {kept[4 * it], kept[4 * it + 1], kept[4 * it + 2],
-                                       kept[4 * it + 3]};
-                f(k, it);
+        for (int it = 0; it < kIT; ++it) {
+            const int64_t i = index(base, w, it, lane);
+            if (vec && i + 4 <= V) {
+                float v[4];
+                unpack_vec<T, 4>(*(const typename VecT<T, 4>::type*)(p + i), v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) key[4 * it + e] = key_of(v[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    key[4 * it + e] = i + e < V ? key_of(to_f32(p[i + e])) : 0u;
             }
-        } else {
-            for (int it = 0; it < groups; ++it) {
-                uint32_t k[4];
-                read(it, lane, k);
-                f(k, it);
+        }
+    }
+    // Largest and smallest key over the workgroup's items, by all threads; w32 of LDS.
+    __device__ __forceinline__ void extremes(uint32_t (&w32)[2][kNW], int64_t V, int64_t base,
+                                             int w, int lane, uint32_t& hi, uint32_t& lo) const {
+        hi = 0;
+        lo = 0xFFFFFFFFu;
+#pragma unroll
+        for (int it = 0; it < kIT; ++it)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = index(base, w, it, lane) + e < V;
+                const uint32_t k = key[4 * it + e];
+                hi = in && k > hi ? k : hi;
+                lo = in && k < lo ? k : lo;
             }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            const uint32_t h = (uint32_t)__shfl_xor((int)hi, d), l = (uint32_t)__shfl_xor((int)lo, d);
+            hi = h > hi ? h : hi;
+            lo = l < lo ? l : lo;
+        }
+        if (lane == 0) {
+            w32[0][w] = hi;
+            w32[1][w] = lo;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kNW; ++i) {
+            hi = w32[0][i] > hi ? w32[0][i] : hi;
+            lo = w32[1][i] < lo ? w32[1][i] : lo;
         }
     }
 };
 
-template <typename T, int NT, int IT, bool KEEP>
-__global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a, double scale) {
-    __shared__ Shared<NT> sm;
-    constexpr int NW = NT / kWave;
-    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
-    const int64_t row = blockIdx.x;
-    Row<T, NT, IT, KEEP> r;
-    r.p = (const T*)a.logits + row * a.V;
-    r.V = a.V;
-    r.vec = (((uintptr_t)r.p) % (4 * sizeof(T))) == 0;
-    r.groups = KEEP ? IT : (int)((a.V + NW * 256 - 1) / (NW * 256));
-    r.span0 = (int64_t)w * r.groups * 256;
-    if constexpr (KEEP) {
+// The choice within a span whose first item has `before` items of the border's key and a sum of
+// `run0` before it.  q of items that stay is left, others' become 0.
+template <typename T>
+__device__ __forceinline__ void keep(const Span<T>& sp, const Row& row, const Border& b,
+                                     uint64_t before, u64 (&q)[kItems], int lane) {
 #pragma unroll
-        for (int it = 0; it < IT; ++it) {
-            uint32_t k[4];
-            r.read(it, lane, k);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r.kept[4 * it + e] = k[e];
-        }
-    }
-    // Largest and smallest key of the row.
-    uint32_t hi = 0, lo = 0xFFFFFFFFu;
-    r.each(lane, [&](const uint32_t (&k)[4], int it) {
+    for (int it = 0; it < kIT; ++it) {
+        uint32_t tie[4], n = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const bool in = r.index(it, lane) + e < a.V;
-            hi = in && k[e] > hi ? k[e] : hi;
-            lo = in && k[e] < lo ? k[e] : lo;
+            tie[e] = sp.key[4 * it + e] == b.key && b.key != 0;
+            n += tie[e];
         }
-    });
+        uint64_t mine = 0;
+        if (__any((int)n)) {
+            const uint32_t lower = wave_before(n, lane);
+            mine = before + lower;
+            before += (uint32_t)__shfl((int)(lower + n), kWave - 1);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (!(sp.key[4 * it + e] > b.key || (tie[e] && mine < b.ties))) q[4 * it + e] = 0;
+            mine += tie[e];
+        }
+    }
+}
+
+// A wave's items of the border's key.
+template <typename T>
+__device__ __forceinline__ uint32_t wave_ties(const Span<T>& sp, const Border& b) {
+    uint32_t n = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) n += sp.key[i] == b.key && b.key != 0;
+    return wave_sum(n);
+}
+
+// The weights of a row's items: min-p's are 0 as well (in a greedy row all weigh the same).
+__device__ __forceinline__ u64 weight_of(const Row& row, uint32_t key) {
+    if (row.greedy) return key > kKeyNegInf ? (u64)row.scale : 0;
+    const double wt = row.weight(key);
+    return wt < (double)row.min_p ? 0 : (u64)(wt * row.scale + 0.5);
+}
+
+// The item at which the running sum, `run0` before the wave's first item, first exceeds target,
+// else the wave's last one with weight; written by the lane that has it.
+template <typename T>
+__device__ __forceinline__ void choose(const SampleArgs& a, const Span<T>& sp, const Row& row,
+                                       const u64 (&q)[kItems], int64_t r, int64_t base, u64 run,
+                                       double target, u64 all, int w, int lane) {
+    int64_t found = -1, tail = -1;
+    uint32_t key_f = 0, key_t = 0;
+#pragma unroll
+    for (int it = 0; it < kIT; ++it) {
+        const u64 own = q[4 * it] + q[4 * it + 1] + q[4 * it + 2] + q[4 * it + 3];
+        u64 c = run + wave_before(own, lane);
+        run += wave_sum(own);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            c += q[4 * it + e];
+            if (q[4 * it + e]) {
+                tail = Span<T>::index(base, w, it, lane) + e;
+                key_t = sp.key[4 * it + e];
+                if (found < 0 && (double)c > target) {
+                    found = tail;
+                    key_f = key_t;
+                }
+            }
+        }
+    }
+    u64 best = found >= 0 ? (u64)found : ~0ull;
+    long long end = (long long)tail;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        const u64 o = __shfl_xor(best, d);
+        const long long t = __shfl_xor(end, d);
+        best = o < best ? o : best;
+        end = t > end ? t : end;
+    }
+    const bool got = best != ~0ull;
+    const int64_t id = got ? (int64_t)best : (int64_t)end;
+    if (got ? found == id : tail == id) {
+        a.ids[r] = (int32_t)id;
+        const double wt = row.greedy ? 1.0 : row.weight(got ? key_f : key_t);
+        if (a.prob) a.prob[r] = (float)(wt * row.scale / (double)all);
+    }
+}
+
+__device__ __forceinline__ void none(const SampleArgs& a, int64_t r) {
+    a.ids[r] = -1;
+    if (a.prob) a.prob[r] = 0.0f;
+}
+
+// Which of n consecutive parts holds the choice: the first whose running sum exceeds the
+// target, the last one with weight if none does.  Whether a part with `sum`, `from` before it,
+// is the one (u below 0 takes the first part with weight).
+__device__ __forceinline__ bool is_part(u64 from, u64 sum, u64 all, double target, bool is_last) {
+    if (!((double)all > target)) return is_last;
+    if (sum == 0 || !((double)(from + sum) > target)) return false;
+    return !((double)from > target) || from == 0;
+}
+
+// ------------------------------------------------------------------ a row in one workgroup
+template <typename T>
+__global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double scale) {
+    __shared__ Shared sm;
+    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
+    const int64_t r = blockIdx.x;
+    const Span<T> sp((const T*)a.logits + r * a.V, a.V, 0, w, lane);
+    for (int b = tid; b < kBins; b += kNT) {
+        sm.cnt[b] = 0;
+        sm.mass[b] = 0;
+    }
+    uint32_t hi, lo;
+    sp.extremes(sm.w32, a.V, 0, w, lane, hi, lo);
+    const Row row(a, r, hi, lo, scale);
+    if (row.bad) {
+        if (tid == 0) none(a, r);
+        return;
+    }
+    u64 q[kItems];
+    Border b{0, 0};
+    if (row.k == 1) {
+        b = Border{hi, 1};
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) q[i] = sp.key[i] == hi ? (u64)scale : 0;
+    } else {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) q[i] = row.fixed(sp.key[i]);
+        if (row.cuts(a.V)) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kItems; ++i)
+                if (q[i]) {
+                    const int bin = row.bin(sp.key[i]);
+                    atomicAdd(&sm.cnt[bin], 1u);
+                    atomicAdd(&sm.mass[bin], q[i]);
+                }
+            __syncthreads();
+            auto each = [&](auto f) {
+#pragma unroll
+                for (int i = 0; i < kItems; ++i)
+                    if (q[i]) f(sp.key[i], q[i]);
+            };
+            b = find_border(sm, row, each, tid, lane, w);
+        }
+        if (row.min_p > 0.0f) {
+            // As weight_of: by the weight itself, not by its rounded q.
+#pragma unroll
+            for (int i = 0; i < kItems; ++i)
+                if (q[i] && row.weight(sp.key[i]) < (double)row.min_p) q[i] = 0;
+        }
+    }
+    __syncthreads();
+    const uint32_t ties = wave_ties(sp, b);
+    if (lane == 0) sm.w32[0][w] = ties;
+    __syncthreads();
+    uint64_t before = 0;
+    for (int i = 0; i < w; ++i) before += sm.w32[0][i];
+    keep(sp, row, b, before, q, lane);
+    u64 sum = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) sum += q[i];
+    sum = wave_sum(sum);
+    if (lane == 0) sm.w64[w] = sum;
+    __syncthreads();
+    u64 all = 0, from = 0;
+    int last = 0;
+#pragma unroll
+    for (int i = 0; i < kNW; ++i) {
+        const u64 s = sm.w64[i];
+        if (i < w) from += s;
+        if (s) last = i;
+        all += s;
+    }
+    const double target = (double)a.u[r] * (double)all;
+    if (is_part(from, sum, all, target, w == last))
+        choose(a, sp, row, q, r, 0, from, target, all, w, lane);
+}
+
+// ------------------------------------------------------------------ a row in several
+struct SpanWs {
+    uint32_t* ext;    // [B][S][2] extremes of each span
+    uint32_t* cnt;    // [B][kBins]
+    u64* mass;        // [B][kBins]
+    uint32_t* found;  // [B] items in the list
+    uint32_t* list;   // [B][V] their keys
+    Border* border;   // [B]
+    u64* sum;         // [B][S] weight above the border
+    uint32_t* ties;   // [B][S] items with the border's key
+};
+
+template <typename T>
+__global__ __launch_bounds__(kNT) void sample_extremes_kernel(SampleArgs a, SpanWs ws, int spans) {
+    __shared__ uint32_t w32[2][kNW];
+    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
+    const int64_t r = blockIdx.x / (unsigned)spans;
+    const int s = (int)(blockIdx.x - (unsigned)r * (unsigned)spans);
+    const int64_t base = (int64_t)s * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    uint32_t hi, lo;
+    sp.extremes(w32, a.V, base, w, lane, hi, lo);
+    if (tid == 0) {
+        ws.ext[2 * blockIdx.x] = hi;
+        ws.ext[2 * blockIdx.x + 1] = lo;
+    }
+    if (s == 0) {
+        for (int b = tid; b < kBins; b += kNT) {
+            ws.cnt[r * kBins + b] = 0;
+            ws.mass[r * kBins + b] = 0;
+        }
+        if (tid == 0) ws.found[r] = 0;
+    }
+}
+
+// The row of a workgroup from its spans' extremes.
+__device__ __forceinline__ Row row_of(const SampleArgs& a, const SpanWs& ws, int64_t r, int spans,
+                                      double scale, uint32_t (&w32)[2][kNW], int tid, int lane,
+                                      int w) {
+    uint32_t hi = 0, lo = 0xFFFFFFFFu;
+    for (int i = tid; i < spans; i += kNT) {
+        const uint32_t h = ws.ext[2 * (r * spans + i)], l = ws.ext[2 * (r * spans + i) + 1];
+        hi = h > hi ? h : hi;
+        lo = l < lo ? l : lo;
+    }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
         const uint32_t h = (uint32_t)__shfl_xor((int)hi, d), l = (uint32_t)__shfl_xor((int)lo, d);
@@ -158,303 +618,244 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a, double scale) 
         lo = l < lo ? l : lo;
     }
     if (lane == 0) {
-        sm.wave32[0][w] = hi;
-        sm.wave32[1][w] = lo;
+        w32[0][w] = hi;
+        w32[1][w] = lo;
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        hi = sm.wave32[0][i] > hi ? sm.wave32[0][i] : hi;
-        lo = sm.wave32[1][i] < lo ? sm.wave32[1][i] : lo;
+    for (int i = 0; i < kNW; ++i) {
+        hi = w32[0][i] > hi ? w32[0][i] : hi;
+        lo = w32[1][i] < lo ? w32[1][i] : lo;
     }
-    const float temp = a.temperature ? a.temperature[row] : 1.0f;
-    if (hi <= kKeyNegInf || hi >= kKeyPosInf || lo < kKeyNegInf || !(temp == temp)) {
-        if (tid == 0) {
-            a.ids[row] = -1;
-            if (a.prob) a.prob[row] = 0.0f;
+    __syncthreads();
+    return Row(a, r, hi, lo, scale);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kNT) void sample_histogram_kernel(SampleArgs a, SpanWs ws, int spans,
+                                                               double scale) {
+    __shared__ uint32_t cnt[kBins];
+    __shared__ u64 mass[kBins];
+    __shared__ uint32_t w32[2][kNW];
+    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
+    const int64_t r = blockIdx.x / (unsigned)spans;
+    const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    for (int b = tid; b < kBins; b += kNT) {
+        cnt[b] = 0;
+        mass[b] = 0;
+    }
+    const Row row = row_of(a, ws, r, spans, scale, w32, tid, lane, w);
+    if (row.bad || row.k == 1 || !row.cuts(a.V)) return;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const u64 q = row.fixed(sp.key[i]);
+        if (q) {
+            const int bin = row.bin(sp.key[i]);
+            atomicAdd(&cnt[bin], 1u);
+            atomicAdd(&mass[bin], q);
         }
+    }
+    __syncthreads();
+    for (int b = tid; b < kBins; b += kNT)
+        if (cnt[b]) {
+            atomicAdd(&ws.cnt[r * kBins + b], cnt[b]);
+            atomicAdd(&ws.mass[r * kBins + b], mass[b]);
+        }
+}
+
+// The items of the bins that can hold a border: top-k's bin, and the bins in which top-p's may
+// lie, whose share is of a sum that top-k's bin makes uncertain.
+template <typename T>
+__global__ __launch_bounds__(kNT) void sample_collect_kernel(SampleArgs a, SpanWs ws, int spans,
+                                                             double scale) {
+    __shared__ Shared sm;
+    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
+    const int64_t r = blockIdx.x / (unsigned)spans;
+    const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    const Row row = row_of(a, ws, r, spans, scale, sm.w32, tid, lane, w);
+    if (row.bad || row.k == 1 || !row.cuts(a.V)) return;
+    uint32_t c = 0, c0;
+    u64 m = 0, m0;
+    for (int b = tid; b < kBins; b += kNT) {
+        sm.cnt[b] = ws.cnt[r * kBins + b];
+        sm.mass[b] = ws.mass[r * kBins + b];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kBPT; ++j) {
+        c += sm.cnt[tid * kBPT + j];
+        m += sm.mass[tid * kBPT + j];
+    }
+    c0 = c;
+    m0 = m;
+    block_before(sm, c, m, lane, w);
+    if (tid == kNT - 1) {
+        sm.lo = c + c0;
+        sm.at_mass = m + m0;
+    }
+    __syncthreads();
+    const uint32_t total = sm.lo;
+    u64 least = sm.at_mass, most = least;  // the sum that top-p's share is of
+    __syncthreads();
+    int k_bin = -1, p_from = 0, p_to = -1;
+    if (row.k < (int64_t)total) {
+        pick<kBins>(sm, sm.cnt, sm.mass, c, m, false, (uint64_t)row.k, 0.0, tid);
+        k_bin = sm.at;
+        least = sm.above_mass;
+        most = sm.above_mass + sm.at_mass;
+        __syncthreads();
+    }
+    if (row.top_p < 1.0f) {
+        pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, (double)row.top_p * (double)least, tid);
+        p_from = sm.at < 0 ? 0 : sm.at;  // none: the least sum is 0, any bin may be it
+        __syncthreads();
+        pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, (double)row.top_p * (double)most, tid);
+        p_to = sm.at;
+    }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i) {
+        const uint32_t key = sp.key[i];
+        if (key <= kKeyNegInf) continue;
+        const int bin = row.bin(key);
+        if ((bin == k_bin || (bin >= p_from && bin <= p_to)) && row.fixed(key))
+            ws.list[r * a.V + atomicAdd(&ws.found[r], 1u)] = key;
+    }
+}
+
+__global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs ws, int spans,
+                                                            double scale) {
+    __shared__ Shared sm;
+    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
+    const int64_t r = blockIdx.x;
+    const Row row = row_of(a, ws, r, spans, scale, sm.w32, tid, lane, w);
+    Border b{0, 0};
+    if (!row.bad && row.k == 1) {
+        b = Border{row.hi, 1};
+    } else if (!row.bad && row.cuts(a.V)) {
+        for (int i = tid; i < kBins; i += kNT) {
+            sm.cnt[i] = ws.cnt[r * kBins + i];
+            sm.mass[i] = ws.mass[r * kBins + i];
+        }
+        __syncthreads();
+        const uint32_t n = ws.found[r];
+        const uint32_t* list = ws.list + r * a.V;
+        b = find_border(sm, row, [&](auto f) {
+            for (uint32_t i = tid; i < n; i += kNT) f(list[i], row.fixed(list[i]));
+        }, tid, lane, w);
+    }
+    if (tid == 0) ws.border[r] = b;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kNT) void sample_sums_kernel(SampleArgs a, SpanWs ws, int spans,
+                                                          double scale) {
+    __shared__ uint32_t w32[2][kNW];
+    __shared__ u64 w64[kNW];
+    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
+    const int64_t r = blockIdx.x / (unsigned)spans;
+    const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    const Row row = row_of(a, ws, r, spans, scale, w32, tid, lane, w);
+    if (row.bad) return;
+    const Border b = ws.border[r];
+    u64 sum = 0;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+        if (sp.key[i] > b.key) sum += weight_of(row, sp.key[i]);
+    sum = wave_sum(sum);
+    const uint32_t ties = wave_ties(sp, b);
+    if (lane == 0) {
+        w64[w] = sum;
+        w32[0][w] = ties;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        ws.sum[blockIdx.x] = w64[0] + w64[1] + w64[2] + w64[3];
+        ws.ties[blockIdx.x] = w32[0][0] + w32[0][1] + w32[0][2] + w32[0][3];
+    }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs ws, int spans,
+                                                            double scale) {
+    __shared__ Shared sm;
+    __shared__ u64 pick_from, pick_all;
+    __shared__ uint64_t pick_ties;
+    __shared__ int pick_span;
+    const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
+    const int64_t r = blockIdx.x;
+    const Row row = row_of(a, ws, r, spans, scale, sm.w32, tid, lane, w);
+    if (row.bad) {
+        if (tid == 0) none(a, r);
         return;
     }
-    const float top_p = a.top_p ? a.top_p[row] : 1.0f;
-    const float min_p = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.0f;
-    const bool greedy = temp <= 0.0f;
-    int64_t k = a.top_k && a.top_k[row] > 0 ? a.top_k[row] : a.V;
-    if (greedy || top_p <= 0.0f) k = 1;
-    const RowParams rp{greedy ? 0.0 : 1.0 / (double)temp, (double)value_of(hi), scale};
-
-    // The border: items with a key above it stay, and the first `ties` of those that have it.
-    uint32_t border = 0;
-    int64_t ties = 0;
-
-    // Descends `hist(digit histogram of the keys with the given upper bits)`; the bin that
-    // holds the border is chosen by `pick`.  count: by counts, else by weights.
-    auto descend = [&](auto member, bool by_mass, uint64_t want_count, double want_mass,
-                       uint64_t& left, uint64_t& mass_above, uint32_t& total) {
-        uint32_t prefix = 0;
-        int shift = 32;
-        mass_above = 0;
-        uint64_t count_above = 0;
-        for (int round = 0; round < 3; ++round) {
-            const int bits = round == 2 ? 10 : 11;
-            const int sh = shift - bits;
-            for (int b = tid; b < kBins; b += NT) {
-                sm.cnt[b] = 0;
-                sm.mass[b] = 0;
-            }
-            if (tid == 0) sm.bin = -1;
-            __syncthreads();
-            r.each(lane, [&](const uint32_t (&key)[4], int it) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool in = key[e] != 0 && member(key[e]) &&
-                                    (round == 0 || (key[e] >> shift) == (prefix >> shift));
-                    if (in) {
-                        const uint32_t b = (key[e] >> sh) & ((1u << bits) - 1);
-                        atomicAdd(&sm.cnt[b], 1u);
-                        if (by_mass) {
-                            const uint64_t q = fixed(weight(key[e], rp), rp);
-                            if (q) atomicAdd(&sm.mass[b], (unsigned long long)q);
-                        }
-                    }
-                }
-            });
-            __syncthreads();
-            // Bins from the highest down, consecutive ones to a thread.
-            constexpr int BPT = kBins / NT;
-            uint32_t c = 0;
-            uint64_t m = 0;
-#pragma unroll
-            for (int j = 0; j < BPT; ++j) {
-                const int b = kBins - 1 - (tid * BPT + j);
-                c += sm.cnt[b];
-                m += sm.mass[b];
-            }
-            uint32_t cb = wave_before(c, lane);
-            uint64_t mb = wave_before((unsigned long long)m, lane);
-            if (lane == kWave - 1) {
-                sm.wave32[0][w] = cb + c;
-                sm.wave64[w] = mb + m;
-            }
-            __syncthreads();
-            for (int i = 0; i < w; ++i) {
-                cb += sm.wave32[0][i];
-                mb += sm.wave64[i];
-            }
-            // The last bin, from the top, that holds items and has less than what is wanted
-            // above it.
-            int mine = -1;
-            uint32_t c_at = 0;
-            uint64_t m_at = 0;
-#pragma unroll
-            for (int j = 0; j < BPT; ++j) {
-                const int pos = tid * BPT + j, b = kBins - 1 - pos;
-                const uint32_t cnt = sm.cnt[b];
-                const bool short_of = by_mass ? (double)(mass_above + mb) < want_mass
-                                              : count_above + cb < want_count;
-                if (cnt && short_of) {
-                    mine = pos;
-                    c_at = cb;
-                    m_at = mb;
-                }
-                cb += cnt;
-                mb += sm.mass[b];
-            }
-            if (mine >= 0) atomicMax(&sm.bin, mine);
-            __syncthreads();
-            if (mine >= 0 && sm.bin == mine) {
-                sm.above32 = c_at;
-                sm.above64 = m_at;
-                sm.at32 = sm.cnt[kBins - 1 - mine];
-            }
-            __syncthreads();
-            const uint32_t digit = (uint32_t)(kBins - 1 - sm.bin);
-            prefix |= digit << sh;
-            shift = sh;
-            count_above += sm.above32;
-            mass_above += sm.above64;
-            total = sm.at32;
-            __syncthreads();
-        }
-        left = want_count - count_above;
-        return prefix;
+    const Border b = ws.border[r];
+    const u64 tie_q = b.key ? weight_of(row, b.key) : 0;
+    const u64* sums = ws.sum + r * spans;
+    const uint32_t* ties = ws.ties + r * spans;
+    // Consecutive spans to a thread.
+    const int per = (spans + kNT - 1) / kNT, s0 = tid * per, s1 = s0 + per < spans ? s0 + per : spans;
+    uint32_t t_own = 0;
+    for (int i = s0; i < s1; ++i) t_own += ties[i];
+    uint32_t t_before = t_own;
+    u64 unused = 0;
+    block_before(sm, t_before, unused, lane, w);
+    auto kept_ties = [&](uint32_t before, uint32_t n) {
+        const uint32_t left = before < b.ties ? b.ties - before : 0;
+        return left < n ? left : n;
     };
-
-    // Sum of the weights of the items above the border and of its ties.
-    auto sum_above = [&](uint32_t edge) {
-        uint64_t s = 0;
-        r.each(lane, [&](const uint32_t (&key)[4], int) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (key[e] > edge) s += fixed(weight(key[e], rp), rp);
-        });
-        s = wave_sum((unsigned long long)s);
-        __syncthreads();
-        if (lane == 0) sm.wave64[w] = s;
-        __syncthreads();
-        s = 0;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) s += sm.wave64[i];
-        return s;
-    };
-
-    uint32_t tie_total = 0;
-    if (k == 1) {
-        border = hi;
-        ties = 1;
-    } else {
-        if (k < a.V) {
-            uint64_t left, m;
-            border = descend([](uint32_t) { return true; }, false, (uint64_t)k, 0.0, left, m,
-                             tie_total);
-            ties = (int64_t)left;
-        }
-        if (top_p < 1.0f) {
-            const uint64_t above = sum_above(border);
-            const uint64_t tie_w = ties ? fixed(weight(border, rp), rp) : 0;
-            const double want = (double)top_p * (double)(above + tie_w * (uint64_t)ties);
-            if ((double)above < want) {
-                // The border lies among the ties (or nowhere, if there are none).
-                if (tie_w) {
-                    int64_t stay = (int64_t)ceil((want - (double)above) / (double)tie_w);
-                    stay = stay < 1 ? 1 : stay;
-                    while (stay > 1 &&
-                           !((double)(above + tie_w * (uint64_t)(stay - 1)) < want)) --stay;
-                    while (stay < ties && (double)(above + tie_w * (uint64_t)stay) < want) ++stay;
-                    ties = stay < ties ? stay : ties;
-                }
-            } else {
-                const uint32_t edge = border;
-                uint64_t left, m;
-                border = descend([edge](uint32_t key) { return key > edge; }, true, 0, want, left,
-                                 m, tie_total);
-                const uint64_t q = fixed(weight(border, rp), rp);
-                ties = tie_total;
-                if (q) {
-                    int64_t stay = (int64_t)ceil((want - (double)m) / (double)q);
-                    stay = stay < 1 ? 1 : stay;
-                    while (stay > 1 && !((double)(m + q * (uint64_t)(stay - 1)) < want)) --stay;
-                    while (stay < ties && (double)(m + q * (uint64_t)stay) < want) ++stay;
-                    ties = stay < ties ? stay : ties;
-                }
-            }
-        }
+    u64 own = 0;
+    uint32_t t = t_before;
+    for (int i = s0; i < s1; ++i) {
+        own += sums[i] + tie_q * kept_ties(t, ties[i]);
+        t += ties[i];
     }
-
-    // How many items with the border's key lie in the spans before this wave's.
-    uint32_t seen = 0;
-    r.each(lane, [&](const uint32_t (&key)[4], int) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) seen += key[e] == border && key[e] != 0;
-    });
-    seen = wave_sum(seen);
     __syncthreads();
-    if (lane == 0) sm.wave32[0][w] = seen;
+    u64 from = own;
+    uint32_t unused32 = 0;
+    block_before(sm, unused32, from, lane, w);
+    if (tid == kNT - 1) pick_all = from + own;
+    if (tid == 0) pick_span = -1;
     __syncthreads();
-    int64_t before = 0;
-    for (int i = 0; i < w; ++i) before += sm.wave32[0][i];
-
-    // A kept item's weight; `rank` counts the border's items so far in order of the index.
-    auto kept_weight = [&](const uint32_t (&key)[4], int64_t& rank, uint64_t (&q)[4],
-                           double (&wt)[4]) {
-        uint32_t tie[4], n = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            tie[e] = key[e] == border && key[e] != 0;
-            n += tie[e];
+    const u64 all = pick_all;
+    const double target = (double)a.u[r] * (double)all;
+    t = t_before;
+    u64 run = from;
+    for (int i = s0; i < s1; ++i) {
+        const u64 s = sums[i] + tie_q * kept_ties(t, ties[i]);
+        if (is_part(run, s, all, target, s != 0 && run + s == all)) {
+            pick_from = run;
+            pick_ties = t;
+            pick_span = i;
         }
-        int64_t mine = 0;
-        if (__any(n)) {
-            const uint32_t lower = wave_before(n, lane);
-            mine = rank + lower;
-            rank += __shfl((int)(lower + n), kWave - 1);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool stays = key[e] > border || (tie[e] && mine < ties);
-            mine += tie[e];
-            wt[e] = 0.0;
-            if (stays) {
-                wt[e] = greedy ? 1.0 : weight(key[e], rp);
-                if (wt[e] < (double)min_p) wt[e] = 0.0;
-            }
-            q[e] = fixed(wt[e], rp);
-        }
-    };
-    uint64_t sum = 0;
-    {
-        int64_t rank = before;
-        r.each(lane, [&](const uint32_t (&key)[4], int) {
-            uint64_t q[4];
-            double wt[4];
-            kept_weight(key, rank, q, wt);
-            sum += q[0] + q[1] + q[2] + q[3];
-        });
+        run += s;
+        t += ties[i];
     }
-    sum = wave_sum((unsigned long long)sum);
-    if (lane == 0) sm.wave64[w] = sum;
     __syncthreads();
-    uint64_t all = 0, from = 0;
-    int last = 0;  // the last wave with a kept item
+    if (pick_span < 0) return;  // no weight anywhere (not reached: the largest weighs 1)
+    const int64_t base = (int64_t)pick_span * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    u64 q[kItems];
 #pragma unroll
-    for (int i = 0; i < NW; ++i) {
-        const uint64_t s = sm.wave64[i];
-        if (i < w) from += s;
-        if (s) last = i;
-        all += s;
-    }
-    // The wave whose running sum first exceeds u times the whole, or the last one.
-    const double target = (double)a.u[row] * (double)all;
-    const bool past_before = (double)from > target, past = (double)(from + sum) > target;
-    const bool mine = past ? !past_before && sum != 0 : false;
-    const bool none = !((double)all > target);
-    if (!(none ? w == last : mine)) {
-        // A u below 0 takes the first kept item: its wave has nothing before it.
-        if (!(target < 0.0 && from == 0 && sum != 0)) return;
-    }
-    {
-        int64_t rank = before;
-        uint64_t run = from;
-        int64_t found = -1, tail = -1;
-        double wf = 0.0, wl = 0.0;
-        r.each(lane, [&](const uint32_t (&key)[4], int it) {
-            uint64_t q[4];
-            double wt[4];
-            kept_weight(key, rank, q, wt);
-            const uint64_t own = q[0] + q[1] + q[2] + q[3];
-            uint64_t c = run + wave_before((unsigned long long)own, lane);
-            run += wave_sum((unsigned long long)own);
+    for (int i = 0; i < kItems; ++i) q[i] = sp.key[i] >= b.key ? weight_of(row, sp.key[i]) : 0;
+    const uint32_t wt = wave_ties(sp, b);
+    if (lane == 0) sm.w32[0][w] = wt;
+    __syncthreads();
+    uint64_t before = pick_ties;
+    for (int i = 0; i < w; ++i) before += sm.w32[0][i];
+    keep(sp, row, b, before, q, lane);
+    u64 sum = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                c += q[e];
-                if (q[e]) {
-                    tail = r.index(it, lane) + e;
-                    wl = wt[e];
-                    if (found < 0 && (double)c > target) {
-                        found = tail;
-                        wf = wl;
-                    }
-                }
-            }
-        });
-        // The least index found by any lane; else the greatest kept one.
-        const unsigned long long key_f =
-            found >= 0 ? (unsigned long long)found : ~0ull;
-        unsigned long long best = key_f;
-        long long end = (long long)tail;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            const unsigned long long o = __shfl_xor(best, d);
-            const long long t = __shfl_xor(end, d);
-            best = o < best ? o : best;
-            end = t > end ? t : end;
-        }
-        const bool got = best != ~0ull;
-        const int64_t id = got ? (int64_t)best : (int64_t)end;
-        if (got ? found == id : tail == id) {
-            a.ids[row] = (int32_t)id;
-            if (a.prob) a.prob[row] = (float)((got ? wf : wl) * scale / (double)all);
-        }
-    }
+    for (int i = 0; i < kItems; ++i) sum += q[i];
+    sum = wave_sum(sum);
+    if (lane == 0) sm.w64[w] = sum;
+    __syncthreads();
+    u64 before_w = pick_from;
+    for (int i = 0; i < w; ++i) before_w += sm.w64[i];
+    if (is_part(before_w, sum, all, target, sum != 0 && before_w + sum == all))
+        choose(a, sp, row, q, r, base, before_w, target, all, w, lane);
 }
 
 // Rows without items.
@@ -465,25 +866,59 @@ __global__ void sample_none_kernel(int32_t* ids, float* prob, int64_t B) {
     if (prob) prob[i] = 0.0f;
 }
 
-template <typename T, int NT, int IT, bool KEEP>
-hipError_t launch_rows(const SampleArgs& a, double scale, hipStream_t stream) {
-    hipLaunchKernelGGL((sample_kernel<T, NT, IT, KEEP>), dim3((unsigned)a.B), dim3(NT), 0, stream,
-                       a, scale);
-    return hipGetLastError();
+int64_t spans_of(int64_t V) { return (V + kSpan - 1) / kSpan; }
+
+SpanWs layout(char* p, int64_t B, int64_t V, size_t* bytes) {
+    size_t at = 0;
+    auto take = [&](size_t n) {
+        char* r = p + at;
+        at += (n + 255) / 256 * 256;
+        return r;
+    };
+    const size_t rows = (size_t)B, spans = (size_t)spans_of(V);
+    SpanWs w;
+    w.ext = (uint32_t*)take(rows * spans * 8);
+    w.cnt = (uint32_t*)take(rows * kBins * 4);
+    w.mass = (u64*)take(rows * kBins * 8);
+    w.found = (uint32_t*)take(rows * 4);
+    w.list = (uint32_t*)take(rows * (size_t)V * 4);
+    w.border = (Border*)take(rows * sizeof(Border));
+    w.sum = (u64*)take(rows * spans * 8);
+    w.ties = (uint32_t*)take(rows * spans * 4);
+    *bytes = at;
+    return w;
 }
 
 template <typename T>
-hipError_t launch_typed(const SampleArgs& a, double scale, hipStream_t stream) {
-    if (a.V <= 256 * 4 * 4) return launch_rows<T, 256, 4, true>(a, scale, stream);
-    if (a.V <= 1024 * 4 * 4) return launch_rows<T, 1024, 4, true>(a, scale, stream);
-    return launch_rows<T, 1024, 1, false>(a, scale, stream);
+hipError_t launch_typed(const SampleArgs& a, double scale, void* p, hipStream_t stream) {
+    const dim3 rows((unsigned)a.B), block(kNT);
+    if (a.V <= kSpan) {
+        hipLaunchKernelGGL(sample_row_kernel<T>, rows, block, 0, stream, a, scale);
+        return hipGetLastError();
+    }
+    const int spans = (int)spans_of(a.V);
+    size_t bytes;
+    const SpanWs ws = layout((char*)p, a.B, a.V, &bytes);
+    const dim3 all((unsigned)(a.B * spans));
+    hipLaunchKernelGGL(sample_extremes_kernel<T>, all, block, 0, stream, a, ws, spans);
+    hipLaunchKernelGGL(sample_histogram_kernel<T>, all, block, 0, stream, a, ws, spans, scale);
+    hipLaunchKernelGGL(sample_collect_kernel<T>, all, block, 0, stream, a, ws, spans, scale);
+    hipLaunchKernelGGL(sample_border_kernel, rows, block, 0, stream, a, ws, spans, scale);
+    hipLaunchKernelGGL(sample_sums_kernel<T>, all, block, 0, stream, a, ws, spans, scale);
+    hipLaunchKernelGGL(sample_choose_kernel<T>, rows, block, 0, stream, a, ws, spans, scale);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t sample_workspace(int64_t, int64_t, IoType) { return 0; }
+size_t sample_workspace(int64_t B, int64_t V, IoType) {
+    if (V <= kSpan || B == 0) return 0;
+    size_t bytes;
+    (void)layout(nullptr, B, V, &bytes);
+    return bytes;
+}
 
-hipError_t launch_sample(const SampleArgs& a, void*, hipStream_t stream) {
+hipError_t launch_sample(const SampleArgs& a, void* ws, hipStream_t stream) {
     if (a.V == 0) {
         hipLaunchKernelGGL(sample_none_kernel, dim3((unsigned)((a.B + 255) / 256)), dim3(256), 0,
                            stream, a.ids, a.prob, a.B);
@@ -492,8 +927,8 @@ hipError_t launch_sample(const SampleArgs& a, void*, hipStream_t stream) {
     int log_v = 0;
     while (((int64_t)1 << log_v) < a.V) ++log_v;
     const double scale = (double)((uint64_t)1 << (62 - log_v));
-    return a.io == IoType::kF32 ? launch_typed<float>(a, scale, stream)
-                                : launch_typed<bf16>(a, scale, stream);
+    return a.io == IoType::kF32 ? launch_typed<float>(a, scale, ws, stream)
+                                : launch_typed<bf16>(a, scale, ws, stream);
 }
 
 }  // namespace recblr
