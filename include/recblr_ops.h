@@ -143,8 +143,8 @@ int recblr_adamw_moments(const recblr_adamw_tensor* tensors, int64_t count,
  * type's lowest, say).  A row with no item (V = 0, all -inf) or none to be
  * chosen by its values (a NaN or +inf among logits, a NaN temperature) gives
  * id -1 and prob 0.
- * w are formed in 64 bits and summed as integers of 2^-(62 - ceil(log2 V)): sums
- * are exact whatever their order, and a w below half of that is 0.
+ * w are formed in 64 bits and summed as integers of 2^-F, F = 62 - ceil(log2 V), at
+ * most 51: sums are exact whatever their order, and a w below half of that is 0.
  * Errors: INVALID_ARGUMENT, UNSUPPORTED (io, V > 2^24, B > 2^31 - 1), WORKSPACE.
  */
 size_t recblr_sample_workspace_size(int64_t B, int64_t V, int io);

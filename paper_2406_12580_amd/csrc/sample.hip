@@ -65,7 +65,7 @@ __device__ __forceinline__ V wave_before(V v, int lane) {
 
 typedef unsigned long long u64;
 
-// e^x for x in (-45, 0]: x = n ln 2 + t with |t| <= ln 2 / 2, and e^t by its Taylor polynomial
+// e^x for x in [-46, 0]: x = n ln 2 + t with |t| <= ln 2 / 2, and e^t by its Taylor polynomial
 // of degree 12, whose remainder is below 2e-16 of it.
 __device__ __forceinline__ double exp_neg(double x) {
     const double n = __builtin_rint(x * 1.4426950408889634074);
@@ -86,6 +86,11 @@ __device__ __forceinline__ double exp_neg(double x) {
     p = __builtin_fma(p, t, 1.0);
     p = __builtin_fma(p, t, 1.0);
     return __builtin_amdgcn_ldexp(p, (int)n);
+}
+
+// The nearest integer of x in [0, 2^51]: 2^52 + x has it in its lowest bits.
+__device__ __forceinline__ u64 rounded(double x) {
+    return (u64)__double_as_longlong(x + 0x1p52) & 0xFFFFFFFFFFFFFull;
 }
 
 // What a row asks for, and the measures that its extremes give.
@@ -112,17 +117,15 @@ struct Row {
         inv_t = greedy ? 0.0 : 1.0 / (double)temp;
         top = value_of(hi);
         max = (double)top;
-        // Items further down than 45 temperatures weigh nothing.
-        const float range = fminf(45.0f * temp, top - value_of(lo < kKeyNegInf ? hi : lo));
+        const float range = fminf(46.0f * temp, top - value_of(lo < kKeyNegInf ? hi : lo));
         bins = range > 0.0f && range < 3e38f ? (float)(kBins - 1) / range : 0.0f;
     }
     __device__ __forceinline__ double weight(uint32_t key) const {
-        const double x = ((double)value_of(key) - max) * inv_t;
-        return key > kKeyNegInf && x > -45.0 ? exp_neg(x) : 0.0;  // e^-45 < 2^-63 rounds to 0
+        // What lies further down than 46 temperatures (-inf and what is no item among it) weighs
+        // e^-46, which no scale up to 2^51 brings to a half.
+        return exp_neg(fmax(((double)value_of(key) - max) * inv_t, -46.0));
     }
-    __device__ __forceinline__ u64 fixed(uint32_t key) const {
-        return (u64)(weight(key) * scale + 0.5);
-    }
+    __device__ __forceinline__ u64 fixed(uint32_t key) const { return rounded(weight(key) * scale); }
     // Rising as the logit falls: both roundings keep the order.
     __device__ __forceinline__ int bin(uint32_t key) const {
         const float b = (top - value_of(key)) * bins;
@@ -237,11 +240,10 @@ __device__ __forceinline__ uint32_t refine(Shared& sm, const Row& row, Each each
         }
         __syncthreads();
         uint32_t lo = 0xFFFFFFFFu, hi = 0;
-        each([&](uint32_t key, u64) {
-            if (key >= from && key <= to && member(key)) {
-                lo = key < lo ? key : lo;
-                hi = key > hi ? key : hi;
-            }
+        each([&](uint32_t key, u64 q) {
+            const bool in = (q != 0) & (key >= from) & (key <= to) & member(key);
+            lo = in && key < lo ? key : lo;
+            hi = in && key > hi ? key : hi;
         });
         if (lo <= hi) {
             atomicMin(&sm.lo, lo);
@@ -254,10 +256,10 @@ __device__ __forceinline__ uint32_t refine(Shared& sm, const Row& row, Each each
         const int bits = 32 - __clz((int)((hi - lo) | 1u));
         const int shift = bits > 8 ? bits - 8 : 0;
         each([&](uint32_t key, u64 q) {
-            if (key >= lo && key <= hi && member(key)) {
+            if ((q != 0) & (key >= lo) & (key <= hi) & member(key)) {
                 const uint32_t b = (hi - key) >> shift;
                 atomicAdd(&sm.fine_cnt[b], 1u);
-                if (q) atomicAdd(&sm.fine_mass[b], q);
+                atomicAdd(&sm.fine_mass[b], q);
             }
         });
         __syncthreads();
@@ -322,7 +324,7 @@ __device__ __forceinline__ Border find_border(Shared& sm, const Row& row, Each e
             pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, want, tid);
             const int bin = sm.at;
             b.key = refine(sm, row, each,
-                           [&](uint32_t key) { return key > edge && row.bin(key) == bin; }, true,
+                           [&](uint32_t key) { return (key > edge) & (row.bin(key) == bin); }, true,
                            0, want, tid, lane, w);
             b.ties = ties_within(sm.at_cnt, row.fixed(b.key), sm.above_mass, want);
         }
@@ -355,19 +357,17 @@ struct Span {
         }
     }
     // Largest and smallest key over the workgroup's items, by all threads; w32 of LDS.
-    __device__ __forceinline__ void extremes(uint32_t (&w32)[2][kNW], int64_t V, int64_t base,
-                                             int w, int lane, uint32_t& hi, uint32_t& lo) const {
+    __device__ __forceinline__ void extremes(uint32_t (&w32)[2][kNW], int w, int lane, uint32_t& hi,
+                                             uint32_t& lo) const {
+        // What is no item has key 0, which as the smallest wraps to the largest.
         hi = 0;
         lo = 0xFFFFFFFFu;
 #pragma unroll
-        for (int it = 0; it < kIT; ++it)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const bool in = index(base, w, it, lane) + e < V;
-                const uint32_t k = key[4 * it + e];
-                hi = in && k > hi ? k : hi;
-                lo = in && k < lo ? k : lo;
-            }
+        for (int i = 0; i < kItems; ++i) {
+            hi = key[i] > hi ? key[i] : hi;
+            lo = key[i] - 1u < lo ? key[i] - 1u : lo;
+        }
+        lo = lo == 0xFFFFFFFFu ? lo : lo + 1u;
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) {
             const uint32_t h = (uint32_t)__shfl_xor((int)hi, d), l = (uint32_t)__shfl_xor((int)lo, d);
@@ -427,7 +427,7 @@ __device__ __forceinline__ uint32_t wave_ties(const Span<T>& sp, const Border& b
 __device__ __forceinline__ u64 weight_of(const Row& row, uint32_t key) {
     if (row.greedy) return key > kKeyNegInf ? (u64)row.scale : 0;
     const double wt = row.weight(key);
-    return wt < (double)row.min_p ? 0 : (u64)(wt * row.scale + 0.5);
+    return wt < (double)row.min_p ? 0 : rounded(wt * row.scale);
 }
 
 // The item at which the running sum, `run0` before the wave's first item, first exceeds target,
@@ -500,7 +500,7 @@ __global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double
         sm.mass[b] = 0;
     }
     uint32_t hi, lo;
-    sp.extremes(sm.w32, a.V, 0, w, lane, hi, lo);
+    sp.extremes(sm.w32, w, lane, hi, lo);
     const Row row(a, r, hi, lo, scale);
     if (row.bad) {
         if (tid == 0) none(a, r);
@@ -527,16 +527,18 @@ __global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double
             __syncthreads();
             auto each = [&](auto f) {
 #pragma unroll
-                for (int i = 0; i < kItems; ++i)
-                    if (q[i]) f(sp.key[i], q[i]);
+                for (int i = 0; i < kItems; ++i) f(sp.key[i], q[i]);
             };
             b = find_border(sm, row, each, tid, lane, w);
         }
         if (row.min_p > 0.0f) {
-            // As weight_of: by the weight itself, not by its rounded q.
+            // As weight_of, by the weight itself; its q tells unless it is next to min_p's.
+            const u64 least = rounded((double)row.min_p * scale);
 #pragma unroll
-            for (int i = 0; i < kItems; ++i)
-                if (q[i] && row.weight(sp.key[i]) < (double)row.min_p) q[i] = 0;
+            for (int i = 0; i < kItems; ++i) {
+                if (q[i] < least) q[i] = 0;
+                else if (q[i] <= least + 1 && row.weight(sp.key[i]) < (double)row.min_p) q[i] = 0;
+            }
         }
     }
     __syncthreads();
@@ -573,6 +575,7 @@ struct SpanWs {
     u64* mass;        // [B][kBins]
     uint32_t* found;  // [B] items in the list
     uint32_t* list;   // [B][V] their keys
+    u64* list_q;      // [B][V] and weights
     Border* border;   // [B]
     u64* sum;         // [B][S] weight above the border
     uint32_t* ties;   // [B][S] items with the border's key
@@ -587,7 +590,7 @@ __global__ __launch_bounds__(kNT) void sample_extremes_kernel(SampleArgs a, Span
     const int64_t base = (int64_t)s * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
     uint32_t hi, lo;
-    sp.extremes(w32, a.V, base, w, lane, hi, lo);
+    sp.extremes(w32, w, lane, hi, lo);
     if (tid == 0) {
         ws.ext[2 * blockIdx.x] = hi;
         ws.ext[2 * blockIdx.x + 1] = lo;
@@ -714,14 +717,30 @@ __global__ __launch_bounds__(kNT) void sample_collect_kernel(SampleArgs a, SpanW
         pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, (double)row.top_p * (double)most, tid);
         p_to = sm.at;
     }
+    u64 q[kItems];
+    uint32_t n = 0;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-        const uint32_t key = sp.key[i];
-        if (key <= kKeyNegInf) continue;
-        const int bin = row.bin(key);
-        if ((bin == k_bin || (bin >= p_from && bin <= p_to)) && row.fixed(key))
-            ws.list[r * a.V + atomicAdd(&ws.found[r], 1u)] = key;
+        const int bin = row.bin(sp.key[i]);
+        const bool in = (sp.key[i] > kKeyNegInf) & ((bin == k_bin) | ((bin >= p_from) & (bin <= p_to)));
+        q[i] = in ? row.fixed(sp.key[i]) : 0;
+        n += q[i] != 0;
     }
+    // One addition to the row's counter for the workgroup's items.
+    uint32_t at = n;
+    u64 unused = 0;
+    __syncthreads();
+    block_before(sm, at, unused, lane, w);
+    if (tid == kNT - 1) sm.hi = at + n ? atomicAdd(&ws.found[r], at + n) : 0u;
+    __syncthreads();
+    at += sm.hi;
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+        if (q[i]) {
+            ws.list[r * a.V + at] = sp.key[i];
+            ws.list_q[r * a.V + at] = q[i];
+            ++at;
+        }
 }
 
 __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs ws, int spans,
@@ -741,8 +760,9 @@ __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs
         __syncthreads();
         const uint32_t n = ws.found[r];
         const uint32_t* list = ws.list + r * a.V;
+        const u64* list_q = ws.list_q + r * a.V;
         b = find_border(sm, row, [&](auto f) {
-            for (uint32_t i = tid; i < n; i += kNT) f(list[i], row.fixed(list[i]));
+            for (uint32_t i = tid; i < n; i += kNT) f(list[i], list_q[i]);
         }, tid, lane, w);
     }
     if (tid == 0) ws.border[r] = b;
@@ -882,6 +902,7 @@ SpanWs layout(char* p, int64_t B, int64_t V, size_t* bytes) {
     w.mass = (u64*)take(rows * kBins * 8);
     w.found = (uint32_t*)take(rows * 4);
     w.list = (uint32_t*)take(rows * (size_t)V * 4);
+    w.list_q = (u64*)take(rows * (size_t)V * 8);
     w.border = (Border*)take(rows * sizeof(Border));
     w.sum = (u64*)take(rows * spans * 8);
     w.ties = (uint32_t*)take(rows * spans * 4);
@@ -926,7 +947,8 @@ hipError_t launch_sample(const SampleArgs& a, void* ws, hipStream_t stream) {
     }
     int log_v = 0;
     while (((int64_t)1 << log_v) < a.V) ++log_v;
-    const double scale = (double)((uint64_t)1 << (62 - log_v));
+    // Sums of V of them stay below 2^62, and one below 2^51.
+    const double scale = (double)((uint64_t)1 << (log_v < 11 ? 51 : 62 - log_v));
     return a.io == IoType::kF32 ? launch_typed<float>(a, scale, ws, stream)
                                 : launch_typed<bf16>(a, scale, ws, stream);
 }
