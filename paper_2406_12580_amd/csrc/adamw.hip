@@ -116,28 +116,41 @@ __device__ __forceinline__ double value2(double s, int c) {
     return s * (q * q * 0x1p-32);
 }
 
-// Nearest code of m on the root's scale.  The fp32 root gives the code to within one; which
-// side of a border between two codes m falls on, s ((c +- 1/2) / 127)^2, is decided in 64 bits.
-__device__ __forceinline__ int code1(double m, float s) {
-    if (!(s > 0.0f)) return 0;
+// A block's scale as the encoders use it: whether it is positive (else all codes are the
+// lowest), a power of two that brings a tiny one into the range of v_rcp_f32, and the inverse.
+struct Scale {
+    float s, up, inv;
+    bool some;
+    __device__ __forceinline__ explicit Scale(float scale) {
+        s = scale;
+        some = s > 0.0f;
+        up = s < 1e-20f ? 0x1p66f : 1.0f;
+        inv = fast_rcp(s * up);
+    }
+};
+
+// Nearest code of m on the root's scale.  Hardware root and reciprocal (an ulp or two) give the
+// code to within one; which side of a border between two codes m falls on, s ((c +- 1/2) /
+// 127)^2, is decided in 64 bits.  IEEE division and roots here cost 45 instructions more.
+__device__ __forceinline__ int code1(double m, const Scale& s) {
     const double a = fabs(m);
-    int c = (int)rintf(127.0f * sqrtf((float)a / s));
+    int c = (int)rintf(127.0f * fast_sqrt((float)a * s.up * s.inv));
     c = c < 0 ? 0 : c > 127 ? 127 : c;
     const double x = a * 16129.0, up = c + 0.5, dn = c - 0.5;
-    if (c < 127 && x > (double)s * (up * up)) ++c;
-    else if (c > 0 && x < (double)s * (dn * dn)) --c;
+    const bool more = x > (double)s.s * (up * up), less = x < (double)s.s * (dn * dn);
+    c += more && c < 127 ? 1 : less && c > 0 ? -1 : 0;
+    c = s.some ? c : 0;
     return m < 0.0 ? -c : c;
 }
 // The same for v: borders s ((c + 1 +- 1/2) / 256)^4.
-__device__ __forceinline__ int code2(double v, float s) {
-    if (!(s > 0.0f)) return 0;
-    int c = (int)rintf(256.0f * sqrtf(sqrtf((float)v / s)));
+__device__ __forceinline__ int code2(double v, const Scale& s) {
+    int c = (int)rintf(256.0f * fast_sqrt(fast_sqrt((float)v * s.up * s.inv)));
     c = c < 1 ? 1 : c > 256 ? 256 : c;
     const double x = v * 0x1p32;
     const double up = (c + 0.5) * (c + 0.5), dn = (c - 0.5) * (c - 0.5);
-    if (c < 256 && x > (double)s * (up * up)) ++c;
-    else if (c > 1 && x < (double)s * (dn * dn)) --c;
-    return c - 1;
+    const bool more = x > (double)s.s * (up * up), less = x < (double)s.s * (dn * dn);
+    c += more && c < 256 ? 1 : less && c > 1 ? -1 : 0;
+    return s.some ? c - 1 : 0;
 }
 
 template <typename T>
@@ -213,11 +226,12 @@ __global__ __launch_bounds__(kNT) void adamw8_kernel(Table tab, AdamWHyper h, fl
         }
         store4(p, i, n, vec, pv);
         const float n1 = __uint_as_float(wave_max(top1)), n2 = __uint_as_float(wave_max(top2));
+        const Scale e1(n1), e2(n2);
         uint32_t o1 = 0, o2 = 0;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            o1 |= (uint32_t)(uint8_t)code1(m[k], n1) << (8 * k);
-            o2 |= (uint32_t)(uint8_t)code2(v[k], n2) << (8 * k);
+            o1 |= (uint32_t)(uint8_t)code1(m[k], e1) << (8 * k);
+            o2 |= (uint32_t)(uint8_t)code2(v[k], e2) << (8 * k);
         }
         store_codes(c1, i, n, vec, o1);
         store_codes(c2, i, n, vec, o2);

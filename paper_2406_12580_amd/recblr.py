@@ -20,6 +20,7 @@ import functools
 import inspect
 import os
 
+import numpy as np
 import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -512,13 +513,13 @@ def _on_device(fn):
     return wrapper
 
 
-def _arg(t, shape, dtype, device, name):
-    """The address of a tensor that has to be as described; None for None."""
+def _arg(t, shape, dtype, index, name):
+    """The address of a tensor that has to be as described, on the GPU `index`; None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape:
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}")
-    if t.device != device or device.type != "cuda":
+    if t.get_device() != index or index < 0:
         raise ValueError(f"{name} must live on the GPU, with the other tensors")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
@@ -544,11 +545,11 @@ def _delta_inputs(q, k, v, g, beta):
         raise ValueError("q must be [B, L, H, Dk]")
     H, HV, Dk, Dv = _delta_heads(q, k, v)
     B, L = q.shape[:2]
-    dt, dev = q.dtype, q.device
+    dt, at = q.dtype, q.get_device()
     io = io_code(dt)
-    ptrs = (_arg(q, (B, L, H, Dk), dt, dev, "q"), _arg(k, (B, L, H, Dk), dt, dev, "k"),
-            _arg(v, (B, L, HV, Dv), dt, dev, "v"), _arg(g, (B, L, HV), dt, dev, "g"),
-            _arg(beta, (B, L, HV), dt, dev, "beta"))
+    ptrs = (_arg(q, (B, L, H, Dk), dt, at, "q"), _arg(k, (B, L, H, Dk), dt, at, "k"),
+            _arg(v, (B, L, HV, Dv), dt, at, "v"), _arg(g, (B, L, HV), dt, at, "g"),
+            _arg(beta, (B, L, HV), dt, at, "beta"))
     return (B, L, H, HV, Dk, Dv), io, ptrs
 
 
@@ -565,14 +566,14 @@ def delta_forward(q, k, v, g, beta, h0=None, scale=None, keep_states=False):
     [B,HV,ceil(L/64),Dk,Dv] float32.  scale defaults to Dk ** -0.5."""
     sizes, io, ptrs = _delta_inputs(q, k, v, g, beta)
     B, L, H, HV, Dk, Dv = sizes
-    dev, f32 = q.device, torch.float32
+    dev, at, f32 = q.device, q.get_device(), torch.float32
     o = torch.empty_like(v)
     hT = torch.empty((B, HV, Dk, Dv), dtype=f32, device=dev)
     states = torch.empty((B, HV, -(-L // DELTA_CHUNK), Dk, Dv), dtype=f32, device=dev) \
         if keep_states else None
     ws, nws = _delta_workspace(OP_DELTA_FORWARD, sizes, io, dev)
     _check(recblr_delta_forward(
-        *ptrs, _arg(h0, (B, HV, Dk, Dv), f32, dev, "h0"), o.data_ptr(), hT.data_ptr(),
+        *ptrs, _arg(h0, (B, HV, Dk, Dv), f32, at, "h0"), o.data_ptr(), hT.data_ptr(),
         states.data_ptr() if keep_states else None, *sizes,
         Dk ** -0.5 if scale is None else scale, io, ws.data_ptr() if nws else None, nws,
         _stream()), "recblr_delta_forward")
@@ -585,15 +586,15 @@ def delta_backward(q, k, v, g, beta, states, do, dhT=None, scale=None, need_dh0=
     dbeta of the inputs' types and dh0 float32 (None unless need_dh0)."""
     sizes, io, ptrs = _delta_inputs(q, k, v, g, beta)
     B, L, H, HV, Dk, Dv = sizes
-    dev, f32 = q.device, torch.float32
+    dev, at, f32 = q.device, q.get_device(), torch.float32
     st = (B, HV, Dk, Dv)
     out = {"dq": torch.empty_like(q), "dk": torch.empty_like(k), "dv": torch.empty_like(v),
            "dg": torch.empty_like(g), "dbeta": torch.empty_like(beta),
            "dh0": torch.empty(st, dtype=f32, device=dev) if need_dh0 else None}
     ws, nws = _delta_workspace(OP_DELTA_BACKWARD, sizes, io, dev)
     _check(recblr_delta_backward(
-        *ptrs, _arg(states, (B, HV, -(-L // DELTA_CHUNK), Dk, Dv), f32, dev, "states"),
-        _arg(do, (B, L, HV, Dv), q.dtype, dev, "do"), _arg(dhT, st, f32, dev, "dhT"),
+        *ptrs, _arg(states, (B, HV, -(-L // DELTA_CHUNK), Dk, Dv), f32, at, "states"),
+        _arg(do, (B, L, HV, Dv), q.dtype, at, "do"), _arg(dhT, st, f32, at, "dhT"),
         *(None if t is None else t.data_ptr() for t in out.values()), *sizes,
         Dk ** -0.5 if scale is None else scale, io, ws.data_ptr() if nws else None, nws,
         _stream()), "recblr_delta_backward")
@@ -608,15 +609,15 @@ def delta_step(q, k, v, g, beta, h_prev, out=None, scale=None):
     if q.dim() != 3:
         raise ValueError("q must be [B, H, Dk]")
     H, HV, Dk, Dv = _delta_heads(q, k, v)
-    B, io, dt, dev = q.shape[0], io_code(q.dtype), q.dtype, q.device
+    B, io, dt, at = q.shape[0], io_code(q.dtype), q.dtype, q.get_device()
     st = (B, HV, Dk, Dv)
     o = torch.empty_like(v)
-    h_next = torch.empty(st, dtype=torch.float32, device=dev) if out is None else out
+    h_next = torch.empty_like(h_prev) if out is None else out
     _check(recblr_delta_step(
-        _arg(q, (B, H, Dk), dt, dev, "q"), _arg(k, (B, H, Dk), dt, dev, "k"),
-        _arg(v, (B, HV, Dv), dt, dev, "v"), _arg(g, (B, HV), dt, dev, "g"),
-        _arg(beta, (B, HV), dt, dev, "beta"), _arg(h_prev, st, torch.float32, dev, "h_prev"),
-        o.data_ptr(), _arg(h_next, st, torch.float32, dev, "out"), B, H, HV, Dk, Dv,
+        _arg(q, (B, H, Dk), dt, at, "q"), _arg(k, (B, H, Dk), dt, at, "k"),
+        _arg(v, (B, HV, Dv), dt, at, "v"), _arg(g, (B, HV), dt, at, "g"),
+        _arg(beta, (B, HV), dt, at, "beta"), _arg(h_prev, st, torch.float32, at, "h_prev"),
+        o.data_ptr(), _arg(h_next, st, torch.float32, at, "out"), B, H, HV, Dk, Dv,
         Dk ** -0.5 if scale is None else scale, io, _stream()), "recblr_delta_step")
     return o, h_next
 
@@ -631,16 +632,16 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     if logits.dim() != 2:
         raise ValueError("logits must be [B, V]")
     B, V = logits.shape
-    io, dev, f32 = io_code(logits.dtype), logits.device, torch.float32
+    io, dev, at, f32 = io_code(logits.dtype), logits.device, logits.get_device(), torch.float32
     ids = torch.empty(B, dtype=torch.int32, device=dev)
     prob = torch.empty(B, dtype=f32, device=dev)
     n = recblr_sample_workspace_size(B, V, io)
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
     _check(recblr_sample(
-        _arg(logits, (B, V), logits.dtype, dev, "logits"), _arg(u, (B,), f32, dev, "u"),
-        _arg(temperature, (B,), f32, dev, "temperature"),
-        _arg(top_k, (B,), torch.int32, dev, "top_k"), _arg(top_p, (B,), f32, dev, "top_p"),
-        _arg(min_p, (B,), f32, dev, "min_p"), ids.data_ptr(), prob.data_ptr(), B, V, io,
+        _arg(logits, (B, V), logits.dtype, at, "logits"), _arg(u, (B,), f32, at, "u"),
+        _arg(temperature, (B,), f32, at, "temperature"),
+        _arg(top_k, (B,), torch.int32, at, "top_k"), _arg(top_p, (B,), f32, at, "top_p"),
+        _arg(min_p, (B,), f32, at, "min_p"), ids.data_ptr(), prob.data_ptr(), B, V, io,
         ws.data_ptr() if n else None, n, _stream()), "recblr_sample")
     return ids, prob
 
@@ -663,6 +664,8 @@ class AdamW:
         if state_bits not in (8, 32):
             raise ValueError("state_bits must be 8 or 32")
         self.dtype, self.device = self.params[0].dtype, self.params[0].device
+        if not self.params[0].is_cuda:
+            raise ValueError("tensors must live on the GPU")
         self._io = io_code(self.dtype)
         self.lr, self.beta1, self.beta2, self.eps = lr, beta1, beta2, eps
         self.state_bits, self.steps = state_bits, step
@@ -701,6 +704,9 @@ class AdamW:
         for entry, n, w in zip(self._table, sizes, decay):
             entry.n, entry.weight_decay = n, w
         self._sizes = sizes
+        # The table's gradient addresses, as one array to assign.
+        self._grads = np.frombuffer(self._table, dtype=np.uint64).reshape(len(sizes), -1)[
+            :, AdamWTensor.grad.offset // 8]
 
     def _flat(self, t, dtype, n, name):
         if t.dtype != dtype or t.numel() != n:
@@ -713,8 +719,13 @@ class AdamW:
         """One update with grads, a tensor for each parameter; lr overrides the rate."""
         if len(grads) != len(self._sizes):
             raise ValueError("grads: one tensor for each parameter is needed")
-        for entry, t, n in zip(self._table, grads, self._sizes):
-            entry.grad = self._flat(t, self.dtype, n, "grads")
+        dtype, index, ptrs = self.dtype, self.device.index, []
+        for t, n in zip(grads, self._sizes):
+            if t.dtype is not dtype or t.numel() != n or t.get_device() != index \
+                    or not t.is_contiguous():
+                self._flat(t, dtype, n, "grads")  # says what is wrong
+            ptrs.append(t.data_ptr())
+        self._grads[:] = ptrs
         _adamw_step(self, self.lr if lr is None else lr, stream=stream)
         self.steps += 1
 
