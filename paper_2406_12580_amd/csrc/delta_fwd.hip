@@ -51,8 +51,11 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
     static_assert(KU >= 1, "every thread stages K");
 
     const int lane0 = threadIdx.x % kWave, w = wave_id();
-    const int64_t head = blockIdx.x / strips;
-    const int n0 = (int)(blockIdx.x - head * strips) * DVT;
+    // A head's strips lie apart by the number of heads, which is a multiple of eight where there
+    // are many: on one XCD, whose L2 reads K once for all.
+    const unsigned heads = gridDim.x / (unsigned)strips;
+    const int64_t head = blockIdx.x % heads;
+    const int n0 = (int)(blockIdx.x / heads) * DVT;
     const int64_t b = head / a.HV;
     const int hv = (int)(head - b * a.HV), h = hv / (a.HV / a.H);
     const int Dk = a.Dk, Dv = a.Dv, width = Dv - n0;

@@ -46,6 +46,7 @@ struct SplitWs {
     float* bt;   // [item][64], backward only
     float* X;    // [head][L][Dv]
     float* S;    // [item][Dk][Dv]
+    float *psi, *phi, *starts;  // of a walk in segments
 };
 
 // What the two preparations share: K's chunk and the decays in LDS, the inverse in tm.
@@ -334,16 +335,25 @@ __global__ __launch_bounds__(NT) void delta_prep_kernel(SplitArgs a, SplitWs ws)
 }
 
 // ------------------------------------------------------------------ the walk
+// The walk is linear in the state that it starts from, so a long one is cut into segments of
+// consecutive chunks: each segment is first walked from nothing (Psi, its end state) and without
+// inputs from the columns of the unit matrix (Phi), the segments' starts follow one from the
+// other as S_{i+1} = Phi_i S_i + Psi_i, and then all segments are walked at once.
 struct WalkArgs {
-    const float* s0;    // may be null
+    const float* s0;    // may be null; of a cut walk, [head][segment][Dk][Dv]
     float* s_end;       // may be null
     float* S;           // the state before each chunk (behind it, backwards)
     void* dv;           // backward: dV = beta Y
     int64_t L;
     int HV, Dk, Dv, chunks, strips;
+    int segments, per;  // chunks of a segment
+    float* psi;         // [head][segment][Dk][Dv]
+    float* phi;         // [head][segment][Dk][Dk]
 };
 
-template <typename T, int DK, bool BWD>
+// PROBE: Psi and Phi of every segment but the last (of a walk, the last in its order); strips
+// behind the state's own are Phi's.
+template <typename T, int DK, bool BWD, bool PROBE>
 __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs ws) {
     using I = Io<T>;
     using E = typename I::Elem;
@@ -354,9 +364,22 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
     __shared__ __attribute__((aligned(16))) E sS[P * kSPlane];
     __shared__ __attribute__((aligned(16))) E sX[P * kXPlane];
     const int lane = threadIdx.x % kWave, ll = lane & 15, g = lane >> 4, w = wave_id();
-    const unsigned head = blockIdx.x / (unsigned)a.strips;
-    const int strip = (int)(blockIdx.x - head * (unsigned)a.strips);
-    const int n0 = strip * SC, width = a.Dv - n0;
+    // Workgroup: (strip, head, segment), so that the strips of a segment, which read the same W
+    // and K^T, are a multiple of eight workgroups apart where there are enough: on one XCD, whose
+    // L2 reads them once (strips next to each other: 108 us for 103).
+    const int all_strips = PROBE ? a.strips + (a.Dk + SC - 1) / SC : a.strips;
+    const int walked = PROBE ? a.segments - 1 : a.segments;
+    const unsigned lines = gridDim.x / (unsigned)all_strips;
+    const unsigned hs = blockIdx.x % lines;
+    const unsigned head = hs / (unsigned)walked;
+    const int segment = (int)(hs - head * (unsigned)walked);
+    const int at_strip = (int)(blockIdx.x / lines);
+    const bool unit = PROBE && at_strip >= a.strips;  // Phi's
+    const int strip = unit ? 0 : at_strip;
+    const int n0 = (unit ? at_strip - a.strips : strip) * SC;
+    const int cols = unit ? a.Dk : a.Dv, width = cols - n0;
+    const int first = segment * a.per;
+    const int count = first + a.per < a.chunks ? a.per : a.chunks - first;
     const bool has_d = DTL >= 4 || w < DTL;
     const int64_t b = head / (unsigned)a.HV, hv = head - b * a.HV;
 
@@ -383,6 +406,7 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
         in.x0 = *(const f4*)(ws.X0 + (((item * a.strips + strip) * 4 + w) * kWave + lane) * 4);
         in.f = *(const f4*)(ws.f + item * C + 16 * w + 4 * (lane >> 4));
         in.et = ws.et[item];
+        if (PROBE && unit) in.x0 = f4{0, 0, 0, 0};
         if (has_d) {
 #pragma unroll
             for (int i = 0; i < SD; ++i) {
@@ -394,23 +418,25 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
                     else
                         in.kt[i][s].p[0] = *(const b8*)(KT + (dt * NC + s) * Frag<T>::kBytes);
                 }
-                if constexpr (BWD)
+                if constexpr (BWD) {
                     in.z[i] = *(const f4*)(ws.Z + (((item * a.strips + strip) * DTL + dt) * kWave +
                                                    lane) * 4);
+                    if (PROBE && unit) in.z[i] = f4{0, 0, 0, 0};
+                }
             }
         }
-        if constexpr (BWD) in.bt = *(const f4*)(ws.bt + item * C + 16 * w + 4 * g);
+        if constexpr (BWD && !PROBE) in.bt = *(const f4*)(ws.bt + item * C + 16 * w + 4 * g);
     };
 
     f4 S[SD];
     auto state_io = [&](const float* p, auto f) {
-        const auto r = wtile::rsrc(p, (uint32_t)(a.Dk * a.Dv * 4));
+        const auto r = wtile::rsrc(p, (uint32_t)(a.Dk * cols * 4));
         if (has_d) {
 #pragma unroll
             for (int i = 0; i < SD; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t o = ll < width ? (uint32_t)((16 * (w + 4 * i) + 4 * g + e) * a.Dv +
+                    const uint32_t o = ll < width ? (uint32_t)((16 * (w + 4 * i) + 4 * g + e) * cols +
                                                                n0 + ll) * 4
                                                   : kNowhere;
                     f(r, S[i], e, (int)o);
@@ -430,7 +456,7 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
         }
     };
     const int64_t state = (int64_t)a.Dk * a.Dv;
-    auto chunk_at = [&](int i) { return BWD ? a.chunks - 1 - i : i; };
+    auto chunk_at = [&](int i) { return BWD ? a.chunks - 1 - first - i : first + i; };
     auto step = [&](In& in, int c) {
         f4 x[2] = {in.x0, {0, 0, 0, 0}};
 #pragma unroll
@@ -439,7 +465,7 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
         const f4 X = x[0] + x[1];
         put<P>(sX, kXPlane, kUS, ll, 16 * w + 4 * g, in.f * X);
         lds_barrier();
-        state_store(a.S + ((int64_t)head * a.chunks + c) * state);
+        if constexpr (!PROBE) state_store(a.S + ((int64_t)head * a.chunks + c) * state);
         if (has_d) {
 #pragma unroll
             for (int i = 0; i < SD; ++i) {
@@ -452,7 +478,7 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
         }
         state_put();
         lds_barrier();
-        {
+        if constexpr (!PROBE) {
             const Rows<float> rx(ws.X + (int64_t)head * a.L * a.Dv + n0, (int64_t)c * C, a.L, a.Dv,
                                  width);
 #pragma unroll
@@ -471,12 +497,20 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
     for (int i = 0; i < SD; ++i) S[i] = f4{0, 0, 0, 0};
     // Two chunks' operands are on their way.  Reads behind the last chunk are of that one again:
     // a read under a condition would have every wait reckon with the branch that has none.
-    const int last = a.chunks - 1;
+    const int last = count - 1;
     In one, two;
     fetch(one, chunk_at(0));
     fetch(two, chunk_at(last < 1 ? last : 1));
-    if (a.s0)
-        state_io(a.s0 + head * state, [](auto r, f4& s, int e, int o) {
+    if (PROBE && unit && has_d) {
+#pragma unroll
+        for (int i = 0; i < SD; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                S[i][e] = 16 * (w + 4 * i) + 4 * g + e == n0 + ll ? 1.0f : 0.0f;
+    }
+    const int64_t start = a.segments > 1 ? (int64_t)head * a.segments + segment : (int64_t)head;
+    if (!PROBE && a.s0)
+        state_io(a.s0 + start * state, [](auto r, f4& s, int e, int o) {
             s[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0));
         });
     state_put();
@@ -487,8 +521,116 @@ __global__ __launch_bounds__(NT, 2) void delta_walk_kernel(WalkArgs a, SplitWs w
         step(two, chunk_at(i + 1));
         fetch(two, chunk_at(i + 3 < last ? i + 3 : last));
     }
-    if (a.chunks & 1) step(one, chunk_at(last));
-    if (a.s_end) state_store(a.s_end + head * state);
+    if (count & 1) step(one, chunk_at(last));
+    if constexpr (PROBE) {
+        const int64_t at = (int64_t)head * a.segments + segment;
+        state_store(unit ? a.phi + at * a.Dk * a.Dk : a.psi + at * state);
+    } else {
+        if (a.s_end && segment == a.segments - 1) state_store(a.s_end + (int64_t)head * state);
+    }
+}
+
+// The segments' starts of one head's strip, one from the other.
+template <typename T, int DK>
+__global__ __launch_bounds__(NT) void delta_join_kernel(WalkArgs a, float* starts) {
+    using I = Io<T>;
+    using E = typename I::Elem;
+    constexpr int P = I::kChain, NK = DK / I::kStep, DTL = DK / 16, SD = DTL < 4 ? 1 : DTL / 4;
+    constexpr int kKS = DK + I::kPad, kSPlane = SC * kKS;
+    __shared__ __attribute__((aligned(16))) E sS[P * kSPlane];
+    const int lane = threadIdx.x % kWave, ll = lane & 15, g = lane >> 4, w = wave_id();
+    const unsigned head = blockIdx.x / (unsigned)a.strips;
+    const int n0 = (int)(blockIdx.x - head * (unsigned)a.strips) * SC, width = a.Dv - n0;
+    const bool has_d = DTL >= 4 || w < DTL;
+    const int64_t state = (int64_t)a.Dk * a.Dv;
+    f4 S[SD];
+    auto offset = [&](int i, int e) {
+        return ll < width ? ((16 * (w + 4 * i) + 4 * g + e) * a.Dv + n0 + ll) * 4 : (int)kNowhere;
+    };
+    auto read = [&](const float* p, int i) {
+        const auto r = wtile::rsrc(p, (uint32_t)(state * 4));
+        f4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, offset(i, e), 0, 0));
+        return v;
+    };
+#pragma unroll
+    for (int i = 0; i < SD; ++i) {
+        S[i] = f4{0, 0, 0, 0};
+        if (a.s0 && has_d) S[i] = read(a.s0 + (int64_t)head * state, i);
+    }
+    constexpr int N = I::kStep / 4;  // a lane's values of a step
+    const bool vec = a.Dk % N == 0;
+    float x[SD][NK][N];
+    f4 psi[SD];
+    auto fetch = [&](int seg) {
+        const int64_t at = (int64_t)head * a.segments + seg;
+        const auto phi = wtile::rsrc(a.phi + at * a.Dk * a.Dk, (uint32_t)(a.Dk * a.Dk * 4));
+#pragma unroll
+        for (int i = 0; i < SD; ++i) {
+            psi[i] = read(a.psi + at * state, i);
+            const int row = 16 * (w + 4 * i) + ll;
+#pragma unroll
+            for (int s = 0; s < NK; ++s) {
+                const int d0 = s * I::kStep + N * g;
+                if (vec) {
+                    const int o = d0 < a.Dk ? (row * a.Dk + d0) * 4 : (int)kNowhere;
+#pragma unroll
+                    for (int e = 0; e < N; e += 4) {
+                        const f4 v = __builtin_bit_cast(
+                            f4, __builtin_amdgcn_raw_buffer_load_b128(phi, o + 4 * e, 0, 0));
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[i][s][e + j] = v[j];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        x[i][s][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+                            phi, d0 + e < a.Dk ? (row * a.Dk + d0 + e) * 4 : (int)kNowhere, 0, 0));
+                }
+            }
+        }
+    };
+    if (has_d && a.segments > 1) fetch(0);
+    for (int seg = 0; seg < a.segments; ++seg) {
+        const int64_t at = (int64_t)head * a.segments + seg;
+        if (has_d) {
+            const auto r = wtile::rsrc(starts + at * state, (uint32_t)(state * 4));
+#pragma unroll
+            for (int i = 0; i < SD; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[i][e]), r, offset(i, e),
+                                                          0, 0);
+                put<P>(sS, kSPlane, kKS, ll, 16 * (w + 4 * i) + 4 * g, S[i]);
+            }
+        }
+        lds_barrier();
+        if (seg + 1 < a.segments && has_d) {
+            typename I::template Made<P> op[SD][NK];
+#pragma unroll
+            for (int i = 0; i < SD; ++i) {
+                S[i] = psi[i];
+#pragma unroll
+                for (int s = 0; s < NK; ++s) {
+                    if constexpr (sizeof(T) == 4)
+                        op[i][s] = F32Op{{x[i][s][0], x[i][s][1], x[i][s][2], x[i][s][3]}};
+                    else
+                        op[i][s] = split<P>(x[i][s]);
+                }
+            }
+            // The last one has no Phi; what is read in its place is not used.
+            fetch(seg + 2 < a.segments ? seg + 1 : seg);
+#pragma unroll
+            for (int s = 0; s < NK; ++s) {
+                const auto st = made<P>(sS, kSPlane, kKS, ll, s * I::kStep, g);
+#pragma unroll
+                for (int i = 0; i < SD; ++i) S[i] = mma(S[i], op[i][s], st);
+            }
+        }
+        lds_barrier();
+    }
 }
 
 // ------------------------------------------------------------------ the outputs
@@ -608,6 +750,14 @@ __global__ __launch_bounds__(NT) void delta_out_kernel(SplitArgs a, const float*
 // ------------------------------------------------------------------ launches
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
+// Segments of a walk of `chunks` by `strips` workgroups in all: as many as give every compute
+// unit one (two were slower: 103 and 108 us for 16 segments of 16384 steps, see below), and none shorter than 8 chunks (cutting costs each segment a second walk and Phi's columns).
+int segments_of(int64_t chunks, int64_t strips) {
+    const int64_t most = chunks / 8, want = 256 / strips;
+    const int64_t n = most < want ? most : want;
+    return n < 3 ? 1 : (int)(n < 64 ? n : 64);
+}
+
 // Layout of the workspace; `bytes` in all.
 template <typename T, int DK>
 SplitWs layout(char* p, int64_t heads, int64_t L, int64_t chunks, int Dk, int Dv, bool bwd,
@@ -629,6 +779,12 @@ SplitWs layout(char* p, int64_t heads, int64_t L, int64_t chunks, int Dk, int Dv
     if (bwd) ws.bt = (float*)take(items * C * 4);
     if (own_x) ws.X = (float*)take((size_t)(heads * L * Dv) * 4);
     if (own_s) ws.S = (float*)take(items * Dk * Dv * 4);
+    const int64_t segs = segments_of(chunks, heads * (int64_t)strips);
+    if (segs > 1) {
+        ws.psi = (float*)take((size_t)(heads * segs) * Dk * Dv * 4);
+        ws.phi = (float*)take((size_t)(heads * segs) * Dk * Dk * 4);
+        ws.starts = (float*)take((size_t)(heads * segs) * Dk * Dv * 4);
+    }
     *bytes = at;
     return ws;
 }
@@ -649,9 +805,27 @@ hipError_t launch_prep(const SplitArgs& a, const SplitWs& ws, hipStream_t stream
     return hipGetLastError();
 }
 template <typename T, int DK, bool BWD>
-hipError_t launch_walk(const WalkArgs& a, int64_t heads, const SplitWs& ws, hipStream_t stream) {
-    hipLaunchKernelGGL((delta_walk_kernel<T, DK, BWD>), dim3((unsigned)(heads * a.strips)),
-                       dim3(NT), 0, stream, a, ws);
+hipError_t launch_walk(WalkArgs a, int64_t heads, const SplitWs& ws, hipStream_t stream) {
+    a.segments = segments_of(a.chunks, heads * a.strips);
+    a.per = (a.chunks + a.segments - 1) / a.segments;
+    a.segments = (a.chunks + a.per - 1) / a.per;
+    if (a.segments > 1) {
+        a.psi = ws.psi;
+        a.phi = ws.phi;
+        const int64_t strips = a.strips + (a.Dk + SC - 1) / SC;
+        hipLaunchKernelGGL((delta_walk_kernel<T, DK, BWD, true>),
+                           dim3((unsigned)(heads * (a.segments - 1) * strips)), dim3(NT), 0, stream,
+                           a, ws);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((delta_join_kernel<T, DK>), dim3((unsigned)(heads * a.strips)), dim3(NT),
+                           0, stream, a, ws.starts);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        a.s0 = ws.starts;
+    }
+    hipLaunchKernelGGL((delta_walk_kernel<T, DK, BWD, false>),
+                       dim3((unsigned)(heads * a.segments * a.strips)), dim3(NT), 0, stream, a, ws);
     return hipGetLastError();
 }
 
@@ -673,7 +847,7 @@ hipError_t forward(const DeltaFwdArgs& a, void* p, size_t* bytes, hipStream_t st
                        : launch_prep<T, DK, false, false>(s, ws, stream);
     if (e != hipSuccess) return e;
     e = launch_walk<T, DK, false>(WalkArgs{a.h0, a.hT, ws.S, nullptr, a.L, a.HV, a.Dk, a.Dv,
-                                           (int)chunks, strips},
+                                           (int)chunks, strips, 1, 0, nullptr, nullptr},
                                   heads, ws, stream);
     if (e != hipSuccess) return e;
     static std::atomic<uint64_t> set[2];
@@ -711,7 +885,7 @@ hipError_t backward(const DeltaBwdArgs& a, float* D, float* Y, void* p, size_t* 
                              : launch_prep<T, DK, true, false>(s, ws, stream);
     if (e != hipSuccess) return e;
     return launch_walk<T, DK, true>(WalkArgs{a.dhT, a.dh0, ws.S, a.dv, a.L, a.HV, a.Dk,
-                                             a.Dv, (int)chunks, strips},
+                                             a.Dv, (int)chunks, strips, 1, 0, nullptr, nullptr},
                                     heads, ws, stream);
 }
 
