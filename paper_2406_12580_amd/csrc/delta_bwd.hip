@@ -93,14 +93,12 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
 #pragma unroll
         for (int i = 0; i < SD; ++i)
 #pragma unroll
-            for (int j = 0; j < SN; ++j)
+            for (int j = 0; j < SN; ++j) {
+                const int n = state_n(j, ll);
+                const uint32_t o = n < width ? (uint32_t)(state_d(i, g) * Dv + n0 + n) * 4 : kNowhere;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int n = state_n(j, ll);
-                    const uint32_t o = n < width ? (uint32_t)((state_d(i, g) + e) * Dv + n0 + n) * 4
-                                                 : kNowhere;
-                    f(r, D[i][j], e, (int)o);
-                }
+                for (int e = 0; e < 4; ++e) f(r, D[i][j], e, (int)(o + (uint32_t)(4 * e * Dv)));
+            }
     };
     auto state_store = [&](float* p) {
         state_io(p, [](auto r, f4& s, int e, int o) {
@@ -280,10 +278,12 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
             for (int j = 0; j < NTL; ++j) {
                 const f4 dv = bt * Y[j];
                 put<L::kChain>(sm.x, L::kXPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, -eg * dv);
+                const uint32_t ov = rv.off(16 * w + 4 * g, 16 * j + ll, width);
+                const uint32_t oy = ry.off(16 * w + 4 * g, 16 * j + ll, width);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    rv.set(rv.off(16 * w + 4 * g + r, 16 * j + ll, width), dv[r]);
-                    ry.set(ry.off(16 * w + 4 * g + r, 16 * j + ll, width), Y[j][r]);
+                    rv.set(rv.next(ov, r), dv[r]);
+                    ry.set(ry.next(oy, r), Y[j][r]);
                 }
             }
         }
@@ -382,12 +382,12 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
         int64_t b, t0, qk_base;
         int h, c;
     };
-    auto item_at = [&](int64_t i) {
-        const int64_t bh = i / chunks;
+    auto item_at = [&](unsigned i) {
+        const unsigned bh = i / (unsigned)chunks, b = bh / (unsigned)a.H;
         Item o;
-        o.c = (int)(i - bh * chunks);
-        o.b = bh / a.H;
-        o.h = (int)(bh - o.b * a.H);
+        o.c = (int)(i - bh * (unsigned)chunks);
+        o.b = b;
+        o.h = (int)(bh - b * (unsigned)a.H);
         o.t0 = (int64_t)o.c * C;
         o.qk_base = (o.b * a.L * a.H + o.h) * Dk;
         return o;
@@ -444,10 +444,11 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
             const int ll = lane & 15, g = lane >> 4;
             const Rows<T> rv((const T*)a.v + v_base, it.t0, a.L, v_step, width);
 #pragma unroll
-            for (int j = 0; j < NTL; ++j)
+            for (int j = 0; j < NTL; ++j) {
+                const uint32_t o = rv.off(16 * w + 4 * g, 16 * j + ll, width);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    vn[j][r] = rv.get(rv.off(16 * w + 4 * g + r, 16 * j + ll, width));
+                for (int r = 0; r < 4; ++r) vn[j][r] = rv.get(rv.next(o, r));
+            }
         }
         if (wave == 4 && n0 == 0) {
             const int64_t t = it.t0 + lane, o = (it.b * a.L + t) * a.HV + hv;
@@ -469,11 +470,11 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
         }
     };
 
-    const int64_t items = a.B * a.H * chunks;
+    const unsigned items = (unsigned)(a.B * a.H * chunks);  // below 2^31
     Item next = item_at(blockIdx.x);
     fetch_qk(next);
     fetch(next, next.h * group, 0);
-    for (int64_t at = blockIdx.x; at < items; at += gridDim.x) {
+    for (unsigned at = blockIdx.x; at < items; at += gridDim.x) {
     const Item it = next;
     const int64_t b = it.b, t0 = it.t0, qk_base = it.qk_base;
     const int h = it.h;
@@ -705,12 +706,17 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
         auto emit = [&](const f4& v, void* out, float* part, int i, int ll, int g) {
             const Rows<T> ro((T*)out + qk_base, t0, a.L, qk_step, Dk);
             const Rows<float> rp(part + qk_base, t0, a.L, qk_step, Dk);
+            const uint32_t oo = ro.off(16 * w + 4 * g, 16 * i + ll, Dk);
+            const uint32_t op = rp.off(16 * w + 4 * g, 16 * i + ll, Dk);
+            f4 x = v;
+            if (!first) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) x[r] += rp.get(rp.next(op, r));
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                float x = v[r];
-                if (!first) x += rp.get(rp.off(16 * w + 4 * g + r, 16 * i + ll, Dk));
-                if (last) ro.set(ro.off(16 * w + 4 * g + r, 16 * i + ll, Dk), x);
-                else rp.set(rp.off(16 * w + 4 * g + r, 16 * i + ll, Dk), x);
+                if (last) ro.set(ro.next(oo, r), x[r]);
+                else rp.set(rp.next(op, r), x[r]);
             }
         };
         f4 x1 = {0, 0, 0, 0}, x2 = x1, KA[DTL];
@@ -846,7 +852,7 @@ hipError_t launch_grad(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t strea
 template <typename T, int DK>
 hipError_t launch_both(const DeltaBwdArgs& a, const BwdWs& ws, bool vec, hipStream_t stream) {
     size_t bytes;
-    const hipError_t e = delta_split(a.B * a.HV, a.L, a.Dv)
+    const hipError_t e = delta_split(a.B * a.HV, a.L, a.Dk, a.Dv)
                              ? launch_delta_split_backward(a, ws.D, ws.Y, ws.split, &bytes, stream)
                          : vec ? launch_state<T, DK, 32, true>(a, ws, stream)
                                : launch_state<T, DK, 32, false>(a, ws, stream);
@@ -881,7 +887,7 @@ size_t sum_bytes(int64_t B, int64_t L, int64_t H, int Dk) {
 size_t delta_backward_workspace(int64_t B, int64_t L, int64_t H, int64_t HV, int Dk, int Dv,
                                 IoType io) {
     size_t split = 0;
-    if (delta_split(B * HV, L, Dv)) {
+    if (delta_split(B * HV, L, Dk, Dv)) {
         DeltaBwdArgs a{};
         a.B = B;
         a.L = L;

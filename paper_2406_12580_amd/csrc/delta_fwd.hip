@@ -80,15 +80,13 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
 #pragma unroll
         for (int i = 0; i < SD; ++i)
 #pragma unroll
-            for (int j = 0; j < SN; ++j)
+            for (int j = 0; j < SN; ++j) {
+                const int n = state_n(j, ll);
+                // Rows behind Dk lie behind the buffer's end.
+                const uint32_t o = n < width ? (uint32_t)(state_d(i, g) * Dv + n0 + n) * 4 : kNowhere;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int n = state_n(j, ll);
-                    // Rows behind Dk lie behind the buffer's end.
-                    const uint32_t o = n < width ? (uint32_t)((state_d(i, g) + e) * Dv + n0 + n) * 4
-                                                 : kNowhere;
-                    f(r, S[i][j], e, (int)o);
-                }
+                for (int e = 0; e < 4; ++e) f(r, S[i][j], e, (int)(o + (uint32_t)(4 * e * Dv)));
+            }
     };
     auto state_store = [&](float* p) {
         state_io(p, [](auto r, f4& s, int e, int o) {
@@ -137,10 +135,11 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
             qn[s] = rq.template get16<VEC>(16 * w + ll, s * I::kStep + I::kUnit * g, Dk);
         const Rows<T> rv(vp, (int64_t)c * C, a.L, v_step, width);
 #pragma unroll
-        for (int j = 0; j < NTL; ++j)
+        for (int j = 0; j < NTL; ++j) {
+            const uint32_t o = rv.off(16 * w + 4 * g, 16 * j + ll, width);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                vn[j][r] = rv.get(rv.off(16 * w + 4 * g + r, 16 * j + ll, width));
+            for (int r = 0; r < 4; ++r) vn[j][r] = rv.get(rv.next(o, r));
+        }
     };
     if (chunks > 0) {
         fetch_k(0);
@@ -175,28 +174,38 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
                 kw[s] = given(sm.k, L::kKS, 16 * w + ll, s * I::kStep, g);
                 qw[s] = __builtin_bit_cast(typename I::Given, qn[s]);
             }
+            // Each step's operands are read while the one before is multiplied.
+            typename I::Given kt[2][NK];
+            auto read_k = [&](int t) {
+#pragma unroll
+                for (int s = 0; s < NK; ++s)
+                    kt[t & 1][s] = given(sm.k, L::kKS, 16 * t + ll, s * I::kStep, g);
+            };
+            read_k(0);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 M[t] = P[t] = f4{0, 0, 0, 0};
+                if (t < 3) read_k(t + 1);
 #pragma unroll
                 for (int s = 0; s < NK; ++s) {
-                    const auto kt = given(sm.k, L::kKS, 16 * t + ll, s * I::kStep, g);
-                    M[t] = mma(M[t], kt, kw[s]);
-                    P[t] = mma(P[t], kt, qw[s]);
+                    M[t] = mma(M[t], kt[t & 1][s], kw[s]);
+                    P[t] = mma(P[t], kt[t & 1][s], qw[s]);
                 }
                 step_end(P[t]);
             }
+            typename I::template Made<L::kChain> st[2];
+            auto read_s = [&](int u) {
+                st[u & 1] = made<L::kChain>(sm.x, L::kSPlane, L::kKS, 16 * (u / NK) + ll,
+                                            u % NK * I::kStep, g);
+            };
+            read_s(0);
 #pragma unroll
-            for (int j = 0; j < NTL; ++j) {
-                KS[j] = O[j] = f4{0, 0, 0, 0};
-#pragma unroll
-                for (int s = 0; s < NK; ++s) {
-                    const auto st = made<L::kChain>(sm.x, L::kSPlane, L::kKS, 16 * j + ll,
-                                                    s * I::kStep, g);
-                    KS[j] = mma(KS[j], kw[s], st);
-                    O[j] = mma(O[j], qw[s], made<L::kOut>(sm.x, L::kSPlane, L::kKS, 16 * j + ll,
-                                                          s * I::kStep, g));
-                }
+            for (int u = 0; u < NTL * NK; ++u) {
+                const int j = u / NK, s = u % NK;
+                if (s == 0) KS[j] = O[j] = f4{0, 0, 0, 0};
+                if (u + 1 < NTL * NK) read_s(u + 1);
+                KS[j] = mma(KS[j], kw[s], st[u & 1]);
+                O[j] = mma(O[j], qw[s], fewer<L::kOut>(st[u & 1]));
                 step_end(O[j]);
             }
             const int i = 16 * w + ll;
@@ -283,10 +292,11 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
             }
         const Rows<T> ro(op, (int64_t)c * C, a.L, v_step, width);
 #pragma unroll
-        for (int j = 0; j < NTL; ++j)
+        for (int j = 0; j < NTL; ++j) {
+            const uint32_t o = ro.off(16 * w + 4 * g, 16 * j + ll, width);
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                ro.set(ro.off(16 * w + 4 * g + r, 16 * j + ll, width), a.scale * O[j][r]);
+            for (int r = 0; r < 4; ++r) ro.set(ro.next(o, r), a.scale * O[j][r]);
+        }
     }
     if (a.hT) state_store(a.hT + head * Dk * Dv);
 }
@@ -322,7 +332,7 @@ hipError_t launch_typed(const DeltaFwdArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t delta_forward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv, IoType io) {
-    if (!delta_split(B * HV, L, Dv)) return 0;
+    if (!delta_split(B * HV, L, Dk, Dv)) return 0;
     DeltaFwdArgs a{};
     a.B = B;
     a.L = L;
@@ -337,7 +347,7 @@ size_t delta_forward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv,
 
 hipError_t launch_delta_forward(const DeltaFwdArgs& a, void* ws, hipStream_t stream) {
     size_t bytes;
-    if (delta_split(a.B * a.HV, a.L, a.Dv)) return launch_delta_split_forward(a, ws, &bytes, stream);
+    if (delta_split(a.B * a.HV, a.L, a.Dk, a.Dv)) return launch_delta_split_forward(a, ws, &bytes, stream);
     return a.io == IoType::kF32 ? launch_typed<float>(a, stream) : launch_typed<bf16>(a, stream);
 }
 

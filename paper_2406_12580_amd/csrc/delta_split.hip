@@ -903,8 +903,18 @@ hipError_t by_type(IoType io, int Dk, F f) {
 
 }  // namespace
 
-bool delta_split(int64_t heads, int64_t L, int Dv) {
-    return heads * ((Dv + 31) / 32) < 256 && L > 2 * C;
+// Which way is the faster one, by what the two cost (us, fitted to 50 measured sizes of both,
+// forward): the walk in one kernel 9 for each chunk and each 512 strips of 32 columns; here 16
+// (36 from 65 columns of K on) for the launches, 2 a chunk of the walk, and 0.034 (0.1) for each
+// chunk of every head.  128 heads, 64 x 64, 1000 steps: 152 and 113 us; 400 heads, 200 steps:
+// 52 and 108 us; 60 heads, 128 x 128, 500 steps: 69 and 78 us; 4 heads, 16384 steps: 2040 us and
+// 290 us (a long walk is cut as well).
+bool delta_split(int64_t heads, int64_t L, int Dk, int Dv) {
+    const double chunks = (double)((L + C - 1) / C), strips = (double)(heads * ((Dv + 31) / 32));
+    const double one = 9.0 * chunks * (strips <= 512.0 ? 1.0 : strips / 512.0);
+    const bool wide = Dk > 64;
+    const double walk = chunks < 24.0 ? 2.0 * chunks : 48.0 + 0.4 * (chunks - 24.0);
+    return (wide ? 36.0 : 16.0) + walk + (wide ? 0.1 : 0.034) * (double)heads * chunks < one;
 }
 
 hipError_t launch_delta_split_forward(const DeltaFwdArgs& a, void* ws, size_t* bytes,

@@ -87,6 +87,17 @@ __device__ __forceinline__ f4 mma(f4 c, const Bf16Op<PA>& a, const Bf16Op<PB>& b
     return c;
 }
 
+// The first planes of an operand.
+template <int P>
+__device__ __forceinline__ F32Op fewer(const F32Op& a) { return a; }
+template <int P, int Q>
+__device__ __forceinline__ Bf16Op<P> fewer(const Bf16Op<Q>& a) {
+    Bf16Op<P> o;
+#pragma unroll
+    for (int i = 0; i < P; ++i) o.p[i] = a.p[i];
+    return o;
+}
+
 // Eight floats as planes.
 template <int P>
 __device__ __forceinline__ Bf16Op<P> split(const float (&x)[8]) {
@@ -217,7 +228,7 @@ __device__ __forceinline__ typename Io<T>::template Made<P> from_acc(const f4* a
 // A chunk's rows of one head, as a buffer: row r, element e at byte (r step + e) sizeof(T).
 // Accesses outside of the rows that exist read zeros and write nothing, so no branch guards
 // them; elements behind a row's end (the next head's) have to be sent out of range by `off`.
-constexpr uint32_t kNowhere = 0x7FFFFFF0u;  // an offset behind every buffer's end
+constexpr uint32_t kNowhere = 0x7F000000u;  // an offset behind every buffer's end
 
 template <typename T>
 struct Rows {
@@ -235,6 +246,9 @@ struct Rows {
     __device__ __forceinline__ uint32_t off(int row, int e, int width) const {
         return e < width ? (uint32_t)row * step + (uint32_t)e * (uint32_t)sizeof(T) : kNowhere;
     }
+    // Element e of row `row` and of those behind it, by adding r * step (an offset out of range
+    // stays there: four rows of the largest tensors are below 2^24 bytes).
+    __device__ __forceinline__ uint32_t next(uint32_t o, int r) const { return o + (uint32_t)r * step; }
     __device__ __forceinline__ float get(uint32_t o) const {
         if constexpr (sizeof(T) == 4)
             return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)o, 0, 0));
@@ -311,7 +325,7 @@ __device__ __forceinline__ void gates_of_chunk(Gates* gt, float g, float beta, f
 // Wave w inverts its own diagonal tile.  Lane column ll; A's rows are read by all lanes alike.
 __device__ __forceinline__ void invert_diagonal(float* tm, int w, int ll, int g) {
     float* b = tm + 16 * w * TS + 16 * w;
-    float x[16];
+    wtile::f16v x;  // a vector: selects among an array's elements would put it into memory
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         float s = i == ll ? 1.0f : 0.0f;
@@ -325,12 +339,18 @@ __device__ __forceinline__ void invert_diagonal(float* tm, int w, int ll, int g)
         x[i] = s;
         // Taken through here, x is formed before the next rows' reads: all 30 of them in flight
         // at once would cost 120 registers.
-        if (i % 4 == 3) asm volatile("" : "+v"(x[i]) : : "memory");
+        if (i % 4 == 3) {
+            asm volatile("" : "+v"(s) : : "memory");
+            x[i] = s;
+        }
     }
     wave_fence();
+    // Each group of 16 lanes writes four of the rows.
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if ((i >> 2) == g) b[i * TS + ll] = x[i];
+    for (int r = 0; r < 4; ++r) {
+        const float lo = g & 1 ? x[4 + r] : x[r], hi = g & 1 ? x[12 + r] : x[8 + r];
+        b[(4 * g + r) * TS + ll] = g & 2 ? hi : lo;
+    }
 }
 
 // Tile product with B as it lies in memory ([k][column]).
