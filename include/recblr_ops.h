@@ -34,7 +34,10 @@ extern "C" {
  * INVALID_ARGUMENT).  g is the logarithm of the decay, usually <= 0; below -100
  * it counts as -100, so -inf clears the state.  A step with g = 0 and beta = 0
  * leaves the state as it is (padding); queries and keys are taken as given
- * (they are usually brought to length one by the caller).
+ * (they are usually brought to length one by the caller).  Inputs are finite, in
+ * padding too (g may be -inf): steps are worked on 64 at a time, and a NaN or an
+ * infinity reaches the outputs of its whole group of 64 steps, those before it
+ * among them, and what follows; other rows and heads are not touched by it.
  */
 enum { RECBLR_OP_DELTA_FORWARD = 16, RECBLR_OP_DELTA_BACKWARD = 17 };
 

@@ -117,15 +117,18 @@ __device__ __forceinline__ double value2(double s, int c) {
 }
 
 // A block's scale as the encoders use it: whether it is positive (else all codes are the
-// lowest), a power of two that brings a tiny one into the range of v_rcp_f32, and the inverse.
+// lowest), a power of two that brings tiny and huge ones (and, in 64 bits, the moments with
+// them) to where neither they nor their inverse are denormal, and that inverse.
 struct Scale {
-    float s, up, inv;
+    float s, inv;
+    double up;
     bool some;
     __device__ __forceinline__ explicit Scale(float scale) {
         s = scale;
         some = s > 0.0f;
-        up = s < 1e-20f ? 0x1p66f : 1.0f;
-        inv = fast_rcp(s * up);
+        const float by = s < 1e-20f ? 0x1p66f : s > 1e20f ? 0x1p-66f : 1.0f;
+        up = by;
+        inv = fast_rcp(s * by);
     }
 };
 
@@ -134,7 +137,7 @@ struct Scale {
 // 127)^2, is decided in 64 bits.  IEEE division and roots here cost 45 instructions more.
 __device__ __forceinline__ int code1(double m, const Scale& s) {
     const double a = fabs(m);
-    int c = (int)rintf(127.0f * fast_sqrt((float)a * s.up * s.inv));
+    int c = (int)rintf(127.0f * fast_sqrt((float)(a * s.up) * s.inv));
     c = c < 0 ? 0 : c > 127 ? 127 : c;
     const double x = a * 16129.0, up = c + 0.5, dn = c - 0.5;
     const bool more = x > (double)s.s * (up * up), less = x < (double)s.s * (dn * dn);
@@ -144,7 +147,7 @@ __device__ __forceinline__ int code1(double m, const Scale& s) {
 }
 // The same for v: borders s ((c + 1 +- 1/2) / 256)^4.
 __device__ __forceinline__ int code2(double v, const Scale& s) {
-    int c = (int)rintf(256.0f * fast_sqrt(fast_sqrt((float)v * s.up * s.inv)));
+    int c = (int)rintf(256.0f * fast_sqrt(fast_sqrt((float)(v * s.up) * s.inv)));
     c = c < 1 ? 1 : c > 256 ? 256 : c;
     const double x = v * 0x1p32;
     const double up = (c + 0.5) * (c + 0.5), dn = (c - 0.5) * (c - 0.5);

@@ -502,10 +502,10 @@ def _on_device(fn):
     @functools.wraps(fn)
     def wrapper(first, *args, stream=None, **kwargs):
         dev = first.device
-        if stream is None and dev.index == torch._C._cuda_getDevice():
-            return fn(first, *args, **kwargs)
         if dev.type != "cuda":
             raise ValueError("tensors must live on the GPU")
+        if stream is None and dev.index == torch._C._cuda_getDevice():
+            return fn(first, *args, **kwargs)
         if stream is not None and stream.device != dev:
             raise ValueError("stream belongs to another device than the tensors")
         with torch.cuda.device(dev), torch.cuda.stream(stream):
@@ -563,7 +563,8 @@ def delta_forward(q, k, v, g, beta, h0=None, scale=None, keep_states=False):
     """Gated delta rule over whole sequences: q, k [B,L,H,Dk], v [B,L,HV,Dv], log decays g and
     strengths beta [B,L,HV], h0 [B,HV,Dk,Dv] float32.  Returns (o [B,L,HV,Dv], hT float32,
     states), states (None unless keep_states) being what delta_backward needs of the forward:
-    [B,HV,ceil(L/64),Dk,Dv] float32.  scale defaults to Dk ** -0.5."""
+    [B,HV,ceil(L/64),Dk,Dv] float32.  scale defaults to Dk ** -0.5.  Padded steps (g = beta = 0)
+    leave the state alone; their q, k and v must be finite, like all inputs."""
     sizes, io, ptrs = _delta_inputs(q, k, v, g, beta)
     B, L, H, HV, Dk, Dv = sizes
     dev, at, f32 = q.device, q.get_device(), torch.float32
@@ -654,7 +655,8 @@ class AdamW:
     s2).  `state` takes over moments that exist: (m1, m2) or (m1, m2, s1, s2), lists of tensors
     with as many elements as the parameters (the scales ceil(n / 256)); `step` counts the
     updates already made.  step(grads) updates parameters and moments in place, on the
-    parameters' device; gradients have the parameters' type and number of elements."""
+    parameters' device; gradients have the parameters' type and number of elements.  A captured
+    step replays with the bias corrections, rates and addresses of its capture."""
 
     def __init__(self, params, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
                  state_bits=32, state=None, step=0):
@@ -704,6 +706,7 @@ class AdamW:
         for entry, n, w in zip(self._table, sizes, decay):
             entry.n, entry.weight_decay = n, w
         self._sizes = sizes
+        self._at = [p.data_ptr() for p in self.params]
         # The table's gradient addresses, as one array to assign.
         self._grads = np.frombuffer(self._table, dtype=np.uint64).reshape(len(sizes), -1)[
             :, AdamWTensor.grad.offset // 8]
@@ -726,11 +729,17 @@ class AdamW:
                 self._flat(t, dtype, n, "grads")  # says what is wrong
             ptrs.append(t.data_ptr())
         self._grads[:] = ptrs
+        at = [p.data_ptr() for p in self.params]
+        if at != self._at:  # a parameter's memory was replaced (p.data = ...)
+            for entry, p, n in zip(self._table, self.params, self._sizes):
+                entry.param = self._flat(p, dtype, n, "params")
+            self._at = at
         _adamw_step(self, self.lr if lr is None else lr, stream=stream)
         self.steps += 1
 
     def moments(self, out=None, stream=None):
-        """The moments as float32: (m1, m2), lists of tensors; out takes them where given."""
+        """The moments as float32: (m1, m2), lists of tensors; out takes them where given
+        (without it, 32-bit moments are the optimiser's own tensors, no copies)."""
         if self.state_bits == 32:
             if out is None:
                 return list(self.m1), list(self.m2)

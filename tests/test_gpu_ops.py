@@ -1,0 +1,752 @@
+"""The operators of recblr_ops.h on the GPU against 64-bit references (ops_reference.py).
+
+Error metric: max |got - want| / (|want| + rms(want)) of each output, as in helpers.py.
+
+Tolerances, from the arithmetic:
+
+* Gated delta rule, fp32: every product is a sum of at most n = Dk + 64 terms (a row of K with
+  the state, and a chunk), each rounded once, so off by at most n 2^-24 of its terms' size; six
+  such products stand behind one another (state, right-hand side, inverse, update, state,
+  output or gradient): 6 n 2^-24.  dg is a running sum of up to 64 differences of such
+  products, most of which cancel: 4 times that.
+* bf16 tensors: rounding 2^-8 of the value at most, and products of two 16-bit planes (2^-16 of
+  each operand, six products): 2^-8 + 6 * 2^-16 < 2^-8 + 2^-13.  dg as above: 64 differences of
+  which each is off by 2^-16 of terms about as large as dg's largest: 2^-8 + 2^-10.  The float
+  states come from three planes (2^-24): the fp32 bar.
+* AdamW: m is a sum of two terms that may cancel, so the step's error counts their sizes, not
+  their difference.  Roundings of the step in fp32: 4 of m (both factors, a product, the sum),
+  3 of sqrt(v) (6 of v, which cannot cancel, halved), the corrections 2, root, eps, its sum,
+  product and quotient 5: 14 * 2^-24 of that size.  Of the parameter: 1 - lr wd, the product,
+  the result: 3 * 2^-24; a bf16 one 2^-8 more.  Moments in float: 4 * 2^-24 of the terms.  8-bit
+  codes are the nearest ones, decided in 64 bits.
+* Sampling: ids are equal; probabilities are rounded to float once.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import ops_reference as ref
+from helpers import floored_rel_err
+
+pytestmark = pytest.mark.gpu
+
+U32, BF16 = 2.0 ** -24, 2.0 ** -8
+
+
+@pytest.fixture(scope="module")
+def rb():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2406_12580_amd import recblr
+    return recblr
+
+
+def dtype_of(io):
+    import torch
+    return torch.float32 if io == "f32" else torch.bfloat16
+
+
+def put(a, io):
+    """A numpy array on the GPU in the I/O type, and what it stands for in 64 bits."""
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).to(dtype_of(io)).cuda()
+    return t, t.double().cpu().numpy()
+
+
+def put32(a):
+    import torch
+    if a is None:
+        return None, None
+    t = torch.from_numpy(np.ascontiguousarray(a)).float().cuda()
+    return t, t.double().cpu().numpy()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+# ------------------------------------------------------------------ gated delta rule
+
+def delta_case(io, B, L, H, HV, Dk, Dv, state=True, seed=0, decay=0.3):
+    r = np.random.default_rng(seed)
+    unit = lambda x: x / np.linalg.norm(x, axis=-1, keepdims=True)  # noqa: E731
+    c = {}
+    for name, a in (("q", unit(r.normal(size=(B, L, H, Dk)))),
+                    ("k", unit(r.normal(size=(B, L, H, Dk)))),
+                    ("v", r.normal(size=(B, L, HV, Dv))),
+                    ("g", -decay * r.random((B, L, HV))), ("beta", r.random((B, L, HV))),
+                    ("do", r.normal(size=(B, L, HV, Dv)))):
+        c[name], c[name + "_"] = put(a, io)
+    for name in ("h0", "dhT"):
+        c[name], c[name + "_"] = put32(0.5 * r.normal(size=(B, HV, Dk, Dv)) if state else None)
+    return c
+
+
+def delta_bars(io, Dk):
+    f32 = 6 * (Dk + 64) * U32
+    if io == "f32":
+        return {"out": f32, "state": f32, "dg": 4 * f32}
+    return {"out": BF16 + 2.0 ** -13, "state": f32, "dg": BF16 + 2.0 ** -10}
+
+
+def close(name, got, want, bar):
+    got = host(got)
+    assert got.shape == want.shape, name
+    assert np.isfinite(got).all(), name
+    err = floored_rel_err(got, want)
+    print(f"ERR {name}: {err:.2e} of {bar:.2e}", flush=True)
+    assert err <= bar, f"{name}: {err:.3e} > {bar:.3e}"
+
+
+def run_delta(rb, c, grads=True, scale=None):
+    a = tuple(c[n] for n in ("q", "k", "v", "g", "beta"))
+    o, hT, states = rb.delta_forward(*a, h0=c["h0"], scale=scale, keep_states=True)
+    out = {"o": o, "hT": hT, "states": states}
+    if grads:
+        out.update(rb.delta_backward(*a, states, c["do"], dhT=c["dhT"], scale=scale))
+    return out
+
+
+def check_delta(rb, io, c, scale=None):
+    out = run_delta(rb, c, scale=scale)
+    want = ref.delta(*(c[n + "_"] for n in ("q", "k", "v", "g", "beta")), h0=c["h0_"],
+                     do=c["do_"], dhT=c["dhT_"], scale=scale)
+    bars = delta_bars(io, c["q"].shape[-1])
+    for name in ("o", "hT", "dq", "dk", "dv", "dg", "dbeta", "dh0"):
+        kind = "state" if name in ("hT", "dh0") else "dg" if name == "dg" else "out"
+        close(name, out[name], want[name], bars[kind])
+    L = c["q"].shape[1]
+    kept = np.stack([want["kept"][t] for t in range(0, L, 64)], axis=2)
+    close("states", out["states"], kept, bars["state"])
+
+
+# Lengths around a chunk, one step, and long enough for every way to walk; head widths from one
+# to 128, odd ones; shared and unshared heads.
+SIZES = [
+    (1, 1, 1, 1, 1, 1), (2, 1, 1, 2, 17, 40), (3, 2, 2, 2, 32, 32), (1, 63, 1, 1, 33, 5),
+    (2, 64, 1, 2, 64, 64), (1, 65, 2, 6, 16, 31), (2, 128, 1, 1, 128, 128), (1, 129, 1, 3, 72, 100),
+    (1, 200, 2, 4, 64, 64), (2, 300, 1, 2, 128, 96), (1, 700, 1, 2, 40, 33), (1, 1700, 1, 1, 64, 48),
+    (1, 1601, 1, 2, 100, 128), (70, 130, 2, 2, 64, 64), (40, 70, 1, 4, 128, 65),
+]
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", SIZES)
+def test_delta(rb, io, size):
+    print(io, size, flush=True)
+    check_delta(rb, io, delta_case(io, *size))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_delta_without_state(rb, io):
+    """No initial state, no gradient of the final one: both count as zero."""
+    c = delta_case(io, 2, 100, 1, 2, 64, 64, state=False)
+    check_delta(rb, io, c, scale=0.7)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [150, 1700])
+def test_delta_padding(rb, io, L):
+    """Steps with g = 0 and beta = 0 leave the state alone, whatever their keys and values."""
+    import torch
+    c = delta_case(io, 3, L, 1, 2, 64, 64, seed=3)
+    for b, n in enumerate((0, 70, L)):  # left padding; the last row is nothing else
+        for name in ("g", "beta"):
+            c[name][b, :n] = 0
+            c[name + "_"][b, :n] = 0
+    check_delta(rb, io, c)
+    o, hT, _ = rb.delta_forward(*(c[n] for n in ("q", "k", "v", "g", "beta")), h0=c["h0"])
+    assert torch.equal(hT[2], c["h0"][2])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [130, 1700])
+def test_delta_strong_decay(rb, io, L):
+    """Decays that clear the state, -inf among them, next to weak ones: what is left of a chunk
+    keeps its precision (running sums of thousands, differences of hundredths)."""
+    c = delta_case(io, 2, L, 1, 2, 64, 64, seed=4, decay=0.02)
+    for t, x in ((5, -60.0), (40, -math.inf), (41, -1e30), (90, -200.0), (L - 3, -math.inf)):
+        c["g"][:, t] = x
+        c["g_"][:, t] = max(x, -300.0)
+    check_delta(rb, io, c)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_delta_alike_keys(rb, io):
+    """Keys that are nearly the same make the chunk's triangular system as far from the unit
+    matrix as it gets (entries near beta); strengths up to two."""
+    c = delta_case(io, 1, 256, 1, 1, 32, 32, seed=5, decay=0.01)
+    base = c["k_"][0, 0, 0]
+    k = base + 0.05 * np.random.default_rng(6).normal(size=c["k_"].shape)
+    c["k"], c["k_"] = put(k / np.linalg.norm(k, axis=-1, keepdims=True), io)
+    c["beta"], c["beta_"] = put(0.9 + 0.9 * c["beta_"] * (np.arange(256) % 7 == 0)[None, :, None], io)
+    check_delta(rb, io, c)
+
+
+def test_delta_nan_stays_in_its_row(rb):
+    """Other rows, other heads and earlier chunks know nothing of a NaN; within its chunk it
+    reaches all steps, as documented (0 times NaN in the chunk's triangular products)."""
+    import torch
+    c = delta_case("f32", 3, 200, 1, 2, 64, 64)
+    good = run_delta(rb, c)
+    c["v"][1, 150, 0, 3] = math.nan
+    bad = run_delta(rb, c)
+    for name in ("o", "hT", "dq", "dk", "dv", "dg", "dbeta", "dh0"):
+        assert torch.equal(good[name][0], bad[name][0]) and torch.equal(good[name][2], bad[name][2])
+    assert torch.isnan(bad["o"][1, 150:, 0, 3]).all() and torch.isfinite(bad["o"][1, :, 1]).all()
+    assert torch.equal(bad["o"][1, :128], good["o"][1, :128])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 200, 2, 4, 64, 64), (1, 1700, 1, 2, 128, 64)])
+def test_delta_repeats_and_graph(rb, io, size):
+    """Bitwise repeatable; a captured graph gives the eager results on every replay, with other
+    work in between."""
+    import torch
+    c = delta_case(io, *size)
+    want = run_delta(rb, c)
+    names = ("o", "hT", "dq", "dk", "dv", "dg", "dbeta", "dh0")
+    again = run_delta(rb, c)
+    assert all(torch.equal(want[n], again[n]) for n in names)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        run_delta(rb, c)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run_delta(rb, c)
+    for _ in range(3):
+        for n in names:
+            got[n].fill_(7.0)
+        run_delta(rb, c)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(want[n], got[n]) for n in names)
+
+
+def test_delta_two_streams(rb):
+    """Two problems at once, each on its stream: as one after the other."""
+    import torch
+    cases = [delta_case("bf16", 4, 300, 1, 2, 64, 64, seed=s) for s in (1, 2)]
+    want = [run_delta(rb, c) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for c, s in zip(cases, streams):
+        a = tuple(c[n] for n in ("q", "k", "v", "g", "beta"))
+        o, hT, st = rb.delta_forward(*a, h0=c["h0"], keep_states=True, stream=s)
+        got.append({"o": o, "hT": hT,
+                    **rb.delta_backward(*a, st, c["do"], dhT=c["dhT"], stream=s)})
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        assert all(torch.equal(w[n], g[n]) for n in g)
+
+
+def test_delta_unaligned_tensors(rb):
+    """Tensors that start two bytes behind a multiple of 16."""
+    import torch
+    c = delta_case("bf16", 2, 150, 1, 2, 64, 64)
+    want = run_delta(rb, c)
+
+    def moved(t):
+        buf = torch.empty(t.numel() + 1, dtype=t.dtype, device=t.device)
+        buf[1:].copy_(t.reshape(-1))
+        return buf[1:].view(t.shape)
+
+    m = {n: moved(t) if n in ("q", "k", "v", "g", "beta", "do") else t for n, t in c.items()}
+    got = run_delta(rb, m)
+    for n in ("o", "hT", "dq", "dk", "dv", "dg", "dbeta", "dh0"):
+        assert torch.equal(want[n], got[n]), n
+
+
+def test_delta_empty(rb):
+    import torch
+    c = delta_case("f32", 2, 5, 1, 2, 8, 8)
+    cut = {n: (t[:, :0] if n in ("q", "k", "v", "g", "beta", "do") else t) for n, t in c.items()}
+    cut = {n: t.contiguous() if isinstance(t, torch.Tensor) else t for n, t in cut.items()}
+    out = run_delta(rb, cut)
+    assert torch.equal(out["hT"], c["h0"]) and torch.equal(out["dh0"], c["dhT"])
+    assert out["o"].numel() == 0 and out["states"].shape[2] == 0
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 1, 1, 1, 1), (3, 1, 2, 17, 40), (8, 2, 4, 128, 128),
+                                  (5, 1, 3, 72, 100), (300, 2, 2, 64, 64), (2, 1, 1, 32, 33),
+                                  (4, 1, 2, 33, 64)])
+def test_delta_step(rb, io, size):
+    import torch
+    B, H, HV, Dk, Dv = size
+    print(io, size, flush=True)
+    c = delta_case(io, B, 1, H, HV, Dk, Dv)
+    one = {n: c[n][:, 0].contiguous() for n in ("q", "k", "v", "g", "beta")}
+    o, h = rb.delta_step(*one.values(), c["h0"])
+    want = ref.delta(*(c[n + "_"] for n in ("q", "k", "v", "g", "beta")), h0=c["h0_"])
+    bars = delta_bars(io, Dk)
+    close("o", o, want["o"][:, 0], bars["out"])
+    close("h", h, want["hT"], bars["state"])
+    state = c["h0"].clone()
+    o2, h2 = rb.delta_step(*one.values(), state, out=state)      # in place
+    assert h2.data_ptr() == state.data_ptr()
+    assert torch.equal(state, h) and torch.equal(o2, o)
+
+
+def test_delta_step_continues_forward(rb):
+    """A prefix by the forward, the rest step by step: the whole forward."""
+    import torch
+    c = delta_case("f32", 2, 80, 1, 2, 64, 32)
+    a = [c[n] for n in ("q", "k", "v", "g", "beta")]
+    o, hT, _ = rb.delta_forward(*a, h0=c["h0"])
+    got, h, _ = rb.delta_forward(*(t[:, :70].contiguous() for t in a), h0=c["h0"])
+    outs = [got]
+    for t in range(70, 80):
+        s, h = rb.delta_step(*(x[:, t].contiguous() for x in a), h, out=h)
+        outs.append(s[:, None])
+    bar = delta_bars("f32", 64)["state"]
+    close("o", torch.cat(outs, 1), host(o), 2 * bar)
+    close("hT", h, host(hT), 2 * bar)
+
+
+def test_delta_binding_refuses(rb):
+    import torch
+    c = delta_case("f32", 2, 8, 1, 2, 8, 8)
+    a = [c[n] for n in ("q", "k", "v", "g", "beta")]
+    with pytest.raises(ValueError):
+        rb.delta_forward(*a[:2], a[2].transpose(0, 1), *a[3:])
+    with pytest.raises(ValueError):
+        rb.delta_forward(a[0].bfloat16(), *a[1:])
+    with pytest.raises(ValueError):
+        rb.delta_forward(*a, h0=c["h0"].double())
+    with pytest.raises(ValueError):
+        rb.delta_forward(*a, h0=c["h0"].transpose(2, 3))     # Dk = Dv: only the order is wrong
+    with pytest.raises(ValueError):
+        rb.delta_backward(*a, c["h0"], c["do"])
+    with pytest.raises(TypeError):
+        rb.delta_forward(*(t.half() for t in a))
+    wide = delta_case("f32", 1, 2, 1, 1, 130, 8)
+    with pytest.raises(rb.RecblrError):
+        rb.delta_forward(*(wide[n] for n in ("q", "k", "v", "g", "beta")))
+
+
+# ------------------------------------------------------------------ AdamW
+
+HYPER = dict(lr=1e-2, beta1=0.9, beta2=0.99, eps=1e-8)
+
+
+def adamw_case(io, sizes, seed=0, shift=0):
+    """Parameters and gradients of the given sizes, views `shift` elements into a buffer."""
+    import torch
+    r = np.random.default_rng(seed)
+
+    def make(scale):
+        out = []
+        for n in sizes:
+            buf = torch.zeros(n + shift, dtype=dtype_of(io), device="cuda")
+            buf[shift:] = torch.from_numpy(scale * r.normal(size=n)).to(dtype_of(io)).cuda()
+            out.append(buf[shift:])
+        return out
+    return make(0.5), lambda: make(1e-2)
+
+
+def check_codes(m, v, c1, c2, s1, s2):
+    """Codes and scales of the 64-bit moments m, v: the scale is the block's largest rounded to
+    float, a code the nearest on the root's scale.  Borders count to 2^-38: with beta1 = 0.9, m
+    is (9 s + g) / 10 of two floats, which often lies between two floats to within a rounding
+    in 64 bits, where both neighbours are right."""
+    n, near = len(m), 1 + 2.0 ** -38
+    for x, c, s, steps, root in ((np.abs(m), np.abs(host(c1)), s1, 127, 2),
+                                 (v, host(c2) + 1, s2, 256, 4)):
+        s = host(s)
+        top = np.pad(x, (0, -n % 256)).reshape(-1, 256).max(1)
+        assert np.all(np.abs(s - top) <= U32 * near * top + 2.0 ** -150)
+        assert np.array_equal(s, s.astype(np.float32))
+        wide = np.repeat(s, 256)[:n]
+        with np.errstate(divide="ignore", invalid="ignore"):
+            at = np.where(wide > 0, steps * (x / wide) ** (1 / root), 0)
+        least = 0 if root == 2 else 1
+        assert np.all(np.abs(np.clip(at, least, steps) - c) <= 0.5 * near)
+    assert np.all((host(c1) == 0) | (np.sign(host(c1)) == np.sign(m)))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("sizes,shift", [
+    ([1], 0), ([1, 2, 3, 4, 5, 255, 256, 257], 0), ([1023, 4095, 4096, 4097, 0, 9000], 0),
+    ([7, 1000, 33], 1), ([5 + 3 * i for i in range(100)], 0)])
+def test_adamw(rb, io, bits, sizes, shift):
+    """Several steps: each is checked from the state that the one before has left."""
+    print(io, bits, sizes[:8], shift, flush=True)
+    params, grads = adamw_case(io, sizes, shift=shift)
+    decay = [0.1 * (i % 3) for i in range(len(sizes))]
+    opt = rb.AdamW(params, weight_decay=decay, state_bits=bits, **HYPER)
+    for t in range(1, 4):
+        g = grads()
+        before = [host(p) for p in params]
+        if bits == 8:
+            olds = [ref.moment_values(m.cpu().numpy(), v.cpu().numpy(), a.cpu().numpy(),
+                                      b.cpu().numpy())
+                    for m, v, a, b in zip(opt.m1, opt.m2, opt.s1, opt.s2)]
+        else:
+            olds = [(host(m), host(v)) for m, v in zip(opt.m1, opt.m2)]
+        opt.step(g)
+        for i, n in enumerate(sizes):
+            if n == 0:
+                continue
+            p, m, v = ref.adamw(before[i], host(g[i]), *olds[i], t, wd=decay[i], **HYPER)
+            b1, b2 = HYPER["beta1"], HYPER["beta2"]
+            size = (np.abs(b1 * olds[i][0]) + np.abs((1 - b1) * host(g[i]))) / (1 - b1 ** t)
+            size = HYPER["lr"] * size / (np.sqrt(v / (1 - b2 ** t)) + HYPER["eps"])
+            slack = 14 * U32 * size + 3 * U32 * np.abs(before[i])
+            slack = slack + (BF16 * np.abs(p) if io == "bf16" else 0)
+            assert np.all(np.abs(host(params[i]) - p) <= slack), (t, i)
+            if bits == 32:
+                assert np.all(np.abs(host(opt.m1[i]) - m) <= 2 * U32 * (np.abs(m) + 1e-2)), (t, i)
+                assert np.all(np.abs(host(opt.m2[i]) - v) <= 4 * U32 * (np.abs(v) + 1e-6)), (t, i)
+            else:
+                check_codes(m, v, opt.m1[i], opt.m2[i], opt.s1[i], opt.s2[i])
+    if bits == 8:
+        m1, m2 = opt.moments()
+        for i, n in enumerate(sizes):
+            a, b = ref.moment_values(opt.m1[i].cpu().numpy(), opt.m2[i].cpu().numpy(),
+                                     opt.s1[i].cpu().numpy(), opt.s2[i].cpu().numpy())
+            assert np.all(np.abs(host(m1[i]) - a) <= U32 * np.abs(a))
+            assert np.all(np.abs(host(m2[i]) - b) <= U32 * np.abs(b))
+
+
+def test_adamw_tiny_and_huge_blocks(rb):
+    """Scales from the least float to large ones: codes as in 64 bits."""
+    import torch
+    n, r = 256 * 7, np.random.default_rng(0)
+    scale = np.repeat([1e-22, 1e-19, 1e-12, 1.0, 1e10, 1e18, 3e19], 256)
+    g = torch.from_numpy(scale * r.normal(size=n)).float().cuda()
+    p = torch.zeros(n, device="cuda")
+    opt = rb.AdamW([p], state_bits=8, weight_decay=0.0, **HYPER)
+    opt.step([g])
+    _, m, v = ref.adamw(np.zeros(n), host(g), np.zeros(n), np.zeros(n), 1, wd=0.0, **HYPER)
+    check_codes(m, v, opt.m1[0], opt.m2[0], opt.s1[0], opt.s2[0])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_zero_and_nan_gradients(rb, bits):
+    """Zero gradients change nothing without decay; a NaN reaches its element (32 bits) or its
+    block's moments (8 bits) and nothing else."""
+    import torch
+    p = torch.randn(1000, device="cuda")
+    old = p.clone()
+    opt = rb.AdamW([p], state_bits=bits, weight_decay=0.0, **HYPER)
+    opt.step([torch.zeros_like(p)])
+    assert torch.equal(p, old)
+    g = torch.ones_like(p)
+    g[300] = math.nan
+    opt.step([g])
+    assert torch.isnan(p[300]) and int(torch.isnan(p).sum()) == 1
+    m1, m2 = opt.moments()
+    for m in (m1[0], m2[0]):
+        bad = torch.isnan(m)
+        if bits == 32:
+            assert bad[300] and int(bad.sum()) == 1
+        else:
+            assert bad[256:512].all() and int(bad.sum()) == 256
+
+
+def test_adamw_takes_over_state_and_stream(rb):
+    import torch
+    params, grads = adamw_case("f32", [500, 300])
+    copy = [p.clone() for p in params]
+    a = rb.AdamW(params, state_bits=8, **HYPER)
+    g = [grads(), grads()]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    a.step(g[0], stream=s)
+    a.step(g[1], lr=0.5, stream=s)
+    b = rb.AdamW(copy, state_bits=8, **HYPER)
+    b.step(g[0])
+    c = rb.AdamW(copy, state_bits=8, state=(b.m1, b.m2, b.s1, b.s2), step=b.steps, **HYPER)
+    c.step(g[1], lr=0.5)
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in zip(params, copy))
+    assert a.steps == c.steps == 2
+
+
+def test_adamw_graph(rb):
+    """A captured step replays on the current parameters and moments."""
+    import torch
+    params, grads = adamw_case("f32", [700, 50])
+    other = [p.clone() for p in params]
+    g = grads()
+    a, b = rb.AdamW(params, **HYPER), rb.AdamW(other, **HYPER)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph):
+        a.step(g)
+    for _ in range(3):
+        graph.replay()
+        b.steps = 0          # the graph holds the first step's bias corrections
+        b.step(g)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(params, other))
+
+
+def test_adamw_follows_replaced_memory(rb):
+    import torch
+    p, q = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    a, b = rb.AdamW([p], **HYPER), rb.AdamW([q], **HYPER)
+    old, g = p.data, torch.ones_like(p)
+    p.data = p.data.clone()
+    a.step([g])
+    b.step([g])
+    assert torch.equal(p, q) and torch.equal(old, g)
+    p.data = torch.ones(200, device="cuda")
+    with pytest.raises(ValueError):
+        a.step([g])
+
+
+def test_adamw_binding_refuses(rb):
+    import torch
+    p = torch.zeros(8, device="cuda")
+    opt = rb.AdamW([p])
+    for bad in ([torch.zeros(7, device="cuda")], [torch.zeros(8, device="cuda").bfloat16()],
+                [torch.zeros(16, device="cuda")[::2]], [torch.zeros(8)], []):
+        with pytest.raises(ValueError):
+            opt.step(bad)
+    assert opt.steps == 0
+    for kw in (dict(state_bits=16), dict(weight_decay=[0.1, 0.2]), dict(state=([p], [p], [p]))):
+        with pytest.raises(ValueError):
+            rb.AdamW([p], **kw)
+    with pytest.raises(rb.RecblrError):
+        rb.AdamW([p, p]).step([torch.zeros_like(p), torch.zeros_like(p)])
+
+
+# ------------------------------------------------------------------ sampling
+
+def check_sample(rb, logits, u, **kw):
+    """logits a torch tensor; kw: float64 / int arrays or None."""
+    import torch
+    B = logits.shape[0]
+    dev = {n: None if a is None else torch.as_tensor(np.asarray(a)).to(
+        torch.int32 if n == "top_k" else torch.float32).cuda() for n, a in kw.items()}
+    ut = torch.as_tensor(np.asarray(u)).float().cuda()
+    ids, prob = rb.sample(logits, ut, **dev)
+    want, wp = ref.sample(host(logits), host(ut),
+                          **{n: None if t is None else host(t) for n, t in dev.items()})
+    assert np.array_equal(ids.cpu().numpy(), want), np.nonzero(ids.cpu().numpy() != want)[0][:5]
+    assert np.all(np.abs(host(prob) - wp) <= 2 * U32 * wp)
+    assert ids.shape == (B,)
+    return want
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 3, 5, 64, 255, 257, 1000, 4095, 4096, 4097, 9001, 20000])
+def test_sample(rb, io, V):
+    """Every combination of limits over the rows; bf16 has many equal logits."""
+    import torch
+    print(io, V, flush=True)
+    B = 48 if V < 5000 else 16
+    r = np.random.default_rng(V)
+    x = torch.from_numpy(3 * r.normal(size=(B, V))).to(dtype_of(io)).cuda()
+    x[r.random((B, V)) < 0.1] = -math.inf
+    u = r.random(B).astype(np.float32)
+    row = np.arange(B)
+    limits = dict(temperature=np.where(row % 7 == 6, 0.0, r.uniform(0.3, 2.0, B)),
+                  top_k=np.where(row % 3 == 0, 0, r.integers(1, V + 2, B)),
+                  top_p=np.where(row % 4 == 0, 1.0, r.uniform(0.05, 1.0, B)),
+                  min_p=np.where(row % 5 == 0, r.uniform(0.0, 0.3, B), 0.0))
+    check_sample(rb, x, u, **limits)
+    check_sample(rb, x, u)
+    for name in limits:
+        check_sample(rb, x, u, **{name: limits[name]})
+
+
+@pytest.mark.parametrize("V", [50, 4096, 10000])
+def test_sample_equal_logits(rb, V):
+    """All alike: sums are whole numbers, borders exact, ties to the lowest index."""
+    import torch
+    x = torch.full((6, V), 2.5, device="cuda")
+    u = [0.0, 0.5, 0.999, 0.25, 0.75, 0.5]
+    got = check_sample(rb, x, u, top_k=[0, 0, 0, 10, 10, 1])
+    assert got.tolist() == [0, V // 2, int(np.float32(0.999) * np.float64(V)), 2, 7, 0]
+    got = check_sample(rb, x, [0.99] * 6, top_p=[1.0, 0.5, 0.25, 0.0, 1e-9, 0.75])
+    assert got[3] == got[4] == 0
+
+
+@pytest.mark.parametrize("V", [40, 6000])
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_sample_masks(rb, io, V):
+    """Rows with nothing left, one item, the type's lowest value as a mask, zeros of both signs,
+    infinities and NaN."""
+    import torch
+    dt = dtype_of(io)
+    low = torch.finfo(dt).min
+    x = torch.full((10, V), -math.inf, device="cuda", dtype=dt)
+    x[1, V - 1] = -5.0
+    x[2] = low
+    x[3] = low
+    x[3, 7], x[3, 9] = 1.0, 2.0
+    x[4, 3], x[4, 5] = 0.0, -0.0
+    x[5] = 1.0
+    x[5, 2] = math.nan
+    x[6] = 1.0
+    x[6, 2] = math.inf
+    x[7] = torch.finfo(dt).max
+    x[8] = 1.0
+    x[8, 0] = -math.nan
+    x[9, V // 2:] = 3.0
+    u = [0.3, 0.9, 0.5, 0.9, 0.6, 0.5, 0.5, 0.5, 0.5, 0.0]
+    got = check_sample(rb, x, u)
+    assert got[0] == got[5] == got[6] == got[8] == -1
+    assert got[1] == V - 1 and got[2] == V // 2 and got[3] == 9 and got[4] == 5
+    assert got[9] == V // 2
+    check_sample(rb, x, u, top_k=[3] * 10, top_p=[0.9] * 10, min_p=[0.1] * 10)
+    got = check_sample(rb, x, u, temperature=[0.0] * 10)
+    assert got[4] == 3 and got[7] == 0                    # the zeros are equal: lowest index
+    import torch as th
+    ids, prob = rb.sample(x, th.full((10,), 0.5, device="cuda"),
+                          temperature=th.full((10,), math.nan, device="cuda"))
+    assert ids.eq(-1).all() and prob.eq(0).all()
+
+
+@pytest.mark.parametrize("V", [100, 5000])
+def test_sample_extreme_parameters(rb, V):
+    """u at and past its ends, temperatures of all sizes, limits past theirs."""
+    import torch
+    r = np.random.default_rng(1)
+    B = 12
+    x = torch.from_numpy(r.normal(size=(B, V))).float().cuda()
+    temp = [1e-30, 1e-6, 0.1, 1.0, 10.0, 1e6, 1e30, math.inf, -1.0, 1.0, 1.0, 1.0]
+    u = [0.5, 0.5, 0.0, 1.0, 1.0 - 2 ** -24, 0.5, 0.5, 0.5, 0.5, 0.3, 0.3, 2.0]
+    check_sample(rb, x, u, temperature=temp)
+    check_sample(rb, x, u, temperature=temp, top_k=[-5, V, V + 1, 2 ** 31 - 1] * 3,
+                 top_p=[2.0, 1.0, 0.5] * 4, min_p=[-1.0, 0.0, 1.0, 5.0] * 3)
+
+
+def test_sample_empty_and_refusals(rb):
+    import torch
+    ids, prob = rb.sample(torch.empty((3, 0), device="cuda"), torch.rand(3, device="cuda"))
+    assert ids.tolist() == [-1, -1, -1] and prob.tolist() == [0, 0, 0]
+    ids, _ = rb.sample(torch.empty((0, 10), device="cuda"), torch.rand(0, device="cuda"))
+    assert ids.shape == (0,)
+    x, u = torch.randn(2, 10, device="cuda"), torch.rand(2, device="cuda")
+    for bad in (dict(top_k=torch.ones(2, device="cuda")), dict(top_p=torch.ones(3, device="cuda")),
+                dict(temperature=torch.ones(2)), dict(min_p=torch.ones(4, device="cuda")[::2])):
+        with pytest.raises(ValueError):
+            rb.sample(x, u, **bad)
+    with pytest.raises(ValueError):
+        rb.sample(x.t(), u)
+    with pytest.raises(ValueError):
+        rb.sample(x, u.double())
+
+
+@pytest.mark.parametrize("V", [3000, 30000])
+def test_sample_graph_and_streams(rb, V):
+    import torch
+    x = torch.randn(20, V, device="cuda")
+    u, p = torch.rand(20, device="cuda"), torch.full((20,), 0.9, device="cuda")
+    k = torch.full((20,), 50, device="cuda", dtype=torch.int32)
+    want = rb.sample(x, u, top_k=k, top_p=p)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    both = [rb.sample(x, u, top_k=k, top_p=p, stream=s) for s in streams]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in both for a, b in zip(g, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = rb.sample(x, u, top_k=k, top_p=p)
+    for _ in range(3):
+        u.copy_(torch.rand(20, device="cuda"))
+        want = rb.sample(x, u, top_k=k, top_p=p)
+        got[0].fill_(-9)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+# ------------------------------------------------------------------ together
+
+def test_train_and_serve_together(rb):
+    """As they are used: a layer of the delta rule between two linear maps and a prediction over
+    items, its gradients through delta_backward, two AdamW steps; then the history read in, one
+    more item decoded, and an answer drawn.  Against the same in 64 bits."""
+    import torch
+    B, L, D, V, H = 3, 70, 16, 50, 2
+    r = np.random.default_rng(0)
+    names = ("E", "Wq", "Wk", "Wv")
+    start = {"E": r.normal(size=(V, D)), **{n: r.normal(size=(D, D)) / 4 for n in names[1:]}}
+    ids, target = r.integers(0, V, (B, L)), r.integers(0, V, B)
+    g64 = -0.1 * r.random((B, L, H))
+    b64 = r.random((B, L, H))
+    dh = D // H
+
+    def loss_and_grads(w, delta):
+        """w: arrays; delta(q, k, v, do) -> (o, dq, dk, dv) with do chosen by the callback."""
+        x = w["E"][ids]
+        q, k, v = (x @ w[n] for n in names[1:])
+        shape = lambda t: t.reshape(B, L, H, dh)  # noqa: E731
+
+        def out_grad(o):
+            y = o[:, -1].reshape(B, D)
+            z = y @ w["E"].T
+            p = np.exp(z - z.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            dz = p.copy()
+            dz[np.arange(B), target] -= 1
+            dz /= B
+            do = np.zeros_like(o)
+            do[:, -1] = (dz @ w["E"]).reshape(B, H, dh)
+            return do, dz.T @ y
+        o, dq, dk, dv, dE = delta(shape(q), shape(k), shape(v), out_grad)
+        grads = {"E": dE}
+        dx = 0
+        for n, d in zip(names[1:], (dq, dk, dv)):
+            d = d.reshape(B, L, D)
+            grads[n] = np.einsum("bli,blj->ij", x, d)
+            dx = dx + d @ w[n].T
+        np.add.at(grads["E"], ids, dx)
+        return grads
+
+    def exact(q, k, v, out_grad):
+        o = ref.delta(q, k, v, g64, b64)["o"]
+        do, dE = out_grad(o)
+        d = ref.delta(q, k, v, g64, b64, do=do)
+        return o, d["dq"], d["dk"], d["dv"], dE
+
+    G, Bt = put(g64, "f32")[0], put(b64, "f32")[0]
+
+    def ours(q, k, v, out_grad):
+        a = [put(t, "f32")[0] for t in (q, k, v)] + [G, Bt]
+        o, _, st = rb.delta_forward(*a, keep_states=True)
+        do, dE = out_grad(host(o))
+        d = rb.delta_backward(*a, st, put(do, "f32")[0])
+        return host(o), host(d["dq"]), host(d["dk"]), host(d["dv"]), dE
+
+    params = {n: put(start[n], "f32")[0] for n in names}
+    w64 = {n: host(params[n]) for n in names}
+    mom = {n: [np.zeros_like(w64[n])] * 2 for n in names}
+    opt = rb.AdamW(list(params.values()), weight_decay=0.1, **HYPER)
+    for t in (1, 2):
+        mine = loss_and_grads({n: host(p) for n, p in params.items()}, ours)
+        want = loss_and_grads(w64, exact)
+        for n in names:  # the linear maps here are numpy's: the recurrence's bar, amplified by L
+            assert floored_rel_err(mine[n], want[n]) <= 6 * (dh + 64) * U32 * L, (t, n)
+        opt.step([put(mine[n], "f32")[0] for n in names])
+        for n in names:
+            w64[n], *m = ref.adamw(w64[n], want[n], *mom[n], t, wd=0.1, **HYPER)
+            mom[n] = m
+            # a first step is lr g / (|g| + eps): an element's sign is all it has of g
+            big = np.abs(want[n]) > 1e-3 * np.abs(want[n]).max()
+            diff = np.abs(host(params[n]) - w64[n])[big]
+            assert diff.max() <= HYPER["lr"] * 6 * (dh + 64) * U32 * L * 1e3, (t, n)
+    # Serving: the history but its last item read in, that one decoded, an item drawn.
+    w = {n: host(p) for n, p in params.items()}
+    x = w["E"][ids]
+    q, k, v = (put((x @ w[n]).reshape(B, L, H, dh), "f32")[0] for n in names[1:])
+    a = (q, k, v, G, Bt)
+    whole = ref.delta(*(host(t) for t in a))["o"][:, -1]
+    _, h, _ = rb.delta_forward(*(t[:, :-1].contiguous() for t in a))
+    o, h = rb.delta_step(*(t[:, -1].contiguous() for t in a), h, out=h)
+    close("decoded", o, whole, 6 * (dh + 64) * U32)
+    logits = put(host(o).reshape(B, D) @ w["E"].T, "f32")[0]
+    logits[torch.arange(B), torch.from_numpy(ids[:, -1])] = -math.inf   # not the same again
+    got = check_sample(rb, logits, [0.1, 0.5, 0.9], top_k=[10] * 3, top_p=[0.9] * 3)
+    assert all(i != j for i, j in zip(got, ids[:, -1]))
