@@ -1,8 +1,8 @@
 // One item a row from logits (recblr_sample): temperature, top-k, top-p, min-p.
 //
 // The items that stay are a run of the order (logit falling, index rising), so a row's
-// selection is one border: a key, and how many of the items with that very key stay; nothing
-// is sorted.  Weights w = exp((l - max) / temperature) are formed in 64 bits and summed as
+// selection is one border: a logit, and how many of the items with that very logit stay;
+// nothing is sorted.  Weights w = exp((l - max) / temperature) are formed in 64 bits and summed as
 // integers q = round(w 2^F): such sums are exact in any order, so atomics repeat bit for bit
 // and a border falls where 64-bit arithmetic puts it.  Items with q = 0 can neither be chosen
 // nor move a border that matters; they take no part.
@@ -10,10 +10,10 @@
 // The border is found on a histogram of counts and weights over kBins equal steps of the logit
 // (uniform steps spread the items of usual logits evenly; the bits of a float do not: its
 // upper eleven put half of a row in twenty bins, whose atomics then wait for each other).  The
-// bin that holds the border is searched further by its keys' own bits, 8 at a time, until one
-// key is left; equal keys (frequent in bf16) are one key from the start.
+// bin that holds the border has a few items most often, which are compared with one another; a
+// fuller one is searched by the floats' own bits, 8 at a time, until few or equal ones are left.
 //
-// A row of up to kSpan items is one workgroup's, keys and weights in its registers from a
+// A row of up to kSpan items is one workgroup's, logits and weights in its registers from a
 // single read.  A longer one takes a workgroup for each span of kSpan items and six short
 // launches: extremes, histogram, the items of the bins that can hold a border, the border
 // itself (on those items alone), sums of the spans, and the choice within one span.
@@ -42,28 +42,61 @@ __device__ __forceinline__ uint32_t key_of(float v) {
 __device__ __forceinline__ float value_of(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
 }
-constexpr uint32_t kKeyNegInf = 0x007FFFFFu;  // key_of(-inf); a NaN's key lies outside
-constexpr uint32_t kKeyPosInf = 0xFF800000u;  // [key_of(-inf), key_of(+inf)]; 0 is no item's
-
-template <typename V>
-__device__ __forceinline__ V wave_sum(V v) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-    return v;
-}
-// Sum over the lanes below this one.
-template <typename V>
-__device__ __forceinline__ V wave_before(V v, int lane) {
-    V s = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const V o = __shfl_up(s, d);
-        if (lane >= d) s += o;
-    }
-    return s - v;
-}
+constexpr float kInf = __builtin_inff();
 
 typedef unsigned long long u64;
+
+// A register of the lanes that a DPP control names (all lanes active), `old` where there is none.
+// These moves take a few cycles, a shuffle through the LDS crossbar a hundred; a row's kernel is
+// a chain of some eighty of them.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t dpp(uint32_t v, uint32_t old) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, kCtrl, kRows, 0xF, false);
+}
+template <int kCtrl, int kRows>
+__device__ __forceinline__ u64 dpp(u64 v, u64 old) {
+    return (u64)dpp<kCtrl, kRows>((uint32_t)(v >> 32), (uint32_t)(old >> 32)) << 32 |
+           dpp<kCtrl, kRows>((uint32_t)v, (uint32_t)old);
+}
+template <int kCtrl, int kRows>
+__device__ __forceinline__ float dpp(float v, float old) {
+    return __uint_as_float(dpp<kCtrl, kRows>(__float_as_uint(v), __float_as_uint(old)));
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) {
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+__device__ __forceinline__ u64 lane_of(u64 v, int lane) {
+    return (u64)lane_of((uint32_t)(v >> 32), lane) << 32 | lane_of((uint32_t)v, lane);
+}
+__device__ __forceinline__ float lane_of(float v, int lane) {
+    return __uint_as_float(lane_of(__float_as_uint(v), lane));
+}
+// op over this lane and those below it: shifts by 1, 2, 4 and 8 within the rows of 16, then a
+// row's last lane to the next row, and the second row's to the upper half.  `none` changes
+// nothing under op.
+template <typename V, typename Op>
+__device__ __forceinline__ V wave_scan(V v, V none, Op op) {
+    v = op(v, dpp<0x111, 0xF>(v, none));
+    v = op(v, dpp<0x112, 0xF>(v, none));
+    v = op(v, dpp<0x114, 0xF>(v, none));
+    v = op(v, dpp<0x118, 0xF>(v, none));
+    v = op(v, dpp<0x142, 0xA>(v, none));
+    return op(v, dpp<0x143, 0xC>(v, none));
+}
+template <typename V>
+__device__ __forceinline__ V wave_upto(V v) {
+    return wave_scan(v, (V)0, [](V a, V b) { return a + b; });
+}
+template <typename V>
+__device__ __forceinline__ V wave_sum(V v) {
+    return lane_of(wave_upto(v), kWave - 1);
+}
+__device__ __forceinline__ float wave_top(float v) {
+    return lane_of(wave_scan(v, -kInf, [](float a, float b) { return fmaxf(a, b); }), kWave - 1);
+}
+__device__ __forceinline__ float wave_least(float v) {
+    return lane_of(wave_scan(v, kInf, [](float a, float b) { return fminf(a, b); }), kWave - 1);
+}
 
 // e^x for x in [-46, 0]: x = n ln 2 + t with |t| <= ln 2 / 2, and e^t by its Taylor polynomial
 // of degree 12, whose remainder is below 2e-16 of it.
@@ -93,50 +126,69 @@ __device__ __forceinline__ u64 rounded(double x) {
     return (u64)__double_as_longlong(x + 0x1p52) & 0xFFFFFFFFFFFFFull;
 }
 
-// What a row asks for, and the measures that its extremes give.
+// What a row asks for, read before its logits' extremes are known.
+struct Ask {
+    float temp, top_p, min_p, u;
+    int32_t top_k;
+    __device__ __forceinline__ Ask(const SampleArgs& a, int64_t row) {
+        temp = a.temperature ? a.temperature[row] : 1.0f;
+        top_p = a.top_p ? a.top_p[row] : 1.0f;
+        min_p = a.min_p ? a.min_p[row] : 0.0f;
+        top_k = a.top_k ? a.top_k[row] : 0;
+        u = a.u[row];
+    }
+};
+
+// That, and the measures that the extremes give.
 struct Row {
     double inv_t, max, scale;
-    float top, bins;     // largest logit; bins to a unit of the logit
+    float top, bins;  // largest logit; bins to a unit of the logit
     float top_p, min_p;
     int64_t k;
     bool bad, greedy;
-    uint32_t hi;
 
-    // Of a row whose largest and smallest keys are hi and lo.
-    __device__ __forceinline__ Row(const SampleArgs& a, int64_t row, uint32_t hi_, uint32_t lo,
-                                   double scale_) {
-        hi = hi_;
+    // Of a row whose largest and smallest logits are hi and lo.
+    __device__ __forceinline__ Row(const Ask& ask, int64_t V, float hi, float lo, double scale_) {
+        top = hi;
         scale = scale_;
-        const float temp = a.temperature ? a.temperature[row] : 1.0f;
-        bad = hi <= kKeyNegInf || hi >= kKeyPosInf || lo < kKeyNegInf || !(temp == temp);
-        top_p = a.top_p ? a.top_p[row] : 1.0f;
-        min_p = a.min_p ? fminf(a.min_p[row], 1.0f) : 0.0f;
+        const float temp = ask.temp;
+        bad = !(hi > -kInf && hi < kInf) || !(temp == temp);
+        top_p = ask.top_p;
+        min_p = fminf(ask.min_p, 1.0f);
         greedy = temp <= 0.0f;
-        k = a.top_k && a.top_k[row] > 0 ? a.top_k[row] : a.V;
+        k = ask.top_k > 0 ? ask.top_k : V;
         if (greedy || top_p <= 0.0f) k = 1;
         inv_t = greedy ? 0.0 : 1.0 / (double)temp;
-        top = value_of(hi);
         max = (double)top;
-        const float range = fminf(46.0f * temp, top - value_of(lo < kKeyNegInf ? hi : lo));
-        bins = range > 0.0f && range < 3e38f ? (float)(kBins - 1) / range : 0.0f;
+        const float range = fminf(46.0f * temp, top - lo);
+        bins = range > 0.0f ? (float)(kBins - 1) / fminf(range, 3e38f) : 0.0f;
     }
-    __device__ __forceinline__ double weight(uint32_t key) const {
-        // What lies further down than 46 temperatures (-inf and what is no item among it) weighs
-        // e^-46, which no scale up to 2^51 brings to a half.
-        return exp_neg(fmax(((double)value_of(key) - max) * inv_t, -46.0));
+    __device__ __forceinline__ double weight(float v) const {
+        // What lies further down than 46 temperatures (-inf and what is no item, a NaN, among it)
+        // weighs e^-46, which no scale up to 2^51 brings to a half.
+        return exp_neg(fmax(((double)v - max) * inv_t, -46.0));
     }
-    __device__ __forceinline__ u64 fixed(uint32_t key) const { return rounded(weight(key) * scale); }
+    __device__ __forceinline__ u64 fixed(float v) const { return rounded(weight(v) * scale); }
     // Rising as the logit falls: both roundings keep the order.
-    __device__ __forceinline__ int bin(uint32_t key) const {
-        const float b = (top - value_of(key)) * bins;
+    __device__ __forceinline__ int bin(float v) const {
+        const float b = (top - v) * bins;
         return b < (float)(kBins - 1) ? (int)b : kBins - 1;
+    }
+    // Whether an item with weight is of a bin in [from, to]; none is where from is -1.
+    __device__ __forceinline__ auto within(int from, int to) const {
+        const float lo = from < 0 ? __builtin_nanf("") : (float)from;
+        const float hi = to < kBins - 1 ? (float)(to + 1) : __builtin_nanf("");
+        return [this, lo, hi](float v) {
+            const float b = (top - v) * bins;
+            return (b >= lo) & !(b >= hi);
+        };
     }
     // Whether a border has to be looked for.
     __device__ __forceinline__ bool cuts(int64_t V) const { return k < V || top_p < 1.0f; }
 };
 
 struct Border {
-    uint32_t key;   // items above it stay,
+    float at;       // items above it stay,
     uint32_t ties;  // and the first `ties` of those that have it
 };
 
@@ -144,8 +196,10 @@ struct Shared {
     uint32_t cnt[kBins];
     u64 mass[kBins];
     uint32_t fine_cnt[kFine];
+    float few[kWave];
     u64 fine_mass[kFine];
-    uint32_t w32[2][kNW];
+    uint32_t w32[kNW];
+    float ext[2][kNW];
     u64 w64[kNW];
     uint32_t lo, hi;
     int at;             // bin found
@@ -153,58 +207,71 @@ struct Shared {
     u64 above_mass, at_mass;
 };
 
-// Workgroup sums of a count and a weight over lower threads.
-__device__ __forceinline__ void block_before(Shared& sm, uint32_t& c, u64& m, int lane, int w) {
-    const uint32_t c0 = c;
-    const u64 m0 = m;
-    c = wave_before(c, lane);
-    m = wave_before(m, lane);
+// A count and a weight of each thread become their sums over lower threads; returned are the
+// workgroup's.  Holds one barrier; another one has to lie between two calls.
+struct Total {
+    uint32_t c;
+    u64 m;
+};
+__device__ __forceinline__ Total block_before(Shared& sm, uint32_t& c, u64& m, int lane, int w) {
+    const uint32_t ci = wave_upto(c);
+    const u64 mi = wave_upto(m);
     if (lane == kWave - 1) {
-        sm.w32[0][w] = c + c0;
-        sm.w64[w] = m + m0;
+        sm.w32[w] = ci;
+        sm.w64[w] = mi;
     }
+    c = ci - c;
+    m = mi - m;
     __syncthreads();
-    for (int i = 0; i < w; ++i) {
-        c += sm.w32[0][i];
-        m += sm.w64[i];
+    Total t{0, 0};
+#pragma unroll
+    for (int i = 0; i < kNW; ++i) {
+        c += i < w ? sm.w32[i] : 0;
+        m += i < w ? sm.w64[i] : 0;
+        t.c += sm.w32[i];
+        t.m += sm.w64[i];
     }
+    return t;
 }
 
-// The last bin that holds items and has less than is wanted before it: fewer than want_cnt
-// items, or a weight below want_mass.  `cnt`, `mass`: N bins in LDS, N / kNT of them to a
-// thread in order, with c and m before the thread's first (whole arrays, base included).
+// A thread's N consecutive bins, with what lies before them.
 template <int N>
-__device__ __forceinline__ void pick(Shared& sm, const uint32_t* cnt, const u64* mass, uint32_t c,
-                                     u64 m, bool by_mass, uint64_t want_cnt, double want_mass,
-                                     int tid) {
-    constexpr int BPT = N / kNT;
-    if (tid == 0) sm.at = -1;
-    __syncthreads();
-    int mine = -1;
-    uint32_t c_at = 0;
-    u64 m_at = 0;
+struct Bins {
+    uint32_t n[N], c;
+    u64 q[N], m;
+    __device__ __forceinline__ Bins(const uint32_t* cnt, const u64* mass, int tid) : c(0), m(0) {
 #pragma unroll
-    for (int j = 0; j < BPT; ++j) {
-        const int b = tid * BPT + j;
-        const uint32_t n = cnt[b];
-        if (n && (by_mass ? (double)m < want_mass : c < want_cnt)) {
-            mine = b;
-            c_at = c;
-            m_at = m;
+        for (int j = 0; j < N; ++j) {
+            n[j] = cnt[tid * N + j];
+            q[j] = mass[tid * N + j];
+            c += n[j];
+            m += q[j];
         }
-        c += n;
-        m += mass[b];
     }
-    if (mine >= 0) atomicMax(&sm.at, mine);
-    __syncthreads();
-    if (mine >= 0 && sm.at == mine) {
-        sm.above_cnt = c_at;
-        sm.above_mass = m_at;
-        sm.at_cnt = cnt[mine];
-        sm.at_mass = mass[mine];
+    // The bin before which there is less than wanted (want_cnt items, or a weight of want_mass)
+    // and with which there is not: it and what lies before it go to sm, by the one thread that
+    // has it.  Ends with a barrier.
+    __device__ __forceinline__ void pick(Shared& sm, bool by_mass, uint64_t want_cnt,
+                                         double want_mass, int tid) const {
+        uint32_t cj = c;
+        u64 mj = m;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool in = by_mass ? (double)mj < want_mass && !((double)(mj + q[j]) < want_mass)
+                                    : cj < want_cnt && !(cj + n[j] < want_cnt);
+            if (in) {
+                sm.at = tid * N + j;
+                sm.above_cnt = cj;
+                sm.above_mass = mj;
+                sm.at_cnt = n[j];
+                sm.at_mass = q[j];
+            }
+            cj += n[j];
+            mj += q[j];
+        }
+        __syncthreads();
     }
-    __syncthreads();
-}
+};
 
 // How many of `ties` items of weight q stay when `before` lies above them and less than `want`
 // may lie before one that stays.
@@ -217,19 +284,62 @@ __device__ __forceinline__ uint32_t ties_within(uint32_t ties, u64 q, u64 before
     return (uint32_t)n;
 }
 
-// Searches one bin further.  each(f) calls f(key, q) for the items that may be of it, member()
-// tells which are; `above` of sm is what lies before the bin and is brought to what lies before
-// the key found, which has sm.at_cnt items.
+// Searches one bin further.  each(f) calls f(v, q) for the items that may be of it (all with
+// weight; NaN is passed over), member() tells which are; `above` of sm is what lies before the bin and is brought to what lies before
+// the logit found, which has sm.at_cnt items.
 template <typename Each, typename Member>
-__device__ __forceinline__ uint32_t refine(Shared& sm, const Row& row, Each each, Member member,
-                                           bool by_mass, uint64_t want_cnt, double want_mass,
-                                           int tid, int lane, int w) {
-    uint32_t from = 0, to = 0xFFFFFFFFu;
+__device__ __forceinline__ float refine(Shared& sm, Each each, Member member, bool by_mass,
+                                        uint64_t want_cnt, double want_mass, int tid, int lane,
+                                        int w) {
+    float from = -kInf, to = kInf;
     uint32_t base_c = sm.above_cnt;
     u64 base_m = sm.above_mass;
     // Each search leaves at most a 128th of the keys' range: five come down to one key.
     for (int depth = 0; depth < 8; ++depth) {
+        const bool few = sm.at_cnt <= (uint32_t)kWave;
         __syncthreads();
+        if (few) {
+            // The usual case: each item is compared with all others, a lane of the first wave an
+            // item.  The border is the lowest logit with less than is wanted before it.
+            if (tid < kWave) sm.few[tid] = -kInf;
+            if (tid == 0) sm.hi = 0;
+            __syncthreads();
+            each([&](float v, u64 q) {
+                if ((v >= from) & (v <= to) & member(v)) {
+                    const uint32_t i = atomicAdd(&sm.hi, 1u);
+                    sm.few[i] = v;
+                    sm.fine_mass[i] = q;
+                }
+            });
+            __syncthreads();
+            if (tid < kWave) {
+                const uint32_t n = sm.hi;
+                const float v = sm.few[tid];
+                uint32_t c = base_c, same = 0;
+                u64 m = base_m;
+                for (uint32_t i = 0; i < n; i += 8) {
+#pragma unroll
+                    for (uint32_t j = i; j < i + 8; ++j) {  // behind the last: -inf, above none
+                        const float o = sm.few[j];
+                        const u64 q = sm.fine_mass[j];
+                        c += o > v;
+                        same += o == v;
+                        m += o > v ? q : 0;
+                    }
+                }
+                const bool in =
+                    (uint32_t)tid < n && (by_mass ? (double)m < want_mass : c < want_cnt);
+                const float least = wave_least(in ? v : kInf);
+                if (in && v == least) {  // equal ones write the same
+                    sm.above_cnt = c;
+                    sm.above_mass = m;
+                    sm.at_cnt = same;
+                }
+                if (tid == 0) sm.few[0] = least;
+            }
+            __syncthreads();
+            return sm.few[0];
+        }
         if (tid == 0) {
             sm.lo = 0xFFFFFFFFu;
             sm.hi = 0;
@@ -240,8 +350,9 @@ __device__ __forceinline__ uint32_t refine(Shared& sm, const Row& row, Each each
         }
         __syncthreads();
         uint32_t lo = 0xFFFFFFFFu, hi = 0;
-        each([&](uint32_t key, u64 q) {
-            const bool in = (q != 0) & (key >= from) & (key <= to) & member(key);
+        each([&](float v, u64) {
+            const bool in = (v >= from) & (v <= to) & member(v);
+            const uint32_t key = key_of(v);
             lo = in && key < lo ? key : lo;
             hi = in && key > hi ? key : hi;
         });
@@ -255,27 +366,28 @@ __device__ __forceinline__ uint32_t refine(Shared& sm, const Row& row, Each each
         if (lo > hi) break;
         const int bits = 32 - __clz((int)((hi - lo) | 1u));
         const int shift = bits > 8 ? bits - 8 : 0;
-        each([&](uint32_t key, u64 q) {
-            if ((q != 0) & (key >= lo) & (key <= hi) & member(key)) {
-                const uint32_t b = (hi - key) >> shift;
+        each([&](float v, u64 q) {
+            if ((v >= from) & (v <= to) & member(v)) {
+                const uint32_t b = (hi - key_of(v)) >> shift;
                 atomicAdd(&sm.fine_cnt[b], 1u);
                 atomicAdd(&sm.fine_mass[b], q);
             }
         });
         __syncthreads();
-        uint32_t c = sm.fine_cnt[tid];
-        u64 m = sm.fine_mass[tid];
-        block_before(sm, c, m, lane, w);
-        pick<kFine>(sm, sm.fine_cnt, sm.fine_mass, c + base_c, m + base_m, by_mass, want_cnt,
-                    want_mass, tid);
-        if (sm.at < 0) break;
-        const uint32_t b = (uint32_t)sm.at;
+        Bins<kFine / kNT> bins(sm.fine_cnt, sm.fine_mass, tid);
+        block_before(sm, bins.c, bins.m, lane, w);
+        bins.c += base_c;
+        bins.m += base_m;
+        bins.pick(sm, by_mass, want_cnt, want_mass, tid);
         base_c = sm.above_cnt;
         base_m = sm.above_mass;
-        to = hi - (b << shift);
-        from = to - ((1u << shift) - 1) < lo || to < ((1u << shift) - 1) ? lo
-                                                                         : to - ((1u << shift) - 1);
-        if (from == to) break;
+        const uint32_t last = hi - ((uint32_t)sm.at << shift);  // the bin's keys end with it
+        const uint32_t n = 1u << shift;
+        const uint32_t first = last - lo < n ? lo : last - n + 1;
+        // Between the zeros' keys, which are one number, lies no item's.
+        to = value_of(last == 0x7FFFFFFFu ? last - 1 : last);
+        from = value_of(first);
+        if (first == last) break;
     }
     return to;
 }
@@ -285,57 +397,42 @@ __device__ __forceinline__ uint32_t refine(Shared& sm, const Row& row, Each each
 template <typename Each>
 __device__ __forceinline__ Border find_border(Shared& sm, const Row& row, Each each, int tid,
                                               int lane, int w) {
-    uint32_t c = 0;
-    u64 m = 0;
-#pragma unroll
-    for (int j = 0; j < kBPT; ++j) {
-        c += sm.cnt[tid * kBPT + j];
-        m += sm.mass[tid * kBPT + j];
-    }
-    const uint32_t c0 = c;
-    const u64 m0 = m;
-    block_before(sm, c, m, lane, w);
-    // Totals stand behind the last thread's bins.
-    if (tid == kNT - 1) {
-        sm.lo = c + c0;
-        sm.at_mass = m + m0;
-    }
-    __syncthreads();
-    const uint32_t total = sm.lo;
-    u64 above = sm.at_mass;
-    __syncthreads();
-    Border b{0, 0};
+    Bins<kBPT> bins(sm.cnt, sm.mass, tid);
+    const Total total = block_before(sm, bins.c, bins.m, lane, w);
+    u64 above = total.m;
+    Border b{-kInf, 0};
     u64 tie_q = 0;
-    if (row.k < (int64_t)total) {
-        pick<kBins>(sm, sm.cnt, sm.mass, c, m, false, (uint64_t)row.k, 0.0, tid);
-        const int bin = sm.at;
-        b.key = refine(sm, row, each, [&](uint32_t key) { return row.bin(key) == bin; }, false,
-                       (uint64_t)row.k, 0.0, tid, lane, w);
+    if (row.k < (int64_t)total.c) {
+        bins.pick(sm, false, (uint64_t)row.k, 0.0, tid);
+        b.at = refine(sm, each, row.within(sm.at, sm.at), false, (uint64_t)row.k, 0.0, tid, lane,
+                      w);
         b.ties = (uint32_t)(row.k - sm.above_cnt);
         above = sm.above_mass;
-        tie_q = row.fixed(b.key);
+        tie_q = row.fixed(b.at);
     }
     if (row.top_p < 1.0f && row.k > 1) {
         const double want = (double)row.top_p * (double)(above + tie_q * (u64)b.ties);
         if ((double)above < want) {
             if (b.ties) b.ties = ties_within(b.ties, tie_q, above, want);
         } else {
-            const uint32_t edge = b.key;
-            pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, want, tid);
-            const int bin = sm.at;
-            b.key = refine(sm, row, each,
-                           [&](uint32_t key) { return (key > edge) & (row.bin(key) == bin); }, true,
-                           0, want, tid, lane, w);
-            b.ties = ties_within(sm.at_cnt, row.fixed(b.key), sm.above_mass, want);
+            const float edge = b.at;
+            __syncthreads();  // what the first search left in sm has been read
+            bins.pick(sm, true, 0, want, tid);
+            const auto in = row.within(sm.at, sm.at);
+            b.at = refine(sm, each, [&](float v) { return (v > edge) & in(v); }, true, 0, want,
+                          tid, lane, w);
+            b.ties = ties_within(sm.at_cnt, row.fixed(b.at), sm.above_mass, want);
         }
     }
     return b;
 }
 
-// A span of a row: its keys in order, a wave's 1024 after another's, groups of four to a lane.
+// A span of a row: its logits in order, a wave's 1024 after another's, groups of four to a lane.
+// What lies behind the row's end is NaN, which no comparison takes; a NaN within the row becomes
+// +inf, which spoils the row as well.
 template <typename T>
 struct Span {
-    uint32_t key[kItems];
+    float v[kItems];
     __device__ __forceinline__ static int64_t index(int64_t base, int w, int it, int lane) {
         return base + (w * kIT + it) * 256 + lane * 4;
     }
@@ -344,89 +441,97 @@ struct Span {
 #pragma unroll
         for (int it = 0; it < kIT; ++it) {
             const int64_t i = index(base, w, it, lane);
+            float x[4];
             if (vec && i + 4 <= V) {
-                float v[4];
-                unpack_vec<T, 4>(*(const typename VecT<T, 4>::type*)(p + i), v);
+                unpack_vec<T, 4>(*(const typename VecT<T, 4>::type*)(p + i), x);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) key[4 * it + e] = key_of(v[e]);
+                for (int e = 0; e < 4; ++e) v[4 * it + e] = x[e] == x[e] ? x[e] : kInf;
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    key[4 * it + e] = i + e < V ? key_of(to_f32(p[i + e])) : 0u;
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = i + e < V ? to_f32(p[i + e]) : 0.0f;
+                    v[4 * it + e] = i + e < V ? (x[e] == x[e] ? x[e] : kInf) : __builtin_nanf("");
+                }
             }
         }
     }
-    // Largest and smallest key over the workgroup's items, by all threads; w32 of LDS.
-    __device__ __forceinline__ void extremes(uint32_t (&w32)[2][kNW], int w, int lane, uint32_t& hi,
-                                             uint32_t& lo) const {
-        // What is no item has key 0, which as the smallest wraps to the largest.
-        hi = 0;
-        lo = 0xFFFFFFFFu;
+    // Between the phases of a kernel: what one has computed from the logits is computed anew by
+    // the next, not kept in registers (kept, it spilled).
+    __device__ __forceinline__ void phase() {
+#pragma unroll
+        for (int i = 0; i < kItems; ++i) asm volatile("" : "+v"(v[i]));
+    }
+    // Largest and smallest logit over the workgroup's items, by all threads; ext of LDS.
+    __device__ __forceinline__ void extremes(float (&ext)[2][kNW], int w, int lane, float& hi,
+                                             float& lo) const {
+        hi = -kInf;
+        lo = kInf;
 #pragma unroll
         for (int i = 0; i < kItems; ++i) {
-            hi = key[i] > hi ? key[i] : hi;
-            lo = key[i] - 1u < lo ? key[i] - 1u : lo;
+            hi = v[i] > hi ? v[i] : hi;
+            lo = v[i] < lo ? v[i] : lo;
         }
-        lo = lo == 0xFFFFFFFFu ? lo : lo + 1u;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            const uint32_t h = (uint32_t)__shfl_xor((int)hi, d), l = (uint32_t)__shfl_xor((int)lo, d);
-            hi = h > hi ? h : hi;
-            lo = l < lo ? l : lo;
-        }
+        all_extremes(ext, w, lane, hi, lo);
+    }
+    __device__ __forceinline__ static void all_extremes(float (&ext)[2][kNW], int w, int lane,
+                                                        float& hi, float& lo) {
+        hi = wave_top(hi);
+        lo = wave_least(lo);
         if (lane == 0) {
-            w32[0][w] = hi;
-            w32[1][w] = lo;
+            ext[0][w] = hi;
+            ext[1][w] = lo;
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < kNW; ++i) {
-            hi = w32[0][i] > hi ? w32[0][i] : hi;
-            lo = w32[1][i] < lo ? w32[1][i] : lo;
+            hi = fmaxf(hi, ext[0][i]);
+            lo = fminf(lo, ext[1][i]);
         }
     }
 };
 
-// The choice within a span whose first item has `before` items of the border's key and a sum of
-// `run0` before it.  q of items that stay is left, others' become 0.
+// The choice within a span whose first item has `before` items of the border's logit before it:
+// q of items that stay is left, others' become 0.
 template <typename T>
-__device__ __forceinline__ void keep(const Span<T>& sp, const Row& row, const Border& b,
-                                     uint64_t before, u64 (&q)[kItems], int lane) {
+__device__ __forceinline__ void keep(const Span<T>& sp, const Border& b, uint32_t before,
+                                     u64 (&q)[kItems]) {
 #pragma unroll
     for (int it = 0; it < kIT; ++it) {
-        uint32_t tie[4], n = 0;
+        const float* v = sp.v + 4 * it;
+        uint32_t n = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            tie[e] = sp.key[4 * it + e] == b.key && b.key != 0;
-            n += tie[e];
-        }
-        uint64_t mine = 0;
-        if (__any((int)n)) {
-            const uint32_t lower = wave_before(n, lane);
-            mine = before + lower;
-            before += (uint32_t)__shfl((int)(lower + n), kWave - 1);
-        }
+        for (int e = 0; e < 4; ++e) n += v[e] == b.at;
+        if (b.ties && __any((int)n)) {
+            const uint32_t upto = wave_upto(n);
+            uint32_t mine = before + upto - n;
+            before += lane_of(upto, kWave - 1);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (!(sp.key[4 * it + e] > b.key || (tie[e] && mine < b.ties))) q[4 * it + e] = 0;
-            mine += tie[e];
+            for (int e = 0; e < 4; ++e) {
+                const bool tie = v[e] == b.at;
+                if (!(v[e] > b.at || (tie && mine < b.ties))) q[4 * it + e] = 0;
+                mine += tie;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!(v[e] > b.at)) q[4 * it + e] = 0;
         }
     }
 }
 
-// A wave's items of the border's key.
+// A wave's items of the border's logit.
 template <typename T>
 __device__ __forceinline__ uint32_t wave_ties(const Span<T>& sp, const Border& b) {
     uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) n += sp.key[i] == b.key && b.key != 0;
-    return wave_sum(n);
+    for (int i = 0; i < kItems; ++i) n += (uint32_t)__popcll(__ballot(sp.v[i] == b.at));
+    return n;
 }
 
 // The weights of a row's items: min-p's are 0 as well (in a greedy row all weigh the same).
-__device__ __forceinline__ u64 weight_of(const Row& row, uint32_t key) {
-    if (row.greedy) return key > kKeyNegInf ? (u64)row.scale : 0;
-    const double wt = row.weight(key);
+__device__ __forceinline__ u64 weight_of(const Row& row, float v) {
+    if (row.greedy) return v > -kInf ? (u64)row.scale : 0;
+    const double wt = row.weight(v);
     return wt < (double)row.min_p ? 0 : rounded(wt * row.scale);
 }
 
@@ -437,39 +542,35 @@ __device__ __forceinline__ void choose(const SampleArgs& a, const Span<T>& sp, c
                                        const u64 (&q)[kItems], int64_t r, int64_t base, u64 run,
                                        double target, u64 all, int w, int lane) {
     int64_t found = -1, tail = -1;
-    uint32_t key_f = 0, key_t = 0;
+    float v_found = 0.0f, v_tail = 0.0f;
 #pragma unroll
     for (int it = 0; it < kIT; ++it) {
         const u64 own = q[4 * it] + q[4 * it + 1] + q[4 * it + 2] + q[4 * it + 3];
-        u64 c = run + wave_before(own, lane);
-        run += wave_sum(own);
+        const u64 upto = wave_upto(own);
+        u64 c = run + upto - own;
+        run += lane_of(upto, kWave - 1);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             c += q[4 * it + e];
             if (q[4 * it + e]) {
                 tail = Span<T>::index(base, w, it, lane) + e;
-                key_t = sp.key[4 * it + e];
+                v_tail = sp.v[4 * it + e];
                 if (found < 0 && (double)c > target) {
                     found = tail;
-                    key_f = key_t;
+                    v_found = v_tail;
                 }
             }
         }
     }
-    u64 best = found >= 0 ? (u64)found : ~0ull;
-    long long end = (long long)tail;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const u64 o = __shfl_xor(best, d);
-        const long long t = __shfl_xor(end, d);
-        best = o < best ? o : best;
-        end = t > end ? t : end;
-    }
-    const bool got = best != ~0ull;
-    const int64_t id = got ? (int64_t)best : (int64_t)end;
+    // Items are fewer than 2^24: their indexes are floats, found or not.
+    const float none = 0x1p24f;
+    const float best = wave_least(found >= 0 ? (float)found : none);
+    const float end = wave_top((float)tail);
+    const bool got = best != none;
+    const int64_t id = (int64_t)(got ? best : end);
     if (got ? found == id : tail == id) {
         a.ids[r] = (int32_t)id;
-        const double wt = row.greedy ? 1.0 : row.weight(got ? key_f : key_t);
+        const double wt = row.greedy ? 1.0 : row.weight(got ? v_found : v_tail);
         if (a.prob) a.prob[r] = (float)(wt * row.scale / (double)all);
     }
 }
@@ -494,41 +595,50 @@ __global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double
     __shared__ Shared sm;
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x;
-    const Span<T> sp((const T*)a.logits + r * a.V, a.V, 0, w, lane);
+    Span<T> sp((const T*)a.logits + r * a.V, a.V, 0, w, lane);
+    const Ask ask(a, r);
     for (int b = tid; b < kBins; b += kNT) {
         sm.cnt[b] = 0;
         sm.mass[b] = 0;
     }
-    uint32_t hi, lo;
-    sp.extremes(sm.w32, w, lane, hi, lo);
-    const Row row(a, r, hi, lo, scale);
+    float hi, lo;
+    sp.extremes(sm.ext, w, lane, hi, lo);
+    const Row row(ask, a.V, hi, lo, scale);
     if (row.bad) {
         if (tid == 0) none(a, r);
         return;
     }
+    sp.phase();
     u64 q[kItems];
-    Border b{0, 0};
+    Border b{-kInf, 0};
     if (row.k == 1) {
-        b = Border{hi, 1};
+        b = Border{row.top, 1};
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) q[i] = sp.key[i] == hi ? (u64)scale : 0;
+        for (int i = 0; i < kItems; ++i) q[i] = sp.v[i] == row.top ? (u64)scale : 0;
     } else {
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) q[i] = row.fixed(sp.key[i]);
+        for (int i = 0; i < kItems; ++i) {
+            q[i] = row.fixed(sp.v[i]);
+            sp.v[i] = q[i] ? sp.v[i] : __builtin_nanf("");
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        sp.phase();
         if (row.cuts(a.V)) {
             __syncthreads();
 #pragma unroll
             for (int i = 0; i < kItems; ++i)
                 if (q[i]) {
-                    const int bin = row.bin(sp.key[i]);
+                    const int bin = row.bin(sp.v[i]);
                     atomicAdd(&sm.cnt[bin], 1u);
                     atomicAdd(&sm.mass[bin], q[i]);
                 }
             __syncthreads();
             auto each = [&](auto f) {
 #pragma unroll
-                for (int i = 0; i < kItems; ++i) f(sp.key[i], q[i]);
+                for (int i = 0; i < kItems; ++i) f(sp.v[i], q[i]);
+                sp.phase();
             };
+            sp.phase();
             b = find_border(sm, row, each, tid, lane, w);
         }
         if (row.min_p > 0.0f) {
@@ -537,17 +647,18 @@ __global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double
 #pragma unroll
             for (int i = 0; i < kItems; ++i) {
                 if (q[i] < least) q[i] = 0;
-                else if (q[i] <= least + 1 && row.weight(sp.key[i]) < (double)row.min_p) q[i] = 0;
+                else if (q[i] <= least + 1 && row.weight(sp.v[i]) < (double)row.min_p) q[i] = 0;
             }
         }
     }
     __syncthreads();
+    sp.phase();
     const uint32_t ties = wave_ties(sp, b);
-    if (lane == 0) sm.w32[0][w] = ties;
+    if (lane == 0) sm.w32[w] = ties;
     __syncthreads();
-    uint64_t before = 0;
-    for (int i = 0; i < w; ++i) before += sm.w32[0][i];
-    keep(sp, row, b, before, q, lane);
+    uint32_t before = 0;
+    for (int i = 0; i < w; ++i) before += sm.w32[i];
+    keep(sp, b, before, q);
     u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) sum += q[i];
@@ -563,34 +674,34 @@ __global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double
         if (s) last = i;
         all += s;
     }
-    const double target = (double)a.u[r] * (double)all;
+    const double target = (double)ask.u * (double)all;
     if (is_part(from, sum, all, target, w == last))
         choose(a, sp, row, q, r, 0, from, target, all, w, lane);
 }
 
 // ------------------------------------------------------------------ a row in several
 struct SpanWs {
-    uint32_t* ext;    // [B][S][2] extremes of each span
+    float* ext;       // [B][S][2] extremes of each span
     uint32_t* cnt;    // [B][kBins]
     u64* mass;        // [B][kBins]
     uint32_t* found;  // [B] items in the list
-    uint32_t* list;   // [B][V] their keys
-    u64* list_q;      // [B][V] and weights
+    float* list;      // [B][V] they
+    u64* list_q;      // [B][V] and their weights
     Border* border;   // [B]
     u64* sum;         // [B][S] weight above the border
-    uint32_t* ties;   // [B][S] items with the border's key
+    uint32_t* ties;   // [B][S] items with the border's logit
 };
 
 template <typename T>
 __global__ __launch_bounds__(kNT) void sample_extremes_kernel(SampleArgs a, SpanWs ws, int spans) {
-    __shared__ uint32_t w32[2][kNW];
+    __shared__ float ext[2][kNW];
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
     const int s = (int)(blockIdx.x - (unsigned)r * (unsigned)spans);
     const int64_t base = (int64_t)s * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
-    uint32_t hi, lo;
-    sp.extremes(w32, w, lane, hi, lo);
+    float hi, lo;
+    sp.extremes(ext, w, lane, hi, lo);
     if (tid == 0) {
         ws.ext[2 * blockIdx.x] = hi;
         ws.ext[2 * blockIdx.x + 1] = lo;
@@ -606,32 +717,16 @@ __global__ __launch_bounds__(kNT) void sample_extremes_kernel(SampleArgs a, Span
 
 // The row of a workgroup from its spans' extremes.
 __device__ __forceinline__ Row row_of(const SampleArgs& a, const SpanWs& ws, int64_t r, int spans,
-                                      double scale, uint32_t (&w32)[2][kNW], int tid, int lane,
-                                      int w) {
-    uint32_t hi = 0, lo = 0xFFFFFFFFu;
+                                      double scale, const Ask& ask, float (&ext)[2][kNW], int tid,
+                                      int lane, int w) {
+    float hi = -kInf, lo = kInf;
     for (int i = tid; i < spans; i += kNT) {
-        const uint32_t h = ws.ext[2 * (r * spans + i)], l = ws.ext[2 * (r * spans + i) + 1];
-        hi = h > hi ? h : hi;
-        lo = l < lo ? l : lo;
+        hi = fmaxf(hi, ws.ext[2 * (r * spans + i)]);
+        lo = fminf(lo, ws.ext[2 * (r * spans + i) + 1]);
     }
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        const uint32_t h = (uint32_t)__shfl_xor((int)hi, d), l = (uint32_t)__shfl_xor((int)lo, d);
-        hi = h > hi ? h : hi;
-        lo = l < lo ? l : lo;
-    }
-    if (lane == 0) {
-        w32[0][w] = hi;
-        w32[1][w] = lo;
-    }
+    Span<float>::all_extremes(ext, w, lane, hi, lo);
     __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kNW; ++i) {
-        hi = w32[0][i] > hi ? w32[0][i] : hi;
-        lo = w32[1][i] < lo ? w32[1][i] : lo;
-    }
-    __syncthreads();
-    return Row(a, r, hi, lo, scale);
+    return Row(ask, a.V, hi, lo, scale);
 }
 
 template <typename T>
@@ -639,22 +734,23 @@ __global__ __launch_bounds__(kNT) void sample_histogram_kernel(SampleArgs a, Spa
                                                                double scale) {
     __shared__ uint32_t cnt[kBins];
     __shared__ u64 mass[kBins];
-    __shared__ uint32_t w32[2][kNW];
+    __shared__ float ext[2][kNW];
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
+    const Ask ask(a, r);
     const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
     for (int b = tid; b < kBins; b += kNT) {
         cnt[b] = 0;
         mass[b] = 0;
     }
-    const Row row = row_of(a, ws, r, spans, scale, w32, tid, lane, w);
+    const Row row = row_of(a, ws, r, spans, scale, ask, ext, tid, lane, w);
     if (row.bad || row.k == 1 || !row.cuts(a.V)) return;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-        const u64 q = row.fixed(sp.key[i]);
+        const u64 q = row.fixed(sp.v[i]);
         if (q) {
-            const int bin = row.bin(sp.key[i]);
+            const int bin = row.bin(sp.v[i]);
             atomicAdd(&cnt[bin], 1u);
             atomicAdd(&mass[bin], q);
         }
@@ -675,55 +771,44 @@ __global__ __launch_bounds__(kNT) void sample_collect_kernel(SampleArgs a, SpanW
     __shared__ Shared sm;
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
+    const Ask ask(a, r);
     const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
-    const Row row = row_of(a, ws, r, spans, scale, sm.w32, tid, lane, w);
+    const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
     if (row.bad || row.k == 1 || !row.cuts(a.V)) return;
-    uint32_t c = 0, c0;
-    u64 m = 0, m0;
     for (int b = tid; b < kBins; b += kNT) {
         sm.cnt[b] = ws.cnt[r * kBins + b];
         sm.mass[b] = ws.mass[r * kBins + b];
     }
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kBPT; ++j) {
-        c += sm.cnt[tid * kBPT + j];
-        m += sm.mass[tid * kBPT + j];
-    }
-    c0 = c;
-    m0 = m;
-    block_before(sm, c, m, lane, w);
-    if (tid == kNT - 1) {
-        sm.lo = c + c0;
-        sm.at_mass = m + m0;
-    }
-    __syncthreads();
-    const uint32_t total = sm.lo;
-    u64 least = sm.at_mass, most = least;  // the sum that top-p's share is of
-    __syncthreads();
-    int k_bin = -1, p_from = 0, p_to = -1;
-    if (row.k < (int64_t)total) {
-        pick<kBins>(sm, sm.cnt, sm.mass, c, m, false, (uint64_t)row.k, 0.0, tid);
+    Bins<kBPT> bins(sm.cnt, sm.mass, tid);
+    const Total total = block_before(sm, bins.c, bins.m, lane, w);
+    u64 least = total.m, most = least;  // the sum that top-p's share is of
+    int k_bin = -1, p_from = -1, p_to = -1;
+    if (row.k < (int64_t)total.c) {
+        bins.pick(sm, false, (uint64_t)row.k, 0.0, tid);
         k_bin = sm.at;
         least = sm.above_mass;
         most = sm.above_mass + sm.at_mass;
         __syncthreads();
     }
     if (row.top_p < 1.0f) {
-        pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, (double)row.top_p * (double)least, tid);
-        p_from = sm.at < 0 ? 0 : sm.at;  // none: the least sum is 0, any bin may be it
-        __syncthreads();
-        pick<kBins>(sm, sm.cnt, sm.mass, c, m, true, 0, (double)row.top_p * (double)most, tid);
+        p_from = 0;  // where the least sum is 0, any bin may be it
+        if (least > 0) {
+            bins.pick(sm, true, 0, (double)row.top_p * (double)least, tid);
+            p_from = sm.at;
+            __syncthreads();
+        }
+        bins.pick(sm, true, 0, (double)row.top_p * (double)most, tid);
         p_to = sm.at;
     }
+    const auto of_k = row.within(k_bin, k_bin), of_p = row.within(p_from, p_to);
     u64 q[kItems];
     uint32_t n = 0;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
-        const int bin = row.bin(sp.key[i]);
-        const bool in = (sp.key[i] > kKeyNegInf) & ((bin == k_bin) | ((bin >= p_from) & (bin <= p_to)));
-        q[i] = in ? row.fixed(sp.key[i]) : 0;
+        const bool in = (sp.v[i] > -kInf) & (of_k(sp.v[i]) | of_p(sp.v[i]));
+        q[i] = in ? row.fixed(sp.v[i]) : 0;
         n += q[i] != 0;
     }
     // One addition to the row's counter for the workgroup's items.
@@ -737,7 +822,7 @@ __global__ __launch_bounds__(kNT) void sample_collect_kernel(SampleArgs a, SpanW
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
         if (q[i]) {
-            ws.list[r * a.V + at] = sp.key[i];
+            ws.list[r * a.V + at] = sp.v[i];
             ws.list_q[r * a.V + at] = q[i];
             ++at;
         }
@@ -748,10 +833,11 @@ __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs
     __shared__ Shared sm;
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x;
-    const Row row = row_of(a, ws, r, spans, scale, sm.w32, tid, lane, w);
-    Border b{0, 0};
+    const Ask ask(a, r);
+    const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
+    Border b{-kInf, 0};
     if (!row.bad && row.k == 1) {
-        b = Border{row.hi, 1};
+        b = Border{row.top, 1};
     } else if (!row.bad && row.cuts(a.V)) {
         for (int i = tid; i < kBins; i += kNT) {
             sm.cnt[i] = ws.cnt[r * kBins + i];
@@ -759,7 +845,7 @@ __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs
         }
         __syncthreads();
         const uint32_t n = ws.found[r];
-        const uint32_t* list = ws.list + r * a.V;
+        const float* list = ws.list + r * a.V;
         const u64* list_q = ws.list_q + r * a.V;
         b = find_border(sm, row, [&](auto f) {
             for (uint32_t i = tid; i < n; i += kNT) f(list[i], list_q[i]);
@@ -771,29 +857,31 @@ __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs
 template <typename T>
 __global__ __launch_bounds__(kNT) void sample_sums_kernel(SampleArgs a, SpanWs ws, int spans,
                                                           double scale) {
-    __shared__ uint32_t w32[2][kNW];
+    __shared__ uint32_t w32[kNW];
+    __shared__ float ext[2][kNW];
     __shared__ u64 w64[kNW];
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
+    const Ask ask(a, r);
     const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
-    const Row row = row_of(a, ws, r, spans, scale, w32, tid, lane, w);
+    const Row row = row_of(a, ws, r, spans, scale, ask, ext, tid, lane, w);
     if (row.bad) return;
     const Border b = ws.border[r];
     u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
-        if (sp.key[i] > b.key) sum += weight_of(row, sp.key[i]);
+        if (sp.v[i] > b.at) sum += weight_of(row, sp.v[i]);
     sum = wave_sum(sum);
     const uint32_t ties = wave_ties(sp, b);
     if (lane == 0) {
         w64[w] = sum;
-        w32[0][w] = ties;
+        w32[w] = ties;
     }
     __syncthreads();
     if (tid == 0) {
         ws.sum[blockIdx.x] = w64[0] + w64[1] + w64[2] + w64[3];
-        ws.ties[blockIdx.x] = w32[0][0] + w32[0][1] + w32[0][2] + w32[0][3];
+        ws.ties[blockIdx.x] = w32[0] + w32[1] + w32[2] + w32[3];
     }
 }
 
@@ -802,17 +890,18 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
                                                             double scale) {
     __shared__ Shared sm;
     __shared__ u64 pick_from, pick_all;
-    __shared__ uint64_t pick_ties;
+    __shared__ uint32_t pick_ties;
     __shared__ int pick_span;
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x;
-    const Row row = row_of(a, ws, r, spans, scale, sm.w32, tid, lane, w);
+    const Ask ask(a, r);
+    const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
     if (row.bad) {
         if (tid == 0) none(a, r);
         return;
     }
     const Border b = ws.border[r];
-    const u64 tie_q = b.key ? weight_of(row, b.key) : 0;
+    const u64 tie_q = b.ties ? weight_of(row, b.at) : 0;
     const u64* sums = ws.sum + r * spans;
     const uint32_t* ties = ws.ties + r * spans;
     // Consecutive spans to a thread.
@@ -840,7 +929,7 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
     if (tid == 0) pick_span = -1;
     __syncthreads();
     const u64 all = pick_all;
-    const double target = (double)a.u[r] * (double)all;
+    const double target = (double)ask.u * (double)all;
     t = t_before;
     u64 run = from;
     for (int i = s0; i < s1; ++i) {
@@ -859,13 +948,13 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
     const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
     u64 q[kItems];
 #pragma unroll
-    for (int i = 0; i < kItems; ++i) q[i] = sp.key[i] >= b.key ? weight_of(row, sp.key[i]) : 0;
+    for (int i = 0; i < kItems; ++i) q[i] = sp.v[i] >= b.at ? weight_of(row, sp.v[i]) : 0;
     const uint32_t wt = wave_ties(sp, b);
-    if (lane == 0) sm.w32[0][w] = wt;
+    if (lane == 0) sm.w32[w] = wt;
     __syncthreads();
-    uint64_t before = pick_ties;
-    for (int i = 0; i < w; ++i) before += sm.w32[0][i];
-    keep(sp, row, b, before, q, lane);
+    uint32_t before = pick_ties;
+    for (int i = 0; i < w; ++i) before += sm.w32[i];
+    keep(sp, b, before, q);
     u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < kItems; ++i) sum += q[i];
@@ -897,11 +986,11 @@ SpanWs layout(char* p, int64_t B, int64_t V, size_t* bytes) {
     };
     const size_t rows = (size_t)B, spans = (size_t)spans_of(V);
     SpanWs w;
-    w.ext = (uint32_t*)take(rows * spans * 8);
+    w.ext = (float*)take(rows * spans * 8);
     w.cnt = (uint32_t*)take(rows * kBins * 4);
     w.mass = (u64*)take(rows * kBins * 8);
     w.found = (uint32_t*)take(rows * 4);
-    w.list = (uint32_t*)take(rows * (size_t)V * 4);
+    w.list = (float*)take(rows * (size_t)V * 4);
     w.list_q = (u64*)take(rows * (size_t)V * 8);
     w.border = (Border*)take(rows * sizeof(Border));
     w.sum = (u64*)take(rows * spans * 8);
