@@ -98,23 +98,29 @@ __device__ __forceinline__ float wave_least(float v) {
     return lane_of(wave_scan(v, kInf, [](float a, float b) { return fminf(a, b); }), kWave - 1);
 }
 
+// A constant in scalar registers: left to the compiler, those of exp_neg are kept in vector ones.
+__device__ __forceinline__ double scalar(double c) {
+    asm("" : "+s"(c));
+    return c;
+}
+
 // e^x for x in [-46, 0]: x = n ln 2 + t with |t| <= ln 2 / 2, and e^t by its Taylor polynomial
 // of degree 12, whose remainder is below 2e-16 of it.
 __device__ __forceinline__ double exp_neg(double x) {
-    const double n = __builtin_rint(x * 1.4426950408889634074);
+    const double n = __builtin_rint(x * scalar(1.4426950408889634074));
     // ln 2 as its nearest double and what that leaves.
-    double t = __builtin_fma(n, -0.69314718055994530942, x);
-    t = __builtin_fma(n, -2.3190468138462996e-17, t);
-    double p = 1.0 / 479001600.0;
-    p = __builtin_fma(p, t, 1.0 / 39916800.0);
-    p = __builtin_fma(p, t, 1.0 / 3628800.0);
-    p = __builtin_fma(p, t, 1.0 / 362880.0);
-    p = __builtin_fma(p, t, 1.0 / 40320.0);
-    p = __builtin_fma(p, t, 1.0 / 5040.0);
-    p = __builtin_fma(p, t, 1.0 / 720.0);
-    p = __builtin_fma(p, t, 1.0 / 120.0);
-    p = __builtin_fma(p, t, 1.0 / 24.0);
-    p = __builtin_fma(p, t, 1.0 / 6.0);
+    double t = __builtin_fma(n, scalar(-0.69314718055994530942), x);
+    t = __builtin_fma(n, scalar(-2.3190468138462996e-17), t);
+    double p = scalar(1.0 / 479001600.0);
+    p = __builtin_fma(p, t, scalar(1.0 / 39916800.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 3628800.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 362880.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 40320.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 5040.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 720.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 120.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 24.0));
+    p = __builtin_fma(p, t, scalar(1.0 / 6.0));
     p = __builtin_fma(p, t, 0.5);
     p = __builtin_fma(p, t, 1.0);
     p = __builtin_fma(p, t, 1.0);
@@ -138,6 +144,23 @@ struct Ask {
         u = a.u[row];
     }
 };
+
+// Whether an item (with weight) is of some bins: its step of the histogram lies in [from, to).
+// A NaN is none's; with to a NaN all further ones are the last bin's.
+struct Within {
+    float top, bins, from, to;
+    __device__ __forceinline__ bool operator()(float v) const {
+        const float b = (top - v) * bins;
+        return (b >= from) & !(b >= to);
+    }
+    // Makes this not known to be as before: else the steps of all of a lane's items are kept
+    // from one use to the next, and spill.
+    __device__ __forceinline__ void anew() { asm volatile("" : "+v"(top)); }
+};
+__device__ __forceinline__ uint32_t key_anew(float v) {
+    asm volatile("" : "+v"(v));
+    return key_of(v);
+}
 
 // That, and the measures that the extremes give.
 struct Row {
@@ -174,14 +197,11 @@ struct Row {
         const float b = (top - v) * bins;
         return b < (float)(kBins - 1) ? (int)b : kBins - 1;
     }
-    // Whether an item with weight is of a bin in [from, to]; none is where from is -1.
-    __device__ __forceinline__ auto within(int from, int to) const {
-        const float lo = from < 0 ? __builtin_nanf("") : (float)from;
-        const float hi = to < kBins - 1 ? (float)(to + 1) : __builtin_nanf("");
-        return [this, lo, hi](float v) {
-            const float b = (top - v) * bins;
-            return (b >= lo) & !(b >= hi);
-        };
+    // Bins from..to; none where from is -1.
+    __device__ __forceinline__ Within within(int from, int to) const {
+        const float none = __builtin_nanf("");
+        return Within{top, bins, from < 0 ? none : (float)from,
+                      to < kBins - 1 ? (float)(to + 1) : none};
     }
     // Whether a border has to be looked for.
     __device__ __forceinline__ bool cuts(int64_t V) const { return k < V || top_p < 1.0f; }
@@ -234,18 +254,19 @@ __device__ __forceinline__ Total block_before(Shared& sm, uint32_t& c, u64& m, i
     return t;
 }
 
-// A thread's N consecutive bins, with what lies before them.
+// A thread's N consecutive bins of a histogram in LDS: what they hold, then what lies before them.
 template <int N>
 struct Bins {
-    uint32_t n[N], c;
-    u64 q[N], m;
-    __device__ __forceinline__ Bins(const uint32_t* cnt, const u64* mass, int tid) : c(0), m(0) {
+    const uint32_t* cnt;
+    const u64* mass;
+    uint32_t c = 0;
+    u64 m = 0;
+    __device__ __forceinline__ Bins(const uint32_t* cnt_, const u64* mass_, int tid)
+        : cnt(cnt_ + tid * N), mass(mass_ + tid * N) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            n[j] = cnt[tid * N + j];
-            q[j] = mass[tid * N + j];
-            c += n[j];
-            m += q[j];
+            c += cnt[j];
+            m += mass[j];
         }
     }
     // The bin before which there is less than wanted (want_cnt items, or a weight of want_mass)
@@ -257,17 +278,19 @@ struct Bins {
         u64 mj = m;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const bool in = by_mass ? (double)mj < want_mass && !((double)(mj + q[j]) < want_mass)
-                                    : cj < want_cnt && !(cj + n[j] < want_cnt);
+            const uint32_t n = cnt[j];
+            const u64 q = mass[j];
+            const bool in = by_mass ? (double)mj < want_mass && !((double)(mj + q) < want_mass)
+                                    : cj < want_cnt && !(cj + n < want_cnt);
             if (in) {
                 sm.at = tid * N + j;
                 sm.above_cnt = cj;
                 sm.above_mass = mj;
-                sm.at_cnt = n[j];
-                sm.at_mass = q[j];
+                sm.at_cnt = n;
+                sm.at_mass = q;
             }
-            cj += n[j];
-            mj += q[j];
+            cj += n;
+            mj += q;
         }
         __syncthreads();
     }
@@ -285,18 +308,19 @@ __device__ __forceinline__ uint32_t ties_within(uint32_t ties, u64 q, u64 before
 }
 
 // Searches one bin further.  each(f) calls f(v, q) for the items that may be of it (all with
-// weight; NaN is passed over), member() tells which are; `above` of sm is what lies before the bin and is brought to what lies before
+// weight; NaN is passed over), those from `from` on that `bin` takes are; `above` of sm is what lies before the bin and is brought to what lies before
 // the logit found, which has sm.at_cnt items.
-template <typename Each, typename Member>
-__device__ __forceinline__ float refine(Shared& sm, Each each, Member member, bool by_mass,
+template <typename Each>
+__device__ __forceinline__ float refine(Shared& sm, Each each, Within bin, float from, bool by_mass,
                                         uint64_t want_cnt, double want_mass, int tid, int lane,
                                         int w) {
-    float from = -kInf, to = kInf;
+    float to = kInf;
     uint32_t base_c = sm.above_cnt;
     u64 base_m = sm.above_mass;
     // Each search leaves at most a 128th of the keys' range: five come down to one key.
     for (int depth = 0; depth < 8; ++depth) {
         const bool few = sm.at_cnt <= (uint32_t)kWave;
+        bin.anew();
         __syncthreads();
         if (few) {
             // The usual case: each item is compared with all others, a lane of the first wave an
@@ -305,7 +329,7 @@ __device__ __forceinline__ float refine(Shared& sm, Each each, Member member, bo
             if (tid == 0) sm.hi = 0;
             __syncthreads();
             each([&](float v, u64 q) {
-                if ((v >= from) & (v <= to) & member(v)) {
+                if ((v >= from) & (v <= to) & bin(v)) {
                     const uint32_t i = atomicAdd(&sm.hi, 1u);
                     sm.few[i] = v;
                     sm.fine_mass[i] = q;
@@ -317,9 +341,10 @@ __device__ __forceinline__ float refine(Shared& sm, Each each, Member member, bo
                 const float v = sm.few[tid];
                 uint32_t c = base_c, same = 0;
                 u64 m = base_m;
-                for (uint32_t i = 0; i < n; i += 8) {
+#pragma unroll 1
+                for (uint32_t i = 0; i < n; i += 4) {
 #pragma unroll
-                    for (uint32_t j = i; j < i + 8; ++j) {  // behind the last: -inf, above none
+                    for (uint32_t j = i; j < i + 4; ++j) {  // behind the last: -inf, above none
                         const float o = sm.few[j];
                         const u64 q = sm.fine_mass[j];
                         c += o > v;
@@ -351,8 +376,8 @@ __device__ __forceinline__ float refine(Shared& sm, Each each, Member member, bo
         __syncthreads();
         uint32_t lo = 0xFFFFFFFFu, hi = 0;
         each([&](float v, u64) {
-            const bool in = (v >= from) & (v <= to) & member(v);
-            const uint32_t key = key_of(v);
+            const bool in = (v >= from) & (v <= to) & bin(v);
+            const uint32_t key = key_anew(v);
             lo = in && key < lo ? key : lo;
             hi = in && key > hi ? key : hi;
         });
@@ -367,8 +392,8 @@ __device__ __forceinline__ float refine(Shared& sm, Each each, Member member, bo
         const int bits = 32 - __clz((int)((hi - lo) | 1u));
         const int shift = bits > 8 ? bits - 8 : 0;
         each([&](float v, u64 q) {
-            if ((v >= from) & (v <= to) & member(v)) {
-                const uint32_t b = (hi - key_of(v)) >> shift;
+            if ((v >= from) & (v <= to) & bin(v)) {
+                const uint32_t b = (hi - key_anew(v)) >> shift;
                 atomicAdd(&sm.fine_cnt[b], 1u);
                 atomicAdd(&sm.fine_mass[b], q);
             }
@@ -404,8 +429,8 @@ __device__ __forceinline__ Border find_border(Shared& sm, const Row& row, Each e
     u64 tie_q = 0;
     if (row.k < (int64_t)total.c) {
         bins.pick(sm, false, (uint64_t)row.k, 0.0, tid);
-        b.at = refine(sm, each, row.within(sm.at, sm.at), false, (uint64_t)row.k, 0.0, tid, lane,
-                      w);
+        b.at = refine(sm, each, row.within(sm.at, sm.at), -kInf, false, (uint64_t)row.k, 0.0, tid,
+                      lane, w);
         b.ties = (uint32_t)(row.k - sm.above_cnt);
         above = sm.above_mass;
         tie_q = row.fixed(b.at);
@@ -415,12 +440,10 @@ __device__ __forceinline__ Border find_border(Shared& sm, const Row& row, Each e
         if ((double)above < want) {
             if (b.ties) b.ties = ties_within(b.ties, tie_q, above, want);
         } else {
-            const float edge = b.at;
+            const float next = value_of(key_of(b.at) + 1);  // the float above the first border
             __syncthreads();  // what the first search left in sm has been read
             bins.pick(sm, true, 0, want, tid);
-            const auto in = row.within(sm.at, sm.at);
-            b.at = refine(sm, each, [&](float v) { return (v > edge) & in(v); }, true, 0, want,
-                          tid, lane, w);
+            b.at = refine(sm, each, row.within(sm.at, sm.at), next, true, 0, want, tid, lane, w);
             b.ties = ties_within(sm.at_cnt, row.fixed(b.at), sm.above_mass, want);
         }
     }
@@ -433,14 +456,14 @@ __device__ __forceinline__ Border find_border(Shared& sm, const Row& row, Each e
 template <typename T>
 struct Span {
     float v[kItems];
-    __device__ __forceinline__ static int64_t index(int64_t base, int w, int it, int lane) {
+    __device__ __forceinline__ static int index(int base, int w, int it, int lane) {
         return base + (w * kIT + it) * 256 + lane * 4;
     }
-    __device__ __forceinline__ Span(const T* p, int64_t V, int64_t base, int w, int lane) {
+    __device__ __forceinline__ Span(const T* p, int V, int base, int w, int lane) {
         const bool vec = ((uintptr_t)p) % (4 * sizeof(T)) == 0;
 #pragma unroll
         for (int it = 0; it < kIT; ++it) {
-            const int64_t i = index(base, w, it, lane);
+            const int i = index(base, w, it, lane);
             float x[4];
             if (vec && i + 4 <= V) {
                 unpack_vec<T, 4>(*(const typename VecT<T, 4>::type*)(p + i), x);
@@ -487,6 +510,8 @@ struct Span {
             hi = fmaxf(hi, ext[0][i]);
             lo = fminf(lo, ext[1][i]);
         }
+        hi = lane_of(hi, 0);
+        lo = lane_of(lo, 0);
     }
 };
 
@@ -539,9 +564,9 @@ __device__ __forceinline__ u64 weight_of(const Row& row, float v) {
 // else the wave's last one with weight; written by the lane that has it.
 template <typename T>
 __device__ __forceinline__ void choose(const SampleArgs& a, const Span<T>& sp, const Row& row,
-                                       const u64 (&q)[kItems], int64_t r, int64_t base, u64 run,
+                                       const u64 (&q)[kItems], int64_t r, int base, u64 run,
                                        double target, u64 all, int w, int lane) {
-    int64_t found = -1, tail = -1;
+    int found = -1, tail = -1;
     float v_found = 0.0f, v_tail = 0.0f;
 #pragma unroll
     for (int it = 0; it < kIT; ++it) {
@@ -567,9 +592,9 @@ __device__ __forceinline__ void choose(const SampleArgs& a, const Span<T>& sp, c
     const float best = wave_least(found >= 0 ? (float)found : none);
     const float end = wave_top((float)tail);
     const bool got = best != none;
-    const int64_t id = (int64_t)(got ? best : end);
+    const int id = (int)(got ? best : end);
     if (got ? found == id : tail == id) {
-        a.ids[r] = (int32_t)id;
+        a.ids[r] = id;
         const double wt = row.greedy ? 1.0 : row.weight(got ? v_found : v_tail);
         if (a.prob) a.prob[r] = (float)(wt * row.scale / (double)all);
     }
@@ -591,11 +616,11 @@ __device__ __forceinline__ bool is_part(u64 from, u64 sum, u64 all, double targe
 
 // ------------------------------------------------------------------ a row in one workgroup
 template <typename T>
-__global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double scale) {
+__global__ __launch_bounds__(kNT, 4) void sample_row_kernel(SampleArgs a, double scale) {
     __shared__ Shared sm;
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x;
-    Span<T> sp((const T*)a.logits + r * a.V, a.V, 0, w, lane);
+    Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, 0, w, lane);
     const Ask ask(a, r);
     for (int b = tid; b < kBins; b += kNT) {
         sm.cnt[b] = 0;
@@ -636,7 +661,6 @@ __global__ __launch_bounds__(kNT, 3) void sample_row_kernel(SampleArgs a, double
             auto each = [&](auto f) {
 #pragma unroll
                 for (int i = 0; i < kItems; ++i) f(sp.v[i], q[i]);
-                sp.phase();
             };
             sp.phase();
             b = find_border(sm, row, each, tid, lane, w);
@@ -698,8 +722,8 @@ __global__ __launch_bounds__(kNT) void sample_extremes_kernel(SampleArgs a, Span
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
     const int s = (int)(blockIdx.x - (unsigned)r * (unsigned)spans);
-    const int64_t base = (int64_t)s * kSpan;
-    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    const int base = s * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
     float hi, lo;
     sp.extremes(ext, w, lane, hi, lo);
     if (tid == 0) {
@@ -738,8 +762,8 @@ __global__ __launch_bounds__(kNT) void sample_histogram_kernel(SampleArgs a, Spa
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
     const Ask ask(a, r);
-    const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
-    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    const int base = (int)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
     for (int b = tid; b < kBins; b += kNT) {
         cnt[b] = 0;
         mass[b] = 0;
@@ -772,8 +796,8 @@ __global__ __launch_bounds__(kNT) void sample_collect_kernel(SampleArgs a, SpanW
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
     const Ask ask(a, r);
-    const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
-    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    const int base = (int)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
     const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
     if (row.bad || row.k == 1 || !row.cuts(a.V)) return;
     for (int b = tid; b < kBins; b += kNT) {
@@ -863,8 +887,8 @@ __global__ __launch_bounds__(kNT) void sample_sums_kernel(SampleArgs a, SpanWs w
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x / (unsigned)spans;
     const Ask ask(a, r);
-    const int64_t base = (int64_t)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
-    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    const int base = (int)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
     const Row row = row_of(a, ws, r, spans, scale, ask, ext, tid, lane, w);
     if (row.bad) return;
     const Border b = ws.border[r];
@@ -944,8 +968,8 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
     }
     __syncthreads();
     if (pick_span < 0) return;  // no weight anywhere (not reached: the largest weighs 1)
-    const int64_t base = (int64_t)pick_span * kSpan;
-    const Span<T> sp((const T*)a.logits + r * a.V, a.V, base, w, lane);
+    const int base = pick_span * kSpan;
+    const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
     u64 q[kItems];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) q[i] = sp.v[i] >= b.at ? weight_of(row, sp.v[i]) : 0;
