@@ -787,6 +787,27 @@ __global__ __launch_bounds__(kNT) void sample_histogram_kernel(SampleArgs a, Spa
         }
 }
 
+// A row's histogram on its way from memory to LDS, read before the row is known.
+struct Fetched {
+    uint32_t cnt[kBPT];
+    u64 mass[kBPT];
+    __device__ __forceinline__ Fetched(const SpanWs& ws, int64_t r, int tid) {
+#pragma unroll
+        for (int j = 0; j < kBPT; ++j) {
+            cnt[j] = ws.cnt[r * kBins + j * kNT + tid];
+            mass[j] = ws.mass[r * kBins + j * kNT + tid];
+        }
+    }
+    __device__ __forceinline__ void put(Shared& sm, int tid) const {
+#pragma unroll
+        for (int j = 0; j < kBPT; ++j) {
+            sm.cnt[j * kNT + tid] = cnt[j];
+            sm.mass[j * kNT + tid] = mass[j];
+        }
+        __syncthreads();
+    }
+};
+
 // The items of the bins that can hold a border: top-k's bin, and the bins in which top-p's may
 // lie, whose share is of a sum that top-k's bin makes uncertain.
 template <typename T>
@@ -798,13 +819,10 @@ __global__ __launch_bounds__(kNT) void sample_collect_kernel(SampleArgs a, SpanW
     const Ask ask(a, r);
     const int base = (int)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
+    const Fetched hist(ws, r, tid);
     const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
     if (row.bad || row.k == 1 || !row.cuts(a.V)) return;
-    for (int b = tid; b < kBins; b += kNT) {
-        sm.cnt[b] = ws.cnt[r * kBins + b];
-        sm.mass[b] = ws.mass[r * kBins + b];
-    }
-    __syncthreads();
+    hist.put(sm, tid);
     Bins<kBPT> bins(sm.cnt, sm.mass, tid);
     const Total total = block_before(sm, bins.c, bins.m, lane, w);
     u64 least = total.m, most = least;  // the sum that top-p's share is of
@@ -858,21 +876,31 @@ __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x;
     const Ask ask(a, r);
+    // Everything is read at once, the list's first items too: they stay in registers, since the
+    // searches go over them up to ten times.
+    constexpr int kHeld = 8;
+    const Fetched hist(ws, r, tid);
+    const uint32_t n = ws.found[r];
+    const float* list = ws.list + r * a.V;
+    const u64* list_q = ws.list_q + r * a.V;
+    float v[kHeld];
+    u64 q[kHeld];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+        const uint32_t i = tid + j * kNT;
+        v[j] = i < n ? list[i] : __builtin_nanf("");
+        q[j] = i < n ? list_q[i] : 0;
+    }
     const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
     Border b{-kInf, 0};
     if (!row.bad && row.k == 1) {
         b = Border{row.top, 1};
     } else if (!row.bad && row.cuts(a.V)) {
-        for (int i = tid; i < kBins; i += kNT) {
-            sm.cnt[i] = ws.cnt[r * kBins + i];
-            sm.mass[i] = ws.mass[r * kBins + i];
-        }
-        __syncthreads();
-        const uint32_t n = ws.found[r];
-        const float* list = ws.list + r * a.V;
-        const u64* list_q = ws.list_q + r * a.V;
+        hist.put(sm, tid);
         b = find_border(sm, row, [&](auto f) {
-            for (uint32_t i = tid; i < n; i += kNT) f(list[i], list_q[i]);
+#pragma unroll
+            for (int j = 0; j < kHeld; ++j) f(v[j], q[j]);
+            for (uint32_t i = tid + kHeld * kNT; i < n; i += kNT) f(list[i], list_q[i]);
         }, tid, lane, w);
     }
     if (tid == 0) ws.border[r] = b;
@@ -889,9 +917,9 @@ __global__ __launch_bounds__(kNT) void sample_sums_kernel(SampleArgs a, SpanWs w
     const Ask ask(a, r);
     const int base = (int)(blockIdx.x - (unsigned)r * (unsigned)spans) * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
+    const Border b = ws.border[r];
     const Row row = row_of(a, ws, r, spans, scale, ask, ext, tid, lane, w);
     if (row.bad) return;
-    const Border b = ws.border[r];
     u64 sum = 0;
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
@@ -919,19 +947,24 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
     const int tid = threadIdx.x, lane = tid % kWave, w = wave_id();
     const int64_t r = blockIdx.x;
     const Ask ask(a, r);
+    const Border b = ws.border[r];
+    const u64* sums = ws.sum + r * spans;
+    const uint32_t* ties = ws.ties + r * spans;
+    // Consecutive spans to a thread.
+    const int per = (spans + kNT - 1) / kNT, s0 = tid * per, s1 = s0 + per < spans ? s0 + per : spans;
+    // The first of them is read ahead: that is all for up to 2^20 items.
+    const u64 first_sum = s0 < s1 ? sums[s0] : 0;
+    const uint32_t first_ties = s0 < s1 ? ties[s0] : 0;
+    auto sum_of = [&](int i) { return i == s0 ? first_sum : sums[i]; };
+    auto ties_of = [&](int i) { return i == s0 ? first_ties : ties[i]; };
     const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
     if (row.bad) {
         if (tid == 0) none(a, r);
         return;
     }
-    const Border b = ws.border[r];
     const u64 tie_q = b.ties ? weight_of(row, b.at) : 0;
-    const u64* sums = ws.sum + r * spans;
-    const uint32_t* ties = ws.ties + r * spans;
-    // Consecutive spans to a thread.
-    const int per = (spans + kNT - 1) / kNT, s0 = tid * per, s1 = s0 + per < spans ? s0 + per : spans;
     uint32_t t_own = 0;
-    for (int i = s0; i < s1; ++i) t_own += ties[i];
+    for (int i = s0; i < s1; ++i) t_own += ties_of(i);
     uint32_t t_before = t_own;
     u64 unused = 0;
     block_before(sm, t_before, unused, lane, w);
@@ -942,8 +975,8 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
     u64 own = 0;
     uint32_t t = t_before;
     for (int i = s0; i < s1; ++i) {
-        own += sums[i] + tie_q * kept_ties(t, ties[i]);
-        t += ties[i];
+        own += sum_of(i) + tie_q * kept_ties(t, ties_of(i));
+        t += ties_of(i);
     }
     __syncthreads();
     u64 from = own;
@@ -957,14 +990,14 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
     t = t_before;
     u64 run = from;
     for (int i = s0; i < s1; ++i) {
-        const u64 s = sums[i] + tie_q * kept_ties(t, ties[i]);
+        const u64 s = sum_of(i) + tie_q * kept_ties(t, ties_of(i));
         if (is_part(run, s, all, target, s != 0 && run + s == all)) {
             pick_from = run;
             pick_ties = t;
             pick_span = i;
         }
         run += s;
-        t += ties[i];
+        t += ties_of(i);
     }
     __syncthreads();
     if (pick_span < 0) return;  // no weight anywhere (not reached: the largest weighs 1)
