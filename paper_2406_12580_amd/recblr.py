@@ -647,6 +647,13 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     return ids, prob
 
 
+# A list of tensors is checked by these in a map each: half the time of a loop over attributes,
+# and a step over a model's few dozen tensors is bound by them.
+_numel, _data_ptr = torch.Tensor.numel, torch.Tensor.data_ptr
+_get_device, _is_contiguous = torch.Tensor.get_device, torch.Tensor.is_contiguous
+_dtype = torch.Tensor.dtype.__get__
+
+
 class AdamW:
     """AdamW over a list of tensors (float32 or bfloat16, all of one type and device).
 
@@ -722,17 +729,16 @@ class AdamW:
         """One update with grads, a tensor for each parameter; lr overrides the rate."""
         if len(grads) != len(self._sizes):
             raise ValueError("grads: one tensor for each parameter is needed")
-        dtype, index, ptrs = self.dtype, self.device.index, []
-        for t, n in zip(grads, self._sizes):
-            if t.dtype is not dtype or t.numel() != n or t.get_device() != index \
-                    or not t.is_contiguous():
-                self._flat(t, dtype, n, "grads")  # says what is wrong
-            ptrs.append(t.data_ptr())
-        self._grads[:] = ptrs
-        at = [p.data_ptr() for p in self.params]
+        if not (list(map(_numel, grads)) == self._sizes and all(map(_is_contiguous, grads))
+                and set(map(_get_device, grads)) == {self.device.index}
+                and set(map(_dtype, grads)) == {self.dtype}):
+            for t, n in zip(grads, self._sizes):
+                self._flat(t, self.dtype, n, "grads")  # says what is wrong
+        self._grads[:] = list(map(_data_ptr, grads))
+        at = list(map(_data_ptr, self.params))
         if at != self._at:  # a parameter's memory was replaced (p.data = ...)
             for entry, p, n in zip(self._table, self.params, self._sizes):
-                entry.param = self._flat(p, dtype, n, "params")
+                entry.param = self._flat(p, self.dtype, n, "params")
             self._at = at
         _adamw_step(self, self.lr if lr is None else lr, stream=stream)
         self.steps += 1
