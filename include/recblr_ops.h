@@ -30,8 +30,8 @@ extern "C" {
  *     o_t = scale S_t^T q_t
  *   q, k : [B][L][H][Dk] io;  v, o : [B][L][HV][Dv] io;  g, beta : [B][L][HV] io
  *   h0, hT and every other state : [B][HV][Dk][Dv] float
- * 1 <= Dk, Dv <= 128 (else UNSUPPORTED), HV a multiple of H (else
- * INVALID_ARGUMENT).  g is the logarithm of the decay, usually <= 0; below -100
+ * 1 <= Dk, Dv <= 128, HV <= 4096, B HV ceil(Dv / 32) and B HV ceil(L / 64) below 2^24
+ * (else UNSUPPORTED), HV a multiple of H (else INVALID_ARGUMENT).  g is the logarithm of the decay, usually <= 0; below -100
  * it counts as -100, so -inf clears the state.  A step with g = 0 and beta = 0
  * leaves the state as it is (padding); queries and keys are taken as given
  * (they are usually brought to length one by the caller).  Inputs are finite, in
@@ -103,7 +103,7 @@ int recblr_delta_step(const void* q, const void* k, const void* v, const void* g
  * Errors: INVALID_ARGUMENT for a NULL list or pointer, misalignment, n < 0,
  * step < 1, or a tensor that is written and overlaps another one of the call
  * (the same tensor listed twice is one case); UNSUPPORTED for other state_bits
- * or io, or n > 2^40.  `tensors` is host memory, read before the call returns.
+ * or io, or n > 2^36 - 4096.  `tensors` is host memory, read before the call returns.
  */
 enum { RECBLR_ADAMW_BLOCK = 256 };
 
@@ -148,7 +148,8 @@ int recblr_adamw_moments(const recblr_adamw_tensor* tensors, int64_t count,
  * id -1 and prob 0.
  * w are formed in 64 bits and summed as integers of 2^-F, F = 62 - ceil(log2 V), at
  * most 51: sums are exact whatever their order, and a w below half of that is 0.
- * Errors: INVALID_ARGUMENT, UNSUPPORTED (io, V > 2^24, B > 2^31 - 1), WORKSPACE.
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED (io, V > 2^24, B max(1, ceil(V / 4096)) >= 2^24),
+ * WORKSPACE.
  */
 size_t recblr_sample_workspace_size(int64_t B, int64_t V, int io);
 int recblr_sample(const void* logits, const float* u, const float* temperature,

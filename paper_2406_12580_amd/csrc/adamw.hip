@@ -300,7 +300,7 @@ hipError_t in_tables(int64_t count, const recblr_adamw_tensor* tensors, Fill fil
     for (int64_t i = 0; i < count; ++i) {
         const int64_t need = (tensors[i].n + kChunk - 1) / kChunk;
         if (need == 0) continue;
-        if (used == kMaxTensors || chunks + need > 0x7FFFFFFF) {
+        if (used == kMaxTensors || chunks + need >= (1 << 24)) {
             const hipError_t e = flush();
             if (e != hipSuccess) return e;
         }

@@ -36,7 +36,9 @@ bool ranges_disjoint(Range* r, int64_t n) {
     return true;
 }
 
-constexpr int64_t kMaxAdamN = (int64_t)1 << 40;
+// A launch has fewer than 2^32 threads: below this many workgroups of 256.
+constexpr int64_t kMaxGroups = (int64_t)1 << 24;
+constexpr int64_t kMaxAdamN = ((int64_t)1 << 36) - 4096;  // 4096 elements to a workgroup
 constexpr int64_t kMaxTensorCount = (int64_t)1 << 24;
 
 int64_t adam_blocks(int64_t n) { return (n + RECBLR_ADAMW_BLOCK - 1) / RECBLR_ADAMW_BLOCK; }
@@ -118,8 +120,8 @@ int recblr_adamw_moments(const recblr_adamw_tensor* tensors, int64_t count,
 static int sample_sizes(int64_t B, int64_t V, int io) {
     if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
     if (B < 0 || V < 0) return RECBLR_ERR_INVALID_ARGUMENT;
-    if (B > 0x7FFFFFFF || V > ((int64_t)1 << 24)) return RECBLR_ERR_UNSUPPORTED;
-    if (B * ((V + 4095) / 4096) > 0x7FFFFFFF) return RECBLR_ERR_UNSUPPORTED;  // a workgroup each
+    if (B >= kMaxGroups || V > ((int64_t)1 << 24)) return RECBLR_ERR_UNSUPPORTED;
+    if (B * ((V + 4095) / 4096) >= kMaxGroups) return RECBLR_ERR_UNSUPPORTED;  // one each
     return RECBLR_OK;
 }
 
@@ -173,11 +175,10 @@ static int delta_sizes(int64_t B, int64_t L, int64_t H, int64_t HV, int64_t Dk, 
     if (B < 0 || L < 0 || H < 1 || HV < 1 || Dk < 1 || Dv < 1 || HV % H)
         return RECBLR_ERR_INVALID_ARGUMENT;
     if (Dk > 128 || Dv > 128) return RECBLR_ERR_UNSUPPORTED;
-    const int64_t top = (int64_t)1 << 24;
-    if (B >= top || HV > 4096 || L >= ((int64_t)1 << 31)) return RECBLR_ERR_UNSUPPORTED;
-    // A strip of at least 32 columns, and a chunk of 64 steps, is a workgroup of its own.
-    if (B * HV > ((int64_t)1 << 28)) return RECBLR_ERR_UNSUPPORTED;
-    if (B > 0 && (L + 63) / 64 * 4 > 0x7FFFFFFF / (B * HV)) return RECBLR_ERR_UNSUPPORTED;
+    if (B >= kMaxGroups || HV > 4096 || L >= ((int64_t)1 << 31)) return RECBLR_ERR_UNSUPPORTED;
+    // A strip of at least 32 columns, and a chunk of 64 steps, may be a workgroup of its own.
+    if (B * HV * ((Dv + 31) / 32) >= kMaxGroups || B * HV * ((L + 63) / 64) >= kMaxGroups)
+        return RECBLR_ERR_UNSUPPORTED;
     return RECBLR_OK;
 }
 

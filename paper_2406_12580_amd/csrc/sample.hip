@@ -709,8 +709,7 @@ struct SpanWs {
     uint32_t* cnt;    // [B][kBins]
     u64* mass;        // [B][kBins]
     uint32_t* found;  // [B] items in the list
-    float* list;      // [B][V] they
-    u64* list_q;      // [B][V] and their weights
+    float* list;      // [B][V] their logits
     Border* border;   // [B]
     u64* sum;         // [B][S] weight above the border
     uint32_t* ties;   // [B][S] items with the border's logit
@@ -865,7 +864,6 @@ __global__ __launch_bounds__(kNT) void sample_collect_kernel(SampleArgs a, SpanW
     for (int i = 0; i < kItems; ++i)
         if (q[i]) {
             ws.list[r * a.V + at] = sp.v[i];
-            ws.list_q[r * a.V + at] = q[i];
             ++at;
         }
 }
@@ -882,14 +880,12 @@ __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs
     const Fetched hist(ws, r, tid);
     const uint32_t n = ws.found[r];
     const float* list = ws.list + r * a.V;
-    const u64* list_q = ws.list_q + r * a.V;
     float v[kHeld];
     u64 q[kHeld];
 #pragma unroll
     for (int j = 0; j < kHeld; ++j) {
         const uint32_t i = tid + j * kNT;
         v[j] = i < n ? list[i] : __builtin_nanf("");
-        q[j] = i < n ? list_q[i] : 0;
     }
     const Row row = row_of(a, ws, r, spans, scale, ask, sm.ext, tid, lane, w);
     Border b{-kInf, 0};
@@ -897,10 +893,12 @@ __global__ __launch_bounds__(kNT) void sample_border_kernel(SampleArgs a, SpanWs
         b = Border{row.top, 1};
     } else if (!row.bad && row.cuts(a.V)) {
         hist.put(sm, tid);
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) q[j] = row.fixed(v[j]);
         b = find_border(sm, row, [&](auto f) {
 #pragma unroll
             for (int j = 0; j < kHeld; ++j) f(v[j], q[j]);
-            for (uint32_t i = tid + kHeld * kNT; i < n; i += kNT) f(list[i], list_q[i]);
+            for (uint32_t i = tid + kHeld * kNT; i < n; i += kNT) f(list[i], row.fixed(list[i]));
         }, tid, lane, w);
     }
     if (tid == 0) ws.border[r] = b;
@@ -1048,7 +1046,6 @@ SpanWs layout(char* p, int64_t B, int64_t V, size_t* bytes) {
     w.mass = (u64*)take(rows * kBins * 8);
     w.found = (uint32_t*)take(rows * 4);
     w.list = (float*)take(rows * (size_t)V * 4);
-    w.list_q = (u64*)take(rows * (size_t)V * 8);
     w.border = (Border*)take(rows * sizeof(Border));
     w.sum = (u64*)take(rows * spans * 8);
     w.ties = (uint32_t*)take(rows * spans * 4);

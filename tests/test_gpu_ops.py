@@ -662,6 +662,104 @@ def test_sample_graph_and_streams(rb, V):
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def guarded(shape, dtype):
+    """A tensor inside a longer one of sevens, and a check that those are still there."""
+    import torch
+    n = math.prod(shape)
+    buf = torch.full((n + 128,), 7, dtype=dtype, device="cuda")
+    view = buf[64:64 + n].view(shape)
+    return view, lambda: bool((buf[:64] == 7).all()) and bool((buf[64 + n:] == 7).all())
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1, 1, 1, 1, 1, 1), (2, 65, 1, 3, 33, 5), (1, 129, 1, 2, 72, 100),
+                                  (1, 1601, 1, 2, 40, 33)])
+def test_delta_writes_its_outputs_only(rb, io, size):
+    import torch
+    print(io, size, flush=True)
+    B, L, H, HV, Dk, Dv = size
+    c = delta_case(io, *size)
+    dt, f32 = dtype_of(io), torch.float32
+    want = run_delta(rb, c)
+    out = {n: guarded(t.shape, f32 if n in ("hT", "states", "dh0") else dt)
+           for n, t in want.items()}
+    ptr = lambda n: (out[n][0] if n in out else c[n]).data_ptr()  # noqa: E731
+    stream = torch.cuda.current_stream().cuda_stream
+    code = 0 if io == "f32" else 1
+    ins = [ptr(n) for n in ("q", "k", "v", "g", "beta")]
+    for op, call, args in (
+            (rb.OP_DELTA_FORWARD, rb.recblr_delta_forward,
+             [*ins, ptr("h0"), ptr("o"), ptr("hT"), ptr("states")]),
+            (rb.OP_DELTA_BACKWARD, rb.recblr_delta_backward,
+             [*ins, ptr("states"), ptr("do"), ptr("dhT")]
+             + [ptr(n) for n in ("dq", "dk", "dv", "dg", "dbeta", "dh0")])):
+        n = rb.recblr_delta_workspace_size(op, *size, code)
+        ws = torch.full((n + 512,), 7, dtype=torch.uint8, device="cuda")
+        at = -(-ws.data_ptr() // 256) * 256
+        assert call(*args, *size, Dk ** -0.5, code, at if n else None, n, stream) == rb.OK
+        torch.cuda.synchronize()
+        assert bool((ws[at - ws.data_ptr() + n:] == 7).all())
+    for n, (t, whole) in out.items():
+        assert whole(), n
+        assert torch.equal(t, want[n]), n
+
+
+@pytest.mark.parametrize("V", [1, 777, 4099])
+def test_sample_and_adamw_write_their_outputs_only(rb, V):
+    import torch
+    B = 3
+    x, u = torch.randn(B, V, device="cuda"), torch.rand(B, device="cuda")
+    p = torch.full((B,), 0.7, device="cuda")
+    want = rb.sample(x, u, top_p=p)
+    (ids, ids_ok), (prob, prob_ok) = guarded((B,), torch.int32), guarded((B,), torch.float32)
+    n = rb.recblr_sample_workspace_size(B, V, 0)
+    ws = torch.full((n + 512,), 7, dtype=torch.uint8, device="cuda")
+    at = -(-ws.data_ptr() // 256) * 256
+    assert rb.recblr_sample(x.data_ptr(), u.data_ptr(), None, None, p.data_ptr(), None,
+                            ids.data_ptr(), prob.data_ptr(), B, V, 0, at if n else None, n,
+                            torch.cuda.current_stream().cuda_stream) == rb.OK
+    torch.cuda.synchronize()
+    assert ids_ok() and prob_ok() and bool((ws[at - ws.data_ptr() + n:] == 7).all())
+    assert torch.equal(ids, want[0]) and torch.equal(prob, want[1])
+    f32, blocks = torch.float32, -(-V // 256)
+    parts = [guarded((V,), f32)] + [guarded((V,), t) for t in (torch.int8, torch.uint8)] \
+        + [guarded((blocks,), f32) for _ in range(2)]
+    for t, _ in parts[1:]:
+        t.zero_()
+    opt = rb.AdamW([parts[0][0]], state_bits=8, state=[[t] for t, _ in parts[1:]], **HYPER)
+    opt.step([torch.randn(V, device="cuda")])
+    torch.cuda.synchronize()
+    assert all(ok() for _, ok in parts)
+
+
+def test_delta_gradients_against_differences(rb):
+    """<grad, direction> against the difference of the loss <o, do> + <hT, dhT> over a step.
+
+    The loss is summed in 64 bits; its difference over 2 e is off by e^2 / 6 times the third
+    derivative (inputs of size one, some ten factors of a product chain: 1e2) and by the
+    forward's own bar times the loss's size over e.  e = 2^-7: 1e-3 and 4e-5 / 2^-6 of a loss
+    whose terms' root of squares is `size`; asked is 1e-2 of it."""
+    c = delta_case("f32", 1, 130, 1, 2, 16, 16, seed=9)
+    out = run_delta(rb, c)
+    r, e = np.random.default_rng(1), 2.0 ** -7
+
+    def loss(**moved):
+        d = {**c, **moved}
+        o, hT, _ = rb.delta_forward(*(d[n] for n in ("q", "k", "v", "g", "beta")), h0=d["h0"])
+        return (host(o) * c["do_"]).sum() + (host(hT) * c["dhT_"]).sum()
+
+    size = math.sqrt((host(out["o"]) ** 2 * c["do_"] ** 2).sum()
+                     + (host(out["hT"]) ** 2 * c["dhT_"] ** 2).sum())
+    for name in ("q", "k", "v", "g", "beta", "h0"):
+        way = r.normal(size=c[name + "_"].shape)
+        way /= np.linalg.norm(way)
+        lo, hi = (put(c[name + "_"] + s * e * way, "f32")[0] for s in (-1, 1))
+        diff = (loss(**{name: hi}) - loss(**{name: lo})) / (2 * e)
+        got = (host(out["d" + name]) * way).sum()
+        print(f"ERR d{name}: {abs(got - diff):.2e} of {1e-2 * size:.2e}", flush=True)
+        assert abs(got - diff) <= 1e-2 * size, name
+
+
 # ------------------------------------------------------------------ together
 
 def test_train_and_serve_together(rb):

@@ -98,6 +98,9 @@ def test_delta_refuses_lengths(rb):
         assert call(rb, L=1 << 31) == rb.ERR_UNSUPPORTED
         # more chunks of all heads than workgroups
         assert call(rb, B=1 << 20, L=1 << 20) == rb.ERR_UNSUPPORTED
+        assert call(rb, B=1 << 12, H=1, HV=1, L=64 << 12) == rb.ERR_UNSUPPORTED
+        # more strips of all heads
+        assert call(rb, B=1 << 21, H=2, HV=2, L=1, Dv=128) == rb.ERR_UNSUPPORTED
 
 
 def test_delta_refuses_pointers(rb):
@@ -177,6 +180,7 @@ def test_adamw_refuses(rb):
     assert update(rb, ok, b1=math.nan) == bad
     assert update(rb, tensors(rb, 8, n=-1)) == bad
     assert update(rb, tensors(rb, 8, n=(1 << 40) + 1)) == rb.ERR_UNSUPPORTED
+    assert update(rb, tensors(rb, 8, n=1 << 36)) == rb.ERR_UNSUPPORTED
     for name in ("param", "grad", "m1", "m2"):
         assert update(rb, tensors(rb, 8, **{name: None})) == bad, name
         assert update(rb, tensors(rb, 8, **{name: addr(40) + 2})) == bad, name
@@ -231,6 +235,7 @@ def test_sample_refuses(rb):
     assert draw(rb, io=2) == rb.ERR_UNSUPPORTED
     assert draw(rb, V=(1 << 24) + 1) == rb.ERR_UNSUPPORTED
     assert draw(rb, B=1 << 31) == rb.ERR_UNSUPPORTED
+    assert draw(rb, B=1 << 24, V=1) == rb.ERR_UNSUPPORTED
     assert draw(rb, B=1 << 30, V=1 << 20) == rb.ERR_UNSUPPORTED
     for name in ("logits", "u", "ids"):
         assert draw(rb, **{name: None}) == bad, name
