@@ -760,6 +760,69 @@ def test_delta_gradients_against_differences(rb):
         assert abs(got - diff) <= 1e-2 * size, name
 
 
+# ------------------------------------------------------------------ offsets past 32 bits
+
+def test_delta_long_offsets(rb):
+    """Tensors of more than 2^31 elements: the last rows as in a call of their own."""
+    import torch
+    B, L, H, D = 9000, 1000, 2, 128
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    dt = torch.bfloat16
+    k = torch.empty(B, L, H, D, device="cuda", dtype=dt).normal_(generator=gen).mul_(D ** -0.5)
+    v = torch.empty(B, L, H, D, device="cuda", dtype=dt).normal_(generator=gen)
+    g = torch.empty(B, L, H, device="cuda", dtype=dt).uniform_(-0.1, 0.0, generator=gen)
+    beta = torch.empty(B, L, H, device="cuda", dtype=dt).uniform_(0.0, 1.0, generator=gen)
+    assert k.numel() > 2 ** 31
+    a = (v, k, v, g, beta)                    # v as the queries: any will do
+    o, hT, st = rb.delta_forward(*a, keep_states=True)
+    assert st.numel() > 2 ** 31
+    grads = rb.delta_backward(*a, st, v)
+    cut = tuple(t[-1000:].clone() for t in a)  # enough rows to be walked the same way
+    o2, hT2, st2 = rb.delta_forward(*cut, keep_states=True)
+    grads2 = rb.delta_backward(*cut, st2, cut[2])
+    for x, y in ((o, o2), (hT, hT2), (st, st2), *((grads[n], grads2[n]) for n in grads)):
+        assert torch.equal(x[-1000:], y)
+
+
+def test_delta_step_long_offsets(rb):
+    import torch
+    B, HV, D = 140000, 4, 64
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    h = torch.empty(B, HV, D, D, device="cuda").normal_(generator=gen)
+    assert h.numel() > 2 ** 31
+    q, k, v = (torch.randn(B, HV, D, device="cuda", generator=gen) / 8 for _ in range(3))
+    g, beta = -torch.rand(B, HV, device="cuda"), torch.rand(B, HV, device="cuda")
+    tail = h[-3:].clone()
+    o, _ = rb.delta_step(q, k, v, g, beta, h, out=h)
+    o2, h2 = rb.delta_step(*(t[-3:].clone() for t in (q, k, v, g, beta)), tail)
+    assert torch.equal(o[-3:], o2) and torch.equal(h[-3:], h2)
+
+
+@pytest.mark.parametrize("B,V", [(1200000, 2000), (300, 8000000)])
+def test_sample_long_offsets(rb, B, V):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.empty(B, V, device="cuda", dtype=torch.bfloat16).normal_(generator=gen)
+    assert x.numel() > 2 ** 31
+    u = torch.rand(B, device="cuda", generator=gen)
+    p = torch.full((B,), 0.9, device="cuda")
+    ids, prob = rb.sample(x, u, top_p=p)
+    ids2, prob2 = rb.sample(x[-3:].clone(), u[-3:].clone(), top_p=p[-3:].clone())
+    assert torch.equal(ids[-3:], ids2) and torch.equal(prob[-3:], prob2)
+    assert int(ids.min()) >= 0 and int(ids.max()) < V
+
+
+def test_adamw_long_offsets(rb):
+    import torch
+    n = 2 ** 31 + 4096 + 3
+    p = torch.ones(n, device="cuda", dtype=torch.bfloat16)
+    g = torch.full_like(p, 0.5)
+    opt = rb.AdamW([p], state_bits=8, weight_decay=0.0, lr=0.25)
+    opt.step([g])
+    assert bool((p[-5000:] == 0.75).all()) and bool((p[:5000] == 0.75).all())
+    assert bool((opt.m1[0][-5000:] == 127).all()) and bool((opt.m2[0][-5000:] == 255).all())
+
+
 # ------------------------------------------------------------------ together
 
 def test_train_and_serve_together(rb):
