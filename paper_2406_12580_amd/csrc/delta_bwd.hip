@@ -346,11 +346,6 @@ struct GradLds {
     float dca[C], dcb[C], db[C], part[8];
 };
 
-__device__ __forceinline__ float sum16(float v) {
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) v += __shfl_xor(v, d);
-    return v;
-}
 __device__ __forceinline__ float whole(const float* m, int, int at) { return m[at]; }
 __device__ __forceinline__ float whole(const __bf16* m, int plane, int at) {
     return (float)m[at] + (float)m[at + plane];
@@ -770,37 +765,34 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * w + 4 * g + r;
-            const float s1 = sum16(x1[r]);
+            const float s1 = lanes::row_sum(x1[r]);
             if (side_b) {
                 if (ll == 0) sm.dcb[i] = s1;
             } else {
-                const float s2 = sum16(x2[r]), sy = sum16(yv[r]);
+                const float s2 = lanes::row_sum(x2[r]), sy = lanes::row_sum(yv[r]);
                 if (ll == 0) {
                     sm.dca[i] = fmaf(sm.gt.bt[i], s2, s1);
                     sm.db[i] = sy + s2;
                 }
             }
         }
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) end += __shfl_xor(end, d);
+        end = lanes::wave_sum(end);
         if (lane == 0) sm.part[wave] = end;
         lds_barrier();
         if (wave == 0) {
-            float s = sm.dca[lane] - sm.dcb[lane];
-            if (lane == C - 1) {
+            // The last step first: sums over the steps from each one on are a scan.
+            const int i = C - 1 - lane;
+            float s = sm.dca[i] - sm.dcb[i];
+            if (lane == 0) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s += sm.part[i];
+                for (int j = 0; j < 8; ++j) s += sm.part[j];
             }
-#pragma unroll
-            for (int d = 1; d < C; d <<= 1) {
-                const float o = __shfl_down(s, d);
-                if (lane + d < C) s += o;
-            }
-            const int64_t t = t0 + lane;
+            s = lanes::wave_upto(s);
+            const int64_t t = t0 + i;
             if (t < a.L) {
                 const int64_t at = (b * a.L + t) * a.HV + hv;
                 store((T*)a.dg + at, s);
-                store((T*)a.dbeta + at, sm.db[lane]);
+                store((T*)a.dbeta + at, sm.db[i]);
             }
         }
         if (!side_b) {

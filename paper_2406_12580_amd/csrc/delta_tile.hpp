@@ -20,6 +20,7 @@
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"
+#include "lanes.hpp"
 #include "ops.hpp"
 #include "wave_tile.hpp"
 
@@ -300,13 +301,8 @@ struct Gates {
 // sequence have g = beta = 0.
 __device__ __forceinline__ void gates_of_chunk(Gates* gt, float g, float beta, float scale,
                                                int lane) {
-    double s = (double)delta_clamp_g(g) * 1.4426950408889634074;
-#pragma unroll
-    for (int d = 1; d < C; d <<= 1) {
-        const double o = __shfl_up(s, d);
-        if (lane >= d) s += o;
-    }
-    const double end = __shfl(s, C - 1);
+    const double s = lanes::wave_upto((double)delta_clamp_g(g) * 1.4426950408889634074);
+    const double end = lanes::lane_of(s, C - 1);
     gt->cum[lane] = s;
     gt->eg[lane] = fast_exp2((float)s);
     gt->el[lane] = fast_exp2((float)(end - s));

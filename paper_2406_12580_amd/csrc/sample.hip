@@ -20,10 +20,13 @@
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"
+#include "lanes.hpp"
 #include "ops.hpp"
 
 namespace recblr {
 namespace {
+
+using namespace lanes;
 
 constexpr int kNT = 256;
 constexpr int kNW = kNT / kWave;
@@ -44,53 +47,6 @@ __device__ __forceinline__ float value_of(uint32_t k) {
 }
 constexpr float kInf = __builtin_inff();
 
-typedef unsigned long long u64;
-
-// A register of the lanes that a DPP control names (all lanes active), `old` where there is none.
-// These moves take a few cycles, a shuffle through the LDS crossbar a hundred; a row's kernel is
-// a chain of some eighty of them.
-template <int kCtrl, int kRows>
-__device__ __forceinline__ uint32_t dpp(uint32_t v, uint32_t old) {
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)v, kCtrl, kRows, 0xF, false);
-}
-template <int kCtrl, int kRows>
-__device__ __forceinline__ u64 dpp(u64 v, u64 old) {
-    return (u64)dpp<kCtrl, kRows>((uint32_t)(v >> 32), (uint32_t)(old >> 32)) << 32 |
-           dpp<kCtrl, kRows>((uint32_t)v, (uint32_t)old);
-}
-template <int kCtrl, int kRows>
-__device__ __forceinline__ float dpp(float v, float old) {
-    return __uint_as_float(dpp<kCtrl, kRows>(__float_as_uint(v), __float_as_uint(old)));
-}
-__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) {
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
-}
-__device__ __forceinline__ u64 lane_of(u64 v, int lane) {
-    return (u64)lane_of((uint32_t)(v >> 32), lane) << 32 | lane_of((uint32_t)v, lane);
-}
-__device__ __forceinline__ float lane_of(float v, int lane) {
-    return __uint_as_float(lane_of(__float_as_uint(v), lane));
-}
-// op over this lane and those below it: shifts by 1, 2, 4 and 8 within the rows of 16, then a
-// row's last lane to the next row, and the second row's to the upper half.  `none` changes
-// nothing under op.
-template <typename V, typename Op>
-__device__ __forceinline__ V wave_scan(V v, V none, Op op) {
-    v = op(v, dpp<0x111, 0xF>(v, none));
-    v = op(v, dpp<0x112, 0xF>(v, none));
-    v = op(v, dpp<0x114, 0xF>(v, none));
-    v = op(v, dpp<0x118, 0xF>(v, none));
-    v = op(v, dpp<0x142, 0xA>(v, none));
-    return op(v, dpp<0x143, 0xC>(v, none));
-}
-template <typename V>
-__device__ __forceinline__ V wave_upto(V v) {
-    return wave_scan(v, (V)0, [](V a, V b) { return a + b; });
-}
-template <typename V>
-__device__ __forceinline__ V wave_sum(V v) {
-    return lane_of(wave_upto(v), kWave - 1);
-}
 __device__ __forceinline__ float wave_top(float v) {
     return lane_of(wave_scan(v, -kInf, [](float a, float b) { return fmaxf(a, b); }), kWave - 1);
 }
