@@ -124,7 +124,7 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
         });
 
     wtile::u4v kn[KU], qn[KU], on[OU];
-    float gn = 0.0f, bn = 0.0f;
+    uint32_t gn = 0, bn = 0;  // raw
     auto fetch = [&](int c) {
         const int tid = wtile::fresh(threadIdx.x);
         const Rows<T> rk(kp, (int64_t)c * C, a.L, qk_step, Dk);
@@ -142,9 +142,9 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
             on[i] = ro.template get16<VEC>(u / OR, u % OR * I::kUnit, width);
         }
         if (w == 0) {
-            const int64_t t = (int64_t)c * C + lane0;
-            gn = t < a.L ? to_f32(gp[t * a.HV]) : 0.0f;
-            bn = t < a.L ? to_f32(bp[t * a.HV]) : 0.0f;
+            const Rows<T> rg(gp, (int64_t)c * C, a.L, a.HV, 1), rb(bp, (int64_t)c * C, a.L, a.HV, 1);
+            gn = rg.raw(rg.off(lane0, 0, 1));
+            bn = rb.raw(rb.off(lane0, 0, 1));
         }
     };
     if (chunks > 0) fetch(chunks - 1);
@@ -167,7 +167,8 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
                 *(wtile::u4v*)(sm.d_o + u / OR * L::kOS + u % OR * I::kUnit) = on[i];
             }
         }
-        if (w == 0) gates_of_chunk(&sm.gt, gn, bn, a.scale, lane0);
+        if (w == 0)
+            gates_of_chunk(&sm.gt, Rows<T>::value(gn), Rows<T>::value(bn), a.scale, lane0);
         lds_barrier();
         {
             const int tid = wtile::fresh(threadIdx.x);
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(NT, 2) void delta_bwd_state_kernel(DeltaBwdArgs a, 
                 }
             }
         }
-        if (c > 0) fetch(c - 1);
+        fetch(c > 0 ? c - 1 : chunks);  // in any case, as in the forward
         const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
 
         f4 X[NTL];
@@ -347,6 +348,8 @@ struct GradLds {
 };
 
 __device__ __forceinline__ float whole(const float* m, int, int at) { return m[at]; }
+__device__ __forceinline__ uint32_t raw_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint32_t raw_of(bf16 v) { return v.bits; }
 __device__ __forceinline__ float whole(const __bf16* m, int plane, int at) {
     return (float)m[at] + (float)m[at + plane];
 }
@@ -391,7 +394,7 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
     // What a head's columns need of memory, on its way.
     wtile::u4v on[OU], kn[KU], qn[KU];
     f4 sn[SU], dn[SU], yn[YU];
-    float gn = 0.0f, bn = 0.0f, vn[NTL][4];
+    uint32_t gn = 0, bn = 0, vn[NTL][4];  // raw
     auto fetch = [&](const Item& it, int hv, int n0) {
         const int tid = wtile::fresh(threadIdx.x), lane = tid % kWave;
         const int64_t head = it.b * a.HV + hv;
@@ -442,13 +445,14 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
             for (int j = 0; j < NTL; ++j) {
                 const uint32_t o = rv.off(16 * w + 4 * g, 16 * j + ll, width);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) vn[j][r] = rv.get(rv.next(o, r));
+                for (int r = 0; r < 4; ++r) vn[j][r] = rv.raw(rv.next(o, r));
             }
         }
         if (wave == 4 && n0 == 0) {
-            const int64_t t = it.t0 + lane, o = (it.b * a.L + t) * a.HV + hv;
-            gn = t < a.L ? to_f32(((const T*)a.g)[o]) : 0.0f;
-            bn = t < a.L ? to_f32(((const T*)a.beta)[o]) : 0.0f;
+            const int64_t t = it.t0 + lane < a.L ? it.t0 + lane : a.L - 1;
+            const int64_t o = (it.b * a.L + t) * a.HV + hv;
+            gn = raw_of(((const T*)a.g)[o]);
+            bn = raw_of(((const T*)a.beta)[o]);
         }
     };
     auto fetch_qk = [&](const Item& it) {
@@ -489,7 +493,9 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
         for (int n0 = 0; n0 < Dv; n0 += NTW) {
             const int width = Dv - n0;
             lds_barrier();  // the previous columns' operands, or head's decays, have been read
-            if (wave == 4 && n0 == 0) gates_of_chunk(&sm.gt, gn, bn, a.scale, lane0);
+            if (wave == 4 && n0 == 0)
+                gates_of_chunk(&sm.gt, t0 + lane0 < a.L ? Rows<T>::value(gn) : 0.0f,
+                               t0 + lane0 < a.L ? Rows<T>::value(bn) : 0.0f, a.scale, lane0);
             const int tid = wtile::fresh(threadIdx.x);
             if (n0 == 0 && hv == h * group) {
 #pragma unroll
@@ -587,8 +593,9 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                     for (int r = 0; r < 4; ++r) {
                         const float y = whole(sm.y, L::kYPlane,
                                               (16 * w + 4 * g + r) * L::kNS + 16 * j + ll);
-                        yv[r] = fmaf(y, vn[j][r], yv[r]);
-                        R[r] = bt[r] * (vn[j][r] - eg[r] * KS[j][r]);
+                        const float v = Rows<T>::value(vn[j][r]);
+                        yv[r] = fmaf(y, v, yv[r]);
+                        R[r] = bt[r] * (v - eg[r] * KS[j][r]);
                     }
                     put<L::kOut>(sm.r, L::kRPlane, L::kUS, 16 * j + ll, 16 * w + 4 * g, R);
                 }

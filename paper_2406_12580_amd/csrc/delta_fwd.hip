@@ -112,7 +112,7 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
         });
 
     wtile::u4v kn[KU], qn[NK];
-    float vn[NTL][4], gn = 0.0f, bn = 0.0f;
+    uint32_t vn[NTL][4], gn = 0, bn = 0;  // raw
     auto fetch_k = [&](int c) {
         const int tid = wtile::fresh(threadIdx.x);
         const Rows<T> r(kp, (int64_t)c * C, a.L, qk_step, Dk);
@@ -122,9 +122,9 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
             kn[i] = r.template get16<VEC>(u / UR, u % UR * I::kUnit, Dk);
         }
         if (w == 0) {
-            const int64_t t = (int64_t)c * C + lane0;
-            gn = t < a.L ? to_f32(gp[t * a.HV]) : 0.0f;
-            bn = t < a.L ? to_f32(bp[t * a.HV]) : 0.0f;
+            const Rows<T> rg(gp, (int64_t)c * C, a.L, a.HV, 1), rb(bp, (int64_t)c * C, a.L, a.HV, 1);
+            gn = rg.raw(rg.off(lane0, 0, 1));
+            bn = rb.raw(rb.off(lane0, 0, 1));
         }
     };
     auto fetch_qv = [&](int c) {
@@ -138,7 +138,7 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
         for (int j = 0; j < NTL; ++j) {
             const uint32_t o = rv.off(16 * w + 4 * g, 16 * j + ll, width);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) vn[j][r] = rv.get(rv.next(o, r));
+            for (int r = 0; r < 4; ++r) vn[j][r] = rv.raw(rv.next(o, r));
         }
     };
     if (chunks > 0) {
@@ -158,9 +158,11 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
                 *(wtile::u4v*)(sm.k + u / UR * L::kKS + u % UR * I::kUnit) = kn[i];
             }
         }
-        if (w == 0) gates_of_chunk(&sm.gt, gn, bn, a.scale, lane0);
+        if (w == 0) gates_of_chunk(&sm.gt, Rows<T>::value(gn), Rows<T>::value(bn), a.scale, lane0);
         lds_barrier();  // K, the decays and the state's operand are in LDS
-        if (c + 1 < chunks) fetch_k(c + 1);
+        // Read ahead in any case (behind the last chunk out of range, so nothing): under a condition
+        // the compiler waits for more than it needs.
+        fetch_k(c + 1);
         const int lane = wtile::fresh(lane0), ll = lane & 15, g = lane >> 4;
 
         // Strips of k k^T and q k^T (lane: row i = 16 w + ll, columns 16 t + 4 g ..), of K S
@@ -229,11 +231,11 @@ __global__ __launch_bounds__(NT, 2) void delta_fwd_kernel(DeltaFwdArgs a, int st
 #pragma unroll
             for (int j = 0; j < NTL; ++j) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) KS[j][r] = bt[r] * (vn[j][r] - eg[r] * KS[j][r]);
+                for (int r = 0; r < 4; ++r) KS[j][r] = bt[r] * (Rows<T>::value(vn[j][r]) - eg[r] * KS[j][r]);
                 O[j] *= eg;
             }
         }
-        if (c + 1 < chunks) fetch_qv(c + 1);
+        fetch_qv(c + 1);
         wave_fence();
         invert_diagonal(sm.tm, w, ll, g);
         lds_barrier();  // the state has been read

@@ -235,14 +235,15 @@ template <typename T>
 struct Rows {
     __amdgpu_buffer_rsrc_t r;
     uint32_t step;  // bytes from row to row
-    // rows [t0, t0 + 64) of the `len` rows from base on, `width` elements wide
+    // rows [t0, t0 + 64) of the `len` rows from base on, `width` elements wide; none from t0 >= len
     __device__ __forceinline__ Rows(const T* base, int64_t t0, int64_t len, int64_t row_elems,
                                     int width) {
         const int64_t left = len - t0;
-        const int rows = left < C ? (int)left : C;
+        const int rows = left < C ? left < 0 ? 0 : (int)left : C;
         step = (uint32_t)(row_elems * sizeof(T));
         r = wtile::rsrc(base + t0 * row_elems,
-                        (uint32_t)((rows - 1) * row_elems + width) * (uint32_t)sizeof(T));
+                        rows > 0 ? (uint32_t)((rows - 1) * row_elems + width) * (uint32_t)sizeof(T)
+                                 : 0u);
     }
     __device__ __forceinline__ uint32_t off(int row, int e, int width) const {
         return e < width ? (uint32_t)row * step + (uint32_t)e * (uint32_t)sizeof(T) : kNowhere;
@@ -250,13 +251,18 @@ struct Rows {
     // Element e of row `row` and of those behind it, by adding r * step (an offset out of range
     // stays there: four rows of the largest tensors are below 2^24 bytes).
     __device__ __forceinline__ uint32_t next(uint32_t o, int r) const { return o + (uint32_t)r * step; }
-    __device__ __forceinline__ float get(uint32_t o) const {
+    // An element as it lies in memory, and its value.  What is read ahead stays raw until it is
+    // used: a conversion next to the load makes the wave wait for it there.
+    __device__ __forceinline__ uint32_t raw(uint32_t o) const {
         if constexpr (sizeof(T) == 4)
-            return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, (int)o, 0, 0));
+            return __builtin_amdgcn_raw_buffer_load_b32(r, (int)o, 0, 0);
         else
-            return __uint_as_float(
-                (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, (int)o, 0, 0) << 16);
+            return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, (int)o, 0, 0);
     }
+    __device__ __forceinline__ static float value(uint32_t raw) {
+        return __uint_as_float(sizeof(T) == 4 ? raw : raw << 16);
+    }
+    __device__ __forceinline__ float get(uint32_t o) const { return value(raw(o)); }
     __device__ __forceinline__ void set(uint32_t o, float v) const {
         if constexpr (sizeof(T) == 4)
             __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), r, (int)o, 0, 0);
