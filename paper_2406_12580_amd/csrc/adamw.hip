@@ -7,7 +7,9 @@
 // copies.  A workgroup takes kChunk consecutive elements of one tensor, found
 // by comparing its number with every tensor's first chunk (all scalar).  A wave
 // takes 256 elements at a time, four to a lane: with codes that is one block of
-// a scale, whose maximum stays within the wave.
+// a scale, whose maximum stays within the wave.  128 million bf16 parameters with 8-bit moments
+// (1.3 GB to move) take 290 us, 4.4 TB/s, where a large copy reaches 4.7; a model's 44 small
+// tensors 6 us of kernel behind 20 us of the call.
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"

@@ -14,6 +14,12 @@
 // and, since every factor e^{c_i - c_j} stands with q_i or k_i on one side and k_j on the other,
 //   dc_i = q_i.dQ_i + beta_i k_i.a_i - k_i.b_i,
 //   dc_63 += e^{c_63} <S, D> + sum_i e^{c_63 - c_i} k_i.(D U_i),    dg_t = sum_{i >= t} dc_i.
+//
+// Both are bound by issue and latency, not by memory.  2048 heads, 200 steps, 64 x 64 bf16: the
+// recurrence 306 us, the rest 537 us; 256 heads, 2048 steps fp32: 460 and 814 us.  Strips of the
+// recurrence are 32 columns (its operands leave no room for 64).  The rest is eight waves on one
+// chunk, four to a side (rows for dQ and a, columns for b), since one wave's half of the products
+// fills 240 registers; two such workgroups do not fit a CU's LDS.
 #include <hip/hip_runtime.h>
 
 #include "delta_tile.hpp"

@@ -11,6 +11,12 @@
 // are; K and the inverse of I + A go through LDS, and in one place there, one after the other,
 // the state, the right-hand side R, and U with the decays up to the chunk's end (so that K is
 // an operand of S' as it was given).
+//
+// What bounds it is the chain of a chunk, some 8 us of products, substitution and hand-overs
+// through LDS with seven barriers, of which two workgroups a CU hide a part: 2048 heads, 200
+// steps, 64 x 64 bf16 with kept states take 188 us (2.0 TB/s), 256 heads, 2048 steps fp32 395 us
+// (77 TFLOP/s, half of what fp32 matrix instructions reach).  Strips are 64 columns where the
+// state then fits the registers, as K, its products and the inverse are formed once a strip.
 #include <hip/hip_runtime.h>
 
 #include "delta_tile.hpp"

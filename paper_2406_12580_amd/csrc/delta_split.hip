@@ -13,6 +13,10 @@
 // W and K^T are written as the walk's operands (a lane's 16 bytes next to its neighbour's), X0
 // and Z as its accumulators, so that it reads them straight into registers, two chunks ahead.
 // The forward's outputs o = scale (diag(e^c) Q S + P U) follow for all chunks at once.
+//
+// 4 heads, 16384 steps, 128 x 128 bf16: preparation 40 and 65 us (backward), the two walks of
+// segments 71 + 76 and 84 + 89 us, joining them 23 us each way, outputs 55 us.  The walks are
+// bound by the latency of their two exchanges a chunk, the others by issue.
 #include <hip/hip_runtime.h>
 
 #include "delta_tile.hpp"
@@ -751,7 +755,8 @@ __global__ __launch_bounds__(NT) void delta_out_kernel(SplitArgs a, const float*
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
 // Segments of a walk of `chunks` by `strips` workgroups in all: as many as give every compute
-// unit one (two were slower: 103 and 108 us for 16 segments of 16384 steps, see below), and none shorter than 8 chunks (cutting costs each segment a second walk and Phi's columns).
+// unit one workgroup (the walk of 16384 steps of 4 heads: 103 us so, 108 us with two), and none
+// shorter than 8 chunks (cutting costs each segment a second walk and Phi's columns).
 int segments_of(int64_t chunks, int64_t strips) {
     const int64_t most = chunks / 8, want = 256 / strips;
     const int64_t n = most < want ? most : want;

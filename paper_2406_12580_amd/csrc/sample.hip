@@ -17,6 +17,11 @@
 // single read.  A longer one takes a workgroup for each span of kSpan items and six short
 // launches: extremes, histogram, the items of the bins that can hold a border, the border
 // itself (on those items alone), sums of the spans, and the choice within one span.
+//
+// What bounds a row is its chain of some twenty short phases with a barrier each, about 15 us, of
+// which four workgroups a CU hide a part: 2048 rows of 3416 take 36 us, 64 of 131072 in bf16
+// 75 us and 4 of 50000 43 us (memory alone: 6, 3.5 and 0.2 us).  Handing a row's last steps to
+// its last workgroup instead of launches of their own took 82 and 41 us for the latter two.
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"
