@@ -16,7 +16,7 @@
 //   dc_63 += e^{c_63} <S, D> + sum_i e^{c_63 - c_i} k_i.(D U_i),    dg_t = sum_{i >= t} dc_i.
 //
 // Both are bound by issue and latency, not by memory.  2048 heads, 200 steps, 64 x 64 bf16: the
-// recurrence 306 us, the rest 537 us; 256 heads, 2048 steps fp32: 460 and 814 us.  Strips of the
+// recurrence 306 us, the rest 481 us; 256 heads, 2048 steps fp32: 460 and 800 us.  Strips of the
 // recurrence are 32 columns (its operands leave no room for 64).  The rest is eight waves on one
 // chunk, four to a side (rows for dQ and a, columns for b), since one wave's half of the products
 // fills 240 registers; two such workgroups do not fit a CU's LDS.
@@ -360,7 +360,8 @@ __device__ __forceinline__ float whole(const __bf16* m, int plane, int at) {
     return (float)m[at] + (float)m[at + plane];
 }
 
-template <typename T, int DK, bool VEC>
+// GROUPED: several value heads to a query head, whose sums go through the workspace.
+template <typename T, int DK, bool VEC, bool GROUPED>
 __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdWs ws) {
     using I = Io<T>;
     using L = GradLds<T, DK>;
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
     const int wave = wave_id(), w = wave & 3;
     const bool side_b = wave < 4;
     const int chunks = (int)((a.L + C - 1) / C);
-    const int group = a.HV / a.H;
+    const int group = GROUPED ? a.HV / a.H : 1;
     const int Dk = a.Dk, Dv = a.Dv;
     const int64_t qk_step = (int64_t)a.H * Dk, v_step = (int64_t)a.HV * Dv;
     // A chunk of a query head.
@@ -710,7 +711,8 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
         lds_barrier();  // S and D have been read: b may take their place
         // The value heads of a query head come one after the other: their sum stands in the
         // workspace as float until the last one (written and read by the same lane).
-        const bool first = hv == h * group, last = hv + 1 == (h + 1) * group;
+        const bool first = !GROUPED || hv == h * group;
+        const bool last = !GROUPED || hv + 1 == (h + 1) * group;
         auto emit = [&](const f4& v, void* out, float* part, int i, int ll, int g) {
             const Rows<T> ro((T*)out + qk_base, t0, a.L, qk_step, Dk);
             const Rows<float> rp(part + qk_base, t0, a.L, qk_step, Dk);
@@ -835,7 +837,7 @@ hipError_t launch_state(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t stre
                        strips);
     return hipGetLastError();
 }
-template <typename T, int DK, bool VEC>
+template <typename T, int DK, bool VEC, bool GROUPED>
 hipError_t launch_grad(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t stream) {
     const int64_t chunks = (a.L + C - 1) / C;
     if (chunks == 0) return hipSuccess;
@@ -843,12 +845,12 @@ hipError_t launch_grad(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t strea
     constexpr int bytes = (int)sizeof(GradLds<T, DK>);
     static_assert(bytes <= 160 * 1024, "LDS of a compute unit");
     const hipError_t e =
-        allow_dynamic_lds((const void*)delta_bwd_grad_kernel<T, DK, VEC>, bytes, lds_set);
+        allow_dynamic_lds((const void*)delta_bwd_grad_kernel<T, DK, VEC, GROUPED>, bytes, lds_set);
     if (e != hipSuccess) return e;
     // As many workgroups as the chip holds; each takes chunks until there are no more, with the
     // next one's reads on their way.
     const int64_t items = a.B * a.H * chunks, fit = 256 * (160 * 1024 / bytes);
-    hipLaunchKernelGGL((delta_bwd_grad_kernel<T, DK, VEC>),
+    hipLaunchKernelGGL((delta_bwd_grad_kernel<T, DK, VEC, GROUPED>),
                        dim3((unsigned)(items < fit ? items : fit)), dim3(GT), bytes, stream, a,
                        ws);
     return hipGetLastError();
@@ -862,7 +864,11 @@ hipError_t launch_both(const DeltaBwdArgs& a, const BwdWs& ws, bool vec, hipStre
                          : vec ? launch_state<T, DK, 32, true>(a, ws, stream)
                                : launch_state<T, DK, 32, false>(a, ws, stream);
     if (e != hipSuccess) return e;
-    return vec ? launch_grad<T, DK, true>(a, ws, stream) : launch_grad<T, DK, false>(a, ws, stream);
+    const bool grouped = a.HV > a.H;
+    return vec ? grouped ? launch_grad<T, DK, true, true>(a, ws, stream)
+                         : launch_grad<T, DK, true, false>(a, ws, stream)
+           : grouped ? launch_grad<T, DK, false, true>(a, ws, stream)
+                     : launch_grad<T, DK, false, false>(a, ws, stream);
 }
 
 template <typename T>
