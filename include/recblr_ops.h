@@ -31,8 +31,9 @@ extern "C" {
  *   q, k : [B][L][H][Dk] io;  v, o : [B][L][HV][Dv] io;  g, beta : [B][L][HV] io
  *   h0, hT and every other state : [B][HV][Dk][Dv] float
  * 1 <= Dk, Dv <= 128, HV <= 4096, B HV ceil(Dv / 32) and B HV ceil(L / 64) below 2^24
- * (else UNSUPPORTED), HV a multiple of H (else INVALID_ARGUMENT).  g is the logarithm of the decay, usually <= 0; below -100
- * it counts as -100, so -inf clears the state.  A step with g = 0 and beta = 0
+ * (else UNSUPPORTED), HV a multiple of H (else INVALID_ARGUMENT).  g is the
+ * logarithm of the decay, usually <= 0; below -100 it counts as -100, so -inf
+ * clears the state.  A step with g = 0 and beta = 0
  * leaves the state as it is (padding); queries and keys are taken as given
  * (they are usually brought to length one by the caller).  Inputs are finite, in
  * padding too (g may be -inf): steps are worked on 64 at a time, and a NaN or an
