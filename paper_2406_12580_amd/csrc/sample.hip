@@ -145,7 +145,9 @@ struct Row {
         inv_t = greedy ? 0.0 : 1.0 / (double)temp;
         max = (double)top;
         const float range = fminf(46.0f * temp, top - lo);
-        bins = range > 0.0f ? (float)(kBins - 1) / fminf(range, 3e38f) : 0.0f;
+        // Finite at both ends of the range's sizes: else the top's step would be 0 times infinity.
+        // A range below 3.4e-36 is then the first bins' alone, and at the end one bin's.
+        bins = range > 0.0f ? fminf((float)(kBins - 1) / fminf(range, 3e38f), 3e38f) : 0.0f;
     }
     __device__ __forceinline__ double weight(float v) const {
         // What lies further down than 46 temperatures (-inf and what is no item, a NaN, among it)
@@ -959,7 +961,10 @@ __global__ __launch_bounds__(kNT) void sample_choose_kernel(SampleArgs a, SpanWs
         t += ties_of(i);
     }
     __syncthreads();
-    if (pick_span < 0) return;  // no weight anywhere (not reached: the largest weighs 1)
+    if (pick_span < 0) {  // no weight anywhere (not reached: the largest weighs 1)
+        if (tid == 0) none(a, r);
+        return;
+    }
     const int base = pick_span * kSpan;
     const Span<T> sp((const T*)a.logits + r * a.V, (int)a.V, base, w, lane);
     u64 q[kItems];

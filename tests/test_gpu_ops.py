@@ -621,6 +621,30 @@ def test_sample_extreme_parameters(rb, V):
                  top_p=[2.0, 1.0, 0.5] * 4, min_p=[-1.0, 0.0, 1.0, 5.0] * 3)
 
 
+@pytest.mark.parametrize("V", [100, 4096, 5000])
+def test_sample_tiny_steps(rb, V):
+    """Temperatures, and distances between logits, at the bottom of float's range: a row's whole
+    range of logits is then smaller than the inverse of the largest float."""
+    import torch
+    r = np.random.default_rng(V)
+    B = 12
+    u = r.random(B)
+    limits = (dict(top_p=[0.9] * B), dict(top_k=[1, 2, 3, 50] * 3), dict(min_p=[0.5] * B),
+              dict(top_p=[0.3, 0.6, 0.999] * 4, top_k=[0, 2, 7, V] * 3, min_p=[0.0, 0.9] * 6))
+    x = torch.from_numpy(r.normal(size=(B, V)))
+    temp = [torch.finfo(torch.float32).tiny, 1e-38, 1e-45, 6e-38, 7e-38, 1e-37] * 2
+    for kw in limits:
+        check_sample(rb, x.float().cuda(), u, temperature=temp, **kw)
+    # All weigh 1 to 64 bits: top-k goes by the logits, sums are whole numbers.
+    for by in (1e-37, 3e-38, 1e-40):
+        for kw in limits:
+            check_sample(rb, (by * x).float().cuda(), u, **kw)
+    z = torch.zeros((B, V), device="cuda")
+    z[:, 0] = 1e-37
+    got = check_sample(rb, z, [0.0, 0.49, 0.51, 0.99] * 3, top_k=[2] * B)
+    assert set(got) == {0, 1}
+
+
 def test_sample_empty_and_refusals(rb):
     import torch
     ids, prob = rb.sample(torch.empty((3, 0), device="cuda"), torch.rand(3, device="cuda"))
