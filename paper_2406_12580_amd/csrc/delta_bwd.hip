@@ -11,9 +11,13 @@
 //   a  = -diag(e^c) Y S^T - (Z . G)_{j < i} K
 //   b  = (scale F . G)^T_{i >= j} Q - (diag(beta) Z . G)^T_{i > j} K + diag(e^{c_63 - c}) U D^T
 //   dK = diag(beta) a + b,   dbeta_i = Y_i.V_i + k_i.a_i
-// and, since every factor e^{c_i - c_j} stands with q_i or k_i on one side and k_j on the other,
-//   dc_i = q_i.dQ_i + beta_i k_i.a_i - k_i.b_i,
-//   dc_63 += e^{c_63} <S, D> + sum_i e^{c_63 - c_i} k_i.(D U_i),    dg_t = sum_{i >= t} dc_i.
+// and dg_t is the sum of the terms that step t's decay is a factor of,
+//   W_ij = G_ij (scale F_ij q_i.k_j - beta_i Z_ij k_i.k_j),
+//   dg_t = e^{c_63} <S, D> + sum_{i >= t} e^{c_i} (scale q_i.S dO_i - beta_i k_i.S Y_i)
+//        + sum_{j < t} e^{c_63 - c_j} k_j.(D U_j) + sum_{i >= t > j} W_ij,
+// so that it is as exact, for its size, as they are.  (As a running sum of dL/dc_i = q_i.dQ_i +
+// beta_i k_i.a_i - k_i.b_i, which needs no W, it holds terms without that decay, of size one,
+// that are meant to cancel: at g = -12 a hundredth of dg was wrong in fp32.)
 //
 // Both are bound by issue and latency, not by memory.  2048 heads, 200 steps, 64 x 64 bf16: the
 // recurrence 306 us, the rest 481 us; 256 heads, 2048 steps fp32: 460 and 800 us.  Strips of the
@@ -351,6 +355,7 @@ struct GradLds {
     float tm[C * TS];
     Gates gt;
     float dca[C], dcb[C], db[C], part[8];
+    float pairs[4 * C];  // [wave][t]: sums of W over i of the wave's strip, i >= t > j
 };
 
 __device__ __forceinline__ float whole(const float* m, int, int at) { return m[at]; }
@@ -702,6 +707,40 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                     }
                 }
         }
+        // W's sums over j < t for each t of a row i, then over the rows i >= t of the strip.
+        if (!side_b) {
+            const int own = 16 * w + ll;
+            const float bi = sm.gt.bt[own];
+            float before = 0.0f;  // of the tiles so far
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (t <= w) {
+                    f4 QK = {0, 0, 0, 0}, KK = QK, upto;
+#pragma unroll
+                    for (int s = 0; s < NK; ++s) {
+                        const auto kt = given(sm.k, L::kKS, 16 * t + ll, s * I::kStep, g);
+                        QK = mma(QK, kt, given(sm.q, L::kKS, 16 * w + ll, s * I::kStep, g));
+                        KK = mma(KK, kt, given(sm.k, L::kKS, 16 * w + ll, s * I::kStep, g));
+                    }
+                    float sum = 0.0f;  // of the lane's four columns
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        upto[r] = sum;
+                        if (16 * t + 4 * g + r < own)
+                            sum += fmaf(F[t][r], QK[r], bi * Z[t][r] * KK[r]);
+                    }
+                    // The row's four lanes lie 16 apart.
+                    const float x16 = __shfl_xor(sum, 16), two = sum + x16;
+                    const float x32 = __shfl_xor(two, 32);
+                    const float base = before + ((g & 1 ? x16 : 0.0f) + (g & 2 ? x32 : 0.0f));
+                    before += two + x32;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        upto[r] = lanes::row_sum(16 * t + 4 * g + r <= own ? base + upto[r] : 0.0f);
+                    if (ll == 0) *(f4*)(sm.pairs + w * C + 16 * t + 4 * g) = upto;
+                    step_end(upto);
+                }
+        }
         typename I::template Made<L::kOut> fo[NC], zo[NC];
 #pragma unroll
         for (int s = 0; s < NC; ++s) {
@@ -745,8 +784,7 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const float kv = (float)sm.k[(16 * w + 4 * g + r) * L::kKS + 16 * i + ll];
-                    x1[r] = fmaf(kv, kb[r], x1[r]);
-                    x2[r] = fmaf(kv, ud[r], x2[r]);
+                    x1[r] = fmaf(kv, ud[r], x1[r]);
                     sm.dk[(16 * w + 4 * g + r) * (DK + 4) + 16 * i + ll] = kb[r];
                 }
                 step_end(kb);
@@ -756,7 +794,14 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
             const f4 bt = *(const f4*)(sm.gt.bt + 16 * w + 4 * g);
 #pragma unroll
             for (int i = 0; i < DTL; ++i) {
-                f4 q = a.scale * eg * X1[i], ka = -eg * X2[i];
+                f4 q = a.scale * eg * X1[i], ka = -eg * X2[i], kv;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int at = (16 * w + 4 * g + r) * L::kKS + 16 * i + ll;
+                    kv[r] = (float)sm.k[at];
+                    x1[r] = fmaf((float)sm.q[at], q[r], fmaf(bt[r] * kv[r], ka[r], x1[r]));
+                }
+                step_end(x1);
 #pragma unroll
                 for (int s = 0; s < NC; ++s) {
                     const auto kt = given_t_acc(sm.k, L::kKS, s * I::kStep, 16 * i, ll, g);
@@ -764,19 +809,13 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
                     ka = mma(ka, zo[s], kt);
                 }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int at = (16 * w + 4 * g + r) * L::kKS + 16 * i + ll;
-                    x1[r] = fmaf((float)sm.q[at], q[r], x1[r]);
-                    x2[r] = fmaf((float)sm.k[at], ka[r], x2[r]);
-                }
+                for (int r = 0; r < 4; ++r) x2[r] = fmaf(kv[r], ka[r], x2[r]);
                 emit(q, a.dq, ws.dq, i, ll, g);
                 KA[i] = bt * ka;
                 step_end(KA[i]);
             }
         }
-        // The rows' sums; <S, D> and the decays behind the steps go to the chunk's last one.
-        float end = side_b ? x2[0] + x2[1] + x2[2] + x2[3] : 0.0f;
-        end = fmaf(sm.gt.eg[C - 1], sd, end);
+        // The rows' sums: side b's of k.(D U), side a's of the state's terms and of k.a.
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int i = 16 * w + 4 * g + r;
@@ -786,28 +825,28 @@ __global__ __launch_bounds__(GT) void delta_bwd_grad_kernel(DeltaBwdArgs a, BwdW
             } else {
                 const float s2 = lanes::row_sum(x2[r]), sy = lanes::row_sum(yv[r]);
                 if (ll == 0) {
-                    sm.dca[i] = fmaf(sm.gt.bt[i], s2, s1);
+                    sm.dca[i] = s1;
                     sm.db[i] = sy + s2;
                 }
             }
         }
-        end = lanes::wave_sum(end);
-        if (lane == 0) sm.part[wave] = end;
+        sd = lanes::wave_sum(sm.gt.eg[C - 1] * sd);
+        if (lane == 0) sm.part[wave] = sd;
         lds_barrier();
         if (wave == 0) {
-            // The last step first: sums over the steps from each one on are a scan.
-            const int i = C - 1 - lane;
-            float s = sm.dca[i] - sm.dcb[i];
-            if (lane == 0) {
+            // A step to a lane: the sums from it on (the last step first, they are a scan) and the
+            // sums before it.
+            const float from = __shfl(lanes::wave_upto(sm.dca[C - 1 - lane]), C - 1 - lane);
+            float s = from + lanes::wave_upto(lane ? sm.dcb[lane - 1] : 0.0f);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) s += sm.part[j];
-            }
-            s = lanes::wave_upto(s);
-            const int64_t t = t0 + i;
+            for (int j = 0; j < 8; ++j) s += sm.part[j];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s += lane < 16 * (j + 1) ? sm.pairs[j * C + lane] : 0.0f;
+            const int64_t t = t0 + lane;
             if (t < a.L) {
                 const int64_t at = (b * a.L + t) * a.HV + hv;
                 store((T*)a.dg + at, s);
-                store((T*)a.dbeta + at, sm.db[i]);
+                store((T*)a.dbeta + at, sm.db[lane]);
             }
         }
         if (!side_b) {

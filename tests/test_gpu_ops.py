@@ -174,6 +174,43 @@ def test_delta_strong_decay(rb, io, L):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 130, 1, 2, 64, 64), (1, 1700, 1, 1, 128, 40),
+                                  (2, 70, 1, 2, 17, 33), (3, 64, 2, 2, 100, 96)])
+@pytest.mark.parametrize("decay", [1.0, 3.0, 8.0, 12.0])
+def test_delta_uniformly_strong_decay(rb, io, size, decay):
+    """Heads that forget quickly at every step: dg is as small as the decay itself, so nothing of
+    size one may be added to it and taken away again.  (dh0 is below the least float.)"""
+    print(io, size, decay, flush=True)
+    c = delta_case(io, *size, seed=11)
+    g = -decay * (1 + 0.1 * np.random.default_rng(12).random(c["g_"].shape))
+    c["g"], c["g_"] = put(g, io)
+    out = run_delta(rb, c)
+    want = ref.delta(*(c[n + "_"] for n in ("q", "k", "v", "g", "beta")), h0=c["h0_"],
+                     do=c["do_"], dhT=c["dhT_"])
+    bars = delta_bars(io, size[4])
+    for name in ("o", "hT", "dq", "dk", "dv", "dg", "dbeta"):
+        kind = "state" if name == "hT" else "dg" if name == "dg" else "out"
+        close(name, out[name], want[name], bars[kind])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2, 130, 1, 2, 64, 64), (1, 1700, 1, 1, 128, 40),
+                                  (2, 70, 2, 2, 17, 33)])
+def test_delta_gradients_of_single_strong_decays(rb, io, size):
+    """dg of strong decays among weak ones, by its own size: every term of a step's dg has that
+    step's decay as a factor, so its error does too, whatever its neighbours' size."""
+    print(io, size, flush=True)
+    c = delta_case(io, *size, seed=13, decay=0.02)
+    strong = np.arange(size[1]) % 7 == 3
+    c["g"], c["g_"] = put(np.where(strong[None, :, None], -12.0, c["g_"]), io)
+    out = run_delta(rb, c)
+    want = ref.delta(*(c[n + "_"] for n in ("q", "k", "v", "g", "beta")), h0=c["h0_"],
+                     do=c["do_"], dhT=c["dhT_"])
+    close("dg", out["dg"][:, strong], want["dg"][:, strong], delta_bars(io, size[4])["dg"])
+    close("dg", out["dg"], want["dg"], delta_bars(io, size[4])["dg"])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_delta_alike_keys(rb, io):
     """Keys that are nearly the same make the chunk's triangular system as far from the unit
     matrix as it gets (entries near beta); strengths up to two."""
