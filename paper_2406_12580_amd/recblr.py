@@ -662,8 +662,10 @@ class AdamW:
     s2).  `state` takes over moments that exist: (m1, m2) or (m1, m2, s1, s2), lists of tensors
     with as many elements as the parameters (the scales ceil(n / 256)); `step` counts the
     updates already made.  step(grads) updates parameters and moments in place, on the
-    parameters' device; gradients have the parameters' type and number of elements.  A captured
-    step replays with the bias corrections, rates and addresses of its capture."""
+    parameters' device; gradients have the parameters' type and number of elements.  The lists
+    and their tensors may be given other memory of the same type and size between two calls
+    (opt.m1[i] = t, p.data = t).  A captured step replays with the bias corrections, rates and
+    addresses of its capture."""
 
     def __init__(self, params, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
                  state_bits=32, state=None, step=0):
@@ -697,23 +699,16 @@ class AdamW:
         self.m1, self.m2 = state[:2]
         self.s1, self.s2 = state[2:] if codes else (None, None)
         self._table = (AdamWTensor * len(sizes))()
-
-        def fill(field, tensors, dtype, counts, name):
-            if len(tensors) != len(sizes):
-                raise ValueError(f"{name}: one tensor for each parameter is needed")
-            for entry, t, n in zip(self._table, tensors, counts):
-                setattr(entry, field, self._flat(t, dtype, n, name))
-
-        fill("param", self.params, self.dtype, sizes, "params")
-        fill("m1", self.m1, types[0], sizes, "m1")
-        fill("m2", self.m2, types[1], sizes, "m2")
+        self._sizes = sizes
+        # The table's fields with the attributes that hold their tensors.
+        self._fields = [("param", "params", self.dtype, sizes), ("m1", "m1", types[0], sizes),
+                        ("m2", "m2", types[1], sizes)]
         if codes:
-            fill("scale1", self.s1, torch.float32, blocks, "s1")
-            fill("scale2", self.s2, torch.float32, blocks, "s2")
+            self._fields += [("scale1", "s1", torch.float32, blocks),
+                             ("scale2", "s2", torch.float32, blocks)]
+        self._fill()
         for entry, n, w in zip(self._table, sizes, decay):
             entry.n, entry.weight_decay = n, w
-        self._sizes = sizes
-        self._at = [p.data_ptr() for p in self.params]
         # The table's gradient addresses, as one array to assign.
         self._grads = np.frombuffer(self._table, dtype=np.uint64).reshape(len(sizes), -1)[
             :, AdamWTensor.grad.offset // 8]
@@ -725,6 +720,29 @@ class AdamW:
             raise ValueError(f"{name}: tensors must be contiguous, on the parameters' GPU")
         return t.data_ptr()
 
+    def _addresses(self):
+        return [list(map(_data_ptr, getattr(self, name))) for _, name, _, _ in self._fields]
+
+    def _fill(self):
+        held = []
+        for field, name, dtype, counts in self._fields:
+            tensors = getattr(self, name)
+            if len(tensors) != len(self._sizes):
+                raise ValueError(f"{name}: one tensor for each parameter is needed")
+            for entry, t, n in zip(self._table, tensors, counts):
+                setattr(entry, field, self._flat(t, dtype, n, name))
+            if field != "param":  # whose memory is their owner's to free
+                held += [t.detach() for t in tensors]
+        # Moments' memory stays theirs for as long as the table names it, whatever becomes of the
+        # tensors: an address that is the same as before is then the same memory.
+        self._held = held
+        self._at = self._addresses()
+
+    def _follow(self):
+        """Brings the table in line with memory that was replaced since the last call."""
+        if self._addresses() != self._at:
+            self._fill()
+
     def step(self, grads, lr=None, stream=None):
         """One update with grads, a tensor for each parameter; lr overrides the rate."""
         if len(grads) != len(self._sizes):
@@ -735,11 +753,7 @@ class AdamW:
             for t, n in zip(grads, self._sizes):
                 self._flat(t, self.dtype, n, "grads")  # says what is wrong
         self._grads[:] = list(map(_data_ptr, grads))
-        at = list(map(_data_ptr, self.params))
-        if at != self._at:  # a parameter's memory was replaced (p.data = ...)
-            for entry, p, n in zip(self._table, self.params, self._sizes):
-                entry.param = self._flat(p, self.dtype, n, "params")
-            self._at = at
+        self._follow()
         _adamw_step(self, self.lr if lr is None else lr, stream=stream)
         self.steps += 1
 
@@ -753,6 +767,7 @@ class AdamW:
                 for a, b in zip(ours, theirs):
                     b.copy_(a.reshape(b.shape))
             return out
+        self._follow()
         return _adamw_moments(self, out, stream=stream)
 
 

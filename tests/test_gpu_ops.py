@@ -540,6 +540,44 @@ def test_adamw_follows_replaced_memory(rb):
         a.step([g])
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_follows_replaced_moments(rb, bits):
+    """Moments and scales that are other tensors, or tensors with other memory, than at first."""
+    import torch
+    params, grads = adamw_case("f32", [700, 300, 0])
+    other = [p.clone() for p in params]
+    a, b = (rb.AdamW(p, state_bits=bits, **HYPER) for p in (params, other))
+    names = ("m1", "m2") if bits == 32 else ("m1", "m2", "s1", "s2")
+    for t in range(4):
+        old = [[x for x in getattr(a, n)] for n in names]
+        kept = [[x.clone() for x in ts] for ts in old]
+        if t == 1:      # another tensor in the list
+            for n in names:
+                getattr(a, n)[0] = getattr(a, n)[0].clone()
+        elif t == 2:    # the same tensor with other memory
+            old = [[x.data for x in ts] for ts in old]
+            for n in names:
+                getattr(a, n)[0].data = getattr(a, n)[0].clone()
+        elif t == 3:    # another list
+            for n in names:
+                setattr(a, n, tuple(x.clone() for x in getattr(a, n)))
+        g = grads()
+        a.step(g)
+        b.step(g)
+        assert all(torch.equal(x, y) for x, y in zip(params, other)), t
+        assert all(torch.equal(x, y) for n in names for x, y in zip(getattr(a, n), getattr(b, n)))
+        if t:           # what was taken out is as it was
+            assert all(torch.equal(x[0], y[0]) for x, y in zip(old, kept)), t
+    assert all(torch.equal(x, y) for m, n in zip(a.moments(), b.moments()) for x, y in zip(m, n))
+    a.m1 = a.m1[:2]
+    with pytest.raises(ValueError):
+        a.step(g)
+    a.m1 = [torch.zeros(5, device="cuda")] * 3
+    with pytest.raises(ValueError):
+        a.step(g)
+    assert a.steps == 4
+
+
 def test_adamw_binding_refuses(rb):
     import torch
     p = torch.zeros(8, device="cuda")
