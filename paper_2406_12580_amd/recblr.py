@@ -651,7 +651,7 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
 # and a step over a model's few dozen tensors is bound by them.
 _numel, _data_ptr = torch.Tensor.numel, torch.Tensor.data_ptr
 _get_device, _is_contiguous = torch.Tensor.get_device, torch.Tensor.is_contiguous
-_dtype = torch.Tensor.dtype.__get__
+_dtype, _nbytes = torch.Tensor.dtype.__get__, torch.Tensor.nbytes.__get__
 
 
 class AdamW:
@@ -706,6 +706,7 @@ class AdamW:
         if codes:
             self._fields += [("scale1", "s1", torch.float32, blocks),
                              ("scale2", "s2", torch.float32, blocks)]
+        self._param_bytes = list(map(_nbytes, self.params))
         self._fill()
         for entry, n, w in zip(self._table, sizes, decay):
             entry.n, entry.weight_decay = n, w
@@ -731,16 +732,18 @@ class AdamW:
                 raise ValueError(f"{name}: one tensor for each parameter is needed")
             for entry, t, n in zip(self._table, tensors, counts):
                 setattr(entry, field, self._flat(t, dtype, n, name))
-            if field != "param":  # whose memory is their owner's to free
+            if field != "param":
                 held += [t.detach() for t in tensors]
         # Moments' memory stays theirs for as long as the table names it, whatever becomes of the
-        # tensors: an address that is the same as before is then the same memory.
+        # tensors: an address that is the same as before is then the same memory.  Parameters'
+        # memory is their owner's to free.
         self._held = held
         self._at = self._addresses()
 
     def _follow(self):
         """Brings the table in line with memory that was replaced since the last call."""
-        if self._addresses() != self._at:
+        if not (self._addresses() == self._at and all(map(_is_contiguous, self.params))
+                and list(map(_nbytes, self.params)) == self._param_bytes):
             self._fill()
 
     def step(self, grads, lr=None, stream=None):

@@ -578,6 +578,22 @@ def test_adamw_follows_replaced_moments(rb, bits):
     assert a.steps == 4
 
 
+def test_adamw_refuses_parameters_cut_in_place(rb):
+    """Parameters that are fewer elements, or in another order, at the same address as before."""
+    import torch
+    p = torch.ones(16, 16, device="cuda")
+    opt, g = rb.AdamW([p], **HYPER), torch.ones(16, 16, device="cuda")
+    opt.step([g])
+    whole = p.data
+    for part in (whole[:8], whole.t(), whole.view(torch.bfloat16)[:, :16]):
+        p.data = part
+        with pytest.raises(ValueError):
+            opt.step([g])
+    p.data = whole
+    opt.step([g])
+    assert opt.steps == 2
+
+
 def test_adamw_binding_refuses(rb):
     import torch
     p = torch.zeros(8, device="cuda")
