@@ -725,20 +725,21 @@ class AdamW:
         return [list(map(_data_ptr, getattr(self, name))) for _, name, _, _ in self._fields]
 
     def _fill(self):
-        held = []
+        held, found = [], []
         for field, name, dtype, counts in self._fields:
             tensors = getattr(self, name)
             if len(tensors) != len(self._sizes):
                 raise ValueError(f"{name}: one tensor for each parameter is needed")
-            for entry, t, n in zip(self._table, tensors, counts):
-                setattr(entry, field, self._flat(t, dtype, n, name))
+            found.append([self._flat(t, dtype, n, name) for t, n in zip(tensors, counts)])
             if field != "param":
                 held += [t.detach() for t in tensors]
+        for (field, *_), addresses in zip(self._fields, found):  # all are right: none is kept else
+            for entry, address in zip(self._table, addresses):
+                setattr(entry, field, address)
         # Moments' memory stays theirs for as long as the table names it, whatever becomes of the
         # tensors: an address that is the same as before is then the same memory.  Parameters'
         # memory is their owner's to free.
-        self._held = held
-        self._at = self._addresses()
+        self._held, self._at = held, found
 
     def _follow(self):
         """Brings the table in line with memory that was replaced since the last call."""

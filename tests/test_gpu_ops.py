@@ -578,6 +578,23 @@ def test_adamw_follows_replaced_moments(rb, bits):
     assert a.steps == 4
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_refused_memory_leaves_no_trace(rb, bits):
+    """A call that is refused for one list's memory has not taken over another's."""
+    import torch
+    p, q = torch.ones(300, device="cuda"), torch.ones(300, device="cuda")
+    a, b = rb.AdamW([p], state_bits=bits, **HYPER), rb.AdamW([q], state_bits=bits, **HYPER)
+    g, data, m1 = torch.ones(300, device="cuda"), p.data, a.m1[0]
+    p.data = away = torch.zeros(300, device="cuda")
+    a.m1[0] = torch.zeros(7, device="cuda")
+    with pytest.raises(ValueError):
+        a.step([g])
+    p.data, a.m1[0] = data, m1
+    a.step([g])
+    b.step([g])
+    assert torch.equal(p, q) and away.eq(0).all()
+
+
 def test_adamw_refuses_parameters_cut_in_place(rb):
     """Parameters that are fewer elements, or in another order, at the same address as before."""
     import torch
