@@ -762,15 +762,11 @@ class AdamW:
         self.steps += 1
 
     def moments(self, out=None, stream=None):
-        """The moments as float32: (m1, m2), lists of tensors; out takes them where given
-        (without it, 32-bit moments are the optimiser's own tensors, no copies)."""
-        if self.state_bits == 32:
-            if out is None:
-                return list(self.m1), list(self.m2)
-            for ours, theirs in zip((self.m1, self.m2), out):
-                for a, b in zip(ours, theirs):
-                    b.copy_(a.reshape(b.shape))
-            return out
+        """The moments as float32: (m1, m2), lists of tensors; out, two lists of float32 tensors
+        with the parameters' numbers of elements, takes them where given (without it, 32-bit
+        moments are the optimiser's own tensors, no copies)."""
+        if self.state_bits == 32 and out is None:
+            return list(self.m1), list(self.m2)
         self._follow()
         return _adamw_moments(self, out, stream=stream)
 
@@ -787,12 +783,19 @@ def _adamw_moments(opt, out):
     if out is None:
         out = tuple([torch.empty(p.shape, dtype=torch.float32, device=opt.device)
                      for p in opt.params] for _ in range(2))
+    if len(out) != 2:
+        raise ValueError("out must be two lists of tensors")
     ptrs = []
     for tensors in out:
         if len(tensors) != len(opt._sizes):
             raise ValueError("out: one tensor for each parameter is needed")
         ptrs.append((_p * len(tensors))(*(opt._flat(t, torch.float32, n, "out")
                                           for t, n in zip(tensors, opt._sizes))))
+    if opt.state_bits == 32:
+        for ours, theirs in zip((opt.m1, opt.m2), out):
+            for a, b in zip(ours, theirs):
+                b.view(-1).copy_(a.view(-1))
+        return out
     _check(recblr_adamw_moments(opt._table, len(opt._sizes), *ptrs, _stream()),
            "recblr_adamw_moments")
     return out

@@ -595,6 +595,39 @@ def test_adamw_refused_memory_leaves_no_trace(rb, bits):
     assert torch.equal(p, q) and away.eq(0).all()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_moments_on_a_stream(rb, bits):
+    """The moments are read on the stream that they are asked for on, behind a step there."""
+    import torch
+    params, grads = adamw_case("f32", [5000, 33])
+    opt, g = rb.AdamW(params, state_bits=bits, **HYPER), grads()
+    out = tuple([torch.full_like(p, 7.0) for p in params] for _ in range(2))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(100_000_000)      # some 50 ms
+    opt.step(g, stream=s)
+    assert opt.moments(out, stream=s) is out
+    s.synchronize()
+    for ours, theirs in zip(opt.moments(), out):
+        assert all(torch.equal(x, y) and y.ne(0).any() for x, y in zip(ours, theirs))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_moments_refuses_outputs(rb, bits):
+    import torch
+    p = [torch.zeros(8, device="cuda"), torch.zeros(3, device="cuda")]
+    opt = rb.AdamW(p, state_bits=bits)
+    new = lambda: [torch.empty_like(t) for t in p]  # noqa: E731
+    assert [len(x) for x in opt.moments((new(), new()))] == [2, 2]
+    for bad in ((new(), new()[:1]), (new()[:1], new()), (new(),), (new(), new(), new()),
+                (new(), [t.bfloat16() for t in p]), (new(), [t.cpu() for t in p]),
+                ([torch.empty(16, device="cuda")[::2], p[1]], new()),
+                ([torch.empty(9, device="cuda"), p[1]], new())):
+        with pytest.raises(ValueError):
+            opt.moments(bad)
+
+
 def test_adamw_refuses_parameters_cut_in_place(rb):
     """Parameters that are fewer elements, or in another order, at the same address as before."""
     import torch
