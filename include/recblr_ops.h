@@ -142,7 +142,8 @@ int recblr_adamw_moments(const recblr_adamw_tensor* tensors, int64_t count,
  *   min_p: of these, those with w_i >= min_p (1 is the largest w).
  * ids is the least i whose running sum of the w that stay, in order of i,
  * exceeds u times their sum (the last item with w > 0 for u >= 1), and prob is
- * w_ids over that sum.  temperature <= 0 takes the first item, prob 1.
+ * w_ids over that sum.  temperature <= 0 takes the first item, prob 1.  A top_p or
+ * min_p that is NaN sets no limit, and a NaN u counts as 1.
  * Masked items have the logit -inf, or any value far below the rest (the
  * type's lowest, say).  A row with no item (V = 0, all -inf) or none to be
  * chosen by its values (a NaN or +inf among logits, a NaN temperature) gives

@@ -138,7 +138,7 @@ struct Row {
         const float temp = ask.temp;
         bad = !(hi > -kInf && hi < kInf) || !(temp == temp);
         top_p = ask.top_p;
-        min_p = fminf(ask.min_p, 1.0f);
+        min_p = ask.min_p > 1.0f ? 1.0f : ask.min_p;  // a NaN stays one, and sets no limit
         greedy = temp <= 0.0f;
         k = ask.top_k > 0 ? ask.top_k : V;
         if (greedy || top_p <= 0.0f) k = 1;

@@ -786,6 +786,23 @@ def test_sample_tiny_steps(rb, V):
     assert set(got) == {0, 1}
 
 
+@pytest.mark.parametrize("V", [100, 5000])
+def test_sample_nan_limits(rb, V):
+    """A limit that is NaN is none; a NaN u counts as 1."""
+    import torch
+    x, u = torch.randn(8, V, device="cuda"), torch.linspace(0.05, 0.95, 8, device="cuda")
+    nan, p = torch.full_like(u, math.nan), torch.full_like(u, 0.8)
+    k = torch.full((8,), V // 2, dtype=torch.int32, device="cuda")
+
+    def same(a, b):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    same(rb.sample(x, u, min_p=nan), rb.sample(x, u))
+    same(rb.sample(x, u, top_p=nan), rb.sample(x, u))
+    same(rb.sample(x, u, top_k=k, top_p=p, min_p=nan), rb.sample(x, u, top_k=k, top_p=p))
+    same(rb.sample(x, u, top_k=k, top_p=nan, min_p=p / 9), rb.sample(x, u, top_k=k, min_p=p / 9))
+    same(rb.sample(x, nan, top_p=p), rb.sample(x, torch.ones_like(u), top_p=p))
+
+
 def test_sample_empty_and_refusals(rb):
     import torch
     ids, prob = rb.sample(torch.empty((3, 0), device="cuda"), torch.rand(3, device="cuda"))
