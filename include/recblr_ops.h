@@ -124,7 +124,8 @@ int recblr_adamw_update(const recblr_adamw_tensor* tensors, int64_t count, int s
                         void* stream);
 
 /* The values that 8-bit moments stand for: m1_out[i], m2_out[i] (float [n], either
- * list may be NULL) from tensors[i].m1, m2 and scales; param and grad are not read. */
+ * list may be NULL) from tensors[i].m1, m2 and scales; param and grad are not read.
+ * Errors as above: an output may overlap no other output and no moment or scale of the call. */
 int recblr_adamw_moments(const recblr_adamw_tensor* tensors, int64_t count,
                          float* const* m1_out, float* const* m2_out, void* stream);
 

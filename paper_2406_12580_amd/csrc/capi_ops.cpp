@@ -36,6 +36,24 @@ bool ranges_disjoint(Range* r, int64_t n) {
     return true;
 }
 
+// The ranges of a call over `count` tensors, up to six each.
+struct Ranges {
+    static constexpr int64_t kSmall = 64;
+    Range small[6 * kSmall];
+    Range* r;
+    int64_t used = 0;
+    explicit Ranges(int64_t count)
+        : r(count > kSmall ? new (std::nothrow) Range[6 * count] : small) {}
+    Ranges(const Ranges&) = delete;
+    ~Ranges() {
+        if (r != small) delete[] r;
+    }
+    void add(const void* p, size_t bytes, bool written) {
+        if (p) r[used++] = Range{(uintptr_t)p, (uintptr_t)p + bytes, written};
+    }
+    bool disjoint() { return ranges_disjoint(r, used); }
+};
+
 // A launch has fewer than 2^32 threads: below this many workgroups of 256.
 constexpr int64_t kMaxGroups = (int64_t)1 << 24;
 constexpr int64_t kMaxAdamN = ((int64_t)1 << 36) - 4096;  // 4096 elements to a workgroup
@@ -59,33 +77,22 @@ int recblr_adamw_update(const recblr_adamw_tensor* tensors, int64_t count, int s
     if (count == 0) return RECBLR_OK;
     const bool bits8 = state_bits == 8;
     const size_t pe = esz(io), me = bits8 ? 1 : 4;
-    constexpr int64_t kSmall = 64;
-    Range small[6 * kSmall];
-    Range* r = small;
-    if (count > kSmall) r = new (std::nothrow) Range[6 * count];
-    if (!r) return RECBLR_ERR_INVALID_ARGUMENT;
-    int st = RECBLR_OK;
-    int64_t used = 0;
-    for (int kind = 0; kind < (bits8 ? 6 : 4) && st == RECBLR_OK; ++kind)
+    Ranges ranges(count);
+    if (!ranges.r) return RECBLR_ERR_INVALID_ARGUMENT;
+    for (int kind = 0; kind < (bits8 ? 6 : 4); ++kind)
         for (int64_t i = 0; i < count; ++i) {
             const recblr_adamw_tensor& t = tensors[i];
-            if (t.n < 0) st = RECBLR_ERR_INVALID_ARGUMENT;
-            else if (t.n > kMaxAdamN) st = RECBLR_ERR_UNSUPPORTED;
-            if (st != RECBLR_OK) break;
+            if (t.n < 0) return RECBLR_ERR_INVALID_ARGUMENT;
+            if (t.n > kMaxAdamN) return RECBLR_ERR_UNSUPPORTED;
             if (t.n == 0) continue;
             const void* p = kind == 0 ? t.param : kind == 1 ? t.grad : kind == 2 ? t.m1
                             : kind == 3 ? t.m2 : kind == 4 ? t.scale1 : (const void*)t.scale2;
             const size_t e = kind < 2 ? pe : kind < 4 ? me : 4;
-            if (!p || !aligned(p, e)) {
-                st = RECBLR_ERR_INVALID_ARGUMENT;
-                break;
-            }
+            if (!p || !aligned(p, e)) return RECBLR_ERR_INVALID_ARGUMENT;
             const size_t bytes = kind < 4 ? (size_t)t.n * e : (size_t)adam_blocks(t.n) * 4;
-            r[used++] = Range{(uintptr_t)p, (uintptr_t)p + bytes, kind != 1};
+            ranges.add(p, bytes, kind != 1);
         }
-    if (st == RECBLR_OK && !ranges_disjoint(r, used)) st = RECBLR_ERR_INVALID_ARGUMENT;
-    if (r != small) delete[] r;
-    if (st != RECBLR_OK) return st;
+    if (!ranges.disjoint()) return RECBLR_ERR_INVALID_ARGUMENT;
     const AdamWHyper h{lr, beta1, beta2, eps, 1.0 / (1.0 - pow(beta1, (double)step)),
                        1.0 / (1.0 - pow(beta2, (double)step))};
     return status_of(launch_adamw(tensors, count, bits8, io_of(io), h, (hipStream_t)stream));
@@ -96,6 +103,8 @@ int recblr_adamw_moments(const recblr_adamw_tensor* tensors, int64_t count,
     if (count < 0 || (count > 0 && !tensors)) return RECBLR_ERR_INVALID_ARGUMENT;
     if (count > kMaxTensorCount) return RECBLR_ERR_UNSUPPORTED;
     if (count == 0 || (!m1_out && !m2_out)) return RECBLR_OK;
+    Ranges ranges(count);
+    if (!ranges.r) return RECBLR_ERR_INVALID_ARGUMENT;
     for (int64_t i = 0; i < count; ++i) {
         const recblr_adamw_tensor& t = tensors[i];
         if (t.n < 0) return RECBLR_ERR_INVALID_ARGUMENT;
@@ -108,10 +117,14 @@ int recblr_adamw_moments(const recblr_adamw_tensor* tensors, int64_t count,
         for (const void* p : {(const void*)a, (const void*)b, (const void*)t.scale1,
                               (const void*)t.scale2})
             if (!aligned(p, 4)) return RECBLR_ERR_INVALID_ARGUMENT;
-        if (!disjoint({{a, 4 * n}, {b, 4 * n}},
-                      {{t.m1, n}, {t.m2, n}, {t.scale1, s}, {t.scale2, s}}))
-            return RECBLR_ERR_INVALID_ARGUMENT;
+        ranges.add(a, 4 * n, true);
+        ranges.add(b, 4 * n, true);
+        ranges.add(t.m1, n, false);
+        ranges.add(t.m2, n, false);
+        ranges.add(t.scale1, s, false);
+        ranges.add(t.scale2, s, false);
     }
+    if (!ranges.disjoint()) return RECBLR_ERR_INVALID_ARGUMENT;
     return status_of(launch_adamw_moments(tensors, count, m1_out, m2_out, (hipStream_t)stream));
 }
 

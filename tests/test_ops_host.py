@@ -220,6 +220,21 @@ def test_adamw_moments_refuses(rb):
     assert call(tensors(rb, 8, bits=8), (ctypes.c_void_p * 2)(addr(50), addr(8))) == bad
 
 
+def test_adamw_moments_refuses_overlap(rb):
+    """Outputs over other tensors' outputs, codes and scales, not only over their own."""
+    def call(n, a, b):
+        lists = [x and (ctypes.c_void_p * n)(*x) for x in (a, b)]
+        return rb.recblr_adamw_moments(tensors(rb, 300, count=n, bits=8), n, *lists, None)
+    bad = rb.ERR_INVALID_ARGUMENT
+    out = [addr(600 + i) for i in range(200)]
+    assert call(2, [out[0], out[0]], None) == bad                 # one output for two tensors
+    assert call(2, [out[0], out[0] + 1196], None) == bad          # the last element of it
+    assert call(2, out[:2], [out[2], out[1]]) == bad              # m2's over another's m1
+    assert call(2, None, [addr(8), out[1]]) == bad                # over the other's codes
+    assert call(2, None, [out[0], addr(4) + 4]) == bad            # over the other's scales
+    assert call(200, out[:199] + [out[77]], None) == bad
+
+
 # ------------------------------------------------------------------ sampling
 
 def draw(rb, **kw):
