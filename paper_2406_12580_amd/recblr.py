@@ -499,17 +499,21 @@ def _on_device(fn):
     The library launches on the current device; outputs and workspace come from
     torch's allocator on the stream of the launch, as in _on_stream.
     """
+    name = next(iter(inspect.signature(fn).parameters))
+
     @functools.wraps(fn)
-    def wrapper(first, *args, stream=None, **kwargs):
-        dev = first.device
+    def wrapper(*args, stream=None, **kwargs):
+        if not args and name not in kwargs:
+            raise TypeError(f"{fn.__name__}() needs the argument {name}")
+        dev = (args[0] if args else kwargs[name]).device
         if dev.type != "cuda":
             raise ValueError("tensors must live on the GPU")
         if stream is None and dev.index == torch._C._cuda_getDevice():
-            return fn(first, *args, **kwargs)
+            return fn(*args, **kwargs)
         if stream is not None and stream.device != dev:
             raise ValueError("stream belongs to another device than the tensors")
         with torch.cuda.device(dev), torch.cuda.stream(stream):
-            return fn(first, *args, **kwargs)
+            return fn(*args, **kwargs)
     return wrapper
 
 

@@ -803,6 +803,13 @@ def test_sample_nan_limits(rb, V):
     same(rb.sample(x, nan, top_p=p), rb.sample(x, torch.ones_like(u), top_p=p))
 
 
+def test_sample_arguments_by_name(rb):
+    import torch
+    x, u = torch.randn(3, 100, device="cuda"), torch.rand(3, device="cuda")
+    for a, b in zip(rb.sample(logits=x, u=u), rb.sample(x, u)):
+        assert torch.equal(a, b)
+
+
 def test_sample_empty_and_refusals(rb):
     import torch
     ids, prob = rb.sample(torch.empty((3, 0), device="cuda"), torch.rand(3, device="cuda"))

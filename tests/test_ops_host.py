@@ -285,6 +285,19 @@ def test_binding_refuses_cpu_tensors(rb):
         rb.AdamW([])
 
 
+def test_binding_takes_the_first_argument_by_name(rb):
+    """As far as the tensors' device, which is refused for CPU tensors."""
+    import torch
+    z = torch.zeros
+    with pytest.raises(ValueError, match="on the GPU"):
+        rb.sample(logits=z(1, 5), u=z(1))
+    with pytest.raises(ValueError, match="on the GPU"):
+        rb.delta_forward(q=z(1, 2, 1, 4), k=z(1, 2, 1, 4), v=z(1, 2, 1, 4), g=z(1, 2, 1),
+                         beta=z(1, 2, 1))
+    with pytest.raises(TypeError):
+        rb.sample()
+
+
 # ------------------------------------------------------------------ the references
 
 def _case(B, L, H, HV, Dk, Dv, seed=0):
