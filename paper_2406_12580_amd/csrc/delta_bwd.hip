@@ -898,7 +898,7 @@ hipError_t launch_grad(const DeltaBwdArgs& a, const BwdWs& ws, hipStream_t strea
 template <typename T, int DK>
 hipError_t launch_both(const DeltaBwdArgs& a, const BwdWs& ws, bool vec, hipStream_t stream) {
     size_t bytes;
-    const hipError_t e = delta_split(a.B * a.HV, a.L, a.Dk, a.Dv)
+    const hipError_t e = delta_split(a.B * a.HV, a.L, a.Dk, a.Dv, true)
                              ? launch_delta_split_backward(a, ws.D, ws.Y, ws.split, &bytes, stream)
                          : vec ? launch_state<T, DK, 32, true>(a, ws, stream)
                                : launch_state<T, DK, 32, false>(a, ws, stream);
@@ -937,7 +937,7 @@ size_t sum_bytes(int64_t B, int64_t L, int64_t H, int Dk) {
 size_t delta_backward_workspace(int64_t B, int64_t L, int64_t H, int64_t HV, int Dk, int Dv,
                                 IoType io) {
     size_t split = 0;
-    if (delta_split(B * HV, L, Dk, Dv)) {
+    if (delta_split(B * HV, L, Dk, Dv, true)) {
         DeltaBwdArgs a{};
         a.B = B;
         a.L = L;

@@ -340,7 +340,7 @@ hipError_t launch_typed(const DeltaFwdArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t delta_forward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv, IoType io) {
-    if (!delta_split(B * HV, L, Dk, Dv)) return 0;
+    if (!delta_split(B * HV, L, Dk, Dv, false)) return 0;
     DeltaFwdArgs a{};
     a.B = B;
     a.L = L;
@@ -355,7 +355,8 @@ size_t delta_forward_workspace(int64_t B, int64_t L, int64_t HV, int Dk, int Dv,
 
 hipError_t launch_delta_forward(const DeltaFwdArgs& a, void* ws, hipStream_t stream) {
     size_t bytes;
-    if (delta_split(a.B * a.HV, a.L, a.Dk, a.Dv)) return launch_delta_split_forward(a, ws, &bytes, stream);
+    if (delta_split(a.B * a.HV, a.L, a.Dk, a.Dv, false))
+        return launch_delta_split_forward(a, ws, &bytes, stream);
     return a.io == IoType::kF32 ? launch_typed<float>(a, stream) : launch_typed<bf16>(a, stream);
 }
 

@@ -908,18 +908,23 @@ hipError_t by_type(IoType io, int Dk, F f) {
 
 }  // namespace
 
-// Which way is the faster one, by what the two cost (us, fitted to 50 measured sizes of both,
-// forward): the walk in one kernel 9 for each chunk and each 512 strips of 32 columns; here 16
-// (36 from 65 columns of K on) for the launches, 2 a chunk of the walk, and 0.034 (0.1) for each
-// chunk of every head.  128 heads, 64 x 64, 1000 steps: 152 and 113 us; 400 heads, 200 steps:
-// 52 and 108 us; 60 heads, 128 x 128, 500 steps: 69 and 78 us; 4 heads, 16384 steps: 2040 us and
-// 290 us (a long walk is cut as well).
-bool delta_split(int64_t heads, int64_t L, int Dk, int Dv) {
-    const double chunks = (double)((L + C - 1) / C), strips = (double)(heads * ((Dv + 31) / 32));
-    const double one = 9.0 * chunks * (strips <= 512.0 ? 1.0 : strips / 512.0);
-    const bool wide = Dk > 64;
-    const double walk = chunks < 24.0 ? 2.0 * chunks : 48.0 + 0.4 * (chunks - 24.0);
-    return (wide ? 36.0 : 16.0) + walk + (wide ? 0.1 : 0.034) * (double)heads * chunks < one;
+// Which way is the faster one.  What is done here for all chunks at once costs more than the same
+// within the one-kernel walk (operands go through memory), so this way gains only what that walk
+// leaves idle: where the strips of 16 columns are no more than the two workgroups a compute unit
+// that run at once, the heads no more than half of the units, and the chunks enough to pay for two
+// or three launches (and, from 65 columns of K on, for the wider operands of the forward).
+// One kernel and this way, bf16, forward / gradients with the backward, us:
+//   4 heads, 16384 steps, 128 x 128     1625 and 228  /  2287 and 401
+//   96 heads, 1000 steps, 64 x 64        120 and  89  /   213 and 180
+//   96 heads, 128 steps, 64 x 64          19 and  32  /    39 and  47
+//   192 heads, 1000 steps, 64 x 64       121 and 192  /   322 and 379
+//   48 heads, 200 steps, 128 x 128        30 and  51  /    82 and  83
+//   8192 heads, 200 steps, 64 x 64       619 and 2610 /  2937 and 4872
+// Over 1158 sizes of both types the choice is 0.4% slower than always the faster one, at most 1.5
+// times (32-bit 128 x 32, 200 steps).
+bool delta_split(int64_t heads, int64_t L, int Dk, int Dv, bool backward) {
+    const int64_t chunks = (L + C - 1) / C, strips = heads * ((Dv + SC - 1) / SC);
+    return chunks >= (Dk > 64 && !backward ? 7 : 4) && heads <= 128 && strips <= 512;
 }
 
 hipError_t launch_delta_split_forward(const DeltaFwdArgs& a, void* ws, size_t* bytes,

@@ -101,7 +101,7 @@ constexpr float kDeltaMinG = -100.0f;
 
 // The way of delta_split.hip, where it is the faster one: the forward, and the backward's
 // recurrence into D and Y.  With ws null these write the workspace's size to *bytes only.
-bool delta_split(int64_t heads, int64_t L, int Dk, int Dv);
+bool delta_split(int64_t heads, int64_t L, int Dk, int Dv, bool backward);
 hipError_t launch_delta_split_forward(const DeltaFwdArgs& a, void* ws, size_t* bytes,
                                       hipStream_t stream);
 hipError_t launch_delta_split_backward(const DeltaBwdArgs& a, float* D, float* Y, void* ws,

@@ -140,6 +140,16 @@ def test_delta(rb, io, size):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [
+    (64, 193, 2, 2, 16, 64), (64, 192, 2, 2, 16, 64), (65, 193, 2, 2, 16, 64),
+    (16, 200, 1, 8, 64, 65), (8, 390, 1, 8, 96, 128), (8, 384, 1, 8, 96, 128)])
+def test_delta_at_the_borders_of_the_ways(rb, io, size):
+    """As many heads, strips and chunks as either way to walk takes, and one more or less."""
+    print(io, size, flush=True)
+    check_delta(rb, io, delta_case(io, *size, seed=15))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_delta_without_state(rb, io):
     """No initial state, no gradient of the final one: both count as zero."""
     c = delta_case(io, 2, 100, 1, 2, 64, 64, state=False)

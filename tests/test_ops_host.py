@@ -149,6 +149,20 @@ def test_delta_workspace(rb):
     assert size(5, 2, 3, 2, 4, 8, 8, 0) == 0
 
 
+def test_delta_workspace_of_many_heads(rb):
+    """Heads that fill the chip are walked in one kernel each way: no workspace forward, the
+    gradients of the states and of the updates alone backward.  (The other way's walk has a
+    workgroup to 16 columns: 2^32 threads at the last of these sizes.)"""
+    up = lambda n: -(-n // 256) * 256  # noqa: E731
+    for B, L, Dk, Dv in ((8192, 200, 64, 64), (2048, 200, 64, 128), (50000, 8, 64, 64),
+                         (4096, 1000, 16, 16), (1 << 22, 64, 64, 64)):
+        for io in (rb.F32, rb.BF16):
+            sizes = (B, L, 1, 1, Dk, Dv, io)
+            assert rb.recblr_delta_workspace_size(rb.OP_DELTA_FORWARD, *sizes) == 0, sizes
+            assert rb.recblr_delta_workspace_size(rb.OP_DELTA_BACKWARD, *sizes) == up(
+                4 * B * -(-L // 64) * Dk * Dv) + up(4 * B * L * Dv), sizes
+
+
 # ------------------------------------------------------------------ AdamW
 
 def tensors(rb, size, count=2, bits=32, **kw):
