@@ -140,6 +140,35 @@ def test_delta(rb, io, size):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("L,Dk,Dv", [(1700, 32, 33), (1700, 33, 40), (3000, 64, 64),
+                                     (1700, 100, 17), (2100, 128, 48)])
+def test_delta_long_memory(rb, io, L, Dk, Dv):
+    """States that last over hundreds of steps, behind keys that turn slowly: what a long stretch
+    of steps does to the state is a full matrix of size one, far from symmetric, so a walk that is
+    cut into stretches has to join them rightly.  Errors of a chunk last as well; those of
+    different chunks are independent, so the bars grow with the root of their number."""
+    print(io, L, Dk, Dv, flush=True)
+    c = delta_case(io, 1, L, 1, 2, Dk, Dv, seed=17, decay=0.002)
+    r = np.random.default_rng(18)
+    k = [r.normal(size=Dk)]
+    for _ in range(L - 1):
+        k.append(0.97 * k[-1] + math.sqrt(1 - 0.97 ** 2) * r.normal(size=Dk))
+    k = np.stack(k)[None, :, None]
+    c["k"], c["k_"] = put(k / np.linalg.norm(k, axis=-1, keepdims=True), io)
+    c["beta"], c["beta_"] = put(0.2 * c["beta_"], io)
+    out = run_delta(rb, c)
+    want = ref.delta(*(c[n + "_"] for n in ("q", "k", "v", "g", "beta")), h0=c["h0_"],
+                     do=c["do_"], dhT=c["dhT_"])
+    f32, grow = delta_bars("f32", Dk)["state"], math.sqrt(-(-L // 64))
+    low = 0.0 if io == "f32" else BF16 + 2.0 ** -13
+    for name in ("o", "hT", "dq", "dk", "dv", "dg", "dbeta", "dh0"):
+        own = 0.0 if name in ("hT", "dh0") else low if name != "dg" or not low else BF16 + 2.0 ** -10
+        close(name, out[name], want[name], own + grow * f32 * (4 if name == "dg" else 1))
+    kept = np.stack([want["kept"][t] for t in range(0, L, 64)], axis=2)
+    close("states", out["states"], kept, grow * f32)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("size", [
     (64, 193, 2, 2, 16, 64), (64, 192, 2, 2, 16, 64), (65, 193, 2, 2, 16, 64),
     (16, 200, 1, 8, 64, 65), (8, 390, 1, 8, 96, 128), (8, 384, 1, 8, 96, 128)])
@@ -957,6 +986,46 @@ def test_delta_gradients_against_differences(rb):
         got = (host(out["d" + name]) * way).sum()
         print(f"ERR d{name}: {abs(got - diff):.2e} of {1e-2 * size:.2e}", flush=True)
         assert abs(got - diff) <= 1e-2 * size, name
+
+
+@pytest.mark.parametrize("L", [70, 260])
+def test_delta_gradients_along_themselves(rb, L):
+    """Each gradient's norm against the difference of the loss along the gradient's own direction
+    (that of 64 bits), where the decay is weak enough for the first state's gradient to count.
+
+    The difference over 2 e is off by what it is in 64 bits and by the forward's bar times the
+    loss's size (root of its terms' squares) over e; both are a fiftieth of the norm at most."""
+    c = delta_case("f32", 1, L, 1, 2, 32, 32, seed=9, decay=0.02)
+    names = ("q", "k", "v", "g", "beta", "h0")
+    out = run_delta(rb, c)
+    exact = {n: c[n + "_"] for n in names}
+    want = ref.delta(**exact, do=c["do_"], dhT=c["dhT_"])
+    e = 2.0 ** -6
+
+    def of(o, hT):
+        return (o * c["do_"]).sum() + (hT * c["dhT_"]).sum()
+
+    def loss(**moved):
+        d = {**c, **moved}
+        o, hT, _ = rb.delta_forward(*(d[n] for n in names[:5]), h0=d["h0"])
+        return of(host(o), host(hT))
+
+    def loss64(**moved):
+        d = ref.delta(**{**exact, **moved})
+        return of(d["o"], d["hT"])
+
+    size = math.sqrt(((want["o"] * c["do_"]) ** 2).sum() + ((want["hT"] * c["dhT_"]) ** 2).sum())
+    for name in names:
+        norm = np.linalg.norm(want["d" + name])
+        way = want["d" + name] / norm
+        up, down = (exact[name] + s * e * way for s in (1, -1))
+        bar = abs((loss64(**{name: up}) - loss64(**{name: down})) / (2 * e) - norm)
+        bar += delta_bars("f32", 32)["state"] * size / e
+        diff = (loss(**{name: put(up, "f32")[0]}) - loss(**{name: put(down, "f32")[0]})) / (2 * e)
+        got = (host(out["d" + name]) * way).sum()
+        print(f"ERR d{name}: {abs(got - diff):.2e} of {bar:.2e}, norm {norm:.2e}", flush=True)
+        assert bar <= norm / 50, name
+        assert abs(got - diff) <= bar, name
 
 
 # ------------------------------------------------------------------ offsets past 32 bits
