@@ -33,9 +33,11 @@ extern "C" {
  * 1 <= Dk, Dv <= 128, HV <= 4096, B HV ceil(Dv / 32) and B HV ceil(L / 64) below 2^24
  * (else UNSUPPORTED), HV a multiple of H (else INVALID_ARGUMENT).  g is the
  * logarithm of the decay, usually <= 0; below -100 it counts as -100, so -inf
- * clears the state.  A step with g = 0 and beta = 0
- * leaves the state as it is (padding); queries and keys are taken as given
- * (they are usually brought to length one by the caller).  Inputs are finite, in
+ * leaves e^-100 of the (finite) state, nothing next to float's rounding.  Where g is
+ * positive, its sums over successive steps of a group of 64 stay below 88, since
+ * their powers of e are formed.  A step with g = 0 and beta = 0 leaves the state
+ * as it is (padding); queries and keys are taken as given (they are usually
+ * brought to length one by the caller).  Inputs are finite, in
  * padding too (g may be -inf): steps are worked on 64 at a time, and a NaN or an
  * infinity reaches the outputs of its whole group of 64 steps, those before it
  * among them, and what follows; other rows and heads are not touched by it.

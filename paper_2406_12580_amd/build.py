@@ -30,7 +30,8 @@ FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # -O3 unswitches the delta rule's gradient kernel on its waves' roles into copies that spill
-# (587 registers of the fp32 one at 64 columns); -O2 keeps it within its registers.
+# (587 registers of the fp32 one at 64 columns); -O2 keeps it within its registers for keys of up
+# to 64, and at 92 to 160 registers in scratch memory beyond.
 OPT = {"delta_bwd.hip": "-O2"}
 
 

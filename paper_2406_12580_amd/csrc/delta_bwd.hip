@@ -20,10 +20,12 @@
 // that are meant to cancel: at g = -12 a hundredth of dg was wrong in fp32.)
 //
 // Both are bound by issue and latency, not by memory.  2048 heads, 200 steps, 64 x 64 bf16: the
-// recurrence 306 us, the rest 481 us; 256 heads, 2048 steps fp32: 460 and 800 us.  Strips of the
-// recurrence are 32 columns (its operands leave no room for 64).  The rest is eight waves on one
-// chunk, four to a side (rows for dQ and a, columns for b), since one wave's half of the products
-// fills 240 registers; two such workgroups do not fit a CU's LDS.
+// recurrence 313 us, the rest 506 us; 256 heads, 2048 steps fp32: 456 and 916 us (W's products are
+// a seventh of the latter, by fp32 instructions).  Strips of the recurrence are 32 columns (its
+// operands leave no room for 64).  The rest is eight waves on one chunk, four to a side (rows for
+// dQ and a, columns for b), since one wave's half of the products fills 232 registers at 64
+// columns of K; from 65 on it takes all 256 and 92 to 160 more in scratch memory.  Two such
+// workgroups do not fit a CU's LDS.
 #include <hip/hip_runtime.h>
 
 #include "delta_tile.hpp"

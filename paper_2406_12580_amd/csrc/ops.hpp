@@ -95,7 +95,7 @@ size_t delta_backward_workspace(int64_t B, int64_t L, int64_t H, int64_t HV, int
 hipError_t launch_delta_backward(const DeltaBwdArgs& a, void* ws, hipStream_t stream);
 hipError_t launch_delta_step(const DeltaStepArgs& a, hipStream_t stream);
 
-// Log decays below this count as this: e^-100 of any state is nothing next to it in fp32,
+// Log decays below this count as this: e^-100 of a state is nothing next to what it was in fp32,
 // and the running sums of g stay finite, where differences of them are taken.
 constexpr float kDeltaMinG = -100.0f;
 
