@@ -250,6 +250,31 @@ def test_delta_gradients_of_single_strong_decays(rb, io, size):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size,grow", [((2, 130, 1, 2, 64, 64), 0.6), ((1, 64, 1, 2, 100, 33), 1.0),
+                                       ((1, 260, 1, 1, 32, 48), 0.25)])
+def test_delta_growing_states(rb, io, size, grow):
+    """Positive log decays, up to a sum of 64 in a group of 64 steps and e^65 of the state."""
+    print(io, size, grow, flush=True)
+    c = delta_case(io, *size, seed=19)
+    g = grow * (0.8 + 0.2 * np.random.default_rng(20).random(c["g_"].shape))
+    c["g"], c["g_"] = put(g, io)
+    check_delta(rb, io, c)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_delta_step_decays(rb, io):
+    """Decays from nothing to a clearing one and a growing one."""
+    c = delta_case(io, 3, 1, 1, 2, 64, 64, seed=21)
+    g = np.array([0.0, -1.0, -12.0, -math.inf, -1e30, 0.7]).reshape(3, 1, 2)
+    c["g"], c["g_"] = put(g, io)
+    one = {n: c[n][:, 0].contiguous() for n in ("q", "k", "v", "g", "beta")}
+    o, h = rb.delta_step(*one.values(), c["h0"])
+    want = ref.delta(*(c[n + "_"] for n in ("q", "k", "v", "g", "beta")), h0=c["h0_"])
+    close("o", o, want["o"][:, 0], delta_bars(io, 64)["out"])
+    close("h", h, want["hT"], delta_bars(io, 64)["state"])
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_delta_alike_keys(rb, io):
     """Keys that are nearly the same make the chunk's triangular system as far from the unit
     matrix as it gets (entries near beta); strengths up to two."""
