@@ -10,8 +10,8 @@
 //
 // With float moments the pass is bound by memory: 134 million fp32 parameters take 705 us (5.3
 // TB/s), bf16 ones 574 us (5.1 TB/s), where a copy of 4 GiB, 16 bytes to a lane, reaches 6.2.
-// With codes it is bound by the arithmetic of the codes, in 64 bits: 562 us (fp32) and 522 us
-// (bf16, 2.6 TB/s), nearly the same for half of the bytes apart.  A model's 45 small tensors are
+// With codes it is bound by the arithmetic of the codes, in 64 bits: 562 us for fp32
+// parameters and 522 us for bf16 ones, 16 and 10 bytes an element (2.6 TB/s).  A model's 45 small tensors are
 // two launches of 6 us, behind 30 us of the call from Python.
 #include <hip/hip_runtime.h>
 
