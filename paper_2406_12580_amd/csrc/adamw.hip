@@ -3,16 +3,18 @@
 //
 // One element reads and writes 28 bytes with float moments (fp32 I/O) and 16
 // with codes.  The tables travel as kernel arguments, so a call is one launch
-// for every kMaxTensors tensors and needs no copies.  A workgroup takes kChunk consecutive elements of one tensor, found
-// by comparing its number with every tensor's first chunk (all scalar).  A wave
-// takes 256 elements at a time, four to a lane: with codes that is one block of
-// a scale, whose maximum stays within the wave.
+// for every kMaxTensors tensors and needs no copies.  A workgroup takes kChunk
+// consecutive elements of one tensor, found by comparing its number with every
+// tensor's first chunk (all scalar).  A wave takes 256 elements at a time, four
+// to a lane: with codes that is one block of a scale, whose maximum stays
+// within the wave.
 //
-// With float moments the pass is bound by memory: 134 million fp32 parameters take 705 us (5.3
-// TB/s), bf16 ones 574 us (5.1 TB/s), where a copy of 4 GiB, 16 bytes to a lane, reaches 6.2.
-// With codes it is bound by the arithmetic of the codes, in 64 bits: 562 us for fp32
-// parameters and 522 us for bf16 ones, 16 and 10 bytes an element (2.6 TB/s).  A model's 45 small tensors are
-// two launches of 6 us, behind 30 us of the call from Python.
+// With float moments the pass is bound by memory: 134 million fp32 parameters
+// take 705 us (5.3 TB/s), bf16 ones 574 us (5.1 TB/s), where a copy of 4 GiB,
+// 16 bytes to a lane, reaches 6.2.  With codes it is bound by their arithmetic,
+// in 64 bits: 562 us for fp32 parameters and 522 us for bf16 ones, 16 and 10
+// bytes an element (2.6 TB/s).  A model's 45 small tensors are two launches of
+// 6 us, behind 30 us of the call from Python.
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"
