@@ -1,7 +1,9 @@
 /*
  * recblr_ops.h - C ABI of librecblr.so next to the BD-LRU layer (recblr.h): a
  * recurrence with a matrix state (the gated delta rule), AdamW over many
- * tensors, and the choice of an item from logits.
+ * tensors, and the choice of an item from logits; the lookup of items in a
+ * table and its gradient, norms and rotation of queries and keys, a policy
+ * loss over logits, and an update of matrices that is orthogonalised (Muon).
  *
  * The conventions of recblr.h hold: dense row-major device tensors aligned to
  * their element size, `io` (RECBLR_F32 or RECBLR_BF16) for the type of the
@@ -161,6 +163,118 @@ int recblr_sample(const void* logits, const float* u, const float* temperature,
                   const int32_t* top_k, const float* top_p, const float* min_p, int32_t* ids,
                   float* prob, int64_t B, int64_t V, int io, void* ws, size_t ws_bytes,
                   void* stream);
+
+/*
+ * Lookup in an item table, and its gradient.
+ *   table, dtable : [V][D] io;  ids : [N] int32;  out, dout : [N][D] io
+ *     out_n = scale table[ids_n],   dtable_v = scale sum over the n with ids_n = v of dout_n
+ * pad_id (usually 0, or -1 for none) marks padding: its rows of out are zeros, and it sends
+ * no gradient.  Any other id outside [0, V) gives a row of NaN and sends no gradient.
+ * accumulate = 0 writes every row of dtable, those of no id as zeros; accumulate = 1 adds to
+ * the rows that ids name and touches no other (a table that the prediction layer shares has
+ * its gradient there already).  An item's rows are summed in fp32 in an order that hangs on
+ * ids alone, and rounded to io once, together with what was there.
+ * Errors: INVALID_ARGUMENT; UNSUPPORTED (io, D > 4096, V >= 2^31 - 1, N > 2^28, N D > 2^33,
+ * V D > 2^40); WORKSPACE.
+ */
+size_t recblr_embed_workspace_size(int64_t N, int64_t V, int64_t D, int io);
+int recblr_embed_forward(const void* table, const int32_t* ids, void* out, int64_t N, int64_t V,
+                         int64_t D, float scale, int32_t pad_id, int io, void* stream);
+int recblr_embed_backward(const int32_t* ids, const void* dout, void* dtable, int64_t N,
+                          int64_t V, int64_t D, float scale, int32_t pad_id, int accumulate,
+                          int io, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Queries and keys of each head, normalised and rotated by their positions, N tokens with H
+ * query and HK key heads of width D.  Of a head's vector x at position p:
+ *     u = x / sqrt(s sum x^2 + eps),  s = 1 (RECBLR_NORM_L2: length one) or 1 / D (_RMS)
+ *     y = R_p (w u)       w : wq or wk, [D] float, NULL for ones
+ * R_p turns the pairs (i, i + rotate / 2), i < rotate / 2, by the angle p base^(-2 i / rotate)
+ * (rotate even, 0 for none; elements from rotate on are not turned).  Angles are formed in 64
+ * bits, whatever the position.
+ *   q [N][H][D], k [N][HK][D] io, tokens q_pitch and k_pitch elements apart (parts of one
+ *   projection's output, say; H D and HK D where they are dense); positions [N] int32, NULL
+ *   where rotate = 0; q_out, k_out dense.
+ * The backward takes the same q and k and the gradients dq_out, dk_out (dense) to dq, dk
+ * (dense) and, where weights are given, dwq, dwk [D] float.
+ * Errors: INVALID_ARGUMENT (also eps <= 0, base <= 0); UNSUPPORTED (io, D > 256, H or HK > 4096,
+ * N >= 2^31 - 256, a pitch of 2^31); WORKSPACE.
+ */
+enum { RECBLR_NORM_L2 = 0, RECBLR_NORM_RMS = 1 };
+size_t recblr_qk_norm_workspace_size(int64_t N, int64_t H, int64_t HK, int64_t D, int io);
+int recblr_qk_norm_forward(const void* q, const void* k, int64_t q_pitch, int64_t k_pitch,
+                           const float* wq, const float* wk, const int32_t* positions,
+                           void* q_out, void* k_out, int64_t N, int64_t H, int64_t HK, int64_t D,
+                           int64_t rotate, double base, int norm, float eps, int io,
+                           void* stream);
+int recblr_qk_norm_backward(const void* q, const void* k, int64_t q_pitch, int64_t k_pitch,
+                            const float* wq, const float* wk, const int32_t* positions,
+                            const void* dq_out, const void* dk_out, void* dq, void* dk,
+                            float* dwq, float* dwk, int64_t N, int64_t H, int64_t HK, int64_t D,
+                            int64_t rotate, double base, int norm, float eps, int io, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/*
+ * Clipped policy loss with a KL term (Schulman et al., "Proximal Policy Optimization") over
+ * rows of logits, and its gradient.  For row n with the chosen item a = ids_n, old_logp_n, its
+ * logarithm of probability under the policy that chose it, advantage A_n, and weight w_n:
+ *     logp_n = log softmax(logits_n / temperature)[a],   r = e^(logp_n - old_logp_n)
+ *     d = ref_logp_n - logp_n
+ *     loss = sum of w_n (-min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl (e^d - d - 1))
+ *     dlogits = gradient of loss
+ *   logits, dlogits : [N][V] io (dlogits may be NULL, or logits itself);  ids : [N] int32
+ *   old_logp, advantage : [N] float;  ref_logp : [N] float, NULL where kl = 0
+ *   weight : [N] float or NULL (ones);  loss : [1] float;  logp : [N] float or NULL
+ * A row with ids_n < 0 is left out whatever it holds: logp 0, dlogits 0 (recblr_sample gives
+ * -1 for a row without items).  ids_n >= V makes the row's logp, dlogits and the loss NaN.
+ * Masked items have the logit -inf or any value far below the rest; their gradient is 0.  Of a
+ * row that is counted, only -inf, a NaN or a +inf make logp, dlogits and the loss NaN.  A
+ * chosen item that is masked by -inf has logp -inf: with kl = 0 its ratio is 0; with kl > 0
+ * its loss is inf and its gradient not finite.  An advantage of 0 has no surrogate whatever r is.
+ * The loss is summed in 64 bits in a fixed order.
+ * Errors: INVALID_ARGUMENT (also a temperature outside [1e-30, 1e30], clip_low, clip_high or
+ * kl < 0 or infinite, any of them NaN, kl > 0 without ref_logp, V = 0 with N > 0); UNSUPPORTED (io,
+ * V > 2^24, N >= 2^22, N ceil(V / 2048) >= 2^24); WORKSPACE.
+ */
+size_t recblr_policy_loss_workspace_size(int64_t N, int64_t V, int io);
+int recblr_policy_loss(const void* logits, const int32_t* ids, const float* old_logp,
+                       const float* advantage, const float* ref_logp, const float* weight,
+                       float* loss, float* logp, void* dlogits, int64_t N, int64_t V,
+                       float temperature, float clip_low, float clip_high, float kl, int io,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Muon (Jordan et al., "Muon: an optimizer for hidden layers"): momentum whose update is
+ * brought near the closest orthogonal matrix, over a list of matrices, in place.
+ *     m = momentum m + (1 - momentum) grad
+ *     U = momentum m + (1 - momentum) grad (nesterov) or m;   X = U / (|U|_F + eps)
+ *     `steps` times:  A = X X^T,  X = a X + (b A + c A^2) X,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *     param = param (1 - lr weight_decay) - lr scale X
+ * (X is taken transposed where it has more rows than columns: the same in exact arithmetic).
+ *   param, grad : [rows][cols] io;  m : [rows][cols] float
+ * The norm is summed in 64 bits.  Operands of the products are held as two fp16 numbers each,
+ * 22 bits of every element, and products are summed in fp32: an error of 2^-22 of the operands'
+ * sizes, which the steps multiply, as they do singular values next to zero, by up to 485 in five
+ * steps (fp32's own rounding, 2^-24, by as much).  A gradient and momentum of zeros
+ * leaves X = 0; a NaN or an infinity reaches all of its own matrix and no other.
+ * Errors: INVALID_ARGUMENT as recblr_adamw_update, also momentum outside [0, 1), eps <= 0,
+ * steps < 1; UNSUPPORTED (io, steps > 64, rows or cols > 2^16, their product > 2^30,
+ * count > 2^20); WORKSPACE.  Matrices with rows or cols = 0 are passed over.  `tensors` is host
+ * memory, read before the call returns.
+ */
+typedef struct {
+    void* param;         /* [rows][cols] io */
+    const void* grad;    /* [rows][cols] io */
+    float* m;            /* [rows][cols] */
+    int64_t rows, cols;
+    double weight_decay;
+    double scale;        /* of the update, e.g. sqrt(max(1, rows / cols)) */
+} recblr_muon_tensor;
+
+size_t recblr_muon_workspace_size(const recblr_muon_tensor* tensors, int64_t count, int io);
+int recblr_muon_update(const recblr_muon_tensor* tensors, int64_t count, int io, double lr,
+                       double momentum, int nesterov, int steps, double eps, void* ws,
+                       size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

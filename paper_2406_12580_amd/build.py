@@ -21,7 +21,7 @@ SOURCES = ["capi.cpp", "scan_fwd.hip", "scan_bwd.hip", "step.hip", "gemm.hip", "
            "gated.hip", "model.hip", "noalloc.hip", "fused_fwd.hip", "fused_bwd.hip",
            "proj_bwd.hip", "ffn.hip", "head.hip", "capi_ops.cpp", "adamw.hip", "sample.hip",
            "delta_step.hip", "delta_fwd.hip", "delta_bwd.hip",
-           "delta_split.hip"]
+           "delta_split.hip", "embed.hip", "qk_norm.hip", "policy.hip", "muon.hip"]
 # Linear layers that the matrix-core tiles do not take go to rocBLAS.
 LIBS = ["-L/opt/rocm/lib", "-lrocblas"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -294,4 +294,287 @@ int recblr_delta_step(const void* q, const void* k, const void* v, const void* g
     return status_of(launch_delta_step(a, (hipStream_t)stream));
 }
 
+// ------------------------------------------------------------------ item lookup
+
+static int embed_sizes(int64_t N, int64_t V, int64_t D, int io) {
+    if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
+    if (N < 0 || V < 0 || D < 1) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (D > 4096 || V >= ((int64_t)1 << 31) - 1 || N > ((int64_t)1 << 28))
+        return RECBLR_ERR_UNSUPPORTED;
+    // The lookup has a workgroup to 512 units of a row or more, the runs' joining one of 512
+    // threads to 64 positions.
+    if (N * D > ((int64_t)1 << 33) || V * D > ((int64_t)1 << 40)) return RECBLR_ERR_UNSUPPORTED;
+    return RECBLR_OK;
+}
+
+size_t recblr_embed_workspace_size(int64_t N, int64_t V, int64_t D, int io) {
+    if (embed_sizes(N, V, D, io) != RECBLR_OK) return 0;
+    return embed_workspace(N, V, D, io_of(io));
+}
+
+int recblr_embed_forward(const void* table, const int32_t* ids, void* out, int64_t N, int64_t V,
+                         int64_t D, float scale, int32_t pad_id, int io, void* stream) {
+    const int st = embed_sizes(N, V, D, io);
+    if (st) return st;
+    if (N == 0) return RECBLR_OK;
+    if (!ids || !out || (V > 0 && !table)) return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t e = esz(io), n = (size_t)(N * D) * e, t = (size_t)(V * D) * e;
+    if (!aligned(table, e) || !aligned(out, e) || !aligned(ids, 4))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!disjoint({{out, n}}, {{table, t}, {ids, (size_t)N * 4}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const EmbedArgs a{ids, table, out, N, V, D, scale, pad_id, false, io_of(io)};
+    return status_of(launch_embed_forward(a, (hipStream_t)stream));
+}
+
+int recblr_embed_backward(const int32_t* ids, const void* dout, void* dtable, int64_t N,
+                          int64_t V, int64_t D, float scale, int32_t pad_id, int accumulate,
+                          int io, void* ws, size_t ws_bytes, void* stream) {
+    int st = embed_sizes(N, V, D, io);
+    if (st) return st;
+    if (V == 0 || (N == 0 && accumulate)) return RECBLR_OK;
+    if (!dtable || (N > 0 && (!ids || !dout))) return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t e = esz(io), n = (size_t)(N * D) * e, t = (size_t)(V * D) * e;
+    if (!aligned(dout, e) || !aligned(dtable, e) || !aligned(ids, 4))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!disjoint({{dtable, t}}, {{dout, n}, {ids, (size_t)N * 4}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t need = embed_workspace(N, V, D, io_of(io));
+    st = check_ws(ws, ws_bytes, need);
+    if (st) return st;
+    if (!disjoint({{ws, need}}, {{dout, n}, {ids, (size_t)N * 4}, {dtable, t}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const EmbedArgs a{ids, dout, dtable, N, V, D, scale, pad_id, accumulate != 0, io_of(io)};
+    return status_of(launch_embed_backward(a, ws, (hipStream_t)stream));
+}
+
+// ------------------------------------------------------------------ norms of queries and keys
+
+static int qk_sizes(int64_t N, int64_t H, int64_t HK, int64_t D, int io) {
+    if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
+    if (N < 0 || H < 1 || HK < 1 || D < 1) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (D > 256 || H > 4096 || HK > 4096 || N >= ((int64_t)1 << 31) - 256)
+        return RECBLR_ERR_UNSUPPORTED;
+    return RECBLR_OK;
+}
+
+size_t recblr_qk_norm_workspace_size(int64_t N, int64_t H, int64_t HK, int64_t D, int io) {
+    if (qk_sizes(N, H, HK, D, io) != RECBLR_OK || N == 0) return 0;
+    return qk_norm_workspace(N, (int)H, (int)HK, (int)D, io_of(io));
+}
+
+// What forward and backward check alike, and their common arguments.
+static int qk_args(QkNormArgs* a, const void* q, const void* k, int64_t q_pitch, int64_t k_pitch,
+                   const float* wq, const float* wk, const int32_t* positions, int64_t N,
+                   int64_t H, int64_t HK, int64_t D, int64_t rotate, double base, int norm,
+                   float eps, int io) {
+    const int st = qk_sizes(N, H, HK, D, io);
+    if (st) return st;
+    if (rotate < 0 || rotate > D || rotate % 2 || q_pitch < H * D || k_pitch < HK * D)
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    if (norm != RECBLR_NORM_L2 && norm != RECBLR_NORM_RMS) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!(eps > 0.0f) || !(base > 0.0)) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (q_pitch >= ((int64_t)1 << 31) || k_pitch >= ((int64_t)1 << 31))
+        return RECBLR_ERR_UNSUPPORTED;
+    if (N > 0 && (!q || !k || (rotate > 0 && !positions))) return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t e = esz(io);
+    if (!aligned(q, e) || !aligned(k, e) || !aligned(wq, 4) || !aligned(wk, 4) ||
+        !aligned(positions, 4))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    *a = QkNormArgs{};
+    a->x[0] = q;
+    a->x[1] = k;
+    a->pitch[0] = q_pitch;
+    a->pitch[1] = k_pitch;
+    a->w[0] = wq;
+    a->w[1] = wk;
+    a->positions = rotate > 0 ? positions : nullptr;
+    a->N = N;
+    a->heads[0] = (int)H;
+    a->heads[1] = (int)HK;
+    a->D = (int)D;
+    a->rotate = (int)rotate;
+    a->base = base;
+    a->share = norm == RECBLR_NORM_RMS ? 1.0f / (float)D : 1.0f;
+    a->eps = eps;
+    a->io = io_of(io);
+    return RECBLR_OK;
+}
+
+// Bytes of N tokens of `width` elements that lie `pitch` apart.
+static size_t pitched(int64_t N, int64_t pitch, int64_t width, size_t e) {
+    return N > 0 ? (size_t)((N - 1) * pitch + width) * e : 0;
+}
+
+int recblr_qk_norm_forward(const void* q, const void* k, int64_t q_pitch, int64_t k_pitch,
+                           const float* wq, const float* wk, const int32_t* positions,
+                           void* q_out, void* k_out, int64_t N, int64_t H, int64_t HK, int64_t D,
+                           int64_t rotate, double base, int norm, float eps, int io,
+                           void* stream) {
+    QkNormArgs a;
+    const int st = qk_args(&a, q, k, q_pitch, k_pitch, wq, wk, positions, N, H, HK, D, rotate,
+                           base, norm, eps, io);
+    if (st) return st;
+    if (N == 0) return RECBLR_OK;
+    if (!q_out || !k_out || !aligned(q_out, esz(io)) || !aligned(k_out, esz(io)))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t e = esz(io), w = (size_t)D * 4;
+    if (!disjoint({{q_out, (size_t)(N * H * D) * e}, {k_out, (size_t)(N * HK * D) * e}},
+                  {{q, pitched(N, q_pitch, H * D, e)}, {k, pitched(N, k_pitch, HK * D, e)},
+                   {wq, w}, {wk, w}, {a.positions, (size_t)N * 4}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    a.out[0] = q_out;
+    a.out[1] = k_out;
+    return status_of(launch_qk_norm_forward(a, (hipStream_t)stream));
+}
+
+int recblr_qk_norm_backward(const void* q, const void* k, int64_t q_pitch, int64_t k_pitch,
+                            const float* wq, const float* wk, const int32_t* positions,
+                            const void* dq_out, const void* dk_out, void* dq, void* dk,
+                            float* dwq, float* dwk, int64_t N, int64_t H, int64_t HK, int64_t D,
+                            int64_t rotate, double base, int norm, float eps, int io, void* ws,
+                            size_t ws_bytes, void* stream) {
+    QkNormArgs a;
+    int st = qk_args(&a, q, k, q_pitch, k_pitch, wq, wk, positions, N, H, HK, D, rotate, base,
+                     norm, eps, io);
+    if (st) return st;
+    // Weights and their gradients come together.
+    if ((dwq != nullptr) != (wq != nullptr) || (dwk != nullptr) != (wk != nullptr))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!aligned(dwq, 4) || !aligned(dwk, 4)) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (N == 0 && !dwq && !dwk) return RECBLR_OK;
+    const size_t e = esz(io), w = (size_t)D * 4;
+    const size_t nq = (size_t)(N * H * D) * e, nk = (size_t)(N * HK * D) * e;
+    if (N > 0) {
+        for (const void* p : {dq_out, dk_out, (const void*)dq, (const void*)dk})
+            if (!p || !aligned(p, e)) return RECBLR_ERR_INVALID_ARGUMENT;
+    }
+    if (!disjoint({{dq, nq}, {dk, nk}, {dwq, w}, {dwk, w}},
+                  {{q, pitched(N, q_pitch, H * D, e)}, {k, pitched(N, k_pitch, HK * D, e)},
+                   {wq, w}, {wk, w}, {a.positions, (size_t)N * 4}, {dq_out, nq}, {dk_out, nk}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t need = dwq || dwk ? recblr_qk_norm_workspace_size(N, H, HK, D, io) : 0;
+    st = check_ws(ws, ws_bytes, need);
+    if (st) return st;
+    if (!disjoint({{ws, need}},
+                  {{q, pitched(N, q_pitch, H * D, e)}, {k, pitched(N, k_pitch, HK * D, e)},
+                   {wq, w}, {wk, w}, {a.positions, (size_t)N * 4}, {dq_out, nq}, {dk_out, nk},
+                   {dq, nq}, {dk, nk}, {dwq, w}, {dwk, w}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    a.dy[0] = dq_out;
+    a.dy[1] = dk_out;
+    a.out[0] = dq;
+    a.out[1] = dk;
+    a.dw[0] = dwq;
+    a.dw[1] = dwk;
+    return status_of(launch_qk_norm_backward(a, ws, (hipStream_t)stream));
+}
+
+// ------------------------------------------------------------------ policy loss
+
+static int policy_sizes(int64_t N, int64_t V, int io) {
+    if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
+    if (N < 0 || V < 0 || (N > 0 && V == 0)) return RECBLR_ERR_INVALID_ARGUMENT;
+    // A row may be 1024 threads, or a piece of 2048 items a workgroup.
+    if (N >= ((int64_t)1 << 22) || V > ((int64_t)1 << 24)) return RECBLR_ERR_UNSUPPORTED;
+    if (N * ((V + 2047) / 2048) >= kMaxGroups) return RECBLR_ERR_UNSUPPORTED;
+    return RECBLR_OK;
+}
+
+size_t recblr_policy_loss_workspace_size(int64_t N, int64_t V, int io) {
+    if (policy_sizes(N, V, io) != RECBLR_OK) return 0;
+    return policy_workspace(N, V, io_of(io));
+}
+
+int recblr_policy_loss(const void* logits, const int32_t* ids, const float* old_logp,
+                       const float* advantage, const float* ref_logp, const float* weight,
+                       float* loss, float* logp, void* dlogits, int64_t N, int64_t V,
+                       float temperature, float clip_low, float clip_high, float kl, int io,
+                       void* ws, size_t ws_bytes, void* stream) {
+    int st = policy_sizes(N, V, io);
+    if (st) return st;
+    if (!(temperature >= 1e-30f && temperature <= 1e30f)) return RECBLR_ERR_INVALID_ARGUMENT;
+    for (float x : {clip_low, clip_high, kl})
+        if (!(x >= 0.0f && x <= 3.0e38f)) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!loss || !aligned(loss, 4)) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (N > 0 && (!logits || !ids || !old_logp || !advantage || (kl > 0.0f && !ref_logp)))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!aligned(logits, esz(io)) || !aligned(dlogits, esz(io)))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    for (const void* p : {(const void*)ids, (const void*)old_logp, (const void*)advantage,
+                          (const void*)ref_logp, (const void*)weight, (const void*)logp})
+        if (!aligned(p, 4)) return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t n = (size_t)(N * V) * esz(io), s = (size_t)N * 4;
+    // dlogits may be logits exactly.
+    if (dlogits != logits && overlaps({dlogits, n}, {logits, n}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    if (!disjoint({{dlogits, n}, {loss, 4}, {logp, s}},
+                  {{ids, s}, {old_logp, s}, {advantage, s}, {ref_logp, s}, {weight, s}}) ||
+        !disjoint({{loss, 4}, {logp, s}}, {{logits, n}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const size_t need = policy_workspace(N, V, io_of(io));
+    st = check_ws(ws, ws_bytes, need);
+    if (st) return st;
+    if (!disjoint({{ws, need}}, {{logits, n}, {dlogits, n}, {loss, 4}, {logp, s}, {ids, s},
+                                 {old_logp, s}, {advantage, s}, {ref_logp, s}, {weight, s}}))
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    const PolicyArgs a{logits, ids, old_logp, advantage, kl > 0.0f ? ref_logp : nullptr, weight,
+                       loss, logp, dlogits, N, V, temperature, clip_low, clip_high, kl,
+                       io_of(io)};
+    return status_of(launch_policy_loss(a, ws, (hipStream_t)stream));
+}
+
+// ------------------------------------------------------------------ Muon
+
+static int muon_sizes(const recblr_muon_tensor* tensors, int64_t count, int io) {
+    if (io != RECBLR_F32 && io != RECBLR_BF16) return RECBLR_ERR_UNSUPPORTED;
+    if (count < 0 || (count > 0 && !tensors)) return RECBLR_ERR_INVALID_ARGUMENT;
+    if (count > ((int64_t)1 << 20)) return RECBLR_ERR_UNSUPPORTED;
+    for (int64_t i = 0; i < count; ++i)
+        if (tensors[i].rows < 0 || tensors[i].cols < 0) return RECBLR_ERR_INVALID_ARGUMENT;
+    constexpr int64_t kSide = (int64_t)1 << 16, kSize = (int64_t)1 << 30;
+    for (int64_t i = 0; i < count; ++i) {
+        const recblr_muon_tensor& t = tensors[i];
+        if (t.rows > kSide || t.cols > kSide || t.rows * t.cols > kSize)
+            return RECBLR_ERR_UNSUPPORTED;
+    }
+    return RECBLR_OK;
+}
+
+size_t recblr_muon_workspace_size(const recblr_muon_tensor* tensors, int64_t count, int io) {
+    if (muon_sizes(tensors, count, io) != RECBLR_OK) return 0;
+    return muon_workspace(tensors, count);
+}
+
+int recblr_muon_update(const recblr_muon_tensor* tensors, int64_t count, int io, double lr,
+                       double momentum, int nesterov, int steps, double eps, void* ws,
+                       size_t ws_bytes, void* stream) {
+    int st = muon_sizes(tensors, count, io);
+    if (st) return st;
+    if (!(momentum >= 0.0 && momentum < 1.0) || !(eps > 0.0) || steps < 1)
+        return RECBLR_ERR_INVALID_ARGUMENT;
+    if (steps > 64) return RECBLR_ERR_UNSUPPORTED;
+    if (count == 0) return RECBLR_OK;
+    const size_t e = esz(io);
+    Ranges ranges(count + 1);
+    if (!ranges.r) return RECBLR_ERR_INVALID_ARGUMENT;
+    for (int kind = 0; kind < 3; ++kind)
+        for (int64_t i = 0; i < count; ++i) {
+            const recblr_muon_tensor& t = tensors[i];
+            const size_t n = (size_t)(t.rows * t.cols);
+            if (n == 0) continue;
+            const void* p = kind == 0 ? t.param : kind == 1 ? t.grad : (const void*)t.m;
+            const size_t each = kind < 2 ? e : 4;
+            if (!p || !aligned(p, each)) return RECBLR_ERR_INVALID_ARGUMENT;
+            ranges.add(p, n * each, kind != 1);
+        }
+    const size_t need = muon_workspace(tensors, count);
+    st = check_ws(ws, ws_bytes, need);
+    if (st) return st;
+    if (need) ranges.add(ws, need, true);
+    if (!ranges.disjoint()) return RECBLR_ERR_INVALID_ARGUMENT;
+    const MuonHyper h{lr, momentum, eps, nesterov != 0, steps};
+    return status_of(launch_muon(tensors, count, io_of(io), h, ws, (hipStream_t)stream));
+}
+
 }  // extern "C"

@@ -1,4 +1,5 @@
-// Launchers behind recblr_ops.h (AdamW, sampling, gated delta rule): internal
+// Launchers behind recblr_ops.h (AdamW, sampling, gated delta rule, item lookup, norms of queries
+// and keys, policy loss, Muon): internal
 // to librecblr.so, called by capi_ops.cpp after it has checked the arguments.
 // Each enqueues on `stream` and returns the launch's status.
 #pragma once
@@ -106,6 +107,68 @@ hipError_t launch_delta_split_forward(const DeltaFwdArgs& a, void* ws, size_t* b
                                       hipStream_t stream);
 hipError_t launch_delta_split_backward(const DeltaBwdArgs& a, float* D, float* Y, void* ws,
                                        size_t* bytes, hipStream_t stream);
+
+// ------------------------------------------------------------------ item lookup
+struct EmbedArgs {
+    const int32_t* ids;
+    const void* src;  // the table, or dout
+    void* dst;        // out, or dtable
+    int64_t N, V, D;
+    float scale;
+    int32_t pad_id;
+    bool accumulate;
+    IoType io;
+};
+size_t embed_workspace(int64_t N, int64_t V, int64_t D, IoType io);
+hipError_t launch_embed_forward(const EmbedArgs& a, hipStream_t stream);
+hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t stream);
+
+// ------------------------------------------------------------------ norms of queries and keys
+struct QkNormArgs {
+    const void* x[2];  // q, k
+    int64_t pitch[2];
+    const float* w[2];         // may be null
+    const int32_t* positions;  // null where rotate = 0
+    const void* dy[2];         // backward
+    void* out[2];              // y, or dx
+    float* dw[2];              // backward, where w is given
+    int64_t N;
+    int heads[2], D, rotate;
+    double base;
+    float share, eps;  // share: 1, or 1 / D
+    IoType io;
+};
+size_t qk_norm_workspace(int64_t N, int H, int HK, int D, IoType io);
+hipError_t launch_qk_norm_forward(const QkNormArgs& a, hipStream_t stream);
+hipError_t launch_qk_norm_backward(const QkNormArgs& a, void* ws, hipStream_t stream);
+
+// ------------------------------------------------------------------ policy loss
+struct PolicyArgs {
+    const void* logits;
+    const int32_t* ids;
+    const float* old_logp;
+    const float* advantage;
+    const float* ref_logp;  // null where kl = 0
+    const float* weight;    // may be null
+    float* loss;
+    float* logp;    // may be null
+    void* dlogits;  // may be null, or logits
+    int64_t N, V;
+    float temperature, clip_low, clip_high, kl;
+    IoType io;
+};
+size_t policy_workspace(int64_t N, int64_t V, IoType io);
+hipError_t launch_policy_loss(const PolicyArgs& a, void* ws, hipStream_t stream);
+
+// ------------------------------------------------------------------ Muon
+struct MuonHyper {
+    double lr, momentum, eps;
+    bool nesterov;
+    int steps;
+};
+size_t muon_workspace(const recblr_muon_tensor* tensors, int64_t count);
+hipError_t launch_muon(const recblr_muon_tensor* tensors, int64_t count, IoType io,
+                       const MuonHyper& h, void* ws, hipStream_t stream);
 
 #ifdef __HIPCC__
 __device__ __forceinline__ float delta_clamp_g(float g) { return g < kDeltaMinG ? kDeltaMinG : g; }

@@ -1,0 +1,440 @@
+// Queries and keys of each head, normalised and rotated by their positions, and the gradients
+// (recblr_qk_norm_forward, _backward).
+//
+// Of a head's vector x, with r = 1 / sqrt(s sum x^2 + eps) and u = r x:
+//   y = R (w u);   backward, with g = R^T dy and a = w g:
+//   dx = r (a - s u (u . a)),   dw = sum over tokens and heads of g u.
+// R turns pairs of elements that lie rotate / 2 apart.  An element is read and written once
+// (2 e bytes forward, 3 e backward); u and r are formed again in the backward.
+//
+// A group of lanes takes a token and walks its heads, so that the token's sines and cosines are
+// formed once for all of them.  A lane holds two 16-byte runs of a head that are each other's
+// partners, so turning them needs no exchange; the two sums of a head are moves between lanes.
+// Widths, rotations, pitches or addresses that are no multiples of that take a wave to a token,
+// an element at a time.
+#include <hip/hip_runtime.h>
+
+#include "device_common.hpp"
+#include "lanes.hpp"
+#include "ops.hpp"
+#include "wave_tile.hpp"
+
+namespace recblr {
+namespace {
+
+using wtile::u4v;
+
+constexpr int kNT = 256;
+constexpr int kMaxD = 256;
+
+struct Params {
+    const void* x[2];
+    const void* dy[2];
+    void* out[2];
+    const float* w[2];
+    int64_t pitch[2];  // elements from token to token of x
+    const int32_t* positions;
+    float* part;  // backward with weights: [groups][2][D]
+    int64_t N;
+    int heads[2], D, R;
+    float share, eps;
+    // turns per position of each pair, base^(-2 i / R) / 2 pi
+    double rate[kMaxD / 2];
+};
+
+// sin and cos of `turns` full turns: whole turns are taken off in 64 bits, so what is left of a
+// far position's angle is exact to fp32.
+__device__ __forceinline__ void turn(double turns, float& sn, float& cs) {
+    const float half_turns = 2.0f * (float)(turns - rint(turns));
+    sincospif(half_turns, &sn, &cs);
+}
+
+template <typename T>
+struct Eight;  // 16 bytes as floats
+template <>
+struct Eight<float> {
+    static constexpr int VE = 4;
+    __device__ __forceinline__ static void get(u4v v, float (&o)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __uint_as_float(v[e]);
+    }
+    __device__ __forceinline__ static u4v put(const float (&o)[4]) {
+        u4v v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(o[e]);
+        return v;
+    }
+};
+template <>
+struct Eight<bf16> {
+    static constexpr int VE = 8;
+    __device__ __forceinline__ static void get(u4v v, float (&o)[8]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            o[2 * e] = bf16_lo(v[e]);
+            o[2 * e + 1] = bf16_hi(v[e]);
+        }
+    }
+    __device__ __forceinline__ static u4v put(const float (&o)[8]) {
+        u4v v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = bf16_pair(o[2 * e], o[2 * e + 1]);
+        return v;
+    }
+};
+
+// Sum over the G lanes of a group (a power of two up to 32), in all of them.
+template <int G>
+__device__ __forceinline__ float group_sum(float v, int lane) {
+    if constexpr (G >= 2) v += lanes::dpp<0xB1, 0xF>(v, 0.0f);   // lanes 1, 0, 3, 2
+    if constexpr (G >= 4) v += lanes::dpp<0x4E, 0xF>(v, 0.0f);   // 2, 3, 0, 1
+    if constexpr (G >= 8) v += lanes::dpp<0x141, 0xF>(v, 0.0f);  // eight in reverse
+    if constexpr (G >= 16) v += lanes::dpp<0x140, 0xF>(v, 0.0f);  // sixteen in reverse
+    if constexpr (G >= 32) v += wtile::row_partner(v, (lane >> 4) & 1);
+    return v;
+}
+
+// Where a lane's two runs of a head lie.  Lanes of the rotated part hold elements i .. and
+// i + R / 2 .., the others two runs behind one another.
+template <int VE>
+struct Place {
+    int a, b;
+    bool turned, some;
+    __device__ __forceinline__ Place(int l, int D, int R) {
+        some = l * 2 * VE < D;
+        turned = l * 2 * VE < R;
+        a = turned ? l * VE : l * 2 * VE;
+        b = turned ? a + R / 2 : a + VE;
+    }
+};
+
+// (a, b) turned by the angle, or back with -sn.
+template <int VE>
+__device__ __forceinline__ void rotate(float (&a)[VE], float (&b)[VE], const float (&sn)[VE],
+                                       const float (&cs)[VE], float sign) {
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+        const float s = sign * sn[e], x = a[e], y = b[e];
+        a[e] = fmaf(x, cs[e], -y * s);
+        b[e] = fmaf(y, cs[e], x * s);
+    }
+}
+
+// kDW: 0 forward, 1 backward, 2 backward with the weights' gradients.
+template <typename T, int G, int kMode>
+__global__ __launch_bounds__(kNT) void head_kernel(Params p) {
+    using E = Eight<T>;
+    constexpr int VE = E::VE, kGroups = kNT / G;
+    const int t = threadIdx.x, lane = t & 63, l = t % G;
+    const Place<VE> at(l, p.D, p.R);
+    const u4v zero = {0, 0, 0, 0};
+    float w[2][2][VE];
+    float dw[2][2][VE];
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+            w[s][0][e] = at.some && p.w[s] ? p.w[s][at.a + e] : 1.0f;
+            w[s][1][e] = at.some && p.w[s] ? p.w[s][at.b + e] : 1.0f;
+            dw[s][0][e] = dw[s][1][e] = 0.0f;
+        }
+    double rate[VE];
+#pragma unroll
+    for (int e = 0; e < VE; ++e) rate[e] = at.turned ? p.rate[at.a + e] : 0.0;
+    for (int64_t n = (int64_t)blockIdx.x * kGroups + t / G; n < p.N;
+         n += (int64_t)gridDim.x * kGroups) {
+        float sn[VE], cs[VE];
+        const double pos = p.R ? (double)p.positions[n] : 0.0;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) turn(pos * rate[e], sn[e], cs[e]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const T* x = (const T*)p.x[s] + n * p.pitch[s];
+            const int64_t row = n * p.heads[s];
+            for (int h = 0; h < p.heads[s]; ++h) {
+                const int64_t o = (row + h) * p.D;
+                u4v ra = zero, rb = zero, da = zero, db = zero;
+                if (at.some) {
+                    ra = *(const u4v*)(x + h * p.D + at.a);
+                    rb = *(const u4v*)(x + h * p.D + at.b);
+                    if constexpr (kMode > 0) {
+                        da = *(const u4v*)((const T*)p.dy[s] + o + at.a);
+                        db = *(const u4v*)((const T*)p.dy[s] + o + at.b);
+                    }
+                }
+                float a[VE], b[VE];
+                E::get(ra, a);
+                E::get(rb, b);
+                float q = 0.0f;
+#pragma unroll
+                for (int e = 0; e < VE; ++e) q = fmaf(a[e], a[e], fmaf(b[e], b[e], q));
+                const float r = 1.0f / sqrtf(fmaf(group_sum<G>(q, lane), p.share, p.eps));
+                if constexpr (kMode == 0) {
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        a[e] *= r * w[s][0][e];
+                        b[e] *= r * w[s][1][e];
+                    }
+                    if (at.turned) rotate(a, b, sn, cs, 1.0f);
+                } else {
+                    float ga[VE], gb[VE];
+                    E::get(da, ga);
+                    E::get(db, gb);
+                    if (at.turned) rotate(ga, gb, sn, cs, -1.0f);
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        a[e] *= r;
+                        b[e] *= r;
+                        if constexpr (kMode == 2) {
+                            dw[s][0][e] = fmaf(ga[e], a[e], dw[s][0][e]);
+                            dw[s][1][e] = fmaf(gb[e], b[e], dw[s][1][e]);
+                        }
+                        ga[e] *= w[s][0][e];
+                        gb[e] *= w[s][1][e];
+                        dot = fmaf(ga[e], a[e], fmaf(gb[e], b[e], dot));
+                    }
+                    dot = group_sum<G>(dot, lane) * p.share;
+#pragma unroll
+                    for (int e = 0; e < VE; ++e) {
+                        a[e] = r * fmaf(-dot, a[e], ga[e]);
+                        b[e] = r * fmaf(-dot, b[e], gb[e]);
+                    }
+                }
+                if (at.some) {
+                    *(u4v*)((T*)p.out[s] + o + at.a) = E::put(a);
+                    *(u4v*)((T*)p.out[s] + o + at.b) = E::put(b);
+                }
+            }
+        }
+    }
+    if constexpr (kMode == 2) {
+        // The groups' sums, in their order.
+        __shared__ float all[kNT][VE + 1];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < VE; ++e) all[t][e] = dw[s][half][e];
+                __syncthreads();
+                for (int i = t; i < G * VE; i += kNT) {
+                    const int li = i / VE, e = i % VE;
+                    const Place<VE> to(li, p.D, p.R);
+                    if (!to.some) continue;
+                    float sum = 0.0f;
+                    for (int g = 0; g < kGroups; ++g) sum += all[g * G + li][e];
+                    p.part[((int64_t)blockIdx.x * 2 + s) * p.D + (half ? to.b : to.a) + e] = sum;
+                }
+            }
+    }
+}
+
+// A wave to a token, element lane + 64 j of a head in its j-th place.
+template <typename T, int kMode>
+__global__ __launch_bounds__(kNT) void any_kernel(Params p) {
+    constexpr int J = kMaxD / kWave;
+    const int lane = threadIdx.x & 63, w0 = wave_id(), half = p.R / 2;
+    float w[2][J], dw[2][J];
+    bool live[J];
+    int mate[J];   // the element's partner
+    float side[J]; // -1 for the first of a pair, 1 for the second, 0 for one that is not turned
+    double rate[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int i = lane + kWave * j;
+        live[j] = i < p.D;
+        const bool turned = i < p.R;
+        side[j] = !turned ? 0.0f : i < half ? -1.0f : 1.0f;
+        mate[j] = !turned ? (live[j] ? i : 0) : i < half ? i + half : i - half;
+        rate[j] = turned ? p.rate[i < half ? i : i - half] : 0.0;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            w[s][j] = live[j] && p.w[s] ? p.w[s][i] : 1.0f;
+            dw[s][j] = 0.0f;
+        }
+    }
+    for (int64_t n = (int64_t)blockIdx.x * 4 + w0; n < p.N; n += (int64_t)gridDim.x * 4) {
+        float sn[J], cs[J];
+        const double pos = p.R ? (double)p.positions[n] : 0.0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) turn(pos * rate[j], sn[j], cs[j]);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            for (int h = 0; h < p.heads[s]; ++h) {
+                const T* x = (const T*)p.x[s] + n * p.pitch[s] + h * p.D;
+                const int64_t o = (n * p.heads[s] + h) * p.D;
+                const T* dy = (const T*)p.dy[s] + o;
+                T* out = (T*)p.out[s] + o;
+                float v[J], q = 0.0f;
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    v[j] = live[j] ? to_f32(x[lane + kWave * j]) : 0.0f;
+                    q = fmaf(v[j], v[j], q);
+                }
+                const float r = 1.0f / sqrtf(fmaf(lanes::wave_sum(q), p.share, p.eps));
+                float y[J];
+                if constexpr (kMode == 0) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const float m = live[j] ? to_f32(x[mate[j]]) : 0.0f;
+                        const float wm = p.w[s] && live[j] ? p.w[s][mate[j]] : 1.0f;
+                        y[j] = v[j] * (r * w[s][j]);
+                        if (side[j] != 0.0f)
+                            y[j] = fmaf(y[j], cs[j], side[j] * (m * (r * wm) * sn[j]));
+                    }
+                } else {
+                    float g[J], dot = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        g[j] = live[j] ? to_f32(dy[lane + kWave * j]) : 0.0f;
+                        const float m = live[j] ? to_f32(dy[mate[j]]) : 0.0f;
+                        if (side[j] != 0.0f) g[j] = fmaf(g[j], cs[j], -side[j] * (m * sn[j]));
+                        v[j] *= r;
+                        if constexpr (kMode == 2) dw[s][j] = fmaf(g[j], v[j], dw[s][j]);
+                        g[j] *= w[s][j];
+                        dot = fmaf(g[j], v[j], dot);
+                    }
+                    dot = lanes::wave_sum(dot) * p.share;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) y[j] = r * fmaf(-dot, v[j], g[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    if (live[j]) out[lane + kWave * j] = from_f32<T>(y[j]);
+            }
+        }
+    }
+    if constexpr (kMode == 2) {
+        __shared__ float all[4][2][kMaxD];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < J; ++j) all[w0][s][lane + kWave * j] = dw[s][j];
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * p.D; i += kNT) {
+            const int s = i >= p.D, e = i - s * p.D;
+            p.part[((int64_t)blockIdx.x * 2 + s) * p.D + e] =
+                ((all[0][s][e] + all[1][s][e]) + all[2][s][e]) + all[3][s][e];
+        }
+    }
+}
+
+// dw: the rows of partial sums, in 64 bits: sixteen runs of rows, then the runs in order.
+__global__ __launch_bounds__(1024) void weights_kernel(const float* part, int rows, int D,
+                                                       float* dwq, float* dwk) {
+    __shared__ double all[16][kWave];
+    const int lane = threadIdx.x & 63, w = wave_id();
+    const int i = blockIdx.x * kWave + lane, cols = 2 * D;
+    const int run = (rows + 15) / 16;
+    double s = 0.0;
+    if (i < cols) {
+        const int end = min(rows, (w + 1) * run);
+#pragma unroll 8
+        for (int r = w * run; r < end; ++r) s += (double)part[(int64_t)r * cols + i];
+    }
+    all[w][lane] = s;
+    __syncthreads();
+    if (w || i >= cols) return;
+    for (int k = 1; k < 16; ++k) s += all[k][lane];
+    float* to = i < D ? dwq : dwk;
+    if (to) to[i < D ? i : i - D] = (float)s;
+}
+
+// ------------------------------------------------------------------ launches
+// Workgroups: as many as there are tokens to take, at most eight to a compute unit; the rows of
+// partial sums four.
+int64_t groups_of(int64_t tokens_each, int64_t N, bool sums) {
+    const int64_t need = (N + tokens_each - 1) / tokens_each, most = sums ? 1024 : 2048;
+    return need < most ? need : most;
+}
+
+// Lanes to a token's heads, where all runs of 16 bytes are aligned; 0: the other kernel.
+int lanes_of(const QkNormArgs& a, bool backward) {
+    const int e = (int)io_bytes(a.io), ve = 16 / e;
+    if (a.D % (2 * ve) || a.rotate % (2 * ve)) return 0;
+    uintptr_t bits = 0;
+    for (int s = 0; s < 2; ++s) {
+        bits |= (uintptr_t)a.x[s] | (uintptr_t)a.out[s] | (uintptr_t)(a.pitch[s] * e);
+        if (backward) bits |= (uintptr_t)a.dy[s];
+    }
+    if (bits & 15u) return 0;
+    int g = 1;
+    while (g * 2 * ve < a.D) g *= 2;
+    return g;
+}
+
+template <typename T, int kMode>
+void launch(const Params& p, int g, unsigned groups, hipStream_t st) {
+    switch (g) {
+        case 0: any_kernel<T, kMode><<<groups, kNT, 0, st>>>(p); break;
+        case 1: head_kernel<T, 1, kMode><<<groups, kNT, 0, st>>>(p); break;
+        case 2: head_kernel<T, 2, kMode><<<groups, kNT, 0, st>>>(p); break;
+        case 4: head_kernel<T, 4, kMode><<<groups, kNT, 0, st>>>(p); break;
+        case 8: head_kernel<T, 8, kMode><<<groups, kNT, 0, st>>>(p); break;
+        case 16: head_kernel<T, 16, kMode><<<groups, kNT, 0, st>>>(p); break;
+        default:
+            if constexpr (sizeof(T) == 4) head_kernel<T, 32, kMode><<<groups, kNT, 0, st>>>(p);
+    }
+}
+
+Params params_of(const QkNormArgs& a) {
+    Params p{};
+    for (int s = 0; s < 2; ++s) {
+        p.x[s] = a.x[s];
+        p.dy[s] = a.dy[s];
+        p.out[s] = a.out[s];
+        p.w[s] = a.w[s];
+        p.pitch[s] = a.pitch[s];
+        p.heads[s] = a.heads[s];
+    }
+    p.positions = a.positions;
+    p.N = a.N;
+    p.D = a.D;
+    p.R = a.rotate;
+    p.share = a.share;
+    p.eps = a.eps;
+    for (int i = 0; i < a.rotate / 2; ++i)
+        p.rate[i] = pow(a.base, -2.0 * i / a.rotate) / 6.283185307179586476925;
+    return p;
+}
+
+}  // namespace
+
+// Rows of partial sums; the fewest tokens to a workgroup are the other kernel's four.
+size_t qk_norm_workspace(int64_t N, int H, int HK, int D, IoType io) {
+    return (size_t)groups_of(4, N, true) * 2 * D * 4;
+}
+
+hipError_t launch_qk_norm_forward(const QkNormArgs& a, hipStream_t st) {
+    const Params p = params_of(a);
+    const int g = lanes_of(a, false);
+    const unsigned groups = (unsigned)groups_of(g ? kNT / g : 4, a.N, false);
+    a.io == IoType::kF32 ? launch<float, 0>(p, g, groups, st) : launch<bf16, 0>(p, g, groups, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_qk_norm_backward(const QkNormArgs& a, void* ws, hipStream_t st) {
+    Params p = params_of(a);
+    const int g = lanes_of(a, true);
+    const bool sums = a.dw[0] || a.dw[1];
+    const unsigned groups = (unsigned)groups_of(g ? kNT / g : 4, a.N, sums);
+    p.part = (float*)ws;
+    if (a.N == 0) {  // no rows to sum
+        if (sums)
+            weights_kernel<<<(unsigned)((2 * a.D + 63) / 64), 1024, 0, st>>>(p.part, 0, a.D,
+                                                                            a.dw[0], a.dw[1]);
+    } else if (sums) {
+        a.io == IoType::kF32 ? launch<float, 2>(p, g, groups, st)
+                             : launch<bf16, 2>(p, g, groups, st);
+        weights_kernel<<<(unsigned)((2 * a.D + 63) / 64), 1024, 0, st>>>(p.part, (int)groups, a.D,
+                                                                        a.dw[0], a.dw[1]);
+    } else {
+        a.io == IoType::kF32 ? launch<float, 1>(p, g, groups, st)
+                             : launch<bf16, 1>(p, g, groups, st);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace recblr

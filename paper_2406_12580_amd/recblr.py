@@ -460,11 +460,15 @@ def adam_update(params, grads, m1, m2, step, lr=1e-3, beta1=0.9, beta2=0.999, ep
 OP_DELTA_FORWARD, OP_DELTA_BACKWARD = 16, 17
 DELTA_CHUNK = 64
 ADAMW_BLOCK = 256
+NORM_L2, NORM_RMS = 0, 1
 
 OPS_EXPORTS = (
     "recblr_delta_workspace_size", "recblr_delta_forward", "recblr_delta_backward",
     "recblr_delta_step", "recblr_adamw_update", "recblr_adamw_moments",
-    "recblr_sample_workspace_size", "recblr_sample",
+    "recblr_sample_workspace_size", "recblr_sample", "recblr_embed_workspace_size",
+    "recblr_embed_forward", "recblr_embed_backward", "recblr_qk_norm_workspace_size",
+    "recblr_qk_norm_forward", "recblr_qk_norm_backward", "recblr_policy_loss_workspace_size",
+    "recblr_policy_loss", "recblr_muon_workspace_size", "recblr_muon_update",
 )
 
 
@@ -474,7 +478,13 @@ class AdamWTensor(ctypes.Structure):
                 ("scale2", _p), ("n", _i64), ("weight_decay", ctypes.c_double)]
 
 
-_d = ctypes.c_double
+class MuonTensor(ctypes.Structure):
+    """recblr_muon_tensor."""
+    _fields_ = [("param", _p), ("grad", _p), ("m", _p), ("rows", _i64), ("cols", _i64),
+                ("weight_decay", ctypes.c_double), ("scale", ctypes.c_double)]
+
+
+_d, _i32 = ctypes.c_double, ctypes.c_int32
 _OPS_SIGS = {
     "recblr_delta_workspace_size": ([_int] + [_i64] * 6 + [_int], _sz),
     "recblr_delta_forward": ([_p] * 9 + [_i64] * 6 + [_f, _int, _p, _sz, _p], _int),
@@ -485,6 +495,19 @@ _OPS_SIGS = {
     "recblr_adamw_moments": ([ctypes.POINTER(AdamWTensor), _i64, _p, _p, _p], _int),
     "recblr_sample_workspace_size": ([_i64, _i64, _int], _sz),
     "recblr_sample": ([_p] * 8 + [_i64, _i64, _int, _p, _sz, _p], _int),
+    "recblr_embed_workspace_size": ([_i64] * 3 + [_int], _sz),
+    "recblr_embed_forward": ([_p] * 3 + [_i64] * 3 + [_f, _i32, _int, _p], _int),
+    "recblr_embed_backward": ([_p] * 3 + [_i64] * 3 + [_f, _i32, _int, _int, _p, _sz, _p], _int),
+    "recblr_qk_norm_workspace_size": ([_i64] * 4 + [_int], _sz),
+    "recblr_qk_norm_forward": ([_p, _p, _i64, _i64] + [_p] * 5 + [_i64] * 5 + [_d, _int, _f, _int,
+                                                                              _p], _int),
+    "recblr_qk_norm_backward": ([_p, _p, _i64, _i64] + [_p] * 9 + [_i64] * 5 + [
+        _d, _int, _f, _int, _p, _sz, _p], _int),
+    "recblr_policy_loss_workspace_size": ([_i64, _i64, _int], _sz),
+    "recblr_policy_loss": ([_p] * 9 + [_i64, _i64, _f, _f, _f, _f, _int, _p, _sz, _p], _int),
+    "recblr_muon_workspace_size": ([ctypes.POINTER(MuonTensor), _i64, _int], _sz),
+    "recblr_muon_update": ([ctypes.POINTER(MuonTensor), _i64, _int, _d, _d, _int, _int, _d, _p,
+                            _sz, _p], _int),
 }
 for _name, (_args, _res) in _OPS_SIGS.items():
     _fn = getattr(_lib, _name)
@@ -803,3 +826,261 @@ def _adamw_moments(opt, out):
     _check(recblr_adamw_moments(opt._table, len(opt._sizes), *ptrs, _stream()),
            "recblr_adamw_moments")
     return out
+
+
+@_on_device
+def embed(table, ids, scale=1.0, pad_id=-1):
+    """Rows of an item table by id: table [V,D], ids int32 of any shape.  Returns
+    scale * table[ids], [*ids.shape,D] of the table's type; rows of pad_id are zeros, those of
+    other ids outside [0, V) NaN."""
+    if table.dim() != 2:
+        raise ValueError("table must be [V, D]")
+    V, D = table.shape
+    io, dt, at = io_code(table.dtype), table.dtype, table.get_device()
+    out = torch.empty((*ids.shape, D), dtype=dt, device=table.device)
+    _check(recblr_embed_forward(
+        _arg(table, (V, D), dt, at, "table"), _arg(ids, ids.shape, torch.int32, at, "ids"),
+        out.data_ptr(), ids.numel(), V, D, scale, pad_id, io, _stream()), "recblr_embed_forward")
+    return out
+
+
+_embed_workspace_size = functools.lru_cache(maxsize=256)(recblr_embed_workspace_size)
+
+
+@_on_device
+def embed_backward(ids, dout, V, scale=1.0, pad_id=-1, into=None):
+    """Gradient of embed's table: ids as given to embed, dout [*ids.shape,D].  Returns
+    [V,D] of dout's type.  With `into`, a gradient of that shape and type that is there already
+    (the prediction layer's, where it shares the table), the rows that ids name are added to in
+    place, and `into` is returned."""
+    if dout.dim() != ids.dim() + 1:
+        raise ValueError("dout must be [*ids.shape, D]")
+    D, N = dout.shape[-1], ids.numel()
+    io, dt, at = io_code(dout.dtype), dout.dtype, ids.get_device()
+    dtable = torch.empty((V, D), dtype=dt, device=ids.device) if into is None else into
+    n = _embed_workspace_size(N, V, D, io)
+    ws = torch.empty(n, dtype=torch.uint8, device=ids.device) if n else None
+    _check(recblr_embed_backward(
+        _arg(ids, ids.shape, torch.int32, at, "ids"),
+        _arg(dout, (*ids.shape, D), dt, at, "dout"), _arg(dtable, (V, D), dt, at, "into"), N, V, D,
+        scale, pad_id, into is not None, io, ws.data_ptr() if n else None, n, _stream()),
+        "recblr_embed_backward")
+    return dtable
+
+
+def _tokens(t, dtype, index, name):
+    """The address of [..., heads, D], dense but for the distance between tokens, and that
+    distance in elements."""
+    if t.dim() < 3 or t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype} of shape [..., heads, D]")
+    if t.get_device() != index or index < 0:
+        raise ValueError(f"{name} must live on the GPU, with the other tensors")
+    H, D = t.shape[-2:]
+    if t.is_contiguous():
+        return t.data_ptr(), H * D
+    ok = (D == 1 or t.stride(-1) == 1) and (H == 1 or t.stride(-2) == D)
+    pitch, count = None, 1  # tokens behind one another at one distance
+    for size, stride in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+        if size != 1:
+            pitch = stride if pitch is None else pitch
+            ok = ok and stride == pitch * count
+        count *= size
+    if not ok or (pitch is not None and pitch < H * D):
+        raise ValueError(f"{name}: heads must be dense and tokens lie at one distance")
+    return t.data_ptr(), H * D if pitch is None else pitch
+
+
+def _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps):
+    """The arguments that qk_norm and qk_norm_backward share, as two lists around the outputs."""
+    dt, at, f32 = q.dtype, q.get_device(), torch.float32
+    io = io_code(dt)
+    if q.dim() < 3 or q.shape[:-2] != k.shape[:-2] or q.shape[-1] != k.shape[-1]:
+        raise ValueError("q and k must be [..., heads, D] with the same tokens and width")
+    lead, (H, D), HK = q.shape[:-2], q.shape[-2:], k.shape[-2]
+    if norm not in ("l2", "rms"):
+        raise ValueError('norm must be "l2" or "rms"')
+    rotate = D // 2 * 2 if rotate is None else rotate
+    if rotate and positions is None:
+        if len(lead) != 2:
+            raise ValueError("positions are needed unless q is [B, L, H, D]")
+        positions = torch.arange(lead[1], dtype=torch.int32, device=q.device).repeat(lead[0])
+        positions = positions.view(lead)
+    (qp, q_pitch), (kp, k_pitch) = _tokens(q, dt, at, "q"), _tokens(k, dt, at, "k")
+    before = (qp, kp, q_pitch, k_pitch, _arg(wq, (D,), f32, at, "wq"),
+              _arg(wk, (D,), f32, at, "wk"),
+              _arg(positions, lead, torch.int32, at, "positions") if rotate else None)
+    N = lead.numel()
+    after = (N, H, HK, D, rotate, base, NORM_RMS if norm == "rms" else NORM_L2, eps, io)
+    return before, after, positions
+
+
+@_on_device
+def qk_norm(q, k, wq=None, wk=None, positions=None, rotate=None, base=10000.0, norm="rms",
+            eps=1e-6):
+    """Queries and keys of each head normalised and rotated by their positions: q [...,H,D],
+    k [...,HK,D] (parts of one projection's output may be given as views of it), weights wq, wk
+    [D] float32 or None, positions int32 of q's leading shape (None: 0 .. L - 1 of q [B,L,H,D]).
+    norm is "rms" or "l2" (length one, as the gated delta rule takes them); of each head the first
+    `rotate` elements are turned (None: all of an even width; 0: none).  Returns (q, k), dense."""
+    before, after, _keep = _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps)
+    qn = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    kn = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    _check(recblr_qk_norm_forward(*before, qn.data_ptr(), kn.data_ptr(), *after, _stream()),
+           "recblr_qk_norm_forward")
+    return qn, kn
+
+
+_qk_norm_workspace_size = functools.lru_cache(maxsize=256)(recblr_qk_norm_workspace_size)
+
+
+@_on_device
+def qk_norm_backward(q, k, dqn, dkn, wq=None, wk=None, positions=None, rotate=None, base=10000.0,
+                     norm="rms", eps=1e-6):
+    """Backward of qk_norm: q, k and the other arguments as given to it, dqn and dkn the gradients
+    of its outputs.  Returns a dict with dq, dk (dense) and dwq, dwk float32 (None without
+    weights)."""
+    before, after, _keep = _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps)
+    dt, at, dev, D = q.dtype, q.get_device(), q.device, q.shape[-1]
+    out = {"dq": torch.empty(q.shape, dtype=dt, device=dev),
+           "dk": torch.empty(k.shape, dtype=dt, device=dev),
+           "dwq": None if wq is None else torch.empty(D, dtype=torch.float32, device=dev),
+           "dwk": None if wk is None else torch.empty(D, dtype=torch.float32, device=dev)}
+    n = 0
+    if wq is not None or wk is not None:
+        n = _qk_norm_workspace_size(*after[:4], after[-1])
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _check(recblr_qk_norm_backward(
+        *before, _arg(dqn, q.shape, dt, at, "dqn"), _arg(dkn, k.shape, dt, at, "dkn"),
+        *(None if t is None else t.data_ptr() for t in out.values()), *after,
+        ws.data_ptr() if n else None, n, _stream()), "recblr_qk_norm_backward")
+    return out
+
+
+_policy_workspace_size = functools.lru_cache(maxsize=256)(recblr_policy_loss_workspace_size)
+
+
+@_on_device
+def policy_loss(logits, ids, old_logp, advantage, ref_logp=None, weight=None, temperature=1.0,
+                clip_low=0.2, clip_high=0.2, kl=0.0, need_grad=True, out=None):
+    """Clipped policy loss with a KL term over rows of logits [N,V], and its gradient.
+
+    ids [N] int32 are the chosen items (`sample` gives them; rows with a negative one are left
+    out), old_logp, advantage [N] float32 what the policy that chose them gave and what came of
+    it, ref_logp [N] float32 a frozen policy's (needed for kl > 0), weight [N] float32 the rows'
+    weights (None: ones; 1/N each makes the loss a mean).  Returns (loss [1] float32, logp [N]
+    float32, dlogits); dlogits (None unless need_grad) goes to `out` where given, which may be
+    logits."""
+    if logits.dim() != 2:
+        raise ValueError("logits must be [N, V]")
+    if kl > 0 and ref_logp is None:
+        raise ValueError("kl > 0 needs ref_logp")
+    N, V = logits.shape
+    io, dt, dev, at, f32 = io_code(logits.dtype), logits.dtype, logits.device,         logits.get_device(), torch.float32
+    loss = torch.empty(1, dtype=f32, device=dev)
+    logp = torch.empty(N, dtype=f32, device=dev)
+    if out is None and need_grad:
+        out = torch.empty_like(logits)
+    n = _policy_workspace_size(N, V, io)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    _check(recblr_policy_loss(
+        _arg(logits, (N, V), dt, at, "logits"), _arg(ids, (N,), torch.int32, at, "ids"),
+        _arg(old_logp, (N,), f32, at, "old_logp"), _arg(advantage, (N,), f32, at, "advantage"),
+        _arg(ref_logp, (N,), f32, at, "ref_logp"), _arg(weight, (N,), f32, at, "weight"),
+        loss.data_ptr(), logp.data_ptr(), _arg(out, (N, V), dt, at, "out"), N, V, temperature,
+        clip_low, clip_high, kl, io, ws.data_ptr() if n else None, n, _stream()),
+        "recblr_policy_loss")
+    return loss, logp, out
+
+
+class Muon:
+    """Muon over a list of matrices (2-D tensors, float32 or bfloat16, all of one type and
+    device): momentum whose update is brought near the closest orthogonal matrix by `steps`
+    Newton-Schulz steps.
+
+    weight_decay is one number or one for each matrix; scale multiplies the update, one number,
+    one for each matrix, or None for sqrt(max(1, rows / columns)).  `state` takes over momenta
+    that exist, float32 tensors with as many elements as the matrices.  step(grads) updates
+    matrices and momenta in place, on the matrices' device; gradients have the matrices' type and
+    shape.  The lists and their tensors may be given other memory of the same type and size
+    between two calls.  A captured step replays with the rates and addresses of its capture, and
+    in the workspace that the capture's memory pool gave it."""
+
+    def __init__(self, params, lr=0.02, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5,
+                 eps=1e-7, scale=None, state=None):
+        self.params = list(params)
+        if not self.params:
+            raise ValueError("no parameters")
+        first = self.params[0]
+        self.dtype, self.device = first.dtype, first.device
+        if not first.is_cuda:
+            raise ValueError("tensors must live on the GPU")
+        if any(p.dim() != 2 for p in self.params):
+            raise ValueError("parameters must be matrices")
+        self._io = io_code(self.dtype)
+        self.lr, self.momentum, self.nesterov = lr, momentum, nesterov
+        self.steps, self.eps = steps, eps
+        self._shapes = [p.shape for p in self.params]
+        sizes = [p.numel() for p in self.params]
+        each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * len(sizes)  # noqa: E731
+        decay = each(weight_decay)
+        scale = [max(1.0, r / c) ** 0.5 if c else 1.0 for r, c in self._shapes]             if scale is None else each(scale)
+        if len(decay) != len(sizes) or len(scale) != len(sizes):
+            raise ValueError("weight_decay and scale must be numbers or one for each parameter")
+        if state is None:
+            state = [torch.zeros(s, dtype=torch.float32, device=self.device)
+                     for s in self._shapes]
+        self.m = list(state)
+        self._table = (MuonTensor * len(sizes))()
+        for entry, (r, c), w, s in zip(self._table, self._shapes, decay, scale):
+            entry.rows, entry.cols, entry.weight_decay, entry.scale = r, c, w, s
+        self._sizes = sizes
+        self._fill()
+        table = np.frombuffer(self._table, dtype=np.uint64).reshape(len(sizes), -1)
+        self._grads = table[:, MuonTensor.grad.offset // 8]
+        self._ws_bytes = recblr_muon_workspace_size(self._table, len(sizes), self._io)
+
+    def _flat(self, t, dtype, shape, name):
+        if t.dtype != dtype or t.numel() != shape.numel() or (name != "state" and
+                                                              t.shape != shape):
+            raise ValueError(f"{name}: a tensor must be {dtype} of shape {tuple(shape)}")
+        if t.device != self.device or not t.is_cuda or not t.is_contiguous():
+            raise ValueError(f"{name}: tensors must be contiguous, on the parameters' GPU")
+        return t.data_ptr()
+
+    def _addresses(self):
+        return list(map(_data_ptr, self.params)), list(map(_data_ptr, self.m))
+
+    def _fill(self):
+        if len(self.params) != len(self._shapes) or len(self.m) != len(self._shapes):
+            raise ValueError("state: one tensor for each parameter is needed")
+        found = ([self._flat(t, self.dtype, s, "params")
+                  for t, s in zip(self.params, self._shapes)],
+                 [self._flat(t, torch.float32, s, "state") for t, s in zip(self.m, self._shapes)])
+        for entry, p, m in zip(self._table, *found):
+            entry.param, entry.m = p, m
+        # Momenta's memory stays theirs for as long as the table names it (see AdamW).
+        self._held, self._at = [t.detach() for t in self.m], found
+
+    def step(self, grads, lr=None, stream=None):
+        """One update with grads, a tensor for each matrix; lr overrides the rate."""
+        if len(grads) != len(self._sizes):
+            raise ValueError("grads: one tensor for each parameter is needed")
+        if not ([g.shape for g in grads] == self._shapes and all(map(_is_contiguous, grads))
+                and set(map(_get_device, grads)) == {self.device.index}
+                and set(map(_dtype, grads)) == {self.dtype}):
+            for t, s in zip(grads, self._shapes):
+                self._flat(t, self.dtype, s, "grads")  # says what is wrong
+        self._grads[:] = list(map(_data_ptr, grads))
+        if not (self._addresses() == self._at and [p.shape for p in self.params] == self._shapes
+                and all(map(_is_contiguous, self.params))):
+            self._fill()
+        _muon_step(self, self.lr if lr is None else lr, stream=stream)
+
+
+@_on_device
+def _muon_step(opt, lr):
+    n = opt._ws_bytes
+    ws = torch.empty(n, dtype=torch.uint8, device=opt.device) if n else None
+    _check(recblr_muon_update(opt._table, len(opt._sizes), opt._io, lr, opt.momentum,
+                              opt.nesterov, opt.steps, opt.eps, ws.data_ptr() if n else None, n,
+                              _stream()), "recblr_muon_update")
