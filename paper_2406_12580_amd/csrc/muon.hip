@@ -21,6 +21,10 @@
 // Larger ones: planes in the workspace, a launch a product over all matrices of the list.
 #include <hip/hip_runtime.h>
 
+#include <stdlib.h>
+
+#include <algorithm>
+
 #include "device_common.hpp"
 #include "lanes.hpp"
 #include "ops.hpp"
@@ -49,15 +53,18 @@ struct Hyper {
 __device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
-// The product of two operands of two fp16 numbers each, the small terms first.
-__device__ __forceinline__ f16v mma(const h8 (&a)[2], const h8 (&b)[2], f16v c) {
-    c = mfma(a[0], b[1], c);
-    c = mfma(a[1], b[0], c);
-    return mfma(a[0], b[0], c);
-}
-__device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
-    hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
+// hi = fp16(v), lo = fp16(v - hi), of N values.
+template <typename V, int N>
+__device__ __forceinline__ void split(const float (&v)[N], V& hi, V& lo) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {  // two to a conversion
+        const h2 h = __builtin_convertvector(f2{v[e], v[e + 1]}, h2);
+        const h2 l = __builtin_convertvector(f2{v[e] - (float)h[0], v[e + 1] - (float)h[1]}, h2);
+        hi[e] = h[0], hi[e + 1] = h[1];
+        lo[e] = l[0], lo[e + 1] = l[1];
+    }
 }
 
 // Momentum and update of an element: the one place where both are formed.
@@ -68,8 +75,13 @@ __device__ __forceinline__ float update_of(const Hyper& h, float m, float g) {
     return h.nesterov ? fmaf(h.mu, m, h.one_mu * g) : m;
 }
 
+// Whether four elements of type T and of float from a multiple of four on are one access.
+__device__ __forceinline__ bool takes_vectors(const void* g, size_t e, const void* m) {
+    return (((uintptr_t)g & (4 * e - 1)) | ((uintptr_t)m & 15)) == 0;
+}
+
 // ------------------------------------------------------------------ small matrices
-constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / kWave;
+constexpr int kSmallThreads = 512, kSmallWaves = kSmallThreads / kWave;
 constexpr int kSmallLds = 150 * 1024;
 constexpr int kMaxSmall = 72;
 
@@ -88,47 +100,163 @@ struct SmallTable {
 };
 static_assert(sizeof(SmallTable) <= 3800, "kernel arguments end at 4 KB");
 
-// Planes in LDS: rows of `width` elements, 8 more to keep rows off each other's banks.
+// Planes in LDS, high and low: rows of `width` elements, 8 more to keep rows off each other's
+// banks.
 __host__ __device__ inline int small_stride(int width) { return width + 8; }
 size_t small_lds(int mp, int np) {
     return (size_t)4 * mp * (small_stride(np) + small_stride(mp));
 }
 
-// k from k0 on of operand row `row`, both planes.
-__device__ __forceinline__ void row_operand(h8 (&o)[2], const _Float16* m, int plane, int stride,
-                                            int row, int k) {
-    o[0] = *(const h8*)(m + row * stride + k);
-    o[1] = *(const h8*)(m + plane + row * stride + k);
-}
-// The same of the transposed: operand row = column col0 + lane % 32.
-__device__ __forceinline__ void col_operand(h8 (&o)[2], const _Float16* m, int plane, int stride,
-                                            int k0, int col0, int lane) {
-    const _Float16* p = m + (k0 + 8 * (lane >> 5) + ((lane & 15) >> 2)) * stride + col0 +
-                        16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-    o[0] = __builtin_bit_cast(h8, wtile::tr_pair((const char*)p, (const char*)(p + 4 * stride)));
-    p += plane;
-    o[1] = __builtin_bit_cast(h8, wtile::tr_pair((const char*)p, (const char*)(p + 4 * stride)));
-}
-// Accumulators of tile (i0, j0), times kUp over their scale, as rows j of a matrix (i runs
-// along them): four values at a time.
-__device__ __forceinline__ void put_tile(_Float16* m, int plane, int stride, int i0, int j0,
-                                         const float (&v)[16], int lane) {
-    _Float16* p = m + (j0 + (lane & 31)) * stride + i0 + 4 * (lane >> 5);
+// Operands of a wave's product of 64 x 32 by 16 of the contraction, from k on: p of rows (or, of
+// the transposed, columns) i0 .. + 63 of one matrix, q of rows j0 .. + 31 of the other.
+struct SmallFrags {
+    h8 p[2][2], q[2];
+    __device__ __forceinline__ static void row(h8 (&o)[2], const _Float16* m, int plane,
+                                               int stride, int row0, int k, int lane) {
+        const _Float16* a = m + (row0 + (lane & 31)) * stride + k + 8 * (lane >> 5);
+        o[0] = *(const h8*)a;
+        o[1] = *(const h8*)(a + plane);
+    }
+    __device__ __forceinline__ static void col(h8 (&o)[2], const _Float16* m, int plane,
+                                               int stride, int col0, int k, int lane) {
+        const _Float16* a = m + (k + 8 * (lane >> 5) + ((lane & 15) >> 2)) * stride + col0 +
+                            16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        h4 hi, lo;
+        for (int pl = 0; pl < 2; ++pl, a += plane)
+            o[pl] = __builtin_bit_cast(
+                h8, wtile::tr_pair((const char*)a, (const char*)(a + 4 * stride)));
+    }
+    template <bool kTurned>
+    __device__ __forceinline__ void read(const _Float16* P, int pplane, int pstride, int i0,
+                                         bool both, const _Float16* Q, int qplane, int qstride,
+                                         int j0, int k, int lane) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            _Float16 a, b;
-            split(v[4 * q + e] * kUp, a, b);
-            hi[e] = a;
-            lo[e] = b;
-        }
-        *(h4*)(p + 8 * q) = hi;
-        *(h4*)(p + plane + 8 * q) = lo;
+        for (int f = 0; f < 2; ++f)
+            if (f == 0 || both) {
+                if constexpr (kTurned) col(p[f], P, pplane, pstride, i0 + 32 * f, k, lane);
+                else row(p[f], P, pplane, pstride, i0 + 32 * f, k, lane);
+            }
+        row(q, Q, qplane, qstride, j0, k, lane);
+    }
+    __device__ __forceinline__ void multiply(f16v (&acc)[2], bool both) const {
+        acc[0] = mfma(p[0][0], q[1], acc[0]);
+        if (both) acc[1] = mfma(p[1][0], q[1], acc[1]);
+        acc[0] = mfma(p[0][1], q[0], acc[0]);
+        if (both) acc[1] = mfma(p[1][1], q[0], acc[1]);
+        acc[0] = mfma(p[0][0], q[0], acc[0]);
+        if (both) acc[1] = mfma(p[1][0], q[0], acc[1]);
+    }
+};
+// acc = sum over K (a multiple of 32) of p q; operands are read one step ahead.
+template <bool kTurned>
+__device__ __forceinline__ void small_product(f16v (&acc)[2], const _Float16* P, int pplane,
+                                              int pstride, int i0, bool both, const _Float16* Q,
+                                              int qplane, int qstride, int j0, int K, int lane) {
+    acc[0] = acc[1] = f16v{};
+    SmallFrags a, b;
+    auto read = [&](SmallFrags& f, int k) {
+        f.read<kTurned>(P, pplane, pstride, i0, both, Q, qplane, qstride, j0, k, lane);
+    };
+    read(a, 0);
+    for (int k = 0; k < K; k += 32) {
+        read(b, k + 16);
+        __builtin_amdgcn_sched_barrier(0);
+        a.multiply(acc, both);
+        read(a, k + 32 < K ? k + 32 : 0);
+        __builtin_amdgcn_sched_barrier(0);
+        b.multiply(acc, both);
     }
 }
+// Accumulators of 64 x 32 from (i0, j0) on, as rows j of a matrix (i runs along them).
+__device__ __forceinline__ void put_tile(_Float16* m, int plane, int stride, int i0, int j0,
+                                         const float (&v)[2][16], bool both, int lane) {
+    _Float16* p = m + (j0 + (lane & 31)) * stride + i0 + 4 * (lane >> 5);
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+        if (f == 0 || both)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float x[4] = {v[f][4 * q], v[f][4 * q + 1], v[f][4 * q + 2],
+                                    v[f][4 * q + 3]};
+                h4 hi, lo;
+                split(x, hi, lo);
+                *(h4*)(p + 32 * f + 8 * q) = hi;
+                *(h4*)(p + plane + 32 * f + 8 * q) = lo;
+            }
+}
 
+// Walks the n elements of a matrix in the order of memory, V together, eight times V to a thread
+// before the next ones: read(slot, i) of them, then use(slot, i, row, column).
+template <int V, typename Read, typename Use>
+__device__ __forceinline__ void in_order(int n, int ld, Read read, Use use) {
+    constexpr int B = 8, kStep = kSmallThreads * V;
+    for (int i0 = threadIdx.x * V; i0 < n; i0 += B * kStep) {
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            if (i0 + j * kStep < n) read(j, i0 + j * kStep);
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const int i = i0 + j * kStep, r = i / ld;
+            if (i < n) use(j, i, r, i - r * ld);
+        }
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void get(const T* p, float (&v)[V]) {
+    if constexpr (V == 1) v[0] = to_f32(*p);
+    else unpack_vec<T, V>(*(const typename VecT<T, V>::type*)p, v);
+}
+template <typename T, int V>
+__device__ __forceinline__ void put(T* p, const float (&v)[V]) {
+    if constexpr (V == 1) {
+        *p = from_f32<T>(v[0]);
+    } else if constexpr (sizeof(T) == 4) {
+        *(f4*)p = f4{v[0], v[1], v[2], v[3]};
+    } else {
+        *(u2v*)p = u2v{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+    }
+}
+// The momentum, and the update, in the parameter's order, to LDS; returns its sum of squares.
+template <typename T, int V>
+__device__ __forceinline__ double small_momentum(const Small& e, const Hyper& h, float* U,
+                                                 int stride) {
+    float g[8][V], m[8][V];
+    double sum = 0.0;
+    in_order<V>(
+        e.rows * e.cols, e.ld,
+        [&](int j, int i) {
+            get<T, V>((const T*)e.g + i, g[j]);
+            get<float, V>(e.m + i, m[j]);
+        },
+        [&](int j, int i, int r, int c) {
+#pragma unroll
+            for (int x = 0; x < V; ++x) {
+                m[j][x] = next_momentum(h, m[j][x], g[j][x]);
+                const float u = update_of(h, m[j][x], g[j][x]);
+                U[r * stride + c + x] = u;
+                sum = fma((double)u, (double)u, sum);
+            }
+            put<float, V>(e.m + i, m[j]);
+        });
+    return sum;
+}
+template <typename T, int V>
+__device__ __forceinline__ void small_apply(const Small& e, const float* U, int stride) {
+    float p[8][V];
+    const float ls = e.ls * kDown;
+    in_order<V>(
+        e.rows * e.cols, e.ld, [&](int j, int i) { get<T, V>((const T*)e.p + i, p[j]); },
+        [&](int j, int i, int r, int c) {
+#pragma unroll
+            for (int x = 0; x < V; ++x)
+                p[j][x] = fmaf(-ls, U[r * stride + c + x], p[j][x] * e.wd);
+            put<T, V>((T*)e.p + i, p[j]);
+        });
+}
+
+// X, A and B are held times kUp.  The parameter, the gradient and the momentum are read and
+// written in the order of memory, through LDS: a wave's own elements of X lie in 64 rows, and
+// reading them from there took 21 of 76 us at 128 x 128.
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallTable tab, Hyper h) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -139,109 +267,97 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallTable tab, Hy
     const int xplane = mp * xs, aplane = mp * as;
     _Float16* X = (_Float16*)smem;
     _Float16* A = X + 2 * xplane;
-    T* param = (T*)e.p;
-    const T* grad = (const T*)e.g;
-    // Wave w has the tile of X's columns i0 .. + 31 and rows j0 .. + 31: lane l row j0 + l % 32
-    // and sixteen columns, 8 (v / 4) + 4 (l / 32) + v % 4.
-    const int mt = mp / 32, nt = np / 32;
-    const bool has = w < mt * nt, has_a = w < mt * mt;
-    const int i0 = has ? w / mt * 32 : 0, j0 = has ? w % mt * 32 : 0;
-    const int ai = has_a ? w / mt * 32 : 0, aj = has_a ? w % mt * 32 : 0;
+    float* U = (float*)smem;  // the update in the parameter's order, before and after the products
+    const int us = e.ld + 1;
+    // A wave has 64 of X's columns (or the last 32), i0 on, and 32 of its rows, j0 on: lane l has
+    // row j0 + l % 32 and of each 32 columns 8 (v / 4) + 4 (l / 32) + v % 4.  The same of A.
+    const int mt = mp / 32, i0 = w / mt * 64, j0 = w % mt * 32;
+    const bool has = i0 < np, two = i0 + 32 < np, has_a = i0 < mp, two_a = i0 + 32 < mp;
     const int row = j0 + (lane & 31), col0 = i0 + 4 * (lane >> 5);
-    auto at = [&](int v) {  // of the parameter
-        const int c = col0 + 8 * (v >> 2) + (v & 3);
-        return (int64_t)(e.tall ? c : row) * e.ld + (e.tall ? row : c);
-    };
-    auto in = [&](int v) { return has && row < e.rows && col0 + 8 * (v >> 2) + (v & 3) < e.cols; };
-    float x[16];
-    double sum = 0.0;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        x[v] = 0.0f;
-        if (in(v)) {
-            const int64_t i = at(v);
-            const float g = to_f32(grad[i]), m = next_momentum(h, e.m[i], g);
-            e.m[i] = m;
-            x[v] = update_of(h, m, g);
-        }
-        sum = fma((double)x[v], (double)x[v], sum);
-    }
+    auto col = [&](int f, int v) { return col0 + 32 * f + 8 * (v >> 2) + (v & 3); };
+    auto at = [&](int f, int v) { return (e.tall ? col(f, v) : row) * us + (e.tall ? row : col(f, v)); };
+    auto in = [&](int f, int v) { return has && row < e.rows && col(f, v) < e.cols; };
+    const bool vec = takes_vectors(e.g, sizeof(T), e.m) && takes_vectors(e.p, sizeof(T), e.m) &&
+                     e.ld % 4 == 0;
+    double sum = vec ? small_momentum<T, 4>(e, h, U, us) : small_momentum<T, 1>(e, h, U, us);
     sum = lanes::wave_sum(sum);
     if (lane == 0) red[w] = sum;
     __syncthreads();
     sum = 0.0;
     for (int k = 0; k < kSmallWaves; ++k) sum += red[k];
-    const float inv = (float)(1.0 / (sqrt(sum) + h.eps));
+    const float inv = (float)(1.0 / (sqrt(sum) + h.eps)) * kUp;
+    float x[2][16];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) x[v] *= inv;
-    if (has) put_tile(X, xplane, xs, i0, j0, x, lane);
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[f][v] = in(f, v) ? U[at(f, v)] * inv : 0.0f;
     __syncthreads();
-    const int ll = lane & 31, k8 = 8 * (lane >> 5);
+    if (has) put_tile(X, xplane, xs, i0, j0, x, two, lane);
+    __syncthreads();
     for (int step = 0; step < h.steps; ++step) {
-        float a[16];
-        f16v acc = {};
+        float a[2][16];
+        f16v acc[2];
         if (has_a) {
-            for (int k = 0; k < np; k += 16) {
-                h8 p[2], q[2];
-                row_operand(p, X, xplane, xs, ai + ll, k + k8);
-                row_operand(q, X, xplane, xs, aj + ll, k + k8);
-                acc = mma(p, q, acc);
-            }
+            small_product<false>(acc, X, xplane, xs, i0, two_a, X, xplane, xs, j0, np, lane);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) a[v] = acc[v] * (kDown * kDown);
-            put_tile(A, aplane, as, ai, aj, a, lane);
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) a[f][v] = acc[f][v] * kDown;
+            put_tile(A, aplane, as, i0, j0, a, two_a, lane);
         }
         __syncthreads();
-        acc = f16v{};
         if (has_a) {
-            for (int k = 0; k < mp; k += 16) {
-                h8 p[2], q[2];
-                row_operand(p, A, aplane, as, ai + ll, k + k8);
-                row_operand(q, A, aplane, as, aj + ll, k + k8);
-                acc = mma(p, q, acc);
-            }
+            small_product<false>(acc, A, aplane, as, i0, two_a, A, aplane, as, j0, mp, lane);
 #pragma unroll
-            for (int v = 0; v < 16; ++v)
-                a[v] = fmaf(kC * (kDown * kDown), acc[v], kB * a[v]);
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) a[f][v] = fmaf(kC * kDown, acc[f][v], kB * a[f][v]);
         }
         __syncthreads();
-        if (has_a) put_tile(A, aplane, as, ai, aj, a, lane);
+        if (has_a) put_tile(A, aplane, as, i0, j0, a, two_a, lane);
         __syncthreads();
-        acc = f16v{};
         if (has) {
-            for (int k = 0; k < mp; k += 16) {
-                h8 p[2], q[2];
-                col_operand(p, X, xplane, xs, k, i0, lane);
-                row_operand(q, A, aplane, as, j0 + ll, k + k8);
-                acc = mma(p, q, acc);
-            }
+            small_product<true>(acc, X, xplane, xs, i0, two, A, aplane, as, j0, mp, lane);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) x[v] = fmaf(kA, x[v], acc[v] * (kDown * kDown));
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[f][v] = fmaf(kDown, acc[f][v], kA * x[f][v]);
         }
+        if (step + 1 == h.steps) break;
         __syncthreads();
-        if (has) put_tile(X, xplane, xs, i0, j0, x, lane);
+        if (has) put_tile(X, xplane, xs, i0, j0, x, two, lane);
         __syncthreads();
     }
+    __syncthreads();
 #pragma unroll
-    for (int v = 0; v < 16; ++v)
-        if (in(v)) {
-            const int64_t i = at(v);
-            param[i] = from_f32<T>(fmaf(-e.ls, x[v], to_f32(param[i]) * e.wd));
-        }
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            if (in(f, v)) U[at(f, v)] = x[f][v];
+    __syncthreads();
+    vec ? small_apply<T, 4>(e, U, us) : small_apply<T, 1>(e, U, us);
 }
 
 // ------------------------------------------------------------------ large matrices
 constexpr int kNT = 256;
-constexpr int kTile = 128;      // output tile; sides are padded to it
-constexpr int kBK = 32;         // contraction a slice
+constexpr int kPad = 64;        // sides are padded to it
 constexpr int kMaxLarge = 16;   // matrices to a launch
 constexpr int kNormChunk = 16384;
+
+// How a matrix of two fp16 numbers an element lies in memory: row by row, 32 elements at a time,
+// their high parts and then their low ones, 128 bytes together.  So the 32 of the contraction that
+// are multiplied at a time are one whole cache line of a row (as planes apart they were two
+// halves of lines, and loads took half as long again).
+constexpr int kBK = 32;
+__host__ __device__ inline int64_t place(int64_t row, int64_t col, int64_t width) {  // of the high part
+    return (row * width + (col & ~(int64_t)31)) * 2 + (col & 31);
+}
 
 struct Large {
     void* p;
     const void* g;
     float* m;
-    // Planes (hi, then lo): X and its transposed, twice, and A and B.
+    // X and its transposed, twice, and A and B (see place()).
     _Float16 *x[2], *xt[2], *a, *b;
     double* norm;    // partial sums of squares
     int64_t n;       // elements
@@ -266,23 +382,52 @@ __device__ __forceinline__ int find(const LargeTable& tab, int at) {
     return __builtin_amdgcn_readfirstlane(k);
 }
 
+// Four elements from i on of n, one access where vec (then i is a multiple of four).
+template <typename T>
+__device__ __forceinline__ void get4(const T* p, int64_t i, int64_t n, bool vec, float (&v)[4]) {
+    if (vec && i + 4 <= n) {
+        unpack_vec<T, 4>(*(const typename VecT<T, 4>::type*)(p + i), v);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = i + k < n ? to_f32(p[i + k]) : 0.0f;
+    }
+}
 // Momentum, and the sums of squares of the update.
 template <typename T>
 __global__ __launch_bounds__(kNT) void momentum_kernel(LargeTable tab, Hyper h) {
+    constexpr int B = 4;  // accesses of a thread on their way
     __shared__ double red[kNT / kWave];
     const Large& e = tab.t[find<&Large::first_chunk>(tab, blockIdx.x)];
     const int chunk = blockIdx.x - e.first_chunk;
-    const int64_t from = (int64_t)chunk * kNormChunk;
+    const int64_t from = (int64_t)chunk * kNormChunk + threadIdx.x * 4;
     const T* g = (const T*)e.g;
+    const bool vec = takes_vectors(e.g, sizeof(T), e.m);
     double sum = 0.0;
-#pragma unroll 8
-    for (int j = 0; j < kNormChunk / kNT; ++j) {
-        const int64_t i = from + j * kNT + threadIdx.x;
-        if (i >= e.n) break;
-        const float gv = to_f32(g[i]), m = next_momentum(h, e.m[i], gv);
-        e.m[i] = m;
-        const double u = update_of(h, m, gv);
-        sum = fma(u, u, sum);
+    for (int j0 = 0; j0 < kNormChunk / (4 * kNT); j0 += B) {
+        float gv[B][4], mv[B][4];
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const int64_t i = from + (j0 + j) * 4 * kNT;
+            get4(g, i, e.n, vec, gv[j]);
+            get4(e.m, i, e.n, vec, mv[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const int64_t i = from + (j0 + j) * 4 * kNT;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {  // what lies behind the end is zeros
+                mv[j][x] = next_momentum(h, mv[j][x], gv[j][x]);
+                const double u = update_of(h, mv[j][x], gv[j][x]);
+                sum = fma(u, u, sum);
+            }
+            if (vec && i + 4 <= e.n) {
+                *(f4*)(e.m + i) = f4{mv[j][0], mv[j][1], mv[j][2], mv[j][3]};
+            } else {
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    if (i + x < e.n) e.m[i + x] = mv[j][x];
+            }
+        }
     }
     sum = lanes::wave_sum(sum);
     if ((threadIdx.x & 63) == 0) red[wave_id()] = sum;
@@ -290,7 +435,7 @@ __global__ __launch_bounds__(kNT) void momentum_kernel(LargeTable tab, Hyper h) 
     if (threadIdx.x == 0) e.norm[chunk] = ((red[0] + red[1]) + red[2]) + red[3];
 }
 
-// X and its transposed as planes, 64 x 64 elements a workgroup; zeros beyond the matrix.
+// X and its transposed, 64 x 64 elements a workgroup; zeros beyond the matrix.
 template <typename T>
 __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     __shared__ double red[kNT / kWave];
@@ -298,6 +443,19 @@ __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     const Large& e = tab.t[find<&Large::first_pack>(tab, blockIdx.x)];
     const int t = threadIdx.x, at = blockIdx.x - e.first_pack;
     const int across = e.np / 64, r0 = at / across * 64, c0 = at % across * 64;  // of X
+    // tile[a][b]: a along the parameter's rows
+    const T* g = (const T*)e.g;
+    const int pr0 = e.tall ? c0 : r0, pc0 = e.tall ? r0 : c0;
+    const int prows = e.tall ? e.cols : e.rows, pcols = e.tall ? e.rows : e.cols;
+    const bool vec = takes_vectors(e.g, sizeof(T), e.m) && e.ld % 4 == 0;
+    float gv[4][4], mv[4][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int a = pr0 + 16 * j + (t >> 4), b = pc0 + 4 * (t & 15);
+        const int n = a < prows ? pcols : 0;  // elements of the row
+        get4(g + (int64_t)a * e.ld, b, n, vec, gv[j]);
+        get4(e.m + (int64_t)a * e.ld, b, n, vec, mv[j]);
+    }
     double sum = 0.0;
     for (int i = t; i < e.chunks; i += kNT) sum += e.norm[i];
     sum = lanes::wave_sum(sum);
@@ -305,32 +463,27 @@ __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     __syncthreads();
     sum = ((red[0] + red[1]) + red[2]) + red[3];
     const float inv = (float)(1.0 / (sqrt(sum) + h.eps)) * kUp;
-    const T* g = (const T*)e.g;
-    // tile[a][b]: a along the parameter's rows
-    const int pr0 = e.tall ? c0 : r0, pc0 = e.tall ? r0 : c0;
-    const int prows = e.tall ? e.cols : e.rows, pcols = e.tall ? e.rows : e.cols;
-    for (int i = t; i < 64 * 64; i += kNT) {
-        const int a = i >> 6, b = i & 63;
-        float u = 0.0f;
-        if (pr0 + a < prows && pc0 + b < pcols) {
-            const int64_t o = (int64_t)(pr0 + a) * e.ld + pc0 + b;
-            u = update_of(h, e.m[o], to_f32(g[o])) * inv;
-        }
-        tile[a][b] = u;
-    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            tile[16 * j + (t >> 4)][4 * (t & 15) + x] = update_of(h, mv[j][x], gv[j][x]) * inv;
     __syncthreads();
-    const int64_t plane = (int64_t)e.mp * e.np;
-    for (int i = t; i < 64 * 64; i += kNT) {
-        const int a = i >> 6, b = i & 63;
-        _Float16 hi, lo;
-        split(e.tall ? tile[b][a] : tile[a][b], hi, lo);
-        _Float16* x = e.x[0] + (int64_t)(r0 + a) * e.np + c0 + b;
-        x[0] = hi;
-        x[plane] = lo;
-        split(e.tall ? tile[a][b] : tile[b][a], hi, lo);
-        x = e.xt[0] + (int64_t)(c0 + a) * e.mp + r0 + b;
-        x[0] = hi;
-        x[plane] = lo;
+    // Eight elements of a row of X, and of its transposed, at a time.
+    auto put = [&](_Float16* to, int a, int b, bool turned) {
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = turned ? tile[b + x][a] : tile[a][b + x];
+        h8 hi, lo;
+        split(v, hi, lo);
+        *(h8*)to = hi;
+        *(h8*)(to + 32) = lo;
+    };
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int a = 32 * j + (t >> 3), b = 8 * (t & 7);
+        put(e.x[0] + place(r0 + a, c0 + b, e.np), a, b, e.tall);
+        put(e.xt[0] + place(c0 + a, r0 + b, e.mp), a, b, !e.tall);
     }
 }
 
@@ -342,134 +495,226 @@ __device__ __forceinline__ void to_lds(const _Float16* g, char* l) {
                                      (__attribute__((address_space(3))) void*)l, 16, 0, 0);
 }
 
-// A slice in LDS: [operand][plane][128 rows][4 chunks of 16 bytes], a row's chunk c at place
-// c ^ (row / 4) % 4, so that 16 rows' reads of one chunk fall on different banks.
-constexpr int kOperand = kTile * kBK * 2;      // bytes of a plane
-constexpr int kStage = 4 * kOperand;           // both operands, both planes
-constexpr int kLargeLds = 2 * kStage;          // two slices
-constexpr int kRowPad = kTile + 4;
+// Tiles.  A workgroup of WI x WJ waves has a tile of kI rows and kJ columns, a wave FI x FJ blocks
+// of 32 x 32.  A slice of 32 of the contraction in LDS: [P, Q][rows][8 chunks of 16 bytes, high
+// and low], a row's chunk c at place c ^ (row / 2) % 8, so that 16 rows' reads of one chunk fall on
+// different banks.  S slices: S - 1 on their way while one is multiplied.
+template <int WI_, int WJ_, int FI_, int FJ_, int S_>
+struct Tile {
+    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_, S = S_;
+    static constexpr int kI = 32 * WI * FI, kJ = 32 * WJ * FJ, kNT = kWave * WI * WJ;
+    static constexpr int kStage = (kI + kJ) * 128;
+    static constexpr int kPieces = kStage / 1024 / (WI * WJ);  // loads of 1 KB, 8 rows, to a wave
+    static constexpr int kRow = kJ + 4;  // floats in a row of the epilogue's buffer
+    static constexpr int kLds = S * kStage > 64 * kRow * 4 ? S * kStage : 64 * kRow * 4;
+};
 
-// Loads of a slice: 32 pieces of 1 KB, 16 rows each; wave w takes eight.
-__device__ __forceinline__ void load_slice(const _Float16* P, int64_t pplane, int pk,
-                                           const _Float16* Q, int64_t qplane, int qk, int k0,
-                                           char* lds, int w, int lane) {
+// Where a lane's pieces of a slice come from: an operand's rows from the tile's first on, `rows`
+// of them (those behind are read as the last one).
+struct Source {
+    const _Float16* p;
+    int rows;
+};
+template <class G>
+struct Loads {
+    const _Float16* at[G::kPieces];
+    int first;
+    __device__ __forceinline__ Loads(const Source& P, const Source& Q, int64_t K, int w,
+                                     int lane) {
+        first = w * G::kPieces;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int piece = w * 8 + j;  // operand, plane, block of 16 rows
-        const int op = piece >> 4, pl = (piece >> 3) & 1, block = piece & 7;
-        const int row = block * 16 + (lane >> 2), chunk = (lane & 3) ^ ((row >> 2) & 3);
-        const _Float16* src = op ? Q + pl * qplane + (int64_t)row * qk
-                                 : P + pl * pplane + (int64_t)row * pk;
-        to_lds(src + k0 + chunk * 8, lds + piece * 1024);
+        for (int j = 0; j < G::kPieces; ++j) {
+            const int block = (first + j) * 8;  // first row of the piece
+            const bool second = block >= G::kI;
+            const int row = block - (second ? G::kI : 0) + (lane >> 3);
+            const int chunk = (lane & 7) ^ ((row >> 1) & 7);
+            const int rows = second ? Q.rows : P.rows, r = row < rows ? row : rows - 1;
+            at[j] = (second ? Q.p : P.p) + r * K * 2 + chunk * 8;
+        }
     }
-}
-__device__ __forceinline__ void slice_operand(h8 (&o)[2], const char* lds, int row, int chunk) {
-    const int at = row * 64 + ((chunk ^ ((row >> 2) & 3)) << 4);
-    o[0] = *(const h8*)(lds + at);
-    o[1] = *(const h8*)(lds + kOperand + at);
+    __device__ __forceinline__ void slice(int64_t s, char* lds) const {
+#pragma unroll
+        for (int j = 0; j < G::kPieces; ++j) to_lds(at[j] + s * 64, lds + (first + j) * 1024);
+    }
+};
+// Operands of 16 of the contraction.
+template <class G>
+struct Frags {
+    h8 p[G::FI][2], q[G::FJ][2];
+    __device__ __forceinline__ void read(const char* lds, int wi, int wj, int ks, int lane) {
+#pragma unroll
+        for (int i = 0; i < G::FI; ++i) one(p[i], lds, wi + 32 * i, ks, lane);
+#pragma unroll
+        for (int j = 0; j < G::FJ; ++j) one(q[j], lds + G::kI * 128, wj + 32 * j, ks, lane);
+    }
+    __device__ __forceinline__ static void one(h8 (&o)[2], const char* lds, int row0, int ks,
+                                               int lane) {
+        const int row = row0 + (lane & 31), chunk = 2 * ks + (lane >> 5), f = (row >> 1) & 7;
+        o[0] = *(const h8*)(lds + row * 128 + ((chunk ^ f) << 4));
+        o[1] = *(const h8*)(lds + row * 128 + (((chunk + 4) ^ f) << 4));
+    }
+    __device__ __forceinline__ void multiply(f16v (&acc)[G::FI][G::FJ]) const {
+#pragma unroll
+        for (int i = 0; i < G::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < G::FJ; ++j) acc[i][j] = mfma(p[i][0], q[j][1], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < G::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < G::FJ; ++j) acc[i][j] = mfma(p[i][1], q[j][0], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < G::FI; ++i)
+#pragma unroll
+            for (int j = 0; j < G::FJ; ++j) acc[i][j] = mfma(p[i][0], q[j][0], acc[i][j]);
+    }
+};
+
+// Waits until at most N of the wave's loads are on their way.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N < 64, "six bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+    asm volatile("" ::: "memory");
 }
 
-template <typename T, Product kKind>
-__global__ __launch_bounds__(kNT, 2) void product_kernel(LargeTable tab, int from) {
+template <typename T, Product kKind, class G>
+__global__ __launch_bounds__(G::kNT, 1) void product_kernel(LargeTable tab, int from) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int t = threadIdx.x, lane = t & 63, w = wave_id();
     constexpr bool kSquare = kKind == kGram || kKind == kPoly;
-    // Workgroups go to the XCDs in turn; each XCD takes a run of tiles.
-    const int all = gridDim.x, xcd = blockIdx.x & 7, per = all / 8, more = all % 8;
-    const int b = xcd * per + (xcd < more ? xcd : more) + (blockIdx.x >> 3);
-    const int k = kSquare ? find<&Large::first_a>(tab, b) : find<&Large::first_x>(tab, b);
+    // A matrix's tiles, eighths of them to the XCDs that workgroups go to in turn.
+    const int k = kSquare ? find<&Large::first_a>(tab, blockIdx.x)
+                          : find<&Large::first_x>(tab, blockIdx.x);
     const Large& e = tab.t[k];
+    const int down = (e.mp + G::kI - 1) / G::kI;
+    const int across = kSquare ? down : (e.np + G::kJ - 1) / G::kJ;
+    const int tiles = kSquare ? down * (down + 1) / 2 : down * across;
+    const int l = blockIdx.x - (kSquare ? e.first_a : e.first_x);
+    const int at = (l & 7) * ((tiles + 7) / 8) + (l >> 3);
+    if (at >= tiles || (l >> 3) >= (tiles + 7) / 8) return;
     int ti, tj;  // tile row and column
     if constexpr (kSquare) {
         // Tiles on and below the diagonal, row by row.
-        const int at = b - e.first_a;
         ti = (int)((sqrtf(8.0f * at + 1.0f) - 1.0f) * 0.5f);
         while (ti * (ti + 1) / 2 > at) --ti;
         while ((ti + 1) * (ti + 2) / 2 <= at) ++ti;
         tj = at - ti * (ti + 1) / 2;
     } else {
-        const int at = b - e.first_x, down = e.mp / kTile;
-        ti = at % down;
-        tj = at / down;
+        // Bands of eight tile rows, column by column.
+        const int band = at / (8 * across), in = at - band * 8 * across;
+        const int high = down - 8 * band < 8 ? down - 8 * band : 8;
+        ti = 8 * band + in % high;
+        tj = in / high;
     }
     const int K = kKind == kGram ? e.np : e.mp;
-    const int64_t aplane = (int64_t)e.mp * e.mp, xplane = (int64_t)e.mp * e.np;
-    const _Float16 *P, *Q;
-    int64_t pplane, qplane;
-    if constexpr (kKind == kGram) {
-        P = Q = e.x[from];
-        pplane = qplane = xplane;
-    } else if constexpr (kKind == kPoly) {
-        P = Q = e.a;
-        pplane = qplane = aplane;
-    } else {
-        P = e.b;
-        Q = e.xt[from];
-        pplane = aplane;
-        qplane = xplane;
-    }
-    P += (int64_t)ti * kTile * K;
-    Q += (int64_t)tj * kTile * K;
-    const int wi = (w >> 1) * 64, wj = (w & 1) * 64;
-    f16v acc[2][2] = {};
+    const int64_t r0 = (int64_t)ti * G::kI, c0 = (int64_t)tj * G::kJ;
+    Source P, Q;
+    P.p = kKind == kGram ? e.x[from] : kKind == kPoly ? e.a : e.b;
+    Q.p = kSquare ? P.p : e.xt[from];
+    P.p += 2 * r0 * K;
+    Q.p += 2 * c0 * K;
+    P.rows = e.mp - (int)r0;
+    Q.rows = (kSquare ? e.mp : e.np) - (int)c0;
+    const Loads<G> loads(P, Q, K, w, lane);
+    const int wi = w / G::WJ * 32 * G::FI, wj = w % G::WJ * 32 * G::FJ;
+    f16v acc[G::FI][G::FJ] = {};
     const int slices = K / kBK;
-    load_slice(P, pplane, K, Q, qplane, K, 0, smem, w, lane);
+    // Operands are read 16 of the contraction ahead of their products.
+    Frags<G> even, odd;
+    auto slice_at = [&](int s) { return smem + (s % G::S) * G::kStage; };
+    auto load = [&](int s) {  // behind the last one: that again, read by nobody
+        loads.slice(s < slices ? s : slices - 1, slice_at(s));
+    };
+#pragma unroll
+    for (int s = 0; s < G::S; ++s) load(s);
+    wait_loads<(G::S - 1) * G::kPieces>();
+    wtile::lds_barrier();
+    even.read(slice_at(0), wi, wj, 0, lane);
     for (int s = 0; s < slices; ++s) {
-        __syncthreads();  // the slice has arrived, and the other half's reads are done
-        if (s + 1 < slices)
-            load_slice(P, pplane, K, Q, qplane, K, (s + 1) * kBK, smem + ((s + 1) & 1) * kStage,
-                       w, lane);
-        const char* lds = smem + (s & 1) * kStage;
-#pragma unroll
-        for (int ks = 0; ks < kBK / 16; ++ks) {
-            h8 p[2][2], q[2][2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                slice_operand(p[i], lds, wi + 32 * i + (lane & 31), 2 * ks + (lane >> 5));
-                slice_operand(q[i], lds + 2 * kOperand, wj + 32 * i + (lane & 31),
-                              2 * ks + (lane >> 5));
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = mma(p[i], q[j], acc[i][j]);
-        }
+        odd.read(slice_at(s), wi, wj, 1, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        even.multiply(acc);
+        // Slice s + 1 has arrived; slice s was read, its place is filled again.
+        wait_loads<(G::S - 2) * G::kPieces>();
+        wtile::lds_barrier();
+        load(s + G::S);
+        even.read(slice_at(s + 1), wi, wj, 0, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        odd.multiply(acc);
     }
+    wait_loads<0>();
     // The tile through LDS, 64 rows at a time: what is added read by rows, results written by
     // rows, and again by columns as the transposed.
-    float* buf = (float*)smem;  // [64][kRowPad]
-    const int64_t r0 = (int64_t)ti * kTile, c0 = (int64_t)tj * kTile;
-    const int64_t width = kSquare ? e.mp : e.np, plane = kSquare ? aplane : xplane;
+    float* buf = (float*)smem;  // [64][kRow]
+    const int64_t width = kSquare ? e.mp : e.np;
     _Float16* out = kKind == kGram ? e.a : kKind == kPoly ? e.b : e.x[from ^ 1];
     _Float16* out_t = kSquare ? out : e.xt[from ^ 1];
     const _Float16* add = kKind == kPoly ? e.a : e.x[from];
-    for (int half = 0; half < 2; ++half) {
-        __syncthreads();
-        if ((w >> 1) == half) {
+    constexpr int kAcross = G::kJ / 8, kRows = G::kNT / kAcross, kCols = G::kNT / 8;
+    for (int band = 0; band < G::kI / 64; ++band) {
+        const int64_t rr = r0 + 64 * band;
+        if (rr >= e.mp) break;
+        // What is read of memory, ahead of the first write.
+        constexpr int kPasses = 64 / kRows, kPassesT = G::kJ / kCols;
+        h8 old[kKind == kGram ? 1 : kPasses][2];
+        float was[kKind == kLast ? (kPasses > kPassesT ? kPasses : kPassesT) : 1][8];
+        if constexpr (kKind != kGram) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int pass = 0; pass < kPasses; ++pass) {
+                const int r = pass * kRows + t / kAcross, c = t % kAcross * 8;
+                if (c0 + c >= width) continue;
+                const int64_t o = place(rr + r, c0 + c, width);
+                old[pass][0] = *(const h8*)(add + o);
+                old[pass][1] = *(const h8*)(add + o + 32);
+            }
+        }
+        if constexpr (kKind == kLast) {
+            if (!e.tall) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                for (int pass = 0; pass < kPasses; ++pass) {
+                    const int64_t r = rr + pass * kRows + t / kAcross, c = c0 + t % kAcross * 8;
+                    const T* param = (const T*)e.p + r * e.ld + c;
 #pragma unroll
-                    for (int v = 0; v < 16; ++v)
-                        buf[(32 * i + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) * kRowPad + wj +
-                            32 * j + (lane & 31)] = acc[i][j][v];
+                    for (int x = 0; x < 8; ++x)
+                        was[pass][x] = r < e.rows && c + x < e.cols ? to_f32(param[x]) : 0.0f;
+                }
+            } else {
+#pragma unroll
+                for (int pass = 0; pass < kPassesT; ++pass) {
+                    const int64_t c = c0 + pass * kCols + t % kCols, r = rr + t / kCols * 8;
+                    const T* param = (const T*)e.p + c * e.ld + r;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        was[pass][x] = c < e.cols && r + x < e.rows ? to_f32(param[x]) : 0.0f;
+                }
+            }
         }
         __syncthreads();
-        const int64_t rr = r0 + 64 * half;
-        // Sixteen rows of eight values a thread at a time.
 #pragma unroll
-        for (int pass = 0; pass < 4; ++pass) {
-            const int r = pass * 16 + (t >> 4), c = (t & 15) * 8;
+        for (int i = 0; i < G::FI; ++i)
+            if ((wi + 32 * i) / 64 == band)
+#pragma unroll
+                for (int j = 0; j < G::FJ; ++j)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        buf[((wi + 32 * i) % 64 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3)) *
+                                G::kRow + wj + 32 * j + (lane & 31)] = acc[i][j][v];
+        __syncthreads();
+#pragma unroll
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const int r = pass * kRows + t / kAcross, c = t % kAcross * 8;
+            if (c0 + c >= width) continue;
+            float* cell = buf + r * G::kRow + c;
             float v[8];
 #pragma unroll
-            for (int x = 0; x < 8; x += 4) *(f4*)(v + x) = *(const f4*)(buf + r * kRowPad + c + x);
-            const int64_t o = (rr + r) * width + c0 + c;
+            for (int x = 0; x < 8; x += 4) *(f4*)(v + x) = *(const f4*)(cell + x);
+            const int64_t o = place(rr + r, c0 + c, width);
             if constexpr (kKind == kGram) {
 #pragma unroll
                 for (int x = 0; x < 8; ++x) v[x] *= kDown;
             } else {
-                const h8 hi = *(const h8*)(add + o), lo = *(const h8*)(add + plane + o);
+                const h8 hi = old[pass][0], lo = old[pass][1];
                 constexpr float ka = kKind == kPoly ? kB : kA, kp = kKind == kPoly ? kC : 1.0f;
 #pragma unroll
                 for (int x = 0; x < 8; ++x)
@@ -481,56 +726,42 @@ __global__ __launch_bounds__(kNT, 2) void product_kernel(LargeTable tab, int fro
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
                         if (c0 + c + x < e.cols)
-                            param[x] = from_f32<T>(
-                                fmaf(-e.ls * kDown, v[x], to_f32(param[x]) * e.wd));
+                            param[x] = from_f32<T>(fmaf(-e.ls * kDown, v[x], was[pass][x] * e.wd));
                 }
             } else {
                 h8 hi, lo;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    _Float16 a, d;
-                    split(v[x], a, d);
-                    hi[x] = a;
-                    lo[x] = d;
-                }
+                split(v, hi, lo);
                 *(h8*)(out + o) = hi;
-                *(h8*)(out + plane + o) = lo;
+                *(h8*)(out + o + 32) = lo;
             }
 #pragma unroll
-            for (int x = 0; x < 8; x += 4) *(f4*)(buf + r * kRowPad + c + x) = *(const f4*)(v + x);
+            for (int x = 0; x < 8; x += 4) *(f4*)(cell + x) = *(const f4*)(v + x);
         }
         if constexpr (kSquare)
-            if (ti == tj) continue;  // it is its own transposed
+            if (ti == tj) continue;  // its own transposed
         __syncthreads();
         // Rows of the transposed: column c of the 64 rows, eight values a thread.
-        const int64_t tw = kSquare ? e.mp : e.mp;
 #pragma unroll
-        for (int pass = 0; pass < 4; ++pass) {
-            const int c = pass * 32 + (t & 31), r = (t >> 5) * 8;
+        for (int pass = 0; pass < kPassesT; ++pass) {
+            const int c = pass * kCols + t % kCols, r = t / kCols * 8;
+            if (c0 + c >= width) continue;
             float v[8];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) v[x] = buf[(r + x) * kRowPad + c];
+            for (int x = 0; x < 8; ++x) v[x] = buf[(r + x) * G::kRow + c];
             if constexpr (kKind == kLast) {
                 if (e.tall && c0 + c < e.cols) {
                     T* param = (T*)e.p + (c0 + c) * e.ld + rr + r;
 #pragma unroll
                     for (int x = 0; x < 8; ++x)
                         if (rr + r + x < e.rows)
-                            param[x] = from_f32<T>(
-                                fmaf(-e.ls * kDown, v[x], to_f32(param[x]) * e.wd));
+                            param[x] = from_f32<T>(fmaf(-e.ls * kDown, v[x], was[pass][x] * e.wd));
                 }
             } else {
-                const int64_t o = (c0 + c) * tw + rr + r;
+                const int64_t o = place(c0 + c, rr + r, e.mp);
                 h8 hi, lo;
-#pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    _Float16 a, d;
-                    split(v[x], a, d);
-                    hi[x] = a;
-                    lo[x] = d;
-                }
+                split(v, hi, lo);
                 *(h8*)(out_t + o) = hi;
-                *(h8*)(out_t + plane + o) = lo;
+                *(h8*)(out_t + o + 32) = lo;
             }
         }
     }
@@ -548,12 +779,12 @@ Shape shape_of(const recblr_muon_tensor& t) {
     s.cols = (int)(s.tall ? t.rows : t.cols);
     s.mp = (s.rows + 31) / 32 * 32;
     s.np = (s.cols + 31) / 32 * 32;
-    // A tile of X, and one of A, to each wave, and the planes in LDS.
-    s.small = (int64_t)(s.mp / 32) * (s.np / 32) <= kSmallWaves &&
+    // 64 x 32 of X, and of A, to each wave, and the planes in LDS.
+    s.small = (int64_t)(s.mp / 32) * ((s.np + 63) / 64) <= kSmallWaves &&
               small_lds(s.mp, s.np) <= (size_t)kSmallLds;
     if (!s.small) {
-        s.mp = (s.rows + kTile - 1) / kTile * kTile;
-        s.np = (s.cols + kTile - 1) / kTile * kTile;
+        s.mp = (s.rows + kPad - 1) / kPad * kPad;
+        s.np = (s.cols + kPad - 1) / kPad * kPad;
     }
     return s;
 }
@@ -565,23 +796,68 @@ size_t large_bytes(const Shape& s, int64_t n) {
            align256((size_t)chunks_of(n) * 8);
 }
 
+// Workgroups of a product, an eighth of each matrix's tiles to an XCD; numbers the matrices'
+// firsts.
+int64_t number_tiles(LargeTable& tab, bool square, int side) {
+    int64_t at = 0;
+    for (int i = 0; i < tab.count; ++i) {
+        Large& l = tab.t[i];
+        const int64_t down = (l.mp + side - 1) / side, across = (l.np + side - 1) / side;
+        (square ? l.first_a : l.first_x) = (int)at;
+        at += ((square ? down * (down + 1) / 2 : down * across) + 7) / 8 * 8;
+    }
+    return at;
+}
+
+using Tile256 = Tile<2, 4, 4, 2, 2>;
+using Tile128 = Tile<2, 2, 2, 2, 2>;
+using Tile64 = Tile<2, 2, 1, 1, 4>;
+
+// The largest tiles of which there are enough.
+int side_of(LargeTable& tab, bool square) {
+    static const int force = getenv("MUON_SIDE") ? atoi(getenv("MUON_SIDE")) : 0;
+    if (force) return force;
+    const int64_t n256 = number_tiles(tab, square, 256), rounds = (n256 + 255) / 256;
+    if (n256 >= 240 * rounds) return 256;
+    return number_tiles(tab, square, 128) >= 384 ? 128 : 64;
+}
+
+template <typename T, Product kKind, class G>
+hipError_t run_product(const LargeTable& tab, int64_t groups, int from, hipStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    const auto kernel = product_kernel<T, kKind, G>;
+    const hipError_t e = allow_dynamic_lds((const void*)kernel, G::kLds, done);
+    if (e != hipSuccess) return e;
+    kernel<<<dim3((unsigned)groups), G::kNT, G::kLds, st>>>(tab, from);
+    return hipGetLastError();
+}
+template <typename T, Product kKind>
+hipError_t run_product(LargeTable& tab, int from, hipStream_t st) {
+    constexpr bool kSquare = kKind == kGram || kKind == kPoly;
+    const int side = side_of(tab, kSquare);
+    const int64_t groups = number_tiles(tab, kSquare, side > 128 && side < 140 ? 128 : side);
+    if (side == 129) return run_product<T, kKind, Tile<2, 2, 2, 2, 4>>(tab, groups, from, st);
+    if (side == 130) return run_product<T, kKind, Tile<4, 2, 1, 2, 2>>(tab, groups, from, st);
+    if (side == 131) return run_product<T, kKind, Tile<4, 4, 1, 1, 2>>(tab, groups, from, st);
+    return side == 256   ? run_product<T, kKind, Tile256>(tab, groups, from, st)
+           : side == 128 ? run_product<T, kKind, Tile128>(tab, groups, from, st)
+                         : run_product<T, kKind, Tile64>(tab, groups, from, st);
+}
+
 template <typename T>
-hipError_t run_large(const LargeTable& tab, const int (&work)[4], const Hyper& h,
-                     hipStream_t st) {
+hipError_t run_large(LargeTable& tab, const int (&work)[2], const Hyper& h, hipStream_t st) {
     momentum_kernel<T><<<dim3((unsigned)work[0]), kNT, 0, st>>>(tab, h);
     pack_kernel<T><<<dim3((unsigned)work[1]), kNT, 0, st>>>(tab, h);
-    int from = 0;
-    for (int s = 0; s < h.steps; ++s) {
-        const dim3 square((unsigned)work[2]), whole((unsigned)work[3]);
-        product_kernel<T, kGram><<<square, kNT, kLargeLds, st>>>(tab, from);
-        product_kernel<T, kPoly><<<square, kNT, kLargeLds, st>>>(tab, from);
-        if (s + 1 < h.steps)
-            product_kernel<T, kNext><<<whole, kNT, kLargeLds, st>>>(tab, from);
-        else
-            product_kernel<T, kLast><<<whole, kNT, kLargeLds, st>>>(tab, from);
-        from ^= 1;
+    hipError_t e = hipGetLastError();
+    for (int s = 0; s < h.steps && e == hipSuccess; ++s) {
+        const int from = s & 1;
+        e = run_product<T, kGram>(tab, from, st);
+        if (e == hipSuccess) e = run_product<T, kPoly>(tab, from, st);
+        if (e == hipSuccess)
+            e = s + 1 < h.steps ? run_product<T, kNext>(tab, from, st)
+                                : run_product<T, kLast>(tab, from, st);
     }
-    return hipGetLastError();
+    return e;
 }
 
 template <typename T>
@@ -603,10 +879,20 @@ hipError_t run(const recblr_muon_tensor* tensors, int64_t count, const MuonHyper
     };
     LargeTable large;
     large.count = 0;
-    int work[4] = {0, 0, 0, 0};
+    int work[2] = {0, 0};
     char* at = (char*)ws;
     auto flush_large = [&]() {
         if (!large.count) return hipSuccess;
+        // Those with the longest products first: their tiles are the last to end.
+        std::stable_sort(large.t, large.t + large.count,
+                         [](const Large& a, const Large& b) { return a.np > b.np; });
+        for (int i = 0; i < large.count; ++i) {
+            Large& l = large.t[i];
+            l.first_chunk = work[0];
+            l.first_pack = work[1];
+            work[0] += l.chunks;
+            work[1] += l.mp / 64 * (l.np / 64);
+        }
         const hipError_t e = run_large<T>(large, work, h, st);
         large.count = 0;
         for (int& x : work) x = 0;
@@ -656,15 +942,6 @@ hipError_t run(const recblr_muon_tensor* tensors, int64_t count, const MuonHyper
         l.np = s.np;
         l.ld = (int)t.cols;
         l.tall = s.tall;
-        l.first_chunk = work[0];
-        l.first_pack = work[1];
-        l.first_a = work[2];
-        l.first_x = work[3];
-        const int mt = s.mp / kTile, nt = s.np / kTile;
-        work[0] += l.chunks;
-        work[1] += s.mp / 64 * (s.np / 64);
-        work[2] += mt * (mt + 1) / 2;
-        work[3] += mt * nt;
         if (large.count == kMaxLarge) {
             const hipError_t e = flush_large();
             if (e != hipSuccess) return e;
