@@ -505,7 +505,7 @@ struct Tile {
     static constexpr int kI = 32 * WI * FI, kJ = 32 * WJ * FJ, kNT = kWave * WI * WJ;
     static constexpr int kStage = (kI + kJ) * 128;
     static constexpr int kPieces = kStage / 1024 / (WI * WJ);  // loads of 1 KB, 8 rows, to a wave
-    static constexpr int kRow = kJ + 4;  // floats in a row of the epilogue's buffer
+    static constexpr int kRow = kJ + 1;  // floats in a row of the epilogue's buffer
     static constexpr int kLds = S * kStage > 64 * kRow * 4 ? S * kStage : 64 * kRow * 4;
 };
 
@@ -532,20 +532,20 @@ struct Loads {
             at[j] = (second ? Q.p : P.p) + r * K * 2 + chunk * 8;
         }
     }
-    __device__ __forceinline__ void slice(int64_t s, char* lds) const {
-#pragma unroll
-        for (int j = 0; j < G::kPieces; ++j) to_lds(at[j] + s * 64, lds + (first + j) * 1024);
+    __device__ __forceinline__ void piece(int j, int64_t s, char* lds) const {
+        to_lds(at[j] + s * 64, lds + (first + j) * 1024);
     }
 };
 // Operands of 16 of the contraction.
 template <class G>
 struct Frags {
+    static constexpr int kReads = G::FI + G::FJ, kMfma = 3 * G::FI * G::FJ;
     h8 p[G::FI][2], q[G::FJ][2];
-    __device__ __forceinline__ void read(const char* lds, int wi, int wj, int ks, int lane) {
-#pragma unroll
-        for (int i = 0; i < G::FI; ++i) one(p[i], lds, wi + 32 * i, ks, lane);
-#pragma unroll
-        for (int j = 0; j < G::FJ; ++j) one(q[j], lds + G::kI * 128, wj + 32 * j, ks, lane);
+    // The n-th of the reads.
+    __device__ __forceinline__ void read(int n, const char* lds, int wi, int wj, int ks,
+                                         int lane) {
+        if (n < G::FI) one(p[n], lds, wi + 32 * n, ks, lane);
+        else one(q[n - G::FI], lds + G::kI * 128, wj + 32 * (n - G::FI), ks, lane);
     }
     __device__ __forceinline__ static void one(h8 (&o)[2], const char* lds, int row0, int ks,
                                                int lane) {
@@ -553,21 +553,39 @@ struct Frags {
         o[0] = *(const h8*)(lds + row * 128 + ((chunk ^ f) << 4));
         o[1] = *(const h8*)(lds + row * 128 + (((chunk + 4) ^ f) << 4));
     }
-    __device__ __forceinline__ void multiply(f16v (&acc)[G::FI][G::FJ]) const {
-#pragma unroll
-        for (int i = 0; i < G::FI; ++i)
-#pragma unroll
-            for (int j = 0; j < G::FJ; ++j) acc[i][j] = mfma(p[i][0], q[j][1], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < G::FI; ++i)
-#pragma unroll
-            for (int j = 0; j < G::FJ; ++j) acc[i][j] = mfma(p[i][1], q[j][0], acc[i][j]);
-#pragma unroll
-        for (int i = 0; i < G::FI; ++i)
-#pragma unroll
-            for (int j = 0; j < G::FJ; ++j) acc[i][j] = mfma(p[i][0], q[j][0], acc[i][j]);
+    // The n-th of the products: low times high of every block, high times low, high times high.
+    __device__ __forceinline__ void multiply(int n, f16v (&acc)[G::FI][G::FJ]) const {
+        const int term = n / (G::FI * G::FJ), i = n / G::FJ % G::FI, j = n % G::FJ;
+        acc[i][j] = mfma(p[i][term == 1], q[j][term == 0], acc[i][j]);
     }
 };
+
+// Eight elements of a parameter's row from column c on, as far as it has them.
+template <typename T>
+__device__ __forceinline__ void get8(const T* p, int64_t r, int64_t c, int rows, int cols, int ld,
+                                     bool vec, float (&v)[8]) {
+    p += r * ld + c;
+    if (vec && r < rows && c + 8 <= cols) {
+        get<T, 4>(p, *(float(*)[4])v);
+        get<T, 4>(p + 4, *(float(*)[4])(v + 4));
+    } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = r < rows && c + x < cols ? to_f32(p[x]) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void put8(T* p, int64_t r, int64_t c, int rows, int cols, int ld,
+                                     bool vec, const float (&v)[8]) {
+    p += r * ld + c;
+    if (vec && r < rows && c + 8 <= cols) {
+        put<T, 4>(p, *(const float(*)[4])v);
+        put<T, 4>(p + 4, *(const float(*)[4])(v + 4));
+    } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+            if (r < rows && c + x < cols) p[x] = from_f32<T>(v[x]);
+    }
+}
 
 // Waits until at most N of the wave's loads are on their way.
 template <int N>
@@ -620,74 +638,86 @@ __global__ __launch_bounds__(G::kNT, 1) void product_kernel(LargeTable tab, int 
     const int wi = w / G::WJ * 32 * G::FI, wj = w % G::WJ * 32 * G::FJ;
     f16v acc[G::FI][G::FJ] = {};
     const int slices = K / kBK;
-    // Operands are read 16 of the contraction ahead of their products.
-    Frags<G> even, odd;
+    // Operands are read 16 of the contraction ahead of their products, and loads of a later slice
+    // lie among the products: issued together they hold a wave up for as long as half of these.
+    using F = Frags<G>;
+    F even, odd;
     auto slice_at = [&](int s) { return smem + (s % G::S) * G::kStage; };
-    auto load = [&](int s) {  // behind the last one: that again, read by nobody
-        loads.slice(s < slices ? s : slices - 1, slice_at(s));
-    };
+    auto known = [&](int s) { return s < slices ? s : slices - 1; };  // the last one again
 #pragma unroll
-    for (int s = 0; s < G::S; ++s) load(s);
+    for (int s = 0; s < G::S; ++s)
+#pragma unroll
+        for (int j = 0; j < G::kPieces; ++j) loads.piece(j, known(s), slice_at(s));
     wait_loads<(G::S - 1) * G::kPieces>();
     wtile::lds_barrier();
-    even.read(slice_at(0), wi, wj, 0, lane);
+#pragma unroll
+    for (int n = 0; n < F::kReads; ++n) even.read(n, slice_at(0), wi, wj, 0, lane);
     for (int s = 0; s < slices; ++s) {
-        odd.read(slice_at(s), wi, wj, 1, lane);
-        __builtin_amdgcn_sched_barrier(0);
-        even.multiply(acc);
+        const char* lds = slice_at(s);
+#pragma unroll
+        for (int n = 0; n < F::kMfma; ++n) {
+#pragma unroll
+            for (int r = 0; r < F::kReads; ++r)
+                if (r * F::kMfma / F::kReads / 2 == n) odd.read(r, lds, wi, wj, 1, lane);
+            even.multiply(n, acc);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         // Slice s + 1 has arrived; slice s was read, its place is filled again.
         wait_loads<(G::S - 2) * G::kPieces>();
         wtile::lds_barrier();
-        load(s + G::S);
-        even.read(slice_at(s + 1), wi, wj, 0, lane);
-        __builtin_amdgcn_sched_barrier(0);
-        odd.multiply(acc);
+        const int next = known(s + G::S);
+        char* place = slice_at(s);
+        lds = slice_at(s + 1);
+#pragma unroll
+        for (int n = 0; n < F::kMfma; ++n) {
+#pragma unroll
+            for (int r = 0; r < F::kReads; ++r)
+                if (r * F::kMfma / F::kReads / 2 == n) even.read(r, lds, wi, wj, 0, lane);
+#pragma unroll
+            for (int j = 0; j < G::kPieces; ++j)
+                if (j * F::kMfma / G::kPieces == n) loads.piece(j, next, place);
+            odd.multiply(n, acc);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     wait_loads<0>();
     // The tile through LDS, 64 rows at a time: what is added read by rows, results written by
-    // rows, and again by columns as the transposed.
+    // rows, and again by columns as the transposed.  Eight values of a row, or of a column, to a
+    // thread.
     float* buf = (float*)smem;  // [64][kRow]
     const int64_t width = kSquare ? e.mp : e.np;
     _Float16* out = kKind == kGram ? e.a : kKind == kPoly ? e.b : e.x[from ^ 1];
     _Float16* out_t = kSquare ? out : e.xt[from ^ 1];
     const _Float16* add = kKind == kPoly ? e.a : e.x[from];
-    constexpr int kAcross = G::kJ / 8, kRows = G::kNT / kAcross, kCols = G::kNT / 8;
+    constexpr int kAcross = G::kJ / 8, kPasses = 64 * kAcross / G::kNT, kRows = 64 / kPasses;
+    constexpr int kPassesT = G::kJ * 8 / G::kNT, kCols = G::kJ / kPassesT;
+    const int r1 = t / kAcross, c1 = t % kAcross * 8;  // by rows
+    const int c2 = t / 8, r2 = t % 8 * 8;              // by columns
+    const bool vec = kKind == kLast && ((uintptr_t)e.p & 15) == 0 &&
+                     e.ld % (16 / (int)sizeof(T)) == 0;
     for (int band = 0; band < G::kI / 64; ++band) {
         const int64_t rr = r0 + 64 * band;
         if (rr >= e.mp) break;
         // What is read of memory, ahead of the first write.
-        constexpr int kPasses = 64 / kRows, kPassesT = G::kJ / kCols;
         h8 old[kKind == kGram ? 1 : kPasses][2];
-        float was[kKind == kLast ? (kPasses > kPassesT ? kPasses : kPassesT) : 1][8];
+        float was[kKind == kLast ? kPasses : 1][8];
+        static_assert(kPasses == kPassesT, "a tile has as many rows in a band as wave columns");
         if constexpr (kKind != kGram) {
 #pragma unroll
             for (int pass = 0; pass < kPasses; ++pass) {
-                const int r = pass * kRows + t / kAcross, c = t % kAcross * 8;
-                if (c0 + c >= width) continue;
-                const int64_t o = place(rr + r, c0 + c, width);
+                if (c0 + c1 >= width) continue;
+                const int64_t o = place(rr + pass * kRows + r1, c0 + c1, width);
                 old[pass][0] = *(const h8*)(add + o);
                 old[pass][1] = *(const h8*)(add + o + 32);
             }
         }
         if constexpr (kKind == kLast) {
-            if (!e.tall) {
 #pragma unroll
-                for (int pass = 0; pass < kPasses; ++pass) {
-                    const int64_t r = rr + pass * kRows + t / kAcross, c = c0 + t % kAcross * 8;
-                    const T* param = (const T*)e.p + r * e.ld + c;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        was[pass][x] = r < e.rows && c + x < e.cols ? to_f32(param[x]) : 0.0f;
-                }
-            } else {
-#pragma unroll
-                for (int pass = 0; pass < kPassesT; ++pass) {
-                    const int64_t c = c0 + pass * kCols + t % kCols, r = rr + t / kCols * 8;
-                    const T* param = (const T*)e.p + c * e.ld + r;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        was[pass][x] = c < e.cols && r + x < e.rows ? to_f32(param[x]) : 0.0f;
-                }
+            for (int pass = 0; pass < kPasses; ++pass) {
+                const int64_t r = rr + (e.tall ? r2 : pass * kRows + r1);
+                const int64_t c = c0 + (e.tall ? pass * kCols + c2 : c1);
+                if (e.tall) get8((const T*)e.p, c, r, e.cols, e.rows, e.ld, vec, was[pass]);
+                else get8((const T*)e.p, r, c, e.rows, e.cols, e.ld, vec, was[pass]);
             }
         }
         __syncthreads();
@@ -703,13 +733,12 @@ __global__ __launch_bounds__(G::kNT, 1) void product_kernel(LargeTable tab, int 
         __syncthreads();
 #pragma unroll
         for (int pass = 0; pass < kPasses; ++pass) {
-            const int r = pass * kRows + t / kAcross, c = t % kAcross * 8;
-            if (c0 + c >= width) continue;
-            float* cell = buf + r * G::kRow + c;
+            const int r = pass * kRows + r1;
+            if (c0 + c1 >= width) continue;
+            float* cell = buf + r * G::kRow + c1;
             float v[8];
 #pragma unroll
-            for (int x = 0; x < 8; x += 4) *(f4*)(v + x) = *(const f4*)(cell + x);
-            const int64_t o = place(rr + r, c0 + c, width);
+            for (int x = 0; x < 8; ++x) v[x] = cell[x];
             if constexpr (kKind == kGram) {
 #pragma unroll
                 for (int x = 0; x < 8; ++x) v[x] *= kDown;
@@ -721,43 +750,38 @@ __global__ __launch_bounds__(G::kNT, 1) void product_kernel(LargeTable tab, int 
                     v[x] = fmaf(kp * kDown, v[x], ka * ((float)hi[x] + (float)lo[x]));
             }
             if constexpr (kKind == kLast) {
-                if (!e.tall && rr + r < e.rows) {
-                    T* param = (T*)e.p + (rr + r) * e.ld + c0 + c;
+                if (!e.tall) {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        if (c0 + c + x < e.cols)
-                            param[x] = from_f32<T>(fmaf(-e.ls * kDown, v[x], was[pass][x] * e.wd));
+                    for (int x = 0; x < 8; ++x) v[x] = fmaf(-e.ls * kDown, v[x], was[pass][x] * e.wd);
+                    put8((T*)e.p, rr + r, c0 + c1, e.rows, e.cols, e.ld, vec, v);
+                    continue;
                 }
             } else {
                 h8 hi, lo;
                 split(v, hi, lo);
+                const int64_t o = place(rr + r, c0 + c1, width);
                 *(h8*)(out + o) = hi;
                 *(h8*)(out + o + 32) = lo;
             }
 #pragma unroll
-            for (int x = 0; x < 8; x += 4) *(f4*)(cell + x) = *(const f4*)(v + x);
+            for (int x = 0; x < 8; ++x) cell[x] = v[x];
         }
-        if constexpr (kSquare)
-            if (ti == tj) continue;  // its own transposed
+        if (kSquare && ti == tj) continue;        // its own transposed
+        if (kKind == kLast && !e.tall) continue;  // nobody reads it
         __syncthreads();
-        // Rows of the transposed: column c of the 64 rows, eight values a thread.
 #pragma unroll
-        for (int pass = 0; pass < kPassesT; ++pass) {
-            const int c = pass * kCols + t % kCols, r = t / kCols * 8;
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const int c = pass * kCols + c2;
             if (c0 + c >= width) continue;
             float v[8];
 #pragma unroll
-            for (int x = 0; x < 8; ++x) v[x] = buf[(r + x) * G::kRow + c];
+            for (int x = 0; x < 8; ++x) v[x] = buf[(r2 + x) * G::kRow + c];
             if constexpr (kKind == kLast) {
-                if (e.tall && c0 + c < e.cols) {
-                    T* param = (T*)e.p + (c0 + c) * e.ld + rr + r;
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        if (rr + r + x < e.rows)
-                            param[x] = from_f32<T>(fmaf(-e.ls * kDown, v[x], was[pass][x] * e.wd));
-                }
+                for (int x = 0; x < 8; ++x) v[x] = fmaf(-e.ls * kDown, v[x], was[pass][x] * e.wd);
+                put8((T*)e.p, c0 + c, rr + r2, e.cols, e.rows, e.ld, vec, v);
             } else {
-                const int64_t o = place(c0 + c, rr + r, e.mp);
+                const int64_t o = place(c0 + c, rr + r2, e.mp);
                 h8 hi, lo;
                 split(v, hi, lo);
                 *(h8*)(out_t + o) = hi;
