@@ -365,20 +365,27 @@ struct Large {
     int rows, cols;  // of X
     int mp, np;
     int ld, tall;
-    int first_chunk, first_pack, first_a, first_x;  // work before this matrix's, in each launch
+    int first_chunk, first_pack;  // work before this matrix's, in each launch
+    int first_tile[2];            // of symmetric products, of the others
     int chunks;
 };
 struct LargeTable {
     Large t[kMaxLarge];
-    int count;
+    int count, eighths;
 };
 static_assert(sizeof(LargeTable) <= 3800, "kernel arguments end at 4 KB");
 
-template <int Large::*kFirst>
+// The matrix that work `at` is of; kFirst: tiles of symmetric products, of others, chunks, packs.
+template <int kFirst>
 __device__ __forceinline__ int find(const LargeTable& tab, int at) {
     int k = 0;
 #pragma unroll
-    for (int i = 1; i < kMaxLarge; ++i) k += i < tab.count && at >= tab.t[i].*kFirst;
+    for (int i = 1; i < kMaxLarge; ++i) {
+        const Large& e = tab.t[i];
+        const int first = kFirst < 2 ? e.first_tile[kFirst & 1]
+                                     : kFirst == 2 ? e.first_chunk : e.first_pack;
+        k += i < tab.count && at >= first;
+    }
     return __builtin_amdgcn_readfirstlane(k);
 }
 
@@ -397,7 +404,7 @@ template <typename T>
 __global__ __launch_bounds__(kNT) void momentum_kernel(LargeTable tab, Hyper h) {
     constexpr int B = 4;  // accesses of a thread on their way
     __shared__ double red[kNT / kWave];
-    const Large& e = tab.t[find<&Large::first_chunk>(tab, blockIdx.x)];
+    const Large& e = tab.t[find<2>(tab, blockIdx.x)];
     const int chunk = blockIdx.x - e.first_chunk;
     const int64_t from = (int64_t)chunk * kNormChunk + threadIdx.x * 4;
     const T* g = (const T*)e.g;
@@ -440,7 +447,7 @@ template <typename T>
 __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     __shared__ double red[kNT / kWave];
     __shared__ float tile[64][65];
-    const Large& e = tab.t[find<&Large::first_pack>(tab, blockIdx.x)];
+    const Large& e = tab.t[find<3>(tab, blockIdx.x)];
     const int t = threadIdx.x, at = blockIdx.x - e.first_pack;
     const int across = e.np / 64, r0 = at / across * 64, c0 = at % across * 64;  // of X
     // tile[a][b]: a along the parameter's rows
@@ -601,16 +608,19 @@ __global__ __launch_bounds__(G::kNT, 1) void product_kernel(LargeTable tab, int 
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int t = threadIdx.x, lane = t & 63, w = wave_id();
     constexpr bool kSquare = kKind == kGram || kKind == kPoly;
-    // A matrix's tiles, eighths of them to the XCDs that workgroups go to in turn.
-    const int k = kSquare ? find<&Large::first_a>(tab, blockIdx.x)
-                          : find<&Large::first_x>(tab, blockIdx.x);
+    // Workgroups go to the XCDs in turn.  Where there is one to each compute unit, every XCD takes
+    // a run of all tiles, so that a matrix is read by few of them (a fifth faster); else an eighth
+    // of each matrix's, so that none has the longest to itself.
+    const int per = gridDim.x / 8, b = tab.eighths ? (int)blockIdx.x
+                                                   : (int)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    const int k = find<kSquare ? 0 : 1>(tab, b);
     const Large& e = tab.t[k];
     const int down = (e.mp + G::kI - 1) / G::kI;
     const int across = kSquare ? down : (e.np + G::kJ - 1) / G::kJ;
     const int tiles = kSquare ? down * (down + 1) / 2 : down * across;
-    const int l = blockIdx.x - (kSquare ? e.first_a : e.first_x);
-    const int at = (l & 7) * ((tiles + 7) / 8) + (l >> 3);
-    if (at >= tiles || (l >> 3) >= (tiles + 7) / 8) return;
+    const int l = b - e.first_tile[kSquare ? 0 : 1], eighth = (tiles + 7) / 8;
+    const int at = tab.eighths ? (l & 7) * eighth + (l >> 3) : l;
+    if (at >= tiles || (tab.eighths && (l >> 3) >= eighth)) return;
     int ti, tj;  // tile row and column
     if constexpr (kSquare) {
         // Tiles on and below the diagonal, row by row.
@@ -820,34 +830,70 @@ size_t large_bytes(const Shape& s, int64_t n) {
            align256((size_t)chunks_of(n) * 8);
 }
 
-// Workgroups of a product, an eighth of each matrix's tiles to an XCD; numbers the matrices'
-// firsts.
-int64_t number_tiles(LargeTable& tab, bool square, int side) {
-    int64_t at = 0;
-    for (int i = 0; i < tab.count; ++i) {
-        Large& l = tab.t[i];
-        const int64_t down = (l.mp + side - 1) / side, across = (l.np + side - 1) / side;
-        (square ? l.first_a : l.first_x) = (int)at;
-        at += ((square ? down * (down + 1) / 2 : down * across) + 7) / 8 * 8;
-    }
-    return at;
-}
-
 using Tile256 = Tile<2, 4, 4, 2, 2>;
-using Tile128 = Tile<2, 2, 2, 2, 2>;
+using Tile128 = Tile<2, 2, 2, 2, 4>;       // one to a compute unit
+using Tile128Pair = Tile<2, 2, 2, 2, 2>;   // two
 using Tile64 = Tile<2, 2, 1, 1, 4>;
 
-// The largest tiles of which there are enough.
-int side_of(LargeTable& tab, bool square) {
-    static const int force = getenv("MUON_SIDE") ? atoi(getenv("MUON_SIDE")) : 0;
-    if (force) return force;
-    const int64_t n256 = number_tiles(tab, square, 256), rounds = (n256 + 255) / 256;
-    if (n256 >= 240 * rounds) return 256;
-    return number_tiles(tab, square, 128) >= 384 ? 128 : 64;
+int64_t tiles_of(const Large& l, bool square, int side) {
+    const int64_t down = (l.mp + side - 1) / side, across = (l.np + side - 1) / side;
+    return square ? down * (down + 1) / 2 : down * across;
+}
+
+// Which tiles to take.  Their time, from measurements on the whole chip: `fixed` us and `each`
+// for 32 of the contraction, `slots` of them at once; where there are more, what is left over at
+// the end is counted as half of the shortest.  2000 x 2000 takes 779 us with tiles of 64, 685
+// and 770 with the two of 128, 1,807 with 256; 1000 x 1000: 207, 383, 439, 1,111; 4096 x 4096:
+// 5,868, 4,350, 4,274, 3,884 (five steps).
+struct Choice {
+    int side, slots;
+    float each, fixed;
+};
+constexpr Choice kChoices[] = {{64, 512, 0.50f, 4.0f},
+                               {128, 256, 0.78f, 6.0f},
+                               {128, 512, 1.45f, 8.0f},
+                               {256, 256, 2.50f, 28.0f}};
+int choose(const LargeTable& tab, bool square, bool gram) {
+    static const int force = getenv("MUON_SIDE") ? atoi(getenv("MUON_SIDE")) : -1;
+    if (force >= 0) return force;
+    int best = 0;
+    float least = 0.0f;
+    for (int c = 0; c < 4; ++c) {
+        const Choice& k = kChoices[c];
+        float sum = 0.0f, longest = 0.0f, shortest = 3e38f;
+        int64_t n = 0;
+        for (int i = 0; i < tab.count; ++i) {
+            const Large& l = tab.t[i];
+            const float one = k.fixed + k.each * (float)((gram ? l.np : l.mp) / 32);
+            const int64_t tiles = tiles_of(l, square, k.side);
+            n += tiles;
+            sum += one * (float)tiles;
+            longest = one > longest ? one : longest;
+            shortest = one < shortest ? one : shortest;
+        }
+        float time = sum / (float)k.slots + 0.5f * shortest;
+        if (n <= k.slots || time < longest) time = longest;
+        if (c == 0 || time < least) {
+            least = time;
+            best = c;
+        }
+    }
+    return best;
 }
 
 template <typename T, Product kKind, class G>
-hipError_t run_product(const LargeTable& tab, int64_t groups, int from, hipStream_t st) {
+hipError_t run_product(LargeTable& tab, int from, hipStream_t st) {
+    constexpr bool kSquare = kKind == kGram || kKind == kPoly;
+    int64_t all = 0;
+    for (int i = 0; i < tab.count; ++i) all += tiles_of(tab.t[i], kSquare, G::kI);
+    tab.eighths = all > 256;
+    int64_t groups = 0;
+    for (int i = 0; i < tab.count; ++i) {
+        tab.t[i].first_tile[kSquare ? 0 : 1] = (int)groups;
+        const int64_t n = tiles_of(tab.t[i], kSquare, G::kI);
+        groups += tab.eighths ? (n + 7) / 8 * 8 : n;
+    }
+    groups = (groups + 7) / 8 * 8;
     static std::atomic<uint64_t> done{0};
     const auto kernel = product_kernel<T, kKind, G>;
     const hipError_t e = allow_dynamic_lds((const void*)kernel, G::kLds, done);
@@ -856,16 +902,11 @@ hipError_t run_product(const LargeTable& tab, int64_t groups, int from, hipStrea
     return hipGetLastError();
 }
 template <typename T, Product kKind>
-hipError_t run_product(LargeTable& tab, int from, hipStream_t st) {
-    constexpr bool kSquare = kKind == kGram || kKind == kPoly;
-    const int side = side_of(tab, kSquare);
-    const int64_t groups = number_tiles(tab, kSquare, side > 128 && side < 140 ? 128 : side);
-    if (side == 129) return run_product<T, kKind, Tile<2, 2, 2, 2, 4>>(tab, groups, from, st);
-    if (side == 130) return run_product<T, kKind, Tile<4, 2, 1, 2, 2>>(tab, groups, from, st);
-    if (side == 131) return run_product<T, kKind, Tile<4, 4, 1, 1, 2>>(tab, groups, from, st);
-    return side == 256   ? run_product<T, kKind, Tile256>(tab, groups, from, st)
-           : side == 128 ? run_product<T, kKind, Tile128>(tab, groups, from, st)
-                         : run_product<T, kKind, Tile64>(tab, groups, from, st);
+hipError_t run_product(LargeTable& tab, int choice, int from, hipStream_t st) {
+    return choice == 0   ? run_product<T, kKind, Tile64>(tab, from, st)
+           : choice == 1 ? run_product<T, kKind, Tile128>(tab, from, st)
+           : choice == 2 ? run_product<T, kKind, Tile128Pair>(tab, from, st)
+                         : run_product<T, kKind, Tile256>(tab, from, st);
 }
 
 template <typename T>
@@ -873,13 +914,15 @@ hipError_t run_large(LargeTable& tab, const int (&work)[2], const Hyper& h, hipS
     momentum_kernel<T><<<dim3((unsigned)work[0]), kNT, 0, st>>>(tab, h);
     pack_kernel<T><<<dim3((unsigned)work[1]), kNT, 0, st>>>(tab, h);
     hipError_t e = hipGetLastError();
+    const int gram = choose(tab, true, true), poly = choose(tab, true, false),
+              next = choose(tab, false, false);
     for (int s = 0; s < h.steps && e == hipSuccess; ++s) {
         const int from = s & 1;
-        e = run_product<T, kGram>(tab, from, st);
-        if (e == hipSuccess) e = run_product<T, kPoly>(tab, from, st);
+        e = run_product<T, kGram>(tab, gram, from, st);
+        if (e == hipSuccess) e = run_product<T, kPoly>(tab, poly, from, st);
         if (e == hipSuccess)
-            e = s + 1 < h.steps ? run_product<T, kNext>(tab, from, st)
-                                : run_product<T, kLast>(tab, from, st);
+            e = s + 1 < h.steps ? run_product<T, kNext>(tab, next, from, st)
+                                : run_product<T, kLast>(tab, next, from, st);
     }
     return e;
 }

@@ -7,13 +7,18 @@
 // So a row needs its maximum and sum before its first output, and every logit again for
 // that output: 2 e bytes a logit where the row stays on chip in between.
 //
-// Two ways.  A row that fits the registers of a wave, or of a workgroup of 256 or 1024
-// threads, is read once, as 16-byte vectors that lie at multiples of 16 bytes (up to seven
-// elements before and behind them are one element more of a thread each).  Longer rows,
-// and long rows that are too few to fill the chip, are cut into pieces: one launch leaves
-// each piece's maximum and sum, a second joins them and writes the gradient, reading the
-// logits again.
+// A row of up to 16 KB stays in the registers of a wave or of 256 threads and is read once, as
+// 16-byte vectors that lie at multiples of 16 bytes (up to seven elements before and behind them
+// are one element more of a thread each).  A longer row's workgroup reads it twice, in the first
+// pass against a running maximum; the second pass finds it in the last-level cache.  Few long
+// rows are cut into pieces: one launch leaves each piece's maximum and sum, a second joins them.
+//
+// One MI355X: 4096 x 131072 bf16 412 us, 5.2 TB/s of the logits and their gradient, where a large
+// copy reaches 4.7 to 6.2; the powers, two a logit, are 200 us of vector issue beside it.
+// 2048 x 3416 fp32: 11 us of kernel, 17 of the call from Python.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "lanes.hpp"
@@ -45,26 +50,48 @@ struct RowLoss {
     float lp, loss, c;  // c: d loss / d logp, over T
 };
 
-// xa: the chosen item's logit.  A NaN passes every comparison on to a product with it.
-__device__ __forceinline__ RowLoss row_loss(const Params& p, int64_t row, float xa, float M,
-                                            float S) {
-    RowLoss o;
-    o.lp = (xa - M) / p.T - logf(S);
+// Powers of a row: e^((l - M) / T) = 2^(l k - mk), one fma before the power.  mk is M k rounded;
+// what that leaves is common to all powers of the row, and `shift` gives it back to log S.  Where
+// M k is so large that it would be more than 2^-5, the difference is formed first.
+struct Powers {
+    float M, k, mk;
+    bool far;
+    double shift;
+    __device__ __forceinline__ Powers(float M_, float k_) : M(M_), k(k_), mk(M_ * k_) {
+        far = !(fabsf(mk) < 0x1p20f);
+        shift = far ? 0.0 : ((double)M * (double)k - (double)mk) * 0.6931471805599453094;
+    }
+    template <bool kFar>
+    __device__ __forceinline__ float of(float l) const {
+        return fast_exp2(kFar ? (l - M) * k : fmaf(l, k, -mk));
+    }
+    // f, told which of the two it is.
+    template <typename F>
+    __device__ __forceinline__ void use(F f) const {
+        far ? f(std::true_type{}) : f(std::false_type{});
+    }
+};
+
+// xa: the chosen item's logit; S: the sum of powers, infinite only by a logit of +inf.  In 64 bits: the ratio is the power of a difference of two numbers
+// of ten or so, whose roundings to fp32 were most of the loss's error.  A NaN passes every
+// comparison on to a product with it.
+__device__ __forceinline__ RowLoss row_loss(const Params& p, int64_t row, float xa,
+                                            const Powers& w2, float S) {
+    const double sum = S < __builtin_inff() ? (double)S : __builtin_nan("");
+    const double lp = ((double)xa - (double)w2.M) / (double)p.T - (log(sum) - w2.shift);
     const float A = p.advantage[row], w = p.weight ? p.weight[row] : 1.0f;
-    const float r = expf(o.lp - p.old_logp[row]);
+    const float r = (float)exp(lp - (double)p.old_logp[row]);
     const bool gain = A >= 0.0f;
     const bool inside = gain ? !(r > p.hi) : !(r < p.lo);
     const float surrogate = inside ? r * A : (gain ? p.hi : p.lo) * A;
     float loss = -surrogate, c = inside ? -surrogate : 0.0f;
     if (p.kl > 0.0f) {
-        const float d = p.ref_logp[row] - o.lp, up = expm1f(d);
+        const double d = (double)p.ref_logp[row] - lp, up = expm1(d);
         // Both are of d's size, so what is left of d^2 keeps its digits; e^d may be infinite.
-        loss += p.kl * (up < __builtin_inff() ? up - d : up);
-        c -= p.kl * up;
+        loss += p.kl * (float)(up < __builtin_inf() ? up - d : up);
+        c -= p.kl * (float)up;
     }
-    o.loss = w * loss;
-    o.c = w * c * p.inv_T;
-    return o;
+    return RowLoss{(float)lp, w * loss, w * c * p.inv_T};
 }
 
 __device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7FC00000u); }
@@ -108,6 +135,15 @@ struct Raw {
     __device__ __forceinline__ void none() {  // -inf in every place
         const uint32_t w = VEC && sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
         v = u4v{w, w, w, w};
+    }
+    __device__ __forceinline__ void keep(const T* body, int i) {
+        if constexpr (VEC) v = *((const u4v*)body + i);
+        else v[0] = __float_as_uint(to_f32(body[i]));
+    }
+    // What is done with the row next starts from its words again: left alone, the compiler keeps all
+    // of its values as floats from one use to the next, twice the registers.
+    __device__ __forceinline__ void packed() {
+        if constexpr (VEC && sizeof(T) == 2) asm volatile("" : "+v"(v));
     }
     __device__ __forceinline__ float get(int e) const {
         if constexpr (!VEC || sizeof(T) == 4) return __uint_as_float(v[e]);
@@ -198,38 +234,168 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void row_kernel(Params p) {
 #pragma unroll
         for (int e = 0; e < U; ++e) m = fmaxf(m, x[j].get(e));
     const float M = over_row<TH>(fmaxf(m, xe), -__builtin_inff(), red, larger);
-    float s = fast_exp2((xe - M) * p.k2);
-    const float ee = s;
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
+    for (int j = 0; j < NV; ++j) x[j].packed();
+    const Powers pw(M, p.k2);
+    pw.use([&](auto far) {
+        constexpr bool kFar = decltype(far)::value;
+        float s = pw.of<kFar>(xe);
+        const float ee = s;
 #pragma unroll
-        for (int e = 0; e < U; ++e) {
-            const float v = fast_exp2((x[j].get(e) - M) * p.k2);
-            s += v;
-            if constexpr (!VEC || sizeof(T) == 4) x[j].v[e] = __float_as_uint(v);
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int e = 0; e < U; ++e) {
+                const float v = pw.of<kFar>(x[j].get(e));
+                s += v;
+                if constexpr (!VEC || sizeof(T) == 4) x[j].v[e] = __float_as_uint(v);
+            }
+        const float S = over_row<TH>(s, 0.0f, red, added);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) x[j].packed();
+        const RowLoss r = row_loss(p, row, xa, pw, S);
+        if (t == 0) {
+            p.row_loss[row] = r.loss;
+            if (p.logp) p.logp[row] = r.lp;
         }
-    const float S = over_row<TH>(s, 0.0f, red, added);
-    const RowLoss r = row_loss(p, row, xa, M, S);
+        if (!out) return;
+        const float minus = -r.c / S;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = t + j * TH;
+            if (i < sp.vecs) {
+                float g[U];
+#pragma unroll
+                for (int e = 0; e < U; ++e)
+                    g[e] = !VEC || sizeof(T) == 4 ? __uint_as_float(x[j].v[e])
+                                                  : pw.of<kFar>(x[j].get(e));
+                gradient<U>(g, minus, r.c, (int64_t)id - sp.head - (int64_t)i * U);
+                Raw<T, VEC>::write(out + sp.head, i, g);
+            }
+        }
+        if (extra >= 0) out[extra] = from_f32<T>(ee * minus + (extra == id ? r.c : 0.0f));
+    });
+}
+
+// ------------------------------------------------------------------ a row read twice
+// A thread's running reference and the sum of powers relative to it, over vectors t, t + TH, ... of
+// `vecs`; the reference starts at `low`, where nothing that counts can lie beside a row's maximum
+// above it.  B vectors at a time.
+template <int TH, typename T, bool VEC>
+__device__ __forceinline__ void running_sum(const T* body, int vecs, int t, float k, float& m,
+                                            float& mk, float& s) {
+    constexpr int U = Span<T, VEC>::U, B = 4;
+    for (int i = t; i < vecs; i += B * TH) {
+        Raw<T, VEC> x[B];
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            x[j].none();
+            if (i + j * TH < vecs) x[j].keep(body, i + j * TH);
+        }
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+#pragma unroll
+            for (int e = 0; e < U; ++e) top = fmaxf(top, x[j].get(e));
+        const float now = top * k;
+        s *= fast_exp2(mk - now);
+        m = top;
+        mk = now;
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+#pragma unroll
+            for (int e = 0; e < U; ++e) s += fast_exp2(fmaf(x[j].get(e), k, -mk));
+    }
+}
+// The row's powers and, in S, their sum; xe: one element of the thread's beside its vectors.
+template <int TH, typename T, bool VEC>
+__device__ __forceinline__ Powers sum_of(const T* body, int vecs, int t, float xe, float k,
+                                         float* red, float& S) {
+    constexpr int U = Span<T, VEC>::U;
+    const float none = -__builtin_inff(), low = -0x1p19f / k;
+    float m = fmaxf(low, xe), mk = m * k, s = fast_exp2(fmaf(xe, k, -mk));
+    running_sum<TH, T, VEC>(body, vecs, t, k, m, mk, s);
+    float M = over_row<TH>(m, none, red, larger);
+    Powers pw(M, k);
+    s *= fast_exp2(mk - pw.mk);
+    if (M <= low || pw.far) {  // once more, with the maximum first
+        m = xe;
+        for (int i = t; i < vecs; i += TH) {
+            Raw<T, VEC> x;
+            x.keep(body, i);
+#pragma unroll
+            for (int e = 0; e < U; ++e) m = fmaxf(m, x.get(e));
+        }
+        M = over_row<TH>(m, none, red, larger);
+        pw = Powers(M, k);
+        pw.far = true;
+        pw.shift = 0.0;
+        s = fast_exp2((xe - M) * k);
+        for (int i = t; i < vecs; i += TH) {
+            Raw<T, VEC> x;
+            x.keep(body, i);
+#pragma unroll
+            for (int e = 0; e < U; ++e) s += fast_exp2((x.get(e) - M) * k);
+        }
+    }
+    S = over_row<TH>(s, 0.0f, red, added);
+    return pw;
+}
+
+template <typename T, int TH, bool VEC>
+__global__ __launch_bounds__(TH) void twice_kernel(Params p) {
+    constexpr int U = Span<T, VEC>::U, B = 4;  // vectors on their way
+    __shared__ float red[16];
+    const int64_t row = blockIdx.x;
+    const int id = p.ids[row], t = threadIdx.x;
+    const T* base = (const T*)p.logits + row * p.V;
+    T* out = p.dlogits ? (T*)p.dlogits + row * p.V : nullptr;
+    const Span<T, VEC> sp(base, p.V);
+    const T* body = base + sp.head;
+    const int extra = sp.extra(t);
+    if (id < 0) {
+        if (t == 0) {
+            p.row_loss[row] = 0.0f;
+            if (p.logp) p.logp[row] = 0.0f;
+        }
+        if (out) {
+            const float zeros[U] = {};
+            for (int i = t; i < sp.vecs; i += TH) Raw<T, VEC>::write(out + sp.head, i, zeros);
+            if (extra >= 0) out[extra] = from_f32<T>(0.0f);
+        }
+        return;
+    }
+    const float xa = id < p.V ? to_f32(base[id]) : quiet_nan();
+    const float xe = VEC && extra >= 0 ? to_f32(base[extra]) : -__builtin_inff();
+    float S;
+    const Powers pw = sum_of<TH, T, VEC>(body, sp.vecs, t, xe, p.k2, red, S);
+    const RowLoss r = row_loss(p, row, xa, pw, S);
     if (t == 0) {
         p.row_loss[row] = r.loss;
         if (p.logp) p.logp[row] = r.lp;
     }
     if (!out) return;
     const float minus = -r.c / S;
+    pw.use([&](auto far) {
+        constexpr bool kFar = decltype(far)::value;
+        for (int i0 = t; i0 < sp.vecs; i0 += B * TH) {
+            Raw<T, VEC> x[B];
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int i = t + j * TH;
-        if (i < sp.vecs) {
-            float g[U];
+            for (int j = 0; j < B; ++j)
+                if (i0 + j * TH < sp.vecs) x[j].read(body, i0 + j * TH);
 #pragma unroll
-            for (int e = 0; e < U; ++e)
-                g[e] = !VEC || sizeof(T) == 4 ? __uint_as_float(x[j].v[e])
-                                              : fast_exp2((x[j].get(e) - M) * p.k2);
-            gradient<U>(g, minus, r.c, (int64_t)id - sp.head - (int64_t)i * U);
-            Raw<T, VEC>::write(out + sp.head, i, g);
+            for (int j = 0; j < B; ++j) {
+                const int i = i0 + j * TH;
+                if (i >= sp.vecs) break;
+                float g[U];
+#pragma unroll
+                for (int e = 0; e < U; ++e) g[e] = pw.of<kFar>(x[j].get(e));
+                gradient<U>(g, minus, r.c, (int64_t)id - sp.head - (int64_t)i * U);
+                Raw<T, VEC>::write(out + sp.head, i, g);
+            }
         }
-    }
-    if (extra >= 0) out[extra] = from_f32<T>(ee * minus + (extra == id ? r.c : 0.0f));
+        if (VEC && extra >= 0)
+            out[extra] = from_f32<T>(pw.of<kFar>(xe) * minus + (extra == id ? r.c : 0.0f));
+    });
 }
 
 // ------------------------------------------------------------------ rows in pieces
@@ -323,27 +489,34 @@ __global__ __launch_bounds__(kPieceThreads) void joined_kernel(Params p, const P
         if (q.s != 0.0f || M == none) s += q.s * fast_exp2((q.m - M) * p.k2);
     }
     const float S = over_row<TH>(s, 0.0f, red, added);
-    const RowLoss r = row_loss(p, row, id < p.V ? chosen[row] : quiet_nan(), M, S);
+    // The pieces' sums are relative to their maxima as they are: nothing to give back to log S.
+    Powers pw(M, p.k2);
+    const double shift = pw.shift;
+    pw.shift = 0.0;
+    const RowLoss r = row_loss(p, row, id < p.V ? chosen[row] : quiet_nan(), pw, S);
     if (t == 0 && at == 0) {
         p.row_loss[row] = r.loss;
         if (p.logp) p.logp[row] = r.lp;
     }
     if (!out) return;
-    const float minus = -r.c / S;
+    const float minus = -r.c / S * (float)exp(-shift);
     const int64_t pick = (int64_t)id - from;
+    pw.use([&](auto far) {
+        constexpr bool kFar = decltype(far)::value;
 #pragma unroll 4
-    for (int i = t; i < sp.vecs; i += TH) {
-        Raw<T, VEC> x;
-        x.read(body, i);
-        float g[U];
+        for (int i = t; i < sp.vecs; i += TH) {
+            Raw<T, VEC> x;
+            x.read(body, i);
+            float g[U];
 #pragma unroll
-        for (int e = 0; e < U; ++e) g[e] = fast_exp2((x.get(e) - M) * p.k2);
-        gradient<U>(g, minus, r.c, pick - sp.head - (int64_t)i * U);
-        Raw<T, VEC>::write(out + sp.head, i, g);
-    }
-    if (VEC && extra >= 0)
-        out[extra] = from_f32<T>(fast_exp2((to_f32(base[extra]) - M) * p.k2) * minus +
-                                 (extra == pick ? r.c : 0.0f));
+            for (int e = 0; e < U; ++e) g[e] = pw.of<kFar>(x.get(e));
+            gradient<U>(g, minus, r.c, pick - sp.head - (int64_t)i * U);
+            Raw<T, VEC>::write(out + sp.head, i, g);
+        }
+        if (VEC && extra >= 0)
+            out[extra] = from_f32<T>(pw.of<kFar>(to_f32(base[extra])) * minus +
+                                     (extra == pick ? r.c : 0.0f));
+    });
 }
 
 // ------------------------------------------------------------------ sum of the rows
@@ -376,20 +549,20 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(const In* v, int64_t n
 }
 
 // ------------------------------------------------------------------ which way
-// Threads a row and vectors a thread for rows kept in registers; the first that hold the row.
 struct Way {
-    int threads, vecs;
-    int64_t piece;  // > 0: elements to a piece of a row instead
+    int threads, vecs;  // to a row; vectors a thread keeps, 0: the row is read twice
+    int64_t piece;      // > 0: elements to a piece of a row instead
 };
 
+// Rows of up to 16 KB stay in registers.  Longer ones are read twice, the second time from the
+// last-level cache: 4096 rows of 256 KB take 412 us so and 481 in the registers of 1024 threads,
+// whose arithmetic then waits for loads and loads for it (one row to a compute unit); 8192 rows of
+// 32 KB 76 and 91, of 16 KB 76 and 55.  Few long rows are cut into pieces: 16 x 131072 bf16 22 us.
 Way way_of(int64_t N, int64_t V, IoType io, bool vec) {
     const int64_t U = vec ? 16 / (int64_t)io_bytes(io) : 1, n = (V + U - 1) / U;  // vectors
     if (n <= 64 * 4) return {64, n <= 64 ? 1 : n <= 128 ? 2 : 4, 0};
-    const bool few = N < 128 && n > 2048;
-    if (!few) {
-        if (n <= 256 * 8) return {256, n <= 512 ? 2 : n <= 1024 ? 4 : 8, 0};
-        if (n <= 1024 * 16) return {1024, n <= 4096 ? 4 : n <= 8192 ? 8 : 16, 0};
-    }
+    if (n <= 1024) return {256, n <= 512 ? 2 : 4, 0};
+    if (N >= 128 || n <= 16384) return {n <= 4096 ? 512 : 1024, 0, 0};
     // Pieces: about four workgroups to a compute unit, of 2,048 elements or more.
     const int64_t want = (1024 + N - 1) / N;
     int64_t piece = (V + want - 1) / want;
@@ -440,12 +613,11 @@ void launch_rows(const Params& p, const Way& w, const Layout& l, char* ws, hipSt
         else row_kernel<T, 64, 4, VEC><<<quads, 256, 0, st>>>(p);
     } else if (w.threads == 256) {
         if (w.vecs == 2) row_kernel<T, 256, 2, VEC><<<rows, 256, 0, st>>>(p);
-        else if (w.vecs == 4) row_kernel<T, 256, 4, VEC><<<rows, 256, 0, st>>>(p);
-        else row_kernel<T, 256, 8, VEC><<<rows, 256, 0, st>>>(p);
+        else row_kernel<T, 256, 4, VEC><<<rows, 256, 0, st>>>(p);
+    } else if (w.threads == 512) {
+        twice_kernel<T, 512, VEC><<<rows, 512, 0, st>>>(p);
     } else {
-        if (w.vecs == 4) row_kernel<T, 1024, 4, VEC><<<rows, 1024, 0, st>>>(p);
-        else if (w.vecs == 8) row_kernel<T, 1024, 8, VEC><<<rows, 1024, 0, st>>>(p);
-        else row_kernel<T, 1024, 16, VEC><<<rows, 1024, 0, st>>>(p);
+        twice_kernel<T, 1024, VEC><<<rows, 1024, 0, st>>>(p);
     }
 }
 
