@@ -8,9 +8,10 @@
 // of a digit become each block's first place within it, and the blocks place their positions,
 // 64 at a time, a lane's place among the lanes of the same digit by ballots.  The sorted
 // positions are cut into pieces of 64, a wave each, whatever items they hold, so a popular
-// item spreads over many waves; a run of an item that lies within a piece is its row, and
-// runs that go over borders leave partial sums, joined by a second launch in their order.
-// Which addition follows which hangs on the ids alone.
+// item spreads over many waves; a run of an item that lies within a piece is its row, runs
+// that go over the borders of pieces are joined by the workgroup of 16 pieces, and those that
+// go over its borders by a second launch, in their order.  Which addition follows which hangs
+// on the ids alone.
 //
 // Few positions: each wave looks for its position's id among all; the first of an id sums them.
 #include <hip/hip_runtime.h>
@@ -58,7 +59,7 @@ __global__ __launch_bounds__(kNT) void lookup_kernel(const T* __restrict__ table
                     v[e] = bf16_pair(some ? bf16_lo(v[e]) * scale : none,
                                      some ? bf16_hi(v[e]) * scale : none);
             }
-            *(u4v*)o = v;
+            __builtin_nontemporal_store(v, (u4v*)o);
         } else {
             *o = from_f32<T>(some ? to_f32(table[(int64_t)id * D + u]) * scale : none);
         }
@@ -75,16 +76,15 @@ __device__ __forceinline__ void read_row(const T* p, float (&v)[VL]) {
         unpack_vec<T, VL>(*(const typename VecT<T, VL>::type*)p, v);
     }
 }
+// The same as it lies in memory, and its values.
 template <typename T, int VL>
-__device__ __forceinline__ void write_row(T* p, const float (&v)[VL], float scale, bool add) {
-    float o[VL];
-    if (add)
-        read_row<T, VL>(p, o);
-    else
-#pragma unroll
-        for (int e = 0; e < VL; ++e) o[e] = 0.0f;
-#pragma unroll
-    for (int e = 0; e < VL; ++e) o[e] = add ? fmaf(scale, v[e], o[e]) : scale * v[e];
+using RawRow = typename VecT<T, VL>::type;
+template <typename T, int VL>
+__device__ __forceinline__ RawRow<T, VL> raw_row(const T* p) {
+    return *(const RawRow<T, VL>*)p;
+}
+template <typename T, int VL>
+__device__ __forceinline__ void put_row(T* p, const float (&o)[VL]) {
     if constexpr (VL == 1) {
         *p = from_f32<T>(o[0]);
     } else {
@@ -109,6 +109,16 @@ struct Grad {
     bool add;
 };
 
+// A row of the gradient while it is summed: old: what is there already, where it is added to.
+template <typename T, int VL>
+__device__ __forceinline__ void end_row(const Grad& g, uint32_t k, int col, const float (&acc)[VL],
+                                        const float (&old)[VL]) {
+    float o[VL];
+#pragma unroll
+    for (int e = 0; e < VL; ++e) o[e] = g.add ? fmaf(g.scale, acc[e], old[e]) : g.scale * acc[e];
+    put_row<T, VL>((T*)g.dtable + (int64_t)k * g.D + col, o);
+}
+
 // ------------------------------------------------------------------ few positions
 constexpr int kFew = 1024;
 
@@ -127,7 +137,8 @@ __global__ __launch_bounds__(kNT) void few_kernel(const int32_t* __restrict__ id
     const int col = ((int)blockIdx.y * kWave + lane) * VL;
     const bool live = col < g.D;
     const T* dout = (const T*)g.dout + col;
-    float acc[VL] = {};
+    float acc[VL] = {}, old[VL] = {};
+    if (g.add && live) read_row<T, VL>((const T*)g.dtable + (int64_t)id * g.D + col, old);
     for (int j0 = i & ~63; j0 < N; j0 += kWave) {
         const int j = j0 + lane;
         uint64_t m = __ballot(j >= i && j < N && all[j < N ? j : 0] == id);
@@ -149,10 +160,13 @@ __global__ __launch_bounds__(kNT) void few_kernel(const int32_t* __restrict__ id
                     for (int e = 0; e < VL; ++e) acc[e] += v[k][e];
         }
     }
-    if (live) write_row<T, VL>((T*)g.dtable + (int64_t)id * g.D + col, acc, g.scale, g.add);
+    if (live) end_row<T, VL>(g, (uint32_t)id, col, acc, old);
 }
 
 // ------------------------------------------------------------------ sorting positions by id
+// Where digit d's number lies in LDS: threads walk runs of digits, 16 numbers apart at most.
+__host__ __device__ inline int skew(int d) { return d + (d >> 4); }
+
 constexpr int kMaxBits = 12, kMaxBins = 1 << kMaxBits;
 constexpr int kMaxBlocks = 512;
 constexpr int kWaves = kNT / kWave;
@@ -199,12 +213,20 @@ __global__ __launch_bounds__(kNT) void count_kernel(Sort s, void* fill, int64_t 
         }
         return;
     }
+    constexpr int B = kTile / kNT;
+    const int64_t from = blockIdx.x * s.each + threadIdx.x;
+    const int64_t to = min(s.N, (int64_t)(blockIdx.x + 1) * s.each);
     for (int i = threadIdx.x; i < n; i += kNT) bins[i] = 0;
-    __syncthreads();
-    const int64_t from = blockIdx.x * s.each, to = min(s.N, from + s.each);
-#pragma unroll 4
-    for (int64_t i = from + threadIdx.x; i < to; i += kNT)
-        atomicAdd(&bins[sort_key(s, i) >> s.shift & (n - 1)], 1u);
+    for (int64_t i0 = from; i0 - threadIdx.x < to; i0 += B * kNT) {
+        uint32_t keys[B];
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            if (i0 + j * kNT < to) keys[j] = sort_key(s, i0 + j * kNT);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            if (i0 + j * kNT < to) atomicAdd(&bins[keys[j] >> s.shift & (n - 1)], 1u);
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kNT) s.counts[(int64_t)blockIdx.x * n + i] = bins[i];
 }
@@ -242,166 +264,277 @@ __global__ __launch_bounds__(1024) void offsets_kernel(Sort s) {
     if (w == 0) s.totals[bin] = whole;
 }
 
+// The lanes that have this lane's digit, of kBits bits, among the live ones.
+template <int kBits>
+__device__ __forceinline__ uint64_t alike(uint32_t d, bool live) {
+    const uint64_t all = __ballot(live);
+    uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+#pragma unroll
+    for (int b = 0; b < kBits; ++b) {
+        const uint32_t x = (uint32_t)((int32_t)(d << (31 - b)) >> 31);  // the bit in every place
+        const uint64_t m = __ballot(x != 0);
+        lo &= ~((uint32_t)m ^ x);
+        hi &= ~((uint32_t)(m >> 32) ^ x);
+    }
+    return (uint64_t)hi << 32 | lo;
+}
+
+// kBits: s.bits or more.
+template <int kBits>
 __global__ __launch_bounds__(kNT) void place_kernel(Sort s) {
-    __shared__ uint32_t next[kWaves][kMaxBins];  // a wave's next place of each digit
+    constexpr int B = kTile / kNT;  // positions of a lane that are read together
+    extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
     __shared__ uint32_t wsum[kWaves];
     const int n = 1 << s.bits, t = threadIdx.x, lane = t & 63, w = wave_id();
+    const int room = skew(n);
+    uint32_t* next = lds + w * room;                               // the wave's next places
+    uint32_t *first = lds + kWaves * room, *total = first + room;  // the block's first; all of them
     const uint64_t below = (1ull << lane) - 1;
-    for (int i = t; i < kWaves * n; i += kNT) next[i / n][i % n] = 0;
-    __syncthreads();
     // A wave's positions are one run of its block's.
-    const int64_t from = blockIdx.x * s.each + w * (s.each / kWaves);
-    const int64_t to = min(s.N, from + s.each / kWaves);
-#pragma unroll 4
-    for (int64_t i = from + lane; i < to; i += kWave)
-        atomicAdd(&next[w][sort_key(s, i) >> s.shift & (n - 1)], 1u);
+    const int64_t from = blockIdx.x * s.each + w * (s.each / kWaves) + lane;
+    const int64_t to = min(s.N, from - lane + s.each / kWaves);
+    uint32_t keys[B];
+#pragma unroll
+    for (int j = 0; j < B; ++j) keys[j] = from + j * kWave < to ? sort_key(s, from + j * kWave) : 0;
+    for (int i = 4 * t; i < kWaves * room; i += 4 * kNT) *(u4v*)(lds + i) = u4v{0, 0, 0, 0};
+    const uint32_t* counts = s.counts + (int64_t)blockIdx.x * n;
+    for (int i0 = t; i0 < n; i0 += 8 * kNT) {
+        uint32_t a[8], b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i0 + j * kNT < n) {
+                a[j] = counts[i0 + j * kNT];
+                b[j] = s.totals[i0 + j * kNT];
+            }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (i0 + j * kNT < n) {
+                first[skew(i0 + j * kNT)] = a[j];
+                total[skew(i0 + j * kNT)] = b[j];
+            }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < B; ++j)
+        if (from + j * kWave < to) atomicAdd(&next[skew(keys[j] >> s.shift & (n - 1))], 1u);
+    for (int64_t i = from + B * kWave; i < to; i += kWave)
+        atomicAdd(&next[skew(sort_key(s, i) >> s.shift & (n - 1))], 1u);
     __syncthreads();
     // Digits before a thread's run of digits, then each digit's first place for each wave.
     const int run = (n + kNT - 1) / kNT;
     uint32_t mine = 0;
-    for (int k = 0; k < run; ++k)
-        if (t * run + k < n) mine += s.totals[t * run + k];
-    uint32_t upto = lanes::wave_scan(mine, 0u, [](uint32_t a, uint32_t b) { return a + b; });
+#pragma unroll 8
+    for (int k = 0; k < run; ++k) mine += t * run + k < n ? total[skew(t * run + k)] : 0;
+    const uint32_t upto = lanes::wave_scan(mine, 0u, [](uint32_t a, uint32_t b) { return a + b; });
     if (lane == kWave - 1) wsum[w] = upto;
     __syncthreads();
     uint32_t at = upto - mine;
     for (int k = 0; k < w; ++k) at += wsum[k];
+#pragma unroll 4
     for (int k = 0; k < run; ++k) {
-        const int d = t * run + k;
-        if (d >= n) break;
-        uint32_t place = at + s.counts[(int64_t)blockIdx.x * n + d];
+        const int d = skew(t * run + k < n ? t * run + k : n - 1);
+        const bool in = t * run + k < n;
+        uint32_t c[kWaves], place = at + first[d];
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) c[v] = lds[v * room + d];
+#pragma unroll
         for (int v = 0; v < kWaves; ++v) {
-            const uint32_t c = next[v][d];
-            next[v][d] = place;
-            place += c;
+            if (in) lds[v * room + d] = place;
+            place += c[v];
         }
-        at += s.totals[d];
+        at += in ? total[d] : 0;
     }
     __syncthreads();
-    for (int64_t i0 = from; i0 < to; i0 += kWave) {
-        const int64_t i = i0 + lane;
-        const bool live = i < to;
-        const uint32_t key = live ? sort_key(s, i) : 0;
-        const uint32_t d = key >> s.shift & (n - 1);
-        uint64_t same = __ballot(live);
-        for (int b = 0; b < s.bits; ++b) {
-            const bool bit = d >> b & 1;
-            const uint64_t m = __ballot(bit);
-            same &= bit ? m : ~m;
+    for (int64_t i0 = from; i0 - lane < to; i0 += B * kWave) {
+        int32_t pos[B];
+        if (i0 != from) {
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+                keys[j] = i0 + j * kWave < to ? sort_key(s, i0 + j * kWave) : 0;
         }
-        if (live) {
-            const int rank = __popcll(same & below);
-            const uint32_t place = next[w][d] + rank;
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const int64_t i = i0 + j * kWave;
+            pos[j] = s.pos_in && i < to ? s.pos_in[i] : (int32_t)i;
+        }
+        uint64_t same[B];
+#pragma unroll
+        for (int j = 0; j < B; ++j)
+            same[j] = alike<kBits>(keys[j] >> s.shift & (n - 1), i0 + j * kWave < to);
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const int slot = skew(keys[j] >> s.shift & (n - 1));
+            if (i0 + j * kWave < to) {
+                const uint32_t place = next[slot] + __popcll(same[j] & below);
+                wave_fence();
+                if ((same[j] >> lane) == 1ull) next[slot] = place + 1;  // the last of its digit
+                s.keys[place] = keys[j];
+                s.pos[place] = pos[j];
+            }
             wave_fence();
-            if ((same >> lane) == 1ull) next[w][d] = place + 1;  // the last of its digit
-            s.keys[place] = key;
-            s.pos[place] = s.pos_in ? s.pos_in[i] : (int32_t)i;
         }
-        wave_fence();
     }
 }
 
 // ------------------------------------------------------------------ sums of runs
-constexpr int kPiece = 64;
+constexpr int kSumWaves = 16, kSumThreads = kSumWaves * kWave;
+constexpr int kPiece = 64, kGroup = kSumWaves * kPiece;  // positions to a wave, to a workgroup
 
-// part: for each piece, the sum of a run that came from before (slot 0) and of one that starts
-// here and goes on (slot 1).
+// part: for each workgroup, the sum of a run that came from before it (slot 0) and of one that
+// starts in it and goes on (slot 1).
 template <typename T, int VL>
-__global__ __launch_bounds__(kNT) void piece_kernel(const uint32_t* __restrict__ keys,
-                                                    const int32_t* __restrict__ pos, int64_t N,
-                                                    int64_t V, Grad g, float* part,
-                                                    int64_t pieces) {
-    const int64_t piece = (int64_t)blockIdx.x * 4 + wave_id();
-    if (piece >= pieces) return;
-    const int lane = threadIdx.x & 63;
-    const int64_t from = piece * kPiece, i = from + lane;
+__global__ __launch_bounds__(kSumThreads, 8) void sum_kernel(const uint32_t* __restrict__ keys,
+                                                          const int32_t* __restrict__ pos,
+                                                          int64_t N, int64_t V, Grad g,
+                                                          float* part) {
+    // Of each wave the same two sums, and whether it has them: 1 a run from before that ends here,
+    // 2 one that passes through, 4 one that starts here and goes on.
+    __shared__ float kept[kSumWaves][2][kWave * VL];
+    __shared__ int kinds[kSumWaves];
+    const int lane = threadIdx.x & 63, w = wave_id();
+    const int64_t from = (int64_t)blockIdx.x * kGroup + w * kPiece, i = from + lane;
     const uint32_t none = (uint32_t)V;
     const uint32_t key = i < N ? keys[i] : none;
     const uint32_t after = i + 1 < N ? keys[i + 1] : none;
     const int at = i < N ? pos[i] : 0;
-    const uint32_t before = from > 0 ? keys[from - 1] : none;
+    const uint32_t before = from > 0 && from <= N ? keys[from - 1] : none;
     const int live = __popcll(__ballot(key != none));  // sorted: the first ones
-    if (live == 0) return;
     const uint64_t ends = __ballot(key != after);
-    bool earlier = lanes::lane_of(key, 0) == before;  // this run came from before
+    bool earlier = live > 0 && lanes::lane_of(key, 0) == before;  // the run came from before
+    int kind = 0;
     const int col = ((int)blockIdx.y * kWave + lane) * VL;
     const bool in = col < g.D;
     const T* dout = (const T*)g.dout + col;
-    float* slot = part + piece * 2 * g.D + col;
+    T* dtable = (T*)g.dtable + col;
     float acc[VL] = {};
-    constexpr int B = 8;
-    for (int j0 = 0; j0 < live; j0 += B) {
-        float v[B][VL];
+    // Rows of eight positions, and what is there already of the items that end among them, are read
+    // before the eight before them are summed and written: reads issued behind a write would be
+    // waited for together with it.
+    constexpr int B = sizeof(RawRow<T, VL>) <= 4 ? 8 : 32 / (int)sizeof(RawRow<T, VL>);
+    struct Rows {  // as they lie in memory: as floats, bf16 rows would halve the waves that fit
+        RawRow<T, VL> v[B], old[B];
+    };
+    auto fetch = [&](Rows& x, int j0) {
 #pragma unroll
         for (int j = 0; j < B; ++j) {
-            const int r = __builtin_amdgcn_readlane(at, j0 + j);  // behind the last one: row 0
-            if (in) read_row<T, VL>(dout + (int64_t)r * g.D, v[j]);
+            const int r = __builtin_amdgcn_readlane(at, (j0 + j) & 63);  // behind the last one: any
+            if (in) x.v[j] = raw_row<T, VL>(dout + (int64_t)r * g.D);
         }
+        if (g.add)
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+                if (j0 + j < live && (ends >> (j0 + j) & 1) && in)
+                    x.old[j] = raw_row<T, VL>(dtable +
+                                              (int64_t)lanes::lane_of(key, j0 + j) * g.D);
+    };
+    auto use = [&](const Rows& x, int j0) {
 #pragma unroll
         for (int j = 0; j < B; ++j) {
             if (j0 + j >= live) break;
+            float v[VL];
+            unpack_vec<T, VL>(x.v[j], v);
 #pragma unroll
-            for (int e = 0; e < VL; ++e) acc[e] += v[j][e];
+            for (int e = 0; e < VL; ++e) acc[e] += v[e];
             if (ends >> (j0 + j) & 1) {
-                const uint32_t k = lanes::lane_of(key, j0 + j);
-                if (in) {
-                    if (earlier) {
+                if (earlier) {
+                    kind |= 1;
 #pragma unroll
-                        for (int e = 0; e < VL; ++e) slot[e] = acc[e];
-                    } else {
-                        write_row<T, VL>((T*)g.dtable + (int64_t)k * g.D + col, acc, g.scale,
-                                         g.add);
-                    }
+                    for (int e = 0; e < VL; ++e) kept[w][0][lane * VL + e] = acc[e];
+                } else if (in) {
+                    unpack_vec<T, VL>(x.old[j], v);
+                    end_row<T, VL>(g, lanes::lane_of(key, j0 + j), col, acc, v);
                 }
                 earlier = false;
 #pragma unroll
                 for (int e = 0; e < VL; ++e) acc[e] = 0.0f;
             }
         }
+    };
+    Rows even, odd;
+    if (live > 0) fetch(even, 0);
+    for (int j0 = 0; j0 < live; j0 += 2 * B) {
+        if (j0 + B < live) fetch(odd, j0 + B);
+        use(even, j0);
+        if (j0 + 2 * B < live) fetch(even, j0 + 2 * B);
+        use(odd, j0 + B);
     }
-    if (live == kPiece && !(ends >> 63) && in) {  // goes on
-        float* to = earlier ? slot : slot + g.D;
+    if (live == kPiece && !(ends >> 63)) {  // goes on
+        kind |= earlier ? 2 : 4;
 #pragma unroll
-        for (int e = 0; e < VL; ++e) to[e] = acc[e];
+        for (int e = 0; e < VL; ++e) kept[w][earlier ? 0 : 1][lane * VL + e] = acc[e];
+    }
+    if (lane == 0) kinds[w] = kind;
+    __syncthreads();
+    // A wave joins the run that starts in it, the first one also the run that came from before.
+    const auto join = [&](int u, bool goes, float* slot) {  // from wave u on, acc holds what is before
+        for (; goes && u < kSumWaves; ++u) {
+#pragma unroll
+            for (int e = 0; e < VL; ++e) acc[e] += kept[u][0][lane * VL + e];
+            goes = kinds[u] & 2;
+        }
+        if (goes) {
+            if (in)
+#pragma unroll
+                for (int e = 0; e < VL; ++e) slot[e] = acc[e];
+        }
+        return goes;
+    };
+    float* slot = part + (int64_t)blockIdx.x * 2 * g.D + col;
+    if (kind & 4) {
+        const uint32_t k = lanes::lane_of(key, kPiece - 1);
+        float old[VL];
+        if (g.add && in) read_row<T, VL>(dtable + (int64_t)k * g.D, old);
+#pragma unroll
+        for (int e = 0; e < VL; ++e) acc[e] = kept[w][1][lane * VL + e];
+        if (!join(w + 1, true, slot + g.D) && in) end_row<T, VL>(g, k, col, acc, old);
+    }
+    if (w == 0 && (kinds[0] & 3)) {
+#pragma unroll
+        for (int e = 0; e < VL; ++e) acc[e] = 0.0f;
+        if (!join(0, true, slot) && in)
+#pragma unroll
+            for (int e = 0; e < VL; ++e) slot[e] = acc[e];
     }
 }
 
 constexpr int kJoin = 512;
 
-// The workgroup of the piece in which a run starts that goes on: its parts in eight runs of
-// pieces, then these in order.
+// The workgroup of the group in which a run starts that goes on: its parts in eight runs of
+// groups, then these in order.
 template <typename T, int VL>
 __global__ __launch_bounds__(kJoin) void join_kernel(const uint32_t* __restrict__ keys, int64_t N,
                                                      int64_t V, Grad g, const float* part,
-                                                     int64_t pieces) {
+                                                     int64_t groups) {
     constexpr int W = kJoin / kWave;
     __shared__ float all[W][kWave * VL];
-    const int64_t p = blockIdx.x, last = p * kPiece + kPiece - 1;
+    const int64_t p = blockIdx.x, last = p * kGroup + kGroup - 1;
     if (last + 1 >= N) return;
     const uint32_t k = keys[last];
     if (k == (uint32_t)V || keys[last + 1] != k) return;
-    if (keys[p * kPiece] == k && p > 0 && keys[p * kPiece - 1] == k) return;  // from before
-    // The last piece whose first key is k: ever larger steps, then halves.
+    if (keys[p * kGroup] == k && p > 0 && keys[p * kGroup - 1] == k) return;  // from before
+    // The last group whose first key is k: ever larger steps, then halves.
     int64_t lo = p + 1, step = 1;
-    while (lo + step < pieces && keys[(lo + step) * kPiece] == k) {
+    while (lo + step < groups && keys[(lo + step) * kGroup] == k) {
         lo += step;
         step *= 2;
     }
-    int64_t hi = min(pieces, lo + step);  // keys[lo * kPiece] == k, and not at hi
+    int64_t hi = min(groups, lo + step);  // keys[lo * kGroup] == k, and not at hi
     while (hi - lo > 1) {
         const int64_t mid = (lo + hi) / 2;
-        if (keys[mid * kPiece] == k) lo = mid;
+        if (keys[mid * kGroup] == k) lo = mid;
         else hi = mid;
     }
     const int lane = threadIdx.x & 63, w = wave_id();
     const int col = ((int)blockIdx.y * kWave + lane) * VL;
     const bool in = col < g.D;
     const int64_t n = lo - p, run = n <= 16 ? n : (n + W - 1) / W;
-    float acc[VL] = {};
+    float acc[VL] = {}, old[VL] = {};
     if (in) {
-        if (w == 0)
+        if (w == 0) {
+            if (g.add) read_row<T, VL>((const T*)g.dtable + (int64_t)k * g.D + col, old);
 #pragma unroll
             for (int e = 0; e < VL; ++e) acc[e] = part[(p * 2 + 1) * g.D + col + e];
+        }
         const int64_t end = min(lo + 1, p + 1 + (w + 1) * run);
 #pragma unroll 8
         for (int64_t q = p + 1 + w * run; q < end; ++q)
@@ -417,13 +550,13 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const uint32_t* __restrict_
 #pragma unroll
                 for (int e = 0; e < VL; ++e) acc[e] += all[v][lane * VL + e];
     }
-    if (w == 0 && in) write_row<T, VL>((T*)g.dtable + (int64_t)k * g.D + col, acc, g.scale, g.add);
+    if (w == 0 && in) end_row<T, VL>(g, k, col, acc, old);
 }
 
 // ------------------------------------------------------------------ launches
 struct Plan {
     int passes, bits, blocks;
-    int64_t each, pieces;
+    int64_t each, groups;
     size_t keys[2], pos[2], counts, totals, part, bytes;
 };
 Plan plan(int64_t N, int64_t V, int64_t D) {
@@ -436,7 +569,7 @@ Plan plan(int64_t N, int64_t V, int64_t D) {
     int64_t each = (N + kMaxBlocks - 1) / kMaxBlocks;
     p.each = (each + kTile - 1) / kTile * kTile;
     p.blocks = (int)((N + p.each - 1) / p.each);
-    p.pieces = (N + kPiece - 1) / kPiece;
+    p.groups = (N + kGroup - 1) / kGroup;
     size_t at = 0;
     for (int i = 0; i < (p.passes > 1 ? 2 : 1); ++i) {
         p.keys[i] = at;
@@ -449,9 +582,21 @@ Plan plan(int64_t N, int64_t V, int64_t D) {
     p.totals = at;
     at += up((size_t)4 << p.bits);
     p.part = at;
-    at += up((size_t)p.pieces * 2 * D * 4);
+    at += up((size_t)p.groups * 2 * D * 4);
     p.bytes = at;
     return p;
+}
+
+int place_lds(int bits) { return (kWaves + 2) * skew(1 << bits) * 4; }
+
+template <int kBits>
+hipError_t launch_place(const Sort& s, hipStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    const hipError_t e =
+        allow_dynamic_lds((const void*)place_kernel<kBits>, place_lds(kBits), done);
+    if (e != hipSuccess) return e;
+    place_kernel<kBits><<<dim3((unsigned)s.blocks), kNT, place_lds(s.bits), st>>>(s);
+    return hipGetLastError();
 }
 
 // Columns of a lane: as many as a wave needs for a row, where rows take accesses that wide.
@@ -474,10 +619,9 @@ void launch_sums(const EmbedArgs& a, const Plan& pl, char* ws, const Grad& g, hi
     const uint32_t* keys = (const uint32_t*)(ws + pl.keys[last]);
     const int32_t* pos = (const int32_t*)(ws + pl.pos[last]);
     float* part = (float*)(ws + pl.part);
-    piece_kernel<T, VL><<<dim3((unsigned)((pl.pieces + 3) / 4), cols), kNT, 0, st>>>(
-        keys, pos, a.N, a.V, g, part, pl.pieces);
-    join_kernel<T, VL><<<dim3((unsigned)pl.pieces, cols), kJoin, 0, st>>>(keys, a.N, a.V, g, part,
-                                                                         pl.pieces);
+    const dim3 grid((unsigned)pl.groups, cols);
+    sum_kernel<T, VL><<<grid, kSumThreads, 0, st>>>(keys, pos, a.N, a.V, g, part);
+    join_kernel<T, VL><<<grid, kJoin, 0, st>>>(keys, a.N, a.V, g, part, pl.groups);
 }
 
 }  // namespace
@@ -535,7 +679,10 @@ hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t st) {
         const int64_t zeros = i ? 0 : fill;
         count_kernel<<<dim3((unsigned)(pl.blocks + zeros)), kNT, 0, st>>>(s, a.dst, bytes);
         offsets_kernel<<<dim3((unsigned)(((1 << pl.bits) + 63) / 64)), 1024, 0, st>>>(s);
-        place_kernel<<<dim3((unsigned)pl.blocks), kNT, 0, st>>>(s);
+        const hipError_t e = pl.bits <= 6   ? launch_place<6>(s, st)
+                             : pl.bits <= 9 ? launch_place<9>(s, st)
+                                            : launch_place<kMaxBits>(s, st);
+        if (e != hipSuccess) return e;
     }
     if (a.N > 0) {
         const Grad g{a.src, a.dst, (int)a.D, a.scale, a.accumulate};
