@@ -21,8 +21,6 @@
 // Larger ones: planes in the workspace, a launch a product over all matrices of the list.
 #include <hip/hip_runtime.h>
 
-#include <stdlib.h>
-
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -365,27 +363,22 @@ struct Large {
     int rows, cols;  // of X
     int mp, np;
     int ld, tall;
-    int first_chunk, first_pack;  // work before this matrix's, in each launch
-    int first_tile[2];            // of symmetric products, of the others
     int chunks;
 };
+enum Work { kSquares, kOthers, kChunks, kPacks };  // tiles of symmetric and other products, ...
 struct LargeTable {
+    int first[4][kMaxLarge];  // the matrices' first work of each kind; unused ones 2^31 - 1
     Large t[kMaxLarge];
     int count, eighths;
 };
 static_assert(sizeof(LargeTable) <= 3800, "kernel arguments end at 4 KB");
 
-// The matrix that work `at` is of; kFirst: tiles of symmetric products, of others, chunks, packs.
-template <int kFirst>
+// The matrix that work `at` is of.
+template <Work kKind>
 __device__ __forceinline__ int find(const LargeTable& tab, int at) {
     int k = 0;
 #pragma unroll
-    for (int i = 1; i < kMaxLarge; ++i) {
-        const Large& e = tab.t[i];
-        const int first = kFirst < 2 ? e.first_tile[kFirst & 1]
-                                     : kFirst == 2 ? e.first_chunk : e.first_pack;
-        k += i < tab.count && at >= first;
-    }
+    for (int i = 1; i < kMaxLarge; ++i) k += at >= tab.first[kKind][i];
     return __builtin_amdgcn_readfirstlane(k);
 }
 
@@ -404,8 +397,8 @@ template <typename T>
 __global__ __launch_bounds__(kNT) void momentum_kernel(LargeTable tab, Hyper h) {
     constexpr int B = 4;  // accesses of a thread on their way
     __shared__ double red[kNT / kWave];
-    const Large& e = tab.t[find<2>(tab, blockIdx.x)];
-    const int chunk = blockIdx.x - e.first_chunk;
+    const int at = find<kChunks>(tab, blockIdx.x), chunk = blockIdx.x - tab.first[kChunks][at];
+    const Large& e = tab.t[at];
     const int64_t from = (int64_t)chunk * kNormChunk + threadIdx.x * 4;
     const T* g = (const T*)e.g;
     const bool vec = takes_vectors(e.g, sizeof(T), e.m);
@@ -447,8 +440,9 @@ template <typename T>
 __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     __shared__ double red[kNT / kWave];
     __shared__ float tile[64][65];
-    const Large& e = tab.t[find<3>(tab, blockIdx.x)];
-    const int t = threadIdx.x, at = blockIdx.x - e.first_pack;
+    const int which = find<kPacks>(tab, blockIdx.x);
+    const Large& e = tab.t[which];
+    const int t = threadIdx.x, at = blockIdx.x - tab.first[kPacks][which];
     const int across = e.np / 64, r0 = at / across * 64, c0 = at % across * 64;  // of X
     // tile[a][b]: a along the parameter's rows
     const T* g = (const T*)e.g;
@@ -613,12 +607,13 @@ __global__ __launch_bounds__(G::kNT, 1) void product_kernel(LargeTable tab, int 
     // of each matrix's, so that none has the longest to itself.
     const int per = gridDim.x / 8, b = tab.eighths ? (int)blockIdx.x
                                                    : (int)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    const int k = find<kSquare ? 0 : 1>(tab, b);
+    constexpr Work kWork = kSquare ? kSquares : kOthers;
+    const int k = find<kWork>(tab, b);
     const Large& e = tab.t[k];
     const int down = (e.mp + G::kI - 1) / G::kI;
     const int across = kSquare ? down : (e.np + G::kJ - 1) / G::kJ;
     const int tiles = kSquare ? down * (down + 1) / 2 : down * across;
-    const int l = b - e.first_tile[kSquare ? 0 : 1], eighth = (tiles + 7) / 8;
+    const int l = b - tab.first[kWork][k], eighth = (tiles + 7) / 8;
     const int at = tab.eighths ? (l & 7) * eighth + (l >> 3) : l;
     if (at >= tiles || (tab.eighths && (l >> 3) >= eighth)) return;
     int ti, tj;  // tile row and column
@@ -854,8 +849,6 @@ constexpr Choice kChoices[] = {{64, 512, 0.50f, 4.0f},
                                {128, 512, 1.45f, 8.0f},
                                {256, 256, 2.50f, 28.0f}};
 int choose(const LargeTable& tab, bool square, bool gram) {
-    static const int force = getenv("MUON_SIDE") ? atoi(getenv("MUON_SIDE")) : -1;
-    if (force >= 0) return force;
     int best = 0;
     float least = 0.0f;
     for (int c = 0; c < 4; ++c) {
@@ -889,7 +882,7 @@ hipError_t run_product(LargeTable& tab, int from, hipStream_t st) {
     tab.eighths = all > 256;
     int64_t groups = 0;
     for (int i = 0; i < tab.count; ++i) {
-        tab.t[i].first_tile[kSquare ? 0 : 1] = (int)groups;
+        tab.first[kSquare ? kSquares : kOthers][i] = (int)groups;
         const int64_t n = tiles_of(tab.t[i], kSquare, G::kI);
         groups += tab.eighths ? (n + 7) / 8 * 8 : n;
     }
@@ -953,10 +946,11 @@ hipError_t run(const recblr_muon_tensor* tensors, int64_t count, const MuonHyper
         // Those with the longest products first: their tiles are the last to end.
         std::stable_sort(large.t, large.t + large.count,
                          [](const Large& a, const Large& b) { return a.np > b.np; });
+        for (auto& kind : large.first) std::fill(kind, kind + kMaxLarge, 0x7FFFFFFF);
         for (int i = 0; i < large.count; ++i) {
             Large& l = large.t[i];
-            l.first_chunk = work[0];
-            l.first_pack = work[1];
+            large.first[kChunks][i] = work[0];
+            large.first[kPacks][i] = work[1];
             work[0] += l.chunks;
             work[1] += l.mp / 64 * (l.np / 64);
         }

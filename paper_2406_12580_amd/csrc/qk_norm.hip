@@ -397,8 +397,13 @@ Params params_of(const QkNormArgs& a) {
     p.R = a.rotate;
     p.share = a.share;
     p.eps = a.eps;
-    for (int i = 0; i < a.rotate / 2; ++i)
-        p.rate[i] = pow(a.base, -2.0 * i / a.rotate) / 6.283185307179586476925;
+    // Every eighth power as it is, those between by products: a call has up to 128 of them.
+    double between[8];
+    for (int i = 0; i < 8 && i < a.rotate / 2; ++i) between[i] = pow(a.base, -2.0 * i / a.rotate);
+    for (int i = 0; i < a.rotate / 2; i += 8) {
+        const double at = pow(a.base, -2.0 * i / a.rotate) / 6.283185307179586476925;
+        for (int j = 0; j < 8 && i + j < a.rotate / 2; ++j) p.rate[i + j] = at * between[j];
+    }
     return p;
 }
 

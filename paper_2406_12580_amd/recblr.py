@@ -890,6 +890,11 @@ def _tokens(t, dtype, index, name):
     return t.data_ptr(), H * D if pitch is None else pitch
 
 
+def _dense_like(t):
+    return torch.empty_like(t) if t.is_contiguous() else \
+        torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps):
     """The arguments that qk_norm and qk_norm_backward share, as two lists around the outputs."""
     dt, at, f32 = q.dtype, q.get_device(), torch.float32
@@ -923,8 +928,7 @@ def qk_norm(q, k, wq=None, wk=None, positions=None, rotate=None, base=10000.0, n
     norm is "rms" or "l2" (length one, as the gated delta rule takes them); of each head the first
     `rotate` elements are turned (None: all of an even width; 0: none).  Returns (q, k), dense."""
     before, after, _keep = _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps)
-    qn = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    kn = torch.empty(k.shape, dtype=q.dtype, device=q.device)
+    qn, kn = _dense_like(q), _dense_like(k)
     _check(recblr_qk_norm_forward(*before, qn.data_ptr(), kn.data_ptr(), *after, _stream()),
            "recblr_qk_norm_forward")
     return qn, kn
@@ -940,11 +944,10 @@ def qk_norm_backward(q, k, dqn, dkn, wq=None, wk=None, positions=None, rotate=No
     of its outputs.  Returns a dict with dq, dk (dense) and dwq, dwk float32 (None without
     weights)."""
     before, after, _keep = _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps)
-    dt, at, dev, D = q.dtype, q.get_device(), q.device, q.shape[-1]
-    out = {"dq": torch.empty(q.shape, dtype=dt, device=dev),
-           "dk": torch.empty(k.shape, dtype=dt, device=dev),
-           "dwq": None if wq is None else torch.empty(D, dtype=torch.float32, device=dev),
-           "dwk": None if wk is None else torch.empty(D, dtype=torch.float32, device=dev)}
+    dt, at, dev = q.dtype, q.get_device(), q.device
+    out = {"dq": _dense_like(q), "dk": _dense_like(k),
+           "dwq": None if wq is None else torch.empty_like(wq),
+           "dwk": None if wk is None else torch.empty_like(wk)}
     n = 0
     if wq is not None or wk is not None:
         n = _qk_norm_workspace_size(*after[:4], after[-1])
@@ -977,7 +980,7 @@ def policy_loss(logits, ids, old_logp, advantage, ref_logp=None, weight=None, te
     N, V = logits.shape
     io, dt, dev, at, f32 = io_code(logits.dtype), logits.dtype, logits.device,         logits.get_device(), torch.float32
     loss = torch.empty(1, dtype=f32, device=dev)
-    logp = torch.empty(N, dtype=f32, device=dev)
+    logp = torch.empty_like(old_logp)
     if out is None and need_grad:
         out = torch.empty_like(logits)
     n = _policy_workspace_size(N, V, io)
