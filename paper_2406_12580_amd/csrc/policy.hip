@@ -18,6 +18,7 @@
 // 2048 x 3416 fp32: 11 us of kernel, 17 of the call from Python.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include "device_common.hpp"
@@ -41,8 +42,8 @@ struct Params {
     void* dlogits;
     float* row_loss;
     int64_t N, V;
-    float T, inv_T, k2;  // temperature; 1 / T; log2(e) / T
-    float lo, hi, kl;    // borders of the ratio
+    float T, inv_T, k, k_lo;  // temperature; 1 / T; log2(e) / T in two parts
+    float lo, hi, kl;         // borders of the ratio; the KL term's weight
 };
 
 // ------------------------------------------------------------------ a row's loss
@@ -50,20 +51,33 @@ struct RowLoss {
     float lp, loss, c;  // c: d loss / d logp, over T
 };
 
-// Powers of a row: e^((l - M) / T) = 2^(l k - mk), one fma before the power.  mk is M k rounded;
-// what that leaves is common to all powers of the row, and `shift` gives it back to log S.  Where
-// M k is so large that it would be more than 2^-5, the difference is formed first.
+// a b as a float: never part of an fma with what is done to it, since others take it as it is.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+// Powers of a row: e^((l - M) / T) = 2^(l K - mk), K = log2(e) / T as two floats, k and the
+// positive rest k_lo (which keeps -inf what it is): rounded to one, K would move log S by the mean
+// of (l - M) / T times 2^-25, and ratios with it.  mk is M k rounded; what that leaves is common to
+// all powers of the row, and `shift` gives it back to log S.  Where M k is so large that it would
+// be more than 2^-5, the difference is formed first.
 struct Powers {
-    float M, k, mk;
+    float M, k, k_lo, mk;
     bool far;
     double shift;
-    __device__ __forceinline__ Powers(float M_, float k_) : M(M_), k(k_), mk(M_ * k_) {
+    __device__ __forceinline__ Powers(float M_, float k_, float k_lo_)
+        : M(M_), k(k_), k_lo(k_lo_), mk(rounded_product(M_, k_)) {
         far = !(fabsf(mk) < 0x1p20f);
-        shift = far ? 0.0 : ((double)M * (double)k - (double)mk) * 0.6931471805599453094;
+        shift = far ? 0.0
+                    : ((double)M * ((double)k + (double)k_lo) - (double)mk) * 0.6931471805599453094;
+    }
+    __device__ __forceinline__ static float to(float l, float k, float k_lo, float mk) {
+        return fast_exp2(fmaf(l, k_lo, fmaf(l, k, -mk)));
     }
     template <bool kFar>
     __device__ __forceinline__ float of(float l) const {
-        return fast_exp2(kFar ? (l - M) * k : fmaf(l, k, -mk));
+        return kFar ? to(l - M, k, k_lo, 0.0f) : to(l, k, k_lo, mk);
     }
     // f, told which of the two it is.
     template <typename F>
@@ -72,9 +86,9 @@ struct Powers {
     }
 };
 
-// xa: the chosen item's logit; S: the sum of powers, infinite only by a logit of +inf.  In 64 bits: the ratio is the power of a difference of two numbers
-// of ten or so, whose roundings to fp32 were most of the loss's error.  A NaN passes every
-// comparison on to a product with it.
+// xa: the chosen item's logit; S: the sum of powers, infinite only by a logit of +inf.  In 64 bits:
+// the ratio is the power of a difference of two numbers of ten or so, whose roundings to fp32 were
+// most of the loss's error.  A NaN passes every comparison on to a product with it.
 __device__ __forceinline__ RowLoss row_loss(const Params& p, int64_t row, float xa,
                                             const Powers& w2, float S) {
     const double sum = S < __builtin_inff() ? (double)S : __builtin_nan("");
@@ -236,7 +250,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void row_kernel(Params p) {
     const float M = over_row<TH>(fmaxf(m, xe), -__builtin_inff(), red, larger);
 #pragma unroll
     for (int j = 0; j < NV; ++j) x[j].packed();
-    const Powers pw(M, p.k2);
+    const Powers pw(M, p.k, p.k_lo);
     pw.use([&](auto far) {
         constexpr bool kFar = decltype(far)::value;
         float s = pw.of<kFar>(xe);
@@ -281,8 +295,8 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void row_kernel(Params p) {
 // `vecs`; the reference starts at `low`, where nothing that counts can lie beside a row's maximum
 // above it.  B vectors at a time.
 template <int TH, typename T, bool VEC>
-__device__ __forceinline__ void running_sum(const T* body, int vecs, int t, float k, float& m,
-                                            float& mk, float& s) {
+__device__ __forceinline__ void running_sum(const T* body, int vecs, int t, float k, float k_lo,
+                                            float& m, float& mk, float& s) {
     constexpr int U = Span<T, VEC>::U, B = 4;
     for (int i = t; i < vecs; i += B * TH) {
         Raw<T, VEC> x[B];
@@ -296,26 +310,26 @@ __device__ __forceinline__ void running_sum(const T* body, int vecs, int t, floa
         for (int j = 0; j < B; ++j)
 #pragma unroll
             for (int e = 0; e < U; ++e) top = fmaxf(top, x[j].get(e));
-        const float now = top * k;
+        const float now = rounded_product(top, k);
         s *= fast_exp2(mk - now);
         m = top;
         mk = now;
 #pragma unroll
         for (int j = 0; j < B; ++j)
 #pragma unroll
-            for (int e = 0; e < U; ++e) s += fast_exp2(fmaf(x[j].get(e), k, -mk));
+            for (int e = 0; e < U; ++e) s += Powers::to(x[j].get(e), k, k_lo, mk);
     }
 }
 // The row's powers and, in S, their sum; xe: one element of the thread's beside its vectors.
 template <int TH, typename T, bool VEC>
 __device__ __forceinline__ Powers sum_of(const T* body, int vecs, int t, float xe, float k,
-                                         float* red, float& S) {
+                                         float k_lo, float* red, float& S) {
     constexpr int U = Span<T, VEC>::U;
     const float none = -__builtin_inff(), low = -0x1p19f / k;
-    float m = fmaxf(low, xe), mk = m * k, s = fast_exp2(fmaf(xe, k, -mk));
-    running_sum<TH, T, VEC>(body, vecs, t, k, m, mk, s);
+    float m = fmaxf(low, xe), mk = rounded_product(m, k), s = Powers::to(xe, k, k_lo, mk);
+    running_sum<TH, T, VEC>(body, vecs, t, k, k_lo, m, mk, s);
     float M = over_row<TH>(m, none, red, larger);
-    Powers pw(M, k);
+    Powers pw(M, k, k_lo);
     s *= fast_exp2(mk - pw.mk);
     if (M <= low || pw.far) {  // once more, with the maximum first
         m = xe;
@@ -326,15 +340,15 @@ __device__ __forceinline__ Powers sum_of(const T* body, int vecs, int t, float x
             for (int e = 0; e < U; ++e) m = fmaxf(m, x.get(e));
         }
         M = over_row<TH>(m, none, red, larger);
-        pw = Powers(M, k);
+        pw = Powers(M, k, k_lo);
         pw.far = true;
         pw.shift = 0.0;
-        s = fast_exp2((xe - M) * k);
+        s = pw.of<true>(xe);
         for (int i = t; i < vecs; i += TH) {
             Raw<T, VEC> x;
             x.keep(body, i);
 #pragma unroll
-            for (int e = 0; e < U; ++e) s += fast_exp2((x.get(e) - M) * k);
+            for (int e = 0; e < U; ++e) s += pw.of<true>(x.get(e));
         }
     }
     S = over_row<TH>(s, 0.0f, red, added);
@@ -367,7 +381,7 @@ __global__ __launch_bounds__(TH) void twice_kernel(Params p) {
     const float xa = id < p.V ? to_f32(base[id]) : quiet_nan();
     const float xe = VEC && extra >= 0 ? to_f32(base[extra]) : -__builtin_inff();
     float S;
-    const Powers pw = sum_of<TH, T, VEC>(body, sp.vecs, t, xe, p.k2, red, S);
+    const Powers pw = sum_of<TH, T, VEC>(body, sp.vecs, t, xe, p.k, p.k_lo, red, S);
     const RowLoss r = row_loss(p, row, xa, pw, S);
     if (t == 0) {
         p.row_loss[row] = r.loss;
@@ -435,15 +449,16 @@ __global__ __launch_bounds__(kPieceThreads) void part_kernel(Params p, Part* par
 #pragma unroll
             for (int e = 0; e < U; ++e) top = fmaxf(top, x[j].get(e));
         const float ref = top == none ? 0.0f : top;  // nothing but -inf so far: powers of 0
-        s *= fast_exp2((m - ref) * p.k2);
+        s *= Powers::to(m - ref, p.k, p.k_lo, 0.0f);
 #pragma unroll
         for (int j = 0; j < B; ++j)
 #pragma unroll
-            for (int e = 0; e < U; ++e) s += fast_exp2((x[j].get(e) - ref) * p.k2);
+            for (int e = 0; e < U; ++e)
+                s += Powers::to(x[j].get(e) - ref, p.k, p.k_lo, 0.0f);
         m = top;
     }
     const float M = over_row<TH>(m, none, red, larger);
-    s *= fast_exp2((m - (M == none ? 0.0f : M)) * p.k2);
+    s *= Powers::to(m - (M == none ? 0.0f : M), p.k, p.k_lo, 0.0f);
     const float S = over_row<TH>(s, 0.0f, red, added);
     if (t == 0) {
         parts[blockIdx.x] = Part{M, S};
@@ -486,11 +501,11 @@ __global__ __launch_bounds__(kPieceThreads) void joined_kernel(Params p, const P
     float s = 0.0f;
     for (int i = t; i < pieces; i += TH) {
         const Part q = parts[i];
-        if (q.s != 0.0f || M == none) s += q.s * fast_exp2((q.m - M) * p.k2);
+        if (q.s != 0.0f || M == none) s += q.s * Powers::to(q.m - M, p.k, p.k_lo, 0.0f);
     }
     const float S = over_row<TH>(s, 0.0f, red, added);
     // The pieces' sums are relative to their maxima as they are: nothing to give back to log S.
-    Powers pw(M, p.k2);
+    Powers pw(M, p.k, p.k_lo);
     const double shift = pw.shift;
     pw.shift = 0.0;
     const RowLoss r = row_loss(p, row, id < p.V ? chosen[row] : quiet_nan(), pw, S);
@@ -628,10 +643,12 @@ size_t policy_workspace(int64_t N, int64_t V, IoType io) { return layout(N, V, i
 hipError_t launch_policy_loss(const PolicyArgs& a, void* ws, hipStream_t st) {
     const Layout l = layout(a.N, a.V, a.io);
     char* w = (char*)ws;
+    const double K = 1.4426950408889634 / a.temperature;
+    float k = (float)K;
+    if ((double)k >= K) k = std::nextafterf(k, 0.0f);  // for a positive rest
     const Params p{a.logits, a.ids, a.old_logp, a.advantage, a.ref_logp, a.weight, a.logp,
                    a.dlogits, (float*)(w + l.rows), a.N, a.V, a.temperature, 1.0f / a.temperature,
-                   (float)(1.4426950408889634 / a.temperature), 1.0f - a.clip_low,
-                   1.0f + a.clip_high, a.kl};
+                   k, (float)(K - (double)k), 1.0f - a.clip_low, 1.0f + a.clip_high, a.kl};
     if (a.N > 0) {
         // Vectors need rows of both tensors to lie alike to 16 bytes.
         const bool vec =

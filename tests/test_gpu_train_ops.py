@@ -182,6 +182,28 @@ def test_embed_runs_at_piece_borders(rb, io, N):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_embed_runs_at_group_borders(rb, io):
+    """The same with groups of 1024 positions, that are added up by themselves."""
+    lengths, ids = [1024, 1023, 1, 1025, 2048, 2047, 2, 1024, 1, 3 * 1024, 3, 1021, 5120], []
+    for i, n in enumerate(lengths * 2):
+        ids += [i] * n
+    c = embed_case(io, len(ids), 100, 64, seed=2)
+    c["ids"] = np.asarray(ids)
+    check_embed(rb, c)
+    c["ids"] = np.random.default_rng(3).permutation(c["ids"])
+    check_embed(rb, c, add=True)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(1100000, 60000, 5), (1500000, 3, 3), (3000, 17000000, 1),
+                                  (1200000, 17000000, 2)])
+def test_embed_many(rb, io, size):
+    """More positions than the blocks take in one turn; tables of three digits."""
+    c = embed_case(io, *size, seed=4, zipf=size[1] < 100000)
+    check_embed(rb, c, scale=0.5)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("N", [30, 2500])
 def test_embed_ids_of_no_row(rb, io, N):
     """Ids behind the table, negative ones, the type's ends and padding (inside or outside)."""
@@ -496,7 +518,7 @@ def test_policy_rows_longer_than_registers(rb, io, V):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
-@pytest.mark.parametrize("size", [(7, 100), (5, 1000), (140, 3001), (3, 30000)])
+@pytest.mark.parametrize("size", [(7, 100), (5, 1000), (140, 3001), (3, 30000), (3, 140000)])
 @pytest.mark.parametrize("kl", [0.0, 0.5])
 def test_policy_left_out_rows(rb, io, size, kl):
     """Negative ids leave their rows out, whatever these hold; ids behind the last item are NaN."""
@@ -516,7 +538,7 @@ def test_policy_left_out_rows(rb, io, size, kl):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
-@pytest.mark.parametrize("size", [(6, 100), (6, 3001), (130, 3001), (6, 30000)])
+@pytest.mark.parametrize("size", [(6, 100), (6, 3001), (130, 3001), (6, 30000), (6, 140000)])
 def test_policy_masks(rb, io, size):
     """Masks by -inf and by the type's lowest value, all but the chosen item, all items alike at
     the lowest value, a masked chosen item; temperatures that make differences overflow."""
@@ -544,7 +566,7 @@ def test_policy_masks(rb, io, size):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
-@pytest.mark.parametrize("size", [(6, 100), (6, 3001), (130, 5000), (6, 30000)])
+@pytest.mark.parametrize("size", [(6, 100), (6, 3001), (130, 5000), (6, 30000), (6, 140000)])
 @pytest.mark.parametrize("v", [math.nan, math.inf, -math.inf])
 def test_policy_rows_without_odds(rb, io, size, v):
     """A NaN, a +inf or nothing but -inf in a row that counts: NaN there and in the loss alone."""
@@ -585,7 +607,7 @@ def test_policy_borders(rb):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
-@pytest.mark.parametrize("size", [(5, 300), (140, 3003), (3, 30001), (130, 70000)])
+@pytest.mark.parametrize("size", [(5, 300), (140, 3003), (3, 30001), (130, 70000), (3, 140001)])
 def test_policy_in_place(rb, io, size):
     """The gradient over the logits, at any alignment; another alignment than theirs; none."""
     import torch
@@ -606,6 +628,58 @@ def test_policy_in_place(rb, io, size):
         inplace = rb.policy_loss(*args(), **how, out=c["logits"])
         assert inplace[2] is c["logits"] and torch.equal(inplace[2], grad)
         assert torch.equal(inplace[0], loss)
+
+
+ROWS = [(6, 100), (6, 3001), (130, 5000), (6, 30000), (6, 140000)]  # each way to take a row
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", ROWS)
+@pytest.mark.parametrize("T", [1.0, 0.7])
+def test_policy_rows_of_one_value(rb, io, size, T):
+    """Odds are one in V, whatever the value.  All powers are alike and near one: a power is off
+    by its argument, U / 2 of at most 1/32, and by 2 ulps, and a chain of n equal terms by n U at
+    most, with n <= 128 a thread, 70 pieces and 16 levels between threads; ratios by that and the
+    roundings of logp's other side, U |log V|, and of three products."""
+    import torch
+    N, V = size
+    c = policy_case(io, N, V, masked=0.0)
+    values = np.array([1.0, -37.5, 999.0, 1234.5, -20000.0, 123456.0])
+    c["logits"][:] = torch.from_numpy(values[np.arange(N) % 6]).to(c["logits"].dtype).cuda()[:, None]
+    c["logits"][:, 0] = -math.inf
+    ids = 1 + c["ids"] % (V - 1)
+    old = torch.full((N,), -math.log(V - 1), device="cuda")
+    bar = (128 + 70 + 16 + 8 + abs(math.log(V))) * U
+    for row in range(6):
+        one = torch.zeros(N, device="cuda")
+        one[row] = 1.0
+        loss, logp, grad = rb.policy_loss(c["logits"], ints(ids), old, one, weight=one,
+                                          temperature=T)
+        print(row, abs(float(loss) + math.exp(-math.log(V - 1) - float(old[0]))) / bar)
+        assert abs(float(loss) + math.exp(-math.log(V - 1) - float(old[0]))) <= bar
+        assert np.allclose(host(logp), -math.log(V - 1), rtol=0, atol=bar + 2 * U * 12)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", ROWS)
+def test_policy_far_logits(rb, io, size):
+    """Logits of a few million, where 2^(l K) against M K would lose their differences, and rows
+    that lie so low beside a running sum's first reference; a temperature near the limits."""
+    import torch
+    N, V = size
+    for at, T in ((3e6, 1.0), (-3e6, 1.0), (-6e5, 0.8), (-4.5e5, 1.0), (3e5, 1.0), (1e30, 1e30), (-2.0, 1e-6)):
+        c = policy_case(io, N, V, seed=9)
+        step = max(abs(at) * 2.0 ** -20, abs(T)) if io == "f32" else max(abs(at) / 128, T)
+        x = at + step * torch.round(torch.from_numpy(
+            np.where(np.isinf(c["logits_"]), 0.0, c["logits_"])).cuda())
+        x[c["logits"] == -math.inf] = -math.inf
+        c["logits"].copy_(x)
+        c["logits_"] = host(c["logits"])
+        lp = ref.policy(c["logits_"], c["ids"], c["old_logp_"], c["advantage_"],
+                        temperature=float(np.float32(T)))["logp"]
+        for k, n in enumerate(("old_logp", "ref_logp")):
+            c[n], c[n + "_"] = put(lp + 0.2 * np.random.default_rng(k).normal(size=N))
+        check_policy(rb, c, T=float(np.float32(T)))
 
 
 @pytest.mark.parametrize("N", [16384, 16385, 40000])
@@ -699,6 +773,61 @@ MUON = [(1, 1), (1, 7), (7, 1), (2, 3), (31, 33), (32, 32), (33, 31), (64, 64), 
 def test_muon(rb, io, shape):
     print(io, shape, flush=True)
     check_muon(rb, muon_case(io, [shape]))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("shapes", [[(520, 1030)], [(1030, 520)], [(1500, 1500)], [(136, 1240)] * 16,
+                                    [(462, 532)] * 16, [(750, 790)] * 16, [(1160, 1320)] * 16,
+                                    [(1320, 1160)] * 4, [(2500, 2500)], [(4000, 4100)],
+                                    [(2001, 1999), (100, 2999), (777, 1301), (90, 80)]])
+def test_muon_large(rb, io, shapes):
+    """Each tile of each of the products, alone and for many matrices, against 64-bit products on
+    the GPU.  Four large directions make every product weigh in the first steps already, whose
+    bounds are small beside a part of a matrix that is wrong."""
+    import torch
+    torch.manual_seed(0)
+    draw = lambda *s: torch.randn(s, device="cuda")  # noqa: E731
+    for low, steps in ((True, 1), (True, 2), (False, 5)):
+        p = [draw(*s).to(dtype_of(io)) * 0.01 for s in shapes]
+        g = [(draw(s[0], 4) @ draw(4, s[1]) + 0.1 * draw(*s) if low else draw(*s)).to(dtype_of(io))
+             for s in shapes]
+        m = [0.1 * draw(*s) for s in shapes]
+        before = [(a.double(), b.double()) for a, b in zip(p, m)]
+        rb.Muon(p, lr=1.0, momentum=0.9, weight_decay=0.1, scale=0.3, state=m, steps=steps).step(g)
+        for i, (rows, cols) in enumerate(shapes):
+            p0, m0 = before[i]
+            m1 = 0.9 * m0 + 0.1 * g[i].double()
+            u = 0.9 * m1 + 0.1 * g[i].double()
+            x = u / (u.norm() + 1e-7)
+            x = x.t().contiguous() if rows > cols else x
+            norms = [float(x.norm())]
+            a, b, c = ref.NS
+            for _ in range(steps):
+                A = x @ x.t().contiguous()
+                x = a * x + (b * A + c * (A @ A)) @ x
+                norms.append(float(x.norm()))
+            x = x.t() if rows > cols else x
+            want = 0.9 * p0 - 0.3 * x
+            size = 0.9 * m0.abs() + 0.1 * g[i].double().abs()
+            assert ((m[i].double() - m1).abs() <= 4 * U * size).all()
+            off = float((p[i].double() - want).norm())
+            bound = 0.3 * (muon_bound(norms, max(rows, cols), steps)
+                           + 8 * U * float(size.norm() / u.norm()) * 3.9 ** steps) \
+                + (4 * U + LAST[io]) * float(p0.norm() + want.norm())
+            print(f"ERR {rows}x{cols} steps {steps}: {off / bound:.4f} of its bound, which is "
+                  f"{bound / 0.3 / norms[-1]:.1e} of x", flush=True)
+            assert off <= bound, (rows, cols)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [1, 2, 3])
+def test_muon_unaligned(rb, io, offset):
+    """Matrices that start anywhere."""
+    shapes = [(33, 40), (128, 128), (40, 33), (140, 260), (261, 140)]
+    c = muon_case(io, shapes, seed=7)
+    for name, t in (("p", io), ("g", io), ("m", "f32")):
+        c[name] = [put(a, t, offset)[0] for a in c[name + "_"]]
+    check_muon(rb, c)
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
@@ -824,7 +953,7 @@ def passes(rb, io, seed=0):
         out[f"qk {D}"] = lambda c=c, how=how: [
             *rb.qk_norm(c["q"], c["k"], **how()),
             *rb.qk_norm_backward(c["q"], c["k"], c["dq"], c["dk"], **how()).values()]
-    for size in ((40, 50), (130, 3000), (3, 30000)):
+    for size in ((40, 50), (130, 3000), (3, 30000), (3, 140000)):
         c = policy_case(io, *size, seed=seed)
         ids = ints(c["ids"])
         out[f"policy {size}"] = lambda c=c, ids=ids: list(rb.policy_loss(
