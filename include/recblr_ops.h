@@ -257,8 +257,8 @@ int recblr_policy_loss(const void* logits, const int32_t* ids, const float* old_
  * sizes, which the steps multiply, as they do singular values next to zero, by up to 485 in five
  * steps (fp32's own rounding, 2^-24, by as much).  A gradient and momentum of zeros
  * leaves X = 0; a NaN or an infinity reaches all of its own matrix and no other.
- * Errors: INVALID_ARGUMENT as recblr_adamw_update, also momentum outside [0, 1), eps <= 0,
- * steps < 1; UNSUPPORTED (io, steps > 64, rows or cols > 2^16, their product > 2^30,
+ * Errors: INVALID_ARGUMENT as recblr_adamw_update, also momentum outside [0, 1),
+ * eps < 1e-300, steps < 1; UNSUPPORTED (io, steps > 64, rows or cols > 2^16, their product > 2^30,
  * count > 2^20); WORKSPACE.  Matrices with rows or cols = 0 are passed over.  `tensors` is host
  * memory, read before the call returns.
  */

@@ -551,7 +551,8 @@ int recblr_muon_update(const recblr_muon_tensor* tensors, int64_t count, int io,
                        size_t ws_bytes, void* stream) {
     int st = muon_sizes(tensors, count, io);
     if (st) return st;
-    if (!(momentum >= 0.0 && momentum < 1.0) || !(eps > 0.0) || steps < 1)
+    // 2^12 / eps is held in 64 bits.
+    if (!(momentum >= 0.0 && momentum < 1.0) || !(eps >= 1e-300) || steps < 1)
         return RECBLR_ERR_INVALID_ARGUMENT;
     if (steps > 64) return RECBLR_ERR_UNSUPPORTED;
     if (count == 0) return RECBLR_OK;

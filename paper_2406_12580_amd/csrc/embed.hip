@@ -143,21 +143,24 @@ __global__ __launch_bounds__(kNT) void few_kernel(const int32_t* __restrict__ id
         const int j = j0 + lane;
         uint64_t m = __ballot(j >= i && j < N && all[j < N ? j : 0] == id);
         while (m) {
-            float v[4][VL];  // four rows' reads at once
-            int n = 0;
+            // Rows read at once; in place of those behind the last one, the first one's again.
+            constexpr int B = VL < 4 ? 16 : 8;
+            RawRow<T, VL> raw[B];
+            const int n = __popcll(m);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (!m) break;
-                const int at = j0 + __builtin_ctzll(m);
+            for (int k = 0; k < B; ++k) {
+                const int at = m ? j0 + __builtin_ctzll(m) : i;
                 m &= m - 1;
-                if (live) read_row<T, VL>(dout + (int64_t)at * g.D, v[k]);
-                n = k + 1;
+                if (live) raw[k] = raw_row<T, VL>(dout + (int64_t)at * g.D);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (k < n)
+            for (int k = 0; k < B; ++k) {
+                if (k >= n) break;
+                float v[VL];
+                unpack_vec<T, VL>(raw[k], v);
 #pragma unroll
-                    for (int e = 0; e < VL; ++e) acc[e] += v[k][e];
+                for (int e = 0; e < VL; ++e) acc[e] += v[e];
+            }
         }
     }
     if (live) end_row<T, VL>(g, (uint32_t)id, col, acc, old);

@@ -283,12 +283,12 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallTable tab, Hy
     __syncthreads();
     sum = 0.0;
     for (int k = 0; k < kSmallWaves; ++k) sum += red[k];
-    const float inv = (float)(1.0 / (sqrt(sum) + h.eps)) * kUp;
+    const double inv = (double)kUp / (sqrt(sum) + h.eps);  // beyond fp32 for the smallest norms
     float x[2][16];
 #pragma unroll
     for (int f = 0; f < 2; ++f)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[f][v] = in(f, v) ? U[at(f, v)] * inv : 0.0f;
+        for (int v = 0; v < 16; ++v) x[f][v] = in(f, v) ? (float)(U[at(f, v)] * inv) : 0.0f;
     __syncthreads();
     if (has) put_tile(X, xplane, xs, i0, j0, x, two, lane);
     __syncthreads();
@@ -463,12 +463,13 @@ __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     if ((t & 63) == 0) red[wave_id()] = sum;
     __syncthreads();
     sum = ((red[0] + red[1]) + red[2]) + red[3];
-    const float inv = (float)(1.0 / (sqrt(sum) + h.eps)) * kUp;
+    const double inv = (double)kUp / (sqrt(sum) + h.eps);  // beyond fp32 for the smallest norms
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-            tile[16 * j + (t >> 4)][4 * (t & 15) + x] = update_of(h, mv[j][x], gv[j][x]) * inv;
+            tile[16 * j + (t >> 4)][4 * (t & 15) + x] =
+                (float)(update_of(h, mv[j][x], gv[j][x]) * inv);
     __syncthreads();
     // Eight elements of a row of X, and of its transposed, at a time.
     auto put = [&](_Float16* to, int a, int b, bool turned) {

@@ -978,7 +978,8 @@ def policy_loss(logits, ids, old_logp, advantage, ref_logp=None, weight=None, te
     if kl > 0 and ref_logp is None:
         raise ValueError("kl > 0 needs ref_logp")
     N, V = logits.shape
-    io, dt, dev, at, f32 = io_code(logits.dtype), logits.dtype, logits.device,         logits.get_device(), torch.float32
+    io, dt, dev, at, f32 = io_code(logits.dtype), logits.dtype, logits.device, \
+        logits.get_device(), torch.float32
     loss = torch.empty(1, dtype=f32, device=dev)
     logp = torch.empty_like(old_logp)
     if out is None and need_grad:
@@ -1026,7 +1027,8 @@ class Muon:
         sizes = [p.numel() for p in self.params]
         each = lambda v: list(v) if isinstance(v, (list, tuple)) else [v] * len(sizes)  # noqa: E731
         decay = each(weight_decay)
-        scale = [max(1.0, r / c) ** 0.5 if c else 1.0 for r, c in self._shapes]             if scale is None else each(scale)
+        scale = [max(1.0, r / c) ** 0.5 if c else 1.0 for r, c in self._shapes] \
+            if scale is None else each(scale)
         if len(decay) != len(sizes) or len(scale) != len(sizes):
             raise ValueError("weight_decay and scale must be numbers or one for each parameter")
         if state is None:

@@ -869,7 +869,7 @@ def test_muon_zero_and_nan(rb):
     assert all(torch.isfinite(c["p"][i]).all() for i in (4, 5))
 
 
-@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e12, 1e30])
+@pytest.mark.parametrize("size", [1e-37, 1e-30, 1e-12, 1e12, 1e30, 5e37])
 def test_muon_scales(rb, size):
     """The update hangs on the gradient's direction alone, as far as eps lets it: its norm is
     formed in 64 bits, so no square over- or underflows."""
