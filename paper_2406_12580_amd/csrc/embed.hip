@@ -14,6 +14,11 @@
 // on the ids alone.
 //
 // Few positions: each wave looks for its position's id among all; the first of an id sums them.
+//
+// One MI355X: 409,600 positions of 64 fp32 over 3,416 items: lookup 19 us, 5.6 TB/s of what it
+// writes; gradient 53: counts with the table's zeros 7, offsets 6, places 15, sums 20 (5.3 TB/s),
+// joins 5.  524,288 of 128 bf16 over a million items: 48 and 98, of which its two passes of
+// digits are 45.  Lookups and sums are bound by memory, the rest by a launch's chain of reads.
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"
@@ -29,6 +34,8 @@ using wtile::u4v;
 constexpr int kNT = 256;
 
 // ------------------------------------------------------------------ lookup
+// Four 16-byte accesses to a thread, of whole rows where these are short; results past the caches,
+// where they would push the table out.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kNT) void lookup_kernel(const T* __restrict__ table,
                                                      const int32_t* __restrict__ ids,
@@ -120,6 +127,8 @@ __device__ __forceinline__ void end_row(const Grad& g, uint32_t k, int col, cons
 }
 
 // ------------------------------------------------------------------ few positions
+// 1024 positions of 64 fp32, all items different, in 11 us (37 by sorting); all the same in 52
+// (32), a chain of a wave.
 constexpr int kFew = 1024;
 
 template <typename T, int VL>
@@ -170,6 +179,8 @@ __global__ __launch_bounds__(kNT) void few_kernel(const int32_t* __restrict__ id
 // Where digit d's number lies in LDS: threads walk runs of digits, 16 numbers apart at most.
 __host__ __device__ inline int skew(int d) { return d + (d >> 4); }
 
+// 12 bits: 3,416 items in one pass of three launches, a million in two; the counts of four waves
+// still fit LDS (104 KB).
 constexpr int kMaxBits = 12, kMaxBins = 1 << kMaxBits;
 constexpr int kMaxBlocks = 512;
 constexpr int kWaves = kNT / kWave;
@@ -282,7 +293,8 @@ __device__ __forceinline__ uint64_t alike(uint32_t d, bool live) {
     return (uint64_t)hi << 32 | lo;
 }
 
-// kBits: s.bits or more.
+// kBits: s.bits or more.  200 blocks of 2,048 positions and 4,096 digits in 15 us, most of it
+// work on the digits' six arrays in LDS.
 template <int kBits>
 __global__ __launch_bounds__(kNT) void place_kernel(Sort s) {
     constexpr int B = kTile / kNT;  // positions of a lane that are read together
@@ -383,6 +395,7 @@ __global__ __launch_bounds__(kNT) void place_kernel(Sort s) {
 constexpr int kSumWaves = 16, kSumThreads = kSumWaves * kWave;
 constexpr int kPiece = 64, kGroup = kSumWaves * kPiece;  // positions to a wave, to a workgroup
 
+// Eight waves to a SIMD: 409,600 rows of 64 fp32 in 20 us, 5.3 TB/s.
 // part: for each workgroup, the sum of a run that came from before it (slot 0) and of one that
 // starts in it and goes on (slot 1).
 template <typename T, int VL>

@@ -13,9 +13,10 @@
 // pass against a running maximum; the second pass finds it in the last-level cache.  Few long
 // rows are cut into pieces: one launch leaves each piece's maximum and sum, a second joins them.
 //
-// One MI355X: 4096 x 131072 bf16 412 us, 5.2 TB/s of the logits and their gradient, where a large
-// copy reaches 4.7 to 6.2; the powers, two a logit, are 200 us of vector issue beside it.
-// 2048 x 3416 fp32: 11 us of kernel, 17 of the call from Python.
+// One MI355X: 4096 x 131072 bf16 417 to 450 us, 4.8 to 5.2 TB/s of the logits and their gradient,
+// where a large copy reaches 4.7 to 6.2; the powers, two a logit, are 200 us of vector issue beside
+// it.  2048 x 3416 fp32: 12 us of kernel, 16 of the call from Python.  Rows of which the chip holds
+// more than the last-level cache at once are read from memory twice: 400 x 1,000,000 bf16 441 us.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -570,7 +571,7 @@ struct Way {
 };
 
 // Rows of up to 16 KB stay in registers.  Longer ones are read twice, the second time from the
-// last-level cache: 4096 rows of 256 KB take 412 us so and 481 in the registers of 1024 threads,
+// last-level cache: 4096 rows of 256 KB take 417 us so and 481 in the registers of 1024 threads,
 // whose arithmetic then waits for loads and loads for it (one row to a compute unit); 8192 rows of
 // 32 KB 76 and 91, of 16 KB 76 and 55.  Few long rows are cut into pieces: 16 x 131072 bf16 22 us.
 Way way_of(int64_t N, int64_t V, IoType io, bool vec) {
