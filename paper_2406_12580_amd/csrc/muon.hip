@@ -85,7 +85,7 @@ __device__ __forceinline__ bool takes_vectors(const void* g, size_t e, const voi
 }
 
 // ------------------------------------------------------------------ small matrices
-constexpr int kSmallThreads = 512, kSmallWaves = kSmallThreads / kWave;
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / kWave;
 constexpr int kSmallLds = 150 * 1024;
 constexpr int kMaxSmall = 72;
 
@@ -111,89 +111,81 @@ size_t small_lds(int mp, int np) {
     return (size_t)4 * mp * (small_stride(np) + small_stride(mp));
 }
 
-// Operands of a wave's product of 64 x 32 by 16 of the contraction, from k on: p of rows (or, of
-// the transposed, columns) i0 .. + 63 of one matrix, q of rows j0 .. + 31 of the other.
+// A matrix of planes in LDS.
+struct Planes {
+    _Float16* at;
+    int plane, stride;
+};
+// Operands of a product of 32 x 32 by 16 of the contraction: p of rows (or, of the transposed,
+// columns) of one matrix, q of rows of the other.
 struct SmallFrags {
-    h8 p[2][2], q[2];
-    __device__ __forceinline__ static void row(h8 (&o)[2], const _Float16* m, int plane,
-                                               int stride, int row0, int k, int lane) {
-        const _Float16* a = m + (row0 + (lane & 31)) * stride + k + 8 * (lane >> 5);
+    h8 p[2], q[2];
+    __device__ __forceinline__ static void row(h8 (&o)[2], const _Float16* a, int plane) {
         o[0] = *(const h8*)a;
         o[1] = *(const h8*)(a + plane);
     }
-    __device__ __forceinline__ static void col(h8 (&o)[2], const _Float16* m, int plane,
-                                               int stride, int col0, int k, int lane) {
-        const _Float16* a = m + (k + 8 * (lane >> 5) + ((lane & 15) >> 2)) * stride + col0 +
-                            16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+    __device__ __forceinline__ static void col(h8 (&o)[2], const _Float16* a, int plane,
+                                               int stride) {
 #pragma unroll
         for (int pl = 0; pl < 2; ++pl, a += plane)
             o[pl] = __builtin_bit_cast(
                 h8, wtile::tr_pair((const char*)a, (const char*)(a + 4 * stride)));
     }
-    template <bool kTurned>
-    __device__ __forceinline__ void read(const _Float16* P, int pplane, int pstride, int i0,
-                                         bool both, const _Float16* Q, int qplane, int qstride,
-                                         int j0, int k, int lane) {
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-            if (f == 0 || both) {
-                if constexpr (kTurned) col(p[f], P, pplane, pstride, i0 + 32 * f, k, lane);
-                else row(p[f], P, pplane, pstride, i0 + 32 * f, k, lane);
-            }
-        row(q, Q, qplane, qstride, j0, k, lane);
-    }
-    __device__ __forceinline__ void multiply(f16v (&acc)[2], bool both) const {
-        acc[0] = mfma(p[0][0], q[1], acc[0]);
-        if (both) acc[1] = mfma(p[1][0], q[1], acc[1]);
-        acc[0] = mfma(p[0][1], q[0], acc[0]);
-        if (both) acc[1] = mfma(p[1][1], q[0], acc[1]);
-        acc[0] = mfma(p[0][0], q[0], acc[0]);
-        if (both) acc[1] = mfma(p[1][0], q[0], acc[1]);
-    }
 };
-// acc = sum over K (a multiple of 32) of p q; operands are read one step ahead.
+// The sum over K (a multiple of 32) of p q, the block at (i0, j0).  Operands are read one step
+// ahead, among the products.
 template <bool kTurned>
-__device__ __forceinline__ void small_product(f16v (&acc)[2], const _Float16* P, int pplane,
-                                              int pstride, int i0, bool both, const _Float16* Q,
-                                              int qplane, int qstride, int j0, int K, int lane) {
-    acc[0] = acc[1] = f16v{};
-    SmallFrags a, b;
-    auto read = [&](SmallFrags& f, int k) {
-        f.read<kTurned>(P, pplane, pstride, i0, both, Q, qplane, qstride, j0, k, lane);
+__device__ __forceinline__ f16v small_product(const Planes& P, int i0, const Planes& Q, int j0,
+                                              int K, int lane) {
+    const _Float16* q = Q.at + (j0 + (lane & 31)) * Q.stride + 8 * (lane >> 5);
+    const _Float16* p =
+        P.at + (kTurned ? (8 * (lane >> 5) + ((lane & 15) >> 2)) * P.stride + i0 +
+                              16 * ((lane >> 4) & 1) + 4 * (lane & 3)
+                        : (i0 + (lane & 31)) * P.stride + 8 * (lane >> 5));
+    f16v acc = {};
+    auto read_p = [&](SmallFrags& f, int k) {
+        if constexpr (kTurned) SmallFrags::col(f.p, p + k * P.stride, P.plane, P.stride);
+        else SmallFrags::row(f.p, p + k, P.plane);
     };
-    read(a, 0);
+    auto step = [&](const SmallFrags& now, SmallFrags& then, int k) {
+        SmallFrags::row(then.q, q + k, Q.plane);
+        acc = mfma(now.p[0], now.q[1], acc);
+        __builtin_amdgcn_sched_barrier(0);
+        read_p(then, k);
+        acc = mfma(now.p[1], now.q[0], acc);
+        __builtin_amdgcn_sched_barrier(0);
+        acc = mfma(now.p[0], now.q[0], acc);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    SmallFrags a, b;
+    SmallFrags::row(a.q, q, Q.plane);
+    read_p(a, 0);
     for (int k = 0; k < K; k += 32) {
-        read(b, k + 16);
-        __builtin_amdgcn_sched_barrier(0);
-        a.multiply(acc, both);
-        read(a, k + 32 < K ? k + 32 : 0);
-        __builtin_amdgcn_sched_barrier(0);
-        b.multiply(acc, both);
+        step(a, b, k + 16);
+        step(b, a, k + 32 < K ? k + 32 : 0);
     }
+    return acc;
 }
-// Accumulators of 64 x 32 from (i0, j0) on, as rows j of a matrix (i runs along them).
-__device__ __forceinline__ void put_tile(_Float16* m, int plane, int stride, int i0, int j0,
-                                         const float (&v)[2][16], bool both, int lane) {
-    _Float16* p = m + (j0 + (lane & 31)) * stride + i0 + 4 * (lane >> 5);
+// A block from (i0, j0) on, as rows j of a matrix (i runs along them).
+__device__ __forceinline__ void put_block(const Planes& M, int i0, int j0, const float (&v)[16],
+                                          int lane) {
+    _Float16* p = M.at + (j0 + (lane & 31)) * M.stride + i0 + 4 * (lane >> 5);
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
-        if (f == 0 || both)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float x[4] = {v[f][4 * q], v[f][4 * q + 1], v[f][4 * q + 2],
-                                    v[f][4 * q + 3]};
-                h4 hi, lo;
-                split(x, hi, lo);
-                *(h4*)(p + 32 * f + 8 * q) = hi;
-                *(h4*)(p + plane + 32 * f + 8 * q) = lo;
-            }
+    for (int q = 0; q < 4; ++q) {
+        const float x[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        h4 hi, lo;
+        split(x, hi, lo);
+        *(h4*)(p + 8 * q) = hi;
+        *(h4*)(p + M.plane + 8 * q) = lo;
+    }
 }
 
-// Walks the n elements of a matrix in the order of memory, V together, eight times V to a thread
+// Walks the n elements of a matrix in the order of memory, V together, kSlots times V to a thread
 // before the next ones: read(slot, i) of them, then use(slot, i, row, column).
+constexpr int kSlots = 4;
 template <int V, typename Read, typename Use>
 __device__ __forceinline__ void in_order(int n, int ld, Read read, Use use) {
-    constexpr int B = 8, kStep = kSmallThreads * V;
+    constexpr int B = kSlots, kStep = kSmallThreads * V;
     for (int i0 = threadIdx.x * V; i0 < n; i0 += B * kStep) {
 #pragma unroll
         for (int j = 0; j < B; ++j)
@@ -224,7 +216,7 @@ __device__ __forceinline__ void put(T* p, const float (&v)[V]) {
 template <typename T, int V>
 __device__ __forceinline__ double small_momentum(const Small& e, const Hyper& h, float* U,
                                                  int stride) {
-    float g[8][V], m[8][V];
+    float g[kSlots][V], m[kSlots][V];
     double sum = 0.0;
     in_order<V>(
         e.rows * e.cols, e.ld,
@@ -246,7 +238,7 @@ __device__ __forceinline__ double small_momentum(const Small& e, const Hyper& h,
 }
 template <typename T, int V>
 __device__ __forceinline__ void small_apply(const Small& e, const float* U, int stride) {
-    float p[8][V];
+    float p[kSlots][V];
     const float ls = e.ls * kDown;
     in_order<V>(
         e.rows * e.cols, e.ld, [&](int j, int i) { get<T, V>((const T*)e.p + i, p[j]); },
@@ -259,28 +251,30 @@ __device__ __forceinline__ void small_apply(const Small& e, const float* U, int 
 }
 
 // X, A and B are held times kUp.  The parameter, the gradient and the momentum are read and
-// written in the order of memory, through LDS: a wave's own elements of X lie in 64 rows, and
-// reading them from there took 21 of 76 us at 128 x 128.
+// written in the order of memory, through LDS: a wave's own elements of X lie in 32 rows, and
+// reading them from there took 21 of 76 us at 128 x 128.  A wave has a block of 32 x 32 of X, and
+// one of A: eight waves of two blocks each read less of LDS and took 51 us where sixteen of one
+// take 45 (64 x 64: 26 and 15).
 template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallTable tab, Hyper h) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ double red[kSmallWaves];
     const Small& e = tab.t[blockIdx.x];
     const int lane = threadIdx.x & 63, w = wave_id();
-    const int mp = e.mp, np = e.np, xs = small_stride(np), as = small_stride(mp);
-    const int xplane = mp * xs, aplane = mp * as;
-    _Float16* X = (_Float16*)smem;
-    _Float16* A = X + 2 * xplane;
+    const int mp = e.mp, np = e.np, mt = mp / 32;
+    Planes X, A;
+    X.stride = small_stride(np), X.plane = mp * X.stride, X.at = (_Float16*)smem;
+    A.stride = small_stride(mp), A.plane = mp * A.stride, A.at = X.at + 2 * X.plane;
     float* U = (float*)smem;  // the update in the parameter's order, before and after the products
     const int us = e.ld + 1;
-    // A wave has 64 of X's columns (or the last 32), i0 on, and 32 of its rows, j0 on: lane l has
-    // row j0 + l % 32 and of each 32 columns 8 (v / 4) + 4 (l / 32) + v % 4.  The same of A.
-    const int mt = mp / 32, i0 = w / mt * 64, j0 = w % mt * 32;
-    const bool has = i0 < np, two = i0 + 32 < np, has_a = i0 < mp, two_a = i0 + 32 < mp;
+    // Columns i0 on, rows j0 on: lane l has row j0 + l % 32 and of the columns
+    // 8 (v / 4) + 4 (l / 32) + v % 4.  The same of A.
+    const int i0 = w / mt * 32, j0 = w % mt * 32;
+    const bool has = i0 < np, has_a = i0 < mp;
     const int row = j0 + (lane & 31), col0 = i0 + 4 * (lane >> 5);
-    auto col = [&](int f, int v) { return col0 + 32 * f + 8 * (v >> 2) + (v & 3); };
-    auto at = [&](int f, int v) { return (e.tall ? col(f, v) : row) * us + (e.tall ? row : col(f, v)); };
-    auto in = [&](int f, int v) { return has && row < e.rows && col(f, v) < e.cols; };
+    auto col = [&](int v) { return col0 + 8 * (v >> 2) + (v & 3); };
+    auto at = [&](int v) { return (e.tall ? col(v) : row) * us + (e.tall ? row : col(v)); };
+    auto in = [&](int v) { return has && row < e.rows && col(v) < e.cols; };
     const bool vec = takes_vectors(e.g, sizeof(T), e.m) && takes_vectors(e.p, sizeof(T), e.m) &&
                      e.ld % 4 == 0;
     double sum = vec ? small_momentum<T, 4>(e, h, U, us) : small_momentum<T, 1>(e, h, U, us);
@@ -290,54 +284,42 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallTable tab, Hy
     sum = 0.0;
     for (int k = 0; k < kSmallWaves; ++k) sum += red[k];
     const double inv = (double)kUp / (sqrt(sum) + h.eps);  // beyond fp32 for the smallest norms
-    float x[2][16];
+    float x[16], a[16];
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) x[f][v] = in(f, v) ? (float)(U[at(f, v)] * inv) : 0.0f;
+    for (int v = 0; v < 16; ++v) x[v] = in(v) ? (float)(U[at(v)] * inv) : 0.0f;
     __syncthreads();
-    if (has) put_tile(X, xplane, xs, i0, j0, x, two, lane);
+    if (has) put_block(X, i0, j0, x, lane);
     __syncthreads();
     for (int step = 0; step < h.steps; ++step) {
-        float a[2][16];
-        f16v acc[2];
         if (has_a) {
-            small_product<false>(acc, X, xplane, xs, i0, two_a, X, xplane, xs, j0, np, lane);
+            const f16v acc = small_product<false>(X, i0, X, j0, np, lane);
 #pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) a[f][v] = acc[f][v] * kDown;
-            put_tile(A, aplane, as, i0, j0, a, two_a, lane);
+            for (int v = 0; v < 16; ++v) a[v] = acc[v] * kDown;
+            put_block(A, i0, j0, a, lane);
         }
         __syncthreads();
         if (has_a) {
-            small_product<false>(acc, A, aplane, as, i0, two_a, A, aplane, as, j0, mp, lane);
+            const f16v acc = small_product<false>(A, i0, A, j0, mp, lane);
 #pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) a[f][v] = fmaf(kC * kDown, acc[f][v], kB * a[f][v]);
+            for (int v = 0; v < 16; ++v) a[v] = fmaf(kC * kDown, acc[v], kB * a[v]);
         }
         __syncthreads();
-        if (has_a) put_tile(A, aplane, as, i0, j0, a, two_a, lane);
+        if (has_a) put_block(A, i0, j0, a, lane);
         __syncthreads();
         if (has) {
-            small_product<true>(acc, X, xplane, xs, i0, two, A, aplane, as, j0, mp, lane);
+            const f16v acc = small_product<true>(X, i0, A, j0, mp, lane);
 #pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) x[f][v] = fmaf(kDown, acc[f][v], kA * x[f][v]);
+            for (int v = 0; v < 16; ++v) x[v] = fmaf(kDown, acc[v], kA * x[v]);
         }
         if (step + 1 == h.steps) break;
         __syncthreads();
-        if (has) put_tile(X, xplane, xs, i0, j0, x, two, lane);
+        if (has) put_block(X, i0, j0, x, lane);
         __syncthreads();
     }
     __syncthreads();
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-            if (in(f, v)) U[at(f, v)] = x[f][v];
+    for (int v = 0; v < 16; ++v)
+        if (in(v)) U[at(v)] = x[v];
     __syncthreads();
     vec ? small_apply<T, 4>(e, U, us) : small_apply<T, 1>(e, U, us);
 }
@@ -816,8 +798,8 @@ Shape shape_of(const recblr_muon_tensor& t) {
     s.cols = (int)(s.tall ? t.rows : t.cols);
     s.mp = (s.rows + 31) / 32 * 32;
     s.np = (s.cols + 31) / 32 * 32;
-    // 64 x 32 of X, and of A, to each wave, and the planes in LDS.
-    s.small = (int64_t)(s.mp / 32) * ((s.np + 63) / 64) <= kSmallWaves &&
+    // A block of 32 x 32 to each wave, and the planes in LDS.
+    s.small = (int64_t)(s.mp / 32) * (s.np / 32) <= kSmallWaves &&
               small_lds(s.mp, s.np) <= (size_t)kSmallLds;
     if (!s.small) {
         s.mp = (s.rows + kPad - 1) / kPad * kPad;

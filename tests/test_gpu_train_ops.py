@@ -765,7 +765,7 @@ def check_muon(rb, c, lr=0.5, momentum=0.9, nesterov=True, wd=0.1, steps=5, scal
 # just beyond it, tall and wide.
 MUON = [(1, 1), (1, 7), (7, 1), (2, 3), (31, 33), (32, 32), (33, 31), (64, 64), (48, 96), (96, 48),
         (64, 256), (256, 64), (128, 128), (127, 129), (129, 127), (128, 136), (1, 512), (1, 513),
-        (512, 32), (32, 520), (128, 256), (200, 200), (300, 130), (130, 700), (1, 3000)]
+        (512, 32), (32, 520), (96, 160), (150, 90), (128, 256), (200, 200), (300, 130), (130, 700), (1, 3000)]
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
