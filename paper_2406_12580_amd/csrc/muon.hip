@@ -79,6 +79,19 @@ __device__ __forceinline__ float update_of(const Hyper& h, float m, float g) {
     return h.nesterov ? fmaf(h.mu, m, h.one_mu * g) : m;
 }
 
+// kUp over the norm and eps, as a factor from 1 to 2 and a power of two: it may lie beyond fp32.
+struct Inverse {
+    float by;
+    int power;
+    __device__ __forceinline__ void of(double squares, double eps) {
+        const double v = (double)kUp / (sqrt(squares) + eps);
+        const int e = ilogb(v);
+        power = e < -2000 ? -2000 : e > 2000 ? 2000 : e;  // of zero or a NaN: `by` stays what v is
+        by = (float)ldexp(v, -power);
+    }
+    __device__ __forceinline__ float times(float u) const { return ldexpf(u, power) * by; }
+};
+
 // Whether four elements of type T and of float from a multiple of four on are one access.
 __device__ __forceinline__ bool takes_vectors(const void* g, size_t e, const void* m) {
     return (((uintptr_t)g & (4 * e - 1)) | ((uintptr_t)m & 15)) == 0;
@@ -259,6 +272,7 @@ template <typename T>
 __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallTable tab, Hyper h) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ double red[kSmallWaves];
+    __shared__ Inverse inverse;
     const Small& e = tab.t[blockIdx.x];
     const int lane = threadIdx.x & 63, w = wave_id();
     const int mp = e.mp, np = e.np, mt = mp / 32;
@@ -281,13 +295,18 @@ __global__ __launch_bounds__(kSmallThreads) void small_kernel(SmallTable tab, Hy
     sum = lanes::wave_sum(sum);
     if (lane == 0) red[w] = sum;
     __syncthreads();
-    sum = 0.0;
-    for (int k = 0; k < kSmallWaves; ++k) sum += red[k];
-    const double inv = (double)kUp / (sqrt(sum) + h.eps);  // beyond fp32 for the smallest norms
+    if (w == 0) {  // one wave: in all of them its 64-bit arithmetic took 2 us
+        sum = 0.0;
+        for (int k = 0; k < kSmallWaves; ++k) sum += red[k];
+        if (lane == 0) inverse.of(sum, h.eps);
+    }
     float x[16], a[16];
 #pragma unroll
-    for (int v = 0; v < 16; ++v) x[v] = in(v) ? (float)(U[at(v)] * inv) : 0.0f;
+    for (int v = 0; v < 16; ++v) x[v] = in(v) ? U[at(v)] : 0.0f;
     __syncthreads();
+    const Inverse inv = inverse;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = inv.times(x[v]);
     if (has) put_block(X, i0, j0, x, lane);
     __syncthreads();
     for (int step = 0; step < h.steps; ++step) {
@@ -428,6 +447,7 @@ __global__ __launch_bounds__(kNT) void momentum_kernel(LargeTable tab, Hyper h) 
 template <typename T>
 __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     __shared__ double red[kNT / kWave];
+    __shared__ Inverse inverse;
     __shared__ float tile[64][65];
     const int which = find<kPacks>(tab, blockIdx.x);
     const Large& e = tab.t[which];
@@ -451,14 +471,15 @@ __global__ __launch_bounds__(kNT) void pack_kernel(LargeTable tab, Hyper h) {
     sum = lanes::wave_sum(sum);
     if ((t & 63) == 0) red[wave_id()] = sum;
     __syncthreads();
-    sum = ((red[0] + red[1]) + red[2]) + red[3];
-    const double inv = (double)kUp / (sqrt(sum) + h.eps);  // beyond fp32 for the smallest norms
+    if (t == 0) inverse.of(((red[0] + red[1]) + red[2]) + red[3], h.eps);
+    __syncthreads();
+    const Inverse inv = inverse;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
             tile[16 * j + (t >> 4)][4 * (t & 15) + x] =
-                (float)(update_of(h, mv[j][x], gv[j][x]) * inv);
+                inv.times(update_of(h, mv[j][x], gv[j][x]));
     __syncthreads();
     // Eight elements of a row of X, and of its transposed, at a time.
     auto put = [&](_Float16* to, int a, int b, bool turned) {
