@@ -16,7 +16,7 @@
 // Few positions: each wave looks for its position's id among all; the first of an id sums them.
 //
 // One MI355X: 409,600 positions of 64 fp32 over 3,416 items: lookup 19 us, 5.6 TB/s of what it
-// writes; gradient 53: counts with the table's zeros 7, offsets 6, places 15, sums 20 (5.3 TB/s),
+// writes; gradient 53: counts with the table's zeros 7, offsets 6, places 14, sums 20 (5.3 TB/s),
 // joins 5.  524,288 of 128 bf16 over a million items: 48 and 98, of which its two passes of
 // digits are 45.  Lookups and sums are bound by memory, the rest by a launch's chain of reads.
 #include <hip/hip_runtime.h>
@@ -185,6 +185,8 @@ constexpr int kMaxBits = 12, kMaxBins = 1 << kMaxBits;
 constexpr int kMaxBlocks = 512;
 constexpr int kWaves = kNT / kWave;
 constexpr int kTile = 2048;  // a block's positions are a multiple of this
+// Twice the waves that have positions, for the digits' work (256 threads: 15 us, not 14).
+constexpr int kPlaceThreads = 512, kEach = kMaxBins / kPlaceThreads;
 
 // ids of no row sort behind all others, as V.
 __device__ __forceinline__ uint32_t key_of(int32_t id, int64_t V, int32_t pad_id) {
@@ -293,39 +295,39 @@ __device__ __forceinline__ uint64_t alike(uint32_t d, bool live) {
     return (uint64_t)hi << 32 | lo;
 }
 
-// kBits: s.bits or more.  200 blocks of 2,048 positions and 4,096 digits in 15 us, most of it
-// work on the digits' six arrays in LDS.
+// kBits: s.bits or more.  200 blocks of 2,048 positions and 4,096 digits in 14 us: a third of it
+// ranks and scattered writes, a third the digits' six arrays in LDS, the rest first reads.
 template <int kBits>
-__global__ __launch_bounds__(kNT) void place_kernel(Sort s) {
-    constexpr int B = kTile / kNT;  // positions of a lane that are read together
+__global__ __launch_bounds__(kPlaceThreads) void place_kernel(Sort s) {
+    constexpr int TH = kPlaceThreads, B = kTile / (kWaves * kWave);  // positions read together
     extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
-    __shared__ uint32_t wsum[kWaves];
+    __shared__ uint32_t wsum[TH / kWave];
     const int n = 1 << s.bits, t = threadIdx.x, lane = t & 63, w = wave_id();
     const int room = skew(n);
     uint32_t* next = lds + w * room;                               // the wave's next places
     uint32_t *first = lds + kWaves * room, *total = first + room;  // the block's first; all of them
     const uint64_t below = (1ull << lane) - 1;
-    // A wave's positions are one run of its block's.
+    // The positions of each of the first waves are one run of the block's; the others have none.
     const int64_t from = blockIdx.x * s.each + w * (s.each / kWaves) + lane;
-    const int64_t to = min(s.N, from - lane + s.each / kWaves);
+    const int64_t to = w < kWaves ? min(s.N, from - lane + s.each / kWaves) : 0;
     uint32_t keys[B];
 #pragma unroll
     for (int j = 0; j < B; ++j) keys[j] = from + j * kWave < to ? sort_key(s, from + j * kWave) : 0;
-    for (int i = 4 * t; i < kWaves * room; i += 4 * kNT) *(u4v*)(lds + i) = u4v{0, 0, 0, 0};
+    for (int i = 4 * t; i < kWaves * room; i += 4 * TH) *(u4v*)(lds + i) = u4v{0, 0, 0, 0};
     const uint32_t* counts = s.counts + (int64_t)blockIdx.x * n;
-    for (int i0 = t; i0 < n; i0 += 8 * kNT) {
-        uint32_t a[8], b[8];
+    for (int i0 = t; i0 < n; i0 += kEach * TH) {
+        uint32_t a[kEach], b[kEach];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i0 + j * kNT < n) {
-                a[j] = counts[i0 + j * kNT];
-                b[j] = s.totals[i0 + j * kNT];
+        for (int j = 0; j < kEach; ++j)
+            if (i0 + j * TH < n) {
+                a[j] = counts[i0 + j * TH];
+                b[j] = s.totals[i0 + j * TH];
             }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (i0 + j * kNT < n) {
-                first[skew(i0 + j * kNT)] = a[j];
-                total[skew(i0 + j * kNT)] = b[j];
+        for (int j = 0; j < kEach; ++j)
+            if (i0 + j * TH < n) {
+                first[skew(i0 + j * TH)] = a[j];
+                total[skew(i0 + j * TH)] = b[j];
             }
     }
     __syncthreads();
@@ -336,7 +338,7 @@ __global__ __launch_bounds__(kNT) void place_kernel(Sort s) {
         atomicAdd(&next[skew(sort_key(s, i) >> s.shift & (n - 1))], 1u);
     __syncthreads();
     // Digits before a thread's run of digits, then each digit's first place for each wave.
-    const int run = (n + kNT - 1) / kNT;
+    const int run = (n + TH - 1) / TH;
     uint32_t mine = 0;
 #pragma unroll 8
     for (int k = 0; k < run; ++k) mine += t * run + k < n ? total[skew(t * run + k)] : 0;
@@ -360,6 +362,7 @@ __global__ __launch_bounds__(kNT) void place_kernel(Sort s) {
         at += in ? total[d] : 0;
     }
     __syncthreads();
+    if (w >= kWaves) return;
     for (int64_t i0 = from; i0 - lane < to; i0 += B * kWave) {
         int32_t pos[B];
         if (i0 != from) {
@@ -611,7 +614,7 @@ hipError_t launch_place(const Sort& s, hipStream_t st) {
     const hipError_t e =
         allow_dynamic_lds((const void*)place_kernel<kBits>, place_lds(kBits), done);
     if (e != hipSuccess) return e;
-    place_kernel<kBits><<<dim3((unsigned)s.blocks), kNT, place_lds(s.bits), st>>>(s);
+    place_kernel<kBits><<<dim3((unsigned)s.blocks), kPlaceThreads, place_lds(s.bits), st>>>(s);
     return hipGetLastError();
 }
 

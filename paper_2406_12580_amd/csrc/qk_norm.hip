@@ -15,7 +15,7 @@
 //
 // Bound by memory.  One MI355X: 204,800 tokens of 2 + 2 heads of 64 bf16, 210 MB forward, 45 us
 // (4.7 TB/s); backward with weights 67 us (4.7 TB/s) and 5 for the weights' sums.  131,072 of 4 + 2
-// heads of 128 fp32, 805 MB: 152 and 230 us (5.3 TB/s).  Heads read one ahead, and results written
+// heads of 128 fp32, 805 MB: both together 361 us (5.6 TB/s).  Heads read one ahead, and results written
 // past the caches, measured the same.
 #include <hip/hip_runtime.h>
 
@@ -351,11 +351,11 @@ __global__ __launch_bounds__(1024) void weights_kernel(const float* part, int ro
 }
 
 // ------------------------------------------------------------------ launches
-// Workgroups: as many as there are tokens to take, at most eight to a compute unit; the rows of
-// partial sums four.
+// Workgroups: as many as there are tokens to take (with eight to a compute unit that go on,
+// 131,072 tokens took 379 us, not 361); rows of partial sums four to a compute unit at most.
 int64_t groups_of(int64_t tokens_each, int64_t N, bool sums) {
-    const int64_t need = (N + tokens_each - 1) / tokens_each, most = sums ? 1024 : 2048;
-    return need < most ? need : most;
+    const int64_t need = (N + tokens_each - 1) / tokens_each;
+    return sums && need > 1024 ? 1024 : need;
 }
 
 // Lanes to a token's heads, where all runs of 16 bytes are aligned; 0: the other kernel.
