@@ -231,7 +231,8 @@ int recblr_qk_norm_backward(const void* q, const void* k, int64_t q_pitch, int64
  * row that is counted, only -inf, a NaN or a +inf make logp, dlogits and the loss NaN.  A
  * chosen item that is masked by -inf has logp -inf: with kl = 0 its ratio is 0; with kl > 0
  * its loss is inf and its gradient not finite.  An advantage of 0 has no surrogate whatever r is.
- * The loss is summed in 64 bits in a fixed order.
+ * A row's numbers are formed in 64 bits, its powers in fp32; the loss is summed in 64 bits in a
+ * fixed order.
  * Errors: INVALID_ARGUMENT (also a temperature outside [1e-30, 1e30], clip_low, clip_high or
  * kl < 0 or infinite, any of them NaN, kl > 0 without ref_logp, V = 0 with N > 0); UNSUPPORTED (io,
  * V > 2^24, N >= 2^22, N ceil(V / 2048) >= 2^24); WORKSPACE.
@@ -240,7 +241,7 @@ size_t recblr_policy_loss_workspace_size(int64_t N, int64_t V, int io);
 int recblr_policy_loss(const void* logits, const int32_t* ids, const float* old_logp,
                        const float* advantage, const float* ref_logp, const float* weight,
                        float* loss, float* logp, void* dlogits, int64_t N, int64_t V,
-                       float temperature, float clip_low, float clip_high, float kl, int io,
+                       double temperature, double clip_low, double clip_high, double kl, int io,
                        void* ws, size_t ws_bytes, void* stream);
 
 /*

@@ -489,15 +489,16 @@ size_t recblr_policy_loss_workspace_size(int64_t N, int64_t V, int io) {
 int recblr_policy_loss(const void* logits, const int32_t* ids, const float* old_logp,
                        const float* advantage, const float* ref_logp, const float* weight,
                        float* loss, float* logp, void* dlogits, int64_t N, int64_t V,
-                       float temperature, float clip_low, float clip_high, float kl, int io,
+                       double temperature, double clip_low, double clip_high, double kl, int io,
                        void* ws, size_t ws_bytes, void* stream) {
     int st = policy_sizes(N, V, io);
     if (st) return st;
-    if (!(temperature >= 1e-30f && temperature <= 1e30f)) return RECBLR_ERR_INVALID_ARGUMENT;
-    for (float x : {clip_low, clip_high, kl})
-        if (!(x >= 0.0f && x <= 3.0e38f)) return RECBLR_ERR_INVALID_ARGUMENT;
+    // As floats, so that the limits are limits for a caller who has a float too.
+    if (!((float)temperature >= 1e-30f && (float)temperature <= 1e30f)) return RECBLR_ERR_INVALID_ARGUMENT;
+    for (double x : {clip_low, clip_high, kl})
+        if (!(x >= 0.0 && x <= 3.0e38)) return RECBLR_ERR_INVALID_ARGUMENT;
     if (!loss || !aligned(loss, 4)) return RECBLR_ERR_INVALID_ARGUMENT;
-    if (N > 0 && (!logits || !ids || !old_logp || !advantage || (kl > 0.0f && !ref_logp)))
+    if (N > 0 && (!logits || !ids || !old_logp || !advantage || (kl > 0.0 && !ref_logp)))
         return RECBLR_ERR_INVALID_ARGUMENT;
     if (!aligned(logits, esz(io)) || !aligned(dlogits, esz(io)))
         return RECBLR_ERR_INVALID_ARGUMENT;
@@ -518,7 +519,7 @@ int recblr_policy_loss(const void* logits, const int32_t* ids, const float* old_
     if (!disjoint({{ws, need}}, {{logits, n}, {dlogits, n}, {loss, 4}, {logp, s}, {ids, s},
                                  {old_logp, s}, {advantage, s}, {ref_logp, s}, {weight, s}}))
         return RECBLR_ERR_INVALID_ARGUMENT;
-    const PolicyArgs a{logits, ids, old_logp, advantage, kl > 0.0f ? ref_logp : nullptr, weight,
+    const PolicyArgs a{logits, ids, old_logp, advantage, kl > 0.0 ? ref_logp : nullptr, weight,
                        loss, logp, dlogits, N, V, temperature, clip_low, clip_high, kl,
                        io_of(io)};
     return status_of(launch_policy_loss(a, ws, (hipStream_t)stream));

@@ -154,7 +154,7 @@ struct PolicyArgs {
     float* logp;    // may be null
     void* dlogits;  // may be null, or logits
     int64_t N, V;
-    float temperature, clip_low, clip_high, kl;
+    double temperature, clip_low, clip_high, kl;
     IoType io;
 };
 size_t policy_workspace(int64_t N, int64_t V, IoType io);

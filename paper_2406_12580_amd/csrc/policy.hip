@@ -7,16 +7,16 @@
 // So a row needs its maximum and sum before its first output, and every logit again for
 // that output: 2 e bytes a logit where the row stays on chip in between.
 //
-// A row of up to 16 KB stays in the registers of a wave or of 256 threads and is read once, as
-// 16-byte vectors that lie at multiples of 16 bytes (up to seven elements before and behind them
-// are one element more of a thread each).  A longer row's workgroup reads it twice, in the first
-// pass against a running maximum; the second pass finds it in the last-level cache.  Few long
-// rows are cut into pieces: one launch leaves each piece's maximum and sum, a second joins them.
+// Rows are read as 16-byte vectors that lie at multiples of 16 bytes (up to seven elements before
+// and behind them are one element more of a thread each).  Those of up to 128 KB stay in the
+// registers of a wave or a workgroup and are read once; of a longer one a workgroup keeps 128 KB,
+// and reads the rest twice, the second time from the last-level cache.  Few long rows are cut into
+// pieces: one launch leaves each piece's maximum and sum, a second joins them.
 //
-// One MI355X: 4096 x 131072 bf16 450 us (417 where the gradient is all zeros), 4.8 TB/s of the
-// logits and their gradient, where a large copy reaches 4.7 to 6.2; the powers, two a logit, are 200 us of vector issue beside
-// it.  2048 x 3416 fp32: 12 us of kernel, 16 of the call from Python.  Rows of which the chip holds
-// more than the last-level cache at once are read from memory twice: 400 x 1,000,000 bf16 441 us.
+// One MI355X: 4096 x 131072 bf16 405 us, 5.3 TB/s of the logits and their gradient, where a large
+// copy reaches 4.7 to 6.2; the powers, two a logit, are 200 us of vector issue beside it.  2048 x
+// 3416 fp32: 13 us of kernel, 16 of the call from Python.  Rows of which the chip holds more than
+// the last-level cache at once come from memory twice: 200 x 1,000,000 bf16 203 us, 3.9 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -43,8 +43,8 @@ struct Params {
     void* dlogits;
     float* row_loss;
     int64_t N, V;
-    float T, inv_T, k, k_lo;  // temperature; 1 / T; log2(e) / T in two parts
-    float lo, hi, kl;         // borders of the ratio; the KL term's weight
+    float k, k_lo;         // log2(e) / T in two parts
+    double T, lo, hi, kl;  // temperature; borders of the ratio; the KL term's weight
 };
 
 // ------------------------------------------------------------------ a row's loss
@@ -93,20 +93,20 @@ struct Powers {
 __device__ __forceinline__ RowLoss row_loss(const Params& p, int64_t row, float xa,
                                             const Powers& w2, float S) {
     const double sum = S < __builtin_inff() ? (double)S : __builtin_nan("");
-    const double lp = ((double)xa - (double)w2.M) / (double)p.T - (log(sum) - w2.shift);
-    const float A = p.advantage[row], w = p.weight ? p.weight[row] : 1.0f;
-    const float r = (float)exp(lp - (double)p.old_logp[row]);
-    const bool gain = A >= 0.0f;
+    const double lp = ((double)xa - (double)w2.M) / p.T - (log(sum) - w2.shift);
+    const double A = p.advantage[row], w = p.weight ? p.weight[row] : 1.0f;
+    const double r = exp(lp - (double)p.old_logp[row]);
+    const bool gain = A >= 0.0;
     const bool inside = gain ? !(r > p.hi) : !(r < p.lo);
-    const float surrogate = inside ? r * A : (gain ? p.hi : p.lo) * A;
-    float loss = -surrogate, c = inside ? -surrogate : 0.0f;
-    if (p.kl > 0.0f) {
+    const double surrogate = inside ? r * A : (gain ? p.hi : p.lo) * A;
+    double loss = -surrogate, c = inside ? -surrogate : 0.0;
+    if (p.kl > 0.0) {
         const double d = (double)p.ref_logp[row] - lp, up = expm1(d);
         // Both are of d's size, so what is left of d^2 keeps its digits; e^d may be infinite.
-        loss += p.kl * (float)(up < __builtin_inf() ? up - d : up);
-        c -= p.kl * (float)up;
+        loss += p.kl * (up < __builtin_inf() ? up - d : up);
+        c -= p.kl * up;
     }
-    return RowLoss{(float)lp, w * loss, w * c * p.inv_T};
+    return RowLoss{(float)lp, (float)(w * loss), (float)(w * c / p.T)};
 }
 
 __device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7FC00000u); }
@@ -197,6 +197,20 @@ __device__ __forceinline__ float over_row(float v, float none, float* red, Op op
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float added(float a, float b) { return a + b; }
 
+// row_loss for the TH threads of a row, by its first wave: in all of them its 64-bit arithmetic
+// is more than the powers of a row of 4,000.
+template <int TH>
+__device__ __forceinline__ RowLoss row_loss_of(const Params& p, int64_t row, float xa,
+                                               const Powers& pw, float S, float* red) {
+    if constexpr (TH == kWave) return row_loss(p, row, xa, pw, S);
+    if (wave_id() == 0) {
+        const RowLoss r = row_loss(p, row, xa, pw, S);
+        if ((threadIdx.x & 63) == 0) red[0] = r.lp, red[1] = r.loss, red[2] = r.c;
+    }
+    __syncthreads();
+    return RowLoss{red[0], red[1], red[2]};
+}
+
 // The gradient of elements whose e^x are given: -(c / S) e^x, c more at the chosen one.
 template <int U>
 __device__ __forceinline__ void gradient(float (&g)[U], float minus, float c, int64_t at) {
@@ -267,7 +281,7 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void row_kernel(Params p) {
         const float S = over_row<TH>(s, 0.0f, red, added);
 #pragma unroll
         for (int j = 0; j < NV; ++j) x[j].packed();
-        const RowLoss r = row_loss(p, row, xa, pw, S);
+        const RowLoss r = row_loss_of<TH>(p, row, xa, pw, S, red);
         if (t == 0) {
             p.row_loss[row] = r.loss;
             if (p.logp) p.logp[row] = r.lp;
@@ -291,21 +305,23 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void row_kernel(Params p) {
     });
 }
 
-// ------------------------------------------------------------------ a row read twice
+// ------------------------------------------------------------------ a row against a running maximum
 // A thread's running reference and the sum of powers relative to it, over vectors t, t + TH, ... of
 // `vecs`; the reference starts at `low`, where nothing that counts can lie beside a row's maximum
-// above it.  B vectors at a time.
-template <int TH, typename T, bool VEC>
+// above it.  B vectors at a time, the first KEPT left in `kept`.
+template <int TH, int KEPT, typename T, bool VEC>
 __device__ __forceinline__ void running_sum(const T* body, int vecs, int t, float k, float k_lo,
-                                            float& m, float& mk, float& s) {
+                                            Raw<T, VEC> (&kept)[KEPT], float& m, float& mk,
+                                            float& s) {
     constexpr int U = Span<T, VEC>::U, B = 4;
-    for (int i = t; i < vecs; i += B * TH) {
-        Raw<T, VEC> x[B];
+    auto read = [&](Raw<T, VEC>* x, int i) {
 #pragma unroll
         for (int j = 0; j < B; ++j) {
             x[j].none();
             if (i + j * TH < vecs) x[j].keep(body, i + j * TH);
         }
+    };
+    auto add = [&](const Raw<T, VEC>* x) {
         float top = m;
 #pragma unroll
         for (int j = 0; j < B; ++j)
@@ -319,16 +335,30 @@ __device__ __forceinline__ void running_sum(const T* body, int vecs, int t, floa
         for (int j = 0; j < B; ++j)
 #pragma unroll
             for (int e = 0; e < U; ++e) s += Powers::to(x[j].get(e), k, k_lo, mk);
+    };
+#pragma unroll
+    for (int c = 0; c < KEPT; c += B) read(kept + c, t + c * TH);
+#pragma unroll
+    for (int c = 0; c < KEPT; c += B) {
+        add(kept + c);
+#pragma unroll
+        for (int j = 0; j < B; ++j) kept[c + j].packed();
+    }
+    for (int i = t + KEPT * TH; i < vecs; i += B * TH) {
+        Raw<T, VEC> x[B];
+        read(x, i);
+        add(x);
     }
 }
 // The row's powers and, in S, their sum; xe: one element of the thread's beside its vectors.
-template <int TH, typename T, bool VEC>
+template <int TH, int KEPT, typename T, bool VEC>
 __device__ __forceinline__ Powers sum_of(const T* body, int vecs, int t, float xe, float k,
-                                         float k_lo, float* red, float& S) {
+                                         float k_lo, Raw<T, VEC> (&kept)[KEPT], float* red,
+                                         float& S) {
     constexpr int U = Span<T, VEC>::U;
     const float none = -__builtin_inff(), low = -0x1p19f / k;
     float m = fmaxf(low, xe), mk = rounded_product(m, k), s = Powers::to(xe, k, k_lo, mk);
-    running_sum<TH, T, VEC>(body, vecs, t, k, k_lo, m, mk, s);
+    running_sum<TH, KEPT, T, VEC>(body, vecs, t, k, k_lo, kept, m, mk, s);
     float M = over_row<TH>(m, none, red, larger);
     Powers pw(M, k, k_lo);
     s *= fast_exp2(mk - pw.mk);
@@ -356,8 +386,8 @@ __device__ __forceinline__ Powers sum_of(const T* body, int vecs, int t, float x
     return pw;
 }
 
-template <typename T, int TH, bool VEC>
-__global__ __launch_bounds__(TH) void twice_kernel(Params p) {
+template <typename T, int TH, int KEPT, bool VEC>
+__global__ __launch_bounds__(TH) void running_kernel(Params p) {
     constexpr int U = Span<T, VEC>::U, B = 4;  // vectors on their way
     __shared__ float red[16];
     const int64_t row = blockIdx.x;
@@ -382,8 +412,9 @@ __global__ __launch_bounds__(TH) void twice_kernel(Params p) {
     const float xa = id < p.V ? to_f32(base[id]) : quiet_nan();
     const float xe = VEC && extra >= 0 ? to_f32(base[extra]) : -__builtin_inff();
     float S;
-    const Powers pw = sum_of<TH, T, VEC>(body, sp.vecs, t, xe, p.k, p.k_lo, red, S);
-    const RowLoss r = row_loss(p, row, xa, pw, S);
+    Raw<T, VEC> kept[KEPT];
+    const Powers pw = sum_of<TH, KEPT, T, VEC>(body, sp.vecs, t, xe, p.k, p.k_lo, kept, red, S);
+    const RowLoss r = row_loss_of<TH>(p, row, xa, pw, S, red);
     if (t == 0) {
         p.row_loss[row] = r.loss;
         if (p.logp) p.logp[row] = r.lp;
@@ -392,21 +423,24 @@ __global__ __launch_bounds__(TH) void twice_kernel(Params p) {
     const float minus = -r.c / S;
     pw.use([&](auto far) {
         constexpr bool kFar = decltype(far)::value;
-        for (int i0 = t; i0 < sp.vecs; i0 += B * TH) {
+        auto put = [&](const Raw<T, VEC>& x, int i) {
+            float g[U];
+#pragma unroll
+            for (int e = 0; e < U; ++e) g[e] = pw.of<kFar>(x.get(e));
+            gradient<U>(g, minus, r.c, (int64_t)id - sp.head - (int64_t)i * U);
+            Raw<T, VEC>::write(out + sp.head, i, g);
+        };
+#pragma unroll
+        for (int c = 0; c < KEPT; ++c)
+            if (t + c * TH < sp.vecs) put(kept[c], t + c * TH);
+        for (int i0 = t + KEPT * TH; i0 < sp.vecs; i0 += B * TH) {
             Raw<T, VEC> x[B];
 #pragma unroll
             for (int j = 0; j < B; ++j)
                 if (i0 + j * TH < sp.vecs) x[j].read(body, i0 + j * TH);
 #pragma unroll
-            for (int j = 0; j < B; ++j) {
-                const int i = i0 + j * TH;
-                if (i >= sp.vecs) break;
-                float g[U];
-#pragma unroll
-                for (int e = 0; e < U; ++e) g[e] = pw.of<kFar>(x[j].get(e));
-                gradient<U>(g, minus, r.c, (int64_t)id - sp.head - (int64_t)i * U);
-                Raw<T, VEC>::write(out + sp.head, i, g);
-            }
+            for (int j = 0; j < B; ++j)
+                if (i0 + j * TH < sp.vecs) put(x[j], i0 + j * TH);
         }
         if (VEC && extra >= 0)
             out[extra] = from_f32<T>(pw.of<kFar>(xe) * minus + (extra == id ? r.c : 0.0f));
@@ -509,7 +543,8 @@ __global__ __launch_bounds__(kPieceThreads) void joined_kernel(Params p, const P
     Powers pw(M, p.k, p.k_lo);
     const double shift = pw.shift;
     pw.shift = 0.0;
-    const RowLoss r = row_loss(p, row, id < p.V ? chosen[row] : quiet_nan(), pw, S);
+    const RowLoss r =
+        row_loss_of<TH>(p, row, id < p.V ? chosen[row] : quiet_nan(), pw, S, red);
     if (t == 0 && at == 0) {
         p.row_loss[row] = r.loss;
         if (p.logp) p.logp[row] = r.lp;
@@ -566,19 +601,22 @@ __global__ __launch_bounds__(kSumThreads) void sum_kernel(const In* v, int64_t n
 
 // ------------------------------------------------------------------ which way
 struct Way {
-    int threads, vecs;  // to a row; vectors a thread keeps, 0: the row is read twice
+    int threads, vecs;  // to a row; vectors that a thread keeps
     int64_t piece;      // > 0: elements to a piece of a row instead
 };
 
-// Rows of up to 16 KB stay in registers.  Longer ones are read twice, the second time from the
-// last-level cache: 4096 rows of 256 KB take 417 us so and 481 in the registers of 1024 threads,
-// whose arithmetic then waits for loads and loads for it (one row to a compute unit); 8192 rows of
-// 32 KB 76 and 91, of 16 KB 76 and 55.  Few long rows are cut into pieces: 16 x 131072 bf16 22 us.
+// Up to 512 vectors of 16 bytes lie in the registers of a wave or of 256 threads and their maximum
+// comes before their powers.  Longer rows are summed against a running maximum, the first vectors
+// of each thread kept and what is behind them read again, from the last-level cache: 8192 rows of
+// 16 KB 48 us (in registers, maximum first, 55), of 32 KB 88 (nothing kept 107), 4096 of 128 KB
+// 190 (204), of 256 KB 405 (450; with 512 threads that keep 16, 412, in registers as a whole
+// 420).  Few long rows are cut into pieces: 16 x 131072 bf16 22 us.
 Way way_of(int64_t N, int64_t V, IoType io, bool vec) {
     const int64_t U = vec ? 16 / (int64_t)io_bytes(io) : 1, n = (V + U - 1) / U;  // vectors
     if (n <= 64 * 4) return {64, n <= 64 ? 1 : n <= 128 ? 2 : 4, 0};
-    if (n <= 1024) return {256, n <= 512 ? 2 : 4, 0};
-    if (N >= 128 || n <= 16384) return {n <= 4096 ? 512 : 1024, 0, 0};
+    if (n <= 256 * 4) return {256, n <= 512 ? 2 : 4, 0};
+    if (n <= 512 * 24) return {512, n <= 512 * 4 ? 4 : n <= 512 * 8 ? 8 : 16, 0};
+    if (N >= 128 || n <= 16384) return {1024, 8, 0};
     // Pieces: about four workgroups to a compute unit, of 2,048 elements or more.
     const int64_t want = (1024 + N - 1) / N;
     int64_t piece = (V + want - 1) / want;
@@ -629,11 +667,13 @@ void launch_rows(const Params& p, const Way& w, const Layout& l, char* ws, hipSt
         else row_kernel<T, 64, 4, VEC><<<quads, 256, 0, st>>>(p);
     } else if (w.threads == 256) {
         if (w.vecs == 2) row_kernel<T, 256, 2, VEC><<<rows, 256, 0, st>>>(p);
-        else row_kernel<T, 256, 4, VEC><<<rows, 256, 0, st>>>(p);
+        else running_kernel<T, 256, 4, VEC><<<rows, 256, 0, st>>>(p);
     } else if (w.threads == 512) {
-        twice_kernel<T, 512, VEC><<<rows, 512, 0, st>>>(p);
+        if (w.vecs == 4) running_kernel<T, 512, 4, VEC><<<rows, 512, 0, st>>>(p);
+        else if (w.vecs == 8) running_kernel<T, 512, 8, VEC><<<rows, 512, 0, st>>>(p);
+        else running_kernel<T, 512, 16, VEC><<<rows, 512, 0, st>>>(p);
     } else {
-        twice_kernel<T, 1024, VEC><<<rows, 1024, 0, st>>>(p);
+        running_kernel<T, 1024, 8, VEC><<<rows, 1024, 0, st>>>(p);
     }
 }
 
@@ -648,8 +688,8 @@ hipError_t launch_policy_loss(const PolicyArgs& a, void* ws, hipStream_t st) {
     float k = (float)K;
     if ((double)k >= K) k = std::nextafterf(k, 0.0f);  // for a positive rest
     const Params p{a.logits, a.ids, a.old_logp, a.advantage, a.ref_logp, a.weight, a.logp,
-                   a.dlogits, (float*)(w + l.rows), a.N, a.V, a.temperature, 1.0f / a.temperature,
-                   k, (float)(K - (double)k), 1.0f - a.clip_low, 1.0f + a.clip_high, a.kl};
+                   a.dlogits, (float*)(w + l.rows), a.N, a.V, k, (float)(K - (double)k),
+                   a.temperature, 1.0 - a.clip_low, 1.0 + a.clip_high, a.kl};
     if (a.N > 0) {
         // Vectors need rows of both tensors to lie alike to 16 bytes.
         const bool vec =

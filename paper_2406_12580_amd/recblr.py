@@ -504,7 +504,7 @@ _OPS_SIGS = {
     "recblr_qk_norm_backward": ([_p, _p, _i64, _i64] + [_p] * 9 + [_i64] * 5 + [
         _d, _int, _f, _int, _p, _sz, _p], _int),
     "recblr_policy_loss_workspace_size": ([_i64, _i64, _int], _sz),
-    "recblr_policy_loss": ([_p] * 9 + [_i64, _i64, _f, _f, _f, _f, _int, _p, _sz, _p], _int),
+    "recblr_policy_loss": ([_p] * 9 + [_i64, _i64, _d, _d, _d, _d, _int, _p, _sz, _p], _int),
     "recblr_muon_workspace_size": ([ctypes.POINTER(MuonTensor), _i64, _int], _sz),
     "recblr_muon_update": ([ctypes.POINTER(MuonTensor), _i64, _int, _d, _d, _int, _int, _d, _p,
                             _sz, _p], _int),
