@@ -181,6 +181,14 @@ struct Raw {
     }
 };
 
+// The sum of f(0) .. f(N - 1), N a power of two, by halves: added to a growing sum one by one, small
+// powers would be rounded off more often than up, and ratios lie a little too high.
+template <int N, typename F>
+__device__ __forceinline__ float sum_by_halves(F f, int from = 0) {
+    if constexpr (N == 1) return f(from);
+    else return sum_by_halves<N / 2>(f, from) + sum_by_halves<N / 2>(f, from + N / 2);
+}
+
 // Over the TH threads that share a row; every one of them gets the result.
 template <int TH, typename Op>
 __device__ __forceinline__ float over_row(float v, float none, float* red, Op op) {
@@ -197,8 +205,8 @@ __device__ __forceinline__ float over_row(float v, float none, float* red, Op op
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float added(float a, float b) { return a + b; }
 
-// row_loss for the TH threads of a row, by its first wave: in all of them its 64-bit arithmetic
-// is more than the powers of a row of 4,000.
+// row_loss for the TH threads of a row, by its first wave (16384 rows of 5,000 bf16 64 us; with its
+// 64-bit arithmetic in all of them 76).
 template <int TH>
 __device__ __forceinline__ RowLoss row_loss_of(const Params& p, int64_t row, float xa,
                                                const Powers& pw, float S, float* red) {
@@ -268,16 +276,12 @@ __global__ __launch_bounds__(TH < 256 ? 256 : TH) void row_kernel(Params p) {
     const Powers pw(M, p.k, p.k_lo);
     pw.use([&](auto far) {
         constexpr bool kFar = decltype(far)::value;
-        float s = pw.of<kFar>(xe);
-        const float ee = s;
-#pragma unroll
-        for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int e = 0; e < U; ++e) {
-                const float v = pw.of<kFar>(x[j].get(e));
-                s += v;
-                if constexpr (!VEC || sizeof(T) == 4) x[j].v[e] = __float_as_uint(v);
-            }
+        const float ee = pw.of<kFar>(xe);
+        const float s = ee + sum_by_halves<NV * U>([&](int i) {
+            const float v = pw.of<kFar>(x[i / U].get(i % U));
+            if constexpr (!VEC || sizeof(T) == 4) x[i / U].v[i % U] = __float_as_uint(v);
+            return v;
+        });
         const float S = over_row<TH>(s, 0.0f, red, added);
 #pragma unroll
         for (int j = 0; j < NV; ++j) x[j].packed();
@@ -331,10 +335,7 @@ __device__ __forceinline__ void running_sum(const T* body, int vecs, int t, floa
         s *= fast_exp2(mk - now);
         m = top;
         mk = now;
-#pragma unroll
-        for (int j = 0; j < B; ++j)
-#pragma unroll
-            for (int e = 0; e < U; ++e) s += Powers::to(x[j].get(e), k, k_lo, mk);
+        s += sum_by_halves<B * U>([&](int i) { return Powers::to(x[i / U].get(i % U), k, k_lo, mk); });
     };
 #pragma unroll
     for (int c = 0; c < KEPT; c += B) read(kept + c, t + c * TH);
@@ -378,8 +379,7 @@ __device__ __forceinline__ Powers sum_of(const T* body, int vecs, int t, float x
         for (int i = t; i < vecs; i += TH) {
             Raw<T, VEC> x;
             x.keep(body, i);
-#pragma unroll
-            for (int e = 0; e < U; ++e) s += pw.of<true>(x.get(e));
+            s += sum_by_halves<U>([&](int e) { return pw.of<true>(x.get(e)); });
         }
     }
     S = over_row<TH>(s, 0.0f, red, added);
@@ -485,11 +485,8 @@ __global__ __launch_bounds__(kPieceThreads) void part_kernel(Params p, Part* par
             for (int e = 0; e < U; ++e) top = fmaxf(top, x[j].get(e));
         const float ref = top == none ? 0.0f : top;  // nothing but -inf so far: powers of 0
         s *= Powers::to(m - ref, p.k, p.k_lo, 0.0f);
-#pragma unroll
-        for (int j = 0; j < B; ++j)
-#pragma unroll
-            for (int e = 0; e < U; ++e)
-                s += Powers::to(x[j].get(e) - ref, p.k, p.k_lo, 0.0f);
+        s += sum_by_halves<B * U>(
+            [&](int i) { return Powers::to(x[i / U].get(i % U) - ref, p.k, p.k_lo, 0.0f); });
         m = top;
     }
     const float M = over_row<TH>(m, none, red, larger);
