@@ -13,7 +13,8 @@
 // go over its borders by a second launch, in their order.  Which addition follows which hangs
 // on the ids alone.
 //
-// Few positions: each wave looks for its position's id among all; the first of an id sums them.
+// Few positions are not sorted: each wave looks for its position's id among all, and the first of
+// an id sums its rows.
 //
 // One MI355X: 409,600 positions of 64 fp32 over 3,416 items: lookup 19 us, 5.6 TB/s of what it
 // writes; gradient 53: counts with the table's zeros 7, offsets 6, places 14, sums 20 (5.3 TB/s),
@@ -127,52 +128,116 @@ __device__ __forceinline__ void end_row(const Grad& g, uint32_t k, int col, cons
 }
 
 // ------------------------------------------------------------------ few positions
-// 1024 positions of 64 fp32, all items different, in 11 us (37 by sorting); all the same in 52
-// (32), a chain of a wave.
-constexpr int kFew = 1024;
+// Every workgroup has all ids in LDS, and each of its waves a position: the first one of an item
+// sums the item's rows.  Those that more than kLight positions name are summed by the whole
+// workgroup, a wave a run of all positions, and the waves' sums in their order.  Rows of 64 fp32:
+// 1,024 positions 7 us, 11 where they all name one item; 4,000 13 to 34, by sorting 31 (a million
+// items: 41); 8,192 24 to 64, by sorting 36.
+constexpr int kFew = 4096, kFewThreads = 1024, kFewWaves = kFewThreads / kWave, kLight = 64;
+
+// The sum of the rows at row(0) .. row(n - 1), by halves in groups of B.
+template <typename T, int VL, typename Row>
+__device__ __forceinline__ void add_rows(const T* dout, int D, bool live, int n, Row row,
+                                         float (&acc)[VL]) {
+    constexpr int B = VL < 4 ? 16 : 8;
+    for (int k0 = 0; k0 < n; k0 += B) {
+        RawRow<T, VL> raw[B];
+#pragma unroll
+        for (int k = 0; k < B; ++k) {  // in place of those behind the last one, the first one's again
+            const int at = row(k0 + k < n ? k0 + k : k0);
+            if (live) raw[k] = raw_row<T, VL>(dout + (int64_t)at * D);
+        }
+        float v[B][VL];
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            unpack_vec<T, VL>(raw[k], v[k]);
+#pragma unroll
+            for (int e = 0; e < VL; ++e) v[k][e] = k0 + k < n ? v[k][e] : 0.0f;
+        }
+#pragma unroll
+        for (int h = B / 2; h > 0; h /= 2)
+#pragma unroll
+            for (int k = 0; k < h; ++k)
+#pragma unroll
+                for (int e = 0; e < VL; ++e) v[k][e] += v[k + h][e];
+#pragma unroll
+        for (int e = 0; e < VL; ++e) acc[e] += v[0][e];
+    }
+}
 
 template <typename T, int VL>
-__global__ __launch_bounds__(kNT) void few_kernel(const int32_t* __restrict__ ids, int N,
-                                                  int64_t V, int32_t pad_id, Grad g) {
-    __shared__ int32_t all[kFew];
-    for (int i = threadIdx.x; i < N; i += kNT) all[i] = ids[i];
+__global__ __launch_bounds__(kFewThreads) void few_kernel(const int32_t* __restrict__ ids, int N,
+                                                          int64_t V, int32_t pad_id, Grad g) {
+    typedef int i4v __attribute__((ext_vector_type(4)));
+    extern __shared__ __attribute__((aligned(16))) int32_t all[];  // -1: no row
+    __shared__ int32_t found[kFewWaves][kLight], heavy[kFewWaves];
+    __shared__ float part[kFewWaves][kWave * VL];
+    const int t = threadIdx.x, lane = t & 63, w = wave_id(), i = blockIdx.x * kFewWaves + w;
+    for (int k = t; k < (N + 255) / 256 * 256; k += kFewThreads) {
+        const int id = k < N ? ids[k] : -1;
+        all[k] = id == pad_id || id < 0 || id >= V ? -1 : id;
+    }
     __syncthreads();
-    const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + wave_id();
-    if (i >= N) return;
-    const int id = all[i];
-    if (id == pad_id || id < 0 || id >= V) return;
-    for (int j = lane; j - lane < i; j += kWave)
-        if (__ballot(j < i && all[j] == id)) return;  // an earlier position has it
     const int col = ((int)blockIdx.y * kWave + lane) * VL;
     const bool live = col < g.D;
     const T* dout = (const T*)g.dout + col;
-    float acc[VL] = {}, old[VL] = {};
-    if (g.add && live) read_row<T, VL>((const T*)g.dtable + (int64_t)id * g.D + col, old);
-    for (int j0 = i & ~63; j0 < N; j0 += kWave) {
-        const int j = j0 + lane;
-        uint64_t m = __ballot(j >= i && j < N && all[j < N ? j : 0] == id);
-        while (m) {
-            // Rows read at once; in place of those behind the last one, the first one's again.
-            constexpr int B = VL < 4 ? 16 : 8;
-            RawRow<T, VL> raw[B];
-            const int n = __popcll(m);
+    const T* table = (const T*)g.dtable + col;
+    const uint64_t below = (1ull << lane) - 1;
+    const int id = __builtin_amdgcn_readfirstlane(i < N ? all[i] : -1);
+    bool first = id >= 0;
+    for (int c = 0; first && c < i; c += 256) {  // none before it
+        const i4v q = *(const i4v*)(all + c + 4 * lane);
+        bool hit = false;
 #pragma unroll
-            for (int k = 0; k < B; ++k) {
-                const int at = m ? j0 + __builtin_ctzll(m) : i;
-                m &= m - 1;
-                if (live) raw[k] = raw_row<T, VL>(dout + (int64_t)at * g.D);
-            }
+        for (int e = 0; e < 4; ++e) hit |= q[e] == id && c + 4 * lane + e < i;
+        first = __ballot(hit) == 0;
+    }
+    int n = 0;
+    for (int c = i & ~255; first && n <= kLight && c < N; c += 256) {
+        const i4v q = *(const i4v*)(all + c + 4 * lane);
 #pragma unroll
-            for (int k = 0; k < B; ++k) {
-                if (k >= n) break;
-                float v[VL];
-                unpack_vec<T, VL>(raw[k], v);
-#pragma unroll
-                for (int e = 0; e < VL; ++e) acc[e] += v[e];
-            }
+        for (int e = 0; e < 4; ++e) {
+            const uint64_t m = __ballot(q[e] == id);  // behind the last one is none
+            const int at = n + __popcll(m & below);
+            if ((m >> lane & 1) && at < kLight) found[w][at] = c + 4 * lane + e;
+            n += __popcll(m);
         }
     }
-    if (live) end_row<T, VL>(g, (uint32_t)id, col, acc, old);
+    wave_fence();
+    if (lane == 0) heavy[w] = n > kLight ? id : -1;
+    float acc[VL] = {}, old[VL] = {};
+    if (first && n <= kLight) {
+        if (g.add && live) read_row<T, VL>(table + (int64_t)id * g.D, old);
+        add_rows<T, VL>(dout, g.D, live, n, [&](int k) { return found[w][k]; }, acc);
+        if (live) end_row<T, VL>(g, (uint32_t)id, col, acc, old);
+    }
+    __syncthreads();
+    const int run = ((N + kWave - 1) / kWave + kFewWaves - 1) / kFewWaves * kWave;
+    for (int h = 0; h < kFewWaves; ++h) {
+        const int item = __builtin_amdgcn_readfirstlane(heavy[h]);
+        if (item < 0) continue;
+#pragma unroll
+        for (int e = 0; e < VL; ++e) acc[e] = 0.0f;
+        if (w == 0 && g.add && live) read_row<T, VL>(table + (int64_t)item * g.D, old);
+        for (int c = w * run; c < (w + 1) * run && c < N; c += kWave) {
+            uint64_t m = __ballot(all[c + lane] == item);
+            add_rows<T, VL>(dout, g.D, live, __popcll(m), [&](int) {
+                const int at = c + __builtin_ctzll(m);
+                m = (m & (m - 1)) ? m & (m - 1) : m;  // the last one stays
+                return at;
+            }, acc);
+        }
+#pragma unroll
+        for (int e = 0; e < VL; ++e) part[w][lane * VL + e] = acc[e];
+        __syncthreads();
+        if (w == 0) {
+            for (int v = 1; v < kFewWaves; ++v)
+#pragma unroll
+                for (int e = 0; e < VL; ++e) acc[e] += part[v][lane * VL + e];
+            if (live) end_row<T, VL>(g, (uint32_t)item, col, acc, old);
+        }
+        __syncthreads();
+    }
 }
 
 // ------------------------------------------------------------------ sorting positions by id
@@ -630,7 +695,8 @@ template <typename T, int VL>
 void launch_sums(const EmbedArgs& a, const Plan& pl, char* ws, const Grad& g, hipStream_t st) {
     const unsigned cols = (unsigned)((a.D + kWave * VL - 1) / (kWave * VL));
     if (a.N <= kFew) {
-        few_kernel<T, VL><<<dim3((unsigned)((a.N + 3) / 4), cols), kNT, 0, st>>>(
+        const dim3 grid((unsigned)((a.N + kFewWaves - 1) / kFewWaves), cols);
+        few_kernel<T, VL><<<grid, kFewThreads, (size_t)(a.N + 255) / 256 * 1024, st>>>(
             a.ids, (int)a.N, a.V, a.pad_id, g);
         return;
     }

@@ -5,9 +5,10 @@ Bounds, element by element, from the arithmetic (U = 2^-24, the largest relative
 rounding to fp32; 2^-8 to bf16):
 
 * Lookup: one product in fp32, then one rounding to the type: equal to that.
-* Its gradient: an item's n rows are added in chains of at most 64 within a piece, and pieces in
-  eight chains that are added up: no more than d = min(n, 64 + n / 512 + 24) additions lie over a
-  term, and the factor, and what was there: (d + 3) U of the sum of the terms' sizes.
+* Its gradient: an item's n rows are added in chains of at most 64 within a piece, 16 pieces in a
+  group, groups of 1024 in eight chains that are added up (up to 4096 positions: by halves of 8 or
+  16, at most 32 of these in a chain, 16 chains): no more than d = min(n, 64 + n / 512 + 24)
+  additions lie over a term, and the factor, and what was there: (d + 3) U of the sum of the terms' sizes.
 * Norms: the sum of D squares has at most D roundings, the root halves them, division, square
   root, products: r and u are off by (D / 2 + 6) U.  A sine's angle is rounded to fp32 (pi U of
   turns up to a half) and sincospif is right to 2 ulps: 8 U of the pair's size, with the products
@@ -143,11 +144,14 @@ def check_embed(rb, c, scale=1.5, pad_id=-1, add=False):
         assert np.array_equal(host(d)[n[:, 0] == 0], c["into_"][n[:, 0] == 0])
 
 
-# Around the few positions' limit (1024), a block (2048), pieces (64); tables of one digit (12
-# bits), two and three; widths of every way to read a row.
+# Around the few positions' limit (4096), a wave's and a workgroup's part of them (64, 1024), a
+# block (2048), pieces (64); tables of one digit (12 bits), two and three; widths of every way to
+# read a row.
 EMBED = [(1, 1, 1), (1, 5, 64), (7, 3, 33), (64, 1, 128), (1000, 50, 48), (1024, 4, 256),
          (1025, 4, 64), (1025, 3000, 100), (2048, 4095, 130), (2049, 4096, 64), (5000, 1, 5),
-         (6001, 2, 64), (9000, 70000, 7), (4500, 300, 600), (70000, 5000, 20)]
+         (6001, 2, 64), (64, 1, 33), (65, 1, 33), (129, 2, 64), (4095, 70, 16),
+         (4096, 4000, 8), (4096, 1, 130), (4097, 300, 8), (4100, 1, 64), (9001, 2, 130),
+         (10240, 4096, 64), (9000, 70000, 7), (4500, 300, 600), (70000, 5000, 20)]
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
@@ -169,13 +173,13 @@ def test_embed_of_one_item(rb, io, N):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
-@pytest.mark.parametrize("N", [200, 5000])
+@pytest.mark.parametrize("N", [200, 4000, 20000])
 def test_embed_runs_at_piece_borders(rb, io, N):
     """Runs that end with a piece, one before or behind it, and that fill whole pieces."""
     lengths, ids = [64, 63, 1, 65, 128, 127, 2, 64, 1, 192, 3, 61, 320], []
-    for i, n in enumerate(lengths * 6):
+    for i, n in enumerate(lengths * 20):
         ids += [i] * n
-    c = embed_case(io, N, 100, 64, seed=2)
+    c = embed_case(io, N, 300, 64, seed=2)
     c["ids"] = np.asarray(ids)[:N]
     check_embed(rb, c)
     check_embed(rb, c, add=True)
@@ -204,7 +208,7 @@ def test_embed_many(rb, io, size):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
-@pytest.mark.parametrize("N", [30, 2500])
+@pytest.mark.parametrize("N", [30, 2500, 12000])
 def test_embed_ids_of_no_row(rb, io, N):
     """Ids behind the table, negative ones, the type's ends and padding (inside or outside)."""
     for pad in (-1, 0, 1 << 30):
@@ -224,10 +228,11 @@ def test_embed_ids_of_no_row(rb, io, N):
 @pytest.mark.parametrize("D", [64, 128, 256, 96])
 def test_embed_unaligned(rb, io, offset, D):
     check_embed(rb, embed_case(io, 1500, 200, D, seed=5, offset=offset))
+    check_embed(rb, embed_case(io, 4500, 200, D, seed=5, offset=offset))
     check_embed(rb, embed_case(io, 15, 200, D, seed=5, offset=offset), add=True)
 
 
-@pytest.mark.parametrize("N", [100, 3000])
+@pytest.mark.parametrize("N", [100, 3000, 12000])
 def test_embed_writes_its_table_only(rb, N):
     """A gradient in the middle of a buffer, at addresses that are no multiples of 16 bytes."""
     import ctypes
@@ -940,7 +945,7 @@ def passes(rb, io, seed=0):
     """name -> (call, its outputs' clones): one pass of every operator, few and many rows."""
     import torch
     out = {}
-    for N in (100, 3000):
+    for N in (100, 3000, 12000):
         c = embed_case(io, N, 300, 64, seed=seed)
         ids = ints(c["ids"])
         out[f"embed {N}"] = lambda c=c, ids=ids: [
@@ -1017,7 +1022,7 @@ def test_two_streams(rb):
     for k in range(2):
         for name, ts in want[k].items():
             assert all(torch.equal(a, b) for a, b in zip(ts, got[k][name])), name
-    c = embed_case("f32", 3000, 300, 64)
+    c = embed_case("f32", 6000, 300, 64)
     ids, s = ints(c["ids"]), torch.cuda.Stream()
     torch.cuda.synchronize()
     d = rb.embed_backward(ids, c["dout"], 300, stream=s)
@@ -1043,6 +1048,11 @@ def test_embed_beyond_31_bits(rb):
     d = rb.embed_backward(ints(ids), dout, V, into=table)
     assert float(d[V - 1, 255]) == 6 and float(d[8_500_000, 0]) == 4 and float(d[V - 2, 9]) == 1504  # 1500 as bf16
     assert float(d[8_388_606].abs().max()) == 0
+    many = np.concatenate([ids, [V - 3] * 5000])      # sorted
+    d = rb.embed_backward(ints(many), torch.ones(len(many), D, dtype=torch.bfloat16,
+                                                 device="cuda"), V)
+    assert float(d[V - 1, 255]) == 2 and float(d[V - 3, 7]) == 4992  # 5000 as bf16
+    assert float(d[8_500_000, 0]) == 1 and float(d[8_388_606].abs().max()) == 0
     few = rb.embed_backward(ints(ids[:6]), dout[:6], V)
     assert float(few[V - 1, 3]) == 2 and float(few.float().sum()) == 6 * D
 
