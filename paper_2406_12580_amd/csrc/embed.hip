@@ -22,6 +22,8 @@
 // digits are 45.  Lookups and sums are bound by memory, the rest by a launch's chain of reads.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "device_common.hpp"
 #include "lanes.hpp"
 #include "ops.hpp"
@@ -165,12 +167,41 @@ __device__ __forceinline__ void add_rows(const T* dout, int D, bool live, int n,
     }
 }
 
+// Zeros to the rows of a run of `each` (at most 32 kFewWaves kWave) that none of the ids in
+// all[0 .. N) names, V rows in all.
+template <typename T>
+__device__ __forceinline__ void clear_others(const int32_t* all, int N, T* table, int64_t V, int D,
+                                             int64_t from, int each, uint32_t* named) {
+    const int t = threadIdx.x, rows = (int)min((int64_t)each, V - from);
+    named[t] = 0;
+    __syncthreads();
+    for (int k = t; k < N; k += kFewThreads) {
+        const int64_t r = all[k] - from;
+        if (r >= 0 && r < rows) atomicOr(&named[r >> 5], 1u << (r & 31));
+    }
+    __syncthreads();
+    table += from * D;
+    auto put = [&](auto zero, int units) {  // of a row
+        for (int j = t; j < rows * units; j += kFewThreads) {
+            const int r = (int)((unsigned)j / (unsigned)units);
+            if (!(named[r >> 5] >> (r & 31) & 1)) ((decltype(zero)*)table)[j] = zero;
+        }
+    };
+    const int bytes = D * (int)sizeof(T);
+    if ((((uintptr_t)table | (unsigned)bytes) & 15) == 0) put(u4v{0, 0, 0, 0}, bytes / 16);
+    else if constexpr (sizeof(T) == 4) put(0u, D);
+    else put((uint16_t)0, D);
+}
+
+// Workgroups from `groups` on clear what no id names, `each` rows of the table.
 template <typename T, int VL>
 __global__ __launch_bounds__(kFewThreads) void few_kernel(const int32_t* __restrict__ ids, int N,
-                                                          int64_t V, int32_t pad_id, Grad g) {
+                                                          int64_t V, int32_t pad_id, Grad g,
+                                                          int groups, int each) {
     typedef int i4v __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) int32_t all[];  // -1: no row
     __shared__ int32_t found[kFewWaves][kLight], heavy[kFewWaves];
+    static_assert(sizeof(found) == 4 * kFewThreads, "a bit for each of 32 rows to a thread");
     __shared__ float part[kFewWaves][kWave * VL];
     const int t = threadIdx.x, lane = t & 63, w = wave_id(), i = blockIdx.x * kFewWaves + w;
     for (int k = t; k < (N + 255) / 256 * 256; k += kFewThreads) {
@@ -178,6 +209,12 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const int32_t* __restr
         all[k] = id == pad_id || id < 0 || id >= V ? -1 : id;
     }
     __syncthreads();
+    if ((int)blockIdx.x >= groups) {
+        if (blockIdx.y == 0)
+            clear_others(all, N, (T*)g.dtable, V, g.D, (int64_t)(blockIdx.x - groups) * each, each,
+                         (uint32_t*)&found[0][0]);
+        return;
+    }
     const int col = ((int)blockIdx.y * kWave + lane) * VL;
     const bool live = col < g.D;
     const T* dout = (const T*)g.dout + col;
@@ -695,9 +732,15 @@ template <typename T, int VL>
 void launch_sums(const EmbedArgs& a, const Plan& pl, char* ws, const Grad& g, hipStream_t st) {
     const unsigned cols = (unsigned)((a.D + kWave * VL - 1) / (kWave * VL));
     if (a.N <= kFew) {
-        const dim3 grid((unsigned)((a.N + kFewWaves - 1) / kFewWaves), cols);
-        few_kernel<T, VL><<<grid, kFewThreads, (size_t)(a.N + 255) / 256 * 1024, st>>>(
-            a.ids, (int)a.N, a.V, a.pad_id, g);
+        const int groups = (int)((a.N + kFewWaves - 1) / kFewWaves);
+        // Rows that a workgroup clears: 512 of them, of 16 to 256 KB each.
+        const int64_t row = a.D * (int64_t)sizeof(T);
+        int64_t each = std::min<int64_t>(std::max<int64_t>(a.V * row / 512, 16384), 262144) / row;
+        each = std::min<int64_t>(std::max<int64_t>(each, 1), 32 * kFewThreads);
+        const int64_t clears = a.accumulate ? 0 : (a.V + each - 1) / each;
+        few_kernel<T, VL><<<dim3((unsigned)(groups + clears), cols), kFewThreads,
+                            (size_t)(a.N + 255) / 256 * 1024, st>>>(a.ids, (int)a.N, a.V, a.pad_id,
+                                                                    g, groups, (int)each);
         return;
     }
     const int last = (pl.passes + 1) % 2;  // passes write buffers 0, 1, 0, ...
@@ -749,7 +792,7 @@ hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t st) {
     s.V = a.V;
     s.each = pl.each;
     s.pad_id = a.pad_id;
-    if (few && fill > 0) count_kernel<<<dim3((unsigned)fill), kNT, 0, st>>>(s, a.dst, bytes);
+    if (a.N == 0 && fill > 0) count_kernel<<<dim3((unsigned)fill), kNT, 0, st>>>(s, a.dst, bytes);
     for (int i = 0; !few && i < pl.passes; ++i) {
         s.ids = i ? nullptr : a.ids;
         s.keys_in = (const uint32_t*)(w + pl.keys[(i + 1) % 2]);

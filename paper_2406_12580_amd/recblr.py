@@ -837,7 +837,7 @@ def embed(table, ids, scale=1.0, pad_id=-1):
         raise ValueError("table must be [V, D]")
     V, D = table.shape
     io, dt, at = io_code(table.dtype), table.dtype, table.get_device()
-    out = torch.empty((*ids.shape, D), dtype=dt, device=table.device)
+    out = table.new_empty((*ids.shape, D))
     _check(recblr_embed_forward(
         _arg(table, (V, D), dt, at, "table"), _arg(ids, ids.shape, torch.int32, at, "ids"),
         out.data_ptr(), ids.numel(), V, D, scale, pad_id, io, _stream()), "recblr_embed_forward")
@@ -857,7 +857,7 @@ def embed_backward(ids, dout, V, scale=1.0, pad_id=-1, into=None):
         raise ValueError("dout must be [*ids.shape, D]")
     D, N = dout.shape[-1], ids.numel()
     io, dt, at = io_code(dout.dtype), dout.dtype, ids.get_device()
-    dtable = torch.empty((V, D), dtype=dt, device=ids.device) if into is None else into
+    dtable = dout.new_empty((V, D)) if into is None else into
     n = _embed_workspace_size(N, V, D, io)
     ws = torch.empty(n, dtype=torch.uint8, device=ids.device) if n else None
     _check(recblr_embed_backward(
