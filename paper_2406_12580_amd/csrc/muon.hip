@@ -65,7 +65,13 @@ __device__ __forceinline__ void split(const float (&v)[N], V& hi, V& lo) {
 #pragma unroll
     for (int e = 0; e < N; e += 2) {  // two to a conversion
         const h2 h = __builtin_convertvector(f2{v[e], v[e + 1]}, h2);
-        const h2 l = __builtin_convertvector(f2{v[e] - (float)h[0], v[e + 1] - (float)h[1]}, h2);
+        // v - (float)h as one instruction (64 x 64: 15.4 -> 14.5 us)
+        const uint32_t both = __builtin_bit_cast(uint32_t, h);
+        float l0, l1;
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(l0) : "v"(both), "v"(v[e]));
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]"
+            : "=v"(l1) : "v"(both), "v"(v[e + 1]));
+        const h2 l = __builtin_convertvector(f2{l0, l1}, h2);
         hi[e] = h[0], hi[e + 1] = h[1];
         lo[e] = l[0], lo[e + 1] = l[1];
     }
