@@ -12,6 +12,8 @@ import numpy as np
 import pytest
 
 import train_ops_reference as ref
+from paper_2406_12580_amd import build as hipbuild
+from test_wave_order import _assembly, _lds_runs
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 A = 0x10000000
@@ -75,7 +77,7 @@ def test_embed_nothing_to_do(rb):
 
 def test_embed_workspace(rb):
     size = rb.recblr_embed_workspace_size
-    assert size(1024, 5000, 64, 0) == 0 and size(1025, 5000, 64, 0) > 0
+    assert size(4096, 5000, 64, 0) == 0 and size(4097, 5000, 64, 0) > 0
     for bad in ((-1, 10, 4, 0), (5000, 10, 0, 0), (5000, 10, 4, 3), (1 << 29, 10, 4, 0)):
         assert size(*bad) == 0
     n = size(5000, 100, 4, 0)
@@ -387,3 +389,22 @@ def test_singular_values_stay_where_the_planes_hold_them():
     f = a * s + b * s ** 3 + c * s ** 5
     assert f.min() >= 0.0 and f.max() <= 1.21
     assert np.abs(b * s ** 2 + c * s ** 4).max() < 3.0
+
+
+# ------------------------------------------------------------------ hand-overs within a wave
+
+def test_embed_hand_overs(tmp_path):
+    """In the compiled kernels: the positions that a wave has found are read behind a fence; a
+    digit's next place is read, fenced, written by the last lane that has it, and fenced before
+    the next positions' lanes read it."""
+    source = os.path.join(hipbuild.CSRC, "embed.hip")
+    lines = _assembly(tmp_path, source)
+    for kernel in ("few_kernelIfLi1", "few_kernelINS_4bf16ELi4"):
+        ops = _lds_runs(lines, kernel)
+        print(kernel, ops)
+        assert ops.count("F") == 1 and "WFWR" in ops, ops  # found, fence, the heavy ones, found
+    for kernel in ("place_kernelILi6", "place_kernelILi9", "place_kernelILi12"):
+        ops = _lds_runs(lines, kernel)
+        print(kernel, ops)
+        steps = ops[ops.rindex("B") + 1:].strip("F") + "F"
+        assert len(steps) >= 16 * 2 and steps == "RFWF" * (len(steps) // 4), ops
