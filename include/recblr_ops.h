@@ -173,7 +173,7 @@ int recblr_sample(const void* logits, const float* u, const float* temperature,
  * accumulate = 0 writes every row of dtable, those of no id as zeros; accumulate = 1 adds to
  * the rows that ids name and touches no other (a table that the prediction layer shares has
  * its gradient there already).  An item's rows are summed in fp32 in an order that hangs on
- * ids alone, and rounded to io once, together with what was there.
+ * ids, widths and alignment alone, and rounded to io once, together with what was there.
  * Errors: INVALID_ARGUMENT; UNSUPPORTED (io, D > 4096, V >= 2^31 - 1, N > 2^28, N D > 2^33,
  * V D > 2^40); WORKSPACE.
  */

@@ -11,7 +11,7 @@
 // item spreads over many waves; a run of an item that lies within a piece is its row, runs
 // that go over the borders of pieces are joined by the workgroup of 16 pieces, and those that
 // go over its borders by a second launch, in their order.  Which addition follows which hangs
-// on the ids alone.
+// on the ids, the width and the alignment alone.
 //
 // Few positions are not sorted: each wave looks for its position's id among all, and the first of
 // an id sums its rows.

@@ -8,14 +8,14 @@
 // (2 e bytes forward, 3 e backward); u and r are formed again in the backward.
 //
 // A group of lanes takes a token and walks its heads, so that the token's sines and cosines are
-// formed once for all of them.  A lane holds two 16-byte runs of a head that are each other's
-// partners, so turning them needs no exchange; the two sums of a head are moves between lanes.
+// formed once for all of them.  A lane holds 16 bytes of a head and the lane beside it their
+// partners; what they trade, and the two sums of a head, are moves between lanes.
 // Widths, rotations, pitches or addresses that are no multiples of that take a wave to a token,
 // an element at a time.
 //
 // Bound by memory.  One MI355X: 204,800 tokens of 2 + 2 heads of 64 bf16, 210 MB forward, 45 us
-// (4.7 TB/s); backward with weights 67 us (4.7 TB/s) and 5 for the weights' sums.  131,072 of 4 + 2
-// heads of 128 fp32, 805 MB: both together 361 us (5.6 TB/s).  Heads read one ahead, and results written
+// (4.7 TB/s); backward with weights 58 us (5.4 TB/s) and 5 for the weights' sums.  131,072 of 4 + 2
+// heads of 128 fp32, 805 MB: both together 360 us (5.6 TB/s).  Heads read one ahead, and results written
 // past the caches, measured the same.
 #include <hip/hip_runtime.h>
 
@@ -90,7 +90,7 @@ struct Eight<bf16> {
     }
 };
 
-// Sum over the G lanes of a group (a power of two up to 32), in all of them.
+// Sum over the G lanes of a group (a power of two), in all of them.
 template <int G>
 __device__ __forceinline__ float group_sum(float v, int lane) {
     if constexpr (G >= 2) v += lanes::dpp<0xB1, 0xF>(v, 0.0f);   // lanes 1, 0, 3, 2
@@ -98,32 +98,35 @@ __device__ __forceinline__ float group_sum(float v, int lane) {
     if constexpr (G >= 8) v += lanes::dpp<0x141, 0xF>(v, 0.0f);  // eight in reverse
     if constexpr (G >= 16) v += lanes::dpp<0x140, 0xF>(v, 0.0f);  // sixteen in reverse
     if constexpr (G >= 32) v += wtile::row_partner(v, (lane >> 4) & 1);
+    if constexpr (G >= 64) v += wtile::half_partner(v, lane >> 5);
     return v;
 }
 
-// Where a lane's two runs of a head lie.  Lanes of the rotated part hold elements i .. and
-// i + R / 2 .., the others two runs behind one another.
+// Where a lane's 16 bytes of a head lie.  In the rotated part, lanes 2 c and 2 c + 1 have the c-th
+// run and its partner, R / 2 further on, so that a load of the wave is whole cache lines (both runs
+// in one lane, half of each line at a time: the backward of 204,800 tokens 67 us, not 58).
 template <int VE>
 struct Place {
-    int a, b;
+    int at, pair;  // first element; of the rotation's pairs
     bool turned, some;
     __device__ __forceinline__ Place(int l, int D, int R) {
-        some = l * 2 * VE < D;
-        turned = l * 2 * VE < R;
-        a = turned ? l * VE : l * 2 * VE;
-        b = turned ? a + R / 2 : a + VE;
+        some = l * VE < D;
+        turned = l * VE < R;
+        pair = (l >> 1) * VE;
+        at = turned ? pair + (l & 1) * (R / 2) : l * VE;
     }
 };
 
-// (a, b) turned by the angle, or back with -sn.
+// v turned by the angle whose sine is sn for the second of a pair, -sn for the first; v as it is
+// where not turned.
 template <int VE>
-__device__ __forceinline__ void rotate(float (&a)[VE], float (&b)[VE], const float (&sn)[VE],
+__device__ __forceinline__ void rotate(float (&v)[VE], bool turned, const float (&sn)[VE],
                                        const float (&cs)[VE], float sign) {
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
-        const float s = sign * sn[e], x = a[e], y = b[e];
-        a[e] = fmaf(x, cs[e], -y * s);
-        b[e] = fmaf(y, cs[e], x * s);
+        const float other = lanes::dpp<0xB1, 0xF>(v[e], 0.0f);
+        const float r = fmaf(v[e], cs[e], sign * sn[e] * other);
+        v[e] = turned ? r : v[e];
     }
 }
 
@@ -134,84 +137,71 @@ __global__ __launch_bounds__(kNT) void head_kernel(Params p) {
     constexpr int VE = E::VE, kGroups = kNT / G;
     const int t = threadIdx.x, lane = t & 63, l = t % G;
     const Place<VE> at(l, p.D, p.R);
-    const u4v zero = {0, 0, 0, 0};
-    float w[2][2][VE];
-    float dw[2][2][VE];
+    float w[2][VE], dw[2][VE];
+    const bool second = l & 1;
+    double rate[VE / 2];  // each lane of a pair forms half of their sines
+#pragma unroll
+    for (int e = 0; e < VE / 2; ++e)
+        rate[e] = at.turned ? p.rate[at.pair + (second ? VE / 2 : 0) + e] : 0.0;
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
-            w[s][0][e] = at.some && p.w[s] ? p.w[s][at.a + e] : 1.0f;
-            w[s][1][e] = at.some && p.w[s] ? p.w[s][at.b + e] : 1.0f;
-            dw[s][0][e] = dw[s][1][e] = 0.0f;
+            w[s][e] = at.some && p.w[s] ? p.w[s][at.at + e] : 1.0f;
+            dw[s][e] = 0.0f;
         }
-    double rate[VE];
-#pragma unroll
-    for (int e = 0; e < VE; ++e) rate[e] = at.turned ? p.rate[at.a + e] : 0.0;
     for (int64_t n = (int64_t)blockIdx.x * kGroups + t / G; n < p.N;
          n += (int64_t)gridDim.x * kGroups) {
         float sn[VE], cs[VE];
         const double pos = p.R ? (double)p.positions[n] : 0.0;
 #pragma unroll
-        for (int e = 0; e < VE; ++e) turn(pos * rate[e], sn[e], cs[e]);
+        for (int e = 0; e < VE / 2; ++e) {
+            float s0, c0;
+            turn(pos * rate[e], s0, c0);
+            const float s1 = lanes::dpp<0xB1, 0xF>(s0, 0.0f), c1 = lanes::dpp<0xB1, 0xF>(c0, 0.0f);
+            sn[e] = second ? s1 : -s0;
+            cs[e] = second ? c1 : c0;
+            sn[VE / 2 + e] = second ? s0 : -s1;
+            cs[VE / 2 + e] = second ? c0 : c1;
+        }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const T* x = (const T*)p.x[s] + n * p.pitch[s];
             const int64_t row = n * p.heads[s];
             for (int h = 0; h < p.heads[s]; ++h) {
-                const int64_t o = (row + h) * p.D;
-                u4v ra = zero, rb = zero, da = zero, db = zero;
+                const int64_t o = (row + h) * p.D + at.at;
+                u4v rx = {0, 0, 0, 0}, rg = {0, 0, 0, 0};
                 if (at.some) {
-                    ra = *(const u4v*)(x + h * p.D + at.a);
-                    rb = *(const u4v*)(x + h * p.D + at.b);
-                    if constexpr (kMode > 0) {
-                        da = *(const u4v*)((const T*)p.dy[s] + o + at.a);
-                        db = *(const u4v*)((const T*)p.dy[s] + o + at.b);
-                    }
+                    rx = *(const u4v*)(x + h * p.D + at.at);
+                    if constexpr (kMode > 0) rg = *(const u4v*)((const T*)p.dy[s] + o);
                 }
-                float a[VE], b[VE];
-                E::get(ra, a);
-                E::get(rb, b);
+                float v[VE];
+                E::get(rx, v);
                 float q = 0.0f;
 #pragma unroll
-                for (int e = 0; e < VE; ++e) q = fmaf(a[e], a[e], fmaf(b[e], b[e], q));
+                for (int e = 0; e < VE; ++e) q = fmaf(v[e], v[e], q);
                 const float r = 1.0f / sqrtf(fmaf(group_sum<G>(q, lane), p.share, p.eps));
                 if constexpr (kMode == 0) {
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        a[e] *= r * w[s][0][e];
-                        b[e] *= r * w[s][1][e];
-                    }
-                    if (at.turned) rotate(a, b, sn, cs, 1.0f);
+                    for (int e = 0; e < VE; ++e) v[e] *= r * w[s][e];
+                    rotate(v, at.turned, sn, cs, 1.0f);
                 } else {
-                    float ga[VE], gb[VE];
-                    E::get(da, ga);
-                    E::get(db, gb);
-                    if (at.turned) rotate(ga, gb, sn, cs, -1.0f);
+                    float g[VE];
+                    E::get(rg, g);
+                    rotate(g, at.turned, sn, cs, -1.0f);
                     float dot = 0.0f;
 #pragma unroll
                     for (int e = 0; e < VE; ++e) {
-                        a[e] *= r;
-                        b[e] *= r;
-                        if constexpr (kMode == 2) {
-                            dw[s][0][e] = fmaf(ga[e], a[e], dw[s][0][e]);
-                            dw[s][1][e] = fmaf(gb[e], b[e], dw[s][1][e]);
-                        }
-                        ga[e] *= w[s][0][e];
-                        gb[e] *= w[s][1][e];
-                        dot = fmaf(ga[e], a[e], fmaf(gb[e], b[e], dot));
+                        v[e] *= r;
+                        if constexpr (kMode == 2) dw[s][e] = fmaf(g[e], v[e], dw[s][e]);
+                        g[e] *= w[s][e];
+                        dot = fmaf(g[e], v[e], dot);
                     }
                     dot = group_sum<G>(dot, lane) * p.share;
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        a[e] = r * fmaf(-dot, a[e], ga[e]);
-                        b[e] = r * fmaf(-dot, b[e], gb[e]);
-                    }
+                    for (int e = 0; e < VE; ++e) v[e] = r * fmaf(-dot, v[e], g[e]);
                 }
-                if (at.some) {
-                    *(u4v*)((T*)p.out[s] + o + at.a) = E::put(a);
-                    *(u4v*)((T*)p.out[s] + o + at.b) = E::put(b);
-                }
+                if (at.some) *(u4v*)((T*)p.out[s] + o) = E::put(v);
             }
         }
     }
@@ -219,22 +209,20 @@ __global__ __launch_bounds__(kNT) void head_kernel(Params p) {
         // The groups' sums, in their order.
         __shared__ float all[kNT][VE + 1];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s) {
+            __syncthreads();
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                __syncthreads();
-#pragma unroll
-                for (int e = 0; e < VE; ++e) all[t][e] = dw[s][half][e];
-                __syncthreads();
-                for (int i = t; i < G * VE; i += kNT) {
-                    const int li = i / VE, e = i % VE;
-                    const Place<VE> to(li, p.D, p.R);
-                    if (!to.some) continue;
-                    float sum = 0.0f;
-                    for (int g = 0; g < kGroups; ++g) sum += all[g * G + li][e];
-                    p.part[((int64_t)blockIdx.x * 2 + s) * p.D + (half ? to.b : to.a) + e] = sum;
-                }
+            for (int e = 0; e < VE; ++e) all[t][e] = dw[s][e];
+            __syncthreads();
+            for (int i = t; i < G * VE; i += kNT) {
+                const int li = i / VE, e = i % VE;
+                const Place<VE> to(li, p.D, p.R);
+                if (!to.some) continue;
+                float sum = 0.0f;
+                for (int g = 0; g < kGroups; ++g) sum += all[g * G + li][e];
+                p.part[((int64_t)blockIdx.x * 2 + s) * p.D + to.at + e] = sum;
             }
+        }
     }
 }
 
@@ -368,8 +356,8 @@ int lanes_of(const QkNormArgs& a, bool backward) {
         if (backward) bits |= (uintptr_t)a.dy[s];
     }
     if (bits & 15u) return 0;
-    int g = 1;
-    while (g * 2 * ve < a.D) g *= 2;
+    int g = 2;  // pairs of lanes
+    while (g * ve < a.D) g *= 2;
     return g;
 }
 
@@ -377,13 +365,13 @@ template <typename T, int kMode>
 void launch(const Params& p, int g, unsigned groups, hipStream_t st) {
     switch (g) {
         case 0: any_kernel<T, kMode><<<groups, kNT, 0, st>>>(p); break;
-        case 1: head_kernel<T, 1, kMode><<<groups, kNT, 0, st>>>(p); break;
         case 2: head_kernel<T, 2, kMode><<<groups, kNT, 0, st>>>(p); break;
         case 4: head_kernel<T, 4, kMode><<<groups, kNT, 0, st>>>(p); break;
         case 8: head_kernel<T, 8, kMode><<<groups, kNT, 0, st>>>(p); break;
         case 16: head_kernel<T, 16, kMode><<<groups, kNT, 0, st>>>(p); break;
+        case 32: head_kernel<T, 32, kMode><<<groups, kNT, 0, st>>>(p); break;
         default:
-            if constexpr (sizeof(T) == 4) head_kernel<T, 32, kMode><<<groups, kNT, 0, st>>>(p);
+            if constexpr (sizeof(T) == 4) head_kernel<T, 64, kMode><<<groups, kNT, 0, st>>>(p);
     }
 }
 
