@@ -828,6 +828,16 @@ def _adamw_moments(opt, out):
     return out
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream  # of a device, here the current one
+
+
+def _dense(t, name):
+    """The address of a tensor that the others are compared with."""
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
 @_on_device
 def embed(table, ids, scale=1.0, pad_id=-1):
     """Rows of an item table by id: table [V,D], ids int32 of any shape.  Returns
@@ -836,11 +846,11 @@ def embed(table, ids, scale=1.0, pad_id=-1):
     if table.dim() != 2:
         raise ValueError("table must be [V, D]")
     V, D = table.shape
-    io, dt, at = io_code(table.dtype), table.dtype, table.get_device()
+    io, at = io_code(table.dtype), table.get_device()
     out = table.new_empty((*ids.shape, D))
     _check(recblr_embed_forward(
-        _arg(table, (V, D), dt, at, "table"), _arg(ids, ids.shape, torch.int32, at, "ids"),
-        out.data_ptr(), ids.numel(), V, D, scale, pad_id, io, _stream()), "recblr_embed_forward")
+        _dense(table, "table"), _arg(ids, ids.shape, torch.int32, at, "ids"), out.data_ptr(),
+        ids.numel(), V, D, scale, pad_id, io, _raw_stream(at)), "recblr_embed_forward")
     return out
 
 
@@ -863,7 +873,7 @@ def embed_backward(ids, dout, V, scale=1.0, pad_id=-1, into=None):
     _check(recblr_embed_backward(
         _arg(ids, ids.shape, torch.int32, at, "ids"),
         _arg(dout, (*ids.shape, D), dt, at, "dout"), _arg(dtable, (V, D), dt, at, "into"), N, V, D,
-        scale, pad_id, into is not None, io, ws.data_ptr() if n else None, n, _stream()),
+        scale, pad_id, into is not None, io, ws.data_ptr() if n else None, n, _raw_stream(at)),
         "recblr_embed_backward")
     return dtable
 
@@ -929,8 +939,8 @@ def qk_norm(q, k, wq=None, wk=None, positions=None, rotate=None, base=10000.0, n
     `rotate` elements are turned (None: all of an even width; 0: none).  Returns (q, k), dense."""
     before, after, _keep = _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps)
     qn, kn = _dense_like(q), _dense_like(k)
-    _check(recblr_qk_norm_forward(*before, qn.data_ptr(), kn.data_ptr(), *after, _stream()),
-           "recblr_qk_norm_forward")
+    _check(recblr_qk_norm_forward(*before, qn.data_ptr(), kn.data_ptr(), *after,
+                                  _raw_stream(q.get_device())), "recblr_qk_norm_forward")
     return qn, kn
 
 
@@ -955,7 +965,7 @@ def qk_norm_backward(q, k, dqn, dkn, wq=None, wk=None, positions=None, rotate=No
     _check(recblr_qk_norm_backward(
         *before, _arg(dqn, q.shape, dt, at, "dqn"), _arg(dkn, k.shape, dt, at, "dkn"),
         *(None if t is None else t.data_ptr() for t in out.values()), *after,
-        ws.data_ptr() if n else None, n, _stream()), "recblr_qk_norm_backward")
+        ws.data_ptr() if n else None, n, _raw_stream(at)), "recblr_qk_norm_backward")
     return out
 
 
@@ -977,7 +987,7 @@ def policy_loss(logits, ids, old_logp, advantage, ref_logp=None, weight=None, te
         raise ValueError("logits must be [N, V]")
     if kl > 0 and ref_logp is None:
         raise ValueError("kl > 0 needs ref_logp")
-    N, V = logits.shape
+    (N, V), row = logits.shape, logits.shape[:1]
     io, dt, dev, at, f32 = io_code(logits.dtype), logits.dtype, logits.device, \
         logits.get_device(), torch.float32
     loss = torch.empty(1, dtype=f32, device=dev)
@@ -987,11 +997,11 @@ def policy_loss(logits, ids, old_logp, advantage, ref_logp=None, weight=None, te
     n = _policy_workspace_size(N, V, io)
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
     _check(recblr_policy_loss(
-        _arg(logits, (N, V), dt, at, "logits"), _arg(ids, (N,), torch.int32, at, "ids"),
-        _arg(old_logp, (N,), f32, at, "old_logp"), _arg(advantage, (N,), f32, at, "advantage"),
-        _arg(ref_logp, (N,), f32, at, "ref_logp"), _arg(weight, (N,), f32, at, "weight"),
+        _dense(logits, "logits"), _arg(ids, row, torch.int32, at, "ids"),
+        _arg(old_logp, row, f32, at, "old_logp"), _arg(advantage, row, f32, at, "advantage"),
+        _arg(ref_logp, row, f32, at, "ref_logp"), _arg(weight, row, f32, at, "weight"),
         loss.data_ptr(), logp.data_ptr(), _arg(out, (N, V), dt, at, "out"), N, V, temperature,
-        clip_low, clip_high, kl, io, ws.data_ptr() if n else None, n, _stream()),
+        clip_low, clip_high, kl, io, ws.data_ptr() if n else None, n, _raw_stream(at)),
         "recblr_policy_loss")
     return loss, logp, out
 
