@@ -908,10 +908,11 @@ def _dense_like(t):
 def _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps):
     """The arguments that qk_norm and qk_norm_backward share, as two lists around the outputs."""
     dt, at, f32 = q.dtype, q.get_device(), torch.float32
-    io = io_code(dt)
-    if q.dim() < 3 or q.shape[:-2] != k.shape[:-2] or q.shape[-1] != k.shape[-1]:
+    io, qs, ks = io_code(dt), q.shape, k.shape
+    lead = qs[:-2]
+    if len(qs) < 3 or lead != ks[:-2] or qs[-1] != ks[-1]:
         raise ValueError("q and k must be [..., heads, D] with the same tokens and width")
-    lead, (H, D), HK = q.shape[:-2], q.shape[-2:], k.shape[-2]
+    H, D, HK = qs[-2], qs[-1], ks[-2]
     if norm not in ("l2", "rms"):
         raise ValueError('norm must be "l2" or "rms"')
     rotate = D // 2 * 2 if rotate is None else rotate
@@ -920,7 +921,10 @@ def _qk_inputs(q, k, wq, wk, positions, rotate, base, norm, eps):
             raise ValueError("positions are needed unless q is [B, L, H, D]")
         positions = torch.arange(lead[1], dtype=torch.int32, device=q.device).repeat(lead[0])
         positions = positions.view(lead)
-    (qp, q_pitch), (kp, k_pitch) = _tokens(q, dt, at, "q"), _tokens(k, dt, at, "k")
+    if q.is_contiguous() and k.is_contiguous() and k.dtype is dt and k.get_device() == at:
+        (qp, q_pitch), (kp, k_pitch) = (q.data_ptr(), H * D), (k.data_ptr(), HK * D)
+    else:
+        (qp, q_pitch), (kp, k_pitch) = _tokens(q, dt, at, "q"), _tokens(k, dt, at, "k")
     before = (qp, kp, q_pitch, k_pitch, _arg(wq, (D,), f32, at, "wq"),
               _arg(wk, (D,), f32, at, "wk"),
               _arg(positions, lead, torch.int32, at, "positions") if rotate else None)
