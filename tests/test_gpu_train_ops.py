@@ -151,7 +151,7 @@ EMBED = [(1, 1, 1), (1, 5, 64), (7, 3, 33), (64, 1, 128), (1000, 50, 48), (1024,
          (1025, 4, 64), (1025, 3000, 100), (2048, 4095, 130), (2049, 4096, 64), (5000, 1, 5),
          (6001, 2, 64), (64, 1, 33), (65, 1, 33), (129, 2, 64), (4095, 70, 16),
          (4096, 4000, 8), (4096, 1, 130), (4097, 300, 8), (4100, 1, 64), (9001, 2, 130),
-         (10240, 4096, 64), (9000, 70000, 7), (4500, 300, 600), (70000, 5000, 20)]
+         (10240, 4096, 64), (70, 9, 4096), (4200, 9, 2049), (9000, 70000, 7), (4500, 300, 600), (70000, 5000, 20)]
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
@@ -419,6 +419,25 @@ def test_qk_norm_positions(rb):
     w = torch.ones(64, device="cuda")
     d = rb.qk_norm_backward(q[:0], q[:0], q[:0], q[:0], wq=w, wk=None)
     assert not d["dwq"].any() and d["dwk"] is None
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [64, 33])
+def test_qk_norm_one_weight(rb, io, D):
+    """Weights for queries or for keys alone: the other one's are ones, and have no gradient."""
+    import torch
+    c = qk_case(io, (3, 40), 2, 1, D, D // 2 * 2, far=50)
+    pos, one = ints(c["pos"]), torch.ones(D, device="cuda")
+    full = dict(wq=c["wq"], wk=c["wk"], positions=pos)
+    for wq, wk in ((c["wq"], None), (None, c["wk"])):
+        some = dict(full, wq=wq, wk=wk)
+        ones = dict(full, wq=one if wq is None else wq, wk=one if wk is None else wk)
+        for a, b in zip(rb.qk_norm(c["q"], c["k"], **some), rb.qk_norm(c["q"], c["k"], **ones)):
+            assert torch.equal(a, b)
+        a = rb.qk_norm_backward(c["q"], c["k"], c["dq"], c["dk"], **some)
+        b = rb.qk_norm_backward(c["q"], c["k"], c["dq"], c["dk"], **ones)
+        for name, w in (("dq", 1), ("dk", 1), ("dwq", wq), ("dwk", wk)):
+            assert a[name] is None if w is None else torch.equal(a[name], b[name]), name
 
 
 def test_qk_norm_nan_stays_in_its_head(rb):
@@ -904,6 +923,18 @@ def test_muon_writes_its_matrices_only(rb):
             torch.cuda.synchronize()
             assert p_ok() and m_ok() and torch.equal(g, before)
             assert torch.isfinite(p).all()
+
+
+def test_muon_shared_gradient(rb):
+    """One gradient for two matrices, small and large ones."""
+    import torch
+    for shape in ((50, 40), (300, 200)):
+        p = [torch.randn(shape, device="cuda")]
+        p.append(p[0].clone())
+        g = torch.randn(shape, device="cuda")
+        before = p[0].clone()
+        rb.Muon(p).step([g, g])
+        assert torch.equal(p[0], p[1]) and not torch.equal(p[0], before)
 
 
 def test_muon_binding(rb):
