@@ -685,6 +685,28 @@ def test_policy_rows_of_one_value(rb, io, size, T):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(2048, 1000), (2048, 4000), (512, 131072)])
+def test_policy_sums_lean_to_no_side(rb, io, size):
+    """The mean error of logp over the rows.  Roundings of logp itself, of numbers of 16 or less, are
+    within U 8 and random: their mean is within 5 sigma = 5 U 8 / sqrt(3 N) < U / 1.9 for N = 2048,
+    U 1.03 for 512.  What a sum loses on one side would not go with the number of rows: small powers
+    added one by one to a sum of 131,072 lose 3 U.  Half a U is left for the powers' own."""
+    import torch
+    N, V = size
+    torch.manual_seed(0)
+    x = (3 * torch.randn(N, V, device="cuda")).to(dtype_of(io))
+    ids = torch.argmax(x.float() / 0.8 - torch.log(-torch.log(torch.rand(N, V, device="cuda"))), 1)
+    z = torch.zeros(N, device="cuda")
+    _, logp, _ = rb.policy_loss(x, ids.int(), z, z, temperature=0.8)
+    want = torch.cat([torch.log_softmax(c.double() / 0.8, 1).gather(1, i[:, None])[:, 0]
+                      for c, i in zip(x.split(128), ids.split(128))])
+    assert float(want.abs().max()) < 16
+    mean = float((logp.double() - want).mean())
+    print(f"mean error {mean / U:.3f} U", flush=True)
+    assert abs(mean) <= (5 * 8 / math.sqrt(3 * N) + 0.5) * U
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("size", ROWS)
 def test_policy_far_logits(rb, io, size):
     """Logits of a few million, where 2^(l K) against M K would lose their differences, and rows
