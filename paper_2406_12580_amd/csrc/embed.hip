@@ -17,7 +17,7 @@
 // an id sums its rows.
 //
 // One MI355X: 409,600 positions of 64 fp32 over 3,416 items: lookup 19 us, 5.6 TB/s of what it
-// writes; gradient 53: counts with the table's zeros 7, offsets 6, places 14, sums 20 (5.3 TB/s),
+// writes; gradient 53: counts with the table's zeros 7, offsets 6, places 13, sums 20 (5.3 TB/s),
 // joins 5.  524,288 of 128 bf16 over a million items: 48 and 98, of which its two passes of
 // digits are 45.  Lookups and sums are bound by memory, the rest by a launch's chain of reads.
 #include <hip/hip_runtime.h>
@@ -287,7 +287,7 @@ constexpr int kMaxBits = 12, kMaxBins = 1 << kMaxBits;
 constexpr int kMaxBlocks = 512;
 constexpr int kWaves = kNT / kWave;
 constexpr int kTile = 2048;  // a block's positions are a multiple of this
-// Twice the waves that have positions, for the digits' work (256 threads: 15 us, not 14).
+// Twice the waves that have positions, for the digits' work (256 threads: a microsecond more).
 constexpr int kPlaceThreads = 512, kEach = kMaxBins / kPlaceThreads;
 
 // ids of no row sort behind all others, as V.
@@ -295,12 +295,14 @@ __device__ __forceinline__ uint32_t key_of(int32_t id, int64_t V, int32_t pad_id
     return id == pad_id || id < 0 || id >= V ? (uint32_t)V : (uint32_t)id;
 }
 
+struct Entry {  // 8 bytes together: scattered writes go by their number
+    uint32_t key;
+    int32_t pos;
+};
 struct Sort {
-    const int32_t* ids;        // the first pass's keys
-    const uint32_t* keys_in;   // later passes'
-    const int32_t* pos_in;
-    uint32_t* keys;
-    int32_t* pos;
+    const int32_t* ids;  // the first pass's keys
+    const Entry* in;     // later passes'
+    Entry* out;
     uint32_t* counts;  // [blocks][bins]
     uint32_t* totals;  // [bins]
     int64_t N, V;
@@ -309,7 +311,7 @@ struct Sort {
     int32_t pad_id;
 };
 __device__ __forceinline__ uint32_t sort_key(const Sort& s, int64_t i) {
-    return s.ids ? key_of(s.ids[i], s.V, s.pad_id) : s.keys_in[i];
+    return s.ids ? key_of(s.ids[i], s.V, s.pad_id) : s.in[i].key;
 }
 
 // Blocks from s.blocks on fill the table with zeros, 16 bytes at a time.
@@ -397,7 +399,7 @@ __device__ __forceinline__ uint64_t alike(uint32_t d, bool live) {
     return (uint64_t)hi << 32 | lo;
 }
 
-// kBits: s.bits or more.  200 blocks of 2,048 positions and 4,096 digits in 14 us: a third of it
+// kBits: s.bits or more.  200 blocks of 2,048 positions and 4,096 digits in 13 us: a third of it
 // ranks and scattered writes, a third the digits' six arrays in LDS, the rest first reads.
 template <int kBits>
 __global__ __launch_bounds__(kPlaceThreads) void place_kernel(Sort s) {
@@ -475,7 +477,7 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(Sort s) {
 #pragma unroll
         for (int j = 0; j < B; ++j) {
             const int64_t i = i0 + j * kWave;
-            pos[j] = s.pos_in && i < to ? s.pos_in[i] : (int32_t)i;
+            pos[j] = !s.ids && i < to ? s.in[i].pos : (int32_t)i;
         }
         uint64_t same[B];
 #pragma unroll
@@ -488,8 +490,7 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(Sort s) {
                 const uint32_t place = next[slot] + __popcll(same[j] & below);
                 wave_fence();
                 if ((same[j] >> lane) == 1ull) next[slot] = place + 1;  // the last of its digit
-                s.keys[place] = keys[j];
-                s.pos[place] = pos[j];
+                s.out[place] = Entry{keys[j], pos[j]};
             }
             wave_fence();
         }
@@ -504,8 +505,7 @@ constexpr int kPiece = 64, kGroup = kSumWaves * kPiece;  // positions to a wave,
 // part: for each workgroup, the sum of a run that came from before it (slot 0) and of one that
 // starts in it and goes on (slot 1).
 template <typename T, int VL>
-__global__ __launch_bounds__(kSumThreads, 8) void sum_kernel(const uint32_t* __restrict__ keys,
-                                                          const int32_t* __restrict__ pos,
+__global__ __launch_bounds__(kSumThreads, 8) void sum_kernel(const Entry* __restrict__ sorted,
                                                           int64_t N, int64_t V, Grad g,
                                                           float* part) {
     // Of each wave the same two sums, and whether it has them: 1 a run from before that ends here,
@@ -515,10 +515,11 @@ __global__ __launch_bounds__(kSumThreads, 8) void sum_kernel(const uint32_t* __r
     const int lane = threadIdx.x & 63, w = wave_id();
     const int64_t from = (int64_t)blockIdx.x * kGroup + w * kPiece, i = from + lane;
     const uint32_t none = (uint32_t)V;
-    const uint32_t key = i < N ? keys[i] : none;
-    const uint32_t after = i + 1 < N ? keys[i + 1] : none;
-    const int at = i < N ? pos[i] : 0;
-    const uint32_t before = from > 0 && from <= N ? keys[from - 1] : none;
+    const Entry mine = i < N ? sorted[i] : Entry{none, 0};
+    const uint32_t key = mine.key;
+    const uint32_t after = i + 1 < N ? sorted[i + 1].key : none;
+    const int at = mine.pos;
+    const uint32_t before = from > 0 && from <= N ? sorted[from - 1].key : none;
     const int live = __popcll(__ballot(key != none));  // sorted: the first ones
     const uint64_t ends = __ballot(key != after);
     bool earlier = live > 0 && lanes::lane_of(key, 0) == before;  // the run came from before
@@ -623,26 +624,27 @@ constexpr int kJoin = 512;
 // The workgroup of the group in which a run starts that goes on: its parts in eight runs of
 // groups, then these in order.
 template <typename T, int VL>
-__global__ __launch_bounds__(kJoin) void join_kernel(const uint32_t* __restrict__ keys, int64_t N,
+__global__ __launch_bounds__(kJoin) void join_kernel(const Entry* __restrict__ sorted, int64_t N,
                                                      int64_t V, Grad g, const float* part,
                                                      int64_t groups) {
     constexpr int W = kJoin / kWave;
     __shared__ float all[W][kWave * VL];
     const int64_t p = blockIdx.x, last = p * kGroup + kGroup - 1;
     if (last + 1 >= N) return;
-    const uint32_t k = keys[last];
-    if (k == (uint32_t)V || keys[last + 1] != k) return;
-    if (keys[p * kGroup] == k && p > 0 && keys[p * kGroup - 1] == k) return;  // from before
+    const uint32_t k = sorted[last].key;
+    if (k == (uint32_t)V || sorted[last + 1].key != k) return;
+    if (sorted[p * kGroup].key == k && p > 0 && sorted[p * kGroup - 1].key == k)
+        return;  // from before
     // The last group whose first key is k: ever larger steps, then halves.
     int64_t lo = p + 1, step = 1;
-    while (lo + step < groups && keys[(lo + step) * kGroup] == k) {
+    while (lo + step < groups && sorted[(lo + step) * kGroup].key == k) {
         lo += step;
         step *= 2;
     }
-    int64_t hi = min(groups, lo + step);  // keys[lo * kGroup] == k, and not at hi
+    int64_t hi = min(groups, lo + step);  // k at lo * kGroup, and not at hi
     while (hi - lo > 1) {
         const int64_t mid = (lo + hi) / 2;
-        if (keys[mid * kGroup] == k) lo = mid;
+        if (sorted[mid * kGroup].key == k) lo = mid;
         else hi = mid;
     }
     const int lane = threadIdx.x & 63, w = wave_id();
@@ -678,7 +680,7 @@ __global__ __launch_bounds__(kJoin) void join_kernel(const uint32_t* __restrict_
 struct Plan {
     int passes, bits, blocks;
     int64_t each, groups;
-    size_t keys[2], pos[2], counts, totals, part, bytes;
+    size_t entries[2], counts, totals, part, bytes;
 };
 Plan plan(int64_t N, int64_t V, int64_t D) {
     auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -693,10 +695,8 @@ Plan plan(int64_t N, int64_t V, int64_t D) {
     p.groups = (N + kGroup - 1) / kGroup;
     size_t at = 0;
     for (int i = 0; i < (p.passes > 1 ? 2 : 1); ++i) {
-        p.keys[i] = at;
-        at += up((size_t)N * 4);
-        p.pos[i] = at;
-        at += up((size_t)N * 4);
+        p.entries[i] = at;
+        at += up((size_t)N * sizeof(Entry));
     }
     p.counts = at;
     at += up(((size_t)p.blocks << p.bits) * 4);
@@ -744,12 +744,11 @@ void launch_sums(const EmbedArgs& a, const Plan& pl, char* ws, const Grad& g, hi
         return;
     }
     const int last = (pl.passes + 1) % 2;  // passes write buffers 0, 1, 0, ...
-    const uint32_t* keys = (const uint32_t*)(ws + pl.keys[last]);
-    const int32_t* pos = (const int32_t*)(ws + pl.pos[last]);
+    const Entry* sorted = (const Entry*)(ws + pl.entries[last]);
     float* part = (float*)(ws + pl.part);
     const dim3 grid((unsigned)pl.groups, cols);
-    sum_kernel<T, VL><<<grid, kSumThreads, 0, st>>>(keys, pos, a.N, a.V, g, part);
-    join_kernel<T, VL><<<grid, kJoin, 0, st>>>(keys, a.N, a.V, g, part, pl.groups);
+    sum_kernel<T, VL><<<grid, kSumThreads, 0, st>>>(sorted, a.N, a.V, g, part);
+    join_kernel<T, VL><<<grid, kJoin, 0, st>>>(sorted, a.N, a.V, g, part, pl.groups);
 }
 
 }  // namespace
@@ -795,10 +794,8 @@ hipError_t launch_embed_backward(const EmbedArgs& a, void* ws, hipStream_t st) {
     if (a.N == 0 && fill > 0) count_kernel<<<dim3((unsigned)fill), kNT, 0, st>>>(s, a.dst, bytes);
     for (int i = 0; !few && i < pl.passes; ++i) {
         s.ids = i ? nullptr : a.ids;
-        s.keys_in = (const uint32_t*)(w + pl.keys[(i + 1) % 2]);
-        s.pos_in = i ? (const int32_t*)(w + pl.pos[(i + 1) % 2]) : nullptr;
-        s.keys = (uint32_t*)(w + pl.keys[i % 2]);
-        s.pos = (int32_t*)(w + pl.pos[i % 2]);
+        s.in = (const Entry*)(w + pl.entries[(i + 1) % 2]);
+        s.out = (Entry*)(w + pl.entries[i % 2]);
         s.counts = (uint32_t*)(w + pl.counts);
         s.totals = (uint32_t*)(w + pl.totals);
         s.blocks = pl.blocks;
