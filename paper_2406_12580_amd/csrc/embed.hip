@@ -17,9 +17,9 @@
 // an id sums its rows.
 //
 // One MI355X: 409,600 positions of 64 fp32 over 3,416 items: lookup 19 us, 5.6 TB/s of what it
-// writes; gradient 53: counts with the table's zeros 7, offsets 6, places 13, sums 20 (5.3 TB/s),
-// joins 5.  524,288 of 128 bf16 over a million items: 48 and 98, of which its two passes of
-// digits are 45.  Lookups and sums are bound by memory, the rest by a launch's chain of reads.
+// writes; gradient 50: counts with the table's zeros 7, offsets 6, places 13, sums 20 (5.3 TB/s),
+// joins 5.  524,288 of 128 bf16 over a million items: 48 and 92, of which its two passes of
+// digits are 41.  Lookups and sums are bound by memory, the rest by a launch's chain of reads.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -281,14 +281,13 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(const int32_t* __restr
 // Where digit d's number lies in LDS: threads walk runs of digits, 16 numbers apart at most.
 __host__ __device__ inline int skew(int d) { return d + (d >> 4); }
 
-// 12 bits: 3,416 items in one pass of three launches, a million in two; the counts of four waves
-// still fit LDS (104 KB).
+// 12 bits: 3,416 items in one pass of three launches, a million in two; the counts of eight waves
+// still fit LDS (136 KB).
 constexpr int kMaxBits = 12, kMaxBins = 1 << kMaxBits;
 constexpr int kMaxBlocks = 512;
-constexpr int kWaves = kNT / kWave;
 constexpr int kTile = 2048;  // a block's positions are a multiple of this
-// Twice the waves that have positions, for the digits' work (256 threads: a microsecond more).
-constexpr int kPlaceThreads = 512, kEach = kMaxBins / kPlaceThreads;
+constexpr int kPlaceThreads = 512, kWaves = kPlaceThreads / kWave;
+constexpr int kEach = kMaxBins / kPlaceThreads;  // digits of a thread
 
 // ids of no row sort behind all others, as V.
 __device__ __forceinline__ uint32_t key_of(int32_t id, int64_t V, int32_t pad_id) {
@@ -399,8 +398,8 @@ __device__ __forceinline__ uint64_t alike(uint32_t d, bool live) {
     return (uint64_t)hi << 32 | lo;
 }
 
-// kBits: s.bits or more.  200 blocks of 2,048 positions and 4,096 digits in 13 us: a third of it
-// ranks and scattered writes, a third the digits' six arrays in LDS, the rest first reads.
+// kBits: s.bits or more.  200 blocks of 2,048 positions and 4,096 digits in 13 us: first reads,
+// the digits' counts of eight waves in LDS, ranks and scattered writes, a third each.
 template <int kBits>
 __global__ __launch_bounds__(kPlaceThreads) void place_kernel(Sort s) {
     constexpr int TH = kPlaceThreads, B = kTile / (kWaves * kWave);  // positions read together
@@ -408,65 +407,54 @@ __global__ __launch_bounds__(kPlaceThreads) void place_kernel(Sort s) {
     __shared__ uint32_t wsum[TH / kWave];
     const int n = 1 << s.bits, t = threadIdx.x, lane = t & 63, w = wave_id();
     const int room = skew(n);
-    uint32_t* next = lds + w * room;                               // the wave's next places
-    uint32_t *first = lds + kWaves * room, *total = first + room;  // the block's first; all of them
+    uint32_t* next = lds + w * room;  // the wave's next places
     const uint64_t below = (1ull << lane) - 1;
-    // The positions of each of the first waves are one run of the block's; the others have none.
+    // A wave's positions are one run of its block's.
     const int64_t from = blockIdx.x * s.each + w * (s.each / kWaves) + lane;
-    const int64_t to = w < kWaves ? min(s.N, from - lane + s.each / kWaves) : 0;
+    const int64_t to = min(s.N, from - lane + s.each / kWaves);
     uint32_t keys[B];
 #pragma unroll
     for (int j = 0; j < B; ++j) keys[j] = from + j * kWave < to ? sort_key(s, from + j * kWave) : 0;
-    for (int i = 4 * t; i < kWaves * room; i += 4 * TH) *(u4v*)(lds + i) = u4v{0, 0, 0, 0};
+    // A thread's digits: the block's first places within them, and all of them.
+    const int run = (n + TH - 1) / TH;
     const uint32_t* counts = s.counts + (int64_t)blockIdx.x * n;
-    for (int i0 = t; i0 < n; i0 += kEach * TH) {
-        uint32_t a[kEach], b[kEach];
+    uint32_t first[kEach], total[kEach], mine = 0;
 #pragma unroll
-        for (int j = 0; j < kEach; ++j)
-            if (i0 + j * TH < n) {
-                a[j] = counts[i0 + j * TH];
-                b[j] = s.totals[i0 + j * TH];
-            }
-#pragma unroll
-        for (int j = 0; j < kEach; ++j)
-            if (i0 + j * TH < n) {
-                first[skew(i0 + j * TH)] = a[j];
-                total[skew(i0 + j * TH)] = b[j];
-            }
+    for (int k = 0; k < kEach; ++k) {
+        const bool in = k < run && t * run + k < n;
+        first[k] = in ? counts[t * run + k] : 0;
+        total[k] = in ? s.totals[t * run + k] : 0;
     }
+    for (int i = 4 * t; i < kWaves * room; i += 4 * TH) *(u4v*)(lds + i) = u4v{0, 0, 0, 0};
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < B; ++j)
         if (from + j * kWave < to) atomicAdd(&next[skew(keys[j] >> s.shift & (n - 1))], 1u);
     for (int64_t i = from + B * kWave; i < to; i += kWave)
         atomicAdd(&next[skew(sort_key(s, i) >> s.shift & (n - 1))], 1u);
-    __syncthreads();
     // Digits before a thread's run of digits, then each digit's first place for each wave.
-    const int run = (n + TH - 1) / TH;
-    uint32_t mine = 0;
-#pragma unroll 8
-    for (int k = 0; k < run; ++k) mine += t * run + k < n ? total[skew(t * run + k)] : 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) mine += total[k];
     const uint32_t upto = lanes::wave_scan(mine, 0u, [](uint32_t a, uint32_t b) { return a + b; });
     if (lane == kWave - 1) wsum[w] = upto;
     __syncthreads();
     uint32_t at = upto - mine;
     for (int k = 0; k < w; ++k) at += wsum[k];
-#pragma unroll 4
-    for (int k = 0; k < run; ++k) {
-        const int d = skew(t * run + k < n ? t * run + k : n - 1);
-        const bool in = t * run + k < n;
-        uint32_t c[kWaves], place = at + first[d];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+        if (k >= run || t * run + k >= n) break;
+        const int d = skew(t * run + k);
+        uint32_t c[kWaves], place = at + first[k];
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) c[v] = lds[v * room + d];
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) {
-            if (in) lds[v * room + d] = place;
+            lds[v * room + d] = place;
             place += c[v];
         }
-        at += in ? total[d] : 0;
+        at += total[k];
     }
     __syncthreads();
-    if (w >= kWaves) return;
     for (int64_t i0 = from; i0 - lane < to; i0 += B * kWave) {
         int32_t pos[B];
         if (i0 != from) {
@@ -708,7 +696,7 @@ Plan plan(int64_t N, int64_t V, int64_t D) {
     return p;
 }
 
-int place_lds(int bits) { return (kWaves + 2) * skew(1 << bits) * 4; }
+int place_lds(int bits) { return kWaves * skew(1 << bits) * 4; }
 
 template <int kBits>
 hipError_t launch_place(const Sort& s, hipStream_t st) {

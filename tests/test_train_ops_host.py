@@ -407,4 +407,4 @@ def test_embed_hand_overs(tmp_path):
         ops = _lds_runs(lines, kernel)
         print(kernel, ops)
         steps = ops[ops.rindex("B") + 1:].strip("F") + "F"
-        assert len(steps) >= 16 * 2 and steps == "RFWF" * (len(steps) // 4), ops
+        assert len(steps) >= 16 and steps == "RFWF" * (len(steps) // 4), ops
