@@ -340,10 +340,12 @@ __global__ __launch_bounds__(1024) void weights_kernel(const float* part, int ro
 
 // ------------------------------------------------------------------ launches
 // Workgroups: as many as there are tokens to take (with eight to a compute unit that go on,
-// 131,072 tokens took 379 us, not 361); rows of partial sums four to a compute unit at most.
+// 131,072 tokens took 379 us, not 361), as far as a launch has them, fewer than 2^32 threads; rows
+// of partial sums four to a compute unit at most.
 int64_t groups_of(int64_t tokens_each, int64_t N, bool sums) {
     const int64_t need = (N + tokens_each - 1) / tokens_each;
-    return sums && need > 1024 ? 1024 : need;
+    const int64_t most = sums ? 1024 : ((int64_t)1 << 32) / kNT - 1;
+    return need < most ? need : most;
 }
 
 // Lanes to a token's heads, where all runs of 16 bytes are aligned; 0: the other kernel.
