@@ -90,16 +90,72 @@ struct Eight<bf16> {
     }
 };
 
-// Sum over the G lanes of a group (a power of two), in all of them.
+// Sums and largest values over the G lanes of a group (a power of two), in all of them.
 template <int G>
-__device__ __forceinline__ float group_sum(float v, int lane) {
-    if constexpr (G >= 2) v += lanes::dpp<0xB1, 0xF>(v, 0.0f);   // lanes 1, 0, 3, 2
-    if constexpr (G >= 4) v += lanes::dpp<0x4E, 0xF>(v, 0.0f);   // 2, 3, 0, 1
-    if constexpr (G >= 8) v += lanes::dpp<0x141, 0xF>(v, 0.0f);  // eight in reverse
-    if constexpr (G >= 16) v += lanes::dpp<0x140, 0xF>(v, 0.0f);  // sixteen in reverse
-    if constexpr (G >= 32) v += wtile::row_partner(v, (lane >> 4) & 1);
-    if constexpr (G >= 64) v += wtile::half_partner(v, lane >> 5);
-    return v;
+struct Group {
+    int lane;
+    template <typename Op>
+    __device__ __forceinline__ float over(float v, Op op) const {
+        if constexpr (G >= 2) v = op(v, lanes::dpp<0xB1, 0xF>(v, 0.0f));   // lanes 1, 0, 3, 2
+        if constexpr (G >= 4) v = op(v, lanes::dpp<0x4E, 0xF>(v, 0.0f));   // 2, 3, 0, 1
+        if constexpr (G >= 8) v = op(v, lanes::dpp<0x141, 0xF>(v, 0.0f));  // eight in reverse
+        if constexpr (G >= 16) v = op(v, lanes::dpp<0x140, 0xF>(v, 0.0f));  // sixteen in reverse
+        if constexpr (G >= 32) v = op(v, wtile::row_partner(v, (lane >> 4) & 1));
+        if constexpr (G >= 64) v = op(v, wtile::half_partner(v, lane >> 5));
+        return v;
+    }
+    __device__ __forceinline__ float sum(float v) const {
+        return over(v, [](float a, float b) { return a + b; });
+    }
+    __device__ __forceinline__ float largest(float v) const {
+        return over(v, [](float a, float b) { return fmaxf(a, b); });
+    }
+};
+struct Wave {
+    __device__ __forceinline__ float sum(float v) const { return lanes::wave_sum(v); }
+    __device__ __forceinline__ float largest(float v) const {
+        v = lanes::wave_scan(v, 0.0f, [](float a, float b) { return fmaxf(a, b); });
+        return lanes::lane_of(v, kWave - 1);
+    }
+};
+
+// The sum of squares of a group's head, N elements a lane, times p.share, and eps.  Where it leaves
+// fp32's range, or comes so near its lower end that squares lose digits, the head is brought near 1
+// first: v by 2^-down, eps by its square.  (A head with an infinity or a NaN has none either.)
+struct Squares {
+    float sum;
+    int down;
+};
+template <int N, typename Lanes>
+__device__ __forceinline__ Squares squares_of(const Params& p, float (&v)[N], const Lanes& all) {
+    auto sum = [&](float eps) {
+        float q = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) q = fmaf(v[e], v[e], q);
+        return fmaf(all.sum(q), p.share, eps);
+    };
+    Squares s{sum(p.eps), 0};
+    const bool far = !(s.sum >= 0x1p-90f && s.sum < __builtin_inff());
+    if (__builtin_expect(__ballot(far) != 0, 0)) {  // of the whole wave: moves between lanes need all of a group
+        float top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) top = fmaxf(top, fabsf(v[e]));
+        top = all.largest(top);
+        const int power = (int)(__float_as_uint(top) >> 23) - 127;
+        s.down = !far ? 0 : power < -60 ? -60 : power > 126 ? 126 : power;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = ldexpf(v[e], -s.down);
+        s.sum = sum(ldexpf(p.eps, -2 * s.down));
+    }
+    return s;
+}
+// dx's factor of what squares_of took off x.
+template <int N>
+__device__ __forceinline__ void bring_back(const Squares& s, float (&v)[N]) {
+    if (__builtin_expect(__ballot(s.down != 0) != 0, 0)) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = ldexpf(v[e], -s.down);
+    }
 }
 
 // Where a lane's 16 bytes of a head lie.  In the rotated part, lanes 2 c and 2 c + 1 have the c-th
@@ -135,7 +191,8 @@ template <typename T, int G, int kMode>
 __global__ __launch_bounds__(kNT) void head_kernel(Params p) {
     using E = Eight<T>;
     constexpr int VE = E::VE, kGroups = kNT / G;
-    const int t = threadIdx.x, lane = t & 63, l = t % G;
+    const int t = threadIdx.x, l = t % G;
+    const Group<G> group{t & 63};
     const Place<VE> at(l, p.D, p.R);
     float w[2][VE], dw[2][VE];
     const bool second = l & 1;
@@ -177,10 +234,8 @@ __global__ __launch_bounds__(kNT) void head_kernel(Params p) {
                 }
                 float v[VE];
                 E::get(rx, v);
-                float q = 0.0f;
-#pragma unroll
-                for (int e = 0; e < VE; ++e) q = fmaf(v[e], v[e], q);
-                const float r = 1.0f / sqrtf(fmaf(group_sum<G>(q, lane), p.share, p.eps));
+                const Squares sq = squares_of(p, v, group);
+                const float r = 1.0f / sqrtf(sq.sum);
                 if constexpr (kMode == 0) {
 #pragma unroll
                     for (int e = 0; e < VE; ++e) v[e] *= r * w[s][e];
@@ -197,9 +252,10 @@ __global__ __launch_bounds__(kNT) void head_kernel(Params p) {
                         g[e] *= w[s][e];
                         dot = fmaf(g[e], v[e], dot);
                     }
-                    dot = group_sum<G>(dot, lane) * p.share;
+                    dot = group.sum(dot) * p.share;
 #pragma unroll
                     for (int e = 0; e < VE; ++e) v[e] = r * fmaf(-dot, v[e], g[e]);
+                    bring_back(sq, v);
                 }
                 if (at.some) *(u4v*)((T*)p.out[s] + o) = E::put(v);
             }
@@ -263,30 +319,30 @@ __global__ __launch_bounds__(kNT) void any_kernel(Params p) {
                 const int64_t o = (n * p.heads[s] + h) * p.D;
                 const T* dy = (const T*)p.dy[s] + o;
                 T* out = (T*)p.out[s] + o;
-                float v[J], q = 0.0f;
+                float v[J], m[J], g[J];  // of x; partners, of x or dy; of dy
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     v[j] = live[j] ? to_f32(x[lane + kWave * j]) : 0.0f;
-                    q = fmaf(v[j], v[j], q);
+                    m[j] = live[j] ? to_f32((kMode ? dy : x)[mate[j]]) : 0.0f;
+                    if constexpr (kMode > 0) g[j] = live[j] ? to_f32(dy[lane + kWave * j]) : 0.0f;
                 }
-                const float r = 1.0f / sqrtf(fmaf(lanes::wave_sum(q), p.share, p.eps));
+                const Squares sq = squares_of(p, v, Wave{});
+                const float r = 1.0f / sqrtf(sq.sum);
                 float y[J];
                 if constexpr (kMode == 0) {
+                    const float by = ldexpf(1.0f, -sq.down);
 #pragma unroll
                     for (int j = 0; j < J; ++j) {
-                        const float m = live[j] ? to_f32(x[mate[j]]) : 0.0f;
                         const float wm = p.w[s] && live[j] ? p.w[s][mate[j]] : 1.0f;
                         y[j] = v[j] * (r * w[s][j]);
                         if (side[j] != 0.0f)
-                            y[j] = fmaf(y[j], cs[j], side[j] * (m * (r * wm) * sn[j]));
+                            y[j] = fmaf(y[j], cs[j], side[j] * (m[j] * by * (r * wm) * sn[j]));
                     }
                 } else {
-                    float g[J], dot = 0.0f;
+                    float dot = 0.0f;
 #pragma unroll
                     for (int j = 0; j < J; ++j) {
-                        g[j] = live[j] ? to_f32(dy[lane + kWave * j]) : 0.0f;
-                        const float m = live[j] ? to_f32(dy[mate[j]]) : 0.0f;
-                        if (side[j] != 0.0f) g[j] = fmaf(g[j], cs[j], -side[j] * (m * sn[j]));
+                        if (side[j] != 0.0f) g[j] = fmaf(g[j], cs[j], -side[j] * (m[j] * sn[j]));
                         v[j] *= r;
                         if constexpr (kMode == 2) dw[s][j] = fmaf(g[j], v[j], dw[s][j]);
                         g[j] *= w[s][j];
@@ -295,6 +351,7 @@ __global__ __launch_bounds__(kNT) void any_kernel(Params p) {
                     dot = lanes::wave_sum(dot) * p.share;
 #pragma unroll
                     for (int j = 0; j < J; ++j) y[j] = r * fmaf(-dot, v[j], g[j]);
+                    bring_back(sq, y);
                 }
 #pragma unroll
                 for (int j = 0; j < J; ++j)

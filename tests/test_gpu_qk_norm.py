@@ -4,7 +4,8 @@ has workgroups for, more elements than 31 bits count.  Ordinary sizes are in tes
 import numpy as np
 import pytest
 
-from test_gpu_train_ops import ints, put, rb  # noqa: F401
+import train_ops_reference as ref
+from test_gpu_train_ops import LAST, U, ints, put, qk_case, rb, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -40,3 +41,46 @@ def test_tokens_beyond_a_launch(rb, io, times, H, D, R):  # noqa: F811
     torch.cuda.synchronize()
     got = rb.qk_norm_backward(q, k, dq, dk, positions=pos, **how)
     assert is_repeated(got["dq"], want[2]) and is_repeated(got["dk"], want[3])
+
+
+def check_far(rb, c, eps):  # noqa: F811
+    io, R, D = c["io"], c["rotate"], c["q"].shape[-1]
+    how = dict(wq=c["wq"], wk=c["wk"], positions=ints(c["pos"]) if R else None, rotate=R,
+               norm=c["norm"], eps=eps)
+    qn, kn = rb.qk_norm(c["q"], c["k"], **how)
+    got = rb.qk_norm_backward(c["q"], c["k"], c["dq"], c["dk"], **how)
+    least = 2.0 ** (-149 if io == "f32" else -133)
+    for name, y in (("q", qn), ("k", kn)):
+        o = ref.qk_norm(c[name + "_"], c["w" + name + "_"], c["pos"], R, 10000.0, c["norm"],
+                        float(np.float32(eps)), dy=c["d" + name + "_"])
+        amp = ref.amplitude(o["y"], R)
+        within(name, y, o["y"], (D / 2 + 18) * U * amp + LAST[io] * np.abs(o["y"]) + 4 * least)
+        dot = (np.abs(o["u"]) * o["a_size"]).sum(-1, keepdims=True)
+        bound = U * o["r"] * ((D / 2 + 24) * o["a_size"]
+                              + o["s"] * np.abs(o["u"]) * dot * (2 * D + 48))
+        within("d" + name, got["d" + name], o["dx"], bound + LAST[io] * np.abs(o["dx"]) + least)
+        if c["w" + name] is not None:
+            rows = o["dx"].size // D
+            within("dw" + name, got["dw" + name], o["dw"], (rows + D / 2 + 20) * U * o["dw_size"])
+
+
+# Heads whose squares are beyond fp32's range at one end or the other, beside ordinary ones.
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("norm,weights", [("rms", True), ("l2", False)])
+@pytest.mark.parametrize("D,R", [(16, 16), (64, 32), (128, 128), (256, 0), (17, 16), (255, 254)])
+@pytest.mark.parametrize("sizes,eps", [((1.0, 1e19, 1e20, 1e25, 1e30, 2e37), 1e-6),
+                                       ((1.0, 1e-6, 1e-19, 1e-22, 1e-30, 1e20), 1e-30),
+                                       ((1.0, 0.0, 1e-19, 1e-22, 1e-36, 1e30), 1e-45)])
+def test_heads_far_from_one(rb, io, norm, weights, D, R, sizes, eps):  # noqa: F811
+    """Elements are within 4.5 of these sizes times 2.  Results have the bounds of ordinary heads,
+    with a floor of a denormal's rounding in place of 1e-38, times what follows it: of y by the
+    weight (below 2) and the rotation, of dx none."""
+    print(io, norm, D, R, sizes, flush=True)
+    c = qk_case(io, (3, 11), 2, 4, D, R, norm=norm, weights=weights, far=100, seed=D)
+    r = np.random.default_rng(1)
+    for name in ("q", "k"):
+        by = r.permutation(np.resize(sizes, c[name].shape[0] * 11 * c[name].shape[2]))
+        x = c[name + "_"] * by.reshape(3, 11, -1, 1)
+        c[name], c[name + "_"] = put(x, io)
+        assert np.isfinite(c[name + "_"]).all()
+    check_far(rb, c, eps)
