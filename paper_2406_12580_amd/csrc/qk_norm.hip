@@ -48,12 +48,19 @@ struct Params {
 };
 
 // sin and cos of `turns` full turns: whole turns are taken off in 64 bits, so what is left of a
-// far position's angle is exact to fp32.  The hardware takes turns; its results over [-1/2, 1/2]
-// are within 2^-23 of the sine (16 million points).
+// far position's angle is exact to fp32.  For bf16 by the hardware, which takes turns: it is off by
+// up to 2^-23, small angles' sines too, and a result's rounding to bf16 by 2^-9 of it (100,000
+// tokens of 4 + 2 heads of 128: 57 us, 61 with fp32's).  For fp32 that would be a third of the
+// results' error, and the function costs nothing beside twice the bytes.
+template <typename T>
 __device__ __forceinline__ void turn(double turns, float& sn, float& cs) {
     const float t = (float)(turns - rint(turns));
-    sn = __builtin_amdgcn_sinf(t);
-    cs = __builtin_amdgcn_cosf(t);
+    if constexpr (sizeof(T) == 4) {
+        sincospif(2.0f * t, &sn, &cs);
+    } else {
+        sn = __builtin_amdgcn_sinf(t);
+        cs = __builtin_amdgcn_cosf(t);
+    }
 }
 
 template <typename T>
@@ -214,7 +221,7 @@ __global__ __launch_bounds__(kNT) void head_kernel(Params p) {
 #pragma unroll
         for (int e = 0; e < VE / 2; ++e) {
             float s0, c0;
-            turn(pos * rate[e], s0, c0);
+            turn<T>(pos * rate[e], s0, c0);
             const float s1 = lanes::dpp<0xB1, 0xF>(s0, 0.0f), c1 = lanes::dpp<0xB1, 0xF>(c0, 0.0f);
             sn[e] = second ? s1 : -s0;
             cs[e] = second ? c1 : c0;
@@ -283,9 +290,11 @@ __global__ __launch_bounds__(kNT) void head_kernel(Params p) {
 }
 
 // A wave to a token, element lane + 64 j of a head in its j-th place: any width and alignment.
-// Partners are read a second time, from the caches.
+// Partners are read a second time, from the caches.  Forward, seven waves to a SIMD with a few
+// registers of constants spilled: 204,800 tokens of 2 + 2 heads of 17 fp32 160 us, of 72 bf16 194;
+// six without 170 and 207.
 template <typename T, int kMode>
-__global__ __launch_bounds__(kNT) void any_kernel(Params p) {
+__global__ __launch_bounds__(kNT, kMode ? 5 : 7) void any_kernel(Params p) {
     constexpr int J = kMaxD / kWave;
     const int lane = threadIdx.x & 63, w0 = wave_id(), half = p.R / 2;
     float w[2][J], dw[2][J];
@@ -311,7 +320,8 @@ __global__ __launch_bounds__(kNT) void any_kernel(Params p) {
         float sn[J], cs[J];
         const double pos = p.R ? (double)p.positions[n] : 0.0;
 #pragma unroll
-        for (int j = 0; j < J; ++j) turn(pos * rate[j], sn[j], cs[j]);
+        for (int j = 0; j < J; ++j)
+            if (kWave * j < p.R) turn<T>(pos * rate[j], sn[j], cs[j]);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             for (int h = 0; h < p.heads[s]; ++h) {
@@ -333,8 +343,9 @@ __global__ __launch_bounds__(kNT) void any_kernel(Params p) {
                     const float by = ldexpf(1.0f, -sq.down);
 #pragma unroll
                     for (int j = 0; j < J; ++j) {
-                        const float wm = p.w[s] && live[j] ? p.w[s][mate[j]] : 1.0f;
                         y[j] = v[j] * (r * w[s][j]);
+                        if (kWave * j >= p.R) continue;
+                        const float wm = p.w[s] && live[j] ? p.w[s][mate[j]] : 1.0f;
                         if (side[j] != 0.0f)
                             y[j] = fmaf(y[j], cs[j], side[j] * (m[j] * by * (r * wm) * sn[j]));
                     }

@@ -84,3 +84,35 @@ def test_heads_far_from_one(rb, io, norm, weights, D, R, sizes, eps):  # noqa: F
         c[name], c[name + "_"] = put(x, io)
         assert np.isfinite(c[name + "_"]).all()
     check_far(rb, c, eps)
+
+
+@pytest.mark.parametrize("D,R", [(64, 64), (256, 128), (33, 32)])
+@pytest.mark.parametrize("far", [3, 5000, 1 << 24])
+def test_sines_keep_their_digits(rb, D, R, far):  # noqa: F811
+    """Heads of a single one at an element of a pair have length one exactly, and are turned to the
+    sine and cosine as they are formed.  An angle's rounding to fp32 is U of it, up to pi, times the
+    other one of the two; sine and cosine are right to 2 ulps, 4 U of themselves; turns in 64 bits
+    are off by three roundings of all of them."""
+    r = np.random.default_rng(far)
+    n = 40 * R
+    pos = r.integers(-far, far + 1, n)
+    i = np.arange(n) % R                              # each element of a pair
+    x = np.zeros((n, 1, D))
+    x[np.arange(n), 0, i] = 1.0
+    q, _ = put(x)
+    y, _ = rb.qk_norm(q, q, positions=ints(pos), rotate=R, norm="l2", eps=1e-30)
+    y = y[:, 0].double().cpu().numpy()
+    pair = i % (R // 2)
+    turns = pos.astype(np.longdouble) * np.longdouble(10000.0) ** (-2.0 * pair.astype(
+        np.longdouble) / R) / (2 * np.longdouble(np.pi) + np.longdouble(2.4492935982947064e-16))
+    a = ((turns - np.rint(turns)) * (2 * np.longdouble(np.pi))).astype(np.float64)
+    sn, cs = np.sin(a), np.cos(a)
+    far_off = 2 * np.pi * 3 * 2.0 ** -52 * np.abs(turns).astype(np.float64)
+    first = i < R // 2
+    for name, at, want, other in (("cos", i, cs, sn),
+                                  ("sin", np.where(first, i + R // 2, i - R // 2),
+                                   np.where(first, sn, -sn), cs)):
+        off = np.abs(y[np.arange(n), at] - want)
+        bound = U * np.abs(a * other) + 4 * U * np.abs(want) + far_off + 1e-16
+        print(f"ERR {name}: {np.max(off / bound):.3f} of its bound, rms {np.sqrt(np.mean(off ** 2)) / U:.3f} U")
+        assert (off <= bound).all()
