@@ -1,5 +1,6 @@
 """The norms of queries and keys on the GPU where sizes and values go far: more tokens than a launch
-has workgroups for, more elements than 31 bits count.  Ordinary sizes are in test_gpu_train_ops.py.
+has workgroups for or than one of a sum takes in a turn, more elements than 31 bits count, heads and
+angles far from one.  Ordinary sizes are in test_gpu_train_ops.py.
 """
 import numpy as np
 import pytest
@@ -116,3 +117,65 @@ def test_sines_keep_their_digits(rb, D, R, far):  # noqa: F811
         bound = U * np.abs(a * other) + 4 * U * np.abs(want) + far_off + 1e-16
         print(f"ERR {name}: {np.max(off / bound):.3f} of its bound, rms {np.sqrt(np.mean(off ** 2)) / U:.3f} U")
         assert (off <= bound).all()
+
+
+# Each number of lanes to a token (0: a wave, an element at a time), by types and widths.
+LANES = [("f32", 8, 2), ("f32", 16, 4), ("f32", 32, 8), ("f32", 64, 16), ("f32", 128, 32),
+         ("f32", 256, 64), ("bf16", 16, 2), ("bf16", 32, 4), ("bf16", 64, 8), ("bf16", 128, 16),
+         ("bf16", 256, 32), ("f32", 17, 0), ("bf16", 100, 0)]
+
+
+def tokens_of_turns(lanes):
+    """(tokens that workgroups of sums take two turns for, and some of them a third with a part of
+    it, tokens to a workgroup): 1024 workgroups are the most."""
+    each = 256 // (lanes or 64)
+    return 1024 * each * 2 + 3 * each + 1, each
+
+
+@pytest.mark.parametrize("io,D,lanes", LANES)
+def test_turns_of_whole_numbers(rb, io, D, lanes):  # noqa: F811
+    """Heads of a single 1 or -1 have length one exactly, and turned by no angle stay as they are; with
+    gradients of small whole numbers all of the results are whole, and so are sums in any order:
+    y = x, dx = dy but for 0 at the one, dw the sums of x dy.  No token is lost or taken twice."""
+    import torch
+    n, _ = tokens_of_turns(lanes)
+    r = np.random.default_rng(D)
+    R = D // 2 * 2
+    how = dict(positions=ints(np.zeros(n)), rotate=R, norm="l2", eps=1e-30,
+               wq=torch.ones(D, device="cuda"), wk=torch.ones(D, device="cuda"))
+    x, dy = {}, {}
+    for name, heads in (("q", 2), ("k", 1)):
+        a = np.zeros((n * heads, D))
+        a[np.arange(n * heads), r.integers(0, D, n * heads)] = r.choice([-1.0, 1.0], n * heads)
+        x[name] = put(a.reshape(n, heads, D), io)
+        dy[name] = put(r.integers(1, 4, (n, heads, D)) * r.choice([-1.0, 1.0], (n, heads, D)), io)
+    got = rb.qk_norm_backward(x["q"][0], x["k"][0], dy["q"][0], dy["k"][0], **how)
+    for name, y in zip("qk", rb.qk_norm(x["q"][0], x["k"][0], **how)):
+        (a, a_), (g, g_) = x[name], dy[name]
+        assert torch.equal(y, a)
+        assert torch.equal(got["d" + name], g.masked_fill(a != 0, 0.0))
+        want = (a_ * g_).sum((0, 1))
+        assert np.array_equal(got["dw" + name].double().cpu().numpy(), want)
+        # one token's part alone: the last one's, whose workgroup has others' turns before it
+        g.zero_()
+        g[-1] = 2.0
+    alone = rb.qk_norm_backward(x["q"][0], x["k"][0], dy["q"][0], dy["k"][0], **how)
+    for name in "qk":
+        assert np.array_equal(alone["dw" + name].double().cpu().numpy(),
+                              2.0 * x[name][1][-1].sum(0))
+
+
+@pytest.mark.parametrize("io,D,lanes", LANES)
+def test_turns(rb, io, D, lanes):  # noqa: F811
+    """A thread adds its own tokens' heads one after another, three turns of them at most, a workgroup
+    its 256 / lanes groups (four waves), and the rest is summed in 64 bits: no more additions than
+    these lie over a term of dw, whose own error is that of u and of a turned pair, (D / 2 + 18) U."""
+    n, each = tokens_of_turns(lanes)
+    c = qk_case(io, (n,), 2, 1, D, D // 4 * 2, far=3000, seed=D)
+    how = dict(wq=c["wq"], wk=c["wk"], positions=ints(c["pos"]), rotate=c["rotate"])
+    got = rb.qk_norm_backward(c["q"], c["k"], c["dq"], c["dk"], **how)
+    for name, heads in (("q", 2), ("k", 1)):
+        o = ref.qk_norm(c[name + "_"], c["w" + name + "_"], c["pos"], c["rotate"],
+                        eps=float(np.float32(1e-6)), dy=c["d" + name + "_"])
+        chain = 3 * heads + each + 1
+        within("dw" + name, got["dw" + name], o["dw"], (chain + D / 2 + 18) * U * o["dw_size"])
