@@ -974,6 +974,7 @@ hipError_t run(const recblr_muon_tensor* tensors, int64_t count, const MuonHyper
         const hipError_t e = run_large<T>(large, work, h, st);
         large.count = 0;
         for (int& x : work) x = 0;
+        at = (char*)ws;  // the next ones' launches come behind these on the stream
         return e;
     };
     for (int64_t i = 0; i < count; ++i) {
@@ -1031,14 +1032,19 @@ hipError_t run(const recblr_muon_tensor* tensors, int64_t count, const MuonHyper
 
 }  // namespace
 
+// That of the kMaxLarge large ones, in the order of the list, that take most together.
 size_t muon_workspace(const recblr_muon_tensor* tensors, int64_t count) {
-    size_t n = 0;
+    size_t most = 0, n = 0;
+    int used = 0;
     for (int64_t i = 0; i < count; ++i) {
         if (nothing(tensors[i])) continue;
         const Shape s = shape_of(tensors[i]);
-        if (!s.small) n += large_bytes(s, tensors[i].rows * tensors[i].cols);
+        if (s.small) continue;
+        n += large_bytes(s, tensors[i].rows * tensors[i].cols);
+        most = std::max(most, n);
+        if (++used == kMaxLarge) used = 0, n = 0;
     }
-    return n;
+    return most;
 }
 
 hipError_t launch_muon(const recblr_muon_tensor* tensors, int64_t count, IoType io,
