@@ -828,7 +828,9 @@ def _adamw_moments(opt, out):
     return out
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream  # of a device, here the current one
+# The stream of a device, here the current one.  A torch built without GPUs has no such call; there
+# wrappers refuse their tensors before they come to it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _dense(t, name):
