@@ -1,8 +1,11 @@
 """Muon's workspace and the policy loss's arguments on the GPU, at the ends of what they accept.
 Ordinary sizes are in test_gpu_train_ops.py."""
+import math
+
+import numpy as np
 import pytest
 
-from test_gpu_train_ops import dtype_of, rb  # noqa: F401
+from test_gpu_train_ops import U, dtype_of, ints, rb  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +41,33 @@ def test_muon_list_in_one_workspace(rb, io):  # noqa: F811
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(p + m, want_p + want_m))
         assert bool((room[:edge] == 77).all()) and bool((room[edge + n:] == 77).all())
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(6, 100), (6, 3001), (130, 5000), (6, 30000), (6, 140000)])
+@pytest.mark.parametrize("T", [0.8, 1.1, 0.7])
+def test_policy_takes_the_temperature_as_it_is(rb, io, size, T):  # noqa: F811
+    """Two items a row, 100 apart, the rarer one chosen: logp is -100 / T but for e^-100, and the
+    ratio to an old logp near it shows the temperature's last digits, whose rounding to fp32 would move
+    it by 100 / T times up to U.  What it is off by itself: the one power of the sum and the sum, 2
+    ulps (4 U), and the loss's rounding, U of a loss of about one."""
+    import torch
+    N, V = size
+    r = np.random.default_rng(V)
+    x = torch.full(size, -math.inf, dtype=dtype_of(io), device="cuda")
+    top, ids = r.integers(0, V, N), r.integers(0, V, N)
+    ids = np.where(ids == top, (top + 1) % V, ids)
+    at = np.resize([0.0, 37.0, -28.0], N)
+    x[torch.arange(N), torch.from_numpy(top)] = torch.from_numpy(at).cuda().to(x.dtype)
+    x[torch.arange(N), torch.from_numpy(ids)] = torch.from_numpy(at - 100).cuda().to(x.dtype)
+    old = np.float32(-100.0 / T)
+    z = torch.zeros(N, device="cuda")
+    one_row = math.exp(-100.0 / T - float(old))
+    assert abs(math.exp(-100.0 / float(np.float32(T)) - float(old)) / one_row - 1) > 15 * U
+    for row in range(6):
+        one = z.clone()
+        one[row] = 1.0
+        loss, logp, _ = rb.policy_loss(x, ints(ids), z + float(old), z + 1, weight=one,
+                                       temperature=T)
+        assert abs(float(loss) + one_row) <= 5 * U * one_row, row
+        assert np.allclose(logp.double().cpu().numpy(), -100.0 / T, rtol=U, atol=4 * U)
