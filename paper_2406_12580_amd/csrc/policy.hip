@@ -683,7 +683,8 @@ hipError_t launch_policy_loss(const PolicyArgs& a, void* ws, hipStream_t st) {
     char* w = (char*)ws;
     const double K = 1.4426950408889634 / a.temperature;
     float k = (float)K;
-    if ((double)k >= K) k = std::nextafterf(k, 0.0f);  // for a positive rest
+    // For a positive rest, as a float too: of temperatures near 10^30 it may lie below the least one.
+    if ((float)(K - (double)k) <= 0.0f) k = std::nextafterf(k, 0.0f);
     const Params p{a.logits, a.ids, a.old_logp, a.advantage, a.ref_logp, a.weight, a.logp,
                    a.dlogits, (float*)(w + l.rows), a.N, a.V, k, (float)(K - (double)k),
                    a.temperature, 1.0 - a.clip_low, 1.0 + a.clip_high, a.kl};

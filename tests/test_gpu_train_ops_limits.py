@@ -71,3 +71,25 @@ def test_policy_takes_the_temperature_as_it_is(rb, io, size, T):  # noqa: F811
                                        temperature=T)
         assert abs(float(loss) + one_row) <= 5 * U * one_row, row
         assert np.allclose(logp.double().cpu().numpy(), -100.0 / T, rtol=U, atol=4 * U)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(6, 100), (6, 3001), (130, 5000), (6, 30000), (6, 140000)])
+def test_policy_masks_at_any_temperature(rb, io, size):  # noqa: F811
+    """Masked items count as nothing also where log2(e) / T lies above a float by less than the least
+    one, at temperatures that make all other items alike: log odds of -log of their number, off by
+    the sum's roundings (128 + 70 + 16 in a chain) and its own."""
+    import torch
+    N, V = size
+    x = torch.randn(size, device="cuda").to(dtype_of(io))
+    x[:, ::3] = -math.inf
+    n = V - (V + 2) // 3
+    z = torch.zeros(N, device="cuda")
+    for T in (2.5118862065898873e+29, 2.5118857130558871e+29, 1e30, 1e29):
+        k = 1.4426950408889634 / T
+        print(size, T, k - float(np.float32(k)), flush=True)
+        loss, logp, grad = rb.policy_loss(x, ints(np.full(N, 1)), z - math.log(n), z + 1,
+                                          temperature=T)
+        bar = (128 + 70 + 16 + 8 + math.log(n)) * U
+        assert np.allclose(logp.double().cpu().numpy(), -math.log(n), rtol=0, atol=bar)
+        assert abs(float(loss) + N) <= 2 * N * bar and not grad[:, ::3].any()
