@@ -998,7 +998,9 @@ def policy_loss(logits, ids, old_logp, advantage, ref_logp=None, weight=None, te
         logits.get_device(), torch.float32
     loss = torch.empty(1, dtype=f32, device=dev)
     logp = torch.empty_like(old_logp)
-    if out is None and need_grad:
+    if not need_grad:
+        out = None
+    elif out is None:
         out = torch.empty_like(logits)
     n = _policy_workspace_size(N, V, io)
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None

@@ -93,3 +93,15 @@ def test_policy_masks_at_any_temperature(rb, io, size):  # noqa: F811
         bar = (128 + 70 + 16 + 8 + math.log(n)) * U
         assert np.allclose(logp.double().cpu().numpy(), -math.log(n), rtol=0, atol=bar)
         assert abs(float(loss) + N) <= 2 * N * bar and not grad[:, ::3].any()
+
+
+def test_policy_without_a_gradient_leaves_out_alone(rb):  # noqa: F811
+    """No gradient is asked for: none is returned, and the logits given as its place stay."""
+    import torch
+    x = torch.randn(5, 40, device="cuda")
+    before, z = x.clone(), torch.zeros(5, device="cuda")
+    args = (x, ints(np.arange(5)), z - 3, z + 1)
+    loss, logp, grad = rb.policy_loss(*args, need_grad=False, out=x)
+    assert grad is None and torch.equal(x, before)
+    want = rb.policy_loss(*args, out=x)
+    assert want[2] is x and torch.equal(want[0], loss) and torch.equal(want[1], logp)
