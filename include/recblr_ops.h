@@ -168,8 +168,8 @@ int recblr_sample(const void* logits, const float* u, const float* temperature,
  * Lookup in an item table, and its gradient.
  *   table, dtable : [V][D] io;  ids : [N] int32;  out, dout : [N][D] io
  *     out_n = scale table[ids_n],   dtable_v = scale sum over the n with ids_n = v of dout_n
- * pad_id (usually 0, or -1 for none) marks padding: its rows of out are zeros, and it sends
- * no gradient.  Any other id outside [0, V) gives a row of NaN and sends no gradient.
+ * pad_id (usually 0, or -1, which no item has) marks padding: its rows of out are zeros, and it
+ * sends no gradient.  Any other id outside [0, V) gives a row of NaN and sends no gradient.
  * accumulate = 0 writes every row of dtable, those of no id as zeros; accumulate = 1 adds to
  * the rows that ids name and touches no other (a table that the prediction layer shares has
  * its gradient there already).  An item's rows are summed in fp32 in an order that hangs on

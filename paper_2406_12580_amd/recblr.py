@@ -843,10 +843,12 @@ def _dense(t, name):
 @_on_device
 def embed(table, ids, scale=1.0, pad_id=-1):
     """Rows of an item table by id: table [V,D], ids int32 of any shape.  Returns
-    scale * table[ids], [*ids.shape,D] of the table's type; rows of pad_id are zeros, those of
-    other ids outside [0, V) NaN."""
+    scale * table[ids], [*ids.shape,D] of the table's type; rows of pad_id are zeros (-1: of no
+    item), those of other ids outside [0, V) NaN."""
     if table.dim() != 2:
         raise ValueError("table must be [V, D]")
+    if not -1 << 31 <= pad_id < 1 << 31:
+        raise ValueError("pad_id must be an int32")
     V, D = table.shape
     io, at = io_code(table.dtype), table.get_device()
     out = table.new_empty((*ids.shape, D))
@@ -867,6 +869,8 @@ def embed_backward(ids, dout, V, scale=1.0, pad_id=-1, into=None):
     place, and `into` is returned."""
     if dout.dim() != ids.dim() + 1:
         raise ValueError("dout must be [*ids.shape, D]")
+    if not -1 << 31 <= pad_id < 1 << 31:
+        raise ValueError("pad_id must be an int32")
     D, N = dout.shape[-1], ids.numel()
     io, dt, at = io_code(dout.dtype), dout.dtype, ids.get_device()
     dtable = dout.new_empty((V, D)) if into is None else into

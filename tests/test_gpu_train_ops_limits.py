@@ -105,3 +105,15 @@ def test_policy_without_a_gradient_leaves_out_alone(rb):  # noqa: F811
     assert grad is None and torch.equal(x, before)
     want = rb.policy_loss(*args, out=x)
     assert want[2] is x and torch.equal(want[0], loss) and torch.equal(want[1], logp)
+
+
+@pytest.mark.parametrize("pad_id", [(1 << 32) + 2, -(1 << 31) - 1, 1 << 31])
+def test_embed_padding_beyond_its_type(rb, pad_id):  # noqa: F811
+    """An id that int32 does not have is refused, not taken for the one that its low bits are."""
+    import torch
+    t, ids = torch.randn(6, 8, device="cuda"), ints([1, 2, 3])
+    with pytest.raises(ValueError, match="pad_id"):
+        rb.embed(t, ids, pad_id=pad_id)
+    with pytest.raises(ValueError, match="pad_id"):
+        rb.embed_backward(ids, t[:3], 6, pad_id=pad_id)
+    assert torch.equal(rb.embed(t, ids, pad_id=-(1 << 31)), t[1:4])
