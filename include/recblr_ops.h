@@ -191,7 +191,7 @@ int recblr_embed_backward(const int32_t* ids, const void* dout, void* dtable, in
  *     y = R_p (w u)       w : wq or wk, [D] float, NULL for ones
  * R_p turns the pairs (i, i + rotate / 2), i < rotate / 2, by the angle p base^(-2 i / rotate)
  * (rotate even, 0 for none; elements from rotate on are not turned).  Angles are formed in 64
- * bits, whatever the position.
+ * bits, whatever the position; heads of any finite size have these results.
  *   q [N][H][D], k [N][HK][D] io, tokens q_pitch and k_pitch elements apart (parts of one
  *   projection's output, say; H D and HK D where they are dense); positions [N] int32, NULL
  *   where rotate = 0; q_out, k_out dense.

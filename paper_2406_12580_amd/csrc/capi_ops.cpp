@@ -301,8 +301,8 @@ static int embed_sizes(int64_t N, int64_t V, int64_t D, int io) {
     if (N < 0 || V < 0 || D < 1) return RECBLR_ERR_INVALID_ARGUMENT;
     if (D > 4096 || V >= ((int64_t)1 << 31) - 1 || N > ((int64_t)1 << 28))
         return RECBLR_ERR_UNSUPPORTED;
-    // The lookup has a workgroup to 512 units of a row or more, the runs' joining one of 512
-    // threads to 64 positions.
+    // The lookup has a workgroup to 512 units of a row or more, sums and joins of runs one of 1,024
+    // and 512 threads to 1,024 positions.
     if (N * D > ((int64_t)1 << 33) || V * D > ((int64_t)1 << 40)) return RECBLR_ERR_UNSUPPORTED;
     return RECBLR_OK;
 }

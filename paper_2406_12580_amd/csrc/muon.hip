@@ -20,11 +20,11 @@
 // 64 x 256): one workgroup does all of it, X in registers as fp32 beside the planes in LDS.
 // Larger ones: planes in the workspace, a launch a product over all matrices of the list.
 //
-// One MI355X, five steps: 14 matrices of up to 128 x 128 in 51 us, 40 of them the largest one's
-// products and barriers on its compute unit.  14 of up to 512 x 512 in 216, 17 launches; 200 x 200
+// One MI355X, five steps: 14 matrices of up to 128 x 128 in 44 us, 36 of them the largest one's
+// products and barriers on its compute unit.  14 of up to 512 x 512 in 218, 17 launches; 200 x 200
 // alone takes 108, 6.4 a launch with next to no work.  Two 2048 x 2048, an 8192 x 2048 and a
-// 999 x 1501 in 3,080: products at 0.83 to 0.91 PFLOP/s (8192 x 8192 of a library 1.09), 150 for
-// momentum, norm and planes, by memory at 5 TB/s.
+// 999 x 1501 in 3,050 to 3,130: products at 0.83 to 0.91 PFLOP/s (8192 x 8192 of a library 1.09),
+// 150 for momentum, norm and planes, by memory at 5 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -14,9 +14,12 @@
 // an element at a time.
 //
 // Bound by memory.  One MI355X: 204,800 tokens of 2 + 2 heads of 64 bf16, 210 MB forward, 45 us
-// (4.7 TB/s); backward with weights 58 us (5.4 TB/s) and 5 for the weights' sums.  131,072 of 4 + 2
+// (4.7 TB/s); backward with weights 57 us (5.5 TB/s) and 5 for the weights' sums.  131,072 of 4 + 2
 // heads of 128 fp32, 805 MB: both together 360 us (5.6 TB/s).  Heads read one ahead, and results written
-// past the caches, measured the same.
+// past the caches, measured the same.  The other widths' kernel, an element at a time: 204,800 tokens
+// of 2 + 2 heads of 17 fp32 160 us forward and 206 backward, bound by its instructions, of 100 bf16
+// 327 and 447 and of 72, half rotated, 194 and 427, instructions in half of the cycles; bytes would
+// take a fifth or less.
 #include <hip/hip_runtime.h>
 
 #include "device_common.hpp"
